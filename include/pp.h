@@ -54,7 +54,10 @@ typedef enum {
     PP_ERR_TIMEOUT = 7      /* a bounded device-side wait gave up (status word set by the kernel) */
 } pp_status_t;
 
-typedef enum { PP_F32 = 0, PP_F16 = 1 } pp_dtype_t;
+/* PP_F32 and PP_F16 are the element types of pruned layers; the others are inputs, outputs and weights of the decoder
+ * operators (pp_rmsnorm_q8, pp_q4_*, pp_moe_*), which say what they take.  PP_E4M3: 8-bit float, 4 exponent and 3
+ * mantissa bits, largest value 448, no infinities. */
+typedef enum { PP_F32 = 0, PP_F16 = 1, PP_BF16 = 2, PP_I8 = 3, PP_E4M3 = 4 } pp_dtype_t;
 typedef enum { PP_ACT_IDENTITY = 0, PP_ACT_RELU = 1 } pp_act_t;
 
 const char* pp_status_string(pp_status_t s);
@@ -425,6 +428,60 @@ pp_status_t pp_forward_noalloc(const pp_packed_t* p, const void* device_image,
                                const void* x, void* y, int batch, pp_act_t act,
                                void* cuda_stream);
 pp_status_t pp_noalloc_status(pp_status_t* status);
+
+/* ------------------------------------------------------------------------- *
+ * Decoder operators: what a language model's decoding step needs around fully-connected layers for one or a few
+ * tokens.  They take device memory throughout (weights too: creation rewrites them on the GPU) and never read an
+ * input before the kernels ahead of them in the stream have finished.  Inference only.
+ *
+ * Root-mean-square normalisation with the residual's addition and a result in 8 bits:
+ *     h = x + residual,  n = h * rsqrt(mean(h^2) + eps) * weight,
+ *     s = max|n| / Q over the row or over each group of columns,  code = round(n / s)   (ties to even)
+ * with Q = 127 for PP_I8 and 448 for PP_E4M3.  h and n are floats throughout; hidden_out and normed_out are rounded
+ * once.  Where max|n| is 0 scale and codes are 0.  A row with a NaN or an infinity has NaN scales; its codes are
+ * unspecified.
+ * x             [rows][cols], rows ldx elements apart, type dtype: PP_F32, PP_F16 or PP_BF16
+ * residual      the same, ldr apart; NULL = 0
+ * weight        [cols], weight_type = dtype or PP_F32
+ * code_type     PP_I8 or PP_E4M3
+ * group         0 = one scale per row, 128 = one per 128 columns (the last group of a row may be shorter)
+ * codes         [rows][cols]; scales float [rows][1 or ceil(cols / 128)]
+ * hidden_out    h in dtype, ldh apart, or NULL; may be residual or x itself (same address and distance)
+ * normed_out    n in dtype, [rows][cols], or NULL
+ * rows >= 0 (0: nothing is done, the arrays may be NULL), 1 <= cols <= 32768.  No other pair of arrays may overlap.  Any alignment of rows works; rows that all
+ * start on 16 bytes (and 8 for codes) are read and written in wider accesses.
+ * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (types, group, cols), PP_ERR_CUDA. */
+pp_status_t pp_rmsnorm_q8(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight, pp_dtype_t dtype,
+                          pp_dtype_t weight_type, int rows, int cols, float eps, pp_dtype_t code_type, int group, void* codes,
+                          float* scales, void* hidden_out, int64_t ldh, void* normed_out, void* cuda_stream);
+
+/* Layer with 4-bit weights and group scales:
+ *     y[b][m] = act( sum_n (q[m][n] - z[m][n / G]) * s[m][n / G] * x[b][n] + bias[m] ),   q, z in 0..15
+ * M, N          outputs and inputs, M <= 2^24, N <= 2^18
+ * group         G: 32, 64 or a multiple of 128 columns per scale; 0 = one scale per row
+ * codes         device, uint8 [M][ceil(N / 2)]: column 2i in the low half of byte i, 2i + 1 in the high half
+ * scales        device, [M][ceil(N / G)], scale_type PP_F16 or PP_BF16
+ * zeros         device, uint8 [M][ceil(N / G)] (the low four bits count), or NULL: every zero point is 8
+ * bias          device, float[M], or NULL
+ * cuda_stream   the stream on which codes, scales, zeros and bias are ready; creation waits for it
+ * pp_q4_forward:
+ * x             device, [batch][N], rows ldx elements apart; PP_F32, PP_F16, PP_BF16, PP_I8 or PP_E4M3
+ * x_scales      8-bit x only, else NULL: float [batch][x_group ? ceil(N / x_group) : 1], the values pp_rmsnorm_q8 writes
+ * x_group       columns per scale of x: 0 = the row, or a multiple of 128
+ * y             device, [batch][M] row-major, y_type PP_F32, PP_F16 or PP_BF16, rounded once from fp32 sums
+ * Every input type enters the products with all its bits (f32 with 24 of them).  Weights are read once for up to 32
+ * vectors (16 for PP_F32); larger batches repeat the pass.  Any alignment of x works.  A vector with an infinity or a
+ * NaN gives outputs that are not finite.  Only enqueues; calls on one handle may overlap on several streams (a handle
+ * is never written).  Results do not depend on scheduling.
+ * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED, PP_ERR_ALLOC, PP_ERR_CUDA.
+ * pp_q4_launch_info: for clusters of 1, 2, 4 and 8 CTAs, how many the device holds at once (for reports). */
+typedef struct pp_q4 pp_q4_t;
+pp_status_t pp_q4_create(pp_q4_t** out, int M, int N, int group, const void* codes, const void* scales, pp_dtype_t scale_type,
+                         const void* zeros, const float* bias, void* cuda_stream);
+pp_status_t pp_q4_destroy(pp_q4_t* layer);
+pp_status_t pp_q4_launch_info(const pp_q4_t* layer, int32_t out[4]);
+pp_status_t pp_q4_forward(pp_q4_t* layer, const void* x, int64_t ldx, pp_dtype_t x_type, const float* x_scales, int x_group, void* y,
+                          pp_dtype_t y_type, int batch, pp_act_t act, void* cuda_stream);
 
 /* Self-check of host-side bookkeeping that needs no GPU (the table that remembers, per device, which kernels
  * already have their shared-memory opt-in): PP_OK, or PP_ERR_INVALID_ARG when a check fails.  One process may

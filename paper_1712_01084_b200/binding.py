@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpp_b200.so")
 
 PP_OK = 0
-PP_F32, PP_F16 = 0, 1
+PP_F32, PP_F16, PP_BF16, PP_I8, PP_E4M3 = 0, 1, 2, 3, 4
 PP_ACT_IDENTITY, PP_ACT_RELU = 0, 1
 
 STATUS_NAMES = {0: "PP_OK", 1: "PP_ERR_INVALID_ARG", 2: "PP_ERR_BAD_PERM", 3: "PP_ERR_BAD_TILE",
@@ -90,6 +90,11 @@ def lib() -> ctypes.CDLL:
         "pp_forward_noalloc": (ci, [vp, vp, vp, vp, ci, ci, vp]),
         "pp_noalloc_status": (ci, [ctypes.POINTER(ci)]),
         "pp_selftest_host": (ci, []),
+        "pp_rmsnorm_q8": (ci, [vp, c64, vp, c64, vp, ci, ci, ci, ci, ctypes.c_float, ci, ci, vp, vp, vp, c64, vp, vp]),
+        "pp_q4_create": (ci, [ctypes.POINTER(vp), ci, ci, ci, vp, vp, ci, vp, vp, vp]),
+        "pp_q4_destroy": (ci, [vp]),
+        "pp_q4_launch_info": (ci, [vp, i32p]),
+        "pp_q4_forward": (ci, [vp, vp, c64, ci, vp, ci, vp, ci, ci, ci, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -636,3 +641,157 @@ def pp_pivot_find(abs_w, levels: int, max_sweeps: int = 32, row_init=None, col_i
                                rp.ctypes.data_as(i32p), cp.ctypes.data_as(i32p), bl.ctypes.data_as(i32p), ctypes.byref(kept)),
            "pp_pivot_find")
     return rp, cp, bl, kept.value
+
+
+# ------------------------------------------------------------ decoder operators
+_TYPES = None       # torch dtype -> pp_dtype_t
+
+
+def _type_of(dtype, name="tensor") -> int:
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: PP_F32, torch.float16: PP_F16, torch.bfloat16: PP_BF16, torch.int8: PP_I8,
+                  torch.float8_e4m3fn: PP_E4M3}
+    try:
+        return _TYPES[dtype]
+    except KeyError:
+        raise TypeError(f"{name}: {dtype} is no type of the library") from None
+
+
+def _raw_stream(device: int, stream=None) -> int:
+    """Handle of the stream to enqueue on: the given one, or the current one of a device."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
+def _rows(x, cols, name, device=None):
+    """(rows, distance of rows) of a CUDA matrix [rows][cols] whose rows are contiguous; a vector is one row."""
+    if not x.is_cuda or (device is not None and x.get_device() != device):
+        raise ValueError(f"{name} must be a CUDA tensor" + ("" if device is None else f" on device {device}"))
+    if x.dim() == 1:
+        if x.shape[0] != cols or (cols > 1 and x.stride(0) != 1):
+            raise ValueError(f"{name} must be [rows][{cols}] with contiguous rows")
+        return 1, cols
+    if x.dim() != 2 or x.shape[1] != cols or (cols > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name} must be [rows][{cols}] with contiguous rows")
+    rows = x.shape[0]
+    return rows, (x.stride(0) if rows > 1 else cols)
+
+
+def _plain(t, shape, name, device, dtypes=None):
+    """A contiguous CUDA tensor of this shape and one of these types, or ValueError / TypeError."""
+    if not t.is_cuda or t.get_device() != device or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a contiguous CUDA tensor {list(shape)} on device {device}")
+    if dtypes is not None and t.dtype not in dtypes:
+        raise TypeError(f"{name} must be one of {dtypes}")
+    return t
+
+
+def pp_rmsnorm_q8(x, weight, residual=None, eps: float = 1e-6, codes: str = "e4m3", group: int = 0, hidden_out=None,
+                  normed: bool = False, stream=None):
+    """Root-mean-square normalisation of x (+ residual) to 8 bits (pp_rmsnorm_q8).
+
+    x, residual: CUDA [rows][cols], rows contiguous, any distance apart; weight [cols] in x's type or float32; codes
+    "e4m3" or "int8"; group 0 (a scale per row) or 128 columns.  Returns (codes, scales, hidden), with the normalised
+    rows in x's type as a fourth where `normed` is set.  hidden is x + residual in x's type: a new tensor, or hidden_out
+    (which may be residual or x); without a residual it is None unless hidden_out is given."""
+    import torch
+    cols = x.shape[-1]
+    rows, ldx = _rows(x, cols, "x")
+    device, dt = x.get_device(), _type_of(x.dtype, "x")
+    _plain(weight, (cols,), "weight", device)
+    wt = _type_of(weight.dtype, "weight")
+    if codes not in ("e4m3", "int8"):
+        raise ValueError("codes must be 'e4m3' or 'int8'")
+    ldr, rp = 0, None
+    if residual is not None:
+        if residual.dtype != x.dtype or residual.shape != x.shape:
+            raise TypeError("residual must have x's shape and type")
+        ldr, rp = _rows(residual, cols, "residual", device)[1], residual.data_ptr()
+        if hidden_out is None:
+            hidden_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    ldh, hp = 0, None
+    if hidden_out is not None:
+        if hidden_out.dtype != x.dtype or hidden_out.shape != x.shape:
+            raise TypeError("hidden_out must have x's shape and type")
+        ldh, hp = _rows(hidden_out, cols, "hidden_out", device)[1], hidden_out.data_ptr()
+    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn if codes == "e4m3" else torch.int8, device=x.device)
+    scales = torch.empty(x.shape[:-1] + (-(-cols // group) if group > 0 else 1,), dtype=torch.float32, device=x.device)
+    n = torch.empty(x.shape, dtype=x.dtype, device=x.device) if normed else None
+    st = lib().pp_rmsnorm_q8(x.data_ptr(), ldx, rp, ldr, weight.data_ptr(), dt, wt, rows, cols, eps,
+                             PP_E4M3 if codes == "e4m3" else PP_I8, group, q.data_ptr(), scales.data_ptr(), hp, ldh,
+                             n.data_ptr() if normed else None, _raw_stream(device, stream))
+    _check(st, "pp_rmsnorm_q8")
+    return (q, scales, hidden_out, n) if normed else (q, scales, hidden_out)
+
+
+class Q4Layer:
+    """Layer with 4-bit weights and group scales (pp_q4_create / pp_q4_forward).
+
+    codes: CUDA uint8 [M][ceil(N/2)], column 2i in the low half of byte i; scales [M][ceil(N/group)] float16 or bfloat16;
+    zeros uint8 like scales, or None (every zero point is 8); bias float32 [M] or None.  group 0: one scale per row."""
+
+    def __init__(self, M, N, group, codes, scales, zeros=None, bias=None, stream=None):
+        import torch
+        M, N, group = int(M), int(N), int(group)
+        groups = -(-N // group) if group > 0 else 1
+        device = codes.get_device() if codes.is_cuda else -1
+        _plain(codes, (M, -(-N // 2)), "codes", device, (torch.uint8,))
+        _plain(scales, (M, groups), "scales", device, (torch.float16, torch.bfloat16))
+        if zeros is not None:
+            _plain(zeros, (M, groups), "zeros", device, (torch.uint8,))
+        if bias is not None:
+            _plain(bias, (M,), "bias", device, (torch.float32,))
+        self._h = ctypes.c_void_p()
+        with torch.cuda.device(device):
+            st = lib().pp_q4_create(ctypes.byref(self._h), M, N, group, codes.data_ptr(), scales.data_ptr(),
+                                    _type_of(scales.dtype), None if zeros is None else zeros.data_ptr(),
+                                    None if bias is None else bias.data_ptr(), _raw_stream(device, stream))
+        _check(st, "pp_q4_create")
+        self.M, self.N, self.group, self.device = M, N, group, device
+
+    def forward(self, x, act: int = PP_ACT_IDENTITY, x_scales=None, out_dtype=None, out=None, stream=None):
+        return pp_q4_forward(self, x, act, x_scales=x_scales, out_dtype=out_dtype, out=out, stream=stream)
+
+    def launch_info(self) -> dict:
+        """Clusters of 1, 2, 4 and 8 CTAs that the device holds at once (pp_q4_launch_info)."""
+        o = np.zeros(4, dtype=np.int32)
+        _check(lib().pp_q4_launch_info(self._h, o.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))), "pp_q4_launch_info")
+        return {f"clusters_of_{1 << i}": int(v) for i, v in enumerate(o)}
+
+    def close(self):
+        if self._h:
+            lib().pp_q4_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def pp_q4_forward(layer: Q4Layer, x, act: int = PP_ACT_IDENTITY, x_scales=None, out_dtype=None, out=None, stream=None):
+    """y[batch][M] = act(W x + b) with 4-bit weights.  x: [batch][N] (or [N]) float32, float16, bfloat16, or int8 /
+    float8_e4m3fn with x_scales, float32 [batch][1] or [batch][ceil(N/128)], as pp_rmsnorm_q8 returns them.  y is
+    float32 unless out_dtype (or out) says float16 or bfloat16.  Enqueues on the current stream."""
+    import torch
+    batch, ldx = _rows(x, layer.N, "x", layer.device)
+    x_group, sp = 0, None
+    if x_scales is not None:
+        n = x_scales.numel() // max(batch, 1)
+        groups = -(-layer.N // 128)
+        if n not in (1, groups) or x_scales.numel() != n * batch:
+            raise ValueError(f"x_scales must hold 1 or {groups} values per row of x")
+        _plain(x_scales, x_scales.shape, "x_scales", layer.device, (torch.float32,))
+        x_group, sp = (0 if n == 1 else 128), x_scales.data_ptr()
+    if out is None:
+        out = torch.empty((batch, layer.M), dtype=out_dtype or torch.float32, device=x.device)
+    elif (not out.is_cuda or out.get_device() != layer.device or not out.is_contiguous() or out.numel() != batch * layer.M or
+          (out_dtype is not None and out.dtype != out_dtype)):
+        raise ValueError("out must be a contiguous CUDA tensor [batch][M] of out_dtype")
+    st = lib().pp_q4_forward(layer._h, x.data_ptr(), ldx, _type_of(x.dtype, "x"), sp, x_group, out.data_ptr(),
+                             _type_of(out.dtype, "out"), batch, int(act), _raw_stream(layer.device, stream))
+    _check(st, "pp_q4_forward")
+    return out

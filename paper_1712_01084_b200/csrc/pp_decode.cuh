@@ -1,0 +1,72 @@
+// What the kernels of a decoder step share (pp_norm.cu, pp_q4.cu, pp_moe.cu): element types, packed loads and
+// stores of eight elements, and the launch with programmatic stream serialization.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "pp.h"
+
+namespace pp {
+
+inline bool is_16bit(int t) { return t == PP_F16 || t == PP_BF16; }
+inline bool is_float(int t) { return t == PP_F32 || is_16bit(t); }
+inline bool is_8bit(int t) { return t == PP_I8 || t == PP_E4M3; }
+inline int type_bytes(int t) { return t == PP_F32 ? 4 : is_16bit(t) ? 2 : 1; }
+inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Launch that lets the kernel's prologue overlap the tail of the previous kernel in the stream: the kernel itself
+// waits (griddepcontrol.wait) before it reads what that kernel may have written and before it writes anything.
+template <typename... P, typename... A>
+inline cudaError_t launch_pdl(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, int cluster, A... args) {
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
+#ifdef __CUDACC__
+__device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(int8_t v) { return (float)v; }
+__device__ __forceinline__ float to_float(__nv_fp8_e4m3 v) { return (float)v; }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+template <typename T, int N> struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Pack { T v[N]; };
+
+// N elements in one (or, for eight floats, two) vector accesses; p is aligned to their size (16 bytes at most).
+template <typename T, int N> __device__ __forceinline__ void load_vec(float (&f)[N], const T* p) {
+    const Pack<T, N> u = *reinterpret_cast<const Pack<T, N>*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = to_float(u.v[i]);
+}
+template <typename T, int N> __device__ __forceinline__ void store_vec(T* p, const float (&f)[N]) {
+    Pack<T, N> u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) u.v[i] = from_float<T>(f[i]);
+    *reinterpret_cast<Pack<T, N>*>(p) = u;
+}
+#endif
+
+}  // namespace pp
