@@ -483,6 +483,44 @@ pp_status_t pp_q4_launch_info(const pp_q4_t* layer, int32_t out[4]);
 pp_status_t pp_q4_forward(pp_q4_t* layer, const void* x, int64_t ldx, pp_dtype_t x_type, const float* x_scales, int x_group, void* y,
                           pp_dtype_t y_type, int batch, pp_act_t act, void* cuda_stream);
 
+/* Mixture-of-experts layer for a few tokens, whole: router, choice, experts, sum.  For each token
+ *     l = R x,  the top_k experts with the largest l (ties: the lowest index),
+ *     p = softmax(l) over all experts, divided by the sum of the chosen ones' where renormalize is not 0,
+ *     y = sum over the chosen e of p_e * D_e ( silu(G_e x) * (U_e x) ),   silu(v) = v / (1 + exp(-v))
+ * E, H, F       experts, width of x and y, inner width of an expert (E <= 256, H, F <= 2^16)
+ * top_k         1..16, <= E
+ * max_tokens    1..32: the workspaces are allocated for it
+ * router        device, [E][H], PP_F32, PP_F16 or PP_BF16
+ * gate_up       device, [E][2F][H]: rows 0..F-1 are G_e, F..2F-1 are U_e; wtype PP_F16 or PP_BF16
+ * down          device, [E][H][F]
+ * pp_moe_create_q4 takes both as 4-bit codes with scales and zero points (both zero-point arrays or neither), laid out
+ * per expert as in pp_q4_create: gate_up_codes [E][2F][ceil(H / 2)], gate_up_scales [E][2F][groups of H],
+ * down_codes [E][H][ceil(F / 2)], down_scales [E][H][groups of F].
+ * cuda_stream   the stream on which the arrays are ready; creation waits for it
+ * pp_moe_forward:
+ * x             device, [tokens][H], rows ldx elements apart; PP_F32, PP_F16 or PP_BF16
+ * y             device, [tokens][H] row-major; PP_F32, PP_F16 or PP_BF16
+ * ids_out       device, int32 [tokens][top_k], or NULL: the chosen experts, best first
+ * gates_out     device, float [tokens][top_k], or NULL: their p
+ * Logits, p and all sums are fp32.  x and act = p silu(G x) (U x) enter the products with 24 bits; with f16 and 4-bit
+ * experts act does so between 2^-11 and 2^27, with an absolute 2^-35 below, and overflows above.  A token with a NaN or an
+ * infinity has outputs that are not finite; other tokens are not touched by it.
+ * One cooperative kernel; results do not depend on scheduling.  Only enqueues.  Calls on one handle must be ordered on
+ * one stream.  Its two grid-wide waits are bounded (tuning key 15): when one gives up y is invalid and pp_moe_status, which
+ * synchronises with the device, reports PP_ERR_TIMEOUT and clears it.
+ * Errors: PP_ERR_INVALID_ARG (also tokens > max_tokens), PP_ERR_UNSUPPORTED, PP_ERR_ALLOC, PP_ERR_CUDA. */
+typedef struct pp_moe pp_moe_t;
+pp_status_t pp_moe_create(pp_moe_t** out, int E, int H, int F, int top_k, int renormalize, int max_tokens, const void* router,
+                          pp_dtype_t router_type, const void* gate_up, const void* down, pp_dtype_t wtype, void* cuda_stream);
+pp_status_t pp_moe_create_q4(pp_moe_t** out, int E, int H, int F, int top_k, int renormalize, int max_tokens, const void* router,
+                             pp_dtype_t router_type, int group, const void* gate_up_codes, const void* gate_up_scales,
+                             const void* gate_up_zeros, const void* down_codes, const void* down_scales, const void* down_zeros,
+                             pp_dtype_t scale_type, void* cuda_stream);
+pp_status_t pp_moe_destroy(pp_moe_t* layer);
+pp_status_t pp_moe_forward(pp_moe_t* layer, const void* x, int64_t ldx, pp_dtype_t x_type, void* y, pp_dtype_t y_type, int tokens,
+                           int32_t* ids_out, float* gates_out, void* cuda_stream);
+pp_status_t pp_moe_status(pp_moe_t* layer, pp_status_t* status);
+
 /* Self-check of host-side bookkeeping that needs no GPU (the table that remembers, per device, which kernels
  * already have their shared-memory opt-in): PP_OK, or PP_ERR_INVALID_ARG when a check fails.  One process may
  * drive several GPUs; every kernel attribute is set once per device. */

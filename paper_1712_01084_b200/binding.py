@@ -94,6 +94,11 @@ def lib() -> ctypes.CDLL:
         "pp_q4_create": (ci, [ctypes.POINTER(vp), ci, ci, ci, vp, vp, ci, vp, vp, vp]),
         "pp_q4_destroy": (ci, [vp]),
         "pp_q4_launch_info": (ci, [vp, i32p]),
+        "pp_moe_create": (ci, [ctypes.POINTER(vp), ci, ci, ci, ci, ci, ci, vp, ci, vp, vp, ci, vp]),
+        "pp_moe_create_q4": (ci, [ctypes.POINTER(vp), ci, ci, ci, ci, ci, ci, vp, ci, ci, vp, vp, vp, vp, vp, vp, ci, vp]),
+        "pp_moe_destroy": (ci, [vp]),
+        "pp_moe_status": (ci, [vp, ctypes.POINTER(ci)]),
+        "pp_moe_forward": (ci, [vp, vp, c64, ci, vp, ci, ci, vp, vp, vp]),
         "pp_q4_forward": (ci, [vp, vp, c64, ci, vp, ci, vp, ci, ci, ci, vp]),
     }
     for name, (res, args) in sig.items():
@@ -795,3 +800,104 @@ def pp_q4_forward(layer: Q4Layer, x, act: int = PP_ACT_IDENTITY, x_scales=None, 
                              _type_of(out.dtype, "out"), batch, int(act), _raw_stream(layer.device, stream))
     _check(st, "pp_q4_forward")
     return out
+
+
+class MoELayer:
+    """Mixture-of-experts layer for a few tokens (pp_moe_create / pp_moe_forward).
+
+    router: CUDA [E][H]; gate_up [E][2 inner][H] (gate rows first) and down [E][H][inner], float16 or bfloat16.
+    MoELayer.q4 takes the experts as 4-bit codes with scales (pp_moe_create_q4)."""
+
+    def __init__(self, router, gate_up, down, *, inner: int, top_k: int, max_tokens: int, renormalize: bool = True, stream=None):
+        import torch
+        E, H, device = self._router(router)
+        two = (torch.float16, torch.bfloat16)
+        _plain(gate_up, (E, 2 * inner, H), "gate_up", device, two)
+        _plain(down, (E, H, inner), "down", device, (gate_up.dtype,))
+        with torch.cuda.device(device):
+            st = lib().pp_moe_create(ctypes.byref(self._h), E, H, int(inner), int(top_k), int(bool(renormalize)), int(max_tokens),
+                                     router.data_ptr(), _type_of(router.dtype, "router"), gate_up.data_ptr(), down.data_ptr(),
+                                     _type_of(gate_up.dtype), _raw_stream(device, stream))
+        self._finish(st, "pp_moe_create", E, H, inner, top_k, max_tokens, device)
+
+    @classmethod
+    def q4(cls, router, gate_up_codes, gate_up_scales, down_codes, down_scales, gate_up_zeros=None, down_zeros=None, *, group: int,
+           inner: int, top_k: int, max_tokens: int, renormalize: bool = True, stream=None) -> "MoELayer":
+        """Experts in 4 bits: codes uint8 [E][rows][ceil(cols/2)], scales float16 or bfloat16 and zeros uint8 [E][rows][groups]."""
+        import torch
+        self = object.__new__(cls)
+        E, H, device = self._router(router)
+        group, inner = int(group), int(inner)
+        two = (torch.float16, torch.bfloat16)
+        for name, codes, scales, zeros, rows, cols in (("gate_up", gate_up_codes, gate_up_scales, gate_up_zeros, 2 * inner, H),
+                                                       ("down", down_codes, down_scales, down_zeros, H, inner)):
+            groups = -(-cols // group) if group > 0 else 1
+            _plain(codes, (E, rows, -(-cols // 2)), name + "_codes", device, (torch.uint8,))
+            _plain(scales, (E, rows, groups), name + "_scales", device, two)
+            if zeros is not None:
+                _plain(zeros, (E, rows, groups), name + "_zeros", device, (torch.uint8,))
+        if gate_up_scales.dtype != down_scales.dtype:
+            raise TypeError("gate_up_scales and down_scales must have one type")
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        with torch.cuda.device(device):
+            st = lib().pp_moe_create_q4(ctypes.byref(self._h), E, H, inner, int(top_k), int(bool(renormalize)), int(max_tokens),
+                                        router.data_ptr(), _type_of(router.dtype, "router"), group, ptr(gate_up_codes),
+                                        ptr(gate_up_scales), ptr(gate_up_zeros), ptr(down_codes), ptr(down_scales), ptr(down_zeros),
+                                        _type_of(gate_up_scales.dtype), _raw_stream(device, stream))
+        self._finish(st, "pp_moe_create_q4", E, H, inner, top_k, max_tokens, device)
+        return self
+
+    def _router(self, router):
+        self._h = ctypes.c_void_p()
+        if router.dim() != 2:
+            raise ValueError("router must be [E][H]")
+        device = router.get_device() if router.is_cuda else -1
+        _plain(router, router.shape, "router", device)
+        return router.shape[0], router.shape[1], device
+
+    def _finish(self, st, where, E, H, inner, top_k, max_tokens, device):
+        _check(st, where)
+        self.E, self.H, self.inner, self.top_k = int(E), int(H), int(inner), int(top_k)
+        self.max_tokens, self.device = int(max_tokens), device
+
+    def forward(self, x, out_dtype=None, out=None, routing: bool = False, stream=None):
+        return pp_moe_forward(self, x, out_dtype=out_dtype, out=out, routing=routing, stream=stream)
+
+    def status(self) -> int:
+        """PP_OK, or PP_ERR_TIMEOUT when a bounded device-side wait gave up (synchronises; clears the flag)."""
+        st = ctypes.c_int(0)
+        _check(lib().pp_moe_status(self._h, ctypes.byref(st)), "pp_moe_status")
+        return st.value
+
+    def close(self):
+        if self._h:
+            lib().pp_moe_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def pp_moe_forward(layer: MoELayer, x, out_dtype=None, out=None, routing: bool = False, stream=None):
+    """y[tokens][H] of a mixture-of-experts layer (pp_moe_forward).  x: [tokens][H] (or [H]) float32, float16 or bfloat16;
+    y in x's type unless out_dtype (or out) says another.  routing: also returns the chosen experts, int32 [tokens][top_k],
+    and their weights, float32.  Enqueues on the current stream."""
+    import torch
+    tokens, ldx = _rows(x, layer.H, "x", layer.device)
+    if out is None:
+        out = torch.empty((tokens, layer.H), dtype=out_dtype or x.dtype, device=x.device)
+    elif (not out.is_cuda or out.get_device() != layer.device or not out.is_contiguous() or out.numel() != tokens * layer.H or
+          (out_dtype is not None and out.dtype != out_dtype)):
+        raise ValueError("out must be a contiguous CUDA tensor [tokens][H] of out_dtype")
+    ids = gates = None
+    if routing:
+        ids = torch.empty((tokens, layer.top_k), dtype=torch.int32, device=x.device)
+        gates = torch.empty((tokens, layer.top_k), dtype=torch.float32, device=x.device)
+    st = lib().pp_moe_forward(layer._h, x.data_ptr(), ldx, _type_of(x.dtype, "x"), out.data_ptr(), _type_of(out.dtype, "out"), tokens,
+                              None if ids is None else ids.data_ptr(), None if gates is None else gates.data_ptr(),
+                              _raw_stream(layer.device, stream))
+    _check(st, "pp_moe_forward")
+    return (out, ids, gates) if routing else out

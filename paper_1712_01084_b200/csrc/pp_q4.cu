@@ -126,7 +126,9 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) q4_kernel(const Q4A
         cp_wait<kDepth - 1>();
         __syncwarp();
         const uint32_t at = ring + slot * a.unit_bytes;
-        q4_unit<NT, SETS, ASYM>(tot, at, lane, x_lane, (uint32_t)(kb * 8 * step), (uint32_t)(step * 2), cs_a + kb * NT * 32, a.bf16_scales != 0);
+        q4_unit<NT, SETS, ASYM>(tot, at, lane, a.bf16_scales != 0,
+                                [&](int nt, int j) { return lds128(x_lane[nt] + (uint32_t)((kb * 4 + j) * step * 2)); },
+                                [&](int nt) { return lds_f2(cs_a + (kb * NT + nt) * 32); });
         __syncwarp();
         fetch(at);
         if (++slot == kDepth) slot = 0;
@@ -217,7 +219,7 @@ cudaError_t opt_in(const void* kernel) {
 
 // Rows of one strip and block to a unit: a thread writes the 16 bytes one lane of q4_unit reads.
 __global__ void q4_pack_kernel(unsigned char* dst, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int rows, int cols,
-                               int group, int groups, int strips, int blocks, int sets, int unit_bytes, int64_t n_units) {
+                               int group, int groups, int strips, int blocks, int sets, int unit_bytes, int paired, int64_t n_units) {
     const int64_t stride = (int64_t)gridDim.x * blockDim.x;
     const int64_t code_ld = (cols + 1) / 2;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n_units * 64; i += stride) {
@@ -233,8 +235,8 @@ __global__ void q4_pack_kernel(unsigned char* dst, const uint8_t* codes, const u
             const int c = block * kQ4UnitCols + 32 * (2 * half + k / 2) + 8 * t + 4 * (k & 1);
             w[k] = 0u;
             for (int h = 0; h < 2; ++h) {
-                const int r = strip * 16 + g + 8 * h;
-                if (r >= rows) continue;
+                const int r = strip_row(rows, paired, strip, g, h);
+                if (r < 0) continue;
                 const uint8_t* p = codes + (row0 + r) * code_ld + c / 2;
                 for (int e = 0; e < 4; ++e) {
                     if (c + e >= cols) break;
@@ -245,9 +247,9 @@ __global__ void q4_pack_kernel(unsigned char* dst, const uint8_t* codes, const u
         }
         *reinterpret_cast<uint4*>(u + half * 512 + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
         if (part < sets * 16) {                               // entry 2 g + h of set part / 16: row g + 8 h
-            const int set = part >> 4, e = part & 15, r = strip * 16 + (e >> 1) + 8 * (e & 1);
+            const int set = part >> 4, e = part & 15, r = strip_row(rows, paired, strip, e >> 1, e & 1);
             const int col = block * kQ4UnitCols + set * (kQ4UnitCols / sets);
-            const bool in = r < rows && col < cols;
+            const bool in = r >= 0 && col < cols;
             const int64_t at = in ? (row0 + r) * groups + (group ? col / group : 0) : 0;
             reinterpret_cast<uint16_t*>(u + 1024)[part] = in ? scales[at] : (uint16_t)0;
             if (zeros) u[1024 + sets * 32 + part] = in ? (uint8_t)((zeros[at] & 15u) << (4 * (e & 1))) : (uint8_t)0;
@@ -258,14 +260,14 @@ __global__ void q4_pack_kernel(unsigned char* dst, const uint8_t* codes, const u
 }  // namespace
 
 cudaError_t launch_q4_pack(void* dst, const void* codes, const void* scales, const void* zeros, int count, int rows, int cols, int group,
-                           cudaStream_t stream) {
-    const int strips = (rows + 15) / 16, blocks = (cols + kQ4UnitCols - 1) / kQ4UnitCols, sets = q4_sets(group);
+                           bool paired, cudaStream_t stream) {
+    const int strips = strips_of(rows, paired), blocks = (cols + kQ4UnitCols - 1) / kQ4UnitCols, sets = q4_sets(group);
     const int groups = group ? (cols + group - 1) / group : 1;
     const int64_t n = (int64_t)count * strips * blocks;
     const unsigned grid = (unsigned)std::min<int64_t>((n * 64 + 255) / 256, 148 * 32);
     q4_pack_kernel<<<grid, 256, 0, stream>>>(static_cast<unsigned char*>(dst), static_cast<const uint8_t*>(codes),
                                              static_cast<const uint16_t*>(scales), static_cast<const uint8_t*>(zeros), rows, cols, group, groups,
-                                             strips, blocks, sets, q4_unit_bytes(sets, zeros != nullptr), n);
+                                             strips, blocks, sets, q4_unit_bytes(sets, zeros != nullptr), paired, n);
     return cudaGetLastError();
 }
 
@@ -293,7 +295,7 @@ extern "C" pp_status_t pp_q4_create(pp_q4_t** out, int M, int N, int group, cons
     L->N = N;
     L->group = group;
     L->sets = q4_sets(group);
-    L->strips = (M + 15) / 16;
+    L->strips = strips_of(M, false);
     L->blocks = (N + kQ4UnitCols - 1) / kQ4UnitCols;
     L->asym = zeros != nullptr;
     L->bf16_scales = scale_type == PP_BF16;
@@ -304,7 +306,7 @@ extern "C" pp_status_t pp_q4_create(pp_q4_t** out, int M, int N, int group, cons
         cudaGetLastError();
         st = PP_ERR_ALLOC;
     }
-    if (st == PP_OK && (launch_q4_pack(L->units, codes, scales, zeros, 1, M, N, group, s) != cudaSuccess ||
+    if (st == PP_OK && (launch_q4_pack(L->units, codes, scales, zeros, 1, M, N, group, false, s) != cudaSuccess ||
                         (bias && cudaMemcpyAsync(L->bias, bias, (size_t)M * 4, cudaMemcpyDeviceToDevice, s) != cudaSuccess) ||
                         cudaStreamSynchronize(s) != cudaSuccess)) st = PP_ERR_CUDA;
     for (int nt = 1; nt <= 4 && st == PP_OK; nt *= 2)

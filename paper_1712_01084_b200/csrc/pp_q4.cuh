@@ -26,9 +26,17 @@ inline __host__ __device__ int q4_unit_bytes(int sets, bool asym) { return 1024 
 inline bool q4_group_ok(int group) { return group == 0 || group == 32 || group == 64 || (group > 0 && group % 128 == 0); }
 
 // Rewrites `count` matrices (codes [count][rows][ceil(cols/2)], scales and zero points [count][rows][groups]) into units
-// at dst ([count][strips][blocks] units); zeros may be null (every zero point is 8).  In pp_q4.cu.
+// at dst ([count][strips][blocks] units); zeros may be null (every zero point is 8).  paired: the first and the second
+// half of the rows (gate and up) share strips, eight rows of each: row g of strip s is row 8s + g of the first half, row
+// 8 + g the same of the second.  In pp_q4.cu.
 cudaError_t launch_q4_pack(void* dst, const void* codes, const void* scales, const void* zeros, int count, int rows, int cols,
-                           int group, cudaStream_t stream);
+                           int group, bool paired, cudaStream_t stream);
+inline __host__ __device__ int strips_of(int rows, bool paired) { return paired ? (rows / 2 + 7) / 8 : (rows + 15) / 16; }
+// Row of a matrix that row g + 8h of a strip holds, -1 where it holds none.
+inline __host__ __device__ int strip_row(int rows, bool paired, int strip, int g, int h) {
+    const int r = paired ? strip * 8 + g : strip * 16 + g + 8 * h;
+    return r >= (paired ? rows / 2 : rows) ? -1 : paired ? r + h * (rows / 2) : r;
+}
 
 #ifdef __CUDACC__
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -82,12 +90,11 @@ __device__ __forceinline__ void q4_fetch(uint32_t slot, const unsigned char* uni
 }
 
 // tot[nt] += W_unit * X for NT tiles of 8 columns.  Lane (g, t) = (lane / 4, lane % 4) holds in tot[nt][0..3] rows g, g,
-// g + 8, g + 8 and columns 8 nt + 2t, + 1, + 0, + 1.  x_lane[nt]: shared address of the lane's input column (8 nt + g) in
-// the unit's first 32 columns, plus 16 t; x_step: bytes to the next 32 columns.  cs: shared address of the input's own
-// scales for this unit and the lane's result columns, one tile of columns every 32 bytes.
-template <int NT, int SETS, bool ASYM>
-__device__ __forceinline__ void q4_unit(float (&tot)[NT][4], uint32_t slot, int lane, const uint32_t (&x_lane)[NT], uint32_t x_off,
-                                        uint32_t x_step, uint32_t cs, bool bf16_scales) {
+// g + 8, g + 8 and columns 8 nt + 2t, + 1, + 0, + 1.  load_x(nt, j): elements 8t .. 8t + 7 of the j-th 32 columns of the
+// unit, of the lane's input column 8 nt + g.  col_scale(nt): the input's own scales for this unit and the lane's two
+// result columns.
+template <int NT, int SETS, bool ASYM, typename LoadX, typename ColScale>
+__device__ __forceinline__ void q4_unit(float (&tot)[NT][4], uint32_t slot, int lane, bool bf16_scales, LoadX load_x, ColScale col_scale) {
     const int g = lane >> 2;
     float acc[NT][4];
     uint32_t z0 = 0xE408E408u, z1 = 0xE480E480u;             // -(1024 + 8), -(1024 + 16 * 8)
@@ -118,7 +125,7 @@ __device__ __forceinline__ void q4_unit(float (&tot)[NT][4], uint32_t slot, int 
         b[3] = hadd2_bits(code_pair<0x00f000f0>(w1 >> 8), z1);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const uint4 x = lds128(x_lane[nt] + x_off + j * x_step);
+            const uint4 x = load_x(nt, j);
             mma_f16(acc[nt], a, x.x, x.y);
             mma_f16(acc[nt], b, x.z, x.w);
         }
@@ -136,7 +143,7 @@ __device__ __forceinline__ void q4_unit(float (&tot)[NT][4], uint32_t slot, int 
             s1 *= 0.0625f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float2 c = lds_f2(cs + nt * 32);
+                const float2 c = col_scale(nt);
                 tot[nt][0] = fmaf(s0 * c.x, acc[nt][0], tot[nt][0]);
                 tot[nt][1] = fmaf(s0 * c.y, acc[nt][1], tot[nt][1]);
                 tot[nt][2] = fmaf(s1 * c.x, acc[nt][2], tot[nt][2]);
