@@ -36,7 +36,7 @@ struct pp_moe {
     bool asym, bf16_scales;
     int strips1, strips2, kb1, kb2;
     int ctas[5];              // CTAs the device holds at once, for clusters of 1, 2 and 4
-    unsigned char *gate_up, *down;
+    unsigned char *gate_up, *down, *gate_up_sets, *down_sets;
     float *router, *logits, *xscale;
     uint16_t *xcols, *acols;
     int* sync;                // [0], [1] arrivals at the two barriers, [2] CTAs that are done, [3] status
@@ -50,7 +50,7 @@ constexpr int kMaxExperts = 256, kMaxTopK = 16, kMaxTokens = 32, kActCols = 3, k
 constexpr int kSpinPolls = 1 << 24;          // seconds; a barrier that is met never gets near it
 
 struct MoeArgs {
-    const unsigned char *gate_up, *down;
+    const unsigned char *gate_up, *down, *gate_up_sets, *down_sets;       // units, and their sets of 4-bit scales
     const float* router;
     XIn in;
     float *logits, *xscale;
@@ -59,7 +59,7 @@ struct MoeArgs {
     void* y;
     int32_t* ids;
     float* gates;
-    int y_type, T, E, H, top_k, renorm, strips1, strips2, kb1, kb2, kpad1, kpad2, router_ld, unit_bytes, cpt, bf16_scales, polls;
+    int y_type, T, E, H, top_k, renorm, strips1, strips2, kb1, kb2, kpad1, kpad2, router_ld, slot_bytes, cpt, bf16_scales, polls;
     int round1, round2;                      // strips of a round in steps 1 and 2
     int red_floats;                          // size of one of the two reduction buffers
     int list_off, scr_off, park_off, red_off;   // shared memory; the weight rings are at 0
@@ -67,18 +67,18 @@ struct MoeArgs {
 
 // ---- weight formats: bytes and columns of a unit, and its product with the columns a lane reads ------------------
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
 
 template <bool BF16> struct Wide {           // 16-bit weights: 16 rows x 32 columns, two operand fragments of 512 bytes
-    static constexpr int kUnitCols = 32, kExtra = 0;
-    static constexpr bool kBf16 = BF16;
+    static constexpr int kUnitCols = 32, kSetBytes = 0;
+    static constexpr bool kBf16 = BF16, kSwap = false;
     template <int NT, typename LoadX>
-    static __device__ __forceinline__ void unit(float (&tot)[NT][4], uint32_t slot, int lane, bool, LoadX load_x) {
-        const uint4 a = lds128(slot + lane * 16), b = lds128(slot + 512 + lane * 16);
+    static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool, LoadX load_x) {
+        const uint4 a = at<uint4>(slot + lane * 16), b = at<uint4>(slot + 512 + lane * 16);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const uint4 x = load_x(nt, 0);
@@ -95,11 +95,11 @@ template <bool BF16> struct Wide {           // 16-bit weights: 16 rows x 32 col
 };
 
 template <int SETS, bool ASYM> struct Q4 {
-    static constexpr int kUnitCols = kQ4UnitCols, kExtra = SETS * (ASYM ? 3 : 2);
-    static constexpr bool kBf16 = false;
+    static constexpr int kUnitCols = kQ4UnitCols, kSetBytes = SETS * (ASYM ? 48 : 32);
+    static constexpr bool kBf16 = false, kSwap = true;        // kSwap: columns 4i + 1 and 4i + 2 of the input change places
     template <int NT, typename LoadX>
-    static __device__ __forceinline__ void unit(float (&tot)[NT][4], uint32_t slot, int lane, bool bf16_scales, LoadX load_x) {
-        q4_unit<NT, SETS, ASYM>(tot, slot, lane, bf16_scales, load_x, [](int) { return make_float2(1.0f, 1.0f); });
+    static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool bf16_scales, LoadX load_x) {
+        q4_unit_f16<NT, SETS, ASYM>(tot, slot, lane, bf16_scales, load_x);
     }
 };
 
@@ -193,16 +193,33 @@ template <bool BF16> __device__ __forceinline__ void split_act(float v, uint16_t
     }
 }
 
+// Columns a token takes.
+template <bool BF16, typename T> __host__ __device__ constexpr int columns() {
+    return std::is_same_v<T, float> ? (BF16 ? 3 : 2) : BF16 && std::is_same_v<T, __half> ? 2 : 1;
+}
+
+// The power of two that brings a magnitude `most` to [2^13, 2^14), and its inverse; below 2^-113 the largest factor whose
+// inverse is a normal number, infinities stay as they are.
+__device__ __forceinline__ void token_scale(float most, float& up, float& down) {
+    uint32_t e = __float_as_uint(most) >> 23;
+    e = e >= 255u ? 140u : e < 14u ? 14u : e;
+    up = __uint_as_float((267u - e) << 23);
+    down = __uint_as_float((e - 13u) << 23);
+}
+
 // ---- step 0 ------------------------------------------------------------------------------------------------------
 // One CTA turns a token into columns.
-template <bool BF16> __device__ void token_columns(const MoeArgs& a, int token, float* part) {
-    const int64_t at = (int64_t)token * a.in.ld;
-    float up = 1.0f, down = 1.0f, v[4];
-    if (!BF16 && a.in.type != PP_F16) {
+template <class W, typename T> __device__ void token_columns(const MoeArgs& a, int token, float* part) {
+    constexpr bool BF16 = W::kBf16;
+    constexpr int cpt = columns<BF16, T>();
+    const T* x = static_cast<const T*>(a.in.x) + (int64_t)token * a.in.ld;
+    float up = 1.0f, down = 1.0f;
+    if (!BF16 && !std::is_same_v<T, __half>) {
         float most = 0.0f;
         for (int c = threadIdx.x * 4; c < a.H; c += kThreads * 4) {
-            load_four(v, a.in, at, c);
-            most = fmaxf(most, fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+            const Pack<T, 4> v = load_four(x, c, a.H, a.in.vec != 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(to_float(v.v[i])));
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
@@ -212,46 +229,58 @@ template <bool BF16> __device__ void token_columns(const MoeArgs& a, int token, 
         most = part[threadIdx.x & (kWarps - 1)];
 #pragma unroll
         for (int o = kWarps / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        block_scale(most, up, down);
+        token_scale(most, up, down);
     }
-    uint16_t* dst = a.xcols + (int64_t)token * a.cpt * a.kpad1;
+    uint16_t* dst = a.xcols + (int64_t)token * cpt * a.kpad1;
     for (int c = threadIdx.x * 4; c < a.kpad1; c += kThreads * 4) {       // zeros up to the padded length
-        load_four(v, a.in, at, c);
+        const Pack<T, 4> v = load_four(x, c, a.H, a.in.vec != 0);
+        Pack<uint16_t, 4> bits[cpt];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float rest = v[i] * up;
-            for (int k = 0; k < a.cpt; ++k) {
-                uint16_t bits;
-                rest -= round16<BF16>(rest, bits);
-                dst[(int64_t)k * a.kpad1 + c + i] = bits;
-            }
+            float rest = to_float(v.v[i]) * up;
+#pragma unroll
+            for (int k = 0; k < cpt; ++k) rest -= round16<BF16>(rest, bits[k].v[W::kSwap && (i == 1 || i == 2) ? 3 - i : i]);
         }
+#pragma unroll
+        for (int k = 0; k < cpt; ++k) *reinterpret_cast<Pack<uint16_t, 4>*>(dst + (int64_t)k * a.kpad1 + c) = bits[k];
     }
     if (threadIdx.x == 0) a.xscale[token] = down;
 }
 
 // A warp's logit of one (token, expert); what cannot be compared ranks last.
-__device__ __forceinline__ void router_logit(const MoeArgs& a, int token, int expert) {
+template <typename T> __device__ __forceinline__ void router_logit(const MoeArgs& a, int token, int expert) {
     const int lane = threadIdx.x & 31;
     const float* r = a.router + (int64_t)expert * a.router_ld;
+    const T* row = static_cast<const T*>(a.in.x) + (int64_t)token * a.in.ld;
     float sum = 0.0f;
-    for (int c0 = lane * 4; c0 < a.H; c0 += 512) {
-        float x[4][4], w[4][4];
+    for (int c0 = lane * 4; c0 < a.H; c0 += 1024) {
+        Pack<T, 4> x[8];
+        float4 w[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
             const int c = c0 + i * 128;
-            w[i][0] = w[i][1] = w[i][2] = w[i][3] = 0.0f;
-            load_four(x[i], a.in, (int64_t)token * a.in.ld, c);
-            if (c < a.H) load_vec(w[i], r + c);
+            if (c >= a.H) break;
+            x[i] = load_four(row, c, a.H, a.in.vec != 0);
+            w[i] = __ldg(reinterpret_cast<const float4*>(r + c));
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sum = fmaf(x[i][j], w[i][j], sum);
+        for (int i = 0; i < 8; ++i) {
+            if (c0 + i * 128 >= a.H) break;
+            sum = fmaf(to_float(x[i].v[0]), w[i].x, sum);
+            sum = fmaf(to_float(x[i].v[1]), w[i].y, sum);
+            sum = fmaf(to_float(x[i].v[2]), w[i].z, sum);
+            sum = fmaf(to_float(x[i].v[3]), w[i].w, sum);
+        }
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) a.logits[token * a.E + expert] = sum == sum ? sum : -INFINITY;
+}
+
+template <class W, typename T> __device__ __forceinline__ void step0(const MoeArgs& a, float* part) {
+    const int warp = threadIdx.x >> 5;
+    for (int t = blockIdx.x; t < a.T; t += gridDim.x) token_columns<W, T>(a, t, part);
+    for (int i = warp * gridDim.x + (gridDim.x - 1 - blockIdx.x); i < a.T * a.E; i += kWarps * gridDim.x) router_logit<T>(a, i / a.E, i % a.E);
 }
 
 // ---- routing, by every CTA for itself ----------------------------------------------------------------------------
@@ -349,9 +378,9 @@ __device__ int route(const MoeArgs& a, const Lists& L) {                   // th
 // blocks v0 .. v0 + nv.  In step 1 a strip belongs to one entry and its blocks are the columns of x; in step 2 a strip is
 // 16 rows of y and its blocks are the entries' columns of act, one entry after another.
 struct Span { int first, count, round, v0, nv; };
-struct Run { const unsigned char* unit; int left, ls, entry, kb; };        // units that lie one after another
+struct Run { const unsigned char *unit, *sets; int left, ls, entry, kb; };        // units that lie one after another
 
-template <int STEP> __device__ __forceinline__ void locate(const MoeArgs& a, const Lists& L, const Span& s, int round, int u, Run& r) {
+template <class W, int STEP> __device__ __forceinline__ void locate(const MoeArgs& a, const Lists& L, const Span& s, int round, int u, Run& r) {
     r.ls = u / s.nv;
     const int v = s.v0 + u - r.ls * s.nv;
     int strip = s.first + round * s.round + r.ls;
@@ -366,7 +395,8 @@ template <int STEP> __device__ __forceinline__ void locate(const MoeArgs& a, con
         r.left = min(a.kb2 - r.kb, s.v0 + s.nv - v);
     }
     const int64_t at = ((int64_t)L.entry[r.entry].x * (STEP == 1 ? a.strips1 : a.strips2) + strip) * (STEP == 1 ? a.kb1 : a.kb2) + r.kb;
-    r.unit = (STEP == 1 ? a.gate_up : a.down) + at * a.unit_bytes;
+    r.unit = (STEP == 1 ? a.gate_up : a.down) + at * 1024;
+    r.sets = (STEP == 1 ? a.gate_up_sets : a.down_sets) + at * W::kSetBytes;
 }
 
 // This warp's units of a round.
@@ -385,9 +415,10 @@ template <class W, int STEP> struct Fetcher {
             run.left = 0;
         }
         if (u < u1) {
-            if (run.left == 0) locate<STEP>(a, L, s, round, u, run);
-            q4_fetch(slot, run.unit, lane, W::kExtra);
-            run.unit += a.unit_bytes;
+            if (run.left == 0) locate<W, STEP>(a, L, s, round, u, run);
+            unit_fetch(slot, run.unit, run.sets, lane, W::kSetBytes / 16);
+            run.unit += 1024;
+            run.sets += W::kSetBytes;
             --run.left;
             ++u;
         }
@@ -401,7 +432,7 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int cpt = STEP == 1 ? a.cpt : kActCols, width = STEP == 1 ? kCap : a.T, kpad = STEP == 1 ? a.kpad1 : a.kpad2;
     const uint16_t* cols = STEP == 1 ? a.xcols : a.acols;
-    const uint32_t ring = smem_addr(smem) + (uint32_t)(warp * kDepth * a.unit_bytes);
+    unsigned char* ring = smem + warp * kDepth * a.slot_bytes;
     float* scr = reinterpret_cast<float*>(smem + a.scr_off) + warp * 16 * kCols;
     float* park = reinterpret_cast<float*>(smem + a.park_off);
     int slot = 0;
@@ -416,7 +447,7 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
         float tot[kTiles][4] = {};
         for (int u = u0; u < u1; ++u) {
             if (run.left == 0) {
-                locate<STEP>(a, L, s, round, u, run);
+                locate<W, STEP>(a, L, s, round, u, run);
                 entry = L.entry[run.entry];
                 tiles = (entry.z * cpt + 7) / 8;
 #pragma unroll
@@ -433,13 +464,13 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
             cp_wait<kDepth - 1>();
             __syncwarp();
             const auto load_x = [&](int nt, int j) { return *reinterpret_cast<const uint4*>(from[nt] + j * 32); };
-            const uint32_t at = ring + slot * a.unit_bytes;
+            unsigned char* at = ring + slot * a.slot_bytes;
             if (tiles == 1) W::template unit<1>(reinterpret_cast<float(&)[1][4]>(tot), at, lane, a.bf16_scales != 0, load_x);
             else W::template unit<kTiles>(tot, at, lane, a.bf16_scales != 0, load_x);
 #pragma unroll
             for (int nt = 0; nt < kTiles; ++nt) from[nt] += W::kUnitCols;
             __syncwarp();
-            f.next(a, L, s, rounds, warp, lane, at);
+            f.next(a, L, s, rounds, warp, lane, smem_addr(at));
             if (++slot == kDepth) slot = 0;
             if (--run.left == 0 || u + 1 == u1) {
                 // add a token's columns and park the sums: piece (warp, strip) has slot warp + strip
@@ -520,7 +551,8 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
                 gate *= scale;
                 up *= scale;
                 const float act = L.pair_gate[p] * (gate / (1.0f + expf(-gate)) * up);
-                split_act<W::kBf16>(act, a.acols + (int64_t)p * kActCols * a.kpad2 + row, a.kpad2);
+                const int at = W::kSwap && ((row & 3) == 1 || (row & 3) == 2) ? row ^ 3 : row;
+                split_act<W::kBf16>(act, a.acols + (int64_t)p * kActCols * a.kpad2 + at, a.kpad2);
             } else {
                 const int token = o / (rs * 16), m = (s.first + round * s.round) * 16 + o - token * rs * 16;
                 if (m >= a.H) continue;
@@ -543,13 +575,14 @@ template <class W> __global__ void __launch_bounds__(kThreads, 1) moe_kernel(con
     pdl_release();
     pdl_wait();
 
-    for (int t = blockIdx.x; t < a.T; t += gridDim.x) token_columns<W::kBf16>(a, t, part);
-    for (int i = warp * gridDim.x + (gridDim.x - 1 - blockIdx.x); i < a.T * a.E; i += kWarps * gridDim.x) router_logit(a, i / a.E, i % a.E);
+    if (a.in.type == PP_BF16) step0<W, __nv_bfloat16>(a, part);
+    else if (a.in.type == PP_F16) step0<W, __half>(a, part);
+    else step0<W, float>(a, part);
     if (S > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");     // the cluster's other CTAs have started
     bool ok = grid_barrier(a.sync, a.sync + 3, S, rank, a.polls, flag);
     if (ok) {
         const int entries = route(a, L);
-        const uint32_t ring = smem_addr(smem) + (uint32_t)(warp * kDepth * a.unit_bytes);
+        const uint32_t ring = smem_addr(smem) + (uint32_t)(warp * kDepth * a.slot_bytes);
         int buffer = 0;
         Span s;
         const int64_t strips = (int64_t)entries * a.strips1;
@@ -561,7 +594,7 @@ template <class W> __global__ void __launch_bounds__(kThreads, 1) moe_kernel(con
         {
             Fetcher<W, 1> f;
             const int rounds = (s.count + s.round - 1) / s.round;
-            for (int d = 0; d < kDepth; ++d) f.next(a, L, s, rounds, warp, lane, ring + d * a.unit_bytes);
+            for (int d = 0; d < kDepth; ++d) f.next(a, L, s, rounds, warp, lane, ring + d * a.slot_bytes);
             stream<W, 1>(a, L, s, f, rounds, smem, S, rank, buffer);
         }
         s.first = a.strips2 * cl / clusters;
@@ -571,7 +604,7 @@ template <class W> __global__ void __launch_bounds__(kThreads, 1) moe_kernel(con
         s.nv = entries * a.kb2 * (rank + 1) / S - s.v0;
         Fetcher<W, 2> f;
         const int rounds = (s.count + s.round - 1) / s.round;
-        for (int d = 0; d < kDepth; ++d) f.next(a, L, s, rounds, warp, lane, ring + d * a.unit_bytes);
+        for (int d = 0; d < kDepth; ++d) f.next(a, L, s, rounds, warp, lane, ring + d * a.slot_bytes);
         ok = grid_barrier(a.sync + 1, a.sync + 3, S, rank, a.polls, flag + 1);
         if (ok) stream<W, 2>(a, L, s, f, rounds, smem, S, rank, buffer);
         cp_wait<0>();
@@ -631,7 +664,7 @@ constexpr int kMaxSmem = 227 * 1024 - 256;       // beside the kernel's few stat
 
 // Strips of a round and the shared memory they take; the most strips that fit, 16 at most (one to a warp).
 size_t plan_smem(MoeArgs& a, int S) {
-    size_t at = (size_t)kWarps * kDepth * a.unit_bytes;
+    size_t at = (size_t)kWarps * kDepth * a.slot_bytes;
     a.list_off = (int)(at = (at + 127) / 128 * 128);
     at += list_bytes(a.T, a.E, a.top_k);
     a.scr_off = (int)at;
@@ -676,7 +709,8 @@ using namespace pp;
 
 extern "C" pp_status_t pp_moe_destroy(pp_moe_t* L) {
     if (!L) return PP_ERR_INVALID_ARG;
-    for (void* p : {static_cast<void*>(L->gate_up), static_cast<void*>(L->down), static_cast<void*>(L->router), static_cast<void*>(L->logits),
+    for (void* p : {static_cast<void*>(L->gate_up), static_cast<void*>(L->down), static_cast<void*>(L->gate_up_sets),
+                    static_cast<void*>(L->down_sets), static_cast<void*>(L->router), static_cast<void*>(L->logits),
                     static_cast<void*>(L->xscale), static_cast<void*>(L->xcols), static_cast<void*>(L->acols), static_cast<void*>(L->sync)})
         cudaFree(p);
     delete L;
@@ -704,7 +738,6 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
     L->sets = wtype < 0 ? q4_sets(group) : 0;
     L->asym = asym;
     const int cols = wtype < 0 ? kQ4UnitCols : 32;
-    const size_t unit = wtype < 0 ? (size_t)q4_unit_bytes(L->sets, asym) : 1024;
     L->strips1 = strips_of(2 * F, true);
     L->strips2 = strips_of(H, false);
     L->kb1 = (H + cols - 1) / cols;
@@ -712,7 +745,9 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
     const size_t pairs = (size_t)max_tokens * top_k, ld = (size_t)(H + 3) / 4 * 4;
     const size_t abytes = pairs * kActCols * L->kb2 * cols * 2;
     pp_status_t st = PP_OK;
-    if (!alloc(&L->gate_up, unit * E * L->strips1 * L->kb1) || !alloc(&L->down, unit * E * L->strips2 * L->kb2) || !alloc(&L->router, ld * E * 4) ||
+    const size_t units1 = (size_t)E * L->strips1 * L->kb1, units2 = (size_t)E * L->strips2 * L->kb2, set_bytes = wtype < 0 ? q4_set_bytes(L->sets, asym) : 0;
+    if (!alloc(&L->gate_up, units1 * 1024) || !alloc(&L->down, units2 * 1024) ||
+        (set_bytes && (!alloc(&L->gate_up_sets, units1 * set_bytes) || !alloc(&L->down_sets, units2 * set_bytes))) || !alloc(&L->router, ld * E * 4) ||
         !alloc(&L->logits, (size_t)max_tokens * E * 4) || !alloc(&L->xscale, (size_t)max_tokens * 4) ||
         !alloc(&L->xcols, (size_t)max_tokens * 3 * L->kb1 * cols * 2) || !alloc(&L->acols, abytes) || !alloc(&L->sync, 16)) {
         cudaGetLastError();
@@ -770,8 +805,8 @@ extern "C" pp_status_t pp_moe_create_q4(pp_moe_t** out, int E, int H, int F, int
     const pp_status_t st = moe_new(out, E, H, F, top_k, renormalize, max_tokens, router, router_type, -1, group, gate_up_zeros != nullptr, s);
     if (st != PP_OK) return st;
     (*out)->bf16_scales = scale_type == PP_BF16;
-    cudaError_t e = launch_q4_pack((*out)->gate_up, gate_up_codes, gate_up_scales, gate_up_zeros, E, 2 * F, H, group, true, s);
-    if (e == cudaSuccess) e = launch_q4_pack((*out)->down, down_codes, down_scales, down_zeros, E, H, F, group, false, s);
+    cudaError_t e = launch_q4_pack((*out)->gate_up, (*out)->gate_up_sets, gate_up_codes, gate_up_scales, gate_up_zeros, E, 2 * F, H, group, true, s);
+    if (e == cudaSuccess) e = launch_q4_pack((*out)->down, (*out)->down_sets, down_codes, down_scales, down_zeros, E, H, F, group, false, s);
     return moe_filled(out, e, s);
 }
 
@@ -822,7 +857,9 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     a.kpad1 = L->kb1 * cols;
     a.kpad2 = L->kb2 * cols;
     a.router_ld = (L->H + 3) / 4 * 4;
-    a.unit_bytes = q4 ? q4_unit_bytes(L->sets, L->asym) : 1024;
+    a.slot_bytes = 1024 + (q4 ? (q4_set_bytes(L->sets, L->asym) + 127) / 128 * 128 : 0);      // slots start on 128 bytes
+    a.gate_up_sets = L->gate_up_sets;
+    a.down_sets = L->down_sets;
     a.cpt = L->wtype == PP_BF16 ? (x_type == PP_BF16 ? 1 : x_type == PP_F16 ? 2 : 3) : (x_type == PP_F32 ? 2 : 1);
     a.bf16_scales = L->bf16_scales;
     a.polls = g_stream_wait_polls;

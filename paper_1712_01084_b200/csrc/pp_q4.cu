@@ -7,6 +7,16 @@
 // every warp keeps a ring of units in flight in shared memory with 16-byte asynchronous copies, requested before the
 // wait for the previous kernel (weights are never written by a kernel).  Partial sums meet in shared memory, those of
 // the other CTAs arrive there through the cluster's distributed shared memory; all are added in one fixed order.
+//
+// The products are the integer tensor-core instruction's (16 x 8 x 32, 8-bit operands, exact sums): the codes need one
+// mask instruction per four weights, where binary16 operands needed 4.5 (8192 x 8192, one vector: the multiply phase then
+// took 13,000 cycles, bound by instruction issue).  x becomes fixed point: each block of 128 columns of a vector is
+// multiplied by a power of two that brings its largest magnitude to (2^22, 0.996 * 2^23], rounded to whole numbers, and
+// written as three signed bytes, one column of the product each: an error of at most 2^-23 of the block's largest
+// element, as small as that of an fp32 sum.  Eight columns cost what one costs, so for one and two vectors the extra
+// columns are free.  8-bit integers are one column, e4m3 values times 2^9 whole numbers of three bytes; both are exact.
+//   sum (q - z) d = sum q d - z sum d  over each set of scales, in exact integers (sum d is made while x is staged and
+// the product starts from -z sum d); then one fp32 multiply-add per set with (scale of the row) * (scale of the column).
 #include "pp_q4.cuh"
 
 #include <algorithm>
@@ -15,7 +25,7 @@
 struct pp_q4 {
     int M, N, group, sets, strips, blocks;
     bool asym, bf16_scales;
-    unsigned char* units;
+    unsigned char *units, *sets_at;   // codes and sets of the units
     float* bias;
     int max_clusters[9];      // clusters of this size that the device holds at once
 };
@@ -23,17 +33,26 @@ struct pp_q4 {
 namespace pp {
 namespace {
 
-constexpr int kWarps = 16, kThreads = kWarps * 32, kDepth = 4, kMaxStrips = 16, kMaxCols = 32;
+constexpr int kWarps = 16, kThreads = kWarps * 32, kMaxStrips = 64, kMaxCols = 48;
+constexpr int kParkLd = 20;           // floats between parked columns of 16 rows: a warp's 32 values hit 32 banks
+// Units each warp keeps in flight: 4 (70 KB an SM) keep HBM busy; with 48 columns staged there is room for 3.
+__host__ __device__ constexpr int depth_of(int nt) { return nt == 6 ? 3 : nt == 1 ? 5 : 4; }
+// Columns of the product a vector takes.
+__host__ __device__ constexpr int columns_of(int xtype) { return xtype == PP_I8 ? 1 : 3; }
+// Tiles of 8 columns: one for up to 8 columns (two vectors of three bytes); else vectors of three bytes take three tiles
+// for eight of them, one tile to a byte, so that a lane holds all three sums of its results.
+int tiles_of(int tokens, int cpt) { return tokens * cpt <= 8 ? 1 : cpt == 3 ? (tokens <= 8 ? 3 : 6) : tokens <= 16 ? 2 : 6; }
 
 struct Q4Args {
-    const unsigned char* units;
+    const unsigned char *units, *sets;
     const float* bias;
     XIn in;
     void* y;
-    int64_t ldy;
-    int y_type, act, tokens, nc;          // nc: columns of the staged input = tokens * columns_per_token
-    int M, strips, blocks, unit_bytes, bf16_scales;
-    int ring_off, cs_off, park_off, red_off;      // shared memory; the staged input is at 0
+    int y_type, act, tokens, nc;          // nc: columns of the staged input
+    int M, blocks, slot_bytes, bf16_scales;
+    int strips_each, strips_more;         // a cluster has strips_each strips, the first strips_more of them one more
+    int blocks_each, blocks_more;         // the same for a CTA of a cluster and the blocks of the columns
+    int plan_off, ring_off, cs_off, sum_off, park_off, red_off;      // shared memory; the staged input is at 0
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -58,92 +77,273 @@ __device__ __forceinline__ void store_y(void* y, int64_t i, int type, float v) {
     else static_cast<__nv_bfloat16*>(y)[i] = __float2bfloat16_rn(v);
 }
 
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
+
+// Four whole numbers of a lane, |v| < 2^23, as three words of signed bytes, the highest first.  Adding 0x808080 carries
+// what a signed byte below cannot hold into the byte above; the sign bits then flip back.
+__device__ __forceinline__ void three_bytes(const int (&v)[4], uint32_t (&w)[3]) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = ((uint32_t)v[i] + 0x808080u) ^ 0x808080u;
+    const uint32_t a = prmt(u[0], u[1], 0x5140), b = prmt(u[2], u[3], 0x5140);
+    w[2] = prmt(a, b, 0x5410);
+    w[1] = prmt(a, b, 0x7632);
+    w[0] = prmt(prmt(u[0], u[1], 0x0062), prmt(u[2], u[3], 0x0062), 0x5410);
+}
+
+// A warp's block of 128 columns of one vector, four per lane: its columns' bytes and what one of them stands for (in
+// `down`, of the lowest byte).  own: an 8-bit input's scale.
+template <typename T> __device__ __forceinline__ void fixed_point(const Pack<T, 4>& x, float own, uint32_t (&w)[3], float& down) {
+    int v[4];
+    if constexpr (std::is_same_v<T, int8_t>) {
+        w[0] = *reinterpret_cast<const uint32_t*>(&x);
+        down = own;
+        return;
+    } else if constexpr (sizeof(T) == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __float2int_rn(to_float(x.v[i]) * 512.0f);
+        // NaN is the only e4m3 value that is not finite: the whole vector is not
+        const bool nan = __any_sync(0xffffffffu, to_float(x.v[0]) + to_float(x.v[1]) + to_float(x.v[2]) + to_float(x.v[3]) !=
+                                                     to_float(x.v[0]) + to_float(x.v[1]) + to_float(x.v[2]) + to_float(x.v[3]));
+        down = nan ? __int_as_float(0x7fffffff) : own * 0x1p-9f;
+    } else {
+        float f[4];
+        uint32_t most = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[i] = to_float(x.v[i]);
+            most = max(most, __float_as_uint(f[i]) & 0x7fffffffu);        // as whole numbers: a NaN is the largest
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        const uint32_t e = max(most >> 23, 23u);                           // smaller blocks keep the scale of 2^-104
+        float up = __uint_as_float((276u - min(e, 254u)) << 23);
+        down = __uint_as_float((min(e, 254u) - 22u) << 23);
+        if (__uint_as_float(most) * up > 8355000.0f) {
+            up *= 0.5f;
+            down *= 2.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __float2int_rn(f[i] * up);
+        if (most >= 0x7f800000u) down = __int_as_float(0x7fffffff);        // an infinity or a NaN: so are the sums
+    }
+    three_bytes(v, w);
+}
+
+// Position of byte c of a vector among the product's NT * 8 columns (see tiles_of).
+template <int NT> __device__ __forceinline__ int column_of(int token, int c, int cpt) {
+    return NT % 3 == 0 && cpt == 3 ? ((token >> 3) * 3 + c) * 8 + (token & 7) : token * cpt + c;
+}
+
+// This CTA's columns of x, laid out [64 columns][column of the product][lane t][8 bytes of 32 columns, 8 of the next];
+// what a column stands for per block (cs), and its sum over each set of scales (sums).  Eight blocks of four elements per
+// lane (four of f32) are requested before the first is converted: a step of this loop is a trip to memory.
+template <typename T, int NT, int SETS>
+__device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, float* cs, int* sums, int k0, int n_k, int warp, int lane) {
+    constexpr int kAhead = sizeof(T) == 4 ? 4 : 8, cpt = std::is_same_v<T, int8_t> ? 1 : 3;
+    const int items = a.tokens * n_k, step = a.nc * 64;
+    const Divider by_blocks(n_k);
+    for (int base = warp; base < items; base += kAhead * kWarps) {
+        Pack<T, 4> v[kAhead];
+        float own[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int item = base + q * kWarps, token = by_blocks.div(item), block = k0 + item - token * n_k;
+            if (item >= items) break;
+            v[q] = load_four(static_cast<const T*>(a.in.x) + token * a.in.ld, block * kQ4UnitCols + lane * 4, a.in.cols, a.in.vec != 0);
+            if (sizeof(T) == 1) own[q] = a.in.scales[(int64_t)token * a.in.scale_ld + (a.in.group_blocks ? block / a.in.group_blocks : 0)];
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int item = base + q * kWarps, token = by_blocks.div(item), kb = item - token * n_k;
+            if (item >= items) break;
+            uint32_t w[3];
+            float down;
+            fixed_point(v[q], own[q], w, down);
+            unsigned char* at = xs + (kb * 2 + (lane >> 4)) * step + token * cpt * 64 + ((lane >> 1) & 3) * 16 + (lane & 8) + (lane & 1) * 4;
+            int sum[2] = {0, 0};                             // 2^16 (highest byte) + (middle byte), and the lowest
+#pragma unroll
+            for (int c = 0; c < cpt; ++c) {
+                *reinterpret_cast<uint32_t*>(at + c * 64) = w[c];
+                sum[c == 2] += __dp4a((int)w[c], 0x01010101, 0) * (cpt == 3 && c == 0 ? 65536 : 1);
+            }
+#pragma unroll
+            for (int c = 0; c < (cpt + 1) / 2; ++c) {
+                if (SETS == 1) {
+                    sum[c] = __reduce_add_sync(0xffffffffu, sum[c]);
+                } else {
+#pragma unroll
+                    for (int o = 16 / SETS; o; o >>= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], o);
+                }
+            }
+            constexpr int kLanes = 32 / SETS;                // of a set
+            const int c = lane & (kLanes - 1);
+            if (c < cpt) {
+                const int col = column_of<NT>(token, c, cpt), middle = (int16_t)sum[0];
+                sums[(kb * SETS + lane / kLanes) * NT * 8 + col] = cpt == 1 || c == 1 ? middle : c == 0 ? (sum[0] - middle) >> 16 : sum[1];
+                if (lane < cpt) cs[kb * NT * 8 + col] = down * (cpt == 1 || c == 2 ? 1.0f : c == 1 ? 256.0f : 65536.0f);
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void mma_u8s8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm(
+        "mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// tot[nt] += W_unit * X for NT tiles of 8 columns.  Lane (g, t) holds in tot[nt][0..3] rows g, g, g + 8, g + 8 and columns
+// 8 nt + 2t, + 1, + 0, + 1.  x: the unit's first 64 columns of the input, x_lane[nt]: offset of the lane's column 8 nt + g in
+// them, x_step: bytes to the next 64.  sums, cs: the lane's two columns for the unit, eight apart from tile to tile.
+// The whole numbers come out of the product on top of 1.5 * 2^23: as floats they are themselves plus that, exactly, for
+// magnitudes up to 2^22 (16 * 15 * 128 * 128 is less).
+template <int NT, int SETS, bool ASYM>
+__device__ __forceinline__ void q4_unit_i8(float (&tot)[NT][4], const unsigned char* slot, int lane, const unsigned char* x,
+                                           const int (&x_lane)[NT], int x_step, const int* sums, const float* cs, bool bf16_scales) {
+    constexpr int kOnTop = 0x4B400000, per_set = 4 / SETS;
+    const int g = lane >> 2;
+    int acc[NT][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                            // 64 columns: two k-slices of 32
+        const uint4 w = at<uint4>(slot + h * 512 + lane * 16);
+        uint4 b[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) b[nt] = at<uint4>(x + h * x_step + x_lane[nt]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int j = 2 * h + k, set = j / per_set;
+            if (j % per_set == 0) {                          // start from -z sum d
+                int z0 = -8, z1 = -128;
+                if (ASYM) {
+                    const uint32_t zz = at<uint16_t>(slot + 1024 + SETS * 32 + set * 16 + g * 2);
+                    z0 = -(int)(zz & 255u);
+                    z1 = -(int)(zz >> 8);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int2 d = *reinterpret_cast<const int2*>(sums + (set * NT + nt) * 8);
+                    acc[nt][0] = z0 * d.x + kOnTop;
+                    acc[nt][1] = z0 * d.y + kOnTop;
+                    acc[nt][2] = z1 * d.x + kOnTop;
+                    acc[nt][3] = z1 * d.y + kOnTop;
+                }
+            }
+            const uint32_t w0 = k ? w.z : w.x, w1 = k ? w.w : w.y;
+            const uint32_t a[4] = {w0 & 0x0f0f0f0fu, w0 & 0xf0f0f0f0u, w1 & 0x0f0f0f0fu, w1 & 0xf0f0f0f0u};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_u8s8(acc[nt], a, k ? b[nt].z : b[nt].x, k ? b[nt].w : b[nt].y);
+            if (j % per_set == per_set - 1) {
+                const float2 s = q4_scales(slot, set, g, bf16_scales);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float2 c = *reinterpret_cast<const float2*>(cs + nt * 8);
+                    tot[nt][0] = fmaf(s.x * c.x, __int_as_float(acc[nt][0]) - 12582912.0f, tot[nt][0]);
+                    tot[nt][1] = fmaf(s.x * c.y, __int_as_float(acc[nt][1]) - 12582912.0f, tot[nt][1]);
+                    tot[nt][2] = fmaf(s.y * c.x, __int_as_float(acc[nt][2]) - 12582912.0f, tot[nt][2]);
+                    tot[nt][3] = fmaf(s.y * c.y, __int_as_float(acc[nt][3]) - 12582912.0f, tot[nt][3]);
+                }
+            }
+        }
+    }
+}
+
 template <int NT, int SETS, bool ASYM>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) q4_kernel(const Q4Args a) {
     extern __shared__ __align__(128) unsigned char smem[];
-    const int S = (int)cluster_size(), rank = (int)cluster_rank();
-    const int n_clusters = gridDim.x / S, cl = blockIdx.x / S;
-    const int s0 = (int)((int64_t)a.strips * cl / n_clusters), n_s = (int)((int64_t)a.strips * (cl + 1) / n_clusters) - s0;
-    const int k0 = a.blocks * rank / S, n_k = a.blocks * (rank + 1) / S - k0;
+    constexpr int kDepth = depth_of(NT);
+    const int S = (int)cluster_size(), rank = (int)cluster_rank(), cl = S == 1 ? blockIdx.x : blockIdx.x / S;
+    const int s0 = cl * a.strips_each + min(cl, a.strips_more), n_s = a.strips_each + (cl < a.strips_more);
+    const int k0 = rank * a.blocks_each + min(rank, a.blocks_more), n_k = a.blocks_each + (rank < a.blocks_more);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int U = n_s * n_k, u0 = U * warp / kWarps, u1 = U * (warp + 1) / kWarps;
     if (S > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
     pdl_release();
 
     // the first units of this warp: nothing in them depends on an earlier kernel
-    const int extra16 = SETS * (ASYM ? 3 : 2);
-    const uint32_t ring = smem_addr(smem + a.ring_off) + (uint32_t)(warp * kDepth * a.unit_bytes);
-    int fs = n_k ? u0 / n_k : 0, fk = n_k ? u0 - fs * n_k : 0, fetched = u0;
-    const unsigned char* src = a.units + ((int64_t)(s0 + fs) * a.blocks + k0 + fk) * a.unit_bytes;
-    auto fetch = [&](uint32_t slot) {
-        if (fetched < u1) {
-            q4_fetch(slot, src, lane, extra16);
-            ++fetched;
-            src += a.unit_bytes;
-            if (++fk == n_k) {
-                fk = 0;
-                src += (int64_t)(a.blocks - n_k) * a.unit_bytes;
-            }
+    unsigned char* ring = smem + a.ring_off + warp * kDepth * a.slot_bytes;
+    const int ls0 = Divider(n_k).div(u0), kb0 = u0 - ls0 * n_k;
+    constexpr int kSetBytes = SETS * (ASYM ? 48 : 32);
+    uint32_t next = (uint32_t)(s0 + ls0) * (uint32_t)a.blocks + (uint32_t)(k0 + kb0);       // unit to fetch (fewer than 2^31 of them)
+    int next_kb = kb0;
+    auto fetch = [&](unsigned char* slot, bool more) {
+        if (more) {
+            unit_fetch(smem_addr(slot), a.units + (size_t)next * kQ4CodeBytes, a.sets + (size_t)next * kSetBytes, lane, kSetBytes / 16);
+            ++next;
+            if (++next_kb == n_k) next_kb = 0, next += (uint32_t)(a.blocks - n_k);
         }
         cp_commit();
     };
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d) fetch(ring + d * a.unit_bytes);
+    for (int d = 0; d < kDepth; ++d) fetch(ring + d * a.slot_bytes, u0 + d < u1);
+    // which warps have units of each strip
+    uint16_t* plan = reinterpret_cast<uint16_t*>(smem + a.plan_off);
+    if (tid < n_s) {
+        uint32_t mask = 0u;
+        for (int w = 0; w < kWarps; ++w) {
+            const int lo = max(U * w / kWarps, tid * n_k), hi = min(U * (w + 1) / kWarps, (tid + 1) * n_k);
+            mask |= (lo < hi ? 1u : 0u) << w;
+        }
+        plan[tid] = (uint16_t)mask;
+    }
 
     pdl_wait();
-    // stage this CTA's columns of x: [32 columns][column of the tile][32 halves]
-    __half* xs = reinterpret_cast<__half*>(smem);
     float* cs = reinterpret_cast<float*>(smem + a.cs_off);
-    const int step = a.nc * 32, cpt = columns_per_token(a.in.type), items = a.tokens * n_k;
-    for (int base = warp; base < items; base += 4 * kWarps) {
-        float v[4][4];
-        int tok[4], kb[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int item = base + q * kWarps;
-            tok[q] = item / n_k;
-            kb[q] = item - tok[q] * n_k;
-            if (item < items) load_four(v[q], a.in, (int64_t)tok[q] * a.in.ld, (k0 + kb[q]) * kQ4UnitCols + lane * 4);
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (base + q * kWarps < items) {
-                const float down = stage_block(v[q], a.in, tok[q], k0 + kb[q], xs + kb[q] * 4 * step + tok[q] * cpt * 32, step);
-                if (lane < cpt) cs[kb[q] * NT * 8 + tok[q] * cpt + lane] = down;
-            }
-        }
+    int* sums = reinterpret_cast<int*>(smem + a.sum_off);
+    switch (a.in.type) {
+        case PP_F32: stage_x<float, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane); break;
+        case PP_F16: stage_x<__half, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane); break;
+        case PP_BF16: stage_x<__nv_bfloat16, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane); break;
+        case PP_I8: stage_x<int8_t, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane); break;
+        default: stage_x<__nv_fp8_e4m3, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane);
     }
     __syncthreads();
 
-    const uint32_t xs_a = smem_addr(smem), cs_a = smem_addr(cs) + t * 8;
-    uint32_t x_lane[NT];
+    const bool by_byte = NT % 3 == 0 && a.nc != a.tokens;
+    const int parked = by_byte ? a.tokens : a.nc;            // columns that are parked: a vector's bytes already added, or not
+    const int step = a.nc * 64;
+    int x_lane[NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) x_lane[nt] = xs_a + (min(nt * 8 + g, a.nc - 1) * 4 + t) * 16;
+    for (int nt = 0; nt < NT; ++nt) {                        // columns past the last repeat one
+        const int c = by_byte ? min(nt / 3 * 8 + g, a.tokens - 1) * 3 + nt % 3 : min(nt * 8 + g, a.nc - 1);
+        x_lane[nt] = (c * 4 + t) * 16;
+    }
     float* park = reinterpret_cast<float*>(smem + a.park_off);
     float tot[NT][4] = {};
-    int slot = 0, ls = n_k ? u0 / n_k : 0, kb = n_k ? u0 - ls * n_k : 0;
+    int slot = 0, ls = ls0, kb = kb0;
     for (int u = u0; u < u1; ++u) {
         cp_wait<kDepth - 1>();
         __syncwarp();
-        const uint32_t at = ring + slot * a.unit_bytes;
-        q4_unit<NT, SETS, ASYM>(tot, at, lane, a.bf16_scales != 0,
-                                [&](int nt, int j) { return lds128(x_lane[nt] + (uint32_t)((kb * 4 + j) * step * 2)); },
-                                [&](int nt) { return lds_f2(cs_a + (kb * NT + nt) * 32); });
+        unsigned char* at = ring + slot * a.slot_bytes;
+        q4_unit_i8<NT, SETS, ASYM>(tot, at, lane, smem + kb * 2 * step, x_lane, step, sums + kb * SETS * NT * 8 + t * 2, cs + kb * NT * 8 + t * 2,
+                                   a.bf16_scales != 0);
         __syncwarp();
-        fetch(at);
+        fetch(at, u + kDepth < u1);
         if (++slot == kDepth) slot = 0;
         if (++kb == n_k || u + 1 == u1) {
             // piece (warp, strip) parks in slot warp + strip: along the units one of the two grows at every change
-            float* p = park + (warp + ls) * 16 * a.nc + g * a.nc;
+            float* p = park + (warp + ls) * kParkLd * parked + g;
+            if (by_byte) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+                for (int nt = 0; nt + 2 < NT; nt += 3) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int c = nt * 8 + 2 * t + (i & 1);
-                    if (c < a.nc) p[(i >> 1) * 8 * a.nc + c] = tot[nt][i];
-                    tot[nt][i] = 0.0f;
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = nt / 3 * 8 + 2 * t + (i & 1);
+                        if (c < parked) p[c * kParkLd + (i >> 1) * 8] = tot[nt][i] + (tot[nt + 1][i] + tot[nt + 2][i]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = nt * 8 + 2 * t + (i & 1);
+                        if (c < parked) p[c * kParkLd + (i >> 1) * 8] = tot[nt][i];
+                    }
                 }
             }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) tot[nt][0] = tot[nt][1] = tot[nt][2] = tot[nt][3] = 0.0f;
             kb = 0;
             ++ls;
         }
@@ -152,37 +352,43 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) q4_kernel(const Q4A
     __syncthreads();
 
     // add the warps' pieces of every row in warp order; each CTA of the cluster finishes an equal part of the results
-    const int rows = n_s * 16, outs = rows * a.tokens, share = (outs + S - 1) / S;
+    const int rows = n_s * 16, outs = rows * a.tokens, share = S == 1 ? outs : (outs + S - 1) / S;
+    const int first = rank * share, last = min(outs, first + share);
+    const int cpt = parked == a.tokens ? 1 : 3;              // parked columns of a vector
+    const Divider by_rows(rows), by_share(share);
     float* red = reinterpret_cast<float*>(smem + a.red_off);
+    float bias = 0.0f;                                       // of this thread's first result: on its way during the barrier
+    if (a.bias && first + tid < last) {
+        const int m = s0 * 16 + (first + tid - by_rows.div(first + tid) * rows);
+        if (m < a.M) bias = __ldg(a.bias + m);
+    }
     if (S > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");      // every CTA of the cluster has started
     for (int o = tid; o < outs; o += kThreads) {
-        const int token = o / rows, r = o - token * rows, strip = r >> 4;
+        const int token = by_rows.div(o), r = o - token * rows, strip = r >> 4;
         float v = 0.0f;
-        if (n_k) {
-            const int w_lo = (int)(((int64_t)kWarps * (strip * n_k + 1) - 1) / U), w_hi = (int)(((int64_t)kWarps * (strip * n_k + n_k) - 1) / U);
-            for (int w = w_lo; w <= w_hi; ++w) {
-                if (U * w / kWarps == U * (w + 1) / kWarps) continue;
-                const float* p = park + ((w + strip) * 16 + (r & 15)) * a.nc + token * cpt;
-                v += cpt == 2 ? p[0] + p[1] : p[0];
-            }
+        for (uint32_t m = plan[strip]; m; m &= m - 1) {
+            const float* p = park + (__ffs((int)m) - 1 + strip) * kParkLd * parked + token * cpt * kParkLd + (r & 15);
+            v += cpt == 1 ? p[0] : p[0] + (p[kParkLd] + p[2 * kParkLd]);
         }
-        const int owner = o / share;
-        if (S > 1) st_cluster(smem_addr(red + rank * share + (o - owner * share)), (uint32_t)owner, v);
-        else red[o] = v;
+        if (S > 1) {
+            const int owner = by_share.div(o);
+            st_cluster(smem_addr(red + rank * share + o - owner * share), (uint32_t)owner, v);
+        } else {
+            red[o] = v;
+        }
     }
     if (S > 1) {
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
-    const int first = rank * share, last = min(outs, first + share);
     for (int o = first + tid; o < last; o += kThreads) {
-        const int token = o / rows, m = s0 * 16 + o - token * rows;
+        const int token = by_rows.div(o), m = s0 * 16 + o - token * rows;
         if (m >= a.M) continue;
         float v = 0.0f;
         for (int q = 0; q < S; ++q) v += red[q * share + o - first];
-        if (a.bias) v += a.bias[m];
+        if (a.bias) v += o == first + tid ? bias : __ldg(a.bias + m);
         if (a.act == PP_ACT_RELU) v = v > 0.0f || v != v ? v : 0.0f;
-        store_y(a.y, (int64_t)token * a.ldy + m, a.y_type, v);
+        store_y(a.y, (int64_t)token * a.M + m, a.y_type, v);
     }
 }
 
@@ -192,21 +398,25 @@ template <int NT> Kernel pick_sets(int sets, bool asym) {
     return sets == 4 ? pick_asym<NT, 4>(asym) : sets == 2 ? pick_asym<NT, 2>(asym) : pick_asym<NT, 1>(asym);
 }
 Kernel pick_kernel(int nt, int sets, bool asym) {
-    return nt == 1 ? pick_sets<1>(sets, asym) : nt == 2 ? pick_sets<2>(sets, asym) : pick_sets<4>(sets, asym);
+    return nt == 1 ? pick_sets<1>(sets, asym) : nt == 2 ? pick_sets<2>(sets, asym) : nt == 3 ? pick_sets<3>(sets, asym) : pick_sets<6>(sets, asym);
 }
 
 constexpr int kMaxSmem = 227 * 1024;
 
 // Shared memory of a launch with clusters of S CTAs that own up to n_s strips each; fills in the offsets.
-size_t plan_smem(Q4Args& a, int S, int n_s) {
-    const int nt = a.nc <= 8 ? 1 : a.nc <= 16 ? 2 : 4, n_k = (a.blocks + S - 1) / S;
-    size_t at = (size_t)n_k * kQ4UnitCols * a.nc * 2;
+size_t plan_smem(Q4Args& a, int sets, int S, int n_s) {
+    const int nt = tiles_of(a.tokens, a.nc / a.tokens), n_k = (a.blocks + S - 1) / S;
+    size_t at = (size_t)n_k * kQ4UnitCols * a.nc;
     a.cs_off = (int)at;
     at += (size_t)n_k * nt * 32;
+    a.sum_off = (int)at;
+    at += (size_t)n_k * sets * nt * 32;
+    a.plan_off = (int)at;
+    at += (size_t)n_s * 2;
     a.ring_off = (int)(at = (at + 127) / 128 * 128);
-    at += (size_t)kWarps * kDepth * a.unit_bytes;
+    at += (size_t)kWarps * depth_of(nt) * a.slot_bytes;
     a.park_off = (int)at;
-    at += (size_t)(n_s + kWarps) * 16 * a.nc * 4;
+    at += (size_t)(n_s + kWarps) * kParkLd * (nt % 3 == 0 ? a.tokens : a.nc) * 4;
     a.red_off = (int)at;
     const size_t outs = (size_t)n_s * 16 * a.tokens;
     at += (outs + S - 1) / S * S * 4;
@@ -217,9 +427,9 @@ cudaError_t opt_in(const void* kernel) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
 }
 
-// Rows of one strip and block to a unit: a thread writes the 16 bytes one lane of q4_unit reads.
-__global__ void q4_pack_kernel(unsigned char* dst, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int rows, int cols,
-                               int group, int groups, int strips, int blocks, int sets, int unit_bytes, int paired, int64_t n_units) {
+// Rows of one strip and block to a unit: a thread writes the 16 bytes one lane of a product reads.
+__global__ void q4_pack_kernel(unsigned char* dst, unsigned char* dst_sets, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int rows, int cols,
+                               int group, int groups, int strips, int blocks, int sets, int set_bytes, int paired, int64_t n_units) {
     const int64_t stride = (int64_t)gridDim.x * blockDim.x;
     const int64_t code_ld = (cols + 1) / 2;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n_units * 64; i += stride) {
@@ -229,10 +439,9 @@ __global__ void q4_pack_kernel(unsigned char* dst, const uint8_t* codes, const u
         const int64_t ms = unit / blocks;                     // matrix * strips + strip
         const int strip = (int)(ms % strips);
         const int64_t row0 = ms / strips * rows;              // first row of the matrix among all rows
-        unsigned char* u = dst + unit * unit_bytes;
         uint32_t w[4];
         for (int k = 0; k < 4; ++k) {
-            const int c = block * kQ4UnitCols + 32 * (2 * half + k / 2) + 8 * t + 4 * (k & 1);
+            const int c = block * kQ4UnitCols + 32 * (2 * half + k / 2) + 8 * t + 4 * (k & 1);      // the word's four columns
             w[k] = 0u;
             for (int h = 0; h < 2; ++h) {
                 const int r = strip_row(rows, paired, strip, g, h);
@@ -241,33 +450,34 @@ __global__ void q4_pack_kernel(unsigned char* dst, const uint8_t* codes, const u
                 for (int e = 0; e < 4; ++e) {
                     if (c + e >= cols) break;
                     const uint32_t q = (p[e / 2] >> (4 * (e & 1))) & 15u;
-                    w[k] |= q << (4 * h + 8 * (e / 2) + 16 * (e & 1));
+                    w[k] |= q << (8 * e + 4 * h);
                 }
             }
         }
-        *reinterpret_cast<uint4*>(u + half * 512 + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(dst + unit * kQ4CodeBytes + half * 512 + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
         if (part < sets * 16) {                               // entry 2 g + h of set part / 16: row g + 8 h
             const int set = part >> 4, e = part & 15, r = strip_row(rows, paired, strip, e >> 1, e & 1);
             const int col = block * kQ4UnitCols + set * (kQ4UnitCols / sets);
             const bool in = r >= 0 && col < cols;
             const int64_t at = in ? (row0 + r) * groups + (group ? col / group : 0) : 0;
-            reinterpret_cast<uint16_t*>(u + 1024)[part] = in ? scales[at] : (uint16_t)0;
-            if (zeros) u[1024 + sets * 32 + part] = in ? (uint8_t)((zeros[at] & 15u) << (4 * (e & 1))) : (uint8_t)0;
+            unsigned char* u = dst_sets + unit * set_bytes;
+            reinterpret_cast<uint16_t*>(u)[part] = in ? scales[at] : (uint16_t)0;
+            if (zeros) u[sets * 32 + part] = in ? (uint8_t)((zeros[at] & 15u) << (4 * (e & 1))) : (uint8_t)0;
         }
     }
 }
 
 }  // namespace
 
-cudaError_t launch_q4_pack(void* dst, const void* codes, const void* scales, const void* zeros, int count, int rows, int cols, int group,
+cudaError_t launch_q4_pack(void* dst, void* dst_sets, const void* codes, const void* scales, const void* zeros, int count, int rows, int cols, int group,
                            bool paired, cudaStream_t stream) {
     const int strips = strips_of(rows, paired), blocks = (cols + kQ4UnitCols - 1) / kQ4UnitCols, sets = q4_sets(group);
     const int groups = group ? (cols + group - 1) / group : 1;
     const int64_t n = (int64_t)count * strips * blocks;
     const unsigned grid = (unsigned)std::min<int64_t>((n * 64 + 255) / 256, 148 * 32);
-    q4_pack_kernel<<<grid, 256, 0, stream>>>(static_cast<unsigned char*>(dst), static_cast<const uint8_t*>(codes),
+    q4_pack_kernel<<<grid, 256, 0, stream>>>(static_cast<unsigned char*>(dst), static_cast<unsigned char*>(dst_sets), static_cast<const uint8_t*>(codes),
                                              static_cast<const uint16_t*>(scales), static_cast<const uint8_t*>(zeros), rows, cols, group, groups,
-                                             strips, blocks, sets, q4_unit_bytes(sets, zeros != nullptr), paired, n);
+                                             strips, blocks, sets, q4_set_bytes(sets, zeros != nullptr), paired, n);
     return cudaGetLastError();
 }
 
@@ -278,6 +488,7 @@ using namespace pp;
 extern "C" pp_status_t pp_q4_destroy(pp_q4_t* L) {
     if (!L) return PP_ERR_INVALID_ARG;
     cudaFree(L->units);
+    cudaFree(L->sets_at);
     cudaFree(L->bias);
     delete L;
     return PP_OK;
@@ -299,18 +510,19 @@ extern "C" pp_status_t pp_q4_create(pp_q4_t** out, int M, int N, int group, cons
     L->blocks = (N + kQ4UnitCols - 1) / kQ4UnitCols;
     L->asym = zeros != nullptr;
     L->bf16_scales = scale_type == PP_BF16;
-    const size_t bytes = (size_t)L->strips * L->blocks * q4_unit_bytes(L->sets, L->asym);
+    const size_t units = (size_t)L->strips * L->blocks;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     pp_status_t st = PP_OK;
-    if ((cudaMalloc(&L->units, bytes) != cudaSuccess || (bias && cudaMalloc(&L->bias, (size_t)M * 4) != cudaSuccess))) {
+    if ((cudaMalloc(&L->units, units * kQ4CodeBytes) != cudaSuccess ||
+         cudaMalloc(&L->sets_at, units * q4_set_bytes(L->sets, L->asym)) != cudaSuccess || (bias && cudaMalloc(&L->bias, (size_t)M * 4) != cudaSuccess))) {
         cudaGetLastError();
         st = PP_ERR_ALLOC;
     }
-    if (st == PP_OK && (launch_q4_pack(L->units, codes, scales, zeros, 1, M, N, group, false, s) != cudaSuccess ||
+    if (st == PP_OK && (launch_q4_pack(L->units, L->sets_at, codes, scales, zeros, 1, M, N, group, false, s) != cudaSuccess ||
                         (bias && cudaMemcpyAsync(L->bias, bias, (size_t)M * 4, cudaMemcpyDeviceToDevice, s) != cudaSuccess) ||
                         cudaStreamSynchronize(s) != cudaSuccess)) st = PP_ERR_CUDA;
-    for (int nt = 1; nt <= 4 && st == PP_OK; nt *= 2)
-        if (opt_in(reinterpret_cast<const void*>(pick_kernel(nt, L->sets, L->asym))) != cudaSuccess) st = PP_ERR_CUDA;
+    for (int nt : {1, 2, 3, 6})
+        if (st == PP_OK && opt_in(reinterpret_cast<const void*>(pick_kernel(nt, L->sets, L->asym))) != cudaSuccess) st = PP_ERR_CUDA;
     // clusters resident at once, for a CTA of ordinary size (the GPCs hold different numbers of SMs)
     for (int S = 1; S <= 8 && st == PP_OK; S *= 2) {
         cudaLaunchAttribute at;
@@ -359,39 +571,49 @@ extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_
     a.in.group_blocks = x_group / kQ4UnitCols;
     a.in.cols = L->N;
     a.in.vec = aligned_to(x, 4 * xb) && (batch == 1 || ldx % 4 == 0);
-    a.ldy = L->M;
     a.y_type = y_type;
     a.act = act;
     a.M = L->M;
-    a.strips = L->strips;
     a.blocks = L->blocks;
-    a.unit_bytes = q4_unit_bytes(L->sets, L->asym);
+    a.sets = L->sets_at;
+    a.slot_bytes = kQ4CodeBytes + (q4_set_bytes(L->sets, L->asym) + 127) / 128 * 128;      // slots start on 128 bytes
     a.bf16_scales = L->bf16_scales;
-    const int cpt = columns_per_token(x_type);
-    int most = kMaxCols / cpt;                       // tokens of one launch
+    const int cpt = columns_of(x_type);
+    int most = std::min(kMaxCols / cpt, 32);                       // tokens of one launch
     for (int b0 = 0; b0 < batch;) {
         a.tokens = std::min(batch - b0, most);
         a.nc = a.tokens * cpt;
         a.in.x = static_cast<const char*>(x) + (int64_t)b0 * ldx * xb;
         a.in.scales = x_scales ? x_scales + (int64_t)b0 * a.in.scale_ld : nullptr;
         a.y = static_cast<char*>(y) + (int64_t)b0 * L->M * yb;
-        // cluster size: the one whose busiest CTA has the fewest units
+        // cluster size and strips to a cluster: the fewest units on the busiest SM, counting what staging a block of a
+        // token's columns costs as half a unit.  More strips than one round of clusters can hold go in several rounds.
         int best = 0, best_n = 0;
         int64_t best_cost = 0;
-        for (int S = 1; S <= 8; S *= 2) {
-            const int n = std::max(std::min(L->strips, L->max_clusters[S]), (L->strips + kMaxStrips - 1) / kMaxStrips);
-            const int n_s = (L->strips + n - 1) / n, n_k = (L->blocks + S - 1) / S;
-            if (S > L->blocks || plan_smem(a, S, n_s) > (size_t)kMaxSmem) continue;
-            const int64_t cost = (int64_t)n_s * n_k;
-            if (!best || cost < best_cost) best = S, best_n = n, best_cost = cost;
+        for (int S = 1; S <= 8 && S <= L->blocks; S *= 2) {
+            const int n_k = (L->blocks + S - 1) / S;
+            for (int rounds = 1; rounds <= L->strips; ++rounds) {
+                const int n = std::min(L->strips, L->max_clusters[S] * rounds), n_s = (L->strips + n - 1) / n;
+                if (n_s > kMaxStrips || plan_smem(a, L->sets, S, n_s) > (size_t)kMaxSmem) {
+                    if (n_s == 1) break;
+                    continue;
+                }
+                const int64_t cost = rounds * (2ll * n_s + a.tokens) * n_k;
+                if (!best || cost < best_cost) best = S, best_n = n, best_cost = cost;
+                break;
+            }
         }
         if (!best) {                                 // x does not fit: fewer tokens at a time
             if (a.tokens == 1) return PP_ERR_UNSUPPORTED;
             most = a.tokens / 2;
             continue;
         }
-        const size_t smem = plan_smem(a, best, (L->strips + best_n - 1) / best_n);
-        const Kernel k = pick_kernel(a.nc <= 8 ? 1 : a.nc <= 16 ? 2 : 4, L->sets, L->asym);
+        const size_t smem = plan_smem(a, L->sets, best, (L->strips + best_n - 1) / best_n);
+        a.strips_each = L->strips / best_n;
+        a.strips_more = L->strips % best_n;
+        a.blocks_each = L->blocks / best;
+        a.blocks_more = L->blocks % best;
+        const Kernel k = pick_kernel(tiles_of(a.tokens, cpt), L->sets, L->asym);
         if (launch_pdl(k, dim3(best * best_n), dim3(kThreads), smem, static_cast<cudaStream_t>(cuda_stream), best, a) != cudaSuccess)
             return PP_ERR_CUDA;
         b0 += a.tokens;
