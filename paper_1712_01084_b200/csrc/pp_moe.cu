@@ -7,14 +7,16 @@
 // on those weights, and for one token by the three steps that wait for one another:
 //   step 0  the first CTAs turn the tokens into columns of the products' type, every warp of the grid takes (token,
 //           expert) pairs of the router;                                                     -- grid barrier --
-//   step 1  every CTA ranks the logits for itself (rank = how many are better: no sorting, no second barrier), lists the
-//           experts that some token chose, and the grid streams their gate and up rows; eight rows of each share a
-//           strip, so the CTA that finishes a strip has both halves of act = p silu(g) u;    -- grid barrier --
-//   step 2  the grid streams the down rows; a strip of 16 rows of y collects all experts, so nothing is summed across
-//           clusters.  The first of these weights are requested before the barrier.
-// A cluster of S CTAs shares a run of strips and splits their columns; its partial sums meet in distributed shared
-// memory.  Inside a CTA the units of a round of strips are dealt to the 16 warps in equal runs, each with a ring of
-// asynchronous copies in flight.  All sums are taken in one fixed order.
+//   step 1  every CTA chooses the experts for itself (a warp per token; no second barrier) and lists those that some token
+//           chose; the grid streams their gate and up rows, eight rows of each to a strip, so
+//           whoever finishes a strip has both halves of act = p silu(g) u;                   -- grid barrier --
+//   step 2  the grid streams the down rows; a strip of 16 rows of y collects all experts.  The first of these weights are
+//           requested before the barrier.
+// In steps 1 and 2 all units (1 KB of weights) form one sequence that is cut into equal parts, one per CTA, wherever that
+// falls; inside a CTA a round of strips is dealt to the 16 warps in equal runs, each with a ring of asynchronous copies in
+// flight.  Warps' sums of a strip meet in shared memory; a strip that a cut divides is finished by the last of its CTAs to
+// arrive, which adds the parts in the order of the CTAs.  So all sums are taken in one fixed order.
+// (Cutting at strips instead left 256 strips of 16 rows to 148 CTAs: 1.73 on average, 2 on the busiest.)
 //
 // Columns.  Products take one 16-bit type, the weights' (binary16 for 4-bit codes).  An input that has more bits than
 // one column holds is split over several: bf16 products take f16 in two and f32 in three columns; binary16 products take
@@ -35,11 +37,13 @@ struct pp_moe {
     int E, H, F, top_k, renorm, max_tokens, wtype, sets;      // wtype: PP_F16, PP_BF16 or -1 for 4-bit codes
     bool asym, bf16_scales;
     int strips1, strips2, kb1, kb2;
-    int ctas[5];              // CTAs the device holds at once, for clusters of 1, 2 and 4
+    int ctas;                 // that the device holds at once
     unsigned char *gate_up, *down, *gate_up_sets, *down_sets;
     float *router, *logits, *xscale;
     uint16_t *xcols, *acols;
-    int* sync;                // [0], [1] arrivals at the two barriers, [2] CTAs that are done, [3] status
+    float* parts;             // [CTA][2][16][width]: its parts of the strips that its first and last cut divide
+    int* sync;                // [0], [1] arrivals at the two barriers, [2] CTAs that are done, [3] status, then arrivals at
+                              // divided strips, [step][the first of the strip's CTAs]
 };
 
 namespace pp {
@@ -53,16 +57,16 @@ struct MoeArgs {
     const unsigned char *gate_up, *down, *gate_up_sets, *down_sets;       // units, and their sets of 4-bit scales
     const float* router;
     XIn in;
-    float *logits, *xscale;
+    float *logits, *xscale, *parts;
     uint16_t *xcols, *acols;
     int* sync;
     void* y;
     int32_t* ids;
     float* gates;
     int y_type, T, E, H, top_k, renorm, strips1, strips2, kb1, kb2, kpad1, kpad2, router_ld, slot_bytes, cpt, bf16_scales, polls;
-    int round1, round2;                      // strips of a round in steps 1 and 2
-    int red_floats;                          // size of one of the two reduction buffers
-    int list_off, scr_off, park_off, red_off;   // shared memory; the weight rings are at 0
+    float per_expert, per_entry;             // 1 / strips1, 1 / kb2
+    int round;                               // strips of a round
+    int list_off, scr_off, park_off;         // shared memory; the weight rings are at 0
 };
 
 // ---- weight formats: bytes and columns of a unit, and its product with the columns a lane reads ------------------
@@ -74,89 +78,54 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint4& a, uint32_t
 }
 
 template <bool BF16> struct Wide {           // 16-bit weights: 16 rows x 32 columns, two operand fragments of 512 bytes
-    static constexpr int kUnitCols = 32, kSetBytes = 0;
+    static constexpr int kUnitCols = 32, kSetBytes = 0, kLoads = 1;       // kLoads: 16-byte reads of a lane and column
     static constexpr bool kBf16 = BF16, kSwap = false;
-    template <int NT, typename LoadX>
-    static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool, LoadX load_x) {
+    template <int NT>
+    static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool, const uint4 (*x)[kLoads]) {
         const uint4 a = at<uint4>(slot + lane * 16), b = at<uint4>(slot + 512 + lane * 16);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const uint4 x = load_x(nt, 0);
             if (BF16) {
-                mma_bf16(tot[nt], a, x.x, x.y);
-                mma_bf16(tot[nt], b, x.z, x.w);
+                mma_bf16(tot[nt], a, x[nt][0].x, x[nt][0].y);
+                mma_bf16(tot[nt], b, x[nt][0].z, x[nt][0].w);
             } else {
                 const uint32_t ar[4] = {a.x, a.y, a.z, a.w}, br[4] = {b.x, b.y, b.z, b.w};
-                mma_f16(tot[nt], ar, x.x, x.y);
-                mma_f16(tot[nt], br, x.z, x.w);
+                mma_f16(tot[nt], ar, x[nt][0].x, x[nt][0].y);
+                mma_f16(tot[nt], br, x[nt][0].z, x[nt][0].w);
             }
         }
     }
 };
 
 template <int SETS, bool ASYM> struct Q4 {
-    static constexpr int kUnitCols = kQ4UnitCols, kSetBytes = SETS * (ASYM ? 48 : 32);
+    static constexpr int kUnitCols = kQ4UnitCols, kSetBytes = SETS * (ASYM ? 48 : 32), kLoads = 4;
     static constexpr bool kBf16 = false, kSwap = true;        // kSwap: columns 4i + 1 and 4i + 2 of the input change places
-    template <int NT, typename LoadX>
-    static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool bf16_scales, LoadX load_x) {
-        q4_unit_f16<NT, SETS, ASYM>(tot, slot, lane, bf16_scales, load_x);
+    template <int NT>
+    static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool bf16_scales, const uint4 (*x)[kLoads]) {
+        q4_unit_f16<NT, SETS, ASYM>(tot, slot, lane, bf16_scales, [&](int nt, int j) { return x[nt][j]; });
     }
 };
 
 // ---- small helpers -----------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t at_rank(uint32_t local, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void st_cluster(uint32_t local, uint32_t rank, float v) {
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at_rank(local, rank)), "f"(v) : "memory");
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-}
-// All CTAs of the cluster, or of the block where it has none.
-__device__ __forceinline__ void group_sync(int S) {
-    if (S > 1) cluster_sync();
-    else __syncthreads();
-}
-
-// Every CTA of the grid has arrived and what it wrote before is visible; false (in every CTA of the cluster alike) if the
-// wait gave up.  One CTA of a cluster polls and tells the others through their shared memory (each barrier has a flag of
-// its own there: a CTA that is slow to read the first must not find the second's answer).
-__device__ __forceinline__ bool grid_barrier(int* counter, int* status, int S, int rank, int polls, int* flag) {
+// Every CTA of the grid has arrived and what it wrote before is visible; false if the wait gave up.
+__device__ __forceinline__ bool grid_barrier(int* counter, int* status, int polls, int* flag) {
     __syncthreads();
     if (threadIdx.x == 0) {
-        __threadfence();
-        atomicAdd(counter, 1);
-        if (rank == 0) {
-            const int limit = polls > 0 ? polls : kSpinPolls;
-            int seen = 0;
-            for (int i = 0; i < limit; ++i) {
-                asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
-                if (seen >= (int)gridDim.x) break;
-            }
-            const bool ok = seen >= (int)gridDim.x;
-            if (!ok) *status = 1;
-            *flag = ok;
-            for (int r = 1; r < S; ++r)
-                asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(at_rank(smem_addr(flag), r)), "r"(ok ? 1 : 0) : "memory");
+        asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(counter) : "memory");
+        const int limit = polls > 0 ? polls : kSpinPolls;
+        int seen = 0;
+        for (int i = 0; i < limit; ++i) {
+            asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
+            if (seen >= (int)gridDim.x) break;
         }
+        *flag = seen >= (int)gridDim.x;
+        if (!*flag) *status = 1;
     }
-    group_sync(S);
+    __syncthreads();
     return *flag != 0;
 }
+
+__device__ __forceinline__ void warm(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 __device__ __forceinline__ void store_y(void* y, int64_t i, int type, float v) {
     if (type == PP_F32) static_cast<float*>(y)[i] = v;
@@ -209,15 +178,16 @@ __device__ __forceinline__ void token_scale(float most, float& up, float& down) 
 
 // ---- step 0 ------------------------------------------------------------------------------------------------------
 // One CTA turns a token into columns.
-template <class W, typename T> __device__ void token_columns(const MoeArgs& a, int token, float* part) {
+template <class W, typename T, bool VEC> __device__ __forceinline__ void token_columns(const MoeArgs& a, int token, float* part) {
     constexpr bool BF16 = W::kBf16;
     constexpr int cpt = columns<BF16, T>();
     const T* x = static_cast<const T*>(a.in.x) + (int64_t)token * a.in.ld;
     float up = 1.0f, down = 1.0f;
     if (!BF16 && !std::is_same_v<T, __half>) {
         float most = 0.0f;
+#pragma unroll 2
         for (int c = threadIdx.x * 4; c < a.H; c += kThreads * 4) {
-            const Pack<T, 4> v = load_four(x, c, a.H, a.in.vec != 0);
+            const Pack<T, 4> v = load_four<VEC>(x, c, a.H);
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(to_float(v.v[i])));
         }
@@ -232,8 +202,9 @@ template <class W, typename T> __device__ void token_columns(const MoeArgs& a, i
         token_scale(most, up, down);
     }
     uint16_t* dst = a.xcols + (int64_t)token * cpt * a.kpad1;
+#pragma unroll 2
     for (int c = threadIdx.x * 4; c < a.kpad1; c += kThreads * 4) {       // zeros up to the padded length
-        const Pack<T, 4> v = load_four(x, c, a.H, a.in.vec != 0);
+        const Pack<T, 4> v = load_four<VEC>(x, c, a.H);
         Pack<uint16_t, 4> bits[cpt];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -247,25 +218,24 @@ template <class W, typename T> __device__ void token_columns(const MoeArgs& a, i
     if (threadIdx.x == 0) a.xscale[token] = down;
 }
 
-// A warp's logit of one (token, expert); what cannot be compared ranks last.
-template <typename T> __device__ __forceinline__ void router_logit(const MoeArgs& a, int token, int expert) {
+// A warp's logit of one (token, expert); what cannot be compared ranks last.  Eight loads of each row are in flight.
+template <typename T, bool VEC> __device__ __forceinline__ void router_logit(const MoeArgs& a, int token, int expert) {
+    constexpr int kAhead = VEC ? 8 : 1;
     const int lane = threadIdx.x & 31;
     const float* r = a.router + (int64_t)expert * a.router_ld;
     const T* row = static_cast<const T*>(a.in.x) + (int64_t)token * a.in.ld;
     float sum = 0.0f;
-    for (int c0 = lane * 4; c0 < a.H; c0 += 1024) {
-        Pack<T, 4> x[8];
-        float4 w[8];
+#pragma unroll 1
+    for (int c0 = lane * 4; c0 < a.H; c0 += kAhead * 128) {
+        Pack<T, 4> x[kAhead];
+        float4 w[kAhead];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = c0 + i * 128;
-            if (c >= a.H) break;
-            x[i] = load_four(row, c, a.H, a.in.vec != 0);
-            w[i] = __ldg(reinterpret_cast<const float4*>(r + c));
+        for (int i = 0; i < kAhead; ++i) {
+            x[i] = load_four<VEC>(row, c0 + i * 128, a.H);                 // zeros past the end: the router's row may repeat there
+            w[i] = __ldg(reinterpret_cast<const float4*>(r + min(c0 + i * 128, a.router_ld - 4)));
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (c0 + i * 128 >= a.H) break;
+        for (int i = 0; i < kAhead; ++i) {
             sum = fmaf(to_float(x[i].v[0]), w[i].x, sum);
             sum = fmaf(to_float(x[i].v[1]), w[i].y, sum);
             sum = fmaf(to_float(x[i].v[2]), w[i].z, sum);
@@ -277,73 +247,119 @@ template <typename T> __device__ __forceinline__ void router_logit(const MoeArgs
     if (lane == 0) a.logits[token * a.E + expert] = sum == sum ? sum : -INFINITY;
 }
 
+// Router pairs go to warp 0 of every CTA, the last CTA first (the first ones have tokens to turn into columns), then warp 1.
+template <class W, typename T, bool VEC> __device__ __forceinline__ void step0(const MoeArgs& a, float* part) {
+    for (int t = blockIdx.x; t < a.T; t += gridDim.x) token_columns<W, T, VEC>(a, t, part);
+    for (int i = (threadIdx.x >> 5) * gridDim.x + (gridDim.x - 1 - blockIdx.x); i < a.T * a.E; i += kWarps * gridDim.x)
+        router_logit<T, VEC>(a, i / a.E, i % a.E);
+}
 template <class W, typename T> __device__ __forceinline__ void step0(const MoeArgs& a, float* part) {
-    const int warp = threadIdx.x >> 5;
-    for (int t = blockIdx.x; t < a.T; t += gridDim.x) token_columns<W, T>(a, t, part);
-    for (int i = warp * gridDim.x + (gridDim.x - 1 - blockIdx.x); i < a.T * a.E; i += kWarps * gridDim.x) router_logit<T>(a, i / a.E, i % a.E);
+    if (a.in.vec) step0<W, T, true>(a, part);
+    else step0<W, T, false>(a, part);
 }
 
 // ---- routing, by every CTA for itself ----------------------------------------------------------------------------
 struct Lists {
     int4* entry;         // {expert, first pair, pairs, 0}: an expert and up to kCap of its tokens
+    int2* plan;          // [strips of a round] {which warps have sums of it, its entry (step 1)}
     int* pair_token;     // pairs (token, expert) in the order of the experts
     float* pair_gate;
+    int* chosen;         // [T][top_k] experts
     float* gate;         // [T][top_k]
-    int* sums;           // scratch of the scan
-    uint8_t* slot;       // [T][E]: which of the token's choices the expert is, 255 none
+    float* xscale;       // [T]
+    uint32_t* tokens;    // [E] which tokens chose the expert
+    int* first;          // [E] its first pair
+    int* sums;           // [warps] scratch of the scan
+    int* cuts;           // [2][2] first and last CTA of the strips that the CTA's ends divide, [4..5] whether it finishes them
 };
-__host__ __device__ inline int list_bytes(int T, int E, int top_k) { return (T * top_k * (16 + 4 + 4 + 4) + 64 + T * E + 127) / 128 * 128; }
-__device__ __forceinline__ Lists lists_at(unsigned char* p, int T, int top_k) {
+__host__ __device__ inline int list_bytes(int T, int E, int top_k) {
+    return (T * top_k * (16 + 4 + 4 + 4 + 4) + 16 * 8 + T * 4 + E * 8 + 16 * 4 + 8 * 4 + 127) / 128 * 128;
+}
+__device__ __forceinline__ Lists lists_at(unsigned char* p, int T, int E, int top_k) {
     Lists L;
     const int n = T * top_k;
     L.entry = reinterpret_cast<int4*>(p);
-    L.pair_token = reinterpret_cast<int*>(L.entry + n);
+    L.plan = reinterpret_cast<int2*>(L.entry + n);
+    L.pair_token = reinterpret_cast<int*>(L.plan + 16);
     L.pair_gate = reinterpret_cast<float*>(L.pair_token + n);
-    L.gate = L.pair_gate + n;
-    L.sums = reinterpret_cast<int*>(L.gate + n);
-    L.slot = reinterpret_cast<uint8_t*>(L.sums + 16);
+    L.chosen = reinterpret_cast<int*>(L.pair_gate + n);
+    L.gate = reinterpret_cast<float*>(L.chosen + n);
+    L.xscale = L.gate + n;
+    L.tokens = reinterpret_cast<uint32_t*>(L.xscale + T);
+    L.first = reinterpret_cast<int*>(L.tokens + E);
+    L.sums = L.first + E;
+    L.cuts = L.sums + 16;
     return L;
 }
 
-__device__ int route(const MoeArgs& a, const Lists& L) {                   // the number of entries
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    for (int i = tid; i < a.T * a.E; i += kThreads) {
-        const int t = i / a.E, e = i - t * a.E;
-        const float* row = a.logits + t * a.E;
-        const float l = row[e];
-        int rank = 0;
-#pragma unroll 8
-        for (int j = 0; j < a.E; ++j) rank += row[j] > l || (row[j] == l && j < e);
-        L.slot[i] = rank < a.top_k ? (uint8_t)rank : (uint8_t)255;
-    }
-    __syncthreads();
-    for (int t = warp; t < a.T; t += kWarps) {
-        const float* row = a.logits + t * a.E;
-        float most = -INFINITY, sum = 0.0f;
-        for (int e = lane; e < a.E; e += 32) most = fmaxf(most, row[e]);
+// A warp chooses a token's experts: the largest logit's key (floats as whole numbers in the same order) top_k times, among
+// equal ones the lowest index; lane j keeps the j-th.  Then the softmax over them, or over all.
+__device__ __forceinline__ void choose(const MoeArgs& a, const Lists& L, int t) {
+    constexpr int kEach = kMaxExperts / 32;
+    const int lane = threadIdx.x & 31, each = (a.E + 31) / 32;
+    const float* row = a.logits + t * a.E;
+    uint32_t key[kEach];
 #pragma unroll
-        for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        for (int e = lane; e < a.E; e += 32)
-            if (!a.renorm || L.slot[t * a.E + e] != 255) sum += expf(row[e] - most);
-#pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        for (int e = lane; e < a.E; e += 32) {
-            const int slot = L.slot[t * a.E + e];
-            if (slot == 255) continue;
-            const float p = expf(row[e] - most) / sum;
-            L.gate[t * a.top_k + slot] = p;
-            if (blockIdx.x == 0) {
-                if (a.ids) a.ids[t * a.top_k + slot] = e;
-                if (a.gates) a.gates[t * a.top_k + slot] = p;
-            }
+    for (int i = 0; i < kEach; ++i) {
+        key[i] = 0u;                                         // below every logit
+        if (i < each && i * 32 + lane < a.E) {
+            const uint32_t u = __float_as_uint(__ldcg(row + i * 32 + lane));
+            key[i] = (int)u < 0 ? ~u : u | 0x80000000u;
         }
     }
+    uint32_t mine = 0u;
+    int expert = 0;
+    for (int j = 0; j < a.top_k; ++j) {
+        uint32_t most = key[0];
+#pragma unroll
+        for (int i = 1; i < kEach; ++i)
+            if (i < each) most = max(most, key[i]);
+        most = __reduce_max_sync(0xffffffffu, most);
+        uint32_t at = 0xffffffffu;
+#pragma unroll
+        for (int i = kEach - 1; i >= 0; --i)
+            if (i < each && key[i] == most) at = i * 32 + lane;
+        at = __reduce_min_sync(0xffffffffu, at);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (i < each && at == i * 32 + lane) key[i] = 0u;
+        if (lane == j) mine = most, expert = (int)at;
+    }
+    const uint32_t u = (int)mine < 0 ? mine & 0x7fffffffu : ~mine;
+    const float l = __uint_as_float(u), most0 = __shfl_sync(0xffffffffu, l, 0);
+    float p = lane < a.top_k ? expf(l - most0) : 0.0f, sum = p;
+    if (!a.renorm) {                                         // the experts that were not chosen count as well
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (i < each && key[i]) {
+                const uint32_t v = (int)key[i] < 0 ? key[i] & 0x7fffffffu : ~key[i];
+                sum += expf(__uint_as_float(v) - most0);
+            }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    p /= sum;
+    if (lane < a.top_k) {
+        const int at = t * a.top_k + lane;
+        L.chosen[at] = expert;
+        L.gate[at] = p;
+        atomicOr(L.tokens + expert, 1u << t);
+        if (blockIdx.x == 0) {
+            if (a.ids) a.ids[at] = expert;
+            if (a.gates) a.gates[at] = p;
+        }
+    }
+}
+
+__device__ __forceinline__ int route(const MoeArgs& a, const Lists& L) {       // the number of entries; L.tokens is zero before
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid < a.T) L.xscale[tid] = __ldcg(a.xscale + tid);
+    for (int t = warp; t < a.T; t += kWarps) choose(a, L, t);
+    __syncthreads();
     // where each expert's pairs and entries start: both counts in one scan (neither exceeds 512)
-    int n = 0;
-    if (tid < a.E)
-        for (int t = 0; t < a.T; ++t) n += L.slot[t * a.E + tid] != 255;
-    int both = n | ((n + kCap - 1) / kCap) << 16;
-    const int mine = both;
+    const int n = tid < a.E ? __popc(L.tokens[tid]) : 0;
+    const int mine = n | ((n + kCap - 1) / kCap) << 16;
+    int both = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int v = __shfl_up_sync(0xffffffffu, both, o);
@@ -351,103 +367,165 @@ __device__ int route(const MoeArgs& a, const Lists& L) {                   // th
     }
     if (lane == 31) L.sums[warp] = both;
     __syncthreads();
-    int before = 0, all = 0;
+    int before = both - mine, all = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) before += L.sums[w];
-        all += L.sums[w];
+    for (int w = 0; w < kMaxExperts / 32; ++w) {
+        const int v = L.sums[w];
+        if (w < warp) before += v;
+        all += v;
     }
-    before += both - mine;
     if (n) {
         const int first = before & 0xffff, entry = before >> 16;
+        L.first[tid] = first;
         for (int i = 0; i * kCap < n; ++i) L.entry[entry + i] = make_int4(tid, first + i * kCap, min(kCap, n - i * kCap), 0);
-        int p = first;
-        for (int t = 0; t < a.T; ++t) {
-            const int slot = L.slot[t * a.E + tid];
-            if (slot == 255) continue;
-            L.pair_token[p] = t;
-            L.pair_gate[p++] = L.gate[t * a.top_k + slot];
-        }
+    }
+    __syncthreads();
+    if (tid < a.T * a.top_k) {                               // at most 512 pairs
+        const int t = tid / a.top_k, e = L.chosen[tid], p = L.first[e] + __popc(L.tokens[e] & ((1u << t) - 1u));
+        L.pair_token[p] = t;
+        L.pair_gate[p] = L.gate[tid];
     }
     __syncthreads();
     return all >> 16;
 }
 
 // ---- steps 1 and 2: the stream of weights ------------------------------------------------------------------------
-// What one CTA does in a step: strips first .. first + count of its cluster, `round` at a time, and of each strip the
-// blocks v0 .. v0 + nv.  In step 1 a strip belongs to one entry and its blocks are the columns of x; in step 2 a strip is
-// 16 rows of y and its blocks are the entries' columns of act, one entry after another.
-struct Span { int first, count, round, v0, nv; };
-struct Run { const unsigned char *unit, *sets; int left, ls, entry, kb; };        // units that lie one after another
+// Units are numbered strip after strip, nv to a strip: in step 1 the blocks of the columns of x (a strip belongs to one
+// entry), in step 2 the entries' blocks of the columns of act, one entry after another (a strip is 16 rows of y).  A CTA
+// has units begin .. end; x below counts them from the start of its first strip, x0 .. x1, and a round is `round` strips.
+struct Span {
+    int nv, ctas, first, x0, x1, rounds, strips;     // ctas: that have units at all; first: the first strip; strips: of this CTA
+    float per_strip;                                 // 1 / nv
+};
+struct Run { const unsigned char *unit, *sets; int left, ls, entry, kb; };        // units that lie one after another; ls: strip - first
 
-template <class W, int STEP> __device__ __forceinline__ void locate(const MoeArgs& a, const Lists& L, const Span& s, int round, int u, Run& r) {
-    r.ls = u / s.nv;
-    const int v = s.v0 + u - r.ls * s.nv;
-    int strip = s.first + round * s.round + r.ls;
+// x / n from the reciprocal of n, for quotients below 2^21.
+__device__ __forceinline__ int divide(int x, int n, float r) {
+    int q = (int)((float)x * r);
+    const int rest = x - q * n;
+    if (rest < 0) --q;
+    if (rest >= n) ++q;
+    return q;
+}
+
+__device__ __forceinline__ Span span_of(int64_t units, int nv, int round) {
+    Span s;
+    s.nv = nv;
+    s.per_strip = 1.0f / (float)nv;
+    s.ctas = (int)min((int64_t)gridDim.x, units);
+    const int64_t begin = units * min((int)blockIdx.x, s.ctas) / s.ctas, end = units * min((int)blockIdx.x + 1, s.ctas) / s.ctas;
+    s.first = (int)(begin / nv);
+    s.x0 = (int)(begin - (int64_t)s.first * nv);
+    s.x1 = s.x0 + (int)(end - begin);
+    s.strips = s.x1 > s.x0 ? (s.x1 + nv - 1) / nv : 0;
+    s.rounds = (s.strips + round - 1) / round;
+    return s;
+}
+
+template <class W, int STEP> __device__ __forceinline__ void locate(const MoeArgs& a, const Lists& L, const Span& s, int x, int stop, Run& r) {
+    r.ls = divide(x, s.nv, s.per_strip);
+    const int v = x - r.ls * s.nv;
+    int strip = s.first + r.ls;
     if (STEP == 1) {
-        r.entry = strip / a.strips1;
+        r.entry = divide(strip, a.strips1, a.per_expert);
         strip -= r.entry * a.strips1;
         r.kb = v;
-        r.left = s.v0 + s.nv - v;
+        r.left = min(s.nv - v, stop - x);
     } else {
-        r.entry = v / a.kb2;
+        r.entry = divide(v, a.kb2, a.per_entry);
         r.kb = v - r.entry * a.kb2;
-        r.left = min(a.kb2 - r.kb, s.v0 + s.nv - v);
+        r.left = min(a.kb2 - r.kb, stop - x);
     }
     const int64_t at = ((int64_t)L.entry[r.entry].x * (STEP == 1 ? a.strips1 : a.strips2) + strip) * (STEP == 1 ? a.kb1 : a.kb2) + r.kb;
     r.unit = (STEP == 1 ? a.gate_up : a.down) + at * 1024;
     r.sets = (STEP == 1 ? a.gate_up_sets : a.down_sets) + at * W::kSetBytes;
 }
 
-// This warp's units of a round.
-__device__ __forceinline__ void warp_range(const Span& s, int round, int warp, int& u0, int& u1) {
-    const int U = min(s.round, s.count - round * s.round) * s.nv;
-    u0 = (int)((int64_t)U * warp / kWarps);
-    u1 = (int)((int64_t)U * (warp + 1) / kWarps);
+// This warp's units of a round: x .. stop (a round has at most 16 strips of 2^20 units).
+__device__ __forceinline__ void warp_range(const Span& s, int round, int strips, int warp, int& x, int& stop) {
+    const int lo = max(s.x0, round * strips * s.nv), n = min(s.x1, (round + 1) * strips * s.nv) - lo;
+    x = lo + (int)((uint32_t)(n * warp) / kWarps);
+    stop = lo + (int)((uint32_t)(n * (warp + 1)) / kWarps);
 }
 
 template <class W, int STEP> struct Fetcher {
-    int round = -1, u = 0, u1 = 0;
+    int round = -1, x = 0, stop = 0;
     Run run;
-    __device__ __forceinline__ void next(const MoeArgs& a, const Lists& L, const Span& s, int rounds, int warp, int lane, uint32_t slot) {
-        while (u == u1 && round < rounds) {
-            if (++round < rounds) warp_range(s, round, warp, u, u1);
+    __device__ __forceinline__ void next(const MoeArgs& a, const Lists& L, const Span& s, int warp, int lane, unsigned char* slot) {
+        while (x == stop && round < s.rounds) {
+            if (++round < s.rounds) warp_range(s, round, a.round, warp, x, stop);
             run.left = 0;
         }
-        if (u < u1) {
-            if (run.left == 0) locate<W, STEP>(a, L, s, round, u, run);
-            unit_fetch(slot, run.unit, run.sets, lane, W::kSetBytes / 16);
+        if (x < stop) {
+            if (run.left == 0) locate<W, STEP>(a, L, s, x, stop, run);
+            unit_fetch(smem_addr(slot), run.unit, run.sets, lane, W::kSetBytes / 16);
             run.unit += 1024;
             run.sets += W::kSetBytes;
             --run.left;
-            ++u;
+            ++x;
         }
         cp_commit();
     }
 };
 
+// What a strip's sums become.  Step 1: act of one (row, pair), step 2: y of one (row, token).
+template <class W> __device__ __forceinline__ void finish_act(const MoeArgs& a, const Lists& L, int entry, int strip, int row8, int pl, float gate, float up) {
+    const int p = L.entry[entry].y + pl, row = (strip - entry * a.strips1) * 8 + row8;
+    const float scale = L.xscale[L.pair_token[p]];
+    gate *= scale;
+    up *= scale;
+    const float act = L.pair_gate[p] * (gate / (1.0f + expf(-gate)) * up);
+    const int at = W::kSwap && ((row & 3) == 1 || (row & 3) == 2) ? row ^ 3 : row;
+    split_act<W::kBf16>(act, a.acols + (int64_t)p * kActCols * a.kpad2 + at, a.kpad2);
+}
+__device__ __forceinline__ void finish_y(const MoeArgs& a, int strip, int row, int token, float v) {
+    const int m = strip * 16 + row;
+    if (m < a.H) store_y(a.y, (int64_t)token * a.H + m, a.y_type, v);
+}
+
 template <class W, int STEP>
-__device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const Span& s, Fetcher<W, STEP>& f, int rounds, unsigned char* smem, int S,
-                                       int rank, int& buffer) {
+__device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const Span& s, Fetcher<W, STEP>& f, unsigned char* smem) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int cpt = STEP == 1 ? a.cpt : kActCols, width = STEP == 1 ? kCap : a.T, kpad = STEP == 1 ? a.kpad1 : a.kpad2;
     const uint16_t* cols = STEP == 1 ? a.xcols : a.acols;
     unsigned char* ring = smem + warp * kDepth * a.slot_bytes;
     float* scr = reinterpret_cast<float*>(smem + a.scr_off) + warp * 16 * kCols;
     float* park = reinterpret_cast<float*>(smem + a.park_off);
+    float* my_parts = a.parts + (int64_t)blockIdx.x * 2 * 16 * width;
+    // the strips that the CTA's ends divide: its first and its last (one, if it has only one)
+    const bool cut_first = s.strips && s.x0 > 0, cut_last = s.strips && s.x1 < s.strips * s.nv;
     int slot = 0;
-    for (int round = 0; round < rounds; ++round) {
-        const int rs = min(s.round, s.count - round * s.round), U = rs * s.nv;
-        int u0, u1, strip = -1, tiles = 1;
-        warp_range(s, round, warp, u0, u1);
+    for (int round = 0; round < s.rounds; ++round) {
+        const int ls0 = round * a.round, rs = min(a.round, s.strips - ls0);
+        int x, stop, strip = -1, tiles = 1;
+        {                                                    // which warps will have sums of each strip: half a warp per strip
+            const int q = tid >> 4, w = tid & 15;
+            int lo, hi;
+            warp_range(s, round, a.round, w, lo, hi);
+            const bool has = q < rs && max(lo, (ls0 + q) * s.nv) < min(hi, (ls0 + q + 1) * s.nv);
+            const uint32_t mask = __ballot_sync(0xffffffffu, has) >> (lane & 16) & 0xffffu;
+            if (w == 0 && q < rs) L.plan[q] = make_int2((int)mask, STEP == 1 ? divide(s.first + ls0 + q, a.strips1, a.per_expert) : 0);
+        }
+        warp_range(s, round, a.round, warp, x, stop);
         Run run;
         run.left = 0;
         const uint16_t* from[kTiles] = {};
+        uint4 xr[kTiles][W::kLoads];
         int4 entry = make_int4(0, 0, 0, 0);
         float tot[kTiles][4] = {};
-        for (int u = u0; u < u1; ++u) {
+        const auto read_columns = [&] {                      // what the lane needs of the next unit's columns
+#pragma unroll
+            for (int nt = 0; nt < kTiles; ++nt) {
+                if (nt < tiles) {
+#pragma unroll
+                    for (int j = 0; j < W::kLoads; ++j) xr[nt][j] = *reinterpret_cast<const uint4*>(from[nt] + j * 32);
+                }
+                from[nt] += W::kUnitCols;
+            }
+        };
+        for (; x < stop; ++x) {
             if (run.left == 0) {
-                locate<W, STEP>(a, L, s, round, u, run);
+                locate<W, STEP>(a, L, s, x, stop, run);
                 entry = L.entry[run.entry];
                 tiles = (entry.z * cpt + 7) / 8;
 #pragma unroll
@@ -456,23 +534,22 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
                     const int row = (STEP == 1 ? L.pair_token[p] : p) * cpt + c % cpt;
                     from[nt] = cols + (int64_t)row * kpad + run.kb * W::kUnitCols + t * 8;
                 }
+                read_columns();
                 if (STEP == 2 && run.ls != strip) {            // a new strip's sums of this warp
                     strip = run.ls;
-                    for (int i = lane; i < 16 * width; i += 32) park[(warp + strip) * 16 * width + i] = 0.0f;
+                    for (int i = lane; i < 16 * width; i += 32) park[(warp + strip - ls0) * 16 * width + i] = 0.0f;
                 }
             }
             cp_wait<kDepth - 1>();
             __syncwarp();
-            const auto load_x = [&](int nt, int j) { return *reinterpret_cast<const uint4*>(from[nt] + j * 32); };
             unsigned char* at = ring + slot * a.slot_bytes;
-            if (tiles == 1) W::template unit<1>(reinterpret_cast<float(&)[1][4]>(tot), at, lane, a.bf16_scales != 0, load_x);
-            else W::template unit<kTiles>(tot, at, lane, a.bf16_scales != 0, load_x);
-#pragma unroll
-            for (int nt = 0; nt < kTiles; ++nt) from[nt] += W::kUnitCols;
+            if (tiles == 1) W::template unit<1>(reinterpret_cast<float(&)[1][4]>(tot), at, lane, a.bf16_scales != 0, xr);
+            else W::template unit<kTiles>(tot, at, lane, a.bf16_scales != 0, xr);
+            if (--run.left) read_columns();                    // in flight while the other warps compute
             __syncwarp();
-            f.next(a, L, s, rounds, warp, lane, smem_addr(at));
+            f.next(a, L, s, warp, lane, at);
             if (++slot == kDepth) slot = 0;
-            if (--run.left == 0 || u + 1 == u1) {
+            if (run.left == 0) {
                 // add a token's columns and park the sums: piece (warp, strip) has slot warp + strip
 #pragma unroll
                 for (int nt = 0; nt < kTiles; ++nt)
@@ -482,17 +559,17 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
                         tot[nt][i] = 0.0f;
                     }
                 __syncwarp();
-                float* tile = park + (warp + run.ls) * 16 * width;
-                for (int i = lane; i < 16 * entry.z; i += 32) {
-                    const int row = i / entry.z, pl = i - row * entry.z;
+                float* tile = park + (warp + run.ls - ls0) * 16 * width;
+                const int row = lane & 15;
+                for (int pl = lane >> 4; pl < entry.z; pl += 2) {
                     const float* c = scr + row * kCols + pl * cpt;
                     if (STEP == 1) {
                         float v = c[0];
                         for (int k = 1; k < cpt; ++k) v += c[k];
-                        tile[row * width + pl] = v;
+                        tile[pl * 16 + row] = v;
                     } else {
                         const float v = W::kBf16 ? c[0] + c[1] + c[2] : fmaf(c[0], 0x1p11f, fmaf(c[1], 2.0f, c[2] * 0x1p-10f));
-                        tile[row * width + L.pair_token[entry.y + pl]] += v;
+                        tile[L.pair_token[entry.y + pl] * 16 + row] += v;
                     }
                 }
                 __syncwarp();
@@ -500,113 +577,132 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
         }
         __syncthreads();
 
-        // the pieces of a row in the order of the warps; each CTA of the cluster finishes an equal part of the results
-        const int outs = rs * (STEP == 1 ? 8 * kCap : 16 * a.T), share = (outs + S - 1) / S;
-        float* red = reinterpret_cast<float*>(smem + a.red_off) + buffer * a.red_floats;
-        buffer ^= 1;
-        const auto pieces = [&](int ls, int at) {
-            float v = 0.0f;
-            if (U) {
-                const int w_lo = (kWarps * (ls * s.nv + 1) - 1) / U, w_hi = (kWarps * (ls * s.nv + s.nv) - 1) / U;
-                for (int w = w_lo; w <= w_hi; ++w)
-                    if ((int)((int64_t)U * w / kWarps) < (int)((int64_t)U * (w + 1) / kWarps)) v += park[(w + ls) * 16 * width + at];
-            }
-            return v;
-        };
-        for (int o = tid; o < outs; o += kThreads) {
-            const int owner = o / share, at = rank * share + o - owner * share;
+        // the pieces of a row in the order of the warps
+        const int per_strip = STEP == 1 ? 8 * kCap : 16 * a.T;
+        const Divider by_strip(per_strip);
+        for (int o = tid; o < rs * per_strip; o += kThreads) {
+            const int q = by_strip.div(o), r = o - q * per_strip, ls = ls0 + q;
+            const bool cut = (ls == 0 && cut_first) || (ls == s.strips - 1 && cut_last);
+            // the strip's slot among this CTA's parts: 0 where an earlier CTA has begun it
+            float* part = my_parts + (ls == 0 && cut_first ? 0 : 16 * width);
+            const int2 plan = L.plan[q];
             if (STEP == 1) {
-                const int ls = o / (8 * kCap), r = o - ls * 8 * kCap, pl = r % kCap;
-                if (pl >= L.entry[(s.first + round * s.round + ls) / a.strips1].z) continue;
-                const float gate = pieces(ls, r), up = pieces(ls, r + 8 * kCap);
-                if (S > 1) {
-                    st_cluster(smem_addr(red + 2 * at), owner, gate);
-                    st_cluster(smem_addr(red + 2 * at + 1), owner, up);
-                } else {
-                    red[2 * at] = gate;
-                    red[2 * at + 1] = up;
-                }
-            } else {
-                const int token = o / (rs * 16), r = o - token * rs * 16;
-                const float v = pieces(r >> 4, (r & 15) * width + token);
-                if (S > 1) st_cluster(smem_addr(red + at), owner, v);
-                else red[at] = v;
-            }
-        }
-        group_sync(S);
-        const int first = rank * share, last = min(outs, first + share);
-        for (int o = first + tid; o < last; o += kThreads) {
-            if (STEP == 1) {
-                const int ls = o / (8 * kCap), r = o - ls * 8 * kCap, pl = r % kCap;
-                const int strip_all = s.first + round * s.round + ls, en = strip_all / a.strips1;
-                const int4 e = L.entry[en];
-                if (pl >= e.z) continue;
+                const int pl = r >> 3, row = r & 7;
+                if (pl >= L.entry[plan.y].z) continue;
                 float gate = 0.0f, up = 0.0f;
-                for (int q = 0; q < S; ++q) {
-                    gate += red[2 * (q * share + o - first)];
-                    up += red[2 * (q * share + o - first) + 1];
+                for (uint32_t m = (uint32_t)plan.x; m; m &= m - 1) {
+                    const float* c = park + (__ffs((int)m) - 1 + q) * 16 * width + pl * 16 + row;
+                    gate += c[0];
+                    up += c[8];
                 }
-                const int p = e.y + pl, row = (strip_all - en * a.strips1) * 8 + r / kCap;
-                const float scale = __ldcg(a.xscale + L.pair_token[p]);
-                gate *= scale;
-                up *= scale;
-                const float act = L.pair_gate[p] * (gate / (1.0f + expf(-gate)) * up);
-                const int at = W::kSwap && ((row & 3) == 1 || (row & 3) == 2) ? row ^ 3 : row;
-                split_act<W::kBf16>(act, a.acols + (int64_t)p * kActCols * a.kpad2 + at, a.kpad2);
+                if (!cut) {
+                    finish_act<W>(a, L, plan.y, s.first + ls, row, pl, gate, up);
+                } else {
+                    __stcg(part + pl * 16 + row, gate);
+                    __stcg(part + pl * 16 + row + 8, up);
+                }
             } else {
-                const int token = o / (rs * 16), m = (s.first + round * s.round) * 16 + o - token * rs * 16;
-                if (m >= a.H) continue;
                 float v = 0.0f;
-                for (int q = 0; q < S; ++q) v += red[q * share + o - first];
-                store_y(a.y, (int64_t)token * a.H + m, a.y_type, v);
+                for (uint32_t m = (uint32_t)plan.x; m; m &= m - 1) v += park[(__ffs((int)m) - 1 + q) * 16 * width + r];
+                if (!cut) finish_y(a, s.first + ls, r & 15, r >> 4, v);
+                else __stcg(part + r, v);
             }
         }
+        __syncthreads();
+    }
+}
+
+// First and last CTA of the strips that this CTA's ends divide (-1: it divides none there): unit x belongs to the last CTA
+// c with units * c / ctas <= x.  Two threads, while the weights are on their way.
+__device__ __forceinline__ void find_cuts(const Lists& L, const Span& s, int64_t units) {
+    const int which = threadIdx.x;
+    if (which < 2) {
+        const bool cut_first = s.strips && s.x0 > 0, cut_last = s.strips && s.x1 < s.strips * s.nv;
+        const bool cut = which == 0 ? cut_first : cut_last && !(cut_first && s.strips == 1);
+        const int64_t lo = (int64_t)(s.first + (which == 0 ? 0 : s.strips - 1)) * s.nv;
+        L.cuts[which] = cut ? (int)(((lo + 1) * s.ctas - 1) / units) : -1;
+        L.cuts[2 + which] = cut ? (int)(((lo + s.nv) * s.ctas - 1) / units) : -1;
+    }
+}
+
+// Divided strips: the last of a strip's CTAs to arrive adds the parts in the order of the CTAs.
+template <class W, int STEP> __device__ __forceinline__ void join(const MoeArgs& a, const Lists& L, const Span& s) {
+    const int tid = threadIdx.x, width = STEP == 1 ? kCap : a.T;
+    if (tid < 2 && L.cuts[tid] >= 0) {                       // behind the barrier that ended the last round
+        int* arrived = a.sync + 4 + (STEP - 1) * gridDim.x + L.cuts[tid];
+        int before;
+        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(arrived) : "memory");
+        const bool last = before == L.cuts[2 + tid] - L.cuts[tid];
+        if (last) *arrived = 0;
+        L.cuts[4 + tid] = last;
+    } else if (tid < 2) {
+        L.cuts[4 + tid] = 0;
+    }
+    __syncthreads();
+    const int per_strip = STEP == 1 ? 8 * kCap : 16 * a.T;
+    for (int o = tid; o < 2 * per_strip; o += kThreads) {
+        const int which = o >= per_strip, r = o - which * per_strip;
+        if (!L.cuts[4 + which]) continue;
+        const int c0 = L.cuts[which], c1 = L.cuts[2 + which], strip = s.first + (which == 0 ? 0 : s.strips - 1);
+        const int pl = r >> 3, row = r & 7, entry = STEP == 1 ? divide(strip, a.strips1, a.per_expert) : 0;
+        if (STEP == 1 && pl >= L.entry[entry].z) continue;
+        const int at = STEP == 1 ? pl * 16 + row : r;
+        float v[2] = {0.0f, 0.0f};
+#pragma unroll 4
+        for (int c = c0; c <= c1; ++c) {
+            const float* part = a.parts + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * 16 * width + at;
+            v[0] += __ldcg(part);
+            if (STEP == 1) v[1] += __ldcg(part + 8);
+        }
+        if (STEP == 1) finish_act<W>(a, L, entry, strip, row, pl, v[0], v[1]);
+        else finish_y(a, strip, r & 15, r >> 4, v[0]);
     }
 }
 
 template <class W> __global__ void __launch_bounds__(kThreads, 1) moe_kernel(const MoeArgs a) {
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float part[kWarps];
-    __shared__ int flag[2];
-    const int S = (int)cluster_size(), rank = (int)cluster_rank(), clusters = gridDim.x / S, cl = blockIdx.x / S;
+    __shared__ int flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Lists L = lists_at(smem + a.list_off, a.T, a.top_k);
-    if (S > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+    const Lists L = lists_at(smem + a.list_off, a.T, a.E, a.top_k);
     pdl_release();
+    // before the wait: the router's rows on their way to L2, and the translations of what is touched first
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.E * a.router_ld / 32; i += gridDim.x * kThreads) warm(a.router + i * 32);
+    if (threadIdx.x == 0) {
+        warm(a.in.x);
+        warm(a.logits);
+        warm(a.xcols);
+        warm(a.acols);
+        warm(a.y);
+        warm(a.parts);
+    }
+    for (int e = threadIdx.x; e < a.E; e += kThreads) L.tokens[e] = 0u;
     pdl_wait();
 
     if (a.in.type == PP_BF16) step0<W, __nv_bfloat16>(a, part);
     else if (a.in.type == PP_F16) step0<W, __half>(a, part);
     else step0<W, float>(a, part);
-    if (S > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");     // the cluster's other CTAs have started
-    bool ok = grid_barrier(a.sync, a.sync + 3, S, rank, a.polls, flag);
+    bool ok = grid_barrier(a.sync, a.sync + 3, a.polls, &flag);
     if (ok) {
         const int entries = route(a, L);
-        const uint32_t ring = smem_addr(smem) + (uint32_t)(warp * kDepth * a.slot_bytes);
-        int buffer = 0;
-        Span s;
-        const int64_t strips = (int64_t)entries * a.strips1;
-        s.first = (int)(strips * cl / clusters);
-        s.count = (int)(strips * (cl + 1) / clusters) - s.first;
-        s.round = a.round1;
-        s.v0 = a.kb1 * rank / S;
-        s.nv = a.kb1 * (rank + 1) / S - s.v0;
-        {
-            Fetcher<W, 1> f;
-            const int rounds = (s.count + s.round - 1) / s.round;
-            for (int d = 0; d < kDepth; ++d) f.next(a, L, s, rounds, warp, lane, ring + d * a.slot_bytes);
-            stream<W, 1>(a, L, s, f, rounds, smem, S, rank, buffer);
+        unsigned char* ring = smem + warp * kDepth * a.slot_bytes;
+        const Span s1 = span_of((int64_t)entries * a.strips1 * a.kb1, a.kb1, a.round);
+        Fetcher<W, 1> f1;
+#pragma unroll 1
+        for (int d = 0; d < kDepth; ++d) f1.next(a, L, s1, warp, lane, ring + d * a.slot_bytes);
+        find_cuts(L, s1, (int64_t)entries * a.strips1 * a.kb1);
+        stream<W, 1>(a, L, s1, f1, smem);
+        const Span s2 = span_of((int64_t)a.strips2 * entries * a.kb2, entries * a.kb2, a.round);
+        Fetcher<W, 2> f2;
+#pragma unroll 1
+        for (int d = 0; d < kDepth; ++d) f2.next(a, L, s2, warp, lane, ring + d * a.slot_bytes);
+        join<W, 1>(a, L, s1);
+        ok = grid_barrier(a.sync + 1, a.sync + 3, a.polls, &flag);
+        if (ok) {
+            find_cuts(L, s2, (int64_t)a.strips2 * entries * a.kb2);
+            stream<W, 2>(a, L, s2, f2, smem);
+            join<W, 2>(a, L, s2);
         }
-        s.first = a.strips2 * cl / clusters;
-        s.count = a.strips2 * (cl + 1) / clusters - s.first;
-        s.round = a.round2;
-        s.v0 = entries * a.kb2 * rank / S;
-        s.nv = entries * a.kb2 * (rank + 1) / S - s.v0;
-        Fetcher<W, 2> f;
-        const int rounds = (s.count + s.round - 1) / s.round;
-        for (int d = 0; d < kDepth; ++d) f.next(a, L, s, rounds, warp, lane, ring + d * a.slot_bytes);
-        ok = grid_barrier(a.sync + 1, a.sync + 3, S, rank, a.polls, flag + 1);
-        if (ok) stream<W, 2>(a, L, s, f, rounds, smem, S, rank, buffer);
         cp_wait<0>();
     }
     __syncthreads();
@@ -662,42 +758,18 @@ Kernel pick_kernel(const pp_moe* L) {
 
 constexpr int kMaxSmem = 227 * 1024 - 256;       // beside the kernel's few static bytes
 
-// Strips of a round and the shared memory they take; the most strips that fit, 16 at most (one to a warp).
-size_t plan_smem(MoeArgs& a, int S) {
+// Strips of a round and the shared memory: the most strips that fit, 16 at most (one to a warp).
+size_t plan_smem(MoeArgs& a) {
     size_t at = (size_t)kWarps * kDepth * a.slot_bytes;
     a.list_off = (int)(at = (at + 127) / 128 * 128);
     at += list_bytes(a.T, a.E, a.top_k);
     a.scr_off = (int)at;
     at += (size_t)kWarps * 16 * kCols * 4;
     a.park_off = (int)at;
-    for (int R = 16;; R /= 2) {
-        a.round1 = a.round2 = R;
-        const size_t park = (size_t)(R + kWarps) * 16 * std::max(kCap, a.T) * 4;
-        a.red_floats = std::max(R * 8 * kCap + S, R * 8 * a.T + S) * 2;
-        a.red_off = (int)(a.park_off + park);
-        const size_t total = a.red_off + (size_t)a.red_floats * 8;
-        if (total <= (size_t)kMaxSmem || R == 1) return total;
+    for (a.round = 16;; a.round /= 2) {
+        const size_t total = at + (size_t)(a.round + kWarps) * 16 * std::max(kCap, a.T) * 4;
+        if (total <= (size_t)kMaxSmem || a.round == 1) return total;
     }
-}
-
-// Resident CTAs of a cooperative launch with clusters of S, 0 if none.
-int resident(Kernel k, int S, size_t smem) {
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = (unsigned)S;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(S);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, k, &cfg) != cudaSuccess) {
-        cudaGetLastError();
-        return 0;
-    }
-    return n * S;
 }
 
 template <typename T> bool alloc(T** p, size_t n) { return cudaMalloc(reinterpret_cast<void**>(p), n) == cudaSuccess; }
@@ -711,7 +783,7 @@ extern "C" pp_status_t pp_moe_destroy(pp_moe_t* L) {
     if (!L) return PP_ERR_INVALID_ARG;
     for (void* p : {static_cast<void*>(L->gate_up), static_cast<void*>(L->down), static_cast<void*>(L->gate_up_sets),
                     static_cast<void*>(L->down_sets), static_cast<void*>(L->router), static_cast<void*>(L->logits),
-                    static_cast<void*>(L->xscale), static_cast<void*>(L->xcols), static_cast<void*>(L->acols), static_cast<void*>(L->sync)})
+                    static_cast<void*>(L->xscale), static_cast<void*>(L->xcols), static_cast<void*>(L->acols), static_cast<void*>(L->parts), static_cast<void*>(L->sync)})
         cudaFree(p);
     delete L;
     return PP_OK;
@@ -743,27 +815,32 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
     L->kb1 = (H + cols - 1) / cols;
     L->kb2 = (F + cols - 1) / cols;
     const size_t pairs = (size_t)max_tokens * top_k, ld = (size_t)(H + 3) / 4 * 4;
-    const size_t abytes = pairs * kActCols * L->kb2 * cols * 2;
+    const size_t units1 = (size_t)E * L->strips1 * L->kb1, units2 = (size_t)E * L->strips2 * L->kb2;
+    const size_t set_bytes = wtype < 0 ? q4_set_bytes(L->sets, asym) : 0, abytes = pairs * kActCols * L->kb2 * cols * 2;
     pp_status_t st = PP_OK;
-    const size_t units1 = (size_t)E * L->strips1 * L->kb1, units2 = (size_t)E * L->strips2 * L->kb2, set_bytes = wtype < 0 ? q4_set_bytes(L->sets, asym) : 0;
-    if (!alloc(&L->gate_up, units1 * 1024) || !alloc(&L->down, units2 * 1024) ||
-        (set_bytes && (!alloc(&L->gate_up_sets, units1 * set_bytes) || !alloc(&L->down_sets, units2 * set_bytes))) || !alloc(&L->router, ld * E * 4) ||
-        !alloc(&L->logits, (size_t)max_tokens * E * 4) || !alloc(&L->xscale, (size_t)max_tokens * 4) ||
-        !alloc(&L->xcols, (size_t)max_tokens * 3 * L->kb1 * cols * 2) || !alloc(&L->acols, abytes) || !alloc(&L->sync, 16)) {
+    // as many CTAs as the device holds at once, asked for with the most shared memory a call may take
+    const void* kernel = reinterpret_cast<const void*>(pick_kernel(L));
+    int device = 0, sms = 0, each = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kThreads, kMaxSmem) != cudaSuccess || each < 1) st = PP_ERR_CUDA;
+    L->ctas = sms;
+    const size_t sync_bytes = (4 + 2 * (size_t)L->ctas) * 4;
+    if (st == PP_OK &&
+        (!alloc(&L->gate_up, units1 * 1024) || !alloc(&L->down, units2 * 1024) ||
+         (set_bytes && (!alloc(&L->gate_up_sets, units1 * set_bytes) || !alloc(&L->down_sets, units2 * set_bytes))) || !alloc(&L->router, ld * E * 4) ||
+         !alloc(&L->logits, (size_t)max_tokens * E * 4) || !alloc(&L->xscale, (size_t)max_tokens * 4) ||
+         !alloc(&L->xcols, (size_t)max_tokens * 3 * L->kb1 * cols * 2) || !alloc(&L->acols, abytes) ||
+         !alloc(&L->parts, (size_t)L->ctas * 2 * 16 * std::max(kCap, max_tokens) * 4) || !alloc(&L->sync, sync_bytes))) {
         cudaGetLastError();
         st = PP_ERR_ALLOC;
     }
     if (st == PP_OK) {
         // act's columns past F are never written and stay zero
-        if (cudaMemsetAsync(L->acols, 0, abytes, s) != cudaSuccess || cudaMemsetAsync(L->sync, 0, 16, s) != cudaSuccess) st = PP_ERR_CUDA;
+        if (cudaMemsetAsync(L->acols, 0, abytes, s) != cudaSuccess || cudaMemsetAsync(L->sync, 0, sync_bytes, s) != cudaSuccess) st = PP_ERR_CUDA;
         router_pack_kernel<<<148, 256, 0, s>>>(L->router, router, router_type, E, H, (int)ld);
-        if (cudaGetLastError() != cudaSuccess ||
-            cudaFuncSetAttribute(reinterpret_cast<const void*>(pick_kernel(L)), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) != cudaSuccess)
-            st = PP_ERR_CUDA;
+        if (cudaGetLastError() != cudaSuccess) st = PP_ERR_CUDA;
     }
-    // one CTA to an SM, whatever the call's shared memory: asked for the most
-    for (int S = 1; S <= 4 && st == PP_OK; S *= 2) L->ctas[S] = resident(pick_kernel(L), S, kMaxSmem);
-    if (st == PP_OK && L->ctas[1] < 1) st = PP_ERR_CUDA;
     if (st != PP_OK) {
         pp_moe_destroy(L);
         return st;
@@ -835,7 +912,7 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     a.in.ld = ldx;
     a.in.type = x_type;
     a.in.cols = L->H;
-    a.in.vec = aligned_to(x, 4 * xb) && (tokens == 1 || ldx % 4 == 0);
+    a.in.vec = aligned_to(x, 4 * xb) && (tokens == 1 || ldx % 4 == 0) && L->H % 4 == 0;
     a.logits = L->logits;
     a.xscale = L->xscale;
     a.xcols = L->xcols;
@@ -863,32 +940,21 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     a.cpt = L->wtype == PP_BF16 ? (x_type == PP_BF16 ? 1 : x_type == PP_F16 ? 2 : 3) : (x_type == PP_F32 ? 2 : 1);
     a.bf16_scales = L->bf16_scales;
     a.polls = g_stream_wait_polls;
-    // cluster size: fewest blocks on the busiest CTA, for the experts the tokens reach at most
-    const int64_t experts = std::min<int64_t>(L->E, (int64_t)tokens * L->top_k);
-    int best = 0;
-    int64_t least = 0;
-    for (int S = 1; S <= 4; S *= 2) {
-        const int64_t n = L->ctas[S] / S;
-        if (n < 1) continue;
-        const int64_t cost = (experts * L->strips1 + n - 1) / n * ((L->kb1 + S - 1) / S) + (L->strips2 + n - 1) / n * ((experts * L->kb2 + S - 1) / S);
-        if (!best || cost < least) best = S, least = cost;
-    }
-    const size_t smem = plan_smem(a, best);
-    cudaLaunchAttribute at[3];
+    a.parts = L->parts;
+    a.per_expert = 1.0f / (float)L->strips1;
+    a.per_entry = 1.0f / (float)L->kb2;
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeCooperative;
     at[0].val.cooperative = 1;
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
-    at[2].id = cudaLaunchAttributeClusterDimension;
-    at[2].val.clusterDim.x = (unsigned)best;
-    at[2].val.clusterDim.y = at[2].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(L->ctas[best]);
+    cfg.gridDim = dim3(L->ctas);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = plan_smem(a);
     cfg.stream = static_cast<cudaStream_t>(cuda_stream);
     cfg.attrs = at;
-    cfg.numAttrs = best > 1 ? 3 : 2;
+    cfg.numAttrs = 2;
     if (cudaLaunchKernelEx(&cfg, pick_kernel(L), a) == cudaSuccess) return PP_OK;
     cudaGetLastError();
     return PP_ERR_CUDA;

@@ -137,9 +137,9 @@ template <int NT> __device__ __forceinline__ int column_of(int token, int c, int
 // This CTA's columns of x, laid out [64 columns][column of the product][lane t][8 bytes of 32 columns, 8 of the next];
 // what a column stands for per block (cs), and its sum over each set of scales (sums).  Eight blocks of four elements per
 // lane (four of f32) are requested before the first is converted: a step of this loop is a trip to memory.
-template <typename T, int NT, int SETS>
-__device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, float* cs, int* sums, int k0, int n_k, int warp, int lane) {
-    constexpr int kAhead = sizeof(T) == 4 ? 4 : 8, cpt = std::is_same_v<T, int8_t> ? 1 : 3;
+template <typename T, bool VEC, int NT, int SETS>
+__device__ __forceinline__ void stage_rows(const Q4Args& a, unsigned char* xs, float* cs, int* sums, int k0, int n_k, int warp, int lane) {
+    constexpr int kAhead = !VEC ? 1 : sizeof(T) == 4 ? 4 : 8, cpt = std::is_same_v<T, int8_t> ? 1 : 3;
     const int items = a.tokens * n_k, step = a.nc * 64;
     const Divider by_blocks(n_k);
     for (int base = warp; base < items; base += kAhead * kWarps) {
@@ -147,9 +147,8 @@ __device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, floa
         float own[kAhead];
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
-            const int item = base + q * kWarps, token = by_blocks.div(item), block = k0 + item - token * n_k;
-            if (item >= items) break;
-            v[q] = load_four(static_cast<const T*>(a.in.x) + token * a.in.ld, block * kQ4UnitCols + lane * 4, a.in.cols, a.in.vec != 0);
+            const int item = min(base + q * kWarps, items - 1), token = by_blocks.div(item), block = k0 + item - token * n_k;
+            v[q] = load_four<VEC>(static_cast<const T*>(a.in.x) + token * a.in.ld, block * kQ4UnitCols + lane * 4, a.in.cols);
             if (sizeof(T) == 1) own[q] = a.in.scales[(int64_t)token * a.in.scale_ld + (a.in.group_blocks ? block / a.in.group_blocks : 0)];
         }
 #pragma unroll
@@ -184,6 +183,12 @@ __device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, floa
             }
         }
     }
+}
+
+template <typename T, int NT, int SETS>
+__device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, float* cs, int* sums, int k0, int n_k, int warp, int lane) {
+    if (a.in.vec) stage_rows<T, true, NT, SETS>(a, xs, cs, sums, k0, n_k, warp, lane);
+    else stage_rows<T, false, NT, SETS>(a, xs, cs, sums, k0, n_k, warp, lane);
 }
 
 __device__ __forceinline__ void mma_u8s8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -570,7 +575,7 @@ extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_
     a.in.scale_ld = x_group ? (L->N + x_group - 1) / x_group : 1;
     a.in.group_blocks = x_group / kQ4UnitCols;
     a.in.cols = L->N;
-    a.in.vec = aligned_to(x, 4 * xb) && (batch == 1 || ldx % 4 == 0);
+    a.in.vec = aligned_to(x, 4 * xb) && (batch == 1 || ldx % 4 == 0) && L->N % 4 == 0;
     a.y_type = y_type;
     a.act = act;
     a.M = L->M;

@@ -143,14 +143,16 @@ struct XIn {
     int type, scale_ld;
     int group_blocks;        // 8-bit types: blocks of 128 columns per scale, 0 = one scale per token
     int cols;
-    int vec;                 // every row starts on an access of four elements
+    int vec;                 // every row starts on an access of four elements and has a multiple of four
 };
 
-// Elements col .. col + 3 of a row, zeros from cols on; vec: they lie on one access.
-template <typename T> __device__ __forceinline__ Pack<T, 4> load_four(const T* row, int col, int cols, bool vec) {
+// Elements col .. col + 3 of a row, zeros from cols on.  VEC: rows start on an access of four elements and cols is a
+// multiple of four; the load then needs no branch, and several of them stay in flight together.
+template <bool VEC, typename T> __device__ __forceinline__ Pack<T, 4> load_four(const T* row, int col, int cols) {
     Pack<T, 4> v{};
-    if (vec && col + 4 <= cols) {
-        v = *reinterpret_cast<const Pack<T, 4>*>(row + col);
+    if (VEC) {
+        v = *reinterpret_cast<const Pack<T, 4>*>(row + min(col, cols - 4));
+        if (col >= cols) v = Pack<T, 4>{};
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
