@@ -49,8 +49,8 @@ struct pp_moe {
 namespace pp {
 namespace {
 
-constexpr int kWarps = 16, kThreads = kWarps * 32, kDepth = 6, kTiles = 2, kCols = 8 * kTiles;
-constexpr int kMaxExperts = 256, kMaxTopK = 16, kMaxTokens = 32, kActCols = 3, kCap = kCols / kActCols;   // tokens of an entry
+constexpr int kWarps = 16, kThreads = kWarps * 32, kMaxCols = 16;
+constexpr int kMaxExperts = 256, kMaxTopK = 16, kMaxTokens = 32, kActCols = 3, kCap = kMaxCols / kActCols;   // tokens of an entry
 constexpr int kSpinPolls = 1 << 24;          // seconds; a barrier that is met never gets near it
 
 struct MoeArgs {
@@ -80,6 +80,9 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint4& a, uint32_t
 template <bool BF16> struct Wide {           // 16-bit weights: 16 rows x 32 columns, two operand fragments of 512 bytes
     static constexpr int kUnitCols = 32, kSetBytes = 0, kLoads = 1;       // kLoads: 16-byte reads of a lane and column
     static constexpr bool kBf16 = BF16, kSwap = false;
+    // The columns' part of a unit (512 bytes a tile) travels in the ring with the weights: read through L1 instead, the first
+    // pass of a CTA over a new expert's columns took twice as long as the others, a trip to L2 per unit.
+    static constexpr bool kRingCols = true;
     template <int NT>
     static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool, const uint4 (*x)[kLoads]) {
         const uint4 a = at<uint4>(slot + lane * 16), b = at<uint4>(slot + 512 + lane * 16);
@@ -100,18 +103,25 @@ template <bool BF16> struct Wide {           // 16-bit weights: 16 rows x 32 col
 template <int SETS, bool ASYM> struct Q4 {
     static constexpr int kUnitCols = kQ4UnitCols, kSetBytes = SETS * (ASYM ? 48 : 32), kLoads = 4;
     static constexpr bool kBf16 = false, kSwap = true;        // kSwap: columns 4i + 1 and 4i + 2 of the input change places
+    static constexpr bool kRingCols = false;                  // 2 KB a tile, twice the weights: no room in the ring
     template <int NT>
     static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool bf16_scales, const uint4 (*x)[kLoads]) {
         q4_unit_f16<NT, SETS, ASYM>(tot, slot, lane, bf16_scales, [&](int nt, int j) { return x[nt][j]; });
     }
 };
 
+// Units in flight per warp.  Calls of one or two tokens need one tile of 8 columns (three columns of act each), others two.
+template <class W, int TILES> __host__ __device__ constexpr int depth() { return W::kRingCols && TILES == 2 ? 4 : 6; }
+
 // ---- small helpers -----------------------------------------------------------------------------------------------
-// Every CTA of the grid has arrived and what it wrote before is visible; false if the wait gave up.
-__device__ __forceinline__ bool grid_barrier(int* counter, int* status, int polls, int* flag) {
+// Grid barrier in two parts.  After the second every CTA of the grid has passed the first and what it wrote before is
+// visible; false if the wait gave up.
+__device__ __forceinline__ void grid_arrive(int* counter) {
     __syncthreads();
+    if (threadIdx.x == 0) asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(counter) : "memory");
+}
+__device__ __forceinline__ bool grid_wait(const int* counter, int* status, int polls, int* flag) {
     if (threadIdx.x == 0) {
-        asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(counter) : "memory");
         const int limit = polls > 0 ? polls : kSpinPolls;
         int seen = 0;
         for (int i = 0; i < limit; ++i) {
@@ -396,6 +406,7 @@ __device__ __forceinline__ int route(const MoeArgs& a, const Lists& L) {       /
 struct Span {
     int nv, ctas, first, x0, x1, rounds, strips;     // ctas: that have units at all; first: the first strip; strips: of this CTA
     float per_strip;                                 // 1 / nv
+    bool whole;                                      // no strip is divided
 };
 struct Run { const unsigned char *unit, *sets; int left, ls, entry, kb; };        // units that lie one after another; ls: strip - first
 
@@ -408,12 +419,27 @@ __device__ __forceinline__ int divide(int x, int n, float r) {
     return q;
 }
 
-__device__ __forceinline__ Span span_of(int64_t units, int nv, int round) {
+// This CTA's part of `strips` strips of nv units.  Cuts fall between strips unless that leaves the busiest CTA with kJoin
+// units more than its equal share: joining a divided strip takes about 3,700 cycles, 84 units at the rate of HBM (148 CTAs:
+// 256 strips of 32 units are faster whole, 256 strips of 3,600 units are not: 519,000 cycles whole, 396,000 cut).
+constexpr int kJoin = 84;
+__device__ __forceinline__ Span span_of(int strips, int nv, int round) {
     Span s;
     s.nv = nv;
     s.per_strip = 1.0f / (float)nv;
-    s.ctas = (int)min((int64_t)gridDim.x, units);
-    const int64_t begin = units * min((int)blockIdx.x, s.ctas) / s.ctas, end = units * min((int)blockIdx.x + 1, s.ctas) / s.ctas;
+    const int grid = (int)gridDim.x, most = (strips + grid - 1) / grid;
+    const int64_t units = (int64_t)strips * nv;
+    s.whole = (int64_t)most * nv - units / grid <= kJoin;
+    int64_t begin, end;
+    if (s.whole) {
+        s.ctas = min(grid, strips);
+        begin = (int64_t)strips * min((int)blockIdx.x, s.ctas) / s.ctas * nv;
+        end = (int64_t)strips * min((int)blockIdx.x + 1, s.ctas) / s.ctas * nv;
+    } else {
+        s.ctas = (int)min((int64_t)grid, units);
+        begin = units * min((int)blockIdx.x, s.ctas) / s.ctas;
+        end = units * min((int)blockIdx.x + 1, s.ctas) / s.ctas;
+    }
     s.first = (int)(begin / nv);
     s.x0 = (int)(begin - (int64_t)s.first * nv);
     s.x1 = s.x0 + (int)(end - begin);
@@ -448,17 +474,42 @@ __device__ __forceinline__ void warp_range(const Span& s, int round, int strips,
     stop = lo + (int)((uint32_t)(n * (warp + 1)) / kWarps);
 }
 
-template <class W, int STEP> struct Fetcher {
-    int round = -1, x = 0, stop = 0;
+// Where a lane reads the columns of a run: column 8 nt + g of the entry's tiles, elements 8t .. of the run's first unit.
+template <class W, int STEP, int TILES>
+__device__ __forceinline__ void run_columns(const MoeArgs& a, const Lists& L, const Run& r, int lane, const uint16_t* (&from)[TILES]) {
+    const int cpt = STEP == 1 ? a.cpt : kActCols, kpad = STEP == 1 ? a.kpad1 : a.kpad2;
+    const int4 entry = L.entry[r.entry];
+#pragma unroll
+    for (int nt = 0; nt < TILES; ++nt) {
+        const int c = nt * 8 + (lane >> 2), pl = cpt == 1 ? c : cpt == 2 ? c >> 1 : c / 3, p = entry.y + min(pl, entry.z - 1);   // columns past the last repeat one
+        const int row = (STEP == 1 ? L.pair_token[p] : p) * cpt + c - pl * cpt;
+        from[nt] = (STEP == 1 ? a.xcols : a.acols) + (int64_t)row * kpad + r.kb * W::kUnitCols + (lane & 3) * 8;
+    }
+}
+
+template <class W, int STEP, int TILES> struct Fetcher {
+    int round = -1, x = 0, stop = 0, tiles = 1;
     Run run;
-    __device__ __forceinline__ void next(const MoeArgs& a, const Lists& L, const Span& s, int warp, int lane, unsigned char* slot) {
+    const uint16_t* from[TILES];
+    __device__ __forceinline__ void next(const MoeArgs& a, const Lists& L, const Span& s, int warp, int lane, unsigned char* slot, bool weights, bool cols) {
         while (x == stop && round < s.rounds) {
             if (++round < s.rounds) warp_range(s, round, a.round, warp, x, stop);
             run.left = 0;
         }
         if (x < stop) {
-            if (run.left == 0) locate<W, STEP>(a, L, s, x, stop, run);
-            unit_fetch(smem_addr(slot), run.unit, run.sets, lane, W::kSetBytes / 16);
+            if (run.left == 0) {
+                locate<W, STEP>(a, L, s, x, stop, run);
+                if (W::kRingCols) run_columns<W, STEP, TILES>(a, L, run, lane, from);
+                if (TILES > 1) tiles = (L.entry[run.entry].z * (STEP == 1 ? a.cpt : kActCols) + 7) / 8;
+            }
+            if (weights) unit_fetch(smem_addr(slot), run.unit, run.sets, lane, W::kSetBytes / 16);
+            if (W::kRingCols) {
+#pragma unroll
+                for (int nt = 0; nt < TILES; ++nt) {
+                    if (cols && nt < tiles) cp_async16_l1(smem_addr(slot) + 1024 + nt * 512 + lane * 16, from[nt]);
+                    from[nt] += W::kUnitCols;
+                }
+            }
             run.unit += 1024;
             run.sets += W::kSetBytes;
             --run.left;
@@ -483,11 +534,11 @@ __device__ __forceinline__ void finish_y(const MoeArgs& a, int strip, int row, i
     if (m < a.H) store_y(a.y, (int64_t)token * a.H + m, a.y_type, v);
 }
 
-template <class W, int STEP>
-__device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const Span& s, Fetcher<W, STEP>& f, unsigned char* smem) {
+template <class W, int STEP, int TILES>
+__device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const Span& s, Fetcher<W, STEP, TILES>& f, unsigned char* smem) {
+    constexpr int kDepth = depth<W, TILES>(), kCols = 8 * TILES;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int cpt = STEP == 1 ? a.cpt : kActCols, width = STEP == 1 ? kCap : a.T, kpad = STEP == 1 ? a.kpad1 : a.kpad2;
-    const uint16_t* cols = STEP == 1 ? a.xcols : a.acols;
+    const int cpt = STEP == 1 ? a.cpt : kActCols, width = STEP == 1 ? kCap : a.T;
     unsigned char* ring = smem + warp * kDepth * a.slot_bytes;
     float* scr = reinterpret_cast<float*>(smem + a.scr_off) + warp * 16 * kCols;
     float* park = reinterpret_cast<float*>(smem + a.park_off);
@@ -509,13 +560,13 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
         warp_range(s, round, a.round, warp, x, stop);
         Run run;
         run.left = 0;
-        const uint16_t* from[kTiles] = {};
-        uint4 xr[kTiles][W::kLoads];
+        const uint16_t* from[TILES] = {};
+        uint4 xr[TILES][W::kLoads];
         int4 entry = make_int4(0, 0, 0, 0);
-        float tot[kTiles][4] = {};
+        float tot[TILES][4] = {};
         const auto read_columns = [&] {                      // what the lane needs of the next unit's columns
 #pragma unroll
-            for (int nt = 0; nt < kTiles; ++nt) {
+            for (int nt = 0; nt < TILES; ++nt) {
                 if (nt < tiles) {
 #pragma unroll
                     for (int j = 0; j < W::kLoads; ++j) xr[nt][j] = *reinterpret_cast<const uint4*>(from[nt] + j * 32);
@@ -527,14 +578,11 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
             if (run.left == 0) {
                 locate<W, STEP>(a, L, s, x, stop, run);
                 entry = L.entry[run.entry];
-                tiles = (entry.z * cpt + 7) / 8;
-#pragma unroll
-                for (int nt = 0; nt < kTiles; ++nt) {
-                    const int c = nt * 8 + g, p = entry.y + min(c / cpt, entry.z - 1);       // columns past the last repeat one
-                    const int row = (STEP == 1 ? L.pair_token[p] : p) * cpt + c % cpt;
-                    from[nt] = cols + (int64_t)row * kpad + run.kb * W::kUnitCols + t * 8;
+                tiles = TILES == 1 ? 1 : (entry.z * cpt + 7) / 8;
+                if (!W::kRingCols) {
+                    run_columns<W, STEP, TILES>(a, L, run, lane, from);
+                    read_columns();
                 }
-                read_columns();
                 if (STEP == 2 && run.ls != strip) {            // a new strip's sums of this warp
                     strip = run.ls;
                     for (int i = lane; i < 16 * width; i += 32) park[(warp + strip - ls0) * 16 * width + i] = 0.0f;
@@ -543,16 +591,22 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
             cp_wait<kDepth - 1>();
             __syncwarp();
             unsigned char* at = ring + slot * a.slot_bytes;
-            if (tiles == 1) W::template unit<1>(reinterpret_cast<float(&)[1][4]>(tot), at, lane, a.bf16_scales != 0, xr);
-            else W::template unit<kTiles>(tot, at, lane, a.bf16_scales != 0, xr);
-            if (--run.left) read_columns();                    // in flight while the other warps compute
+            if (W::kRingCols) {
+#pragma unroll
+                for (int nt = 0; nt < TILES; ++nt)
+                    if (nt < tiles) xr[nt][0] = *reinterpret_cast<const uint4*>(at + 1024 + nt * 512 + lane * 16);
+            }
+            if (TILES == 1 || tiles == 1) W::template unit<1>(reinterpret_cast<float(&)[1][4]>(tot), at, lane, a.bf16_scales != 0, xr);
+            else W::template unit<TILES>(tot, at, lane, a.bf16_scales != 0, xr);
+            --run.left;
+            if (!W::kRingCols && run.left) read_columns();     // in flight while the other warps compute
             __syncwarp();
-            f.next(a, L, s, warp, lane, at);
+            f.next(a, L, s, warp, lane, at, true, true);
             if (++slot == kDepth) slot = 0;
             if (run.left == 0) {
                 // add a token's columns and park the sums: piece (warp, strip) has slot warp + strip
 #pragma unroll
-                for (int nt = 0; nt < kTiles; ++nt)
+                for (int nt = 0; nt < TILES; ++nt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         scr[(g + (i >> 1) * 8) * kCols + nt * 8 + 2 * t + (i & 1)] = tot[nt][i];
@@ -659,7 +713,8 @@ template <class W, int STEP> __device__ __forceinline__ void join(const MoeArgs&
     }
 }
 
-template <class W> __global__ void __launch_bounds__(kThreads, 1) moe_kernel(const MoeArgs a) {
+template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe_kernel(const MoeArgs a) {
+    constexpr int kDepth = depth<W, TILES>();
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float part[kWarps];
     __shared__ int flag;
@@ -682,26 +737,34 @@ template <class W> __global__ void __launch_bounds__(kThreads, 1) moe_kernel(con
     if (a.in.type == PP_BF16) step0<W, __nv_bfloat16>(a, part);
     else if (a.in.type == PP_F16) step0<W, __half>(a, part);
     else step0<W, float>(a, part);
-    bool ok = grid_barrier(a.sync, a.sync + 3, a.polls, &flag);
+    grid_arrive(a.sync);
+    bool ok = grid_wait(a.sync, a.sync + 3, a.polls, &flag);
     if (ok) {
         const int entries = route(a, L);
         unsigned char* ring = smem + warp * kDepth * a.slot_bytes;
-        const Span s1 = span_of((int64_t)entries * a.strips1 * a.kb1, a.kb1, a.round);
-        Fetcher<W, 1> f1;
+        {
+            const Span s = span_of(entries * a.strips1, a.kb1, a.round);
+            Fetcher<W, 1, TILES> f;
 #pragma unroll 1
-        for (int d = 0; d < kDepth; ++d) f1.next(a, L, s1, warp, lane, ring + d * a.slot_bytes);
-        find_cuts(L, s1, (int64_t)entries * a.strips1 * a.kb1);
-        stream<W, 1>(a, L, s1, f1, smem);
-        const Span s2 = span_of((int64_t)a.strips2 * entries * a.kb2, entries * a.kb2, a.round);
-        Fetcher<W, 2> f2;
+            for (int d = 0; d < kDepth; ++d) f.next(a, L, s, warp, lane, ring + d * a.slot_bytes, true, true);
+            if (!s.whole) find_cuts(L, s, (int64_t)entries * a.strips1 * a.kb1);
+            stream<W, 1, TILES>(a, L, s, f, smem);
+            if (!s.whole) join<W, 1>(a, L, s);
+        }
+        grid_arrive(a.sync + 1);
+        const Span s = span_of(a.strips2, entries * a.kb2, a.round);
+        Fetcher<W, 2, TILES> f, g;                           // ahead of the barrier the weights, behind it their columns
 #pragma unroll 1
-        for (int d = 0; d < kDepth; ++d) f2.next(a, L, s2, warp, lane, ring + d * a.slot_bytes);
-        join<W, 1>(a, L, s1);
-        ok = grid_barrier(a.sync + 1, a.sync + 3, a.polls, &flag);
+        for (int d = 0; d < kDepth; ++d) f.next(a, L, s, warp, lane, ring + d * a.slot_bytes, true, false);
+        ok = grid_wait(a.sync + 1, a.sync + 3, a.polls, &flag);
         if (ok) {
-            find_cuts(L, s2, (int64_t)a.strips2 * entries * a.kb2);
-            stream<W, 2>(a, L, s2, f2, smem);
-            join<W, 2>(a, L, s2);
+            if (W::kRingCols) {
+#pragma unroll 1
+                for (int d = 0; d < kDepth; ++d) g.next(a, L, s, warp, lane, ring + d * a.slot_bytes, false, true);
+            }
+            if (!s.whole) find_cuts(L, s, (int64_t)a.strips2 * entries * a.kb2);
+            stream<W, 2, TILES>(a, L, s, W::kRingCols ? g : f, smem);
+            if (!s.whole) join<W, 2>(a, L, s);
         }
         cp_wait<0>();
     }
@@ -748,23 +811,24 @@ cudaError_t launch_wide_pack(void* dst, const void* w, int count, int rows, int 
 }
 
 using Kernel = void (*)(const MoeArgs);
-Kernel pick_kernel(const pp_moe* L) {
-    if (L->wtype == PP_BF16) return moe_kernel<Wide<true>>;
-    if (L->wtype == PP_F16) return moe_kernel<Wide<false>>;
-    if (L->sets == 4) return L->asym ? moe_kernel<Q4<4, true>> : moe_kernel<Q4<4, false>>;
-    if (L->sets == 2) return L->asym ? moe_kernel<Q4<2, true>> : moe_kernel<Q4<2, false>>;
-    return L->asym ? moe_kernel<Q4<1, true>> : moe_kernel<Q4<1, false>>;
+template <int TILES> Kernel pick_kernel(const pp_moe* L) {
+    if (L->wtype == PP_BF16) return moe_kernel<Wide<true>, TILES>;
+    if (L->wtype == PP_F16) return moe_kernel<Wide<false>, TILES>;
+    if (L->sets == 4) return L->asym ? moe_kernel<Q4<4, true>, TILES> : moe_kernel<Q4<4, false>, TILES>;
+    if (L->sets == 2) return L->asym ? moe_kernel<Q4<2, true>, TILES> : moe_kernel<Q4<2, false>, TILES>;
+    return L->asym ? moe_kernel<Q4<1, true>, TILES> : moe_kernel<Q4<1, false>, TILES>;
 }
+int tiles_of(int tokens) { return tokens * kActCols <= 8 ? 1 : 2; }
 
 constexpr int kMaxSmem = 227 * 1024 - 256;       // beside the kernel's few static bytes
 
 // Strips of a round and the shared memory: the most strips that fit, 16 at most (one to a warp).
-size_t plan_smem(MoeArgs& a) {
-    size_t at = (size_t)kWarps * kDepth * a.slot_bytes;
+size_t plan_smem(MoeArgs& a, int depth, int tiles) {
+    size_t at = (size_t)kWarps * depth * a.slot_bytes;
     a.list_off = (int)(at = (at + 127) / 128 * 128);
     at += list_bytes(a.T, a.E, a.top_k);
     a.scr_off = (int)at;
-    at += (size_t)kWarps * 16 * kCols * 4;
+    at += (size_t)kWarps * 16 * 8 * tiles * 4;
     a.park_off = (int)at;
     for (a.round = 16;; a.round /= 2) {
         const size_t total = at + (size_t)(a.round + kWarps) * 16 * std::max(kCap, a.T) * 4;
@@ -819,11 +883,13 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
     const size_t set_bytes = wtype < 0 ? q4_set_bytes(L->sets, asym) : 0, abytes = pairs * kActCols * L->kb2 * cols * 2;
     pp_status_t st = PP_OK;
     // as many CTAs as the device holds at once, asked for with the most shared memory a call may take
-    const void* kernel = reinterpret_cast<const void*>(pick_kernel(L));
-    int device = 0, sms = 0, each = 0;
-    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) != cudaSuccess ||
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kThreads, kMaxSmem) != cudaSuccess || each < 1) st = PP_ERR_CUDA;
+    int device = 0, sms = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) st = PP_ERR_CUDA;
+    for (Kernel kernel : {pick_kernel<1>(L), pick_kernel<2>(L)}) {
+        int each = 0;
+        if (st == PP_OK && (cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) != cudaSuccess ||
+                            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kThreads, kMaxSmem) != cudaSuccess || each < 1)) st = PP_ERR_CUDA;
+    }
     L->ctas = sms;
     const size_t sync_bytes = (4 + 2 * (size_t)L->ctas) * 4;
     if (st == PP_OK &&
@@ -934,7 +1000,8 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     a.kpad1 = L->kb1 * cols;
     a.kpad2 = L->kb2 * cols;
     a.router_ld = (L->H + 3) / 4 * 4;
-    a.slot_bytes = 1024 + (q4 ? (q4_set_bytes(L->sets, L->asym) + 127) / 128 * 128 : 0);      // slots start on 128 bytes
+    const int tiles = tiles_of(tokens), depth = q4 || tiles == 1 ? 6 : 4;        // as depth() of the kernel
+    a.slot_bytes = 1024 + (q4 ? (q4_set_bytes(L->sets, L->asym) + 127) / 128 * 128 : 512 * tiles);      // slots start on 128 bytes
     a.gate_up_sets = L->gate_up_sets;
     a.down_sets = L->down_sets;
     a.cpt = L->wtype == PP_BF16 ? (x_type == PP_BF16 ? 1 : x_type == PP_F16 ? 2 : 3) : (x_type == PP_F32 ? 2 : 1);
@@ -951,11 +1018,11 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(L->ctas);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = plan_smem(a);
+    cfg.dynamicSmemBytes = plan_smem(a, depth, tiles);
     cfg.stream = static_cast<cudaStream_t>(cuda_stream);
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, pick_kernel(L), a) == cudaSuccess) return PP_OK;
+    if (cudaLaunchKernelEx(&cfg, tiles == 1 ? pick_kernel<1>(L) : pick_kernel<2>(L), a) == cudaSuccess) return PP_OK;
     cudaGetLastError();
     return PP_ERR_CUDA;
 }
