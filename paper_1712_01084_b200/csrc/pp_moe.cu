@@ -304,15 +304,14 @@ __device__ __forceinline__ Lists lists_at(unsigned char* p, int T, int E, int to
 
 // A warp chooses a token's experts: the largest logit's key (floats as whole numbers in the same order) top_k times, among
 // equal ones the lowest index; lane j keeps the j-th.  Then the softmax over them, or over all.
-__device__ __forceinline__ void choose(const MoeArgs& a, const Lists& L, int t) {
-    constexpr int kEach = kMaxExperts / 32;
-    const int lane = threadIdx.x & 31, each = (a.E + 31) / 32;
+template <int kEach> __device__ __forceinline__ void choose(const MoeArgs& a, const Lists& L, int t) {       // kEach: logits of a lane
+    const int lane = threadIdx.x & 31;
     const float* row = a.logits + t * a.E;
     uint32_t key[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         key[i] = 0u;                                         // below every logit
-        if (i < each && i * 32 + lane < a.E) {
+        if (i * 32 + lane < a.E) {
             const uint32_t u = __float_as_uint(__ldcg(row + i * 32 + lane));
             key[i] = (int)u < 0 ? ~u : u | 0x80000000u;
         }
@@ -322,17 +321,16 @@ __device__ __forceinline__ void choose(const MoeArgs& a, const Lists& L, int t) 
     for (int j = 0; j < a.top_k; ++j) {
         uint32_t most = key[0];
 #pragma unroll
-        for (int i = 1; i < kEach; ++i)
-            if (i < each) most = max(most, key[i]);
+        for (int i = 1; i < kEach; ++i) most = max(most, key[i]);
         most = __reduce_max_sync(0xffffffffu, most);
         uint32_t at = 0xffffffffu;
 #pragma unroll
         for (int i = kEach - 1; i >= 0; --i)
-            if (i < each && key[i] == most) at = i * 32 + lane;
+            if (key[i] == most) at = i * 32 + lane;
         at = __reduce_min_sync(0xffffffffu, at);
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
-            if (i < each && at == i * 32 + lane) key[i] = 0u;
+            if (at == i * 32 + lane) key[i] = 0u;
         if (lane == j) mine = most, expert = (int)at;
     }
     const uint32_t u = (int)mine < 0 ? mine & 0x7fffffffu : ~mine;
@@ -341,7 +339,7 @@ __device__ __forceinline__ void choose(const MoeArgs& a, const Lists& L, int t) 
     if (!a.renorm) {                                         // the experts that were not chosen count as well
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
-            if (i < each && key[i]) {
+            if (key[i]) {
                 const uint32_t v = (int)key[i] < 0 ? key[i] & 0x7fffffffu : ~key[i];
                 sum += expf(__uint_as_float(v) - most0);
             }
@@ -364,7 +362,11 @@ __device__ __forceinline__ void choose(const MoeArgs& a, const Lists& L, int t) 
 __device__ __forceinline__ int route(const MoeArgs& a, const Lists& L) {       // the number of entries; L.tokens is zero before
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid < a.T) L.xscale[tid] = __ldcg(a.xscale + tid);
-    for (int t = warp; t < a.T; t += kWarps) choose(a, L, t);
+    for (int t = warp; t < a.T; t += kWarps) {
+        if (a.E <= 32) choose<1>(a, L, t);
+        else if (a.E <= 64) choose<2>(a, L, t);
+        else choose<kMaxExperts / 32>(a, L, t);
+    }
     __syncthreads();
     // where each expert's pairs and entries start: both counts in one scan (neither exceeds 512)
     const int n = tid < a.E ? __popc(L.tokens[tid]) : 0;
@@ -427,23 +429,24 @@ __device__ __forceinline__ Span span_of(int strips, int nv, int round) {
     Span s;
     s.nv = nv;
     s.per_strip = 1.0f / (float)nv;
-    const int grid = (int)gridDim.x, most = (strips + grid - 1) / grid;
-    const int64_t units = (int64_t)strips * nv;
-    s.whole = (int64_t)most * nv - units / grid <= kJoin;
-    int64_t begin, end;
+    const int grid = (int)gridDim.x, cta = (int)blockIdx.x;
+    const int each = strips / grid, more = strips - each * grid;                 // strips of a CTA, CTAs with one more
+    s.whole = (int64_t)(more ? grid - more : 0) * nv <= (int64_t)kJoin * grid;
     if (s.whole) {
         s.ctas = min(grid, strips);
-        begin = (int64_t)strips * min((int)blockIdx.x, s.ctas) / s.ctas * nv;
-        end = (int64_t)strips * min((int)blockIdx.x + 1, s.ctas) / s.ctas * nv;
+        s.first = each * cta + min(cta, more);
+        s.x0 = 0;
+        s.strips = each + (cta < more);
+        s.x1 = s.strips * nv;
     } else {
+        const int64_t units = (int64_t)strips * nv;
         s.ctas = (int)min((int64_t)grid, units);
-        begin = units * min((int)blockIdx.x, s.ctas) / s.ctas;
-        end = units * min((int)blockIdx.x + 1, s.ctas) / s.ctas;
+        const int64_t begin = units * min(cta, s.ctas) / s.ctas, end = units * min(cta + 1, s.ctas) / s.ctas;
+        s.first = (int)(begin / nv);
+        s.x0 = (int)(begin - (int64_t)s.first * nv);
+        s.x1 = s.x0 + (int)(end - begin);
+        s.strips = s.x1 > s.x0 ? (s.x1 + nv - 1) / nv : 0;
     }
-    s.first = (int)(begin / nv);
-    s.x0 = (int)(begin - (int64_t)s.first * nv);
-    s.x1 = s.x0 + (int)(end - begin);
-    s.strips = s.x1 > s.x0 ? (s.x1 + nv - 1) / nv : 0;
     s.rounds = (s.strips + round - 1) / round;
     return s;
 }
@@ -487,33 +490,41 @@ __device__ __forceinline__ void run_columns(const MoeArgs& a, const Lists& L, co
     }
 }
 
+// A warp's asynchronous copies, unit after unit of its runs.
 template <class W, int STEP, int TILES> struct Fetcher {
-    int round = -1, x = 0, stop = 0, tiles = 1;
-    Run run;
+    int round = -1, x = 0, stop = 0, left = 0, tiles = 1;    // x: where the next run starts, left: units of this one
+    const unsigned char *unit = nullptr, *sets = nullptr;    // this lane's bytes of them
     const uint16_t* from[TILES];
-    __device__ __forceinline__ void next(const MoeArgs& a, const Lists& L, const Span& s, int warp, int lane, unsigned char* slot, bool weights, bool cols) {
-        while (x == stop && round < s.rounds) {
-            if (++round < s.rounds) warp_range(s, round, a.round, warp, x, stop);
-            run.left = 0;
-        }
-        if (x < stop) {
-            if (run.left == 0) {
-                locate<W, STEP>(a, L, s, x, stop, run);
-                if (W::kRingCols) run_columns<W, STEP, TILES>(a, L, run, lane, from);
-                if (TILES > 1) tiles = (L.entry[run.entry].z * (STEP == 1 ? a.cpt : kActCols) + 7) / 8;
+    __device__ __forceinline__ void next(const MoeArgs& a, const Lists& L, const Span& s, int warp, int lane, uint32_t slot, bool weights, bool cols) {
+        if (left == 0) {
+            while (x == stop && round < s.rounds)
+                if (++round < s.rounds) warp_range(s, round, a.round, warp, x, stop);
+            if (x < stop) {
+                Run r;
+                locate<W, STEP>(a, L, s, x, stop, r);
+                x += left = r.left;
+                unit = r.unit + lane * 16;
+                sets = r.sets + lane * 16;
+                if (W::kRingCols) run_columns<W, STEP, TILES>(a, L, r, lane, from);
+                if (TILES > 1) tiles = (L.entry[r.entry].z * (STEP == 1 ? a.cpt : kActCols) + 7) / 8;
             }
-            if (weights) unit_fetch(smem_addr(slot), run.unit, run.sets, lane, W::kSetBytes / 16);
+        }
+        if (left) {
+            --left;
+            if (weights) {
+                cp_async16(slot, unit);
+                cp_async16(slot + 512, unit + 512);
+                if (lane < W::kSetBytes / 16) cp_async16(slot + 1024, sets);
+            }
+            unit += 1024;
+            sets += W::kSetBytes;
             if (W::kRingCols) {
 #pragma unroll
                 for (int nt = 0; nt < TILES; ++nt) {
-                    if (cols && nt < tiles) cp_async16_l1(smem_addr(slot) + 1024 + nt * 512 + lane * 16, from[nt]);
+                    if (cols && nt < tiles) cp_async16_l1(slot + 1024 + nt * 512, from[nt]);
                     from[nt] += W::kUnitCols;
                 }
             }
-            run.unit += 1024;
-            run.sets += W::kSetBytes;
-            --run.left;
-            ++x;
         }
         cp_commit();
     }
@@ -539,13 +550,12 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
     constexpr int kDepth = depth<W, TILES>(), kCols = 8 * TILES;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int cpt = STEP == 1 ? a.cpt : kActCols, width = STEP == 1 ? kCap : a.T;
-    unsigned char* ring = smem + warp * kDepth * a.slot_bytes;
+    unsigned char *ring = smem + warp * kDepth * a.slot_bytes, *ring_end = ring + kDepth * a.slot_bytes, *at = ring;
     float* scr = reinterpret_cast<float*>(smem + a.scr_off) + warp * 16 * kCols;
     float* park = reinterpret_cast<float*>(smem + a.park_off);
     float* my_parts = a.parts + (int64_t)blockIdx.x * 2 * 16 * width;
     // the strips that the CTA's ends divide: its first and its last (one, if it has only one)
     const bool cut_first = s.strips && s.x0 > 0, cut_last = s.strips && s.x1 < s.strips * s.nv;
-    int slot = 0;
     for (int round = 0; round < s.rounds; ++round) {
         const int ls0 = round * a.round, rs = min(a.round, s.strips - ls0);
         int x, stop, strip = -1, tiles = 1;
@@ -574,36 +584,37 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
                 from[nt] += W::kUnitCols;
             }
         };
-        for (; x < stop; ++x) {
-            if (run.left == 0) {
-                locate<W, STEP>(a, L, s, x, stop, run);
-                entry = L.entry[run.entry];
-                tiles = TILES == 1 ? 1 : (entry.z * cpt + 7) / 8;
-                if (!W::kRingCols) {
-                    run_columns<W, STEP, TILES>(a, L, run, lane, from);
-                    read_columns();
-                }
-                if (STEP == 2 && run.ls != strip) {            // a new strip's sums of this warp
-                    strip = run.ls;
-                    for (int i = lane; i < 16 * width; i += 32) park[(warp + strip - ls0) * 16 * width + i] = 0.0f;
-                }
+        while (x < stop) {
+            locate<W, STEP>(a, L, s, x, stop, run);
+            x += run.left;
+            entry = L.entry[run.entry];
+            tiles = TILES == 1 ? 1 : (entry.z * cpt + 7) / 8;
+            if (!W::kRingCols) {
+                run_columns<W, STEP, TILES>(a, L, run, lane, from);
+                read_columns();
             }
-            cp_wait<kDepth - 1>();
-            __syncwarp();
-            unsigned char* at = ring + slot * a.slot_bytes;
-            if (W::kRingCols) {
+            if (STEP == 2 && run.ls != strip) {                // a new strip's sums of this warp
+                strip = run.ls;
+                for (int i = lane; i < 16 * width; i += 32) park[(warp + strip - ls0) * 16 * width + i] = 0.0f;
+            }
+            do {
+                cp_wait<kDepth - 1>();
+                if (!W::kRingCols) __syncwarp();               // sets are read by other lanes than copied them; nothing else is
+                if (W::kRingCols) {
 #pragma unroll
-                for (int nt = 0; nt < TILES; ++nt)
-                    if (nt < tiles) xr[nt][0] = *reinterpret_cast<const uint4*>(at + 1024 + nt * 512 + lane * 16);
-            }
-            if (TILES == 1 || tiles == 1) W::template unit<1>(reinterpret_cast<float(&)[1][4]>(tot), at, lane, a.bf16_scales != 0, xr);
-            else W::template unit<TILES>(tot, at, lane, a.bf16_scales != 0, xr);
-            --run.left;
-            if (!W::kRingCols && run.left) read_columns();     // in flight while the other warps compute
-            __syncwarp();
-            f.next(a, L, s, warp, lane, at, true, true);
-            if (++slot == kDepth) slot = 0;
-            if (run.left == 0) {
+                    for (int nt = 0; nt < TILES; ++nt)
+                        if (nt < tiles) xr[nt][0] = *reinterpret_cast<const uint4*>(at + 1024 + nt * 512 + lane * 16);
+                }
+                if (TILES == 1 || tiles == 1) W::template unit<1>(reinterpret_cast<float(&)[1][4]>(tot), at, lane, a.bf16_scales != 0, xr);
+                else W::template unit<TILES>(tot, at, lane, a.bf16_scales != 0, xr);
+                --run.left;
+                if (!W::kRingCols && run.left) read_columns();     // in flight while the other warps compute
+                if (!W::kRingCols) __syncwarp();
+                f.next(a, L, s, warp, lane, smem_addr(at) + lane * 16, true, true);
+                at += a.slot_bytes;
+                if (at == ring_end) at = ring;
+            } while (run.left);
+            {
                 // add a token's columns and park the sums: piece (warp, strip) has slot warp + strip
 #pragma unroll
                 for (int nt = 0; nt < TILES; ++nt)
@@ -741,7 +752,7 @@ template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe
     bool ok = grid_wait(a.sync, a.sync + 3, a.polls, &flag);
     if (ok) {
         const int entries = route(a, L);
-        unsigned char* ring = smem + warp * kDepth * a.slot_bytes;
+        const uint32_t ring = smem_addr(smem) + warp * kDepth * a.slot_bytes + lane * 16;
         {
             const Span s = span_of(entries * a.strips1, a.kb1, a.round);
             Fetcher<W, 1, TILES> f;
