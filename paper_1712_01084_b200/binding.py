@@ -649,39 +649,45 @@ def pp_pivot_find(abs_w, levels: int, max_sweeps: int = 32, row_init=None, col_i
 
 
 # ------------------------------------------------------------ decoder operators
-_TYPES = None       # torch dtype -> pp_dtype_t
+# These calls are a few microseconds on the GPU, so what the host does per call counts: torch and the library are looked
+# up once, and every check is one attribute of the tensor.
+_torch = None
+_TYPES = {}         # torch dtype -> pp_dtype_t
+
+
+def _load_torch():
+    global _torch
+    import torch
+    _TYPES.update({torch.float32: PP_F32, torch.float16: PP_F16, torch.bfloat16: PP_BF16, torch.int8: PP_I8,
+                   torch.float8_e4m3fn: PP_E4M3})
+    _torch = torch
+    lib()
+    return torch
 
 
 def _type_of(dtype, name="tensor") -> int:
-    global _TYPES
-    if _TYPES is None:
-        import torch
-        _TYPES = {torch.float32: PP_F32, torch.float16: PP_F16, torch.bfloat16: PP_BF16, torch.int8: PP_I8,
-                  torch.float8_e4m3fn: PP_E4M3}
-    try:
-        return _TYPES[dtype]
-    except KeyError:
-        raise TypeError(f"{name}: {dtype} is no type of the library") from None
+    t = _TYPES.get(dtype)
+    if t is None:
+        raise TypeError(f"{name}: {dtype} is no type of the library")
+    return t
 
 
 def _raw_stream(device: int, stream=None) -> int:
     """Handle of the stream to enqueue on: the given one, or the current one of a device."""
-    import torch
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    return _torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
-def _rows(x, cols, name, device=None):
+def _rows(x, cols, name, device):
     """(rows, distance of rows) of a CUDA matrix [rows][cols] whose rows are contiguous; a vector is one row."""
-    if not x.is_cuda or (device is not None and x.get_device() != device):
-        raise ValueError(f"{name} must be a CUDA tensor" + ("" if device is None else f" on device {device}"))
-    if x.dim() == 1:
-        if x.shape[0] != cols or (cols > 1 and x.stride(0) != 1):
-            raise ValueError(f"{name} must be [rows][{cols}] with contiguous rows")
-        return 1, cols
-    if x.dim() != 2 or x.shape[1] != cols or (cols > 1 and x.stride(1) != 1):
-        raise ValueError(f"{name} must be [rows][{cols}] with contiguous rows")
-    rows = x.shape[0]
-    return rows, (x.stride(0) if rows > 1 else cols)
+    if x.get_device() != device or device < 0:
+        raise ValueError(f"{name} must be a CUDA tensor" + ("" if device < 0 else f" on device {device}"))
+    shape = x.shape
+    if shape[-1] == cols and len(shape) <= 2:
+        if x.is_contiguous():
+            return (shape[0] if len(shape) == 2 else 1), cols
+        if len(shape) == 2 and (cols == 1 or x.stride(1) == 1):
+            return shape[0], (x.stride(0) if shape[0] > 1 else cols)
+    raise ValueError(f"{name} must be [rows][{cols}] with contiguous rows")
 
 
 def _plain(t, shape, name, device, dtypes=None):
@@ -701,33 +707,42 @@ def pp_rmsnorm_q8(x, weight, residual=None, eps: float = 1e-6, codes: str = "e4m
     "e4m3" or "int8"; group 0 (a scale per row) or 128 columns.  Returns (codes, scales, hidden), with the normalised
     rows in x's type as a fourth where `normed` is set.  hidden is x + residual in x's type: a new tensor, or hidden_out
     (which may be residual or x); without a residual it is None unless hidden_out is given."""
-    import torch
-    cols = x.shape[-1]
-    rows, ldx = _rows(x, cols, "x")
-    device, dt = x.get_device(), _type_of(x.dtype, "x")
-    _plain(weight, (cols,), "weight", device)
-    wt = _type_of(weight.dtype, "weight")
-    if codes not in ("e4m3", "int8"):
+    torch = _torch or _load_torch()
+    shape = x.shape
+    cols, device, dtype = shape[-1], x.get_device(), x.dtype
+    rows, ldx = _rows(x, cols, "x", device)
+    dt, wdt = _TYPES.get(dtype), _TYPES.get(weight.dtype)
+    if dt is None or wdt is None:
+        raise TypeError(f"x, weight: {dtype}, {weight.dtype} are no types of the library")
+    if weight.get_device() != device or weight.numel() != cols or not weight.is_contiguous():
+        raise ValueError(f"weight must be a contiguous CUDA tensor [{cols}] on device {device}")
+    if codes == "e4m3":
+        code, q = PP_E4M3, x.new_empty(shape, dtype=torch.float8_e4m3fn)
+    elif codes == "int8":
+        code, q = PP_I8, x.new_empty(shape, dtype=torch.int8)
+    else:
         raise ValueError("codes must be 'e4m3' or 'int8'")
-    ldr, rp = 0, None
+    ldr = ldh = 0
+    rp = hp = n = None
     if residual is not None:
-        if residual.dtype != x.dtype or residual.shape != x.shape:
+        if residual.dtype != dtype or residual.shape != shape:
             raise TypeError("residual must have x's shape and type")
         ldr, rp = _rows(residual, cols, "residual", device)[1], residual.data_ptr()
         if hidden_out is None:
-            hidden_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    ldh, hp = 0, None
-    if hidden_out is not None:
-        if hidden_out.dtype != x.dtype or hidden_out.shape != x.shape:
+            hidden_out = x.new_empty(shape)
+            ldh, hp = cols, hidden_out.data_ptr()
+    if hidden_out is not None and hp is None:
+        if hidden_out.dtype != dtype or hidden_out.shape != shape:
             raise TypeError("hidden_out must have x's shape and type")
         ldh, hp = _rows(hidden_out, cols, "hidden_out", device)[1], hidden_out.data_ptr()
-    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn if codes == "e4m3" else torch.int8, device=x.device)
-    scales = torch.empty(x.shape[:-1] + (-(-cols // group) if group > 0 else 1,), dtype=torch.float32, device=x.device)
-    n = torch.empty(x.shape, dtype=x.dtype, device=x.device) if normed else None
-    st = lib().pp_rmsnorm_q8(x.data_ptr(), ldx, rp, ldr, weight.data_ptr(), dt, wt, rows, cols, eps,
-                             PP_E4M3 if codes == "e4m3" else PP_I8, group, q.data_ptr(), scales.data_ptr(), hp, ldh,
-                             n.data_ptr() if normed else None, _raw_stream(device, stream))
-    _check(st, "pp_rmsnorm_q8")
+    scales = x.new_empty((*shape[:-1], -(-cols // group) if group > 0 else 1), dtype=torch.float32)
+    if normed:
+        n = x.new_empty(shape)
+    st = _lib.pp_rmsnorm_q8(x.data_ptr(), ldx, rp, ldr, weight.data_ptr(), dt, wdt, rows, cols, eps, code, group, q.data_ptr(),
+                            scales.data_ptr(), hp, ldh, n.data_ptr() if normed else None,
+                            torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
+    if st:
+        raise PPError(st, "pp_rmsnorm_q8")
     return (q, scales, hidden_out, n) if normed else (q, scales, hidden_out)
 
 
@@ -738,7 +753,7 @@ class Q4Layer:
     zeros uint8 like scales, or None (every zero point is 8); bias float32 [M] or None.  group 0: one scale per row."""
 
     def __init__(self, M, N, group, codes, scales, zeros=None, bias=None, stream=None):
-        import torch
+        torch = _torch or _load_torch()
         M, N, group = int(M), int(N), int(group)
         groups = -(-N // group) if group > 0 else 1
         device = codes.get_device() if codes.is_cuda else -1
@@ -781,24 +796,33 @@ def pp_q4_forward(layer: Q4Layer, x, act: int = PP_ACT_IDENTITY, x_scales=None, 
     """y[batch][M] = act(W x + b) with 4-bit weights.  x: [batch][N] (or [N]) float32, float16, bfloat16, or int8 /
     float8_e4m3fn with x_scales, float32 [batch][1] or [batch][ceil(N/128)], as pp_rmsnorm_q8 returns them.  y is
     float32 unless out_dtype (or out) says float16 or bfloat16.  Enqueues on the current stream."""
-    import torch
-    batch, ldx = _rows(x, layer.N, "x", layer.device)
+    torch = _torch
+    device = layer.device
+    batch, ldx = _rows(x, layer.N, "x", device)
     x_group, sp = 0, None
     if x_scales is not None:
-        n = x_scales.numel() // max(batch, 1)
-        groups = -(-layer.N // 128)
-        if n not in (1, groups) or x_scales.numel() != n * batch:
+        n, groups = x_scales.numel(), -(-layer.N // 128)
+        if n == batch:
+            x_group = 0
+        elif n == batch * groups:
+            x_group = 128
+        else:
             raise ValueError(f"x_scales must hold 1 or {groups} values per row of x")
-        _plain(x_scales, x_scales.shape, "x_scales", layer.device, (torch.float32,))
-        x_group, sp = (0 if n == 1 else 128), x_scales.data_ptr()
+        if x_scales.get_device() != device or not x_scales.is_contiguous() or x_scales.dtype != torch.float32:
+            raise ValueError("x_scales must be a contiguous float32 CUDA tensor on the layer's device")
+        sp = x_scales.data_ptr()
     if out is None:
-        out = torch.empty((batch, layer.M), dtype=out_dtype or torch.float32, device=x.device)
-    elif (not out.is_cuda or out.get_device() != layer.device or not out.is_contiguous() or out.numel() != batch * layer.M or
+        out = x.new_empty((batch, layer.M), dtype=out_dtype or torch.float32)
+    elif (out.get_device() != device or not out.is_contiguous() or out.numel() != batch * layer.M or
           (out_dtype is not None and out.dtype != out_dtype)):
         raise ValueError("out must be a contiguous CUDA tensor [batch][M] of out_dtype")
-    st = lib().pp_q4_forward(layer._h, x.data_ptr(), ldx, _type_of(x.dtype, "x"), sp, x_group, out.data_ptr(),
-                             _type_of(out.dtype, "out"), batch, int(act), _raw_stream(layer.device, stream))
-    _check(st, "pp_q4_forward")
+    xt, yt = _TYPES.get(x.dtype), _TYPES.get(out.dtype)
+    if xt is None or yt is None:
+        raise TypeError(f"x, out: {x.dtype}, {out.dtype} are no types of the library")
+    st = _lib.pp_q4_forward(layer._h, x.data_ptr(), ldx, xt, sp, x_group, out.data_ptr(), yt, batch, act,
+                            torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
+    if st:
+        raise PPError(st, "pp_q4_forward")
     return out
 
 
@@ -809,7 +833,7 @@ class MoELayer:
     MoELayer.q4 takes the experts as 4-bit codes with scales (pp_moe_create_q4)."""
 
     def __init__(self, router, gate_up, down, *, inner: int, top_k: int, max_tokens: int, renormalize: bool = True, stream=None):
-        import torch
+        torch = _torch or _load_torch()
         E, H, device = self._router(router)
         two = (torch.float16, torch.bfloat16)
         _plain(gate_up, (E, 2 * inner, H), "gate_up", device, two)
@@ -824,7 +848,7 @@ class MoELayer:
     def q4(cls, router, gate_up_codes, gate_up_scales, down_codes, down_scales, gate_up_zeros=None, down_zeros=None, *, group: int,
            inner: int, top_k: int, max_tokens: int, renormalize: bool = True, stream=None) -> "MoELayer":
         """Experts in 4 bits: codes uint8 [E][rows][ceil(cols/2)], scales float16 or bfloat16 and zeros uint8 [E][rows][groups]."""
-        import torch
+        torch = _torch or _load_torch()
         self = object.__new__(cls)
         E, H, device = self._router(router)
         group, inner = int(group), int(inner)
@@ -885,19 +909,24 @@ def pp_moe_forward(layer: MoELayer, x, out_dtype=None, out=None, routing: bool =
     """y[tokens][H] of a mixture-of-experts layer (pp_moe_forward).  x: [tokens][H] (or [H]) float32, float16 or bfloat16;
     y in x's type unless out_dtype (or out) says another.  routing: also returns the chosen experts, int32 [tokens][top_k],
     and their weights, float32.  Enqueues on the current stream."""
-    import torch
-    tokens, ldx = _rows(x, layer.H, "x", layer.device)
+    torch = _torch
+    device = layer.device
+    tokens, ldx = _rows(x, layer.H, "x", device)
     if out is None:
-        out = torch.empty((tokens, layer.H), dtype=out_dtype or x.dtype, device=x.device)
-    elif (not out.is_cuda or out.get_device() != layer.device or not out.is_contiguous() or out.numel() != tokens * layer.H or
+        out = x.new_empty((tokens, layer.H), dtype=out_dtype or x.dtype)
+    elif (out.get_device() != device or not out.is_contiguous() or out.numel() != tokens * layer.H or
           (out_dtype is not None and out.dtype != out_dtype)):
         raise ValueError("out must be a contiguous CUDA tensor [tokens][H] of out_dtype")
     ids = gates = None
     if routing:
-        ids = torch.empty((tokens, layer.top_k), dtype=torch.int32, device=x.device)
-        gates = torch.empty((tokens, layer.top_k), dtype=torch.float32, device=x.device)
-    st = lib().pp_moe_forward(layer._h, x.data_ptr(), ldx, _type_of(x.dtype, "x"), out.data_ptr(), _type_of(out.dtype, "out"), tokens,
-                              None if ids is None else ids.data_ptr(), None if gates is None else gates.data_ptr(),
-                              _raw_stream(layer.device, stream))
-    _check(st, "pp_moe_forward")
+        ids = x.new_empty((tokens, layer.top_k), dtype=torch.int32)
+        gates = x.new_empty((tokens, layer.top_k), dtype=torch.float32)
+    xt, yt = _TYPES.get(x.dtype), _TYPES.get(out.dtype)
+    if xt is None or yt is None:
+        raise TypeError(f"x, out: {x.dtype}, {out.dtype} are no types of the library")
+    st = _lib.pp_moe_forward(layer._h, x.data_ptr(), ldx, xt, out.data_ptr(), yt, tokens, ids.data_ptr() if routing else None,
+                             gates.data_ptr() if routing else None,
+                             torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
+    if st:
+        raise PPError(st, "pp_moe_forward")
     return (out, ids, gates) if routing else out

@@ -64,8 +64,16 @@ template <typename T, int N> __device__ __forceinline__ void load_vec(float (&f)
 }
 template <typename T, int N> __device__ __forceinline__ void store_vec(T* p, const float (&f)[N]) {
     Pack<T, N> u;
+    if constexpr (std::is_same_v<T, float>) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) u.v[i] = from_float<T>(f[i]);
+        for (int i = 0; i < N; ++i) u.v[i] = f[i];
+    } else {                                                 // two conversions in one instruction
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            if constexpr (std::is_same_v<T, __half>) *reinterpret_cast<__half2*>(u.v + i) = __floats2half2_rn(f[i], f[i + 1]);
+            else *reinterpret_cast<__nv_bfloat162*>(u.v + i) = __floats2bfloat162_rn(f[i], f[i + 1]);
+        }
+    }
     *reinterpret_cast<Pack<T, N>*>(p) = u;
 }
 #endif

@@ -66,6 +66,25 @@ def test_norm_matches_definition(dtype, codes, group, rows, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("codes,group", [("e4m3", 0), ("int8", 128)])
+@pytest.mark.parametrize("rows,cols", [(1300, 8192), (2500, 4096), (9600, 136), (1190, 10240), (5000, 1000)])
+def test_norm_many_rows(dtype, codes, group, rows, cols):
+    g, t = _gen(rows + cols), TYPES[dtype]
+    big = torch.randn(2, rows, cols + 8, generator=g, device="cuda").to(t)
+    x, r = big[0, :, :cols], big[1, :, 8:]
+    w = (1 + 0.3 * torch.randn(cols, generator=g, device="cuda")).to(t)
+    keep = r.clone()
+    got = pb.pp_rmsnorm_q8(x, w, residual=r, eps=1e-5, codes=codes, group=group, hidden_out=r, normed=True)
+    _check_norm(x, keep, w, 1e-5, codes, group, (got[0], got[1], got[2].clone()))
+    n = _norm64(x, keep, w, 1e-5, 1.0, group)[1]                             # among millions of values some are f16 subnormals,
+    least = 2.0 ** -25 if dtype == "f16" else 0.0                            # whose rounding is up to half of 2^-24
+    assert bool(((got[3].double() - n).abs() <= n.abs() * (ROUND[t] + 6e-6) + least).all())
+    q, s, _ = pb.pp_rmsnorm_q8(x, w, eps=1e-5, codes=codes, group=group)     # without a residual
+    _check_norm(x, None, w, 1e-5, codes, group, (q, s, None))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("cols,off", [(1024, 0), (1024, 3), (1001, 1), (512, 8)])
 @pytest.mark.parametrize("in_place", ["residual", "x"])
 def test_norm_strided_rows_in_place(cols, off, in_place):
