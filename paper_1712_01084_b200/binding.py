@@ -679,15 +679,15 @@ def _raw_stream(device: int, stream=None) -> int:
 
 def _rows(x, cols, name, device):
     """(rows, distance of rows) of a CUDA matrix [rows][cols] whose rows are contiguous; a vector is one row."""
-    if x.get_device() != device or device < 0:
-        raise ValueError(f"{name} must be a CUDA tensor" + ("" if device < 0 else f" on device {device}"))
     shape = x.shape
-    if shape[-1] == cols and len(shape) <= 2:
+    if len(shape) == 2 and shape[1] == cols and x.get_device() == device >= 0:
         if x.is_contiguous():
-            return (shape[0] if len(shape) == 2 else 1), cols
-        if len(shape) == 2 and (cols == 1 or x.stride(1) == 1):
+            return shape[0], cols
+        if cols == 1 or x.stride(1) == 1:
             return shape[0], (x.stride(0) if shape[0] > 1 else cols)
-    raise ValueError(f"{name} must be [rows][{cols}] with contiguous rows")
+    elif len(shape) == 1 and shape[0] == cols and x.get_device() == device >= 0 and x.is_contiguous():
+        return 1, cols
+    raise ValueError(f"{name} must be a CUDA tensor [rows][{cols}] with contiguous rows" + ("" if device < 0 else f" on device {device}"))
 
 
 def _plain(t, shape, name, device, dtypes=None):
@@ -708,8 +708,9 @@ def pp_rmsnorm_q8(x, weight, residual=None, eps: float = 1e-6, codes: str = "e4m
     rows in x's type as a fourth where `normed` is set.  hidden is x + residual in x's type: a new tensor, or hidden_out
     (which may be residual or x); without a residual it is None unless hidden_out is given."""
     torch = _torch or _load_torch()
-    shape = x.shape
-    cols, device, dtype = shape[-1], x.get_device(), x.dtype
+    shape, device, dtype = x.shape, x.get_device(), x.dtype
+    cols = shape[-1]
+    plain = x.is_contiguous()
     rows, ldx = _rows(x, cols, "x", device)
     dt, wdt = _TYPES.get(dtype), _TYPES.get(weight.dtype)
     if dt is None or wdt is None:
@@ -717,29 +718,33 @@ def pp_rmsnorm_q8(x, weight, residual=None, eps: float = 1e-6, codes: str = "e4m
     if weight.get_device() != device or weight.numel() != cols or not weight.is_contiguous():
         raise ValueError(f"weight must be a contiguous CUDA tensor [{cols}] on device {device}")
     if codes == "e4m3":
-        code, q = PP_E4M3, x.new_empty(shape, dtype=torch.float8_e4m3fn)
+        code, code_dtype = PP_E4M3, torch.float8_e4m3fn
     elif codes == "int8":
-        code, q = PP_I8, x.new_empty(shape, dtype=torch.int8)
+        code, code_dtype = PP_I8, torch.int8
     else:
         raise ValueError("codes must be 'e4m3' or 'int8'")
+    like = x if plain else x.new_empty(shape)                # empty_like of a contiguous tensor takes the least time
+    q = torch.empty_like(like, dtype=code_dtype)
     ldr = ldh = 0
-    rp = hp = n = None
+    rp = hp = np_ = n = None
     if residual is not None:
         if residual.dtype != dtype or residual.shape != shape:
             raise TypeError("residual must have x's shape and type")
         ldr, rp = _rows(residual, cols, "residual", device)[1], residual.data_ptr()
         if hidden_out is None:
-            hidden_out = x.new_empty(shape)
+            hidden_out = torch.empty_like(like)
             ldh, hp = cols, hidden_out.data_ptr()
     if hidden_out is not None and hp is None:
         if hidden_out.dtype != dtype or hidden_out.shape != shape:
             raise TypeError("hidden_out must have x's shape and type")
         ldh, hp = _rows(hidden_out, cols, "hidden_out", device)[1], hidden_out.data_ptr()
-    scales = x.new_empty((*shape[:-1], -(-cols // group) if group > 0 else 1), dtype=torch.float32)
+    groups = -(-cols // group) if group > 0 else 1
+    scales = x.new_empty((rows, groups) if len(shape) == 2 else (groups,), dtype=torch.float32)
     if normed:
-        n = x.new_empty(shape)
+        n = torch.empty_like(like)
+        np_ = n.data_ptr()
     st = _lib.pp_rmsnorm_q8(x.data_ptr(), ldx, rp, ldr, weight.data_ptr(), dt, wdt, rows, cols, eps, code, group, q.data_ptr(),
-                            scales.data_ptr(), hp, ldh, n.data_ptr() if normed else None,
+                            scales.data_ptr(), hp, ldh, np_,
                             torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
     if st:
         raise PPError(st, "pp_rmsnorm_q8")

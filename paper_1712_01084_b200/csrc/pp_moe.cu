@@ -106,7 +106,7 @@ template <int SETS, bool ASYM> struct Q4 {
     static constexpr bool kRingCols = false;                  // 2 KB a tile, twice the weights: no room in the ring
     template <int NT>
     static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool bf16_scales, const uint4 (*x)[kLoads]) {
-        q4_unit_f16<NT, SETS, ASYM>(tot, slot, lane, bf16_scales, [&](int nt, int j) { return x[nt][j]; });
+        q4_unit_f16<NT, SETS, ASYM>(tot, slot, lane, bf16_scales, [&](int nt, int j) { return x[nt][j]; }, [](int) { return make_float2(1.0f, 1.0f); });
     }
 };
 
@@ -177,15 +177,6 @@ template <bool BF16, typename T> __host__ __device__ constexpr int columns() {
     return std::is_same_v<T, float> ? (BF16 ? 3 : 2) : BF16 && std::is_same_v<T, __half> ? 2 : 1;
 }
 
-// The power of two that brings a magnitude `most` to [2^13, 2^14), and its inverse; below 2^-113 the largest factor whose
-// inverse is a normal number, infinities stay as they are.
-__device__ __forceinline__ void token_scale(float most, float& up, float& down) {
-    uint32_t e = __float_as_uint(most) >> 23;
-    e = e >= 255u ? 140u : e < 14u ? 14u : e;
-    up = __uint_as_float((267u - e) << 23);
-    down = __uint_as_float((e - 13u) << 23);
-}
-
 // ---- step 0 ------------------------------------------------------------------------------------------------------
 // One CTA turns a token into columns.
 template <class W, typename T, bool VEC> __device__ __forceinline__ void token_columns(const MoeArgs& a, int token, float* part) {
@@ -209,7 +200,7 @@ template <class W, typename T, bool VEC> __device__ __forceinline__ void token_c
         most = part[threadIdx.x & (kWarps - 1)];
 #pragma unroll
         for (int o = kWarps / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        token_scale(most, up, down);
+        f16_scale(most, up, down);
     }
     uint16_t* dst = a.xcols + (int64_t)token * cpt * a.kpad1;
 #pragma unroll 2

@@ -8,15 +8,18 @@
 // wait for the previous kernel (weights are never written by a kernel).  Partial sums meet in shared memory, those of
 // the other CTAs arrive there through the cluster's distributed shared memory; all are added in one fixed order.
 //
-// The products are the integer tensor-core instruction's (16 x 8 x 32, 8-bit operands, exact sums): the codes need one
-// mask instruction per four weights, where binary16 operands needed 4.5 (8192 x 8192, one vector: the multiply phase then
-// took 13,000 cycles, bound by instruction issue).  x becomes fixed point: each block of 128 columns of a vector is
-// multiplied by a power of two that brings its largest magnitude to (2^22, 0.996 * 2^23], rounded to whole numbers, and
-// written as three signed bytes, one column of the product each: an error of at most 2^-23 of the block's largest
-// element, as small as that of an fp32 sum.  Eight columns cost what one costs, so for one and two vectors the extra
-// columns are free.  8-bit integers are one column, e4m3 values times 2^9 whole numbers of three bytes; both are exact.
+// Products, one or two vectors (eight of 8-bit integers): the integer tensor-core instruction (16 x 8 x 32, 8-bit operands,
+// exact sums).  The codes need one mask instruction per four weights, where binary16 operands need 4.5.  x becomes fixed
+// point: each block of 128 columns of a vector is multiplied by a power of two that brings its largest magnitude to
+// (2^22, 0.996 * 2^23], rounded to whole numbers, and written as three signed bytes, one column of the product each: an
+// error of at most 2^-23 of the block's largest element, as small as that of an fp32 sum.  Eight columns cost what one
+// costs, so the extra columns are free.  8-bit integers are one column, e4m3 values times 2^9 whole numbers of three
+// bytes; both are exact.
 //   sum (q - z) d = sum q d - z sum d  over each set of scales, in exact integers (sum d is made while x is staged and
 // the product starts from -z sum d); then one fp32 multiply-add per set with (scale of the row) * (scale of the column).
+// More vectors: binary16 products (16 x 8 x 16, fp32 sums), where a vector takes one column, an f32 vector two (the second
+// holds what the first one's 11 bits leave over); bf16 and f32 blocks of 128 columns are brought to [2^13, 2^14) by a power
+// of two first.  Eight vectors would be 24 columns of bytes.
 #include "pp_q4.cuh"
 
 #include <algorithm>
@@ -33,15 +36,16 @@ struct pp_q4 {
 namespace pp {
 namespace {
 
-constexpr int kWarps = 16, kThreads = kWarps * 32, kMaxStrips = 64, kMaxCols = 48;
+constexpr int kWarps = 16, kThreads = kWarps * 32, kMaxStrips = 64, kMaxTokens = 16;
 constexpr int kParkLd = 20;           // floats between parked columns of 16 rows: a warp's 32 values hit 32 banks
-// Units each warp keeps in flight: 4 (70 KB an SM) keep HBM busy; with 48 columns staged there is room for 3.
-__host__ __device__ constexpr int depth_of(int nt) { return nt == 6 ? 3 : nt == 1 ? 5 : 4; }
+// Units each warp keeps in flight: 4 (70 KB an SM) keep HBM busy.  With one tile of columns a fifth still lets two CTAs share
+// an SM, so that the next call's first units are on their way during this one's end; with 32 columns there is room for 3.
+__host__ __device__ constexpr int depth_of(int nt) { return nt == 4 ? 3 : nt == 1 ? 5 : 4; }
 // Columns of the product a vector takes.
-__host__ __device__ constexpr int columns_of(int xtype) { return xtype == PP_I8 ? 1 : 3; }
-// Tiles of 8 columns: one for up to 8 columns (two vectors of three bytes); else vectors of three bytes take three tiles
-// for eight of them, one tile to a byte, so that a lane holds all three sums of its results.
-int tiles_of(int tokens, int cpt) { return tokens * cpt <= 8 ? 1 : cpt == 3 ? (tokens <= 8 ? 3 : 6) : tokens <= 16 ? 2 : 6; }
+__host__ __device__ constexpr int columns_of(bool bytes, int xtype) { return bytes ? (xtype == PP_I8 ? 1 : 3) : xtype == PP_F32 ? 2 : 1; }
+bool as_bytes(int tokens, int xtype) { return tokens * columns_of(true, xtype) <= 8; }
+// (16 vectors to a launch: 32 of bf16 in one, four tiles, took 53 us, in two 40 us; 8192 x 8192)
+int tiles_of(int nc) { return nc <= 8 ? 1 : nc <= 16 ? 2 : 4; }
 
 struct Q4Args {
     const unsigned char *units, *sets;
@@ -129,19 +133,43 @@ template <typename T> __device__ __forceinline__ void fixed_point(const Pack<T, 
     three_bytes(v, w);
 }
 
-// Position of byte c of a vector among the product's NT * 8 columns (see tiles_of).
-template <int NT> __device__ __forceinline__ int column_of(int token, int c, int cpt) {
-    return NT % 3 == 0 && cpt == 3 ? ((token >> 3) * 3 + c) * 8 + (token & 7) : token * cpt + c;
+// A warp's block of 128 columns of one vector in binary16, four per lane, columns 4i + 1 and 4i + 2 exchanged; rest: what
+// f32 leaves over.  The result is the power of two to multiply with.
+template <typename T> __device__ __forceinline__ float halves(const Pack<T, 4>& x, uint2& h, uint2& rest) {
+    float f[4], down = 1.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = to_float(x.v[i]);
+    if constexpr (std::is_same_v<T, float> || std::is_same_v<T, __nv_bfloat16>) {
+        uint32_t most = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = max(most, __float_as_uint(f[i]) & 0x7fffffffu);
+        float up;
+        f16_scale(__uint_as_float(__reduce_max_sync(0xffffffffu, most)), up, down);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] *= up;
+    }
+    const __half2 a = __floats2half2_rn(f[0], f[2]), b = __floats2half2_rn(f[1], f[3]);
+    h = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+    if constexpr (std::is_same_v<T, float>) {
+        const float2 p = __half22float2(a), q = __half22float2(b);
+        const __half2 c = __floats2half2_rn(f[0] - p.x, f[2] - p.y), d = __floats2half2_rn(f[1] - q.x, f[3] - q.y);
+        rest = make_uint2(*reinterpret_cast<const uint32_t*>(&c), *reinterpret_cast<const uint32_t*>(&d));
+    }
+    return down;
 }
 
-// This CTA's columns of x, laid out [64 columns][column of the product][lane t][8 bytes of 32 columns, 8 of the next];
-// what a column stands for per block (cs), and its sum over each set of scales (sums).  Eight blocks of four elements per
-// lane (four of f32) are requested before the first is converted: a step of this loop is a trip to memory.
-template <typename T, bool VEC, int NT, int SETS>
-__device__ __forceinline__ void stage_rows(const Q4Args& a, unsigned char* xs, float* cs, int* sums, int k0, int n_k, int warp, int lane) {
-    constexpr int kAhead = !VEC ? 1 : sizeof(T) == 4 ? 4 : 8, cpt = std::is_same_v<T, int8_t> ? 1 : 3;
+// This CTA's columns of x and, per block of 128 columns, what a column stands for (cs) and its sum over each set of scales
+// (sums, bytes only).  Bytes are laid out [64 columns][column of the product][lane t][8 bytes of 32 columns, 8 of the next],
+// halves [32 columns][column of the product][lane t][8 halves]: what a lane reads at once.  Several blocks of four elements
+// per lane are requested before the first is converted, as a step of this loop is a trip to memory (two where a warp has two).
+// then(): called once the first of them are on their way.
+template <typename T, bool VEC, bool BYTES, int NT, int SETS, typename Then>
+__device__ __forceinline__ void stage_rows(const Q4Args& a, unsigned char* xs, float* cs, int* sums, int k0, int n_k, int warp, int lane, Then then) {
+    constexpr int kAhead = !VEC ? 1 : BYTES ? 2 : sizeof(T) == 4 ? 4 : 8;
+    constexpr int cpt = BYTES ? (std::is_same_v<T, int8_t> ? 1 : 3) : std::is_same_v<T, float> ? 2 : 1;
     const int items = a.tokens * n_k, step = a.nc * 64;
     const Divider by_blocks(n_k);
+    if (warp >= items) then();
     for (int base = warp; base < items; base += kAhead * kWarps) {
         Pack<T, 4> v[kAhead];
         float own[kAhead];
@@ -151,44 +179,54 @@ __device__ __forceinline__ void stage_rows(const Q4Args& a, unsigned char* xs, f
             v[q] = load_four<VEC>(static_cast<const T*>(a.in.x) + token * a.in.ld, block * kQ4UnitCols + lane * 4, a.in.cols);
             if (sizeof(T) == 1) own[q] = a.in.scales[(int64_t)token * a.in.scale_ld + (a.in.group_blocks ? block / a.in.group_blocks : 0)];
         }
+        if (base == warp) then();
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
             const int item = base + q * kWarps, token = by_blocks.div(item), kb = item - token * n_k;
             if (item >= items) break;
-            uint32_t w[3];
-            float down;
-            fixed_point(v[q], own[q], w, down);
-            unsigned char* at = xs + (kb * 2 + (lane >> 4)) * step + token * cpt * 64 + ((lane >> 1) & 3) * 16 + (lane & 8) + (lane & 1) * 4;
-            int sum[2] = {0, 0};                             // 2^16 (highest byte) + (middle byte), and the lowest
+            if constexpr (BYTES) {
+                uint32_t w[3];
+                float down;
+                fixed_point(v[q], own[q], w, down);
+                unsigned char* at = xs + (kb * 2 + (lane >> 4)) * step + token * cpt * 64 + ((lane >> 1) & 3) * 16 + (lane & 8) + (lane & 1) * 4;
+                int sum[2] = {0, 0};                         // 2^16 (highest byte) + (middle byte), and the lowest
 #pragma unroll
-            for (int c = 0; c < cpt; ++c) {
-                *reinterpret_cast<uint32_t*>(at + c * 64) = w[c];
-                sum[c == 2] += __dp4a((int)w[c], 0x01010101, 0) * (cpt == 3 && c == 0 ? 65536 : 1);
-            }
-#pragma unroll
-            for (int c = 0; c < (cpt + 1) / 2; ++c) {
-                if (SETS == 1) {
-                    sum[c] = __reduce_add_sync(0xffffffffu, sum[c]);
-                } else {
-#pragma unroll
-                    for (int o = 16 / SETS; o; o >>= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], o);
+                for (int c = 0; c < cpt; ++c) {
+                    *reinterpret_cast<uint32_t*>(at + c * 64) = w[c];
+                    sum[c == 2] += __dp4a((int)w[c], 0x01010101, 0) * (cpt == 3 && c == 0 ? 65536 : 1);
                 }
-            }
-            constexpr int kLanes = 32 / SETS;                // of a set
-            const int c = lane & (kLanes - 1);
-            if (c < cpt) {
-                const int col = column_of<NT>(token, c, cpt), middle = (int16_t)sum[0];
-                sums[(kb * SETS + lane / kLanes) * NT * 8 + col] = cpt == 1 || c == 1 ? middle : c == 0 ? (sum[0] - middle) >> 16 : sum[1];
-                if (lane < cpt) cs[kb * NT * 8 + col] = down * (cpt == 1 || c == 2 ? 1.0f : c == 1 ? 256.0f : 65536.0f);
+#pragma unroll
+                for (int c = 0; c < (cpt + 1) / 2; ++c) {
+                    if (SETS == 1) {
+                        sum[c] = __reduce_add_sync(0xffffffffu, sum[c]);
+                    } else {
+#pragma unroll
+                        for (int o = 16 / SETS; o; o >>= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], o);
+                    }
+                }
+                constexpr int kLanes = 32 / SETS;            // of a set
+                const int c = lane & (kLanes - 1);
+                if (c < cpt) {
+                    const int col = token * cpt + c, middle = (int16_t)sum[0];
+                    sums[(kb * SETS + lane / kLanes) * NT * 8 + col] = cpt == 1 || c == 1 ? middle : c == 0 ? (sum[0] - middle) >> 16 : sum[1];
+                    if (lane < cpt) cs[kb * NT * 8 + col] = down * (cpt == 1 || c == 2 ? 1.0f : c == 1 ? 256.0f : 65536.0f);
+                }
+            } else {
+                uint2 h, rest;
+                const float down = halves(v[q], h, rest);
+                unsigned char* at = xs + (kb * 4 + (lane >> 3)) * step + token * cpt * 64 + (lane & 7) * 8;
+                *reinterpret_cast<uint2*>(at) = h;
+                if (cpt == 2) *reinterpret_cast<uint2*>(at + 64) = rest;
+                if (lane < cpt) cs[kb * NT * 8 + token * cpt + lane] = sizeof(T) == 1 ? own[q] : down;
             }
         }
     }
 }
 
-template <typename T, int NT, int SETS>
-__device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, float* cs, int* sums, int k0, int n_k, int warp, int lane) {
-    if (a.in.vec) stage_rows<T, true, NT, SETS>(a, xs, cs, sums, k0, n_k, warp, lane);
-    else stage_rows<T, false, NT, SETS>(a, xs, cs, sums, k0, n_k, warp, lane);
+template <typename T, bool BYTES, int NT, int SETS, typename Then>
+__device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, float* cs, int* sums, int k0, int n_k, int warp, int lane, Then then) {
+    if (a.in.vec) stage_rows<T, true, BYTES, NT, SETS>(a, xs, cs, sums, k0, n_k, warp, lane, then);
+    else stage_rows<T, false, BYTES, NT, SETS>(a, xs, cs, sums, k0, n_k, warp, lane, then);
 }
 
 __device__ __forceinline__ void mma_u8s8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -253,7 +291,7 @@ __device__ __forceinline__ void q4_unit_i8(float (&tot)[NT][4], const unsigned c
     }
 }
 
-template <int NT, int SETS, bool ASYM>
+template <bool BYTES, int NT, int SETS, bool ASYM>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) q4_kernel(const Q4Args a) {
     extern __shared__ __align__(128) unsigned char smem[];
     constexpr int kDepth = depth_of(NT);
@@ -266,91 +304,108 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) q4_kernel(const Q4A
     pdl_release();
 
     // the first units of this warp: nothing in them depends on an earlier kernel
-    unsigned char* ring = smem + a.ring_off + warp * kDepth * a.slot_bytes;
     const int ls0 = Divider(n_k).div(u0), kb0 = u0 - ls0 * n_k;
     constexpr int kSetBytes = SETS * (ASYM ? 48 : 32);
-    uint32_t next = (uint32_t)(s0 + ls0) * (uint32_t)a.blocks + (uint32_t)(k0 + kb0);       // unit to fetch (fewer than 2^31 of them)
-    int next_kb = kb0;
-    auto fetch = [&](unsigned char* slot, bool more) {
-        if (more) {
-            unit_fetch(smem_addr(slot), a.units + (size_t)next * kQ4CodeBytes, a.sets + (size_t)next * kSetBytes, lane, kSetBytes / 16);
-            ++next;
-            if (++next_kb == n_k) next_kb = 0, next += (uint32_t)(a.blocks - n_k);
+    unsigned char *const ring = smem + a.ring_off + warp * kDepth * a.slot_bytes, *const ring_end = ring + kDepth * a.slot_bytes;
+    const int64_t at0 = (int64_t)(s0 + ls0) * a.blocks + k0 + kb0;
+    const unsigned char *unit = a.units + at0 * kQ4CodeBytes + lane * 16, *sets = a.sets + at0 * kSetBytes + lane * 16;
+    int todo = u1 - u0, run = n_k - kb0;                     // units still to request, and those of them in this strip
+    auto fetch = [&](uint32_t slot) {
+        if (todo > 0) {
+            --todo;
+            cp_async16(slot, unit);
+            cp_async16(slot + 512, unit + 512);
+            if (lane < kSetBytes / 16) cp_async16(slot + 1024, sets);
+            unit += kQ4CodeBytes;
+            sets += kSetBytes;
+            if (--run == 0) {
+                run = n_k;
+                unit += (int64_t)(a.blocks - n_k) * kQ4CodeBytes;
+                sets += (int64_t)(a.blocks - n_k) * kSetBytes;
+            }
         }
         cp_commit();
     };
+    // (with more vectors the rest of the ring is requested behind x, which it would hold back: 4096 x 9216, eight vectors,
+    // 12.6 -> 11.1 us; one vector is small and loses by it, 4096 x 4096 5.7 -> 5.9 us)
+    constexpr int kEarly = BYTES ? kDepth : 3;
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d) fetch(ring + d * a.slot_bytes, u0 + d < u1);
-    // which warps have units of each strip
+    for (int d = 0; d < kEarly; ++d) fetch(smem_addr(ring) + d * a.slot_bytes + lane * 16);
+    // which warps have units of each strip: half a warp looks at one
     uint16_t* plan = reinterpret_cast<uint16_t*>(smem + a.plan_off);
-    if (tid < n_s) {
-        uint32_t mask = 0u;
-        for (int w = 0; w < kWarps; ++w) {
-            const int lo = max(U * w / kWarps, tid * n_k), hi = min(U * (w + 1) / kWarps, (tid + 1) * n_k);
-            mask |= (lo < hi ? 1u : 0u) << w;
-        }
-        plan[tid] = (uint16_t)mask;
+    for (int base = 0; base < n_s; base += kThreads / 16) {
+        const int strip = base + (tid >> 4), w = tid & 15;
+        const bool has = strip < n_s && max(U * w / kWarps, strip * n_k) < min(U * (w + 1) / kWarps, (strip + 1) * n_k);
+        const uint32_t mask = __ballot_sync(0xffffffffu, has) >> (lane & 16);
+        if (w == 0 && strip < n_s) plan[strip] = (uint16_t)mask;
     }
 
     pdl_wait();
     float* cs = reinterpret_cast<float*>(smem + a.cs_off);
     int* sums = reinterpret_cast<int*>(smem + a.sum_off);
+    const auto rest = [&] {
+#pragma unroll
+        for (int d = kEarly; d < kDepth; ++d) fetch(smem_addr(ring) + d * a.slot_bytes + lane * 16);
+    };
     switch (a.in.type) {
-        case PP_F32: stage_x<float, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane); break;
-        case PP_F16: stage_x<__half, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane); break;
-        case PP_BF16: stage_x<__nv_bfloat16, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane); break;
-        case PP_I8: stage_x<int8_t, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane); break;
-        default: stage_x<__nv_fp8_e4m3, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane);
+        case PP_F32: stage_x<float, BYTES, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane, rest); break;
+        case PP_F16: stage_x<__half, BYTES, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane, rest); break;
+        case PP_BF16: stage_x<__nv_bfloat16, BYTES, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane, rest); break;
+        case PP_I8: stage_x<int8_t, BYTES, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane, rest); break;
+        default: stage_x<__nv_fp8_e4m3, BYTES, NT, SETS>(a, smem, cs, sums, k0, n_k, warp, lane, rest);
     }
     __syncthreads();
 
-    const bool by_byte = NT % 3 == 0 && a.nc != a.tokens;
-    const int parked = by_byte ? a.tokens : a.nc;            // columns that are parked: a vector's bytes already added, or not
-    const int step = a.nc * 64;
+    const bool paired = !BYTES && a.nc != a.tokens;          // f32 in halves: a vector's two columns are neighbours in one lane
+    const int parked = paired ? a.tokens : a.nc;             // columns that are parked
+    const int step = a.nc * 64;                              // bytes to the next 64 columns of bytes, 32 columns of halves
+    constexpr int kSteps = BYTES ? 2 : 4;                    // of a unit
     int x_lane[NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {                        // columns past the last repeat one
-        const int c = by_byte ? min(nt / 3 * 8 + g, a.tokens - 1) * 3 + nt % 3 : min(nt * 8 + g, a.nc - 1);
-        x_lane[nt] = (c * 4 + t) * 16;
-    }
+    for (int nt = 0; nt < NT; ++nt) x_lane[nt] = (min(nt * 8 + g, a.nc - 1) * 4 + t) * 16;       // columns past the last repeat it
     float* park = reinterpret_cast<float*>(smem + a.park_off);
     float tot[NT][4] = {};
-    int slot = 0, ls = ls0, kb = kb0;
-    for (int u = u0; u < u1; ++u) {
-        cp_wait<kDepth - 1>();
-        __syncwarp();
-        unsigned char* at = ring + slot * a.slot_bytes;
-        q4_unit_i8<NT, SETS, ASYM>(tot, at, lane, smem + kb * 2 * step, x_lane, step, sums + kb * SETS * NT * 8 + t * 2, cs + kb * NT * 8 + t * 2,
-                                   a.bf16_scales != 0);
-        __syncwarp();
-        fetch(at, u + kDepth < u1);
-        if (++slot == kDepth) slot = 0;
-        if (++kb == n_k || u + 1 == u1) {
-            // piece (warp, strip) parks in slot warp + strip: along the units one of the two grows at every change
-            float* p = park + (warp + ls) * kParkLd * parked + g;
-            if (by_byte) {
-#pragma unroll
-                for (int nt = 0; nt + 2 < NT; nt += 3) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int c = nt / 3 * 8 + 2 * t + (i & 1);
-                        if (c < parked) p[c * kParkLd + (i >> 1) * 8] = tot[nt][i] + (tot[nt + 1][i] + tot[nt + 2][i]);
-                    }
-                }
+    unsigned char* at = ring;
+    int ls = ls0, kb = kb0;
+    for (int left = u1 - u0; left > 0; ++ls, kb = 0) {
+        int n = min(n_k - kb, left);
+        left -= n;
+        const unsigned char* x = smem + kb * kSteps * step;
+        const int* sum = sums + kb * SETS * NT * 8 + t * 2;
+        const float* c = cs + kb * NT * 8 + t * 2;
+        do {
+            cp_wait<kDepth - 1>();
+            __syncwarp();
+            if constexpr (BYTES) {
+                q4_unit_i8<NT, SETS, ASYM>(tot, at, lane, x, x_lane, step, sum, c, a.bf16_scales != 0);
             } else {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int c = nt * 8 + 2 * t + (i & 1);
-                        if (c < parked) p[c * kParkLd + (i >> 1) * 8] = tot[nt][i];
-                    }
-                }
+                q4_unit_f16<NT, SETS, ASYM>(tot, at, lane, a.bf16_scales != 0,
+                                            [&](int nt, int j) { return *reinterpret_cast<const uint4*>(x + j * step + x_lane[nt]); },
+                                            [&](int nt) { return *reinterpret_cast<const float2*>(c + nt * 8); });
             }
+            __syncwarp();
+            fetch(smem_addr(at) + lane * 16);
+            at += a.slot_bytes;
+            if (at == ring_end) at = ring;
+            x += kSteps * step;
+            sum += SETS * NT * 8;
+            c += NT * 8;
+        } while (--n);
+        // piece (warp, strip) parks in slot warp + strip: along the units one of the two grows at every change
+        float* p = park + (warp + ls) * kParkLd * parked + g;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) tot[nt][0] = tot[nt][1] = tot[nt][2] = tot[nt][3] = 0.0f;
-            kb = 0;
-            ++ls;
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int col = nt * 8 + 2 * t;
+                if (paired) {
+                    if (col < a.nc) p[col / 2 * kParkLd + h * 8] = tot[nt][2 * h] + tot[nt][2 * h + 1];
+                } else {
+                    if (col < parked) p[col * kParkLd + h * 8] = tot[nt][2 * h];
+                    if (col + 1 < parked) p[(col + 1) * kParkLd + h * 8] = tot[nt][2 * h + 1];
+                }
+                tot[nt][2 * h] = tot[nt][2 * h + 1] = 0.0f;
+            }
         }
     }
     cp_wait<0>();
@@ -398,30 +453,31 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) q4_kernel(const Q4A
 }
 
 using Kernel = void (*)(const Q4Args);
-template <int NT, int SETS> Kernel pick_asym(bool asym) { return asym ? q4_kernel<NT, SETS, true> : q4_kernel<NT, SETS, false>; }
-template <int NT> Kernel pick_sets(int sets, bool asym) {
-    return sets == 4 ? pick_asym<NT, 4>(asym) : sets == 2 ? pick_asym<NT, 2>(asym) : pick_asym<NT, 1>(asym);
+template <bool BYTES, int NT, int SETS> Kernel pick_asym(bool asym) { return asym ? q4_kernel<BYTES, NT, SETS, true> : q4_kernel<BYTES, NT, SETS, false>; }
+template <bool BYTES, int NT> Kernel pick_sets(int sets, bool asym) {
+    return sets == 4 ? pick_asym<BYTES, NT, 4>(asym) : sets == 2 ? pick_asym<BYTES, NT, 2>(asym) : pick_asym<BYTES, NT, 1>(asym);
 }
-Kernel pick_kernel(int nt, int sets, bool asym) {
-    return nt == 1 ? pick_sets<1>(sets, asym) : nt == 2 ? pick_sets<2>(sets, asym) : nt == 3 ? pick_sets<3>(sets, asym) : pick_sets<6>(sets, asym);
+Kernel pick_kernel(bool bytes, int nt, int sets, bool asym) {
+    return bytes ? pick_sets<true, 1>(sets, asym) : nt == 1 ? pick_sets<false, 1>(sets, asym) : nt == 2 ? pick_sets<false, 2>(sets, asym) : pick_sets<false, 4>(sets, asym);
 }
 
 constexpr int kMaxSmem = 227 * 1024;
 
 // Shared memory of a launch with clusters of S CTAs that own up to n_s strips each; fills in the offsets.
-size_t plan_smem(Q4Args& a, int sets, int S, int n_s) {
-    const int nt = tiles_of(a.tokens, a.nc / a.tokens), n_k = (a.blocks + S - 1) / S;
-    size_t at = (size_t)n_k * kQ4UnitCols * a.nc;
+size_t plan_smem(Q4Args& a, bool bytes, int sets, int S, int n_s) {
+    const int nt = tiles_of(a.nc), n_k = (a.blocks + S - 1) / S;
+    size_t at = (size_t)n_k * kQ4UnitCols * a.nc * (bytes ? 1 : 2);
     a.cs_off = (int)at;
     at += (size_t)n_k * nt * 32;
     a.sum_off = (int)at;
-    at += (size_t)n_k * sets * nt * 32;
+    if (bytes) at += (size_t)n_k * sets * nt * 32;
     a.plan_off = (int)at;
     at += (size_t)n_s * 2;
     a.ring_off = (int)(at = (at + 127) / 128 * 128);
     at += (size_t)kWarps * depth_of(nt) * a.slot_bytes;
     a.park_off = (int)at;
-    at += (size_t)(n_s + kWarps) * kParkLd * (nt % 3 == 0 ? a.tokens : a.nc) * 4;
+    const bool paired = !bytes && a.nc != a.tokens;
+    at += (size_t)(n_s + kWarps) * kParkLd * (paired ? a.tokens : a.nc) * 4;
     a.red_off = (int)at;
     const size_t outs = (size_t)n_s * 16 * a.tokens;
     at += (outs + S - 1) / S * S * 4;
@@ -526,8 +582,8 @@ extern "C" pp_status_t pp_q4_create(pp_q4_t** out, int M, int N, int group, cons
     if (st == PP_OK && (launch_q4_pack(L->units, L->sets_at, codes, scales, zeros, 1, M, N, group, false, s) != cudaSuccess ||
                         (bias && cudaMemcpyAsync(L->bias, bias, (size_t)M * 4, cudaMemcpyDeviceToDevice, s) != cudaSuccess) ||
                         cudaStreamSynchronize(s) != cudaSuccess)) st = PP_ERR_CUDA;
-    for (int nt : {1, 2, 3, 6})
-        if (st == PP_OK && opt_in(reinterpret_cast<const void*>(pick_kernel(nt, L->sets, L->asym))) != cudaSuccess) st = PP_ERR_CUDA;
+    for (int nt : {0, 1, 2, 4})
+        if (st == PP_OK && opt_in(reinterpret_cast<const void*>(pick_kernel(nt == 0, nt, L->sets, L->asym))) != cudaSuccess) st = PP_ERR_CUDA;
     // clusters resident at once, for a CTA of ordinary size (the GPCs hold different numbers of SMs)
     for (int S = 1; S <= 8 && st == PP_OK; S *= 2) {
         cudaLaunchAttribute at;
@@ -541,7 +597,7 @@ extern "C" pp_status_t pp_q4_create(pp_q4_t** out, int M, int N, int group, cons
         cfg.attrs = &at;
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, pick_kernel(1, L->sets, L->asym), &cfg) != cudaSuccess || n < 1) st = PP_ERR_CUDA;
+        if (cudaOccupancyMaxActiveClusters(&n, pick_kernel(true, 1, L->sets, L->asym), &cfg) != cudaSuccess || n < 1) st = PP_ERR_CUDA;
         L->max_clusters[S] = n;
     }
     if (st != PP_OK) {
@@ -583,11 +639,11 @@ extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_
     a.sets = L->sets_at;
     a.slot_bytes = kQ4CodeBytes + (q4_set_bytes(L->sets, L->asym) + 127) / 128 * 128;      // slots start on 128 bytes
     a.bf16_scales = L->bf16_scales;
-    const int cpt = columns_of(x_type);
-    int most = std::min(kMaxCols / cpt, 32);                       // tokens of one launch
+    int most = kMaxTokens;                       // tokens of one launch
     for (int b0 = 0; b0 < batch;) {
         a.tokens = std::min(batch - b0, most);
-        a.nc = a.tokens * cpt;
+        const bool bytes = as_bytes(a.tokens, x_type);
+        a.nc = a.tokens * columns_of(bytes, x_type);
         a.in.x = static_cast<const char*>(x) + (int64_t)b0 * ldx * xb;
         a.in.scales = x_scales ? x_scales + (int64_t)b0 * a.in.scale_ld : nullptr;
         a.y = static_cast<char*>(y) + (int64_t)b0 * L->M * yb;
@@ -599,7 +655,7 @@ extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_
             const int n_k = (L->blocks + S - 1) / S;
             for (int rounds = 1; rounds <= L->strips; ++rounds) {
                 const int n = std::min(L->strips, L->max_clusters[S] * rounds), n_s = (L->strips + n - 1) / n;
-                if (n_s > kMaxStrips || plan_smem(a, L->sets, S, n_s) > (size_t)kMaxSmem) {
+                if (n_s > kMaxStrips || plan_smem(a, bytes, L->sets, S, n_s) > (size_t)kMaxSmem) {
                     if (n_s == 1) break;
                     continue;
                 }
@@ -613,12 +669,12 @@ extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_
             most = a.tokens / 2;
             continue;
         }
-        const size_t smem = plan_smem(a, L->sets, best, (L->strips + best_n - 1) / best_n);
+        const size_t smem = plan_smem(a, bytes, L->sets, best, (L->strips + best_n - 1) / best_n);
         a.strips_each = L->strips / best_n;
         a.strips_more = L->strips % best_n;
         a.blocks_each = L->blocks / best;
         a.blocks_more = L->blocks % best;
-        const Kernel k = pick_kernel(tiles_of(a.tokens, cpt), L->sets, L->asym);
+        const Kernel k = pick_kernel(bytes, tiles_of(a.nc), L->sets, L->asym);
         if (launch_pdl(k, dim3(best * best_n), dim3(kThreads), smem, static_cast<cudaStream_t>(cuda_stream), best, a) != cudaSuccess)
             return PP_ERR_CUDA;
         b0 += a.tokens;

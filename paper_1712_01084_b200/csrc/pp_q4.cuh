@@ -86,11 +86,12 @@ __device__ __forceinline__ float2 q4_scales(const unsigned char* slot, int set, 
 // tot[nt] += W_unit * X for NT tiles of 8 columns of binary16.  (word & 0x000f000f) | 0x64006400 is the pair 1024 + q of
 // columns 0 and 2, adding -(1024 + z) leaves q - z exactly; four bits higher the same gives 16 (q - z), a byte further
 // columns 1 and 3.  A word of eight weights costs one shift, four logic and four add instructions; products are exact,
-// sums are fp32 and scaled once per set.  Lane (g, t) holds in tot[nt][0..3] rows g, g, g + 8, g + 8 and columns 8 nt + 2t,
-// + 1, + 0, + 1.  load_x(nt, j): elements 8t .. 8t + 7 of the j-th 32 columns of the unit, of the lane's input column
+// sums are fp32 and scaled once per set, by the row's and the column's scale.  Lane (g, t) holds in tot[nt][0..3] rows g, g,
+// g + 8, g + 8 and columns 8 nt + 2t, + 1, + 0, + 1.  col_scale(nt): those two columns' scales.  load_x(nt, j): elements 8t .. 8t + 7 of the j-th 32 columns of the unit, of the lane's input column
 // 8 nt + g, each four of them in the order 0, 2, 1, 3.
-template <int NT, int SETS, bool ASYM, typename LoadX>
-__device__ __forceinline__ void q4_unit_f16(float (&tot)[NT][4], const unsigned char* slot, int lane, bool bf16_scales, LoadX load_x) {
+template <int NT, int SETS, bool ASYM, typename LoadX, typename ColScale>
+__device__ __forceinline__ void q4_unit_f16(float (&tot)[NT][4], const unsigned char* slot, int lane, bool bf16_scales, LoadX load_x,
+                                            ColScale col_scale) {
     const int g = lane >> 2;
     float acc[NT][4];
     uint32_t z0 = 0xE408E408u, z1 = 0xE480E480u;             // -(1024 + 8), -(1024 + 16 * 8)
@@ -129,10 +130,11 @@ __device__ __forceinline__ void q4_unit_f16(float (&tot)[NT][4], const unsigned 
             const float2 s = q4_scales(slot, set, g, bf16_scales);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                tot[nt][0] = fmaf(s.x, acc[nt][0], tot[nt][0]);
-                tot[nt][1] = fmaf(s.x, acc[nt][1], tot[nt][1]);
-                tot[nt][2] = fmaf(s.y, acc[nt][2], tot[nt][2]);
-                tot[nt][3] = fmaf(s.y, acc[nt][3], tot[nt][3]);
+                const float2 c = col_scale(nt);
+                tot[nt][0] = fmaf(s.x * c.x, acc[nt][0], tot[nt][0]);
+                tot[nt][1] = fmaf(s.x * c.y, acc[nt][1], tot[nt][1]);
+                tot[nt][2] = fmaf(s.y * c.x, acc[nt][2], tot[nt][2]);
+                tot[nt][3] = fmaf(s.y * c.y, acc[nt][3], tot[nt][3]);
             }
         }
     }
@@ -162,6 +164,15 @@ template <bool VEC, typename T> __device__ __forceinline__ Pack<T, 4> load_four(
             if (col + i < cols) v.v[i] = row[col + i];
     }
     return v;
+}
+
+// The power of two that brings a magnitude `most` to [2^13, 2^14), and its inverse; below 2^-113 the largest factor whose
+// inverse is a normal number, infinities stay as they are.
+__device__ __forceinline__ void f16_scale(float most, float& up, float& down) {
+    uint32_t e = __float_as_uint(most) >> 23;
+    e = e >= 255u ? 140u : e < 14u ? 14u : e;
+    up = __uint_as_float((267u - e) << 23);
+    down = __uint_as_float((e - 13u) << 23);
 }
 
 // i / n for 0 <= i < 2^20 by the reciprocal of n: an integer division takes as long as a trip to L2.
