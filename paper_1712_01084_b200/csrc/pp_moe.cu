@@ -18,12 +18,13 @@
 // arrive, which adds the parts in the order of the CTAs.  So all sums are taken in one fixed order.
 // (Cutting at strips instead left 256 strips of 16 rows to 148 CTAs: 1.73 on average, 2 on the busiest.)
 //
-// Columns.  Products take one 16-bit type, the weights' (binary16 for 4-bit codes).  An input that has more bits than
-// one column holds is split over several: bf16 products take f16 in two and f32 in three columns; binary16 products take
-// a token times the power of two that brings its largest magnitude to [2^13, 2^14), in one column for bf16 and two for
-// f32.  act is f32 and always takes three: in bf16 these are its 24 bits; in binary16, where no scale is known before
-// all of act is, they hold act * 2^-11, the rest * 2^-1 and the rest * 2^10, which together are act to 24 bits between
-// 2^-11 and 2^27 and to an absolute 2^-35 below.
+// Columns.  Products with 16-bit weights take the weights' type.  An input that has more bits than one column holds is split
+// over several: bf16 products take f16 in two and f32 in three columns; binary16 products take a token times the power of
+// two that brings its largest magnitude to [2^13, 2^14), in one column for bf16 and two for f32.  4-bit gate and up rows are
+// multiplied as integers, with the token in fixed point as three columns of bytes (pp_q4.cu says how and why).  act is f32
+// and always takes three columns: in bf16 these are its 24 bits; in binary16 (4-bit experts too), where no scale is known
+// before all of act is, they hold act * 2^-11, the rest * 2^-1 and the rest * 2^10, which together are act to 24 bits
+// between 2^-11 and 2^27 and to an absolute 2^-35 below.
 #include "pp_q4.cuh"
 
 #include <algorithm>
@@ -41,6 +42,7 @@ struct pp_moe {
     unsigned char *gate_up, *down, *gate_up_sets, *down_sets;
     float *router, *logits, *xscale;
     uint16_t *xcols, *acols;
+    int* xmeta;
     float* parts;             // [CTA][2][16][width]: its parts of the strips that its first and last cut divide
     int* sync;                // [0], [1] arrivals at the two barriers, [2] CTAs that are done, [3] status, then arrivals at
                               // divided strips, [step][the first of the strip's CTAs]
@@ -50,7 +52,7 @@ namespace pp {
 namespace {
 
 constexpr int kWarps = 16, kThreads = kWarps * 32, kMaxCols = 16;
-constexpr int kMaxExperts = 256, kMaxTopK = 16, kMaxTokens = 32, kActCols = 3, kCap = kMaxCols / kActCols;   // tokens of an entry
+constexpr int kMaxExperts = 256, kMaxTopK = 16, kMaxTokens = 32, kActCols = 3, kMaxCap = kMaxCols / kActCols;
 constexpr int kSpinPolls = 1 << 24;          // seconds; a barrier that is met never gets near it
 
 struct MoeArgs {
@@ -59,6 +61,7 @@ struct MoeArgs {
     XIn in;
     float *logits, *xscale, *parts;
     uint16_t *xcols, *acols;
+    int* xmeta;                              // 4-bit experts: [token's column][block] {its sums over the sets, its scale}
     int* sync;
     void* y;
     int32_t* ids;
@@ -66,7 +69,9 @@ struct MoeArgs {
     int y_type, T, E, H, top_k, renorm, strips1, strips2, kb1, kb2, kpad1, kpad2, router_ld, slot_bytes, cpt, bf16_scales, polls;
     float per_expert, per_entry;             // 1 / strips1, 1 / kb2
     int round;                               // strips of a round
+    int cap;                                 // tokens of an entry, at most
     int list_off, scr_off, park_off;         // shared memory; the weight rings are at 0
+    int bytes_off;                           // 4-bit experts: where the tokens' bytes go, 0 if they stay in global memory
 };
 
 // ---- weight formats: bytes and columns of a unit, and its product with the columns a lane reads ------------------
@@ -77,40 +82,57 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint4& a, uint32_t
         : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
 
+// Cols<STEP>: what a lane holds of one tile of 8 columns for a unit.
 template <bool BF16> struct Wide {           // 16-bit weights: 16 rows x 32 columns, two operand fragments of 512 bytes
-    static constexpr int kUnitCols = 32, kSetBytes = 0, kLoads = 1;       // kLoads: 16-byte reads of a lane and column
-    static constexpr bool kBf16 = BF16, kSwap = false;
+    static constexpr int kUnitCols = 32, kSetBytes = 0;
+    static constexpr bool kBf16 = BF16, kBytes = false, kSwap = false;
     // The columns' part of a unit (512 bytes a tile) travels in the ring with the weights: read through L1 instead, the first
     // pass of a CTA over a new expert's columns took twice as long as the others, a trip to L2 per unit.
     static constexpr bool kRingCols = true;
-    template <int NT>
-    static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool, const uint4 (*x)[kLoads]) {
+    template <int STEP> struct Cols { uint4 x[1]; };
+    template <int STEP, int NT>
+    static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool, const Cols<STEP>* x) {
         const uint4 a = at<uint4>(slot + lane * 16), b = at<uint4>(slot + 512 + lane * 16);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+            const uint4 v = x[nt].x[0];
             if (BF16) {
-                mma_bf16(tot[nt], a, x[nt][0].x, x[nt][0].y);
-                mma_bf16(tot[nt], b, x[nt][0].z, x[nt][0].w);
+                mma_bf16(tot[nt], a, v.x, v.y);
+                mma_bf16(tot[nt], b, v.z, v.w);
             } else {
                 const uint32_t ar[4] = {a.x, a.y, a.z, a.w}, br[4] = {b.x, b.y, b.z, b.w};
-                mma_f16(tot[nt], ar, x[nt][0].x, x[nt][0].y);
-                mma_f16(tot[nt], br, x[nt][0].z, x[nt][0].w);
+                mma_f16(tot[nt], ar, v.x, v.y);
+                mma_f16(tot[nt], br, v.z, v.w);
             }
         }
     }
 };
 
 template <int SETS, bool ASYM> struct Q4 {
-    static constexpr int kUnitCols = kQ4UnitCols, kSetBytes = SETS * (ASYM ? 48 : 32), kLoads = 4;
-    static constexpr bool kBf16 = false, kSwap = true;        // kSwap: columns 4i + 1 and 4i + 2 of the input change places
-    static constexpr bool kRingCols = false;                  // 2 KB a tile, twice the weights: no room in the ring
-    template <int NT>
-    static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool bf16_scales, const uint4 (*x)[kLoads]) {
-        q4_unit_f16<NT, SETS, ASYM>(tot, slot, lane, bf16_scales, [&](int nt, int j) { return x[nt][j]; }, [](int) { return make_float2(1.0f, 1.0f); });
+    static constexpr int kUnitCols = kQ4UnitCols, kSetBytes = SETS * (ASYM ? 48 : 32), kMeta = SETS == 1 ? 2 : SETS == 2 ? 4 : 8;
+    static constexpr int kSets = SETS;
+    static constexpr bool kBf16 = false, kBytes = true;       // kBytes: step 1 multiplies whole numbers
+    static constexpr bool kSwap = true;                       // columns 4i + 1 and 4i + 2 of act change places
+    static constexpr bool kRingCols = false;                  // as many bytes as the weights and more: no room in the ring
+    template <int STEP> struct Cols {                         // step 1: 16 bytes of each 64 columns; sums and scales of two result columns
+        uint4 x[STEP == 1 ? 2 : 4];
+        alignas(16) int meta[2][STEP == 1 ? kMeta : 4];
+    };
+    template <int STEP, int NT>
+    static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool bf16_scales, const Cols<STEP>* x) {
+        if constexpr (STEP == 1) {
+            q4_unit_i8<NT, SETS, ASYM>(tot, slot, lane, bf16_scales, [&](int nt, int h) { return x[nt].x[h]; },
+                                       [&](int nt, int set) { return make_int2(x[nt].meta[0][set], x[nt].meta[1][set]); },
+                                       [&](int nt) { return make_float2(__int_as_float(x[nt].meta[0][SETS]), __int_as_float(x[nt].meta[1][SETS])); });
+        } else {
+            q4_unit_f16<NT, SETS, ASYM>(tot, slot, lane, bf16_scales, [&](int nt, int j) { return x[nt].x[j]; },
+                                        [](int) { return make_float2(1.0f, 1.0f); });
+        }
     }
 };
 
-// Units in flight per warp.  Calls of one or two tokens need one tile of 8 columns (three columns of act each), others two.
+// Units in flight per warp.  Where entries have one or two tokens one tile of 8 columns will do (three columns of act each),
+// others need two.
 template <class W, int TILES> __host__ __device__ constexpr int depth() { return W::kRingCols && TILES == 2 ? 4 : 6; }
 
 // ---- small helpers -----------------------------------------------------------------------------------------------
@@ -211,12 +233,33 @@ template <class W, typename T, bool VEC> __device__ __forceinline__ void token_c
         for (int i = 0; i < 4; ++i) {
             float rest = to_float(v.v[i]) * up;
 #pragma unroll
-            for (int k = 0; k < cpt; ++k) rest -= round16<BF16>(rest, bits[k].v[W::kSwap && (i == 1 || i == 2) ? 3 - i : i]);
+            for (int k = 0; k < cpt; ++k) rest -= round16<BF16>(rest, bits[k].v[i]);
         }
 #pragma unroll
         for (int k = 0; k < cpt; ++k) *reinterpret_cast<Pack<uint16_t, 4>*>(dst + (int64_t)k * a.kpad1 + c) = bits[k];
     }
     if (threadIdx.x == 0) a.xscale[token] = down;
+}
+
+// The same for 4-bit experts: a warp per block of 128 columns.
+template <int SETS, int META, typename T, bool VEC> __device__ __forceinline__ void token_bytes(const MoeArgs& a, int token) {
+    const int lane = threadIdx.x & 31;
+    const T* x = static_cast<const T*>(a.in.x) + (int64_t)token * a.in.ld;
+    for (int kb = threadIdx.x >> 5; kb < a.kb1; kb += kWarps) {
+        uint32_t w[3];
+        float down;
+        fixed_point(load_four<VEC>(x, kb * kQ4UnitCols + lane * 4, a.H), 1.0f, w, down);
+        unsigned char* dst = reinterpret_cast<unsigned char*>(a.xcols) + (int64_t)token * 3 * a.kpad1 + kb * kQ4UnitCols + byte_offset(lane);
+#pragma unroll
+        for (int c = 0; c < 3; ++c) *reinterpret_cast<uint32_t*>(dst + (int64_t)c * a.kpad1) = w[c];
+        const int sum = byte_sums<SETS>(w, 3, lane), c = lane & (32 / SETS - 1);
+        if (c < 3) {
+            int* meta = a.xmeta + ((int64_t)(token * 3 + c) * a.kb1 + kb) * META;
+            meta[lane / (32 / SETS)] = sum;
+            if (lane < 3) meta[SETS] = __float_as_int(down * (c == 2 ? 1.0f : c == 1 ? 256.0f : 65536.0f));
+        }
+    }
+    if (threadIdx.x == 0) a.xscale[token] = 1.0f;
 }
 
 // A warp's logit of one (token, expert); what cannot be compared ranks last.  Eight loads of each row are in flight.
@@ -250,7 +293,10 @@ template <typename T, bool VEC> __device__ __forceinline__ void router_logit(con
 
 // Router pairs go to warp 0 of every CTA, the last CTA first (the first ones have tokens to turn into columns), then warp 1.
 template <class W, typename T, bool VEC> __device__ __forceinline__ void step0(const MoeArgs& a, float* part) {
-    for (int t = blockIdx.x; t < a.T; t += gridDim.x) token_columns<W, T, VEC>(a, t, part);
+    for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
+        if constexpr (W::kBytes) token_bytes<W::kSets, W::kMeta, T, VEC>(a, t);
+        else token_columns<W, T, VEC>(a, t, part);
+    }
     for (int i = (threadIdx.x >> 5) * gridDim.x + (gridDim.x - 1 - blockIdx.x); i < a.T * a.E; i += kWarps * gridDim.x)
         router_logit<T, VEC>(a, i / a.E, i % a.E);
 }
@@ -261,8 +307,8 @@ template <class W, typename T> __device__ __forceinline__ void step0(const MoeAr
 
 // ---- routing, by every CTA for itself ----------------------------------------------------------------------------
 struct Lists {
-    int4* entry;         // {expert, first pair, pairs, 0}: an expert and up to kCap of its tokens
-    int2* plan;          // [strips of a round] {which warps have sums of it, its entry (step 1)}
+    int4* entry;         // {expert, first pair, pairs, 0}: an expert and up to `cap` of its tokens
+    int2* plan;          // [32, the most strips of a round] {which warps have sums of it, its entry (step 1)}
     int* pair_token;     // pairs (token, expert) in the order of the experts
     float* pair_gate;
     int* chosen;         // [T][top_k] experts
@@ -271,17 +317,19 @@ struct Lists {
     uint32_t* tokens;    // [E] which tokens chose the expert
     int* first;          // [E] its first pair
     int* sums;           // [warps] scratch of the scan
+    const unsigned char* xbytes;     // 4-bit experts: the tokens' bytes and what is kept of them, in shared memory where they fit
+    const int* xmeta;
     int* cuts;           // [2][2] first and last CTA of the strips that the CTA's ends divide, [4..5] whether it finishes them
 };
 __host__ __device__ inline int list_bytes(int T, int E, int top_k) {
-    return (T * top_k * (16 + 4 + 4 + 4 + 4) + 16 * 8 + T * 4 + E * 8 + 16 * 4 + 8 * 4 + 127) / 128 * 128;
+    return (T * top_k * (16 + 4 + 4 + 4 + 4) + 32 * 8 + T * 4 + E * 8 + 16 * 4 + 8 * 4 + 127) / 128 * 128;
 }
 __device__ __forceinline__ Lists lists_at(unsigned char* p, int T, int E, int top_k) {
     Lists L;
     const int n = T * top_k;
     L.entry = reinterpret_cast<int4*>(p);
     L.plan = reinterpret_cast<int2*>(L.entry + n);
-    L.pair_token = reinterpret_cast<int*>(L.plan + 16);
+    L.pair_token = reinterpret_cast<int*>(L.plan + 32);
     L.pair_gate = reinterpret_cast<float*>(L.pair_token + n);
     L.chosen = reinterpret_cast<int*>(L.pair_gate + n);
     L.gate = reinterpret_cast<float*>(L.chosen + n);
@@ -361,7 +409,7 @@ __device__ __forceinline__ int route(const MoeArgs& a, const Lists& L) {       /
     __syncthreads();
     // where each expert's pairs and entries start: both counts in one scan (neither exceeds 512)
     const int n = tid < a.E ? __popc(L.tokens[tid]) : 0;
-    const int mine = n | ((n + kCap - 1) / kCap) << 16;
+    const int mine = n | ((n + a.cap - 1) / a.cap) << 16;
     int both = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -380,7 +428,7 @@ __device__ __forceinline__ int route(const MoeArgs& a, const Lists& L) {       /
     if (n) {
         const int first = before & 0xffff, entry = before >> 16;
         L.first[tid] = first;
-        for (int i = 0; i * kCap < n; ++i) L.entry[entry + i] = make_int4(tid, first + i * kCap, min(kCap, n - i * kCap), 0);
+        for (int i = 0; i * a.cap < n; ++i) L.entry[entry + i] = make_int4(tid, first + i * a.cap, min(a.cap, n - i * a.cap), 0);
     }
     __syncthreads();
     if (tid < a.T * a.top_k) {                               // at most 512 pairs
@@ -461,31 +509,70 @@ template <class W, int STEP> __device__ __forceinline__ void locate(const MoeArg
     r.sets = (STEP == 1 ? a.gate_up_sets : a.down_sets) + at * W::kSetBytes;
 }
 
-// This warp's units of a round: x .. stop (a round has at most 16 strips of 2^20 units).
+// This warp's units of a round: x .. stop (a round has at most 2^25 units).
 __device__ __forceinline__ void warp_range(const Span& s, int round, int strips, int warp, int& x, int& stop) {
     const int lo = max(s.x0, round * strips * s.nv), n = min(s.x1, (round + 1) * strips * s.nv) - lo;
     x = lo + (int)((uint32_t)(n * warp) / kWarps);
     stop = lo + (int)((uint32_t)(n * (warp + 1)) / kWarps);
 }
 
-// Where a lane reads the columns of a run: column 8 nt + g of the entry's tiles, elements 8t .. of the run's first unit.
-template <class W, int STEP, int TILES>
-__device__ __forceinline__ void run_columns(const MoeArgs& a, const Lists& L, const Run& r, int lane, const uint16_t* (&from)[TILES]) {
-    const int cpt = STEP == 1 ? a.cpt : kActCols, kpad = STEP == 1 ? a.kpad1 : a.kpad2;
-    const int4 entry = L.entry[r.entry];
+// Where a lane reads the columns of a run, from its first unit on: its input column 8 nt + g of the entry's tiles and, of
+// bytes, what is kept of its two result columns.
+template <class W, int STEP, int TILES> struct ColumnsAt {
+    static constexpr bool kBytes = W::kBytes && STEP == 1;
+    const unsigned char* x[TILES];
+    const int* meta[kBytes ? TILES : 1][2];
+    __device__ __forceinline__ void set(const MoeArgs& a, const Lists& L, const Run& r, int lane, int tiles) {
+        const int cpt = STEP == 1 ? a.cpt : kActCols;
+        const int4 entry = L.entry[r.entry];
+        const auto row = [&](int c) {                        // columns past the last repeat one
+            const int pl = cpt == 1 ? c : cpt == 2 ? c >> 1 : c / 3, p = entry.y + min(pl, entry.z - 1);
+            return (STEP == 1 ? L.pair_token[p] : p) * cpt + c - pl * cpt;
+        };
 #pragma unroll
-    for (int nt = 0; nt < TILES; ++nt) {
-        const int c = nt * 8 + (lane >> 2), pl = cpt == 1 ? c : cpt == 2 ? c >> 1 : c / 3, p = entry.y + min(pl, entry.z - 1);   // columns past the last repeat one
-        const int row = (STEP == 1 ? L.pair_token[p] : p) * cpt + c - pl * cpt;
-        from[nt] = (STEP == 1 ? a.xcols : a.acols) + (int64_t)row * kpad + r.kb * W::kUnitCols + (lane & 3) * 8;
+        for (int nt = 0; nt < TILES; ++nt) {
+            if (nt >= tiles) break;
+            const int64_t at = (int64_t)row(nt * 8 + (lane >> 2)) * (STEP == 1 ? a.kpad1 : a.kpad2) + r.kb * W::kUnitCols;
+            x[nt] = (kBytes ? L.xbytes : reinterpret_cast<const unsigned char*>(STEP == 1 ? a.xcols : a.acols) + at) + at + (lane & 3) * 16;
+            if constexpr (kBytes) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) meta[nt][i] = L.xmeta + (row(nt * 8 + (lane & 3) * 2 + i) * a.kb1 + r.kb) * W::kMeta;
+            }
+        }
     }
-}
+    __device__ __forceinline__ void advance() {
+#pragma unroll
+        for (int nt = 0; nt < TILES; ++nt) {
+            x[nt] += W::kUnitCols * (kBytes ? 1 : 2);
+            if constexpr (kBytes) meta[nt][0] += W::kMeta, meta[nt][1] += W::kMeta;
+        }
+    }
+    __device__ __forceinline__ void read(typename W::template Cols<STEP> (&c)[TILES], int tiles) const {
+#pragma unroll
+        for (int nt = 0; nt < TILES; ++nt) {
+            if (nt >= tiles) break;
+#pragma unroll
+            for (int j = 0; j < (int)(sizeof(c[nt].x) / 16); ++j) c[nt].x[j] = *reinterpret_cast<const uint4*>(x[nt] + j * 64);
+            if constexpr (kBytes) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if constexpr (W::kMeta == 2) {
+                        *reinterpret_cast<int2*>(c[nt].meta[i]) = *reinterpret_cast<const int2*>(meta[nt][i]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < W::kMeta; k += 4) *reinterpret_cast<int4*>(c[nt].meta[i] + k) = *reinterpret_cast<const int4*>(meta[nt][i] + k);
+                    }
+                }
+            }
+        }
+    }
+};
 
 // A warp's asynchronous copies, unit after unit of its runs.
 template <class W, int STEP, int TILES> struct Fetcher {
     int round = -1, x = 0, stop = 0, left = 0, tiles = 1;    // x: where the next run starts, left: units of this one
     const unsigned char *unit = nullptr, *sets = nullptr;    // this lane's bytes of them
-    const uint16_t* from[TILES];
+    ColumnsAt<W, STEP, TILES> from;
     __device__ __forceinline__ void next(const MoeArgs& a, const Lists& L, const Span& s, int warp, int lane, uint32_t slot, bool weights, bool cols) {
         if (left == 0) {
             while (x == stop && round < s.rounds)
@@ -496,8 +583,8 @@ template <class W, int STEP, int TILES> struct Fetcher {
                 x += left = r.left;
                 unit = r.unit + lane * 16;
                 sets = r.sets + lane * 16;
-                if (W::kRingCols) run_columns<W, STEP, TILES>(a, L, r, lane, from);
                 if (TILES > 1) tiles = (L.entry[r.entry].z * (STEP == 1 ? a.cpt : kActCols) + 7) / 8;
+                if (W::kRingCols) from.set(a, L, r, lane, tiles);
             }
         }
         if (left) {
@@ -511,10 +598,9 @@ template <class W, int STEP, int TILES> struct Fetcher {
             sets += W::kSetBytes;
             if (W::kRingCols) {
 #pragma unroll
-                for (int nt = 0; nt < TILES; ++nt) {
-                    if (cols && nt < tiles) cp_async16_l1(slot + 1024 + nt * 512, from[nt]);
-                    from[nt] += W::kUnitCols;
-                }
+                for (int nt = 0; nt < TILES; ++nt)
+                    if (cols && nt < tiles) cp_async16_l1(slot + 1024 + nt * 512, from.x[nt]);
+                from.advance();
             }
         }
         cp_commit();
@@ -527,7 +613,7 @@ template <class W> __device__ __forceinline__ void finish_act(const MoeArgs& a, 
     const float scale = L.xscale[L.pair_token[p]];
     gate *= scale;
     up *= scale;
-    const float act = L.pair_gate[p] * (gate / (1.0f + expf(-gate)) * up);
+    const float act = L.pair_gate[p] * (__fdividef(gate, 1.0f + expf(-gate)) * up);
     const int at = W::kSwap && ((row & 3) == 1 || (row & 3) == 2) ? row ^ 3 : row;
     split_act<W::kBf16>(act, a.acols + (int64_t)p * kActCols * a.kpad2 + at, a.kpad2);
 }
@@ -540,7 +626,7 @@ template <class W, int STEP, int TILES>
 __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const Span& s, Fetcher<W, STEP, TILES>& f, unsigned char* smem) {
     constexpr int kDepth = depth<W, TILES>(), kCols = 8 * TILES;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int cpt = STEP == 1 ? a.cpt : kActCols, width = STEP == 1 ? kCap : a.T;
+    const int cpt = STEP == 1 ? a.cpt : kActCols, width = STEP == 1 ? a.cap : a.T;
     unsigned char *ring = smem + warp * kDepth * a.slot_bytes, *ring_end = ring + kDepth * a.slot_bytes, *at = ring;
     float* scr = reinterpret_cast<float*>(smem + a.scr_off) + warp * 16 * kCols;
     float* park = reinterpret_cast<float*>(smem + a.park_off);
@@ -561,107 +647,106 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
         warp_range(s, round, a.round, warp, x, stop);
         Run run;
         run.left = 0;
-        const uint16_t* from[TILES] = {};
-        uint4 xr[TILES][W::kLoads];
+        ColumnsAt<W, STEP, TILES> from;
+        typename W::template Cols<STEP> xr[TILES];           // what the lane needs of the next unit's columns
         int4 entry = make_int4(0, 0, 0, 0);
         float tot[TILES][4] = {};
-        const auto read_columns = [&] {                      // what the lane needs of the next unit's columns
-#pragma unroll
-            for (int nt = 0; nt < TILES; ++nt) {
-                if (nt < tiles) {
-#pragma unroll
-                    for (int j = 0; j < W::kLoads; ++j) xr[nt][j] = *reinterpret_cast<const uint4*>(from[nt] + j * 32);
-                }
-                from[nt] += W::kUnitCols;
-            }
-        };
-        while (x < stop) {
+        const auto begin_run = [&] {
             locate<W, STEP>(a, L, s, x, stop, run);
             x += run.left;
             entry = L.entry[run.entry];
             tiles = TILES == 1 ? 1 : (entry.z * cpt + 7) / 8;
             if (!W::kRingCols) {
-                run_columns<W, STEP, TILES>(a, L, run, lane, from);
-                read_columns();
+                from.set(a, L, run, lane, tiles);
+                from.read(xr, tiles);
             }
-            if (STEP == 2 && run.ls != strip) {                // a new strip's sums of this warp
-                strip = run.ls;
-                for (int i = lane; i < 16 * width; i += 32) park[(warp + strip - ls0) * 16 * width + i] = 0.0f;
-            }
+        };
+        if (x < stop) begin_run();
+        while (run.left) {
             do {
                 cp_wait<kDepth - 1>();
                 if (!W::kRingCols) __syncwarp();               // sets are read by other lanes than copied them; nothing else is
                 if (W::kRingCols) {
 #pragma unroll
                     for (int nt = 0; nt < TILES; ++nt)
-                        if (nt < tiles) xr[nt][0] = *reinterpret_cast<const uint4*>(at + 1024 + nt * 512 + lane * 16);
+                        if (nt < tiles) xr[nt].x[0] = *reinterpret_cast<const uint4*>(at + 1024 + nt * 512 + lane * 16);
                 }
-                if (TILES == 1 || tiles == 1) W::template unit<1>(reinterpret_cast<float(&)[1][4]>(tot), at, lane, a.bf16_scales != 0, xr);
-                else W::template unit<TILES>(tot, at, lane, a.bf16_scales != 0, xr);
+                if (TILES == 1 || tiles == 1) W::template unit<STEP, 1>(reinterpret_cast<float(&)[1][4]>(tot), at, lane, a.bf16_scales != 0, xr);
+                else W::template unit<STEP, TILES>(tot, at, lane, a.bf16_scales != 0, xr);
                 --run.left;
-                if (!W::kRingCols && run.left) read_columns();     // in flight while the other warps compute
+                if (!W::kRingCols && run.left) {                   // in flight while the other warps compute
+                    from.advance();
+                    from.read(xr, tiles);
+                }
                 if (!W::kRingCols) __syncwarp();
                 f.next(a, L, s, warp, lane, smem_addr(at) + lane * 16, true, true);
                 at += a.slot_bytes;
                 if (at == ring_end) at = ring;
             } while (run.left);
-            {
-                // add a token's columns and park the sums: piece (warp, strip) has slot warp + strip
+            // add a token's columns and park the sums: piece (warp, strip) has slot warp + strip.  The next run's first columns
+            // are requested in between.
 #pragma unroll
-                for (int nt = 0; nt < TILES; ++nt)
+            for (int nt = 0; nt < TILES; ++nt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        scr[(g + (i >> 1) * 8) * kCols + nt * 8 + 2 * t + (i & 1)] = tot[nt][i];
-                        tot[nt][i] = 0.0f;
-                    }
-                __syncwarp();
-                float* tile = park + (warp + run.ls - ls0) * 16 * width;
-                const int row = lane & 15;
-                for (int pl = lane >> 4; pl < entry.z; pl += 2) {
-                    const float* c = scr + row * kCols + pl * cpt;
-                    if (STEP == 1) {
-                        float v = c[0];
-                        for (int k = 1; k < cpt; ++k) v += c[k];
-                        tile[pl * 16 + row] = v;
-                    } else {
-                        const float v = W::kBf16 ? c[0] + c[1] + c[2] : fmaf(c[0], 0x1p11f, fmaf(c[1], 2.0f, c[2] * 0x1p-10f));
-                        tile[L.pair_token[entry.y + pl] * 16 + row] += v;
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    scr[(g + (i >> 1) * 8) * kCols + nt * 8 + 2 * t + (i & 1)] = tot[nt][i];
+                    tot[nt][i] = 0.0f;
                 }
-                __syncwarp();
+            const int first = entry.y, pairs = entry.z, ls = run.ls;
+            if (x < stop) begin_run();
+            float* tile = park + (warp + ls - ls0) * 16 * width;
+            if (STEP == 2 && ls != strip) {                    // a new strip's sums of this warp
+                strip = ls;
+                for (int i = lane; i < 16 * width; i += 32) tile[i] = 0.0f;
             }
+            __syncwarp();
+            const int row = lane & 15;
+            for (int pl = lane >> 4; pl < pairs; pl += 2) {
+                const float* c = scr + row * kCols + pl * cpt;
+                if (STEP == 1) {
+                    float v = c[0];
+                    for (int k = 1; k < cpt; ++k) v += c[k];
+                    tile[pl * 16 + row] = v;
+                } else {
+                    const float v = W::kBf16 ? c[0] + c[1] + c[2] : fmaf(c[0], 0x1p11f, fmaf(c[1], 2.0f, c[2] * 0x1p-10f));
+                    tile[L.pair_token[first + pl] * 16 + row] += v;
+                }
+            }
+            __syncwarp();
         }
         __syncthreads();
 
         // the pieces of a row in the order of the warps
-        const int per_strip = STEP == 1 ? 8 * kCap : 16 * a.T;
-        const Divider by_strip(per_strip);
-        for (int o = tid; o < rs * per_strip; o += kThreads) {
-            const int q = by_strip.div(o), r = o - q * per_strip, ls = ls0 + q;
-            const bool cut = (ls == 0 && cut_first) || (ls == s.strips - 1 && cut_last);
-            // the strip's slot among this CTA's parts: 0 where an earlier CTA has begun it
-            float* part = my_parts + (ls == 0 && cut_first ? 0 : 16 * width);
-            const int2 plan = L.plan[q];
-            if (STEP == 1) {
-                const int pl = r >> 3, row = r & 7;
-                if (pl >= L.entry[plan.y].z) continue;
-                float gate = 0.0f, up = 0.0f;
-                for (uint32_t m = (uint32_t)plan.x; m; m &= m - 1) {
-                    const float* c = park + (__ffs((int)m) - 1 + q) * 16 * width + pl * 16 + row;
-                    gate += c[0];
-                    up += c[8];
+        const auto pieces = [&](uint32_t mask, int q, int at) {
+            float v = 0.0f;
+            for (; mask; mask &= mask - 1) v += park[(__ffs((int)mask) - 1 + q) * 16 * width + at];
+            return v;
+        };
+        // a divided strip's slot among this CTA's parts: 0 where an earlier CTA has begun it
+        const auto cut = [&](int ls) { return (ls == 0 && cut_first) || (ls == s.strips - 1 && cut_last); };
+        const auto part = [&](int ls) { return my_parts + (ls == 0 && cut_first ? 0 : 16 * width); };
+        if (STEP == 1) {
+            for (int o = tid >> 1; o < rs * 8; o += kThreads / 2) {        // two threads to a strip's row: even and odd pairs
+                const int q = o >> 3, row = o & 7, ls = ls0 + q;
+                const int2 plan = L.plan[q];
+                for (int pl = tid & 1; pl < L.entry[plan.y].z; pl += 2) {
+                    const float gate = pieces((uint32_t)plan.x, q, pl * 16 + row), up = pieces((uint32_t)plan.x, q, pl * 16 + row + 8);
+                    if (!cut(ls)) {
+                        finish_act<W>(a, L, plan.y, s.first + ls, row, pl, gate, up);
+                    } else {
+                        __stcg(part(ls) + pl * 16 + row, gate);
+                        __stcg(part(ls) + pl * 16 + row + 8, up);
+                    }
                 }
-                if (!cut) {
-                    finish_act<W>(a, L, plan.y, s.first + ls, row, pl, gate, up);
-                } else {
-                    __stcg(part + pl * 16 + row, gate);
-                    __stcg(part + pl * 16 + row + 8, up);
-                }
-            } else {
-                float v = 0.0f;
-                for (uint32_t m = (uint32_t)plan.x; m; m &= m - 1) v += park[(__ffs((int)m) - 1 + q) * 16 * width + r];
-                if (!cut) finish_y(a, s.first + ls, r & 15, r >> 4, v);
-                else __stcg(part + r, v);
+            }
+        } else {
+            const int per_strip = 16 * a.T;
+            const Divider by_strip(per_strip);
+            for (int o = tid; o < rs * per_strip; o += kThreads) {
+                const int q = by_strip.div(o), r = o - q * per_strip, ls = ls0 + q;
+                const float v = pieces((uint32_t)L.plan[q].x, q, r);
+                if (!cut(ls)) finish_y(a, s.first + ls, r & 15, r >> 4, v);
+                else __stcg(part(ls) + r, v);
             }
         }
         __syncthreads();
@@ -683,7 +768,7 @@ __device__ __forceinline__ void find_cuts(const Lists& L, const Span& s, int64_t
 
 // Divided strips: the last of a strip's CTAs to arrive adds the parts in the order of the CTAs.
 template <class W, int STEP> __device__ __forceinline__ void join(const MoeArgs& a, const Lists& L, const Span& s) {
-    const int tid = threadIdx.x, width = STEP == 1 ? kCap : a.T;
+    const int tid = threadIdx.x, width = STEP == 1 ? a.cap : a.T;
     if (tid < 2 && L.cuts[tid] >= 0) {                       // behind the barrier that ended the last round
         int* arrived = a.sync + 4 + (STEP - 1) * gridDim.x + L.cuts[tid];
         int before;
@@ -695,7 +780,7 @@ template <class W, int STEP> __device__ __forceinline__ void join(const MoeArgs&
         L.cuts[4 + tid] = 0;
     }
     __syncthreads();
-    const int per_strip = STEP == 1 ? 8 * kCap : 16 * a.T;
+    const int per_strip = STEP == 1 ? 8 * a.cap : 16 * a.T;
     for (int o = tid; o < 2 * per_strip; o += kThreads) {
         const int which = o >= per_strip, r = o - which * per_strip;
         if (!L.cuts[4 + which]) continue;
@@ -721,7 +806,7 @@ template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe
     __shared__ float part[kWarps];
     __shared__ int flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Lists L = lists_at(smem + a.list_off, a.T, a.E, a.top_k);
+    Lists L = lists_at(smem + a.list_off, a.T, a.E, a.top_k);
     pdl_release();
     // before the wait: the router's rows on their way to L2, and the translations of what is touched first
     for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.E * a.router_ld / 32; i += gridDim.x * kThreads) warm(a.router + i * 32);
@@ -742,7 +827,23 @@ template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe
     grid_arrive(a.sync);
     bool ok = grid_wait(a.sync, a.sync + 3, a.polls, &flag);
     if (ok) {
+        if constexpr (W::kBytes) {                            // the tokens' bytes are on their way while the experts are chosen
+            L.xbytes = reinterpret_cast<const unsigned char*>(a.xcols);
+            L.xmeta = a.xmeta;
+            if (a.bytes_off) {
+                const int n = a.T * 3 * a.kpad1 / 16, m = (a.T * 3 * a.kb1 * W::kMeta + 3) / 4;
+                for (int i = threadIdx.x; i < n; i += kThreads) cp_async16(smem_addr(smem + a.bytes_off) + i * 16, reinterpret_cast<const uint4*>(a.xcols) + i);
+                for (int i = threadIdx.x; i < m; i += kThreads) cp_async16(smem_addr(smem + a.bytes_off) + (n + i) * 16, reinterpret_cast<const uint4*>(a.xmeta) + i);
+                L.xbytes = smem + a.bytes_off;
+                L.xmeta = reinterpret_cast<const int*>(smem + a.bytes_off + n * 16);
+            }
+            cp_commit();
+        }
         const int entries = route(a, L);
+        if constexpr (W::kBytes) {
+            cp_wait<0>();
+            __syncthreads();
+        }
         const uint32_t ring = smem_addr(smem) + warp * kDepth * a.slot_bytes + lane * 16;
         {
             const Span s = span_of(entries * a.strips1, a.kb1, a.round);
@@ -820,21 +921,28 @@ template <int TILES> Kernel pick_kernel(const pp_moe* L) {
     if (L->sets == 2) return L->asym ? moe_kernel<Q4<2, true>, TILES> : moe_kernel<Q4<2, false>, TILES>;
     return L->asym ? moe_kernel<Q4<1, true>, TILES> : moe_kernel<Q4<1, false>, TILES>;
 }
-int tiles_of(int tokens) { return tokens * kActCols <= 8 ? 1 : 2; }
+// Tokens of an entry: what two tiles of columns hold, or what one does where few experts have more tokens than that (their
+// weights are then read again): up to one token to an expert on average.
+int cap_of(int tokens, int top_k, int E) { return tokens * top_k <= E ? 8 / kActCols : kMaxCap; }
+int tiles_of(int tokens, int cap) { return std::min(tokens, cap) * kActCols <= 8 ? 1 : 2; }
 
 constexpr int kMaxSmem = 227 * 1024 - 256;       // beside the kernel's few static bytes
 
-// Strips of a round and the shared memory: the most strips that fit, 16 at most (one to a warp).
-size_t plan_smem(MoeArgs& a, int depth, int tiles) {
+// Strips of a round and the shared memory: the most strips that fit, 32 at most.
+size_t plan_smem(MoeArgs& a, int depth, int tiles, int meta) {
     size_t at = (size_t)kWarps * depth * a.slot_bytes;
     a.list_off = (int)(at = (at + 127) / 128 * 128);
     at += list_bytes(a.T, a.E, a.top_k);
     a.scr_off = (int)at;
     at += (size_t)kWarps * 16 * 8 * tiles * 4;
     a.park_off = (int)at;
-    for (a.round = 16;; a.round /= 2) {
-        const size_t total = at + (size_t)(a.round + kWarps) * 16 * std::max(kCap, a.T) * 4;
-        if (total <= (size_t)kMaxSmem || a.round == 1) return total;
+    for (a.round = 32;; a.round /= 2) {
+        const size_t total = at + (size_t)(a.round + kWarps) * 16 * std::max(a.cap, a.T) * 4;
+        if (total > (size_t)kMaxSmem && a.round > 1) continue;
+        const size_t bytes = meta ? (size_t)a.T * 3 * a.kpad1 + (size_t)a.T * 3 * a.kb1 * meta * 4 + 16 : 0;
+        const bool fits = bytes && total + bytes <= (size_t)kMaxSmem;
+        a.bytes_off = fits ? (int)total : 0;
+        return total + (fits ? bytes : 0);
     }
 }
 
@@ -849,7 +957,7 @@ extern "C" pp_status_t pp_moe_destroy(pp_moe_t* L) {
     if (!L) return PP_ERR_INVALID_ARG;
     for (void* p : {static_cast<void*>(L->gate_up), static_cast<void*>(L->down), static_cast<void*>(L->gate_up_sets),
                     static_cast<void*>(L->down_sets), static_cast<void*>(L->router), static_cast<void*>(L->logits),
-                    static_cast<void*>(L->xscale), static_cast<void*>(L->xcols), static_cast<void*>(L->acols), static_cast<void*>(L->parts), static_cast<void*>(L->sync)})
+                    static_cast<void*>(L->xscale), static_cast<void*>(L->xcols), static_cast<void*>(L->acols), static_cast<void*>(L->xmeta), static_cast<void*>(L->parts), static_cast<void*>(L->sync)})
         cudaFree(p);
     delete L;
     return PP_OK;
@@ -899,7 +1007,8 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
          (set_bytes && (!alloc(&L->gate_up_sets, units1 * set_bytes) || !alloc(&L->down_sets, units2 * set_bytes))) || !alloc(&L->router, ld * E * 4) ||
          !alloc(&L->logits, (size_t)max_tokens * E * 4) || !alloc(&L->xscale, (size_t)max_tokens * 4) ||
          !alloc(&L->xcols, (size_t)max_tokens * 3 * L->kb1 * cols * 2) || !alloc(&L->acols, abytes) ||
-         !alloc(&L->parts, (size_t)L->ctas * 2 * 16 * std::max(kCap, max_tokens) * 4) || !alloc(&L->sync, sync_bytes))) {
+         (wtype < 0 && !alloc(&L->xmeta, (size_t)max_tokens * 3 * L->kb1 * 32)) ||
+         !alloc(&L->parts, (size_t)L->ctas * 2 * 16 * std::max(kMaxCap, max_tokens) * 4) || !alloc(&L->sync, sync_bytes))) {
         cudaGetLastError();
         st = PP_ERR_ALLOC;
     }
@@ -985,6 +1094,7 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     a.xscale = L->xscale;
     a.xcols = L->xcols;
     a.acols = L->acols;
+    a.xmeta = L->xmeta;
     a.sync = L->sync;
     a.y = y;
     a.ids = ids_out;
@@ -1002,11 +1112,12 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     a.kpad1 = L->kb1 * cols;
     a.kpad2 = L->kb2 * cols;
     a.router_ld = (L->H + 3) / 4 * 4;
-    const int tiles = tiles_of(tokens), depth = q4 || tiles == 1 ? 6 : 4;        // as depth() of the kernel
+    a.cap = cap_of(tokens, L->top_k, L->E);
+    const int tiles = tiles_of(tokens, a.cap), depth = q4 || tiles == 1 ? 6 : 4;        // as depth() of the kernel
     a.slot_bytes = 1024 + (q4 ? (q4_set_bytes(L->sets, L->asym) + 127) / 128 * 128 : 512 * tiles);      // slots start on 128 bytes
     a.gate_up_sets = L->gate_up_sets;
     a.down_sets = L->down_sets;
-    a.cpt = L->wtype == PP_BF16 ? (x_type == PP_BF16 ? 1 : x_type == PP_F16 ? 2 : 3) : (x_type == PP_F32 ? 2 : 1);
+    a.cpt = q4 ? 3 : L->wtype == PP_BF16 ? (x_type == PP_BF16 ? 1 : x_type == PP_F16 ? 2 : 3) : (x_type == PP_F32 ? 2 : 1);
     a.bf16_scales = L->bf16_scales;
     a.polls = g_stream_wait_polls;
     a.parts = L->parts;
@@ -1020,7 +1131,7 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(L->ctas);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = plan_smem(a, depth, tiles);
+    cfg.dynamicSmemBytes = plan_smem(a, depth, tiles, !q4 ? 0 : L->sets == 1 ? 2 : L->sets == 2 ? 4 : 8);        // as kMeta
     cfg.stream = static_cast<cudaStream_t>(cuda_stream);
     cfg.attrs = at;
     cfg.numAttrs = 2;

@@ -81,58 +81,6 @@ __device__ __forceinline__ void store_y(void* y, int64_t i, int type, float v) {
     else static_cast<__nv_bfloat16*>(y)[i] = __float2bfloat16_rn(v);
 }
 
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
-
-// Four whole numbers of a lane, |v| < 2^23, as three words of signed bytes, the highest first.  Adding 0x808080 carries
-// what a signed byte below cannot hold into the byte above; the sign bits then flip back.
-__device__ __forceinline__ void three_bytes(const int (&v)[4], uint32_t (&w)[3]) {
-    uint32_t u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = ((uint32_t)v[i] + 0x808080u) ^ 0x808080u;
-    const uint32_t a = prmt(u[0], u[1], 0x5140), b = prmt(u[2], u[3], 0x5140);
-    w[2] = prmt(a, b, 0x5410);
-    w[1] = prmt(a, b, 0x7632);
-    w[0] = prmt(prmt(u[0], u[1], 0x0062), prmt(u[2], u[3], 0x0062), 0x5410);
-}
-
-// A warp's block of 128 columns of one vector, four per lane: its columns' bytes and what one of them stands for (in
-// `down`, of the lowest byte).  own: an 8-bit input's scale.
-template <typename T> __device__ __forceinline__ void fixed_point(const Pack<T, 4>& x, float own, uint32_t (&w)[3], float& down) {
-    int v[4];
-    if constexpr (std::is_same_v<T, int8_t>) {
-        w[0] = *reinterpret_cast<const uint32_t*>(&x);
-        down = own;
-        return;
-    } else if constexpr (sizeof(T) == 1) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __float2int_rn(to_float(x.v[i]) * 512.0f);
-        // NaN is the only e4m3 value that is not finite: the whole vector is not
-        const bool nan = __any_sync(0xffffffffu, to_float(x.v[0]) + to_float(x.v[1]) + to_float(x.v[2]) + to_float(x.v[3]) !=
-                                                     to_float(x.v[0]) + to_float(x.v[1]) + to_float(x.v[2]) + to_float(x.v[3]));
-        down = nan ? __int_as_float(0x7fffffff) : own * 0x1p-9f;
-    } else {
-        float f[4];
-        uint32_t most = 0u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[i] = to_float(x.v[i]);
-            most = max(most, __float_as_uint(f[i]) & 0x7fffffffu);        // as whole numbers: a NaN is the largest
-        }
-        most = __reduce_max_sync(0xffffffffu, most);
-        const uint32_t e = max(most >> 23, 23u);                           // smaller blocks keep the scale of 2^-104
-        float up = __uint_as_float((276u - min(e, 254u)) << 23);
-        down = __uint_as_float((min(e, 254u) - 22u) << 23);
-        if (__uint_as_float(most) * up > 8355000.0f) {
-            up *= 0.5f;
-            down *= 2.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __float2int_rn(f[i] * up);
-        if (most >= 0x7f800000u) down = __int_as_float(0x7fffffff);        // an infinity or a NaN: so are the sums
-    }
-    three_bytes(v, w);
-}
-
 // A warp's block of 128 columns of one vector in binary16, four per lane, columns 4i + 1 and 4i + 2 exchanged; rest: what
 // f32 leaves over.  The result is the power of two to multiply with.
 template <typename T> __device__ __forceinline__ float halves(const Pack<T, 4>& x, uint2& h, uint2& rest) {
@@ -189,26 +137,13 @@ __device__ __forceinline__ void stage_rows(const Q4Args& a, unsigned char* xs, f
                 float down;
                 fixed_point(v[q], own[q], w, down);
                 unsigned char* at = xs + (kb * 2 + (lane >> 4)) * step + token * cpt * 64 + ((lane >> 1) & 3) * 16 + (lane & 8) + (lane & 1) * 4;
-                int sum[2] = {0, 0};                         // 2^16 (highest byte) + (middle byte), and the lowest
 #pragma unroll
-                for (int c = 0; c < cpt; ++c) {
-                    *reinterpret_cast<uint32_t*>(at + c * 64) = w[c];
-                    sum[c == 2] += __dp4a((int)w[c], 0x01010101, 0) * (cpt == 3 && c == 0 ? 65536 : 1);
-                }
-#pragma unroll
-                for (int c = 0; c < (cpt + 1) / 2; ++c) {
-                    if (SETS == 1) {
-                        sum[c] = __reduce_add_sync(0xffffffffu, sum[c]);
-                    } else {
-#pragma unroll
-                        for (int o = 16 / SETS; o; o >>= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], o);
-                    }
-                }
+                for (int c = 0; c < cpt; ++c) *reinterpret_cast<uint32_t*>(at + c * 64) = w[c];
+                const int sum = byte_sums<SETS>(w, cpt, lane);
                 constexpr int kLanes = 32 / SETS;            // of a set
-                const int c = lane & (kLanes - 1);
+                const int c = lane & (kLanes - 1), col = token * cpt + c;
                 if (c < cpt) {
-                    const int col = token * cpt + c, middle = (int16_t)sum[0];
-                    sums[(kb * SETS + lane / kLanes) * NT * 8 + col] = cpt == 1 || c == 1 ? middle : c == 0 ? (sum[0] - middle) >> 16 : sum[1];
+                    sums[(kb * SETS + lane / kLanes) * NT * 8 + col] = sum;
                     if (lane < cpt) cs[kb * NT * 8 + col] = down * (cpt == 1 || c == 2 ? 1.0f : c == 1 ? 256.0f : 65536.0f);
                 }
             } else {
@@ -227,68 +162,6 @@ template <typename T, bool BYTES, int NT, int SETS, typename Then>
 __device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, float* cs, int* sums, int k0, int n_k, int warp, int lane, Then then) {
     if (a.in.vec) stage_rows<T, true, BYTES, NT, SETS>(a, xs, cs, sums, k0, n_k, warp, lane, then);
     else stage_rows<T, false, BYTES, NT, SETS>(a, xs, cs, sums, k0, n_k, warp, lane, then);
-}
-
-__device__ __forceinline__ void mma_u8s8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm(
-        "mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// tot[nt] += W_unit * X for NT tiles of 8 columns.  Lane (g, t) holds in tot[nt][0..3] rows g, g, g + 8, g + 8 and columns
-// 8 nt + 2t, + 1, + 0, + 1.  x: the unit's first 64 columns of the input, x_lane[nt]: offset of the lane's column 8 nt + g in
-// them, x_step: bytes to the next 64.  sums, cs: the lane's two columns for the unit, eight apart from tile to tile.
-// The whole numbers come out of the product on top of 1.5 * 2^23: as floats they are themselves plus that, exactly, for
-// magnitudes up to 2^22 (16 * 15 * 128 * 128 is less).
-template <int NT, int SETS, bool ASYM>
-__device__ __forceinline__ void q4_unit_i8(float (&tot)[NT][4], const unsigned char* slot, int lane, const unsigned char* x,
-                                           const int (&x_lane)[NT], int x_step, const int* sums, const float* cs, bool bf16_scales) {
-    constexpr int kOnTop = 0x4B400000, per_set = 4 / SETS;
-    const int g = lane >> 2;
-    int acc[NT][4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {                            // 64 columns: two k-slices of 32
-        const uint4 w = at<uint4>(slot + h * 512 + lane * 16);
-        uint4 b[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) b[nt] = at<uint4>(x + h * x_step + x_lane[nt]);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int j = 2 * h + k, set = j / per_set;
-            if (j % per_set == 0) {                          // start from -z sum d
-                int z0 = -8, z1 = -128;
-                if (ASYM) {
-                    const uint32_t zz = at<uint16_t>(slot + 1024 + SETS * 32 + set * 16 + g * 2);
-                    z0 = -(int)(zz & 255u);
-                    z1 = -(int)(zz >> 8);
-                }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int2 d = *reinterpret_cast<const int2*>(sums + (set * NT + nt) * 8);
-                    acc[nt][0] = z0 * d.x + kOnTop;
-                    acc[nt][1] = z0 * d.y + kOnTop;
-                    acc[nt][2] = z1 * d.x + kOnTop;
-                    acc[nt][3] = z1 * d.y + kOnTop;
-                }
-            }
-            const uint32_t w0 = k ? w.z : w.x, w1 = k ? w.w : w.y;
-            const uint32_t a[4] = {w0 & 0x0f0f0f0fu, w0 & 0xf0f0f0f0u, w1 & 0x0f0f0f0fu, w1 & 0xf0f0f0f0u};
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_u8s8(acc[nt], a, k ? b[nt].z : b[nt].x, k ? b[nt].w : b[nt].y);
-            if (j % per_set == per_set - 1) {
-                const float2 s = q4_scales(slot, set, g, bf16_scales);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const float2 c = *reinterpret_cast<const float2*>(cs + nt * 8);
-                    tot[nt][0] = fmaf(s.x * c.x, __int_as_float(acc[nt][0]) - 12582912.0f, tot[nt][0]);
-                    tot[nt][1] = fmaf(s.x * c.y, __int_as_float(acc[nt][1]) - 12582912.0f, tot[nt][1]);
-                    tot[nt][2] = fmaf(s.y * c.x, __int_as_float(acc[nt][2]) - 12582912.0f, tot[nt][2]);
-                    tot[nt][3] = fmaf(s.y * c.y, __int_as_float(acc[nt][3]) - 12582912.0f, tot[nt][3]);
-                }
-            }
-        }
-    }
 }
 
 template <bool BYTES, int NT, int SETS, bool ASYM>
@@ -377,7 +250,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) q4_kernel(const Q4A
             cp_wait<kDepth - 1>();
             __syncwarp();
             if constexpr (BYTES) {
-                q4_unit_i8<NT, SETS, ASYM>(tot, at, lane, x, x_lane, step, sum, c, a.bf16_scales != 0);
+                q4_unit_i8<NT, SETS, ASYM>(tot, at, lane, a.bf16_scales != 0,
+                                           [&](int nt, int h) { return *reinterpret_cast<const uint4*>(x + h * step + x_lane[nt]); },
+                                           [&](int nt, int set) { return *reinterpret_cast<const int2*>(sum + (set * NT + nt) * 8); },
+                                           [&](int nt) { return *reinterpret_cast<const float2*>(c + nt * 8); });
             } else {
                 q4_unit_f16<NT, SETS, ASYM>(tot, at, lane, a.bf16_scales != 0,
                                             [&](int nt, int j) { return *reinterpret_cast<const uint4*>(x + j * step + x_lane[nt]); },

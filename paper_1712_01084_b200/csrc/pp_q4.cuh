@@ -182,6 +182,146 @@ struct Divider {
     __device__ __forceinline__ explicit Divider(int d) : r(1.0f / (float)d), n(d) {}
     __device__ __forceinline__ int div(int i) const { return (int)(((float)i + 0.5f) * r); }
 };
+
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
+
+// Four whole numbers of a lane, |v| < 2^23, as three words of signed bytes, the highest first.  Adding 0x808080 carries
+// what a signed byte below cannot hold into the byte above; the sign bits then flip back.
+__device__ __forceinline__ void three_bytes(const int (&v)[4], uint32_t (&w)[3]) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = ((uint32_t)v[i] + 0x808080u) ^ 0x808080u;
+    const uint32_t a = prmt(u[0], u[1], 0x5140), b = prmt(u[2], u[3], 0x5140);
+    w[2] = prmt(a, b, 0x5410);
+    w[1] = prmt(a, b, 0x7632);
+    w[0] = prmt(prmt(u[0], u[1], 0x0062), prmt(u[2], u[3], 0x0062), 0x5410);
+}
+
+// A warp's block of 128 columns of one vector, four per lane: its columns' bytes and what one of them stands for (in
+// `down`, of the lowest byte).  own: an 8-bit input's scale.
+template <typename T> __device__ __forceinline__ void fixed_point(const Pack<T, 4>& x, float own, uint32_t (&w)[3], float& down) {
+    int v[4];
+    if constexpr (std::is_same_v<T, int8_t>) {
+        w[0] = *reinterpret_cast<const uint32_t*>(&x);
+        down = own;
+        return;
+    } else if constexpr (sizeof(T) == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __float2int_rn(to_float(x.v[i]) * 512.0f);
+        // NaN is the only e4m3 value that is not finite: the whole vector is not
+        const bool nan = __any_sync(0xffffffffu, to_float(x.v[0]) + to_float(x.v[1]) + to_float(x.v[2]) + to_float(x.v[3]) !=
+                                                     to_float(x.v[0]) + to_float(x.v[1]) + to_float(x.v[2]) + to_float(x.v[3]));
+        down = nan ? __int_as_float(0x7fffffff) : own * 0x1p-9f;
+    } else {
+        float f[4];
+        uint32_t most = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[i] = to_float(x.v[i]);
+            most = max(most, __float_as_uint(f[i]) & 0x7fffffffu);        // as whole numbers: a NaN is the largest
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        const uint32_t e = max(most >> 23, 23u);                           // smaller blocks keep the scale of 2^-104
+        float up = __uint_as_float((276u - min(e, 254u)) << 23);
+        down = __uint_as_float((min(e, 254u) - 22u) << 23);
+        if (__uint_as_float(most) * up > 8355000.0f) {
+            up *= 0.5f;
+            down *= 2.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __float2int_rn(f[i] * up);
+        if (most >= 0x7f800000u) down = __int_as_float(0x7fffffff);        // an infinity or a NaN: so are the sums
+    }
+    three_bytes(v, w);
+}
+
+// The sums of a warp's three columns of bytes over each set of scales: lanes 0 .. cpt - 1 of a set's lanes have column `lane`'s.
+template <int SETS> __device__ __forceinline__ int byte_sums(const uint32_t (&w)[3], int cpt, int lane) {
+    int sum[2] = {0, 0};                                     // 2^16 (highest byte) + (middle byte), and the lowest
+    if (cpt == 1) {
+        sum[0] = __dp4a((int)w[0], 0x01010101, 0);
+    } else {
+        sum[0] = __dp4a((int)w[0], 0x01010101, 0) * 65536 + __dp4a((int)w[1], 0x01010101, 0);
+        sum[1] = __dp4a((int)w[2], 0x01010101, 0);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        if (c == 1 && cpt == 1) break;
+        if (SETS == 1) {
+            sum[c] = __reduce_add_sync(0xffffffffu, sum[c]);
+        } else {
+#pragma unroll
+            for (int o = 16 / SETS; o; o >>= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], o);
+        }
+    }
+    const int c = lane & (32 / SETS - 1), middle = (int16_t)sum[0];
+    return cpt == 1 || c == 1 ? middle : c == 0 ? (sum[0] - middle) >> 16 : sum[1];
+}
+// Where a lane's four bytes of a block lie among its column's 128: [64 columns][lane t][8 bytes of 32 columns, 8 of the next].
+__device__ __forceinline__ int byte_offset(int lane) { return (lane >> 4) * 64 + ((lane >> 1) & 3) * 16 + (lane & 8) + (lane & 1) * 4; }
+
+__device__ __forceinline__ void mma_u8s8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm(
+        "mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// tot[nt] += W_unit * X for NT tiles of 8 columns.  Lane (g, t) holds in tot[nt][0..3] rows g, g, g + 8, g + 8 and columns
+// 8 nt + 2t, + 1, + 0, + 1.  load_x(nt, h): the lane's 16 bytes of its input column 8 nt + g in the h-th 64 columns of the unit;
+// sums(nt, set) and col_scale(nt): of the lane's two result columns.
+// The whole numbers come out of the product on top of 1.5 * 2^23: as floats they are themselves plus that, exactly, for
+// magnitudes up to 2^22 (16 * 15 * 128 * 128 is less).
+template <int NT, int SETS, bool ASYM, typename LoadX, typename Sums, typename ColScale>
+__device__ __forceinline__ void q4_unit_i8(float (&tot)[NT][4], const unsigned char* slot, int lane, bool bf16_scales, LoadX load_x, Sums sums,
+                                           ColScale col_scale) {
+    constexpr int kOnTop = 0x4B400000, per_set = 4 / SETS;
+    const int g = lane >> 2;
+    int acc[NT][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                            // 64 columns: two k-slices of 32
+        const uint4 w = at<uint4>(slot + h * 512 + lane * 16);
+        uint4 b[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) b[nt] = load_x(nt, h);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int j = 2 * h + k, set = j / per_set;
+            if (j % per_set == 0) {                          // start from -z sum d
+                int z0 = -8, z1 = -128;
+                if (ASYM) {
+                    const uint32_t zz = at<uint16_t>(slot + 1024 + SETS * 32 + set * 16 + g * 2);
+                    z0 = -(int)(zz & 255u);
+                    z1 = -(int)(zz >> 8);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int2 d = sums(nt, set);
+                    acc[nt][0] = z0 * d.x + kOnTop;
+                    acc[nt][1] = z0 * d.y + kOnTop;
+                    acc[nt][2] = z1 * d.x + kOnTop;
+                    acc[nt][3] = z1 * d.y + kOnTop;
+                }
+            }
+            const uint32_t w0 = k ? w.z : w.x, w1 = k ? w.w : w.y;
+            const uint32_t a[4] = {w0 & 0x0f0f0f0fu, w0 & 0xf0f0f0f0u, w1 & 0x0f0f0f0fu, w1 & 0xf0f0f0f0u};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_u8s8(acc[nt], a, k ? b[nt].z : b[nt].x, k ? b[nt].w : b[nt].y);
+            if (j % per_set == per_set - 1) {
+                const float2 s = q4_scales(slot, set, g, bf16_scales);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float2 c = col_scale(nt);
+                    tot[nt][0] = fmaf(s.x * c.x, __int_as_float(acc[nt][0]) - 12582912.0f, tot[nt][0]);
+                    tot[nt][1] = fmaf(s.x * c.y, __int_as_float(acc[nt][1]) - 12582912.0f, tot[nt][1]);
+                    tot[nt][2] = fmaf(s.y * c.x, __int_as_float(acc[nt][2]) - 12582912.0f, tot[nt][2]);
+                    tot[nt][3] = fmaf(s.y * c.y, __int_as_float(acc[nt][3]) - 12582912.0f, tot[nt][3]);
+                }
+            }
+        }
+    }
+}
+
 #endif
 
 }  // namespace pp
