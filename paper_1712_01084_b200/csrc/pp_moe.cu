@@ -96,14 +96,19 @@ template <bool BF16> struct Wide {           // 16-bit weights: 16 rows x 32 col
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const uint4 v = x[nt].x[0];
+            // the instruction cuts what its sum cannot hold; over a long row the cuts would add up, all towards zero, so
+            // each unit's sum is rounded into the total
+            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             if (BF16) {
-                mma_bf16(tot[nt], a, v.x, v.y);
-                mma_bf16(tot[nt], b, v.z, v.w);
+                mma_bf16(acc, a, v.x, v.y);
+                mma_bf16(acc, b, v.z, v.w);
             } else {
                 const uint32_t ar[4] = {a.x, a.y, a.z, a.w}, br[4] = {b.x, b.y, b.z, b.w};
-                mma_f16(tot[nt], ar, v.x, v.y);
-                mma_f16(tot[nt], br, v.z, v.w);
+                mma_f16(acc, ar, v.x, v.y);
+                mma_f16(acc, br, v.z, v.w);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tot[nt][i] += acc[i];
         }
     }
 };
