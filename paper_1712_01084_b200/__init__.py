@@ -2,12 +2,13 @@
 as hand-written sm_100a CUDA behind a small C library.
 
 ``synth`` draws seeded inputs; ``binding`` (imported on first attribute access)
-marshals arguments into the C library ``libpp_b200.so``.  There is no CPU or
+marshals arguments into the C library ``libpp_b200.so``; ``decode_block`` is an
+example of the decoder operators.  There is no CPU or
 PyTorch fallback: without the compiled library every call raises.
 """
 import importlib
 
-__all__ = ["synth", "binding"]
+__all__ = ["synth", "binding", "decode_block"]
 
 
 def __getattr__(name):

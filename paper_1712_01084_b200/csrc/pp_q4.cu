@@ -38,9 +38,11 @@ namespace {
 
 constexpr int kWarps = 16, kThreads = kWarps * 32, kMaxStrips = 64, kMaxTokens = 16;
 constexpr int kParkLd = 20;           // floats between parked columns of 16 rows: a warp's 32 values hit 32 banks
-// Units each warp keeps in flight: 4 (70 KB an SM) keep HBM busy.  With one tile of columns a fifth still lets two CTAs share
-// an SM, so that the next call's first units are on their way during this one's end; with 32 columns there is room for 3.
-__host__ __device__ constexpr int depth_of(int nt) { return nt == 4 ? 3 : nt == 1 ? 5 : 4; }
+// Units each warp keeps in flight: 4 (70 KB an SM) keep HBM busy; 7 where x is small, so that more of the next call's weights
+// are on their way during this one's end; with 32 columns there is room for 3.  (7 also leave room for one CTA to an SM
+// only.  With two, the next call's CTAs start beside this one's; 8192 x 8192 then takes 8.7 us a call, but 12 us whenever
+// the CTAs of a call land on one SM twice, which lasts until the stream runs dry.  One: 9.3 us, always.)
+__host__ __device__ constexpr int depth_of(int nt) { return nt == 4 ? 3 : nt == 1 ? 7 : 4; }
 // Columns of the product a vector takes.
 __host__ __device__ constexpr int columns_of(bool bytes, int xtype) { return bytes ? (xtype == PP_I8 ? 1 : 3) : xtype == PP_F32 ? 2 : 1; }
 bool as_bytes(int tokens, int xtype) { return tokens * columns_of(true, xtype) <= 8; }
@@ -165,7 +167,7 @@ __device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, floa
 }
 
 template <bool BYTES, int NT, int SETS, bool ASYM>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) q4_kernel(const Q4Args a) {
+__global__ void __launch_bounds__(kThreads, BYTES ? 2 : 1) q4_kernel(const Q4Args a) {
     extern __shared__ __align__(128) unsigned char smem[];
     constexpr int kDepth = depth_of(NT);
     const int S = (int)cluster_size(), rank = (int)cluster_rank(), cl = S == 1 ? blockIdx.x : blockIdx.x / S;
@@ -174,7 +176,6 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) q4_kernel(const Q4A
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int U = n_s * n_k, u0 = U * warp / kWarps, u1 = U * (warp + 1) / kWarps;
     if (S > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
-    pdl_release();
 
     // the first units of this warp: nothing in them depends on an earlier kernel
     const int ls0 = Divider(n_k).div(u0), kb0 = u0 - ls0 * n_k;
@@ -214,6 +215,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) q4_kernel(const Q4A
     }
 
     pdl_wait();
+    pdl_release();                       // not before the previous call has ended: the one after this must not run ahead of both
     float* cs = reinterpret_cast<float*>(smem + a.cs_off);
     int* sums = reinterpret_cast<int*>(smem + a.sum_off);
     const auto rest = [&] {

@@ -6,6 +6,7 @@
     python -m paper_1712_01084_b200.run_case cfg4 --steps 64 --calls 2
     python -m paper_1712_01084_b200.run_case cfg5 --k 32 --batch 20 --no-tile      # chunked matrix-vector kernel
     python -m paper_1712_01084_b200.run_case cfg5 --k 128 --batch 128 --tile-kernel 2     # clustered tile kernel
+    python -m paper_1712_01084_b200.run_case decode --batch 1 --calls 6                   # norm, 4-bit product, mixture of experts
 
 Calls rotate over `--copies` independent copies of the layer(s) (default: enough to exceed twice the L2, at
 most 4) so that a profiled launch does not find its weights in L2.  Plain launches on the current stream, one
@@ -21,7 +22,7 @@ import numpy as np
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    ap.add_argument("case", choices=["cfg1", "cfg2", "cfg3", "cfg4", "cfg5"])
+    ap.add_argument("case", choices=["cfg1", "cfg2", "cfg3", "cfg4", "cfg5", "decode"])
     ap.add_argument("--k", type=int, default=128, help="cfg5: kept tiles per block-row (of 128)")
     ap.add_argument("--batch", type=int, default=1)
     ap.add_argument("--steps", type=int, default=256, help="cfg4: recurrent steps per call")
@@ -51,6 +52,18 @@ def main():
     def copies_for(weight_bytes):
         return args.copies if args.copies > 0 else max(1, min(4, -(-2 * l2 // max(1, weight_bytes)) + 1))
 
+    if args.case == "decode":
+        from .decode_block import DecodeBlock
+        R = args.copies if args.copies > 0 else 2
+        blocks = [DecodeBlock(2048, 1024, 64, 8, args.batch, "q4") for _ in range(R)]
+        a = torch.randn(args.batch, 2048, device="cuda").bfloat16()
+        h = torch.zeros_like(a)
+        for i in range(args.calls):
+            a, h = blocks[i % R].step(a, h)
+        torch.cuda.synchronize()
+        print(f"decode block 2048, 64 experts of 1024, 8 a token, batch {args.batch}: {args.calls} calls over {R} copies; "
+              f"status {blocks[0].moe.status()}")
+        return
     if args.case == "cfg3":
         wl = synth.config3(batch=args.batch)
         R = copies_for(sum(l.T * l.B * l.B * 2 for l in wl.layers))
