@@ -53,6 +53,7 @@ namespace {
 
 constexpr int kWarps = 16, kThreads = kWarps * 32, kMaxCols = 16;
 constexpr int kMaxExperts = 256, kMaxTopK = 16, kMaxTokens = 32, kActCols = 3, kMaxCap = kMaxCols / kActCols;
+constexpr int kRouterParts = 2;            // of a logit, at most
 constexpr int kSpinPolls = 1 << 24;          // seconds; a barrier that is met never gets near it
 
 struct MoeArgs {
@@ -67,6 +68,7 @@ struct MoeArgs {
     int32_t* ids;
     float* gates;
     int y_type, T, E, H, top_k, renorm, strips1, strips2, kb1, kb2, kpad1, kpad2, router_ld, slot_bytes, cpt, bf16_scales, polls;
+    int router_parts, router_cols;           // parts of a logit, columns of a part
     float per_expert, per_entry;             // 1 / strips1, 1 / kb2
     int round;                               // strips of a round
     int cap;                                 // tokens of an entry, at most
@@ -86,9 +88,6 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint4& a, uint32_t
 template <bool BF16> struct Wide {           // 16-bit weights: 16 rows x 32 columns, two operand fragments of 512 bytes
     static constexpr int kUnitCols = 32, kSetBytes = 0;
     static constexpr bool kBf16 = BF16, kBytes = false, kSwap = false;
-    // The columns' part of a unit (512 bytes a tile) travels in the ring with the weights: read through L1 instead, the first
-    // pass of a CTA over a new expert's columns took twice as long as the others, a trip to L2 per unit.
-    static constexpr bool kRingCols = true;
     template <int STEP> struct Cols { uint4 x[1]; };
     template <int STEP, int NT>
     static __device__ __forceinline__ void unit(float (&tot)[NT][4], const unsigned char* slot, int lane, bool, const Cols<STEP>* x) {
@@ -118,7 +117,6 @@ template <int SETS, bool ASYM> struct Q4 {
     static constexpr int kSets = SETS;
     static constexpr bool kBf16 = false, kBytes = true;       // kBytes: step 1 multiplies whole numbers
     static constexpr bool kSwap = true;                       // columns 4i + 1 and 4i + 2 of act change places
-    static constexpr bool kRingCols = false;                  // as many bytes as the weights and more: no room in the ring
     template <int STEP> struct Cols {                         // step 1: 16 bytes of each 64 columns; sums and scales of two result columns
         uint4 x[STEP == 1 ? 2 : 4];
         alignas(16) int meta[2][STEP == 1 ? kMeta : 4];
@@ -136,9 +134,13 @@ template <int SETS, bool ASYM> struct Q4 {
     }
 };
 
-// Units in flight per warp.  Where entries have one or two tokens one tile of 8 columns will do (three columns of act each),
-// others need two.
-template <class W, int TILES> __host__ __device__ constexpr int depth() { return W::kRingCols && TILES == 2 ? 4 : 6; }
+// The columns of 16-bit experts' units (512 bytes a tile) travel in the ring with the weights: read through L1 instead, the
+// first pass of a CTA over a new expert's columns took twice as long as the others, a trip to L2 per unit.  4-bit experts
+// read the tokens' bytes in step 1 from shared memory, where they are few enough, and act in step 2 through L1, a unit
+// ahead (2 KB a tile beside 1 KB of weights: in a ring of three units, all that fit, step 2 took 5 % longer).
+__host__ __device__ constexpr int pad128(int n) { return (n + 127) / 128 * 128; }       // slots and their parts start on 128 bytes
+// Units in flight per warp.
+template <class W, int TILES> __host__ __device__ constexpr int depth() { return !W::kBytes && TILES == 2 ? 4 : 6; }
 
 // ---- small helpers -----------------------------------------------------------------------------------------------
 // Grid barrier in two parts.  After the second every CTA of the grid has passed the first and what it wrote before is
@@ -267,20 +269,20 @@ template <int SETS, int META, typename T, bool VEC> __device__ __forceinline__ v
     if (threadIdx.x == 0) a.xscale[token] = 1.0f;
 }
 
-// A warp's logit of one (token, expert); what cannot be compared ranks last.  Eight loads of each row are in flight.
-template <typename T, bool VEC> __device__ __forceinline__ void router_logit(const MoeArgs& a, int token, int expert) {
-    constexpr int kAhead = VEC ? 8 : 1;
+// A warp's part of the logit of one (token, expert): columns from .. to.
+template <typename T, bool VEC> __device__ __forceinline__ float router_part(const MoeArgs& a, int token, int expert, int from, int to) {
+    constexpr int kAhead = VEC ? 4 : 1;
     const int lane = threadIdx.x & 31;
     const float* r = a.router + (int64_t)expert * a.router_ld;
     const T* row = static_cast<const T*>(a.in.x) + (int64_t)token * a.in.ld;
     float sum = 0.0f;
 #pragma unroll 1
-    for (int c0 = lane * 4; c0 < a.H; c0 += kAhead * 128) {
+    for (int c0 = from + lane * 4; c0 < to; c0 += kAhead * 128) {
         Pack<T, 4> x[kAhead];
         float4 w[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            x[i] = load_four<VEC>(row, c0 + i * 128, a.H);                 // zeros past the end: the router's row may repeat there
+            x[i] = load_four<VEC>(row, c0 + i * 128, to);                  // zeros past the end: the router's row may repeat there
             w[i] = __ldg(reinterpret_cast<const float4*>(r + min(c0 + i * 128, a.router_ld - 4)));
         }
 #pragma unroll
@@ -293,17 +295,21 @@ template <typename T, bool VEC> __device__ __forceinline__ void router_logit(con
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) a.logits[token * a.E + expert] = sum == sum ? sum : -INFINITY;
+    return sum;
 }
 
-// Router pairs go to warp 0 of every CTA, the last CTA first (the first ones have tokens to turn into columns), then warp 1.
+// Parts of logits go to warp 0 of every CTA, the last CTA first (the first ones have tokens to turn into columns), then to
+// warp 1 and so on; a row is cut into as many parts as keep every warp at one.
 template <class W, typename T, bool VEC> __device__ __forceinline__ void step0(const MoeArgs& a, float* part) {
     for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
         if constexpr (W::kBytes) token_bytes<W::kSets, W::kMeta, T, VEC>(a, t);
         else token_columns<W, T, VEC>(a, t, part);
     }
-    for (int i = (threadIdx.x >> 5) * gridDim.x + (gridDim.x - 1 - blockIdx.x); i < a.T * a.E; i += kWarps * gridDim.x)
-        router_logit<T, VEC>(a, i / a.E, i % a.E);
+    for (int i = (threadIdx.x >> 5) * gridDim.x + (gridDim.x - 1 - blockIdx.x); i < a.T * a.E * a.router_parts; i += kWarps * gridDim.x) {
+        const int k = i / (a.T * a.E), pair = i - k * a.T * a.E, from = k * a.router_cols;
+        const float v = router_part<T, VEC>(a, pair / a.E, pair % a.E, from, min(a.H, from + a.router_cols));
+        if ((threadIdx.x & 31) == 0) a.logits[i] = v;
+    }
 }
 template <class W, typename T> __device__ __forceinline__ void step0(const MoeArgs& a, float* part) {
     if (a.in.vec) step0<W, T, true>(a, part);
@@ -350,13 +356,18 @@ __device__ __forceinline__ Lists lists_at(unsigned char* p, int T, int E, int to
 // equal ones the lowest index; lane j keeps the j-th.  Then the softmax over them, or over all.
 template <int kEach> __device__ __forceinline__ void choose(const MoeArgs& a, const Lists& L, int t) {       // kEach: logits of a lane
     const int lane = threadIdx.x & 31;
-    const float* row = a.logits + t * a.E;
+    const float* row = a.logits + t * a.E;                   // [part][token][expert]
     uint32_t key[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         key[i] = 0u;                                         // below every logit
         if (i * 32 + lane < a.E) {
-            const uint32_t u = __float_as_uint(__ldcg(row + i * 32 + lane));
+            float v[kRouterParts], l = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kRouterParts; ++k) v[k] = k < a.router_parts ? __ldcg(row + k * a.T * a.E + i * 32 + lane) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < kRouterParts; ++k) l += v[k];
+            const uint32_t u = __float_as_uint(l == l ? l : -INFINITY);    // what cannot be compared ranks last
             key[i] = (int)u < 0 ? ~u : u | 0x80000000u;
         }
     }
@@ -589,7 +600,7 @@ template <class W, int STEP, int TILES> struct Fetcher {
                 unit = r.unit + lane * 16;
                 sets = r.sets + lane * 16;
                 if (TILES > 1) tiles = (L.entry[r.entry].z * (STEP == 1 ? a.cpt : kActCols) + 7) / 8;
-                if (W::kRingCols) from.set(a, L, r, lane, tiles);
+                if (!W::kBytes) from.set(a, L, r, lane, tiles);
             }
         }
         if (left) {
@@ -601,7 +612,7 @@ template <class W, int STEP, int TILES> struct Fetcher {
             }
             unit += 1024;
             sets += W::kSetBytes;
-            if (W::kRingCols) {
+            if (!W::kBytes) {
 #pragma unroll
                 for (int nt = 0; nt < TILES; ++nt)
                     if (cols && nt < tiles) cp_async16_l1(slot + 1024 + nt * 512, from.x[nt]);
@@ -630,6 +641,7 @@ __device__ __forceinline__ void finish_y(const MoeArgs& a, int strip, int row, i
 template <class W, int STEP, int TILES>
 __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const Span& s, Fetcher<W, STEP, TILES>& f, unsigned char* smem) {
     constexpr int kDepth = depth<W, TILES>(), kCols = 8 * TILES;
+    constexpr bool kRing = !W::kBytes;                       // columns come with the weights
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int cpt = STEP == 1 ? a.cpt : kActCols, width = STEP == 1 ? a.cap : a.T;
     unsigned char *ring = smem + warp * kDepth * a.slot_bytes, *ring_end = ring + kDepth * a.slot_bytes, *at = ring;
@@ -661,7 +673,7 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
             x += run.left;
             entry = L.entry[run.entry];
             tiles = TILES == 1 ? 1 : (entry.z * cpt + 7) / 8;
-            if (!W::kRingCols) {
+            if (!kRing) {
                 from.set(a, L, run, lane, tiles);
                 from.read(xr, tiles);
             }
@@ -670,8 +682,8 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
         while (run.left) {
             do {
                 cp_wait<kDepth - 1>();
-                if (!W::kRingCols) __syncwarp();               // sets are read by other lanes than copied them; nothing else is
-                if (W::kRingCols) {
+                if (W::kBytes) __syncwarp();                   // sets are read by other lanes than copied them; nothing else is
+                if (kRing) {
 #pragma unroll
                     for (int nt = 0; nt < TILES; ++nt)
                         if (nt < tiles) xr[nt].x[0] = *reinterpret_cast<const uint4*>(at + 1024 + nt * 512 + lane * 16);
@@ -679,11 +691,11 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
                 if (TILES == 1 || tiles == 1) W::template unit<STEP, 1>(reinterpret_cast<float(&)[1][4]>(tot), at, lane, a.bf16_scales != 0, xr);
                 else W::template unit<STEP, TILES>(tot, at, lane, a.bf16_scales != 0, xr);
                 --run.left;
-                if (!W::kRingCols && run.left) {                   // in flight while the other warps compute
+                if (!kRing && run.left) {                   // in flight while the other warps compute
                     from.advance();
                     from.read(xr, tiles);
                 }
-                if (!W::kRingCols) __syncwarp();
+                if (W::kBytes) __syncwarp();
                 f.next(a, L, s, warp, lane, smem_addr(at) + lane * 16, true, true);
                 at += a.slot_bytes;
                 if (at == ring_end) at = ring;
@@ -721,21 +733,30 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
         }
         __syncthreads();
 
-        // the pieces of a row in the order of the warps
+        // The pieces of a row in the order of the warps.  With fewer strips than warps a strip has many: then four lanes take
+        // every fourth warp's and add theirs up (16 reads behind one another took 1,000 cycles).
+        const bool four = rs < kWarps;
+        const int shift = four ? 2 : 0, sub = four ? tid & 3 : 0;
         const auto pieces = [&](uint32_t mask, int q, int at) {
             float v = 0.0f;
-            for (; mask; mask &= mask - 1) v += park[(__ffs((int)mask) - 1 + q) * 16 * width + at];
+            for (mask &= four ? 0x1111u << sub : 0xffffu; mask; mask &= mask - 1) v += park[(__ffs((int)mask) - 1 + q) * 16 * width + at];
+            if (four) {
+                v += __shfl_xor_sync(0xffffffffu, v, 1);
+                v += __shfl_xor_sync(0xffffffffu, v, 2);
+            }
             return v;
         };
         // a divided strip's slot among this CTA's parts: 0 where an earlier CTA has begun it
         const auto cut = [&](int ls) { return (ls == 0 && cut_first) || (ls == s.strips - 1 && cut_last); };
         const auto part = [&](int ls) { return my_parts + (ls == 0 && cut_first ? 0 : 16 * width); };
         if (STEP == 1) {
-            for (int o = tid >> 1; o < rs * 8; o += kThreads / 2) {        // two threads to a strip's row: even and odd pairs
+            for (int o = tid >> shift; o < rs * 8; o += kThreads >> shift) {               // four: a warp has the eight rows of one strip
                 const int q = o >> 3, row = o & 7, ls = ls0 + q;
                 const int2 plan = L.plan[q];
-                for (int pl = tid & 1; pl < L.entry[plan.y].z; pl += 2) {
+                const int pairs = L.entry[plan.y].z;
+                for (int pl = 0; pl < pairs; ++pl) {
                     const float gate = pieces((uint32_t)plan.x, q, pl * 16 + row), up = pieces((uint32_t)plan.x, q, pl * 16 + row + 8);
+                    if (four && sub != (pl & 3)) continue;
                     if (!cut(ls)) {
                         finish_act<W>(a, L, plan.y, s.first + ls, row, pl, gate, up);
                     } else {
@@ -745,11 +766,12 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
                 }
             }
         } else {
-            const int per_strip = 16 * a.T;
+            const int per_strip = 16 * a.T, outs = rs * per_strip;
             const Divider by_strip(per_strip);
-            for (int o = tid; o < rs * per_strip; o += kThreads) {
+            for (int o = tid >> shift; o < outs; o += kThreads >> shift) {                 // four: outs is a multiple of the warp's eight
                 const int q = by_strip.div(o), r = o - q * per_strip, ls = ls0 + q;
                 const float v = pieces((uint32_t)L.plan[q].x, q, r);
+                if (sub) continue;
                 if (!cut(ls)) finish_y(a, s.first + ls, r & 15, r >> 4, v);
                 else __stcg(part(ls) + r, v);
             }
@@ -806,7 +828,6 @@ template <class W, int STEP> __device__ __forceinline__ void join(const MoeArgs&
 }
 
 template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe_kernel(const MoeArgs a) {
-    constexpr int kDepth = depth<W, TILES>();
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float part[kWarps];
     __shared__ int flag;
@@ -849,6 +870,7 @@ template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe
             cp_wait<0>();
             __syncthreads();
         }
+        constexpr int kDepth = depth<W, TILES>();
         const uint32_t ring = smem_addr(smem) + warp * kDepth * a.slot_bytes + lane * 16;
         {
             const Span s = span_of(entries * a.strips1, a.kb1, a.round);
@@ -866,12 +888,12 @@ template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe
         for (int d = 0; d < kDepth; ++d) f.next(a, L, s, warp, lane, ring + d * a.slot_bytes, true, false);
         ok = grid_wait(a.sync + 1, a.sync + 3, a.polls, &flag);
         if (ok) {
-            if (W::kRingCols) {
+            if (!W::kBytes) {
 #pragma unroll 1
                 for (int d = 0; d < kDepth; ++d) g.next(a, L, s, warp, lane, ring + d * a.slot_bytes, false, true);
             }
             if (!s.whole) find_cuts(L, s, (int64_t)a.strips2 * entries * a.kb2);
-            stream<W, 2, TILES>(a, L, s, W::kRingCols ? g : f, smem);
+            stream<W, 2, TILES>(a, L, s, W::kBytes ? f : g, smem);
             if (!s.whole) join<W, 2>(a, L, s);
         }
         cp_wait<0>();
@@ -934,8 +956,8 @@ int tiles_of(int tokens, int cap) { return std::min(tokens, cap) * kActCols <= 8
 constexpr int kMaxSmem = 227 * 1024 - 256;       // beside the kernel's few static bytes
 
 // Strips of a round and the shared memory: the most strips that fit, 32 at most.
-size_t plan_smem(MoeArgs& a, int depth, int tiles, int meta) {
-    size_t at = (size_t)kWarps * depth * a.slot_bytes;
+size_t plan_smem(MoeArgs& a, int ring, int tiles, int meta) {
+    size_t at = (size_t)kWarps * ring;
     a.list_off = (int)(at = (at + 127) / 128 * 128);
     at += list_bytes(a.T, a.E, a.top_k);
     a.scr_off = (int)at;
@@ -1010,7 +1032,7 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
     if (st == PP_OK &&
         (!alloc(&L->gate_up, units1 * 1024) || !alloc(&L->down, units2 * 1024) ||
          (set_bytes && (!alloc(&L->gate_up_sets, units1 * set_bytes) || !alloc(&L->down_sets, units2 * set_bytes))) || !alloc(&L->router, ld * E * 4) ||
-         !alloc(&L->logits, (size_t)max_tokens * E * 4) || !alloc(&L->xscale, (size_t)max_tokens * 4) ||
+         !alloc(&L->logits, (size_t)max_tokens * E * kRouterParts * 4) || !alloc(&L->xscale, (size_t)max_tokens * 4) ||
          !alloc(&L->xcols, (size_t)max_tokens * 3 * L->kb1 * cols * 2) || !alloc(&L->acols, abytes) ||
          (wtype < 0 && !alloc(&L->xmeta, (size_t)max_tokens * 3 * L->kb1 * 32)) ||
          !alloc(&L->parts, (size_t)L->ctas * 2 * 16 * std::max(kMaxCap, max_tokens) * 4) || !alloc(&L->sync, sync_bytes))) {
@@ -1117,9 +1139,13 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     a.kpad1 = L->kb1 * cols;
     a.kpad2 = L->kb2 * cols;
     a.router_ld = (L->H + 3) / 4 * 4;
+    a.router_parts = std::max(1, std::min({kRouterParts, L->ctas * kWarps / (tokens * L->E), (L->H + 127) / 128}));
+    a.router_cols = ((L->H + a.router_parts - 1) / a.router_parts + 127) / 128 * 128;
     a.cap = cap_of(tokens, L->top_k, L->E);
-    const int tiles = tiles_of(tokens, a.cap), depth = q4 || tiles == 1 ? 6 : 4;        // as depth() of the kernel
-    a.slot_bytes = 1024 + (q4 ? (q4_set_bytes(L->sets, L->asym) + 127) / 128 * 128 : 512 * tiles);      // slots start on 128 bytes
+    const int tiles = tiles_of(tokens, a.cap);
+    const Kernel kernel = tiles == 1 ? pick_kernel<1>(L) : pick_kernel<2>(L);
+    a.slot_bytes = 1024 + (q4 ? pad128(q4_set_bytes(L->sets, L->asym)) : 512 * tiles);
+    const int ring = (!q4 && tiles == 2 ? 4 : 6) * a.slot_bytes;           // as depth() of the kernel
     a.gate_up_sets = L->gate_up_sets;
     a.down_sets = L->down_sets;
     a.cpt = q4 ? 3 : L->wtype == PP_BF16 ? (x_type == PP_BF16 ? 1 : x_type == PP_F16 ? 2 : 3) : (x_type == PP_F32 ? 2 : 1);
@@ -1136,11 +1162,11 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(L->ctas);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = plan_smem(a, depth, tiles, !q4 ? 0 : L->sets == 1 ? 2 : L->sets == 2 ? 4 : 8);        // as kMeta
+    cfg.dynamicSmemBytes = plan_smem(a, ring, tiles, !q4 ? 0 : L->sets == 1 ? 2 : L->sets == 2 ? 4 : 8);        // as kMeta
     cfg.stream = static_cast<cudaStream_t>(cuda_stream);
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, tiles == 1 ? pick_kernel<1>(L) : pick_kernel<2>(L), a) == cudaSuccess) return PP_OK;
+    if (cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess) return PP_OK;
     cudaGetLastError();
     return PP_ERR_CUDA;
 }
