@@ -948,9 +948,12 @@ template <int TILES> Kernel pick_kernel(const pp_moe* L) {
     if (L->sets == 2) return L->asym ? moe_kernel<Q4<2, true>, TILES> : moe_kernel<Q4<2, false>, TILES>;
     return L->asym ? moe_kernel<Q4<1, true>, TILES> : moe_kernel<Q4<1, false>, TILES>;
 }
-// Tokens of an entry: what two tiles of columns hold, or what one does where few experts have more tokens than that (their
-// weights are then read again): up to one token to an expert on average.
-int cap_of(int tokens, int top_k, int E) { return tokens * top_k <= E ? 8 / kActCols : kMaxCap; }
+// Tokens of an entry: what two tiles of columns hold, or what one does, two, where few experts have more than that (their
+// weights are then read again, from L2).  16-bit experts, bound by HBM, take two while they have less than a token each on
+// average (64 experts of 2048 x 1024, 8 a token: 4 tokens 61.7 us with two, 62.5 with five; 8 tokens 101.8 and 98.4); 4-bit
+// experts, bound by the products, up to two tokens each (4 tokens 33.8 and 41.5 us, 16 tokens 77.7 and 83.6; 8 experts of
+// 4096 x 2048, 4 tokens each, 69.3 and 57.9).
+int cap_of(int tokens, int top_k, int E, bool q4) { return (q4 ? tokens * top_k <= 2 * E : tokens * top_k < E) ? 8 / kActCols : kMaxCap; }
 int tiles_of(int tokens, int cap) { return std::min(tokens, cap) * kActCols <= 8 ? 1 : 2; }
 
 constexpr int kMaxSmem = 227 * 1024 - 256;       // beside the kernel's few static bytes
@@ -1141,7 +1144,7 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     a.router_ld = (L->H + 3) / 4 * 4;
     a.router_parts = std::max(1, std::min({kRouterParts, L->ctas * kWarps / (tokens * L->E), (L->H + 127) / 128}));
     a.router_cols = ((L->H + a.router_parts - 1) / a.router_parts + 127) / 128 * 128;
-    a.cap = cap_of(tokens, L->top_k, L->E);
+    a.cap = cap_of(tokens, L->top_k, L->E, q4);
     const int tiles = tiles_of(tokens, a.cap);
     const Kernel kernel = tiles == 1 ? pick_kernel<1>(L) : pick_kernel<2>(L);
     a.slot_bytes = 1024 + (q4 ? pad128(q4_set_bytes(L->sets, L->asym)) : 512 * tiles);
