@@ -649,19 +649,25 @@ def pp_pivot_find(abs_w, levels: int, max_sweeps: int = 32, row_init=None, col_i
 
 
 # ------------------------------------------------------------ decoder operators
-# These calls are a few microseconds on the GPU, so what the host does per call counts: torch and the library are looked
-# up once, and every check is one attribute of the tensor.
+# These calls are a few microseconds on the GPU, so what the host does per call counts: the calls' checks, their new
+# tensors and the C call are in csrc/torch/pp_torch.cpp, which gets the C functions' addresses from the loaded library.
 _torch = None
+_fast = None        # the module _pp_torch
 _TYPES = {}         # torch dtype -> pp_dtype_t
 
 
 def _load_torch():
-    global _torch
+    global _torch, _fast
     import torch
+    library = lib()
+    try:
+        from . import _pp_torch
+    except ImportError as e:
+        raise ImportError("_pp_torch.so: build it with `python -m paper_1712_01084_b200.build`") from e
+    _pp_torch.init(*(ctypes.cast(f, ctypes.c_void_p).value for f in (library.pp_rmsnorm_q8, library.pp_q4_forward, library.pp_moe_forward)))
     _TYPES.update({torch.float32: PP_F32, torch.float16: PP_F16, torch.bfloat16: PP_BF16, torch.int8: PP_I8,
                    torch.float8_e4m3fn: PP_E4M3})
-    _torch = torch
-    lib()
+    _fast, _torch = _pp_torch, torch
     return torch
 
 
@@ -675,19 +681,6 @@ def _type_of(dtype, name="tensor") -> int:
 def _raw_stream(device: int, stream=None) -> int:
     """Handle of the stream to enqueue on: the given one, or the current one of a device."""
     return _torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
-
-
-def _rows(x, cols, name, device):
-    """(rows, distance of rows) of a CUDA matrix [rows][cols] whose rows are contiguous; a vector is one row."""
-    shape = x.shape
-    if len(shape) == 2 and shape[1] == cols and x.get_device() == device >= 0:
-        if x.is_contiguous():
-            return shape[0], cols
-        if cols == 1 or x.stride(1) == 1:
-            return shape[0], (x.stride(0) if shape[0] > 1 else cols)
-    elif len(shape) == 1 and shape[0] == cols and x.get_device() == device >= 0 and x.is_contiguous():
-        return 1, cols
-    raise ValueError(f"{name} must be a CUDA tensor [rows][{cols}] with contiguous rows" + ("" if device < 0 else f" on device {device}"))
 
 
 def _plain(t, shape, name, device, dtypes=None):
@@ -707,48 +700,12 @@ def pp_rmsnorm_q8(x, weight, residual=None, eps: float = 1e-6, codes: str = "e4m
     "e4m3" or "int8"; group 0 (a scale per row) or 128 columns.  Returns (codes, scales, hidden), with the normalised
     rows in x's type as a fourth where `normed` is set.  hidden is x + residual in x's type: a new tensor, or hidden_out
     (which may be residual or x); without a residual it is None unless hidden_out is given."""
-    torch = _torch or _load_torch()
-    shape, device, dtype = x.shape, x.get_device(), x.dtype
-    cols = shape[-1]
-    plain = x.is_contiguous()
-    rows, ldx = _rows(x, cols, "x", device)
-    dt, wdt = _TYPES.get(dtype), _TYPES.get(weight.dtype)
-    if dt is None or wdt is None:
-        raise TypeError(f"x, weight: {dtype}, {weight.dtype} are no types of the library")
-    if weight.get_device() != device or weight.numel() != cols or not weight.is_contiguous():
-        raise ValueError(f"weight must be a contiguous CUDA tensor [{cols}] on device {device}")
-    if codes == "e4m3":
-        code, code_dtype = PP_E4M3, torch.float8_e4m3fn
-    elif codes == "int8":
-        code, code_dtype = PP_I8, torch.int8
-    else:
-        raise ValueError("codes must be 'e4m3' or 'int8'")
-    like = x if plain else x.new_empty(shape)                # empty_like of a contiguous tensor takes the least time
-    q = torch.empty_like(like, dtype=code_dtype)
-    ldr = ldh = 0
-    rp = hp = np_ = n = None
-    if residual is not None:
-        if residual.dtype != dtype or residual.shape != shape:
-            raise TypeError("residual must have x's shape and type")
-        ldr, rp = _rows(residual, cols, "residual", device)[1], residual.data_ptr()
-        if hidden_out is None:
-            hidden_out = torch.empty_like(like)
-            ldh, hp = cols, hidden_out.data_ptr()
-    if hidden_out is not None and hp is None:
-        if hidden_out.dtype != dtype or hidden_out.shape != shape:
-            raise TypeError("hidden_out must have x's shape and type")
-        ldh, hp = _rows(hidden_out, cols, "hidden_out", device)[1], hidden_out.data_ptr()
-    groups = -(-cols // group) if group > 0 else 1
-    scales = x.new_empty((rows, groups) if len(shape) == 2 else (groups,), dtype=torch.float32)
-    if normed:
-        n = torch.empty_like(like)
-        np_ = n.data_ptr()
-    st = _lib.pp_rmsnorm_q8(x.data_ptr(), ldx, rp, ldr, weight.data_ptr(), dt, wdt, rows, cols, eps, code, group, q.data_ptr(),
-                            scales.data_ptr(), hp, ldh, np_,
-                            torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
-    if st:
-        raise PPError(st, "pp_rmsnorm_q8")
-    return (q, scales, hidden_out, n) if normed else (q, scales, hidden_out)
+    if _fast is None:
+        _load_torch()
+    r = _fast.rmsnorm_q8(x, weight, residual, eps, codes, group, hidden_out, normed, None if stream is None else stream.cuda_stream)
+    if r.__class__ is int:
+        raise PPError(r, "pp_rmsnorm_q8")
+    return r
 
 
 class Q4Layer:
@@ -801,34 +758,11 @@ def pp_q4_forward(layer: Q4Layer, x, act: int = PP_ACT_IDENTITY, x_scales=None, 
     """y[batch][M] = act(W x + b) with 4-bit weights.  x: [batch][N] (or [N]) float32, float16, bfloat16, or int8 /
     float8_e4m3fn with x_scales, float32 [batch][1] or [batch][ceil(N/128)], as pp_rmsnorm_q8 returns them.  y is
     float32 unless out_dtype (or out) says float16 or bfloat16.  Enqueues on the current stream."""
-    torch = _torch
-    device = layer.device
-    batch, ldx = _rows(x, layer.N, "x", device)
-    x_group, sp = 0, None
-    if x_scales is not None:
-        n, groups = x_scales.numel(), -(-layer.N // 128)
-        if n == batch:
-            x_group = 0
-        elif n == batch * groups:
-            x_group = 128
-        else:
-            raise ValueError(f"x_scales must hold 1 or {groups} values per row of x")
-        if x_scales.get_device() != device or not x_scales.is_contiguous() or x_scales.dtype != torch.float32:
-            raise ValueError("x_scales must be a contiguous float32 CUDA tensor on the layer's device")
-        sp = x_scales.data_ptr()
-    if out is None:
-        out = x.new_empty((batch, layer.M), dtype=out_dtype or torch.float32)
-    elif (out.get_device() != device or not out.is_contiguous() or out.numel() != batch * layer.M or
-          (out_dtype is not None and out.dtype != out_dtype)):
-        raise ValueError("out must be a contiguous CUDA tensor [batch][M] of out_dtype")
-    xt, yt = _TYPES.get(x.dtype), _TYPES.get(out.dtype)
-    if xt is None or yt is None:
-        raise TypeError(f"x, out: {x.dtype}, {out.dtype} are no types of the library")
-    st = _lib.pp_q4_forward(layer._h, x.data_ptr(), ldx, xt, sp, x_group, out.data_ptr(), yt, batch, act,
-                            torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
-    if st:
-        raise PPError(st, "pp_q4_forward")
-    return out
+    r = _fast.q4_forward(layer._h.value, layer.M, layer.N, layer.device, x, act, x_scales, out_dtype, out,
+                         None if stream is None else stream.cuda_stream)
+    if r.__class__ is int:
+        raise PPError(r, "pp_q4_forward")
+    return r
 
 
 class MoELayer:
@@ -914,24 +848,8 @@ def pp_moe_forward(layer: MoELayer, x, out_dtype=None, out=None, routing: bool =
     """y[tokens][H] of a mixture-of-experts layer (pp_moe_forward).  x: [tokens][H] (or [H]) float32, float16 or bfloat16;
     y in x's type unless out_dtype (or out) says another.  routing: also returns the chosen experts, int32 [tokens][top_k],
     and their weights, float32.  Enqueues on the current stream."""
-    torch = _torch
-    device = layer.device
-    tokens, ldx = _rows(x, layer.H, "x", device)
-    if out is None:
-        out = x.new_empty((tokens, layer.H), dtype=out_dtype or x.dtype)
-    elif (out.get_device() != device or not out.is_contiguous() or out.numel() != tokens * layer.H or
-          (out_dtype is not None and out.dtype != out_dtype)):
-        raise ValueError("out must be a contiguous CUDA tensor [tokens][H] of out_dtype")
-    ids = gates = None
-    if routing:
-        ids = x.new_empty((tokens, layer.top_k), dtype=torch.int32)
-        gates = x.new_empty((tokens, layer.top_k), dtype=torch.float32)
-    xt, yt = _TYPES.get(x.dtype), _TYPES.get(out.dtype)
-    if xt is None or yt is None:
-        raise TypeError(f"x, out: {x.dtype}, {out.dtype} are no types of the library")
-    st = _lib.pp_moe_forward(layer._h, x.data_ptr(), ldx, xt, out.data_ptr(), yt, tokens, ids.data_ptr() if routing else None,
-                             gates.data_ptr() if routing else None,
-                             torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
-    if st:
-        raise PPError(st, "pp_moe_forward")
-    return (out, ids, gates) if routing else out
+    r = _fast.moe_forward(layer._h.value, layer.H, layer.top_k, layer.device, x, out_dtype, out, routing,
+                          None if stream is None else stream.cuda_stream)
+    if r.__class__ is int:
+        raise PPError(r, "pp_moe_forward")
+    return r

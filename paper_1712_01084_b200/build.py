@@ -1,4 +1,5 @@
-"""Compile the CUDA sources under csrc/ into libpp_b200.so (sm_100a only)."""
+"""Compile the CUDA sources under csrc/ into libpp_b200.so (sm_100a only), and csrc/torch/ into _pp_torch.so, the entry of the
+decoder operators for PyTorch tensors."""
 from __future__ import annotations
 
 import glob
@@ -10,6 +11,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpp_b200.so")
+TORCH_SRC = os.path.join(CSRC, "torch", "pp_torch.cpp")
+TORCH_LIB = os.path.join(HERE, "_pp_torch.so")
 
 
 def sources():
@@ -25,7 +28,28 @@ def needs_build() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_torch(force: bool = False) -> str:
+    """The extension module: plain C++ against the headers of the installed PyTorch."""
+    newest = max(os.path.getmtime(TORCH_SRC), os.path.getmtime(os.path.join(ROOT, "include", "pp.h")))
+    if not force and os.path.exists(TORCH_LIB) and os.path.getmtime(TORCH_LIB) >= newest:
+        return TORCH_LIB
+    import sysconfig
+    import torch
+    base = torch.__path__[0]
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    include = [os.path.join(ROOT, "include"), os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"),
+               os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    lib = os.path.join(base, "lib")
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
+                          [x for d in include for x in ("-isystem" if d.startswith(base) else "-I", d)] +
+                          ["-o", TORCH_LIB, TORCH_SRC, "-L" + lib, "-Wl,-rpath," + lib, "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda",
+                           "-lc10"])
+    return TORCH_LIB
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_torch(force)
     if not force and not needs_build():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
