@@ -55,6 +55,7 @@ struct Q4Args {
     XIn in;
     void* y;
     int y_type, act, tokens, nc;          // nc: columns of the staged input
+    int y_vec;                            // four results of a vector lie in one access
     int M, blocks, slot_bytes, bf16_scales;
     int strips_each, strips_more;         // a cluster has strips_each strips, the first strips_more of them one more
     int blocks_each, blocks_more;         // the same for a CTA of a cluster and the blocks of the columns
@@ -71,16 +72,30 @@ __device__ __forceinline__ uint32_t cluster_size() {
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void st_cluster(uint32_t local, uint32_t rank, float v) {
+template <typename V> __device__ __forceinline__ void st_cluster(uint32_t local, uint32_t rank, const V& v) {     // 1 or 4 floats
     uint32_t remote;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(rank));
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote), "f"(v) : "memory");
+    if constexpr (sizeof(V) == 4) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote), "f"(v.v[0]) : "memory");
+    else asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(remote), "f"(v.v[0]), "f"(v.v[1]), "f"(v.v[2]), "f"(v.v[3]) : "memory");
 }
 
-__device__ __forceinline__ void store_y(void* y, int64_t i, int type, float v) {
-    if (type == PP_F32) static_cast<float*>(y)[i] = v;
-    else if (type == PP_F16) static_cast<__half*>(y)[i] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16*>(y)[i] = __float2bfloat16_rn(v);
+// N results from i on, the first n of them; in one access where vec says so.
+template <typename T, int N> __device__ __forceinline__ void store_as(T* y, const Pack<float, N>& v, int n, bool vec) {
+    Pack<T, N> p;
+#pragma unroll
+    for (int i = 0; i < N; ++i) p.v[i] = from_float<T>(v.v[i]);
+    if (vec) {
+        *reinterpret_cast<Pack<T, N>*>(y) = p;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n) y[i] = p.v[i];
+    }
+}
+template <int N> __device__ __forceinline__ void store_y(void* y, int64_t i, int type, const Pack<float, N>& v, int n, bool vec) {
+    if (type == PP_F32) store_as(static_cast<float*>(y) + i, v, n, vec);
+    else if (type == PP_F16) store_as(static_cast<__half*>(y) + i, v, n, vec);
+    else store_as(static_cast<__nv_bfloat16*>(y) + i, v, n, vec);
 }
 
 // A warp's block of 128 columns of one vector in binary16, four per lane, columns 4i + 1 and 4i + 2 exchanged; rest: what
@@ -166,6 +181,7 @@ __device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, floa
     else stage_rows<T, false, BYTES, NT, SETS>(a, xs, cs, sums, k0, n_k, warp, lane, then);
 }
 
+// (64 registers a thread with bytes: 8192 x 8192 takes 9.7 us, with the 70 to 80 that it would use 9.95)
 template <bool BYTES, int NT, int SETS, bool ASYM>
 __global__ void __launch_bounds__(kThreads, BYTES ? 2 : 1) q4_kernel(const Q4Args a) {
     extern __shared__ __align__(128) unsigned char smem[];
@@ -201,8 +217,9 @@ __global__ void __launch_bounds__(kThreads, BYTES ? 2 : 1) q4_kernel(const Q4Arg
         cp_commit();
     };
     // (with more vectors the rest of the ring is requested behind x, which it would hold back: 4096 x 9216, eight vectors,
-    // 12.6 -> 11.1 us; one vector is small and loses by it, 4096 x 4096 5.7 -> 5.9 us)
-    constexpr int kEarly = BYTES ? kDepth : 3;
+    // 12.6 us for all of it before x, 10.2 for two; 8192 x 8192, sixteen f32 vectors, 25.2 and 23.5.  One vector is small
+    // and loses by it: 4096 x 4096 5.7 -> 5.9 us)
+    constexpr int kEarly = BYTES ? kDepth : 2;
 #pragma unroll
     for (int d = 0; d < kEarly; ++d) fetch(smem_addr(ring) + d * a.slot_bytes + lane * 16);
     // which warps have units of each strip: half a warp looks at one
@@ -289,24 +306,34 @@ __global__ void __launch_bounds__(kThreads, BYTES ? 2 : 1) q4_kernel(const Q4Arg
     cp_wait<0>();
     __syncthreads();
 
-    // add the warps' pieces of every row in warp order; each CTA of the cluster finishes an equal part of the results
-    const int rows = n_s * 16, outs = rows * a.tokens, share = S == 1 ? outs : (outs + S - 1) / S;
+    // add the warps' pieces of every row in warp order; each CTA of the cluster finishes an equal part of the results.  With
+    // more vectors a thread has four rows (8192 x 8192, sixteen f32 vectors: one row 29.0 us a call, four 25.5); one vector leaves most
+    // threads without a row then (4096 x 4096: 4.9 and 5.3 us).
+    constexpr int kRows = BYTES ? 1 : 4;
+    using Rows = Pack<float, kRows>;
+    const int per_token = n_s * (16 / kRows), outs = per_token * a.tokens, share = S == 1 ? outs : (outs + S - 1) / S;
     const int first = rank * share, last = min(outs, first + share);
     const int cpt = parked == a.tokens ? 1 : 3;              // parked columns of a vector
-    const Divider by_rows(rows), by_share(share);
-    float* red = reinterpret_cast<float*>(smem + a.red_off);
-    float bias = 0.0f;                                       // of this thread's first result: on its way during the barrier
-    if (a.bias && first + tid < last) {
-        const int m = s0 * 16 + (first + tid - by_rows.div(first + tid) * rows);
-        if (m < a.M) bias = __ldg(a.bias + m);
-    }
+    const Divider by_token(per_token), by_share(share);
+    Rows* red = reinterpret_cast<Rows*>(smem + a.red_off);
+    Rows bias{};                                             // of this thread's first results: on their way during the barrier
+    const auto row_of = [&](int o) { return s0 * 16 + (o - by_token.div(o) * per_token) * kRows; };
+    const auto load_bias = [&](int m) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+            if (m + i < a.M) bias.v[i] = __ldg(a.bias + m + i);
+    };
+    if (a.bias && first + tid < last) load_bias(row_of(first + tid));
     if (S > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");      // every CTA of the cluster has started
     for (int o = tid; o < outs; o += kThreads) {
-        const int token = by_rows.div(o), r = o - token * rows, strip = r >> 4;
-        float v = 0.0f;
+        const int token = by_token.div(o), r = (o - token * per_token) * kRows, strip = r >> 4;
+        Rows v{};
         for (uint32_t m = plan[strip]; m; m &= m - 1) {
             const float* p = park + (__ffs((int)m) - 1 + strip) * kParkLd * parked + token * cpt * kParkLd + (r & 15);
-            v += cpt == 1 ? p[0] : p[0] + (p[kParkLd] + p[2 * kParkLd]);
+            Rows w = *reinterpret_cast<const Rows*>(p);
+            if (BYTES && cpt == 3) w.v[0] += p[kParkLd] + p[2 * kParkLd];
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) v.v[i] += w.v[i];
         }
         if (S > 1) {
             const int owner = by_share.div(o);
@@ -320,13 +347,21 @@ __global__ void __launch_bounds__(kThreads, BYTES ? 2 : 1) q4_kernel(const Q4Arg
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
     for (int o = first + tid; o < last; o += kThreads) {
-        const int token = by_rows.div(o), m = s0 * 16 + o - token * rows;
+        const int token = by_token.div(o), m = row_of(o);
         if (m >= a.M) continue;
-        float v = 0.0f;
-        for (int q = 0; q < S; ++q) v += red[q * share + o - first];
-        if (a.bias) v += o == first + tid ? bias : __ldg(a.bias + m);
-        if (a.act == PP_ACT_RELU) v = v > 0.0f || v != v ? v : 0.0f;
-        store_y(a.y, (int64_t)token * a.M + m, a.y_type, v);
+        Rows v{};
+        for (int q = 0; q < S; ++q) {
+            const Rows w = red[q * share + o - first];
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) v.v[i] += w.v[i];
+        }
+        if (a.bias && o != first + tid) load_bias(m);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            if (a.bias) v.v[i] += bias.v[i];
+            if (a.act == PP_ACT_RELU) v.v[i] = v.v[i] > 0.0f || v.v[i] != v.v[i] ? v.v[i] : 0.0f;
+        }
+        store_y(a.y, (int64_t)token * a.M + m, a.y_type, v, a.M - m, kRows == 1 || a.y_vec);
     }
 }
 
@@ -357,8 +392,8 @@ size_t plan_smem(Q4Args& a, bool bytes, int sets, int S, int n_s) {
     const bool paired = !bytes && a.nc != a.tokens;
     at += (size_t)(n_s + kWarps) * kParkLd * (paired ? a.tokens : a.nc) * 4;
     a.red_off = (int)at;
-    const size_t outs = (size_t)n_s * 16 * a.tokens;
-    at += (outs + S - 1) / S * S * 4;
+    const size_t row = bytes ? 1 : 4, outs = (size_t)n_s * 16 / row * a.tokens;       // rows to a thread
+    at += (outs + S - 1) / S * S * row * 4;
     return at;
 }
 
@@ -525,6 +560,7 @@ extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_
         a.in.x = static_cast<const char*>(x) + (int64_t)b0 * ldx * xb;
         a.in.scales = x_scales ? x_scales + (int64_t)b0 * a.in.scale_ld : nullptr;
         a.y = static_cast<char*>(y) + (int64_t)b0 * L->M * yb;
+        a.y_vec = L->M % 4 == 0 && aligned_to(a.y, 4 * yb);
         // cluster size and strips to a cluster: the fewest units on the busiest SM, counting what staging a block of a
         // token's columns costs as half a unit.  More strips than one round of clusters can hold go in several rounds.
         int best = 0, best_n = 0;
