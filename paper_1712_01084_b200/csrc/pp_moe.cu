@@ -25,6 +25,9 @@
 // and always takes three columns: in bf16 these are its 24 bits; in binary16 (4-bit experts too), where no scale is known
 // before all of act is, they hold act * 2^-11, the rest * 2^-1 and the rest * 2^10, which together are act to 24 bits
 // between 2^-11 and 2^27 and to an absolute 2^-35 below.
+//
+// us a call: 64 experts of 4096 x 2048, 8 a token, bf16, 16 tokens 442 (6.4 TB/s); 64 of 2048 x 1024, 4 tokens, 4 bits 33.5
+// (of 13 for the bytes: bound by instructions); 8 experts of 1024, 2 a token, one token 14.1 (bound by the steps' latency).
 #include "pp_q4.cuh"
 
 #include <algorithm>

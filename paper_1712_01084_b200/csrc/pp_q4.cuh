@@ -66,13 +66,6 @@ template <uint32_t MASK> __device__ __forceinline__ uint32_t code_pair(uint32_t 
     return d;
 }
 
-// Asynchronous copies of a unit (1024 bytes, then set16 pieces of 16 bytes of its sets) by a warp.
-__device__ __forceinline__ void unit_fetch(uint32_t slot, const unsigned char* codes, const unsigned char* sets, int lane, int set16) {
-    cp_async16(slot + lane * 16, codes + lane * 16);
-    cp_async16(slot + 512 + lane * 16, codes + 512 + lane * 16);
-    if (lane < set16) cp_async16(slot + 1024 + lane * 16, sets + lane * 16);
-}
-
 // Scales of rows g and g + 8 in a set of a unit, the second with its 1/16.
 __device__ __forceinline__ float2 q4_scales(const unsigned char* slot, int set, int g, bool bf16_scales) {
     const uint32_t ss = at<uint32_t>(slot + 1024 + set * 32 + g * 4);
