@@ -26,8 +26,8 @@
 // before all of act is, they hold act * 2^-11, the rest * 2^-1 and the rest * 2^10, which together are act to 24 bits
 // between 2^-11 and 2^27 and to an absolute 2^-35 below.
 //
-// us a call: 64 experts of 4096 x 2048, 8 a token, bf16, 16 tokens 442 (6.4 TB/s); 64 of 2048 x 1024, 4 tokens, 4 bits 33.5
-// (of 13 for the bytes: bound by instructions); 8 experts of 1024, 2 a token, one token 14.1 (bound by the steps' latency).
+// us a call: 64 experts of 4096 x 2048, 8 a token, bf16, 16 tokens 442 (6.4 TB/s); 64 of 2048 x 1024, 4 tokens, 4 bits 32.9
+// (of 13 for the bytes: bound by instructions); 8 experts of 1024, 2 a token, one token 13.5 (bound by the steps' latency).
 #include "pp_q4.cuh"
 
 #include <algorithm>
@@ -72,7 +72,9 @@ struct MoeArgs {
     float* gates;
     int y_type, T, E, H, top_k, renorm, strips1, strips2, kb1, kb2, kpad1, kpad2, router_ld, slot_bytes, cpt, bf16_scales, polls;
     int router_parts, router_cols;           // parts of a logit, columns of a part
-    float per_expert, per_entry;             // 1 / strips1, 1 / kb2
+    float per_expert, per_entry, per_kb1, per_cta, per_cap, per_top_k;       // 1 / strips1, 1 / kb2, 1 / kb1, 1 / grid, ...
+    double per_cta64;
+    int round_log2;                          // of the strips of a round
     int round;                               // strips of a round
     int cap;                                 // tokens of an entry, at most
     int list_off, scr_off, park_off;         // shared memory; the weight rings are at 0
@@ -319,6 +321,15 @@ template <class W, typename T> __device__ __forceinline__ void step0(const MoeAr
     else step0<W, T, false>(a, part);
 }
 
+// x / n from the reciprocal of n, for quotients below 2^21.
+__device__ __forceinline__ int divide(int x, int n, float r) {
+    int q = (int)((float)x * r);
+    const int rest = x - q * n;
+    if (rest < 0) --q;
+    if (rest >= n) ++q;
+    return q;
+}
+
 // ---- routing, by every CTA for itself ----------------------------------------------------------------------------
 struct Lists {
     int4* entry;         // {expert, first pair, pairs, 0}: an expert and up to `cap` of its tokens
@@ -428,7 +439,7 @@ __device__ __forceinline__ int route(const MoeArgs& a, const Lists& L) {       /
     __syncthreads();
     // where each expert's pairs and entries start: both counts in one scan (neither exceeds 512)
     const int n = tid < a.E ? __popc(L.tokens[tid]) : 0;
-    const int mine = n | ((n + a.cap - 1) / a.cap) << 16;
+    const int mine = n | divide(n + a.cap - 1, a.cap, a.per_cap) << 16;
     int both = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -451,7 +462,7 @@ __device__ __forceinline__ int route(const MoeArgs& a, const Lists& L) {       /
     }
     __syncthreads();
     if (tid < a.T * a.top_k) {                               // at most 512 pairs
-        const int t = tid / a.top_k, e = L.chosen[tid], p = L.first[e] + __popc(L.tokens[e] & ((1u << t) - 1u));
+        const int t = divide(tid, a.top_k, a.per_top_k), e = L.chosen[tid], p = L.first[e] + __popc(L.tokens[e] & ((1u << t) - 1u));
         L.pair_token[p] = t;
         L.pair_gate[p] = L.gate[tid];
     }
@@ -470,25 +481,17 @@ struct Span {
 };
 struct Run { const unsigned char *unit, *sets; int left, ls, entry, kb; };        // units that lie one after another; ls: strip - first
 
-// x / n from the reciprocal of n, for quotients below 2^21.
-__device__ __forceinline__ int divide(int x, int n, float r) {
-    int q = (int)((float)x * r);
-    const int rest = x - q * n;
-    if (rest < 0) --q;
-    if (rest >= n) ++q;
-    return q;
-}
-
 // This CTA's part of `strips` strips of nv units.  Cuts fall between strips unless that leaves the busiest CTA with kJoin
 // units more than its equal share: joining a divided strip takes about 3,700 cycles, 84 units at the rate of HBM (148 CTAs:
 // 256 strips of 32 units are faster whole, 256 strips of 3,600 units are not: 519,000 cycles whole, 396,000 cut).
 constexpr int kJoin = 84;
-__device__ __forceinline__ Span span_of(int strips, int nv, int round) {
+// (Divisions by reciprocals: a CTA's way from the choice to its first copies holds four of them.)
+__device__ __forceinline__ Span span_of(const MoeArgs& a, int strips, int nv, float per_strip) {
     Span s;
     s.nv = nv;
-    s.per_strip = 1.0f / (float)nv;
+    s.per_strip = per_strip;
     const int grid = (int)gridDim.x, cta = (int)blockIdx.x;
-    const int each = strips / grid, more = strips - each * grid;                 // strips of a CTA, CTAs with one more
+    const int each = divide(strips, grid, a.per_cta), more = strips - each * grid;   // strips of a CTA, CTAs with one more
     s.whole = (int64_t)(more ? grid - more : 0) * nv <= (int64_t)kJoin * grid;
     if (s.whole) {
         s.ctas = min(grid, strips);
@@ -497,15 +500,24 @@ __device__ __forceinline__ Span span_of(int strips, int nv, int round) {
         s.strips = each + (cta < more);
         s.x1 = s.strips * nv;
     } else {
-        const int64_t units = (int64_t)strips * nv;
+        const int64_t units = (int64_t)strips * nv;           // below 2^34
         s.ctas = (int)min((int64_t)grid, units);
-        const int64_t begin = units * min(cta, s.ctas) / s.ctas, end = units * min(cta + 1, s.ctas) / s.ctas;
-        s.first = (int)(begin / nv);
-        s.x0 = (int)(begin - (int64_t)s.first * nv);
+        const auto start = [&](int c) {                       // units * c / ctas
+            if (units <= grid) return min((int64_t)c, units);
+            const int64_t n = units * c;                      // below 2^53
+            int64_t q = (int64_t)((double)n * a.per_cta64);
+            const int64_t rest = n - q * grid;
+            return rest < 0 ? q - 1 : rest >= grid ? q + 1 : q;
+        };
+        const int64_t begin = start(cta), end = start(cta + 1);
+        int first = (int)((float)begin * per_strip);          // at most 2^22 strips: off by one at most
+        const int64_t rest = begin - (int64_t)first * nv;
+        s.first = first += rest < 0 ? -1 : rest >= nv ? 1 : 0;
+        s.x0 = (int)(begin - (int64_t)first * nv);
         s.x1 = s.x0 + (int)(end - begin);
-        s.strips = s.x1 > s.x0 ? (s.x1 + nv - 1) / nv : 0;
+        s.strips = s.x1 > s.x0 ? divide(s.x1 + nv - 1, nv, per_strip) : 0;
     }
-    s.rounds = (s.strips + round - 1) / round;
+    s.rounds = (s.strips + a.round - 1) >> a.round_log2;
     return s;
 }
 
@@ -876,7 +888,7 @@ template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe
         constexpr int kDepth = depth<W, TILES>();
         const uint32_t ring = smem_addr(smem) + warp * kDepth * a.slot_bytes + lane * 16;
         {
-            const Span s = span_of(entries * a.strips1, a.kb1, a.round);
+            const Span s = span_of(a, entries * a.strips1, a.kb1, a.per_kb1);
             Fetcher<W, 1, TILES> f;
 #pragma unroll 1
             for (int d = 0; d < kDepth; ++d) f.next(a, L, s, warp, lane, ring + d * a.slot_bytes, true, true);
@@ -885,7 +897,7 @@ template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe
             if (!s.whole) join<W, 1>(a, L, s);
         }
         grid_arrive(a.sync + 1);
-        const Span s = span_of(a.strips2, entries * a.kb2, a.round);
+        const Span s = span_of(a, a.strips2, entries * a.kb2, __frcp_rn((float)(entries * a.kb2)));
         Fetcher<W, 2, TILES> f, g;                           // ahead of the barrier the weights, behind it their columns
 #pragma unroll 1
         for (int d = 0; d < kDepth; ++d) f.next(a, L, s, warp, lane, ring + d * a.slot_bytes, true, false);
@@ -969,7 +981,7 @@ size_t plan_smem(MoeArgs& a, int ring, int tiles, int meta) {
     a.scr_off = (int)at;
     at += (size_t)kWarps * 16 * 8 * tiles * 4;
     a.park_off = (int)at;
-    for (a.round = 32;; a.round /= 2) {
+    for (a.round = 32, a.round_log2 = 5;; a.round /= 2, --a.round_log2) {
         const size_t total = at + (size_t)(a.round + kWarps) * 16 * std::max(a.cap, a.T) * 4;
         if (total > (size_t)kMaxSmem && a.round > 1) continue;
         const size_t bytes = meta ? (size_t)a.T * 3 * a.kpad1 + (size_t)a.T * 3 * a.kb1 * meta * 4 + 16 : 0;
@@ -1160,6 +1172,11 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     a.parts = L->parts;
     a.per_expert = 1.0f / (float)L->strips1;
     a.per_entry = 1.0f / (float)L->kb2;
+    a.per_kb1 = 1.0f / (float)L->kb1;
+    a.per_cta = 1.0f / (float)L->ctas;
+    a.per_cta64 = 1.0 / (double)L->ctas;
+    a.per_cap = 1.0f / (float)a.cap;
+    a.per_top_k = 1.0f / (float)L->top_k;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeCooperative;
     at[0].val.cooperative = 1;
