@@ -26,8 +26,8 @@
 // before all of act is, they hold act * 2^-11, the rest * 2^-1 and the rest * 2^10, which together are act to 24 bits
 // between 2^-11 and 2^27 and to an absolute 2^-35 below.
 //
-// us a call: 64 experts of 4096 x 2048, 8 a token, bf16, 16 tokens 442 (6.4 TB/s); 64 of 2048 x 1024, 4 tokens, 4 bits 32.9
-// (of 13 for the bytes: bound by instructions); 8 experts of 1024, 2 a token, one token 13.5 (bound by the steps' latency).
+// us a call: 64 experts of 4096 x 2048, 8 a token, bf16, 16 tokens 442 (6.4 TB/s); 64 of 2048 x 1024, 4 tokens, 4 bits 33.0
+// (of 13 for the bytes: bound by instructions); 8 experts of 1024, 2 a token, one token 13.0 (bound by the steps' latency).
 #include "pp_q4.cuh"
 
 #include <algorithm>
@@ -416,11 +416,20 @@ template <int kEach> __device__ __forceinline__ void choose(const MoeArgs& a, co
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     p /= sum;
+    int rank = 0;
+    if (a.T == 1)
+        for (int j = 0; j < a.top_k; ++j) rank += __shfl_sync(0xffffffffu, expert, j) < expert;
     if (lane < a.top_k) {
         const int at = t * a.top_k + lane;
-        L.chosen[at] = expert;
-        L.gate[at] = p;
-        atomicOr(L.tokens + expert, 1u << t);
+        if (a.T == 1) {                                      // every expert has one pair: its place is its rank
+            L.entry[rank] = make_int4(expert, rank, 1, 0);
+            L.pair_token[rank] = 0;
+            L.pair_gate[rank] = p;
+        } else {
+            L.chosen[at] = expert;
+            L.gate[at] = p;
+            atomicOr(L.tokens + expert, 1u << t);
+        }
         if (blockIdx.x == 0) {
             if (a.ids) a.ids[at] = expert;
             if (a.gates) a.gates[at] = p;
@@ -430,13 +439,15 @@ template <int kEach> __device__ __forceinline__ void choose(const MoeArgs& a, co
 
 __device__ __forceinline__ int route(const MoeArgs& a, const Lists& L) {       // the number of entries; L.tokens is zero before
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid < a.T) L.xscale[tid] = __ldcg(a.xscale + tid);
+    const float xscale = tid < a.T ? __ldcg(a.xscale + tid) : 0.0f;       // stored behind the choice, which would wait for it
     for (int t = warp; t < a.T; t += kWarps) {
         if (a.E <= 32) choose<1>(a, L, t);
         else if (a.E <= 64) choose<2>(a, L, t);
         else choose<kMaxExperts / 32>(a, L, t);
     }
+    if (tid < a.T) L.xscale[tid] = xscale;
     __syncthreads();
+    if (a.T == 1) return a.top_k;                            // its lists are made (8 experts: 13.3 us, through the counts below 13.6)
     // where each expert's pairs and entries start: both counts in one scan (neither exceeds 512)
     const int n = tid < a.E ? __popc(L.tokens[tid]) : 0;
     const int mine = n | divide(n + a.cap - 1, a.cap, a.per_cap) << 16;
