@@ -107,6 +107,12 @@ template <typename F> PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F body)
         if (got != want) raise(PyExc_TypeError, "%zd arguments, %zd expected", got, want);
         return body();
     } catch (const Raised&) {
+    } catch (const c10::OutOfMemoryError& e) {
+        PyObject* torch = PyImport_ImportModule("torch");
+        PyObject* type = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+        if (type) PyErr_SetString(type, e.what_without_backtrace());
+        Py_XDECREF(type);
+        Py_XDECREF(torch);
     } catch (const c10::Error& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
     } catch (const std::exception& e) {
