@@ -509,8 +509,8 @@ pp_status_t pp_q4_forward(pp_q4_t* layer, const void* x, int64_t ldx, pp_dtype_t
  * between 2^-11 and 2^27, with an absolute 2^-35 below, and overflows above.  A token with a NaN or an
  * infinity has outputs that are not finite; other tokens are not touched by it.
  * One cooperative kernel; results do not depend on scheduling.  Only enqueues.  Calls on one handle must be ordered on
- * one stream.  Its two grid-wide waits are bounded (tuning key 15): when one gives up y is invalid and pp_moe_status, which
- * synchronises with the device, reports PP_ERR_TIMEOUT and clears it.
+ * one stream.  Its two grid-wide waits are bounded (tuning key 15): when one gives up y is invalid, and so is what later calls
+ * on the handle write, until pp_moe_status, which synchronises with the device, reports PP_ERR_TIMEOUT and clears it.
  * Errors: PP_ERR_INVALID_ARG (also tokens > max_tokens), PP_ERR_UNSUPPORTED, PP_ERR_ALLOC, PP_ERR_CUDA. */
 typedef struct pp_moe pp_moe_t;
 pp_status_t pp_moe_create(pp_moe_t** out, int E, int H, int F, int top_k, int renormalize, int max_tokens, const void* router,

@@ -1002,6 +1002,7 @@ size_t plan_smem(MoeArgs& a, int ring, int tiles, int meta) {
     }
 }
 
+size_t sync_bytes(int ctas) { return (4 + 2 * (size_t)ctas) * 4; }
 template <typename T> bool alloc(T** p, size_t n) { return cudaMalloc(reinterpret_cast<void**>(p), n) == cudaSuccess; }
 
 }  // namespace
@@ -1057,20 +1058,19 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
                             cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kThreads, kMaxSmem) != cudaSuccess || each < 1)) st = PP_ERR_CUDA;
     }
     L->ctas = sms;
-    const size_t sync_bytes = (4 + 2 * (size_t)L->ctas) * 4;
     if (st == PP_OK &&
         (!alloc(&L->gate_up, units1 * 1024) || !alloc(&L->down, units2 * 1024) ||
          (set_bytes && (!alloc(&L->gate_up_sets, units1 * set_bytes) || !alloc(&L->down_sets, units2 * set_bytes))) || !alloc(&L->router, ld * E * 4) ||
          !alloc(&L->logits, (size_t)max_tokens * E * kRouterParts * 4) || !alloc(&L->xscale, (size_t)max_tokens * 4) ||
          !alloc(&L->xcols, (size_t)max_tokens * 3 * L->kb1 * cols * 2) || !alloc(&L->acols, abytes) ||
          (wtype < 0 && !alloc(&L->xmeta, (size_t)max_tokens * 3 * L->kb1 * 32)) ||
-         !alloc(&L->parts, (size_t)L->ctas * 2 * 16 * std::max(kMaxCap, max_tokens) * 4) || !alloc(&L->sync, sync_bytes))) {
+         !alloc(&L->parts, (size_t)L->ctas * 2 * 16 * std::max(kMaxCap, max_tokens) * 4) || !alloc(&L->sync, sync_bytes(L->ctas)))) {
         cudaGetLastError();
         st = PP_ERR_ALLOC;
     }
     if (st == PP_OK) {
         // act's columns past F are never written and stay zero
-        if (cudaMemsetAsync(L->acols, 0, abytes, s) != cudaSuccess || cudaMemsetAsync(L->sync, 0, sync_bytes, s) != cudaSuccess) st = PP_ERR_CUDA;
+        if (cudaMemsetAsync(L->acols, 0, abytes, s) != cudaSuccess || cudaMemsetAsync(L->sync, 0, sync_bytes(L->ctas), s) != cudaSuccess) st = PP_ERR_CUDA;
         router_pack_kernel<<<148, 256, 0, s>>>(L->router, router, router_type, E, H, (int)ld);
         if (cudaGetLastError() != cudaSuccess) st = PP_ERR_CUDA;
     }
@@ -1124,7 +1124,9 @@ extern "C" pp_status_t pp_moe_status(pp_moe_t* L, pp_status_t* status) {
     if (!L || !status) return PP_ERR_INVALID_ARG;
     int raised = 0;
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&raised, L->sync + 3, 4, cudaMemcpyDeviceToHost) != cudaSuccess) return PP_ERR_CUDA;
-    if (raised && cudaMemset(L->sync + 3, 0, 4) != cudaSuccess) return PP_ERR_CUDA;
+    // a wait that gave up leaves divided strips with some of their CTAs counted and nobody to take the count back: the whole of
+    // it starts anew (not at the kernel's end: ordering that behind the other CTAs' counts costs every call 0.7 us)
+    if (raised && cudaMemset(L->sync, 0, sync_bytes(L->ctas)) != cudaSuccess) return PP_ERR_CUDA;
     *status = raised ? PP_ERR_TIMEOUT : PP_OK;
     return PP_OK;
 }

@@ -223,6 +223,31 @@ def test_moe_grid_wait_runs_out():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("E,k,H,F,T", [(2, 1, 4096, 80, 1),       # step 1 is cut inside strips: 10 of 128 units
+                                       (256, 16, 192, 64, 32)],   # step 2: 12 strips of about 440 units
+                         ids=["gate_up", "down"])
+def test_moe_recovers_after_a_wait_ran_out_at_divided_strips(E, k, H, F, T):
+    """A CTA that gave up never arrives at the strips it shares; the next call must not count those that did."""
+    c = Case(E + H, E, k, H, F, "bf16", T)
+    x = torch.randn(T, H, generator=_gen(12), device="cuda").bfloat16()
+    want = c.check(x, torch.float32)
+    raised = 0
+    for polls in (1, 2, 3, 4, 6, 8, 12, 16, 24, 32):
+        pb.pp_set_tuning(15, polls)
+        try:
+            for _ in range(4):
+                pb.pp_moe_forward(c.layer, x, out_dtype=torch.float32)
+                raised += c.layer.status() == 7
+        finally:
+            pb.pp_set_tuning(15, 0)
+        for _ in range(3):
+            assert torch.equal(pb.pp_moe_forward(c.layer, x, out_dtype=torch.float32), want)
+        assert c.layer.status() == pb.PP_OK
+    assert raised > 0
+    c.check(x, torch.float32)
+
+
+@pytest.mark.gpu
 def test_moe_refusals():
     E, H, F = 4, 64, 32
     r = torch.zeros(E, H, device="cuda")
