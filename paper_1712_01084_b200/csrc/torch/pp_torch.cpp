@@ -88,9 +88,18 @@ at::Tensor fresh(at::IntArrayRef shape, at::ScalarType t, int device) {
     return at::Tensor(at::detail::empty_cuda(shape, t, at::Device(at::kCUDA, (c10::DeviceIndex)device), std::nullopt));
 }
 
-void* stream_of(PyObject* o, int device) {
-    return o == Py_None ? c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream() : address(o);
-}
+// The device and the stream of a call, the given one or the current one.  The given one is made current until the call is over:
+// a new tensor then comes from its own memory, and is not what an earlier tensor of another stream has just left with work on
+// it still to come.
+struct Enqueue {
+    c10::cuda::CUDAGuard device;
+    c10::cuda::OptionalCUDAStreamGuard given;
+    void* stream;
+    Enqueue(PyObject* o, int d) : device((c10::DeviceIndex)d) {
+        if (o != Py_None) given.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(address(o)), (c10::DeviceIndex)d));
+        stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)d).stream();
+    }
+};
 
 // An output tensor: the given one, checked, or a new one.
 at::Tensor output(PyObject* out, PyObject* out_dtype, at::ScalarType standard, int64_t rows, int64_t cols, int device) {
@@ -147,7 +156,7 @@ PyObject* rmsnorm_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (eps == -1.0 && PyErr_Occurred()) throw Raised{};
         const int group = number(a[5]);
         const bool normed = truth(a[7]);
-        const c10::cuda::CUDAGuard on(device);
+        const Enqueue on(a[8], device);
 
         const void* r = nullptr;
         Rows rr{0, 0}, rh{0, 0};
@@ -173,7 +182,7 @@ PyObject* rmsnorm_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const pp_status_t st = g_rmsnorm_q8(x.const_data_ptr(), rx.ld, r, rr.ld, w.const_data_ptr(), dt, wt, rx.rows, (int)cols, (float)eps, code,
                                             group, q.data_ptr(), static_cast<float*>(scales.data_ptr()),
                                             hidden.defined() ? hidden.data_ptr() : nullptr, rh.ld, normed ? norm.data_ptr() : nullptr,
-                                            stream_of(a[8], device));
+                                            on.stream);
         if (st != PP_OK) return PyLong_FromLong(st);
         PyObject* out = PyTuple_New(normed ? 4 : 3);
         if (!out) return nullptr;
@@ -205,10 +214,10 @@ PyObject* q4_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
             x_group = s.numel() == rx.rows ? 0 : 128;
             scales = static_cast<const float*>(s.const_data_ptr());
         }
-        const c10::cuda::CUDAGuard on(device);
+        const Enqueue on(a[9], device);
         const at::Tensor y = output(a[8], a[7], at::kFloat, rx.rows, M, device);
         const pp_status_t st = g_q4_forward(static_cast<pp_q4_t*>(address(a[0])), x.const_data_ptr(), rx.ld, xt, scales, x_group, y.data_ptr(),
-                                            type_of(y.scalar_type(), "out"), rx.rows, (pp_act_t)number(a[5]), stream_of(a[9], device));
+                                            type_of(y.scalar_type(), "out"), rx.rows, (pp_act_t)number(a[5]), on.stream);
         if (st != PP_OK) return PyLong_FromLong(st);
         return a[8] != Py_None ? keep(a[8]) : THPVariable_Wrap(y);
     });
@@ -223,7 +232,7 @@ PyObject* moe_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Rows rx = rows_of(x, H, "x", device);
         const pp_dtype_t xt = type_of(x.scalar_type(), "x");
         const bool routing = truth(a[7]);
-        const c10::cuda::CUDAGuard on(device);
+        const Enqueue on(a[8], device);
         const at::Tensor y = output(a[6], a[5], x.scalar_type(), rx.rows, H, device);
         at::Tensor ids, gates;
         if (routing) {
@@ -232,7 +241,7 @@ PyObject* moe_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         const pp_status_t st = g_moe_forward(static_cast<pp_moe_t*>(address(a[0])), x.const_data_ptr(), rx.ld, xt, y.data_ptr(),
                                              type_of(y.scalar_type(), "out"), rx.rows, routing ? static_cast<int32_t*>(ids.data_ptr()) : nullptr,
-                                             routing ? static_cast<float*>(gates.data_ptr()) : nullptr, stream_of(a[8], device));
+                                             routing ? static_cast<float*>(gates.data_ptr()) : nullptr, on.stream);
         if (st != PP_OK) return PyLong_FromLong(st);
         PyObject* out = a[6] != Py_None ? keep(a[6]) : THPVariable_Wrap(y);
         if (!routing || !out) return out;
