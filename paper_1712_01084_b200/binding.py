@@ -295,6 +295,16 @@ def _stream_ptr(stream=None):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _new_float(shape, device, stream):
+    """A float32 output in the memory of the stream it is written on.  Made on the current stream instead, it may lie where an
+    earlier tensor still has readers waiting there."""
+    import torch
+    if stream is None:                          # (the context manager takes 2.9 us)
+        return torch.empty(shape, dtype=torch.float32, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=torch.float32, device=device)
+
+
 def _require_cuda(t, name):
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous CUDA tensor")
@@ -396,7 +406,7 @@ def pp_forward(layer: Layer, x, act: int = PP_ACT_IDENTITY, out=None, stream=Non
     import torch
     x2 = _check_x(x, layer.N, layer.wdtype)
     batch = x2.shape[0]
-    y = torch.empty((batch, layer.M), dtype=torch.float32, device=x.device) if out is None else out
+    y = _new_float((batch, layer.M), x.device, stream) if out is None else out
     _require_cuda(y, "out")
     if y.dtype != torch.float32 or y.numel() != batch * layer.M:
         raise ValueError("out must be float32 [batch][M]")
@@ -430,7 +440,7 @@ def pp_forward_pivoted(layer: Layer, x, act: int = PP_ACT_IDENTITY, out=None, st
     x2 = _check_x(x, layer.N, layer.wdtype)
     batch = x2.shape[0]
     m_pad = -(-layer.M // layer.B) * layer.B
-    y = torch.empty((batch, m_pad), dtype=torch.float32, device=x.device) if out is None else out
+    y = _new_float((batch, m_pad), x.device, stream) if out is None else out
     _require_cuda(y, "out")
     if y.dtype != torch.float32 or y.numel() != batch * m_pad:
         raise ValueError("out must be float32 [batch][M_pad]")
@@ -525,7 +535,7 @@ def pp_chain_forward(chain: Chain, x, out=None, stream=None):
     x2 = _check_x(x, first.N, first.wdtype)
     batch = x2.shape[0]
     width = -(-last.M // last.B) * last.B if chain.output_pivoted else last.M
-    y = torch.empty((batch, width), dtype=torch.float32, device=x.device) if out is None else out
+    y = _new_float((batch, width), x.device, stream) if out is None else out
     _require_cuda(y, "out")
     if y.dtype != torch.float32 or y.numel() != batch * width:
         raise ValueError("out must be float32 [batch][M] ([batch][M_pad] when the output stays pivoted)")
@@ -614,7 +624,7 @@ class LayoutStudy:
         _require_cuda(x, "x")
         if x.dtype != torch.float32 or x.numel() != self.size:
             raise ValueError("x must be float32 with `size` elements")
-        y = torch.empty(self.size, dtype=torch.float32, device=x.device) if out is None else out
+        y = _new_float(self.size, x.device, stream) if out is None else out
         _check(lib().pp_layout_forward(self._h, x.data_ptr(), y.data_ptr(), _stream_ptr(stream)), "pp_layout_forward")
         return y
 

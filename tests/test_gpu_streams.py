@@ -90,3 +90,39 @@ def test_decoder_operators_take_the_default_stream(pb, operator):
         assert torch.cuda.current_stream() == current
     torch.cuda.synchronize()
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, want))
+
+
+def _layer(pb, batch=8):
+    from paper_1712_01084_b200 import synth
+    wl = synth.config5(k=16, batch=batch, scale=0.25)
+    return pb.Layer.from_synth(wl.layers[0]), torch.from_numpy(wl.x).cuda()
+
+
+def _forward(pb):
+    L, x = _layer(pb)
+    return lambda stream=None: (pb.pp_forward(L, x, stream=stream),)
+
+
+def _pivoted(pb):
+    L, x = _layer(pb)
+    return lambda stream=None: (pb.pp_forward_pivoted(L, x, stream=stream),)
+
+
+def _chain(pb):
+    L, x = _layer(pb)
+    C = pb.pp_chain_create([L], [0], 8)
+    return lambda stream=None: (pb.pp_chain_forward(C, x, stream=stream),)
+
+
+def _layout(pb):
+    import numpy as np
+    rng = np.random.default_rng(5)
+    perm = np.arange(1024, dtype=np.int32)
+    S = pb.LayoutStudy(1024, 32, pb.PP_LAYOUT_BRC, pb.PP_MAP_ROWS_PER_LANE, perm, perm, rng.standard_normal(32 * 32 * 32).astype(np.float32))
+    x = torch.randn(1024, generator=_gen(6), device="cuda")
+    return lambda stream=None: (S.forward(x, stream=stream),)
+
+
+@pytest.mark.parametrize("make", [_forward, _pivoted, _chain, _layout], ids=["layer", "pivoted", "chain", "layout"])
+def test_layers_allocate_on_the_given_stream(pb, make):
+    _check_stream_argument(make(pb))
