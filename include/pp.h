@@ -438,8 +438,9 @@ pp_status_t pp_noalloc_status(pp_status_t* status);
  *     h = x + residual,  n = h * rsqrt(mean(h^2) + eps) * weight,
  *     s = max|n| / Q over the row or over each group of columns,  code = round(n / s)   (ties to even)
  * with Q = 127 for PP_I8 and 448 for PP_E4M3.  h and n are floats throughout; hidden_out and normed_out are rounded
- * once.  Where max|n| is 0 scale and codes are 0.  A row with a NaN or an infinity has NaN scales; its codes are
- * unspecified.
+ * once.  Where max|n| is 0 scale and codes are 0.  A row with a NaN, an infinity or squares whose sum is beyond
+ * fp32 (elements of some 10^17) has NaN in all its scales and in normed_out; a weight that is NaN has it in the scales of the row
+ * or group that it lies in.  Their codes are unspecified.  eps = 0 leaves a row of zeros undefined (NaN scales).
  * x             [rows][cols], rows ldx elements apart, type dtype: PP_F32, PP_F16 or PP_BF16
  * residual      the same, ldr apart; NULL = 0
  * weight        [cols], weight_type = dtype or PP_F32

@@ -37,11 +37,17 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+// The larger of two, a NaN before all: fmaxf would drop it, and an infinity times a weight of 0 is one.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
 // Largest of a warp's, or of each half warp's, values >= 0 (which order as whole numbers do; a NaN is the largest).
 template <int W> __device__ __forceinline__ float lanes_max(float v) {
     if (W == 32) return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
 #pragma unroll
-    for (int o = W / 2; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    for (int o = W / 2; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
 
@@ -111,7 +117,7 @@ __device__ __forceinline__ void finish_row(const NormArgs& a, int64_t row, float
         for (int i = 0; i < 8; ++i) {                        // h and w are 0 past the row's end
             sum = fmaf(h[c][i], h[c][i], sum);
             h[c][i] *= w[i];
-            top[c][!VEC && i >= 4] = fmaxf(top[c][!VEC && i >= 4], fabsf(h[c][i]));
+            top[c][!VEC && i >= 4] = max_nan(top[c][!VEC && i >= 4], fabsf(h[c][i]));
         }
         if (GROUPED) {
             if (VEC) {
@@ -121,7 +127,7 @@ __device__ __forceinline__ void finish_row(const NormArgs& a, int64_t row, float
                 top[c][1] = lanes_max<32>(top[c][1]);
             }
         } else {
-            most = fmaxf(most, fmaxf(top[c][0], top[c][1]));
+            most = max_nan(most, max_nan(top[c][0], top[c][1]));
         }
     }
     sum = warp_sum(sum);
@@ -133,7 +139,9 @@ __device__ __forceinline__ void finish_row(const NormArgs& a, int64_t row, float
     __syncthreads();
     sum = warp_sum(lane < n_warps ? part[lane] : 0.0f);
     if (!GROUPED) most = lanes_max<32>(lane < n_warps ? part[32 + lane] : 0.0f);
-    const float rms = rsqrtf(fmaf(sum, a.per_col, a.eps));
+    // a sum that is not finite (an element that is not, or squares beyond fp32) makes every scale of the row NaN: the root's 0
+    // would make them 0
+    const float rms = sum < INFINITY ? rsqrtf(fmaf(sum, a.per_col, a.eps)) : __int_as_float(0x7fffffff);
 
     uint8_t* codes = static_cast<uint8_t*>(a.codes) + row * a.cols;
     if (!GROUPED && threadIdx.x == 0) a.scales[row] = rms * most * (1.0f / kTop);

@@ -145,6 +145,34 @@ def test_norm_rows_of_zeros_nan_inf_and_tiny(codes, group):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("codes", ["e4m3", "int8"])
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("rows,cols,off", [(3, 512, 0), (3, 509, 1), (1600, 4096, 0)], ids=["few", "odd", "many"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_rows_that_are_not_finite_have_nan_scales(dtype, rows, cols, off, codes, group):
+    """All of a row's scales are NaN, whatever the weight at the odd element, and no other row is touched."""
+    t = TYPES[dtype]
+    x = torch.randn(rows, cols + off, generator=_gen(20), device="cuda").to(t)[:, off:]
+    w = (1 + 0.3 * torch.randn(cols, generator=_gen(21), device="cuda")).to(t)
+    w[300] = 0.0                                                             # infinity times 0
+    clean = pb.pp_rmsnorm_q8(x, w, codes=codes, group=group, normed=True)
+    for at, value in ((5, float("inf")), (300, float("inf")), (300, float("-inf")), (300, float("nan")), (130, 3e19)):
+        bad = x.clone()
+        bad[1, at] = value                                                   # the last: finite, its square is not
+        got = pb.pp_rmsnorm_q8(bad, w, codes=codes, group=group, normed=True)
+        assert bool(torch.isnan(got[1][1]).all()) and bool(torch.isnan(got[3][1]).all())
+        keep = [0, rows - 1]
+        for a, b in zip(got, clean):
+            if a is not None:
+                assert torch.equal(a[keep].view(torch.uint8), b[keep].view(torch.uint8))
+    odd = w.clone()
+    odd[200] = float("nan")
+    scales = pb.pp_rmsnorm_q8(x, odd, codes=codes, group=group)[1]
+    nan = torch.isnan(scales)
+    assert bool(nan[:, 1 if group else 0].all()) and int(nan.sum()) == rows
+
+
+@pytest.mark.gpu
 def test_norm_refusals():
     x, w = torch.zeros(2, 256, device="cuda"), torch.zeros(256, device="cuda")
     with pytest.raises(ValueError):
