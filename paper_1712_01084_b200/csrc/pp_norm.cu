@@ -261,8 +261,8 @@ __global__ void __launch_bounds__(kRowsThreads, 2) rmsnorm_q8_rows_kernel(const 
 #pragma unroll
     for (int c = 0; c < CH; ++c) load_weights<T, true>(a, c, w[c]);
     const T *x = static_cast<const T*>(a.x), *r = static_cast<const T*>(a.r);
-    const auto fetch = [&](int row, int stage) {
-        if (row < a.rows) {
+    const auto fetch = [&](uint32_t row, int stage) {
+        if (row < (uint32_t)a.rows) {
             const uint32_t dst = (uint32_t)__cvta_generic_to_shared(smem + stage * a.stage_bytes);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
@@ -278,11 +278,11 @@ __global__ void __launch_bounds__(kRowsThreads, 2) rmsnorm_q8_rows_kernel(const 
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    const int step = gridDim.x;
+    const uint32_t step = gridDim.x, rows = (uint32_t)a.rows;        // rows asked for ahead may pass 2^31
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) fetch(blockIdx.x + s * step, s);
     int stage = 0, parity = 0;
-    for (int row = blockIdx.x; row < a.rows; row += step) {
+    for (uint32_t row = blockIdx.x; row < rows; row += step) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
         const unsigned char* at = smem + stage * a.stage_bytes;
         float h[CH][8];

@@ -173,6 +173,25 @@ def test_norm_rows_that_are_not_finite_have_nan_scales(dtype, rows, cols, off, c
 
 
 @pytest.mark.gpu
+def test_norm_of_nearly_all_rows_that_an_int_counts():
+    """The kernel for many rows asks for rows ahead of the one it works on: their numbers pass 2^31."""
+    rows, cols = 2 ** 31 - 1, 8
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 100 * 2 ** 30:
+        pytest.skip("takes 60 GB of device memory")
+    x = torch.empty(rows, cols, device="cuda", dtype=torch.bfloat16)
+    ends = [slice(0, 5000), slice(rows - 20000, rows)]
+    for i, e in enumerate(ends):
+        x[e] = torch.randn(x[e].shape, generator=_gen(30 + i), device="cuda").bfloat16()
+    w = (1 + 0.3 * torch.randn(cols, generator=_gen(32), device="cuda")).bfloat16()
+    q, s, _ = pb.pp_rmsnorm_q8(x, w, eps=1e-5)
+    for e in ends:
+        _check_norm(x[e], None, w, 1e-5, "e4m3", 0, (q[e], s[e], None))
+    del x, q, s
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 def test_norm_refusals():
     x, w = torch.zeros(2, 256, device="cuda"), torch.zeros(256, device="cuda")
     with pytest.raises(ValueError):
