@@ -19,6 +19,14 @@ inline bool is_8bit(int t) { return t == PP_I8 || t == PP_E4M3; }
 inline int type_bytes(int t) { return t == PP_F32 ? 4 : is_16bit(t) ? 2 : 1; }
 inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// A call's status.  An error of a launch is also kept by the runtime for whoever asks next: that is taken away with it, or the
+// next call that looks behind a launch of its own would report this one's.
+inline pp_status_t status_of(cudaError_t e) {
+    if (e == cudaSuccess) return PP_OK;
+    cudaGetLastError();
+    return PP_ERR_CUDA;
+}
+
 // Launch that lets the kernel's prologue overlap the tail of the previous kernel in the stream: the kernel itself
 // waits (griddepcontrol.wait) before it reads what that kernel may have written and before it writes anything.
 template <typename... P, typename... A>

@@ -1065,7 +1065,6 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
          !alloc(&L->xcols, (size_t)max_tokens * 3 * L->kb1 * cols * 2) || !alloc(&L->acols, abytes) ||
          (wtype < 0 && !alloc(&L->xmeta, (size_t)max_tokens * 3 * L->kb1 * 32)) ||
          !alloc(&L->parts, (size_t)L->ctas * 2 * 16 * std::max(kMaxCap, max_tokens) * 4) || !alloc(&L->sync, sync_bytes(L->ctas)))) {
-        cudaGetLastError();
         st = PP_ERR_ALLOC;
     }
     if (st == PP_OK) {
@@ -1075,6 +1074,7 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
         if (cudaGetLastError() != cudaSuccess) st = PP_ERR_CUDA;
     }
     if (st != PP_OK) {
+        cudaGetLastError();
         pp_moe_destroy(L);
         return st;
     }
@@ -1084,10 +1084,12 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
 
 static pp_status_t moe_filled(pp_moe_t** out, cudaError_t e, cudaStream_t s) {
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-    if (e == cudaSuccess) return PP_OK;
-    pp_moe_destroy(*out);
-    *out = nullptr;
-    return PP_ERR_CUDA;
+    const pp_status_t st = status_of(e);
+    if (st != PP_OK) {
+        pp_moe_destroy(*out);
+        *out = nullptr;
+    }
+    return st;
 }
 
 extern "C" pp_status_t pp_moe_create(pp_moe_t** out, int E, int H, int F, int top_k, int renormalize, int max_tokens, const void* router,
@@ -1202,7 +1204,5 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     cfg.stream = static_cast<cudaStream_t>(cuda_stream);
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess) return PP_OK;
-    cudaGetLastError();
-    return PP_ERR_CUDA;
+    return status_of(cudaLaunchKernelEx(&cfg, kernel, a));
 }

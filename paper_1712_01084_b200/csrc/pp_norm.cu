@@ -385,5 +385,5 @@ extern "C" pp_status_t pp_rmsnorm_q8(const void* x, int64_t ldx, const void* res
     const cudaError_t e = dtype == PP_F32 ? launch_type<float>(a, vec, group != 0, code_type == PP_E4M3, s)
                         : dtype == PP_F16 ? launch_type<__half>(a, vec, group != 0, code_type == PP_E4M3, s)
                                           : launch_type<__nv_bfloat16>(a, vec, group != 0, code_type == PP_E4M3, s);
-    return e == cudaSuccess ? PP_OK : PP_ERR_CUDA;
+    return status_of(e);
 }

@@ -492,7 +492,6 @@ extern "C" pp_status_t pp_q4_create(pp_q4_t** out, int M, int N, int group, cons
     pp_status_t st = PP_OK;
     if ((cudaMalloc(&L->units, units * kQ4CodeBytes) != cudaSuccess ||
          cudaMalloc(&L->sets_at, units * q4_set_bytes(L->sets, L->asym)) != cudaSuccess || (bias && cudaMalloc(&L->bias, (size_t)M * 4) != cudaSuccess))) {
-        cudaGetLastError();
         st = PP_ERR_ALLOC;
     }
     if (st == PP_OK && (launch_q4_pack(L->units, L->sets_at, codes, scales, zeros, 1, M, N, group, false, s) != cudaSuccess ||
@@ -517,6 +516,7 @@ extern "C" pp_status_t pp_q4_create(pp_q4_t** out, int M, int N, int group, cons
         L->max_clusters[S] = n;
     }
     if (st != PP_OK) {
+        cudaGetLastError();
         pp_q4_destroy(L);
         return st;
     }
@@ -592,8 +592,8 @@ extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_
         a.blocks_each = L->blocks / best;
         a.blocks_more = L->blocks % best;
         const Kernel k = pick_kernel(bytes, tiles_of(a.nc), L->sets, L->asym);
-        if (launch_pdl(k, dim3(best * best_n), dim3(kThreads), smem, static_cast<cudaStream_t>(cuda_stream), best, a) != cudaSuccess)
-            return PP_ERR_CUDA;
+        const pp_status_t st = status_of(launch_pdl(k, dim3(best * best_n), dim3(kThreads), smem, static_cast<cudaStream_t>(cuda_stream), best, a));
+        if (st != PP_OK) return st;
         b0 += a.tokens;
     }
     return PP_OK;

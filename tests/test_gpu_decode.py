@@ -391,6 +391,33 @@ def test_decode_operators_on_another_stream_and_in_sequence():
 
 
 @pytest.mark.gpu
+def test_a_failed_launch_is_not_reported_by_the_next_call():
+    """Launches into a stream capture that is no longer valid fail on the host; a layer made after them does not."""
+    L, driver = pb.lib(), pb.ctypes.CDLL("libcuda.so.1")
+    x, w = torch.randn(2, 256, device="cuda"), torch.ones(256, device="cuda")
+    codes, s, _, _ = _q4_data(40, 64, 256, 64, False)
+    layer = pb.Q4Layer(64, 256, 64, codes, s)
+    q, scales, y = torch.empty(2, 256, device="cuda", dtype=torch.int8), torch.empty(2, device="cuda"), torch.empty(2, 64, device="cuda")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    handle = pb.ctypes.c_void_p(side.cuda_stream)
+    p = lambda t: pb.ctypes.c_void_p(t.data_ptr())  # noqa: E731
+    calls = (lambda: L.pp_rmsnorm_q8(p(x), 256, None, 0, p(w), pb.PP_F32, pb.PP_F32, 2, 256, 1e-6, pb.PP_I8, 0, p(q), p(scales), None, 0, None, handle),
+             lambda: L.pp_q4_forward(layer._h, p(x), 256, pb.PP_F32, None, 0, p(y), pb.PP_F32, 2, 0, handle))
+    for call in calls:
+        assert driver.cuStreamBeginCapture_v2(handle, 2) == 0
+        assert driver.cuStreamSynchronize(handle) != 0                       # not allowed there: the capture is invalid from now on
+        status = call()
+        graph = pb.ctypes.c_void_p()
+        assert driver.cuStreamEndCapture(handle, pb.ctypes.byref(graph)) != 0 and not graph
+        assert status == 5
+        pb.Q4Layer(64, 256, 64, codes, s).close()
+        assert call() == 0
+    side.synchronize()
+    _check_y(y, _q4_data(40, 64, 256, 64, False)[3], x.double())
+
+
+@pytest.mark.gpu
 def test_q4_in_a_graph():
     codes, s, _, w = _q4_data(15, 512, 1024, 64, False)
     L = pb.Q4Layer(512, 1024, 64, codes, s)
