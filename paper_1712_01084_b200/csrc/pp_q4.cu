@@ -46,6 +46,7 @@ constexpr int kParkLd = 20;           // floats between parked columns of 16 row
 // only.  With two, the next call's CTAs start beside this one's; 8192 x 8192 then takes 8.7 us a call, but 12 us whenever
 // the CTAs of a call land on one SM twice, which lasts until the stream runs dry.  One: 9.3 us, always.)
 __host__ __device__ constexpr int depth_of(int nt) { return nt == 4 ? 3 : nt == 1 ? 7 : 4; }
+constexpr int kShallow = 4;           // of binary16 products with one tile, where x leaves no room for 7
 // Columns of the product a vector takes.
 __host__ __device__ constexpr int columns_of(bool bytes, int xtype) { return bytes ? (xtype == PP_I8 ? 1 : 3) : xtype == PP_F32 ? 2 : 1; }
 bool as_bytes(int tokens, int xtype) { return tokens * columns_of(true, xtype) <= 8; }
@@ -185,10 +186,10 @@ __device__ __forceinline__ void stage_x(const Q4Args& a, unsigned char* xs, floa
 }
 
 // (64 registers a thread with bytes: 8192 x 8192 takes 9.7 us, with the 70 to 80 that it would use 9.95)
-template <bool BYTES, int NT, int SETS, bool ASYM>
+template <bool BYTES, int NT, int SETS, bool ASYM, int DEPTH>
 __global__ void __launch_bounds__(kThreads, BYTES ? 2 : 1) q4_kernel(const Q4Args a) {
     extern __shared__ __align__(128) unsigned char smem[];
-    constexpr int kDepth = depth_of(NT);
+    constexpr int kDepth = DEPTH;
     const int S = (int)cluster_size(), rank = (int)cluster_rank(), cl = S == 1 ? blockIdx.x : blockIdx.x / S;
     const int s0 = cl * a.strips_each + min(cl, a.strips_more), n_s = a.strips_each + (cl < a.strips_more);
     const int k0 = rank * a.blocks_each + min(rank, a.blocks_more), n_k = a.blocks_each + (rank < a.blocks_more);
@@ -368,19 +369,26 @@ __global__ void __launch_bounds__(kThreads, BYTES ? 2 : 1) q4_kernel(const Q4Arg
     }
 }
 
+// How a launch multiplies: whole numbers or binary16, and units that each warp keeps in flight.
+struct Form { bool bytes; int depth; };
+
 using Kernel = void (*)(const Q4Args);
-template <bool BYTES, int NT, int SETS> Kernel pick_asym(bool asym) { return asym ? q4_kernel<BYTES, NT, SETS, true> : q4_kernel<BYTES, NT, SETS, false>; }
-template <bool BYTES, int NT> Kernel pick_sets(int sets, bool asym) {
-    return sets == 4 ? pick_asym<BYTES, NT, 4>(asym) : sets == 2 ? pick_asym<BYTES, NT, 2>(asym) : pick_asym<BYTES, NT, 1>(asym);
+template <bool BYTES, int NT, int SETS, int DEPTH> Kernel pick_asym(bool asym) {
+    return asym ? q4_kernel<BYTES, NT, SETS, true, DEPTH> : q4_kernel<BYTES, NT, SETS, false, DEPTH>;
 }
-Kernel pick_kernel(bool bytes, int nt, int sets, bool asym) {
-    return bytes ? pick_sets<true, 1>(sets, asym) : nt == 1 ? pick_sets<false, 1>(sets, asym) : nt == 2 ? pick_sets<false, 2>(sets, asym) : pick_sets<false, 4>(sets, asym);
+template <bool BYTES, int NT, int DEPTH = depth_of(NT)> Kernel pick_sets(int sets, bool asym) {
+    return sets == 4 ? pick_asym<BYTES, NT, 4, DEPTH>(asym) : sets == 2 ? pick_asym<BYTES, NT, 2, DEPTH>(asym) : pick_asym<BYTES, NT, 1, DEPTH>(asym);
+}
+Kernel pick_kernel(Form f, int nt, int sets, bool asym) {
+    return f.bytes ? pick_sets<true, 1>(sets, asym) : nt == 4 ? pick_sets<false, 4>(sets, asym) : nt == 2 ? pick_sets<false, 2>(sets, asym)
+         : f.depth == kShallow ? pick_sets<false, 1, kShallow>(sets, asym) : pick_sets<false, 1>(sets, asym);
 }
 
 constexpr int kMaxSmem = 227 * 1024;
 
 // Shared memory of a launch with clusters of S CTAs that own up to n_s strips each; fills in the offsets.
-size_t plan_smem(Q4Args& a, bool bytes, int sets, int S, int n_s) {
+size_t plan_smem(Q4Args& a, Form f, int sets, int S, int n_s) {
+    const bool bytes = f.bytes;
     const int nt = tiles_of(a.nc), n_k = (a.blocks + S - 1) / S;
     size_t at = (size_t)n_k * kQ4UnitCols * a.nc * (bytes ? 1 : 2);
     a.cs_off = (int)at;
@@ -390,7 +398,7 @@ size_t plan_smem(Q4Args& a, bool bytes, int sets, int S, int n_s) {
     a.plan_off = (int)at;
     at += (size_t)n_s * 2;
     a.ring_off = (int)(at = (at + 127) / 128 * 128);
-    at += (size_t)kWarps * depth_of(nt) * a.slot_bytes;
+    at += (size_t)kWarps * f.depth * a.slot_bytes;
     a.park_off = (int)at;
     const bool paired = !bytes && a.nc != a.tokens;
     at += (size_t)(n_s + kWarps) * kParkLd * (paired ? a.tokens : a.nc) * 4;
@@ -497,8 +505,10 @@ extern "C" pp_status_t pp_q4_create(pp_q4_t** out, int M, int N, int group, cons
     if (st == PP_OK && (launch_q4_pack(L->units, L->sets_at, codes, scales, zeros, 1, M, N, group, false, s) != cudaSuccess ||
                         (bias && cudaMemcpyAsync(L->bias, bias, (size_t)M * 4, cudaMemcpyDeviceToDevice, s) != cudaSuccess) ||
                         cudaStreamSynchronize(s) != cudaSuccess)) st = PP_ERR_CUDA;
-    for (int nt : {0, 1, 2, 4})
-        if (st == PP_OK && opt_in(reinterpret_cast<const void*>(pick_kernel(nt == 0, nt, L->sets, L->asym))) != cudaSuccess) st = PP_ERR_CUDA;
+    for (const Kernel k : {pick_kernel({true, 0}, 1, L->sets, L->asym), pick_kernel({false, kShallow}, 1, L->sets, L->asym),
+                           pick_kernel({false, 0}, 1, L->sets, L->asym), pick_kernel({false, 0}, 2, L->sets, L->asym),
+                           pick_kernel({false, 0}, 4, L->sets, L->asym)})
+        if (st == PP_OK && opt_in(reinterpret_cast<const void*>(k)) != cudaSuccess) st = PP_ERR_CUDA;
     // clusters resident at once, for a CTA of ordinary size (the GPCs hold different numbers of SMs)
     for (int S = 1; S <= 8 && st == PP_OK; S *= 2) {
         cudaLaunchAttribute at;
@@ -512,7 +522,7 @@ extern "C" pp_status_t pp_q4_create(pp_q4_t** out, int M, int N, int group, cons
         cfg.attrs = &at;
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, pick_kernel(true, 1, L->sets, L->asym), &cfg) != cudaSuccess || n < 1) st = PP_ERR_CUDA;
+        if (cudaOccupancyMaxActiveClusters(&n, pick_kernel({true, 0}, 1, L->sets, L->asym), &cfg) != cudaSuccess || n < 1) st = PP_ERR_CUDA;
         L->max_clusters[S] = n;
     }
     if (st != PP_OK) {
@@ -558,8 +568,6 @@ extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_
     int most = kMaxTokens;                       // tokens of one launch
     for (int b0 = 0; b0 < batch;) {
         a.tokens = std::min(batch - b0, most);
-        const bool bytes = as_bytes(a.tokens, x_type);
-        a.nc = a.tokens * columns_of(bytes, x_type);
         a.in.x = static_cast<const char*>(x) + (int64_t)b0 * ldx * xb;
         a.in.scales = x_scales ? x_scales + (int64_t)b0 * a.in.scale_ld : nullptr;
         a.y = static_cast<char*>(y) + (int64_t)b0 * L->M * yb;
@@ -568,30 +576,40 @@ extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_
         // token's columns costs as half a unit.  More strips than one round of clusters can hold go in several rounds.
         int best = 0, best_n = 0;
         int64_t best_cost = 0;
-        for (int S = 1; S <= 8 && S <= L->blocks; S *= 2) {
-            const int n_k = (L->blocks + S - 1) / S;
-            for (int rounds = 1; rounds <= L->strips; ++rounds) {
-                const int n = std::min(L->strips, L->max_clusters[S] * rounds), n_s = (L->strips + n - 1) / n;
-                if (n_s > kMaxStrips || plan_smem(a, bytes, L->sets, S, n_s) > (size_t)kMaxSmem) {
-                    if (n_s == 1) break;
-                    continue;
+        Form form{};
+        const auto plan = [&](Form f) {
+            form = f;
+            a.nc = a.tokens * columns_of(f.bytes, x_type);
+            for (int S = 1; S <= 8 && S <= L->blocks; S *= 2) {
+                const int n_k = (L->blocks + S - 1) / S;
+                for (int rounds = 1; rounds <= L->strips; ++rounds) {
+                    const int n = std::min(L->strips, L->max_clusters[S] * rounds), n_s = (L->strips + n - 1) / n;
+                    if (n_s > kMaxStrips || plan_smem(a, f, L->sets, S, n_s) > (size_t)kMaxSmem) {
+                        if (n_s == 1) break;
+                        continue;
+                    }
+                    const int64_t cost = rounds * (2ll * n_s + a.tokens) * n_k;
+                    if (!best || cost < best_cost) best = S, best_n = n, best_cost = cost;
+                    break;
                 }
-                const int64_t cost = rounds * (2ll * n_s + a.tokens) * n_k;
-                if (!best || cost < best_cost) best = S, best_n = n, best_cost = cost;
-                break;
             }
-        }
-        if (!best) {                                 // x does not fit: fewer tokens at a time
+            return best != 0;
+        };
+        // bytes, where they are the faster form and fit (a float vector of up to some 150,000 columns); then binary16, a shorter
+        // ring before fewer vectors, as fewer vectors read the weights again
+        const int nt = tiles_of(a.tokens * columns_of(false, x_type));
+        if (!(as_bytes(a.tokens, x_type) && plan({true, depth_of(1)})) && !plan({false, depth_of(nt)}) && nt == 1) plan({false, kShallow});
+        if (!best) {                                 // x does not fit: fewer tokens at a time (one does, up to the 2^18 columns of a layer)
             if (a.tokens == 1) return PP_ERR_UNSUPPORTED;
             most = a.tokens / 2;
             continue;
         }
-        const size_t smem = plan_smem(a, bytes, L->sets, best, (L->strips + best_n - 1) / best_n);
+        const size_t smem = plan_smem(a, form, L->sets, best, (L->strips + best_n - 1) / best_n);
         a.strips_each = L->strips / best_n;
         a.strips_more = L->strips % best_n;
         a.blocks_each = L->blocks / best;
         a.blocks_more = L->blocks % best;
-        const Kernel k = pick_kernel(bytes, tiles_of(a.nc), L->sets, L->asym);
+        const Kernel k = pick_kernel(form, tiles_of(a.nc), L->sets, L->asym);
         const pp_status_t st = status_of(launch_pdl(k, dim3(best * best_n), dim3(kThreads), smem, static_cast<cudaStream_t>(cuda_stream), best, a));
         if (st != PP_OK) return st;
         b0 += a.tokens;

@@ -304,6 +304,23 @@ def test_q4_batches(xt, batch):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("group,zeros", [(0, False), (0, True), (32, False), (32, True), (64, True), (128, False)])
+@pytest.mark.parametrize("N", [2 ** 18, 2 ** 18 - 129, 158720 + 128, 120000])
+def test_q4_widest_layers_take_every_input(N, group, zeros):
+    M = 37
+    codes, s, z, w = _q4_data(N + group, M, N, group, zeros)
+    L = pb.Q4Layer(M, N, group, codes, s, z)
+    for batch in (1, 2, 3, 9):
+        x = torch.randn(batch, N, generator=_gen(41), device="cuda")
+        for t in TYPES.values():
+            _check_y(pb.pp_q4_forward(L, x.to(t)), w, x.to(t).double())
+        for kind in ("int8", "e4m3"):
+            q, xs, val = _x8(x, kind, True)
+            _check_y(pb.pp_q4_forward(L, q, x_scales=xs), w, val)
+    L.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M,N,batch", [(8192, 8192, 1), (8192, 8192, 16), (4096, 9216, 8), (20000, 256, 3), (64, 70000, 2), (48, 200000, 16)])
 def test_q4_large(M, N, batch):
     codes, s, z, w = _q4_data(11, M, N, 128, True)
