@@ -21,7 +21,7 @@
 // Columns.  Products with 16-bit weights take the weights' type.  An input that has more bits than one column holds is split
 // over several: bf16 products take f16 in two and f32 in three columns; binary16 products take a token times the power of
 // two that brings its largest magnitude to [2^13, 2^14), in one column for bf16 and two for f32.  4-bit gate and up rows are
-// multiplied as integers, with the token in fixed point as three columns of bytes (pp_q4.cu says how and why).  act is f32
+// multiplied as integers, with the token in fixed point as four columns of bytes (pp_q4.cu says how and why).  act is f32
 // and always takes three columns: in bf16 these are its 24 bits; in binary16 (4-bit experts too), where no scale is known
 // before all of act is, they hold act * 2^-11, the rest * 2^-1 and the rest * 2^10, which together are act to 24 bits
 // between 2^-11 and 2^27 and to an absolute 2^-35 below.
@@ -56,6 +56,7 @@ namespace {
 
 constexpr int kWarps = 16, kThreads = kWarps * 32, kMaxCols = 16;
 constexpr int kMaxExperts = 256, kMaxTopK = 16, kMaxTokens = 32, kActCols = 3, kMaxCap = kMaxCols / kActCols;
+constexpr int kByteCols = byte_columns<float>();      // of a token with 4-bit experts
 constexpr int kRouterParts = 2;            // of a logit, at most
 constexpr int kSpinPolls = 1 << 24;          // seconds; a barrier that is met never gets near it
 
@@ -258,17 +259,17 @@ template <int SETS, int META, typename T, bool VEC> __device__ __forceinline__ v
     const int lane = threadIdx.x & 31;
     const T* x = static_cast<const T*>(a.in.x) + (int64_t)token * a.in.ld;
     for (int kb = threadIdx.x >> 5; kb < a.kb1; kb += kWarps) {
-        uint32_t w[3];
+        uint32_t w[kByteCols];
         float down;
         fixed_point(load_four<VEC>(x, kb * kQ4UnitCols + lane * 4, a.H), 1.0f, w, down);
-        unsigned char* dst = reinterpret_cast<unsigned char*>(a.xcols) + (int64_t)token * 3 * a.kpad1 + kb * kQ4UnitCols + byte_offset(lane);
+        unsigned char* dst = reinterpret_cast<unsigned char*>(a.xcols) + (int64_t)token * kByteCols * a.kpad1 + kb * kQ4UnitCols + byte_offset(lane);
 #pragma unroll
-        for (int c = 0; c < 3; ++c) *reinterpret_cast<uint32_t*>(dst + (int64_t)c * a.kpad1) = w[c];
-        const int sum = byte_sums<SETS>(w, 3, lane), c = lane & (32 / SETS - 1);
-        if (c < 3) {
-            int* meta = a.xmeta + ((int64_t)(token * 3 + c) * a.kb1 + kb) * META;
+        for (int c = 0; c < kByteCols; ++c) *reinterpret_cast<uint32_t*>(dst + (int64_t)c * a.kpad1) = w[c];
+        const int sum = byte_sums<SETS>(w, lane), c = lane & (32 / SETS - 1);
+        if (c < kByteCols) {
+            int* meta = a.xmeta + ((int64_t)(token * kByteCols + c) * a.kb1 + kb) * META;
             meta[lane / (32 / SETS)] = sum;
-            if (lane < 3) meta[SETS] = __float_as_int(down * (c == 2 ? 1.0f : c == 1 ? 256.0f : 65536.0f));
+            if (lane < kByteCols) meta[SETS] = __float_as_int(down * byte_weight<kByteCols>(c));
         }
     }
     if (threadIdx.x == 0) a.xscale[token] = 1.0f;
@@ -568,7 +569,7 @@ template <class W, int STEP, int TILES> struct ColumnsAt {
         const int cpt = STEP == 1 ? a.cpt : kActCols;
         const int4 entry = L.entry[r.entry];
         const auto row = [&](int c) {                        // columns past the last repeat one
-            const int pl = cpt == 1 ? c : cpt == 2 ? c >> 1 : c / 3, p = entry.y + min(pl, entry.z - 1);
+            const int pl = kBytes ? c / kByteCols : cpt == 1 ? c : cpt == 2 ? c >> 1 : c / 3, p = entry.y + min(pl, entry.z - 1);
             return (STEP == 1 ? L.pair_token[p] : p) * cpt + c - pl * cpt;
         };
 #pragma unroll
@@ -883,7 +884,7 @@ template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe
             L.xbytes = reinterpret_cast<const unsigned char*>(a.xcols);
             L.xmeta = a.xmeta;
             if (a.bytes_off) {
-                const int n = a.T * 3 * a.kpad1 / 16, m = (a.T * 3 * a.kb1 * W::kMeta + 3) / 4;
+                const int n = a.T * kByteCols * a.kpad1 / 16, m = (a.T * kByteCols * a.kb1 * W::kMeta + 3) / 4;
                 for (int i = threadIdx.x; i < n; i += kThreads) cp_async16(smem_addr(smem + a.bytes_off) + i * 16, reinterpret_cast<const uint4*>(a.xcols) + i);
                 for (int i = threadIdx.x; i < m; i += kThreads) cp_async16(smem_addr(smem + a.bytes_off) + (n + i) * 16, reinterpret_cast<const uint4*>(a.xmeta) + i);
                 L.xbytes = smem + a.bytes_off;
@@ -979,7 +980,9 @@ template <int TILES> Kernel pick_kernel(const pp_moe* L) {
 // average (64 experts of 2048 x 1024, 8 a token: 4 tokens 61.7 us with two, 62.5 with five; 8 tokens 101.8 and 98.4); 4-bit
 // experts, bound by the products, up to two tokens each (4 tokens 33.8 and 41.5 us, 16 tokens 77.7 and 83.6; 8 experts of
 // 4096 x 2048, 4 tokens each, 69.3 and 57.9).
-int cap_of(int tokens, int top_k, int E, bool q4) { return (q4 ? tokens * top_k <= 2 * E : tokens * top_k < E) ? 8 / kActCols : kMaxCap; }
+int cap_of(int tokens, int top_k, int E, bool q4) {
+    return (q4 ? tokens * top_k <= 2 * E : tokens * top_k < E) ? 8 / (q4 ? kByteCols : kActCols) : q4 ? kMaxCols / kByteCols : kMaxCap;
+}
 int tiles_of(int tokens, int cap) { return std::min(tokens, cap) * kActCols <= 8 ? 1 : 2; }
 
 constexpr int kMaxSmem = 227 * 1024 - 256;       // beside the kernel's few static bytes
@@ -995,7 +998,7 @@ size_t plan_smem(MoeArgs& a, int ring, int tiles, int meta) {
     for (a.round = 32, a.round_log2 = 5;; a.round /= 2, --a.round_log2) {
         const size_t total = at + (size_t)(a.round + kWarps) * 16 * std::max(a.cap, a.T) * 4;
         if (total > (size_t)kMaxSmem && a.round > 1) continue;
-        const size_t bytes = meta ? (size_t)a.T * 3 * a.kpad1 + (size_t)a.T * 3 * a.kb1 * meta * 4 + 16 : 0;
+        const size_t bytes = meta ? (size_t)a.T * kByteCols * a.kpad1 + (size_t)a.T * kByteCols * a.kb1 * meta * 4 + 16 : 0;
         const bool fits = bytes && total + bytes <= (size_t)kMaxSmem;
         a.bytes_off = fits ? (int)total : 0;
         return total + (fits ? bytes : 0);
@@ -1063,7 +1066,7 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
          (set_bytes && (!alloc(&L->gate_up_sets, units1 * set_bytes) || !alloc(&L->down_sets, units2 * set_bytes))) || !alloc(&L->router, ld * E * 4) ||
          !alloc(&L->logits, (size_t)max_tokens * E * kRouterParts * 4) || !alloc(&L->xscale, (size_t)max_tokens * 4) ||
          !alloc(&L->xcols, (size_t)max_tokens * 3 * L->kb1 * cols * 2) || !alloc(&L->acols, abytes) ||
-         (wtype < 0 && !alloc(&L->xmeta, (size_t)max_tokens * 3 * L->kb1 * 32)) ||
+         (wtype < 0 && !alloc(&L->xmeta, (size_t)max_tokens * kByteCols * L->kb1 * 32)) ||
          !alloc(&L->parts, (size_t)L->ctas * 2 * 16 * std::max(kMaxCap, max_tokens) * 4) || !alloc(&L->sync, sync_bytes(L->ctas)))) {
         st = PP_ERR_ALLOC;
     }
@@ -1181,7 +1184,7 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     const int ring = (!q4 && tiles == 2 ? 4 : 6) * a.slot_bytes;           // as depth() of the kernel
     a.gate_up_sets = L->gate_up_sets;
     a.down_sets = L->down_sets;
-    a.cpt = q4 ? 3 : L->wtype == PP_BF16 ? (x_type == PP_BF16 ? 1 : x_type == PP_F16 ? 2 : 3) : (x_type == PP_F32 ? 2 : 1);
+    a.cpt = q4 ? kByteCols : L->wtype == PP_BF16 ? (x_type == PP_BF16 ? 1 : x_type == PP_F16 ? 2 : 3) : (x_type == PP_F32 ? 2 : 1);
     a.bf16_scales = L->bf16_scales;
     a.polls = g_stream_wait_polls;
     a.parts = L->parts;

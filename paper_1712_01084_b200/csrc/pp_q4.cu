@@ -11,15 +11,16 @@
 // Products, one or two vectors (eight of 8-bit integers): the integer tensor-core instruction (16 x 8 x 32, 8-bit operands,
 // exact sums).  The codes need one mask instruction per four weights, where binary16 operands need 4.5.  x becomes fixed
 // point: each block of 128 columns of a vector is multiplied by a power of two that brings its largest magnitude to
-// (2^22, 0.996 * 2^23], rounded to whole numbers, and written as three signed bytes, one column of the product each: an
-// error of at most 2^-23 of the block's largest element, as small as that of an fp32 sum.  Eight columns cost what one
-// costs, so the extra columns are free.  8-bit integers are one column, e4m3 values times 2^9 whole numbers of three
-// bytes; both are exact.
+// (2^30, 0.996 * 2^31], rounded to whole numbers, and written as four signed bytes, one column of the product each: an
+// error of at most 2^-31 of the block's largest element.  Eight columns cost what one costs, so the extra columns are free.
+// (Three bytes would do for blocks of even elements; beside an element 10^4 times as large, in rows whose weight is 0
+// there, they err by several times an fp32 sum's 10^-5.)  8-bit integers are one column, e4m3 values times 2^9 whole numbers
+// of three bytes; both are exact.
 //   sum (q - z) d = sum q d - z sum d  over each set of scales, in exact integers (sum d is made while x is staged and
 // the product starts from -z sum d); then one fp32 multiply-add per set with (scale of the row) * (scale of the column).
 // More vectors: binary16 products (16 x 8 x 16, fp32 sums), where a vector takes one column, an f32 vector two (the second
 // holds what the first one's 11 bits leave over); bf16 and f32 blocks of 128 columns are brought to [2^13, 2^14) by a power
-// of two first.  Eight vectors would be 24 columns of bytes.
+// of two first.  Eight vectors would be 32 columns of bytes.
 //
 // 8192 x 8192, us a call: one vector 9.3 to 9.7 (3.6 TB/s), four of bf16 11.5, eight 13.4, sixteen 17.0, sixteen of f32 23.5
 // (there a unit costs 256 cycles of matrix instructions and 300 of shared memory); 4096 x 4096, one vector, 4.9.
@@ -48,7 +49,7 @@ constexpr int kParkLd = 20;           // floats between parked columns of 16 row
 __host__ __device__ constexpr int depth_of(int nt) { return nt == 4 ? 3 : nt == 1 ? 7 : 4; }
 constexpr int kShallow = 4;           // of binary16 products with one tile, where x leaves no room for 7
 // Columns of the product a vector takes.
-__host__ __device__ constexpr int columns_of(bool bytes, int xtype) { return bytes ? (xtype == PP_I8 ? 1 : 3) : xtype == PP_F32 ? 2 : 1; }
+__host__ __device__ constexpr int columns_of(bool bytes, int xtype) { return bytes ? (xtype == PP_I8 ? 1 : xtype == PP_E4M3 ? 3 : 4) : xtype == PP_F32 ? 2 : 1; }
 bool as_bytes(int tokens, int xtype) { return tokens * columns_of(true, xtype) <= 8; }
 // (16 vectors to a launch: 32 of bf16 in one, four tiles, took 53 us, in two launches 34 us; 8192 x 8192)
 int tiles_of(int nc) { return nc <= 8 ? 1 : nc <= 16 ? 2 : 4; }
@@ -135,7 +136,7 @@ template <typename T> __device__ __forceinline__ float halves(const Pack<T, 4>& 
 template <typename T, bool VEC, bool BYTES, int NT, int SETS, typename Then>
 __device__ __forceinline__ void stage_rows(const Q4Args& a, unsigned char* xs, float* cs, int* sums, int k0, int n_k, int warp, int lane, Then then) {
     constexpr int kAhead = !VEC ? 1 : BYTES ? 2 : sizeof(T) == 4 ? 4 : 8;
-    constexpr int cpt = BYTES ? (std::is_same_v<T, int8_t> ? 1 : 3) : std::is_same_v<T, float> ? 2 : 1;
+    constexpr int cpt = BYTES ? byte_columns<T>() : std::is_same_v<T, float> ? 2 : 1;
     const int items = a.tokens * n_k, step = a.nc * 64;
     const Divider by_blocks(n_k);
     if (warp >= items) then();
@@ -154,18 +155,18 @@ __device__ __forceinline__ void stage_rows(const Q4Args& a, unsigned char* xs, f
             const int item = base + q * kWarps, token = by_blocks.div(item), kb = item - token * n_k;
             if (item >= items) break;
             if constexpr (BYTES) {
-                uint32_t w[3];
+                uint32_t w[cpt];
                 float down;
                 fixed_point(v[q], own[q], w, down);
                 unsigned char* at = xs + (kb * 2 + (lane >> 4)) * step + token * cpt * 64 + ((lane >> 1) & 3) * 16 + (lane & 8) + (lane & 1) * 4;
 #pragma unroll
                 for (int c = 0; c < cpt; ++c) *reinterpret_cast<uint32_t*>(at + c * 64) = w[c];
-                const int sum = byte_sums<SETS>(w, cpt, lane);
+                const int sum = byte_sums<SETS>(w, lane);
                 constexpr int kLanes = 32 / SETS;            // of a set
                 const int c = lane & (kLanes - 1), col = token * cpt + c;
                 if (c < cpt) {
                     sums[(kb * SETS + lane / kLanes) * NT * 8 + col] = sum;
-                    if (lane < cpt) cs[kb * NT * 8 + col] = down * (cpt == 1 || c == 2 ? 1.0f : c == 1 ? 256.0f : 65536.0f);
+                    if (lane < cpt) cs[kb * NT * 8 + col] = down * byte_weight<cpt>(c);
                 }
             } else {
                 uint2 h, rest;
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, BYTES ? 2 : 1) q4_kernel(const Q4Arg
     using Rows = Pack<float, kRows>;
     const int per_token = n_s * (16 / kRows), outs = per_token * a.tokens, share = S == 1 ? outs : (outs + S - 1) / S;
     const int first = rank * share, last = min(outs, first + share);
-    const int cpt = parked == a.tokens ? 1 : 3;              // parked columns of a vector
+    const int cpt = !BYTES || a.in.type == PP_I8 ? 1 : a.in.type == PP_E4M3 ? 3 : 4;     // parked columns of a vector
     const Divider by_token(per_token), by_share(share);
     Rows* red = reinterpret_cast<Rows*>(smem + a.red_off);
     Rows bias{};                                             // of this thread's first results: on their way during the barrier
@@ -335,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, BYTES ? 2 : 1) q4_kernel(const Q4Arg
         for (uint32_t m = plan[strip]; m; m &= m - 1) {
             const float* p = park + (__ffs((int)m) - 1 + strip) * kParkLd * parked + token * cpt * kParkLd + (r & 15);
             Rows w = *reinterpret_cast<const Rows*>(p);
-            if (BYTES && cpt == 3) w.v[0] += p[kParkLd] + p[2 * kParkLd];
+            if (BYTES && cpt > 1) w.v[0] += p[kParkLd] + (cpt == 4 ? p[2 * kParkLd] + p[3 * kParkLd] : p[2 * kParkLd]);
 #pragma unroll
             for (int i = 0; i < kRows; ++i) v.v[i] += w.v[i];
         }
@@ -595,7 +596,7 @@ extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_
             }
             return best != 0;
         };
-        // bytes, where they are the faster form and fit (a float vector of up to some 150,000 columns); then binary16, a shorter
+        // bytes, where they are the faster form and fit (a float vector of up to some 120,000 columns); then binary16, a shorter
         // ring before fewer vectors, as fewer vectors read the weights again
         const int nt = tiles_of(a.tokens * columns_of(false, x_type));
         if (!(as_bytes(a.tokens, x_type) && plan({true, depth_of(1)})) && !plan({false, depth_of(nt)}) && nt == 1) plan({false, kShallow});

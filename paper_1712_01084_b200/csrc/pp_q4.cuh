@@ -178,34 +178,42 @@ struct Divider {
 
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
 
-// Four whole numbers of a lane, |v| < 2^23, as three words of signed bytes, the highest first.  Adding 0x808080 carries
-// what a signed byte below cannot hold into the byte above; the sign bits then flip back.
-__device__ __forceinline__ void three_bytes(const int (&v)[4], uint32_t (&w)[3]) {
+// Columns of bytes that a vector takes: an 8-bit integer is one, an e4m3 value times 2^9 a whole number of three, floats are
+// fixed point of four.
+template <typename T> __host__ __device__ constexpr int byte_columns() { return std::is_same_v<T, int8_t> ? 1 : sizeof(T) == 1 ? 3 : 4; }
+// What column c of N stands for, in units of the last.
+template <int N> __device__ __forceinline__ float byte_weight(int c) { return __int_as_float((127 + 8 * (N - 1 - c)) << 23); }
+
+// Four whole numbers of a lane, |v| < 0.996 * 2^(8N - 1), as N words of signed bytes, the highest first.  Adding 0x80808080
+// carries what a signed byte below cannot hold into the byte above; the sign bits then flip back.
+template <int N> __device__ __forceinline__ void signed_bytes(const int (&v)[4], uint32_t (&w)[N]) {
     uint32_t u[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = ((uint32_t)v[i] + 0x808080u) ^ 0x808080u;
-    const uint32_t a = prmt(u[0], u[1], 0x5140), b = prmt(u[2], u[3], 0x5140);
-    w[2] = prmt(a, b, 0x5410);
-    w[1] = prmt(a, b, 0x7632);
-    w[0] = prmt(prmt(u[0], u[1], 0x0062), prmt(u[2], u[3], 0x0062), 0x5410);
+    for (int i = 0; i < 4; ++i) u[i] = ((uint32_t)v[i] + 0x80808080u) ^ 0x80808080u;
+    const uint32_t a = prmt(u[0], u[1], 0x5140), b = prmt(u[2], u[3], 0x5140), c = prmt(u[0], u[1], 0x7362), d = prmt(u[2], u[3], 0x7362);
+    w[N - 1] = prmt(a, b, 0x5410);
+    w[N - 2] = prmt(a, b, 0x7632);
+    w[N - 3] = prmt(c, d, 0x5410);
+    if (N == 4) w[0] = prmt(c, d, 0x7632);
 }
 
 // A warp's block of 128 columns of one vector, four per lane: its columns' bytes and what one of them stands for (in
 // `down`, of the lowest byte).  own: an 8-bit input's scale.
-template <typename T> __device__ __forceinline__ void fixed_point(const Pack<T, 4>& x, float own, uint32_t (&w)[3], float& down) {
-    int v[4];
+template <typename T> __device__ __forceinline__ void fixed_point(const Pack<T, 4>& x, float own, uint32_t (&w)[byte_columns<T>()], float& down) {
     if constexpr (std::is_same_v<T, int8_t>) {
         w[0] = *reinterpret_cast<const uint32_t*>(&x);
         down = own;
-        return;
     } else if constexpr (sizeof(T) == 1) {
+        int v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = __float2int_rn(to_float(x.v[i]) * 512.0f);
         // NaN is the only e4m3 value that is not finite: the whole vector is not
         const bool nan = __any_sync(0xffffffffu, to_float(x.v[0]) + to_float(x.v[1]) + to_float(x.v[2]) + to_float(x.v[3]) !=
                                                      to_float(x.v[0]) + to_float(x.v[1]) + to_float(x.v[2]) + to_float(x.v[3]));
         down = nan ? __int_as_float(0x7fffffff) : own * 0x1p-9f;
+        signed_bytes<3>(v, w);
     } else {
+        int v[4];
         float f[4];
         uint32_t most = 0u;
 #pragma unroll
@@ -214,41 +222,37 @@ template <typename T> __device__ __forceinline__ void fixed_point(const Pack<T, 
             most = max(most, __float_as_uint(f[i]) & 0x7fffffffu);        // as whole numbers: a NaN is the largest
         }
         most = __reduce_max_sync(0xffffffffu, most);
-        const uint32_t e = max(most >> 23, 23u);                           // smaller blocks keep the scale of 2^-104
-        float up = __uint_as_float((276u - min(e, 254u)) << 23);
-        down = __uint_as_float((min(e, 254u) - 22u) << 23);
-        if (__uint_as_float(most) * up > 8355000.0f) {
+        const uint32_t e = min(max(most >> 23, 31u), 254u);                // blocks below 2^-96 keep the scale of that
+        float up = __uint_as_float((284u - e) << 23);
+        down = __uint_as_float((e - 30u) << 23);
+        if (__uint_as_float(most) * up > 2139062016.0f) {                  // the largest float below 0x7f7f7f7f
             up *= 0.5f;
             down *= 2.0f;
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = __float2int_rn(f[i] * up);
         if (most >= 0x7f800000u) down = __int_as_float(0x7fffffff);        // an infinity or a NaN: so are the sums
+        signed_bytes<4>(v, w);
     }
-    three_bytes(v, w);
 }
 
-// The sums of a warp's three columns of bytes over each set of scales: lanes 0 .. cpt - 1 of a set's lanes have column `lane`'s.
-template <int SETS> __device__ __forceinline__ int byte_sums(const uint32_t (&w)[3], int cpt, int lane) {
-    int sum[2] = {0, 0};                                     // 2^16 (highest byte) + (middle byte), and the lowest
-    if (cpt == 1) {
-        sum[0] = __dp4a((int)w[0], 0x01010101, 0);
-    } else {
-        sum[0] = __dp4a((int)w[0], 0x01010101, 0) * 65536 + __dp4a((int)w[1], 0x01010101, 0);
-        sum[1] = __dp4a((int)w[2], 0x01010101, 0);
-    }
+// The sums of a warp's N columns of bytes over each set of scales: lanes 0 .. N - 1 of a set's lanes have column `lane`'s.
+template <int SETS, int N> __device__ __forceinline__ int byte_sums(const uint32_t (&w)[N], int lane) {
+    constexpr int kWords = (N + 1) / 2;
+    int sum[kWords];                                         // 2^16 (one column's) + (the next one's), or one alone
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        if (c == 1 && cpt == 1) break;
+    for (int i = 0; i < kWords; ++i) {
+        sum[i] = __dp4a((int)w[2 * i], 0x01010101, 0);
+        if (2 * i + 1 < N) sum[i] = sum[i] * 65536 + __dp4a((int)w[2 * i + 1], 0x01010101, 0);
         if (SETS == 1) {
-            sum[c] = __reduce_add_sync(0xffffffffu, sum[c]);
+            sum[i] = __reduce_add_sync(0xffffffffu, sum[i]);
         } else {
 #pragma unroll
-            for (int o = 16 / SETS; o; o >>= 1) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], o);
+            for (int o = 16 / SETS; o; o >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
         }
     }
-    const int c = lane & (32 / SETS - 1), middle = (int16_t)sum[0];
-    return cpt == 1 || c == 1 ? middle : c == 0 ? (sum[0] - middle) >> 16 : sum[1];
+    const int c = lane & (32 / SETS - 1), s = c >= 2 && kWords > 1 ? sum[kWords - 1] : sum[0], low = (int16_t)s;
+    return N == 1 || (N == 3 && c == 2) ? s : c & 1 ? low : (s - low) >> 16;
 }
 // Where a lane's four bytes of a block lie among its column's 128: [64 columns][lane t][8 bytes of 32 columns, 8 of the next].
 __device__ __forceinline__ int byte_offset(int lane) { return (lane >> 4) * 64 + ((lane >> 1) & 3) * 16 + (lane & 8) + (lane & 1) * 4; }

@@ -355,6 +355,29 @@ def test_q4_strides_alignment_and_range(xt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("xt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("group", [32, 64, 128, 0])
+@pytest.mark.parametrize("ratio", [1e3, 1e4])
+def test_q4_elements_that_stand_out_beside_zero_weights(xt, group, ratio):
+    """One element of 128 a thousand or ten thousand times the rest, in columns where every other row's weight is 0: in those
+    rows the tolerance is that of the rest alone, 0.8 SUM |w| on average.  Fixed point of 31 bits errs by up to 2^-31 * 2e4 =
+    0.93 SUM of |w| where the errors of 127 elements agree, by a tenth of that where they are independent."""
+    M, N = 64, 1000
+    codes, s, _, w = _q4_data(50 + group, M, N, group, False)
+    out = torch.arange(60, N, 128, device="cuda")
+    for c in out.tolist():                                                   # the zero point, 8: a weight of 0
+        low = c % 2 == 0
+        codes[::2, c // 2] = (codes[::2, c // 2] & (0xF0 if low else 0x0F)) | (0x08 if low else 0x80)
+    w[::2, out] = 0.0
+    L = pb.Q4Layer(M, N, group, codes, s)
+    for batch in (1, 2, 3):
+        x = torch.randn(batch, N, generator=_gen(51), device="cuda")
+        x[:, out] = ratio * (1 + torch.rand(batch, len(out), generator=_gen(52), device="cuda"))
+        x = x.to(TYPES[xt])
+        _check_y(pb.pp_q4_forward(L, x), w, x.double())
+
+
+@pytest.mark.gpu
 def test_q4_not_finite_inputs_stay_in_their_row():
     M, N = 64, 512
     codes, s, z, w = _q4_data(13, M, N, 128, False)

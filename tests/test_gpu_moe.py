@@ -149,6 +149,29 @@ def test_moe_range_of_inputs(weights):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 2, 6])
+@pytest.mark.parametrize("xt", ["f32", "bf16"])
+def test_moe_four_bit_tokens_with_elements_that_stand_out(xt, T):
+    """Elements of a token ten thousand times the rest where router, gate and up have zeros: the tolerance is the rest's."""
+    E, k, H, F = 4, 2, 512, 64
+    g = _gen(13)
+    out = torch.arange(60, H, 128, device="cuda")
+    c = object.__new__(Case)
+    c.E, c.k, c.H, c.F, c.renorm = E, k, H, F, True
+    r = torch.randn(E, H, generator=g, device="cuda") / H ** 0.5
+    r[:, out] = 0.0
+    uc, us, _, c.u = _codes(g, E, 2 * F, H, 128, False)
+    uc[..., out // 2] = (uc[..., out // 2] & 0xF0) | 0x08                     # even columns: the low half, the zero point 8
+    c.u[..., out] = 0.0
+    dc, ds, _, c.d = _codes(g, E, H, F, 128, False)
+    c.r = r.double()
+    c.layer = pb.MoELayer.q4(r, uc, us, dc, ds, group=128, inner=F, top_k=k, max_tokens=T)
+    x = torch.randn(T, H, generator=g, device="cuda")
+    x[:, out] = 1e4 * (1 + torch.rand(T, len(out), generator=g, device="cuda"))
+    c.check(x.to(TYPES[xt]), torch.float32)
+
+
+@pytest.mark.gpu
 def test_moe_ties_go_to_the_lowest_index():
     E, H = 12, 64
     r = torch.zeros(E, H, device="cuda")
