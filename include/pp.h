@@ -506,8 +506,9 @@ pp_status_t pp_q4_forward(pp_q4_t* layer, const void* x, int64_t ldx, pp_dtype_t
  * ids_out       device, int32 [tokens][top_k], or NULL: the chosen experts, best first
  * gates_out     device, float [tokens][top_k], or NULL: their p
  * Logits, p and all sums are fp32.  x and act = p silu(G x) (U x) enter the products with 22 to 24 bits (x with 4-bit
- * experts: fixed point per 128 columns, as in pp_q4_forward for one vector); with f16 and 4-bit experts act does so
- * between 2^-11 and 2^27, with an absolute 2^-35 below, and overflows above.  A token with a NaN or an
+ * experts: fixed point per 128 columns, as in pp_q4_forward for one vector); with f16 and 4-bit experts act does so down to
+ * 2^-35 of the largest value that the norms of the token and of the layer's gate and up rows allow, with an absolute 2^-59 of it
+ * below.  A token with a NaN or an
  * infinity has outputs that are not finite; other tokens are not touched by it.
  * One cooperative kernel; results do not depend on scheduling.  Only enqueues.  Calls on one handle must be ordered on
  * one stream.  Its two grid-wide waits are bounded (tuning key 15): when one gives up y is invalid, and so is what later calls

@@ -22,15 +22,18 @@
 // over several: bf16 products take f16 in two and f32 in three columns; binary16 products take a token times the power of
 // two that brings its largest magnitude to [2^13, 2^14), in one column for bf16 and two for f32.  4-bit gate and up rows are
 // multiplied as integers, with the token in fixed point as four columns of bytes (pp_q4.cu says how and why).  act is f32
-// and always takes three columns: in bf16 these are its 24 bits; in binary16 (4-bit experts too), where no scale is known
-// before all of act is, they hold act * 2^-11, the rest * 2^-1 and the rest * 2^10, which together are act to 24 bits
-// between 2^-11 and 2^27 and to an absolute 2^-35 below.
+// and always takes three columns: in bf16 these are its 24 bits; in binary16 (4-bit experts too) they hold v * 2^-11, the
+// rest * 2^-1 and the rest * 2^10, which together are v to 24 bits between 2^-11 and 2^27 and to an absolute 2^-35 below.  No
+// element's size is known before all of act is, but a bound is: |G x| |U x| <= |G| |U| |x|^2 in norms of rows and token.  v is
+// act times the token's power of two that brings this bound to 2^26, so it cannot overflow, and 24 bits hold down to 2^-35 of
+// the bound (powers of two are up to 4 above it); with random rows the bound is about H times a typical element.  y takes the power of two back.
 //
 // us a call: 64 experts of 4096 x 2048, 8 a token, bf16, 16 tokens 442 (6.4 TB/s); 64 of 2048 x 1024, 4 tokens, 4 bits 33.0
 // (of 13 for the bytes: bound by instructions); 8 experts of 1024, 2 a token, one token 13.0 (bound by the steps' latency).
 #include "pp_q4.cuh"
 
 #include <algorithm>
+#include <cmath>
 #include <new>
 
 namespace pp {
@@ -40,6 +43,7 @@ extern int g_stream_wait_polls;
 struct pp_moe {
     int E, H, F, top_k, renorm, max_tokens, wtype, sets;      // wtype: PP_F16, PP_BF16 or -1 for 4-bit codes
     bool asym, bf16_scales;
+    int act_bound;
     int strips1, strips2, kb1, kb2;
     int ctas;                 // that the device holds at once
     unsigned char *gate_up, *down, *gate_up_sets, *down_sets;
@@ -64,7 +68,7 @@ struct MoeArgs {
     const unsigned char *gate_up, *down, *gate_up_sets, *down_sets;       // units, and their sets of 4-bit scales
     const float* router;
     XIn in;
-    float *logits, *xscale, *parts;
+    float *logits, *xscale, *parts;           // xscale: [tokens] of the inputs, then [tokens] of act
     uint16_t *xcols, *acols;
     int* xmeta;                              // 4-bit experts: [token's column][block] {its sums over the sets, its scale}
     int* sync;
@@ -79,6 +83,7 @@ struct MoeArgs {
     int round;                               // strips of a round
     int cap;                                 // tokens of an entry, at most
     int list_off, scr_off, park_off;         // shared memory; the weight rings are at 0
+    int act_bound;                           // |row of G| |row of U| <= 2^act_bound
     int bytes_off;                           // 4-bit experts: where the tokens' bytes go, 0 if they stay in global memory
 };
 
@@ -207,6 +212,14 @@ template <bool BF16> __device__ __forceinline__ void split_act(float v, uint16_t
     }
 }
 
+// The power of two of a token's act: 2^26 / (a bound of its elements), sum: the squares of the token.  Every fp32 number times
+// the smallest, 2^-101, still fits the three columns.
+__device__ __forceinline__ float act_scale(float sum, int act_bound) {
+    const int e = (int)(__float_as_uint(sum) >> 23 & 255u) - 126;         // sum < 2^e
+    return __uint_as_float((uint32_t)(min(max(26 - e - act_bound, -101), 126) + 127) << 23);
+}
+__device__ __forceinline__ float inverse_power(float p) { return __uint_as_float((254u << 23) - __float_as_uint(p)); }
+
 // Columns a token takes.
 template <bool BF16, typename T> __host__ __device__ constexpr int columns() {
     return std::is_same_v<T, float> ? (BF16 ? 3 : 2) : BF16 && std::is_same_v<T, __half> ? 2 : 1;
@@ -218,24 +231,36 @@ template <class W, typename T, bool VEC> __device__ __forceinline__ void token_c
     constexpr bool BF16 = W::kBf16;
     constexpr int cpt = columns<BF16, T>();
     const T* x = static_cast<const T*>(a.in.x) + (int64_t)token * a.in.ld;
-    float up = 1.0f, down = 1.0f;
-    if (!BF16 && !std::is_same_v<T, __half>) {
-        float most = 0.0f;
+    float up = 1.0f, down = 1.0f, act = 1.0f;
+    if (!BF16) {
+        float most = 0.0f, sum = 0.0f;
 #pragma unroll 2
         for (int c = threadIdx.x * 4; c < a.H; c += kThreads * 4) {
             const Pack<T, 4> v = load_four<VEC>(x, c, a.H);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(to_float(v.v[i])));
+            for (int i = 0; i < 4; ++i) {
+                const float f = to_float(v.v[i]);
+                most = fmaxf(most, fabsf(f));
+                sum = fmaf(f, f, sum);
+            }
         }
 #pragma unroll
-        for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        for (int o = 16; o; o >>= 1) {
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        }
         __syncthreads();                                     // an earlier token's values have been read
-        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = most;
+        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = most, part[kWarps + (threadIdx.x >> 5)] = sum;
         __syncthreads();
         most = part[threadIdx.x & (kWarps - 1)];
+        sum = part[kWarps + (threadIdx.x & (kWarps - 1))];
 #pragma unroll
-        for (int o = kWarps / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        f16_scale(most, up, down);
+        for (int o = kWarps / 2; o; o >>= 1) {
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        }
+        if (!std::is_same_v<T, __half>) f16_scale(most, up, down);
+        act = act_scale(sum, a.act_bound);
     }
     uint16_t* dst = a.xcols + (int64_t)token * cpt * a.kpad1;
 #pragma unroll 2
@@ -251,17 +276,21 @@ template <class W, typename T, bool VEC> __device__ __forceinline__ void token_c
 #pragma unroll
         for (int k = 0; k < cpt; ++k) *reinterpret_cast<Pack<uint16_t, 4>*>(dst + (int64_t)k * a.kpad1 + c) = bits[k];
     }
-    if (threadIdx.x == 0) a.xscale[token] = down;
+    if (threadIdx.x == 0) a.xscale[token] = down, a.xscale[a.T + token] = act;
 }
 
 // The same for 4-bit experts: a warp per block of 128 columns.
-template <int SETS, int META, typename T, bool VEC> __device__ __forceinline__ void token_bytes(const MoeArgs& a, int token) {
+template <int SETS, int META, typename T, bool VEC> __device__ __forceinline__ void token_bytes(const MoeArgs& a, int token, float* part) {
     const int lane = threadIdx.x & 31;
+    float squares = 0.0f;
     const T* x = static_cast<const T*>(a.in.x) + (int64_t)token * a.in.ld;
     for (int kb = threadIdx.x >> 5; kb < a.kb1; kb += kWarps) {
         uint32_t w[kByteCols];
         float down;
-        fixed_point(load_four<VEC>(x, kb * kQ4UnitCols + lane * 4, a.H), 1.0f, w, down);
+        const Pack<T, 4> v = load_four<VEC>(x, kb * kQ4UnitCols + lane * 4, a.H);
+        fixed_point(v, 1.0f, w, down);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) squares = fmaf(to_float(v.v[i]), to_float(v.v[i]), squares);
         unsigned char* dst = reinterpret_cast<unsigned char*>(a.xcols) + (int64_t)token * kByteCols * a.kpad1 + kb * kQ4UnitCols + byte_offset(lane);
 #pragma unroll
         for (int c = 0; c < kByteCols; ++c) *reinterpret_cast<uint32_t*>(dst + (int64_t)c * a.kpad1) = w[c];
@@ -272,7 +301,18 @@ template <int SETS, int META, typename T, bool VEC> __device__ __forceinline__ v
             if (lane < kByteCols) meta[SETS] = __float_as_int(down * byte_weight<kByteCols>(c));
         }
     }
-    if (threadIdx.x == 0) a.xscale[token] = 1.0f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
+    __syncthreads();                                         // an earlier token's have been read
+    if (lane == 0) part[threadIdx.x >> 5] = squares;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        squares = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) squares += part[w];
+        a.xscale[token] = 1.0f;
+        a.xscale[a.T + token] = act_scale(squares, a.act_bound);
+    }
 }
 
 // A warp's part of the logit of one (token, expert): columns from .. to.
@@ -308,7 +348,7 @@ template <typename T, bool VEC> __device__ __forceinline__ float router_part(con
 // warp 1 and so on; a row is cut into as many parts as keep every warp at one.
 template <class W, typename T, bool VEC> __device__ __forceinline__ void step0(const MoeArgs& a, float* part) {
     for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
-        if constexpr (W::kBytes) token_bytes<W::kSets, W::kMeta, T, VEC>(a, t);
+        if constexpr (W::kBytes) token_bytes<W::kSets, W::kMeta, T, VEC>(a, t, part);
         else token_columns<W, T, VEC>(a, t, part);
     }
     for (int i = (threadIdx.x >> 5) * gridDim.x + (gridDim.x - 1 - blockIdx.x); i < a.T * a.E * a.router_parts; i += kWarps * gridDim.x) {
@@ -339,7 +379,7 @@ struct Lists {
     float* pair_gate;
     int* chosen;         // [T][top_k] experts
     float* gate;         // [T][top_k]
-    float* xscale;       // [T]
+    float* xscale;       // [T], then act's [T]
     uint32_t* tokens;    // [E] which tokens chose the expert
     int* first;          // [E] its first pair
     int* sums;           // [warps] scratch of the scan
@@ -348,7 +388,7 @@ struct Lists {
     int* cuts;           // [2][2] first and last CTA of the strips that the CTA's ends divide, [4..5] whether it finishes them
 };
 __host__ __device__ inline int list_bytes(int T, int E, int top_k) {
-    return (T * top_k * (16 + 4 + 4 + 4 + 4) + 32 * 8 + T * 4 + E * 8 + 16 * 4 + 8 * 4 + 127) / 128 * 128;
+    return (T * top_k * (16 + 4 + 4 + 4 + 4) + 32 * 8 + T * 8 + E * 8 + 16 * 4 + 8 * 4 + 127) / 128 * 128;
 }
 __device__ __forceinline__ Lists lists_at(unsigned char* p, int T, int E, int top_k) {
     Lists L;
@@ -360,7 +400,7 @@ __device__ __forceinline__ Lists lists_at(unsigned char* p, int T, int E, int to
     L.chosen = reinterpret_cast<int*>(L.pair_gate + n);
     L.gate = reinterpret_cast<float*>(L.chosen + n);
     L.xscale = L.gate + n;
-    L.tokens = reinterpret_cast<uint32_t*>(L.xscale + T);
+    L.tokens = reinterpret_cast<uint32_t*>(L.xscale + 2 * T);
     L.first = reinterpret_cast<int*>(L.tokens + E);
     L.sums = L.first + E;
     L.cuts = L.sums + 16;
@@ -440,13 +480,13 @@ template <int kEach> __device__ __forceinline__ void choose(const MoeArgs& a, co
 
 __device__ __forceinline__ int route(const MoeArgs& a, const Lists& L) {       // the number of entries; L.tokens is zero before
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const float xscale = tid < a.T ? __ldcg(a.xscale + tid) : 0.0f;       // stored behind the choice, which would wait for it
+    const float xscale = tid < 2 * a.T ? __ldcg(a.xscale + tid) : 0.0f;       // stored behind the choice, which would wait for it
     for (int t = warp; t < a.T; t += kWarps) {
         if (a.E <= 32) choose<1>(a, L, t);
         else if (a.E <= 64) choose<2>(a, L, t);
         else choose<kMaxExperts / 32>(a, L, t);
     }
-    if (tid < a.T) L.xscale[tid] = xscale;
+    if (tid < 2 * a.T) L.xscale[tid] = xscale;
     __syncthreads();
     if (a.T == 1) return a.top_k;                            // its lists are made (8 experts: 13.3 us, through the counts below 13.6)
     // where each expert's pairs and entries start: both counts in one scan (neither exceeds 512)
@@ -653,15 +693,18 @@ template <class W, int STEP, int TILES> struct Fetcher {
 // What a strip's sums become.  Step 1: act of one (row, pair), step 2: y of one (row, token).
 template <class W> __device__ __forceinline__ void finish_act(const MoeArgs& a, const Lists& L, int entry, int strip, int row8, int pl, float gate, float up) {
     const int p = L.entry[entry].y + pl, row = (strip - entry * a.strips1) * 8 + row8;
-    const float scale = L.xscale[L.pair_token[p]];
+    const int token = L.pair_token[p];
+    const float scale = L.xscale[token];
     gate *= scale;
     up *= scale;
-    const float act = L.pair_gate[p] * (__fdividef(gate, 1.0f + expf(-gate)) * up);
+    float act = L.pair_gate[p] * (__fdividef(gate, 1.0f + expf(-gate)) * up);
+    if (!W::kBf16) act *= L.xscale[a.T + token];
     const int at = W::kSwap && ((row & 3) == 1 || (row & 3) == 2) ? row ^ 3 : row;
     split_act<W::kBf16>(act, a.acols + (int64_t)p * kActCols * a.kpad2 + at, a.kpad2);
 }
-__device__ __forceinline__ void finish_y(const MoeArgs& a, int strip, int row, int token, float v) {
+template <class W> __device__ __forceinline__ void finish_y(const MoeArgs& a, const Lists& L, int strip, int row, int token, float v) {
     const int m = strip * 16 + row;
+    if (!W::kBf16) v *= inverse_power(L.xscale[a.T + token]);
     if (m < a.H) store_y(a.y, (int64_t)token * a.H + m, a.y_type, v);
 }
 
@@ -799,7 +842,7 @@ __device__ __forceinline__ void stream(const MoeArgs& a, const Lists& L, const S
                 const int q = by_strip.div(o), r = o - q * per_strip, ls = ls0 + q;
                 const float v = pieces((uint32_t)L.plan[q].x, q, r);
                 if (sub) continue;
-                if (!cut(ls)) finish_y(a, s.first + ls, r & 15, r >> 4, v);
+                if (!cut(ls)) finish_y<W>(a, L, s.first + ls, r & 15, r >> 4, v);
                 else __stcg(part(ls) + r, v);
             }
         }
@@ -850,13 +893,13 @@ template <class W, int STEP> __device__ __forceinline__ void join(const MoeArgs&
             if (STEP == 1) v[1] += __ldcg(part + 8);
         }
         if (STEP == 1) finish_act<W>(a, L, entry, strip, row, pl, v[0], v[1]);
-        else finish_y(a, strip, r & 15, r >> 4, v[0]);
+        else finish_y<W>(a, L, strip, r & 15, r >> 4, v[0]);
     }
 }
 
 template <class W, int TILES> __global__ void __launch_bounds__(kThreads, 1) moe_kernel(const MoeArgs a) {
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ float part[kWarps];
+    __shared__ float part[2 * kWarps];
     __shared__ int flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     Lists L = lists_at(smem + a.list_off, a.T, a.E, a.top_k);
@@ -959,6 +1002,51 @@ __global__ void router_pack_kernel(float* dst, const void* r, int type, int E, i
     }
 }
 
+// The largest square of a row's norm among gate rows (most[0]) and up rows (most[1]) of all experts, rows that are not finite left
+// out (what they give is not finite either); a warp to a row.  scales: of 4-bit codes, else binary16 weights.
+__global__ void row_norms_kernel(unsigned long long* most, const void* w, const uint16_t* scales, const uint8_t* zeros, bool bf16_scales, int64_t rows,
+                                 int F, int cols, int group) {
+    const int lane = threadIdx.x & 31, groups = group ? (cols + group - 1) / group : 1;
+    const int64_t code_ld = (cols + 1) / 2, step = (int64_t)gridDim.x * (blockDim.x >> 5);
+    for (int64_t r = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5); r < rows; r += step) {
+        double sum = 0.0;
+        for (int c = lane; c < cols; c += 32) {
+            float v;
+            if (scales) {
+                const int64_t at = r * groups + (group ? c / group : 0);
+                const uint16_t s = scales[at];
+                const int q = static_cast<const uint8_t*>(w)[r * code_ld + c / 2] >> (4 * (c & 1)) & 15, z = zeros ? zeros[at] & 15 : 8;
+                v = (float)(q - z) * (bf16_scales ? __uint_as_float((uint32_t)s << 16) : __half2float(__ushort_as_half(s)));
+            } else {
+                v = __half2float(static_cast<const __half*>(w)[r * cols + c]);
+            }
+            sum += (double)v * v;
+        }
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0 && sum < INFINITY) atomicMax(most + (r % (2 * F) >= F), (unsigned long long)__double_as_longlong(sum));
+    }
+}
+
+// The exponent of a power of two that no product of a gate row's and an up row's norm exceeds.
+cudaError_t find_act_bound(pp_moe* L, const void* w, const void* scales, const void* zeros, int group, cudaStream_t stream) {
+    unsigned long long* most = nullptr;
+    double norms[2] = {0.0, 0.0};
+    const int64_t rows = (int64_t)L->E * 2 * L->F;
+    cudaError_t e = cudaMalloc(&most, sizeof(norms));
+    if (e == cudaSuccess) e = cudaMemsetAsync(most, 0, sizeof(norms), stream);
+    if (e == cudaSuccess) {
+        row_norms_kernel<<<(unsigned)std::min<int64_t>((rows + 7) / 8, 148 * 16), 256, 0, stream>>>(
+            most, w, static_cast<const uint16_t*>(scales), static_cast<const uint8_t*>(zeros), L->bf16_scales, rows, L->F, L->H, group);
+        e = cudaGetLastError();
+    }
+    if (e == cudaSuccess) e = cudaMemcpyAsync(norms, most, sizeof(norms), cudaMemcpyDeviceToHost, stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+    cudaFree(most);
+    // (rounding of the sums in fp32 has room above the bound: 2^26 of 2^27)
+    if (e == cudaSuccess) L->act_bound = norms[0] > 0.0 && norms[1] > 0.0 ? (int)std::ceil(0.5 * (std::log2(norms[0]) + std::log2(norms[1]))) : 0;
+    return e;
+}
+
 cudaError_t launch_wide_pack(void* dst, const void* w, int count, int rows, int cols, bool paired, cudaStream_t stream) {
     const int strips = strips_of(rows, paired), blocks = (cols + 31) / 32;
     const int64_t n = (int64_t)count * strips * blocks;
@@ -985,7 +1073,7 @@ int cap_of(int tokens, int top_k, int E, bool q4) {
 }
 int tiles_of(int tokens, int cap) { return std::min(tokens, cap) * kActCols <= 8 ? 1 : 2; }
 
-constexpr int kMaxSmem = 227 * 1024 - 256;       // beside the kernel's few static bytes
+constexpr int kMaxSmem = 227 * 1024 - 384;       // beside the kernel's few static bytes
 
 // Strips of a round and the shared memory: the most strips that fit, 32 at most.
 size_t plan_smem(MoeArgs& a, int ring, int tiles, int meta) {
@@ -1064,7 +1152,7 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
     if (st == PP_OK &&
         (!alloc(&L->gate_up, units1 * 1024) || !alloc(&L->down, units2 * 1024) ||
          (set_bytes && (!alloc(&L->gate_up_sets, units1 * set_bytes) || !alloc(&L->down_sets, units2 * set_bytes))) || !alloc(&L->router, ld * E * 4) ||
-         !alloc(&L->logits, (size_t)max_tokens * E * kRouterParts * 4) || !alloc(&L->xscale, (size_t)max_tokens * 4) ||
+         !alloc(&L->logits, (size_t)max_tokens * E * kRouterParts * 4) || !alloc(&L->xscale, (size_t)max_tokens * 8) ||
          !alloc(&L->xcols, (size_t)max_tokens * 3 * L->kb1 * cols * 2) || !alloc(&L->acols, abytes) ||
          (wtype < 0 && !alloc(&L->xmeta, (size_t)max_tokens * kByteCols * L->kb1 * 32)) ||
          !alloc(&L->parts, (size_t)L->ctas * 2 * 16 * std::max(kMaxCap, max_tokens) * 4) || !alloc(&L->sync, sync_bytes(L->ctas)))) {
@@ -1105,6 +1193,7 @@ extern "C" pp_status_t pp_moe_create(pp_moe_t** out, int E, int H, int F, int to
     if (st != PP_OK) return st;
     cudaError_t e = launch_wide_pack((*out)->gate_up, gate_up, E, 2 * F, H, true, s);
     if (e == cudaSuccess) e = launch_wide_pack((*out)->down, down, E, H, F, false, s);
+    if (e == cudaSuccess && wtype == PP_F16) e = find_act_bound(*out, gate_up, nullptr, nullptr, 0, s);
     return moe_filled(out, e, s);
 }
 
@@ -1122,6 +1211,7 @@ extern "C" pp_status_t pp_moe_create_q4(pp_moe_t** out, int E, int H, int F, int
     (*out)->bf16_scales = scale_type == PP_BF16;
     cudaError_t e = launch_q4_pack((*out)->gate_up, (*out)->gate_up_sets, gate_up_codes, gate_up_scales, gate_up_zeros, E, 2 * F, H, group, true, s);
     if (e == cudaSuccess) e = launch_q4_pack((*out)->down, (*out)->down_sets, down_codes, down_scales, down_zeros, E, H, F, group, false, s);
+    if (e == cudaSuccess) e = find_act_bound(*out, gate_up_codes, gate_up_scales, gate_up_zeros, group, s);
     return moe_filled(out, e, s);
 }
 
@@ -1168,6 +1258,7 @@ extern "C" pp_status_t pp_moe_forward(pp_moe_t* L, const void* x, int64_t ldx, p
     a.H = L->H;
     a.top_k = L->top_k;
     a.renorm = L->renorm;
+    a.act_bound = L->act_bound;
     a.strips1 = L->strips1;
     a.strips2 = L->strips2;
     a.kb1 = L->kb1;

@@ -186,6 +186,46 @@ def test_moe_ties_go_to_the_lowest_index():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("weights,xt", [("bf16", "f32"), ("f16", "f32"), ("f16", "bf16"), ("q4", "f32"), ("q4", "bf16")])
+@pytest.mark.parametrize("T", [1, 16])
+def test_moe_tokens_of_any_size(weights, xt, T):
+    """Tokens from 1e-15 to 1e15 in one call: act goes from 1e-30 to 1e30, far out of binary16 on both sides.  One expert, so
+    that its weight is 1.  act enters the down products with an absolute error of at most 2^-59 |x|^2 |G row| |U row|."""
+    c = Case(14, 1, 1, 320, 72, weights, T)
+    u, d = c.u[0], c.d[0]
+    scales = torch.logspace(-15, 15, 16, device="cuda")
+    for i in range(0, 16, T):
+        x = (torch.randn(T, c.H, generator=_gen(i), device="cuda") * scales[i:i + T, None]).to(TYPES[xt])
+        y, x = pb.pp_moe_forward(c.layer, x, out_dtype=torch.float32).double(), x.double()
+        gu, mass = x @ u.T, 1e-5 * (x.abs() @ u.abs().T)
+        g, v, dg, dv = gu[:, :c.F], gu[:, c.F:], mass[:, :c.F], mass[:, c.F:]
+        silu = g * torch.sigmoid(g)
+        act = silu * v
+        d_act = 1.1 * dg * v.abs() + (silu.abs() + 1.1 * dg) * dv + act.abs() * 1.4e-5
+        norms = u.norm(dim=1)
+        floor = 2.0 ** -59 * (x * x).sum(1, keepdim=True) * norms[:c.F].max() * norms[c.F:].max()
+        err, bound = (y - act @ d.T).abs(), (d_act + floor) @ d.abs().T
+        assert bool((err <= bound).all()), float((err / bound).max())
+
+
+@pytest.mark.gpu
+def test_moe_act_bound_leaves_out_rows_that_are_not_finite():
+    """An infinite weight in one expert must not cost the others their bits."""
+    c = Case(15, 4, 1, 256, 64, "f16", 4)
+    g = _gen(15)
+    r = torch.randn(4, 256, generator=g, device="cuda") / 16
+    r[3] = 0.0
+    u, d = (c.u.clone().half(), c.d.half())
+    u[3, 5, 7], u[3, 64 + 9, 3] = float("inf"), float("nan")
+    x = torch.randn(4, 256, generator=g, device="cuda").half()
+    r[3] = -100 * x[0].float()                                               # never chosen by any token like the first
+    x = x[:1].expand(4, -1).contiguous()
+    c.r, c.u, c.d = r.half().double(), u.double(), d.double()
+    c.layer = pb.MoELayer(r.half(), u, d, inner=64, top_k=1, max_tokens=4)
+    c.check(x, torch.float32)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("weights", ["bf16", "q4"])
 def test_moe_not_finite_tokens_stay_alone(weights):
     c = Case(7, 8, 2, 256, 64, weights, 4)
