@@ -127,6 +127,23 @@ def test_moe_larger(weights):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("weights,E,k,H,F,T", [
+    ("bf16", 2, 1, 4096, 80, 1),         # 10 strips of 128 units: every strip on several CTAs
+    ("f16", 2, 2, 4096, 1000, 1),        # 250 strips: one and a half to a CTA
+    ("bf16", 4, 2, 2800, 600, 3),        # 88 units to a strip, just more than a join costs; several tokens
+    ("f16", 16, 4, 4100, 200, 16),       # two tiles of columns, a last unit of four columns
+    ("q4", 2, 1, 11008, 80, 1),          # 86 units of 128 columns
+    ("q4", 8, 2, 11000, 72, 5),
+    ("bf16", 2, 2, 4096, 14336, 1)])     # wide experts of an ordinary size: 3,584 strips, 32 over
+def test_moe_strips_of_gate_and_up_that_several_ctas_share(weights, E, k, H, F, T):
+    c = Case(E * H + F, E, k, H, F, weights, T)
+    x = torch.randn(T, H, generator=_gen(T), device="cuda").bfloat16()
+    y = c.check(x, torch.float32)
+    for _ in range(3):
+        assert torch.equal(y, pb.pp_moe_forward(c.layer, x, out_dtype=torch.float32))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("weights", ["bf16", "f16", "q4"])
 def test_moe_strides_and_alignment(weights):
     c = Case(5, 8, 2, 333, 80, weights, 4)
