@@ -674,6 +674,9 @@ def _load_torch():
         from . import _pp_torch
     except ImportError as e:
         raise ImportError("_pp_torch.so: build it with `python -m paper_1712_01084_b200.build`") from e
+    if _pp_torch.made_for != f"made for torch {torch.__version__}":
+        raise ImportError(f"_pp_torch.so was {_pp_torch.made_for}, this is {torch.__version__}: build it again with "
+                          "`python -m paper_1712_01084_b200.build`")
     _pp_torch.init(*(ctypes.cast(f, ctypes.c_void_p).value for f in (library.pp_rmsnorm_q8, library.pp_q4_forward, library.pp_moe_forward)))
     _TYPES.update({torch.float32: PP_F32, torch.float16: PP_F16, torch.bfloat16: PP_BF16, torch.int8: PP_I8,
                    torch.float8_e4m3fn: PP_E4M3})

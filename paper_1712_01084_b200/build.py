@@ -28,10 +28,21 @@ def needs_build() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def needs_build_torch() -> bool:
+    """Whether the extension module is missing, older than its sources or made for another PyTorch: its C++ interface is
+    that of one version, whose name the module holds."""
+    import torch
+    if not os.path.exists(TORCH_LIB):
+        return True
+    if os.path.getmtime(TORCH_LIB) < max(os.path.getmtime(TORCH_SRC), os.path.getmtime(os.path.join(ROOT, "include", "pp.h"))):
+        return True
+    with open(TORCH_LIB, "rb") as f:
+        return f"made for torch {torch.__version__}\0".encode() not in f.read()
+
+
 def build_torch(force: bool = False) -> str:
     """The extension module: plain C++ against the headers of the installed PyTorch."""
-    newest = max(os.path.getmtime(TORCH_SRC), os.path.getmtime(os.path.join(ROOT, "include", "pp.h")))
-    if not force and os.path.exists(TORCH_LIB) and os.path.getmtime(TORCH_LIB) >= newest:
+    if not force and not needs_build_torch():
         return TORCH_LIB
     import sysconfig
     import torch
@@ -41,7 +52,8 @@ def build_torch(force: bool = False) -> str:
                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
     lib = os.path.join(base, "lib")
     subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
-                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           f'-DPP_TORCH_VERSION="made for torch {torch.__version__}"'] +
                           [x for d in include for x in ("-isystem" if d.startswith(base) else "-I", d)] +
                           ["-o", TORCH_LIB, TORCH_SRC, "-L" + lib, "-Wl,-rpath," + lib, "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda",
                            "-lc10"])
@@ -49,7 +61,7 @@ def build_torch(force: bool = False) -> str:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    build_torch(force)
+    """The library alone, which needs nvcc and no PyTorch."""
     if not force and not needs_build():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
@@ -64,3 +76,4 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_torch(force="--force" in sys.argv))

@@ -277,4 +277,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pp_torch", "Decoder operators on 
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__pp_torch() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__pp_torch() {
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "made_for", PP_TORCH_VERSION) != 0) Py_CLEAR(m);
+    return m;
+}
