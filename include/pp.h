@@ -449,7 +449,8 @@ pp_status_t pp_noalloc_status(pp_status_t* status);
  * codes         [rows][cols]; scales float [rows][1 or ceil(cols / 128)]
  * hidden_out    h in dtype, ldh apart, or NULL; may be residual or x itself (same address and distance)
  * normed_out    n in dtype, [rows][cols], or NULL
- * rows >= 0 (0: nothing is done, the arrays may be NULL), 1 <= cols <= 32768.  No other pair of arrays may overlap.  Any alignment of rows works; rows that all
+ * rows >= 0 (0: nothing is done, the arrays may be NULL), 1 <= cols <= 32768.  No other pair of arrays may overlap (hidden_out
+ * across x or residual is refused).  Any alignment of rows works; rows that all
  * start on 16 bytes (and 8 for codes) are read and written in wider accesses.
  * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (types, group, cols), PP_ERR_CUDA. */
 pp_status_t pp_rmsnorm_q8(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight, pp_dtype_t dtype,
@@ -469,7 +470,8 @@ pp_status_t pp_rmsnorm_q8(const void* x, int64_t ldx, const void* residual, int6
  * x             device, [batch][N], rows ldx elements apart; PP_F32, PP_F16, PP_BF16, PP_I8 or PP_E4M3
  * x_scales      8-bit x only, else NULL: float [batch][x_group ? ceil(N / x_group) : 1], the values pp_rmsnorm_q8 writes
  * x_group       columns per scale of x: 0 = the row, or a multiple of 128
- * y             device, [batch][M] row-major, y_type PP_F32, PP_F16 or PP_BF16, rounded once from fp32 sums
+ * y             device, [batch][M] row-major, y_type PP_F32, PP_F16 or PP_BF16, rounded once from fp32 sums; no byte of it in x
+ *               or x_scales
  * Up to two vectors (eight of PP_I8) of up to some 120,000 columns: float inputs enter the products as fixed point, per 128 columns of a vector, with an
  * error of at most 2^-31 of the largest magnitude among those 128, and sums are exact over a group's columns (up to 128).
  * More vectors, or wider ones: f32 enters with 22 bits, bf16 and f16 with all of theirs.  8-bit inputs enter exactly.  Sums are fp32.

@@ -19,6 +19,25 @@ inline bool is_8bit(int t) { return t == PP_I8 || t == PP_E4M3; }
 inline int type_bytes(int t) { return t == PP_F32 ? 4 : is_16bit(t) ? 2 : 1; }
 inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// Whether rows of two matrices share bytes (w: bytes of a row, ld: bytes between rows).  Matrices that lie in one another's gaps
+// are told apart where both have one distance or one has one row or none between; others in each other's range count as apart.
+inline bool share_bytes(const void* p, int64_t w_p, int64_t ld_p, int64_t rows_p, const void* q, int64_t w_q, int64_t ld_q, int64_t rows_q) {
+    if (!p || !q || rows_p < 1 || rows_q < 1) return false;
+    if (rows_p == 1 || ld_p == w_p) w_p *= rows_p, ld_p = w_p, rows_p = 1;
+    if (rows_q == 1 || ld_q == w_q) w_q *= rows_q, ld_q = w_q, rows_q = 1;
+    const int64_t d = (int64_t)(reinterpret_cast<intptr_t>(q) - reinterpret_cast<intptr_t>(p));
+    if (d >= (rows_p - 1) * ld_p + w_p || -d >= (rows_q - 1) * ld_q + w_q) return false;
+    if (rows_p == 1 && rows_q == 1) return true;
+    if (rows_p == 1) return share_bytes(q, w_q, ld_q, rows_q, p, w_p, ld_p, rows_p);
+    if (rows_q == 1) {                                       // a row that starts before q's end: the last such one ends behind q's start
+        const int64_t last = (d + w_q - 1) / ld_p < rows_p - 1 ? (d + w_q - 1) / ld_p : rows_p - 1;
+        return last * ld_p + w_p > d;
+    }
+    if (ld_p != ld_q) return false;
+    const int64_t in = (d % ld_p + ld_p) % ld_p;             // where q's rows start between p's
+    return in < w_p || in + w_q > ld_p;
+}
+
 // A call's status.  An error of a launch is also kept by the runtime for whoever asks next: that is taken away with it, or the
 // next call that looks behind a launch of its own would report this one's.
 inline pp_status_t status_of(cudaError_t e) {

@@ -375,6 +375,11 @@ extern "C" pp_status_t pp_rmsnorm_q8(const void* x, int64_t ldx, const void* res
     if (!aligned_to(x, tb) || !aligned_to(residual, tb) || !aligned_to(hidden_out, tb) || !aligned_to(normed_out, tb) ||
         !aligned_to(weight, (size_t)type_bytes(weight_type)) || !aligned_to(scales, 4)) return PP_ERR_INVALID_ARG;
     if (rows == 0) return PP_OK;
+    const int64_t width = (int64_t)cols * (int64_t)tb;
+    const auto crosses_hidden = [&](const void* p, int64_t ld) {          // over it but not in its place
+        return share_bytes(p, width, ld * (int64_t)tb, rows, hidden_out, width, ldh * (int64_t)tb, rows) && !(p == hidden_out && (rows == 1 || ld == ldh));
+    };
+    if (crosses_hidden(x, ldx) || crosses_hidden(residual, ldr)) return PP_ERR_INVALID_ARG;
     NormArgs a{x, residual, weight, codes, hidden_out, normed_out, scales, ldx, ldr, ldh,
                cols, group ? (cols + 127) / 128 : 1, eps, 1.0f / (float)cols, weight_type == PP_F32, rows, 0};
     // eight elements to an access where every row of every array starts on one

@@ -543,13 +543,17 @@ extern "C" pp_status_t pp_q4_launch_info(const pp_q4_t* L, int32_t out[4]) {
 
 extern "C" pp_status_t pp_q4_forward(pp_q4_t* L, const void* x, int64_t ldx, pp_dtype_t x_type, const float* x_scales, int x_group, void* y,
                                      pp_dtype_t y_type, int batch, pp_act_t act, void* cuda_stream) {
-    if (!L || !x || !y || x == y || batch < 1 || (batch > 1 && ldx < L->N)) return PP_ERR_INVALID_ARG;
+    if (!L || !x || !y || batch < 1 || (batch > 1 && ldx < L->N)) return PP_ERR_INVALID_ARG;
     if (act != PP_ACT_IDENTITY && act != PP_ACT_RELU) return PP_ERR_INVALID_ARG;
     if ((!is_float(x_type) && !is_8bit(x_type)) || !is_float(y_type)) return PP_ERR_UNSUPPORTED;
     if (is_8bit(x_type) ? !x_scales : x_scales != nullptr) return PP_ERR_INVALID_ARG;
     if (x_group != 0 && (!is_8bit(x_type) || x_group < 0 || x_group % kQ4UnitCols != 0)) return PP_ERR_UNSUPPORTED;
     const int xb = type_bytes(x_type), yb = type_bytes(y_type);
     if (!aligned_to(x, xb) || !aligned_to(y, yb) || !aligned_to(x_scales, 4)) return PP_ERR_INVALID_ARG;
+    const int64_t y_bytes = (int64_t)batch * L->M * yb;
+    const int64_t scales_bytes = (int64_t)batch * (x_group ? (L->N + x_group - 1) / x_group : 1) * 4;
+    if (share_bytes(x, (int64_t)L->N * xb, ldx * xb, batch, y, y_bytes, y_bytes, 1) ||
+        share_bytes(x_scales, scales_bytes, scales_bytes, 1, y, y_bytes, y_bytes, 1)) return PP_ERR_INVALID_ARG;
     Q4Args a{};
     a.units = L->units;
     a.bias = L->bias;

@@ -475,6 +475,33 @@ def test_q4_in_a_graph():
 
 
 @pytest.mark.gpu
+def test_outputs_that_cross_inputs_are_refused():
+    """Other CTAs still read what one writes.  Matrices in each other's gaps, and hidden_out in the place of an input, pass."""
+    big = torch.randn(9, 1024, device="cuda")
+    w = torch.ones(256, device="cuda")
+    x = big[:8, :256]
+    for out in (big[1:, :256], big[:8, 128:384], big[:8, 1:257]):
+        for args in (dict(x=x, hidden_out=out), dict(x=big[:8, 512:768], residual=x, hidden_out=out)):
+            with pytest.raises(pb.PPError) as e:
+                pb.pp_rmsnorm_q8(weight=w, **args)
+            assert e.value.status == 1
+    for out in (big[:8, 256:512], big[1:, 768:], x):
+        pb.pp_rmsnorm_q8(x, w, hidden_out=out)
+    codes, s, _, m = _q4_data(60, 96, 256, 64, False)
+    L = pb.Q4Layer(96, 256, 64, codes, s)
+    flat = torch.randn(8 * 1024, device="cuda")
+    x = flat.view(8, 1024)[:, :256]
+    for start in (0, 255, 1024 - 96 * 8 + 1, 1000, 7 * 1024 + 255):
+        with pytest.raises(pb.PPError) as e:
+            pb.pp_q4_forward(L, x, out=flat[start:start + 96 * 8].view(8, 96))
+        assert e.value.status == 1
+    keep = x.clone()
+    y = pb.pp_q4_forward(L, x, out=flat[256:256 + 96 * 8].view(8, 96))      # just fits between two rows
+    assert torch.equal(x, keep)
+    _check_y(y, m, keep.double())
+
+
+@pytest.mark.gpu
 def test_q4_refusals():
     codes, s, z, _ = _q4_data(16, 64, 256, 64, True)
     for bad in (dict(group=16), dict(group=96), dict(group=-64)):
