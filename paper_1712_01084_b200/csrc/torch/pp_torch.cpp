@@ -105,7 +105,7 @@ struct Enqueue {
 at::Tensor output(PyObject* out, PyObject* out_dtype, at::ScalarType standard, int64_t rows, int64_t cols, int device) {
     if (out == Py_None) return fresh({rows, cols}, dtype(out_dtype, standard), device);
     const at::Tensor& y = tensor(out, "out");
-    if (!y.is_cuda() || y.get_device() != device || !y.is_contiguous() || y.numel() != rows * cols ||
+    if (!y.is_cuda() || y.get_device() != device || !y.is_contiguous() || y.numel() != rows * cols || (y.dim() == 2 && rows > 1 && y.size(0) != rows) ||
         (out_dtype != Py_None && y.scalar_type() != dtype(out_dtype, standard)))
         raise(PyExc_ValueError, "out must be a contiguous CUDA tensor [%lld][%lld] of out_dtype", (long long)rows, (long long)cols);
     return y;
@@ -212,6 +212,8 @@ PyObject* q4_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
             if (!s.is_cuda() || s.get_device() != device || !s.is_contiguous() || s.scalar_type() != at::kFloat)
                 raise(PyExc_ValueError, "x_scales must be a contiguous float32 CUDA tensor on device %d", device);
             x_group = s.numel() == rx.rows ? 0 : 128;
+            if (x_group && rx.rows > 1 && s.dim() == 2 && s.size(0) != rx.rows)
+                raise(PyExc_ValueError, "x_scales must be [%d][%lld]", rx.rows, (long long)groups);
             scales = static_cast<const float*>(s.const_data_ptr());
         }
         const Enqueue on(a[9], device);

@@ -502,6 +502,24 @@ def test_outputs_that_cross_inputs_are_refused():
 
 
 @pytest.mark.gpu
+def test_matrices_the_wrong_way_round_are_refused():
+    """They hold as many elements as the right ones."""
+    codes, s, _, _ = _q4_data(60, 96, 256, 64, False)
+    L = pb.Q4Layer(96, 256, 64, codes, s)
+    q = torch.zeros(4, 256, device="cuda", dtype=torch.int8)
+    with pytest.raises(ValueError, match="x_scales"):
+        pb.pp_q4_forward(L, q, x_scales=torch.ones(2, 4, device="cuda"))
+    for scales in (torch.ones(4, 2, device="cuda"), torch.ones(4, 1, device="cuda"), torch.ones(4, device="cuda")):
+        assert pb.pp_q4_forward(L, q, x_scales=scales).shape == (4, 96)
+    pb.pp_q4_forward(L, q[0], x_scales=torch.ones(2, device="cuda"))
+    x = torch.zeros(4, 256, device="cuda")
+    with pytest.raises(ValueError, match="out"):
+        pb.pp_q4_forward(L, x, out=torch.empty(96, 4, device="cuda"))
+    for shape in ((4, 96), (4 * 96,)):
+        assert pb.pp_q4_forward(L, x, out=torch.empty(shape, device="cuda")).shape == shape
+
+
+@pytest.mark.gpu
 def test_q4_refusals():
     codes, s, z, _ = _q4_data(16, 64, 256, 64, True)
     for bad in (dict(group=16), dict(group=96), dict(group=-64)):
