@@ -45,7 +45,7 @@ struct pp_moe {
     bool asym, bf16_scales;
     int act_bound;
     int strips1, strips2, kb1, kb2;
-    int ctas;                 // that the device holds at once
+    int device, ctas;         // ctas: that the device holds at once
     unsigned char *gate_up, *down, *gate_up_sets, *down_sets;
     float *router, *logits, *xscale;
     uint16_t *xcols, *acols;
@@ -1148,6 +1148,7 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
         if (st == PP_OK && (cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) != cudaSuccess ||
                             cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kThreads, kMaxSmem) != cudaSuccess || each < 1)) st = PP_ERR_CUDA;
     }
+    L->device = device;
     L->ctas = sms;
     if (st == PP_OK &&
         (!alloc(&L->gate_up, units1 * 1024) || !alloc(&L->down, units2 * 1024) ||
@@ -1217,6 +1218,17 @@ extern "C" pp_status_t pp_moe_create_q4(pp_moe_t** out, int E, int H, int F, int
 
 extern "C" pp_status_t pp_moe_status(pp_moe_t* L, pp_status_t* status) {
     if (!L || !status) return PP_ERR_INVALID_ARG;
+    // the layer's device, whichever is the caller's: the counters are cleared only when none of its kernels is on the way
+    struct On {
+        int before = -1;
+        explicit On(int device) {
+            int now = 0;
+            if (cudaGetDevice(&now) == cudaSuccess && now != device && cudaSetDevice(device) == cudaSuccess) before = now;
+        }
+        ~On() {
+            if (before >= 0) cudaSetDevice(before);
+        }
+    } on(L->device);
     int raised = 0;
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&raised, L->sync + 3, 4, cudaMemcpyDeviceToHost) != cudaSuccess) return PP_ERR_CUDA;
     // a wait that gave up leaves divided strips with some of their CTAs counted and nobody to take the count back: the whole of
