@@ -46,6 +46,17 @@ inline pp_status_t status_of(cudaError_t e) {
     return PP_ERR_CUDA;
 }
 
+// SMs of the current device, asked for once per device (148 on a whole B200).
+inline int sm_count() {
+    static int known[64] = {};
+    int device = 0, n = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return 148;
+    if (device < 64 && known[device]) return known[device];
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) n = 148;
+    if (device < 64) known[device] = n;
+    return n;
+}
+
 // Launch that lets the kernel's prologue overlap the tail of the previous kernel in the stream: the kernel itself
 // waits (griddepcontrol.wait) before it reads what that kernel may have written and before it writes anything.
 template <typename... P, typename... A>

@@ -1035,7 +1035,7 @@ cudaError_t find_act_bound(pp_moe* L, const void* w, const void* scales, const v
     cudaError_t e = cudaMalloc(&most, sizeof(norms));
     if (e == cudaSuccess) e = cudaMemsetAsync(most, 0, sizeof(norms), stream);
     if (e == cudaSuccess) {
-        row_norms_kernel<<<(unsigned)std::min<int64_t>((rows + 7) / 8, 148 * 16), 256, 0, stream>>>(
+        row_norms_kernel<<<(unsigned)std::min<int64_t>((rows + 7) / 8, sm_count() * 16), 256, 0, stream>>>(
             most, w, static_cast<const uint16_t*>(scales), static_cast<const uint8_t*>(zeros), L->bf16_scales, rows, L->F, L->H, group);
         e = cudaGetLastError();
     }
@@ -1050,7 +1050,7 @@ cudaError_t find_act_bound(pp_moe* L, const void* w, const void* scales, const v
 cudaError_t launch_wide_pack(void* dst, const void* w, int count, int rows, int cols, bool paired, cudaStream_t stream) {
     const int strips = strips_of(rows, paired), blocks = (cols + 31) / 32;
     const int64_t n = (int64_t)count * strips * blocks;
-    const unsigned grid = (unsigned)std::min<int64_t>((n * 64 + 255) / 256, 148 * 32);
+    const unsigned grid = (unsigned)std::min<int64_t>((n * 64 + 255) / 256, sm_count() * 32);
     wide_pack_kernel<<<grid, 256, 0, stream>>>(static_cast<unsigned char*>(dst), static_cast<const uint16_t*>(w), rows, cols, strips, blocks, paired, n);
     return cudaGetLastError();
 }
@@ -1162,7 +1162,7 @@ static pp_status_t moe_new(pp_moe_t** out, int E, int H, int F, int top_k, int r
     if (st == PP_OK) {
         // act's columns past F are never written and stay zero
         if (cudaMemsetAsync(L->acols, 0, abytes, s) != cudaSuccess || cudaMemsetAsync(L->sync, 0, sync_bytes(L->ctas), s) != cudaSuccess) st = PP_ERR_CUDA;
-        router_pack_kernel<<<148, 256, 0, s>>>(L->router, router, router_type, E, H, (int)ld);
+        router_pack_kernel<<<sm_count(), 256, 0, s>>>(L->router, router, router_type, E, H, (int)ld);
         if (cudaGetLastError() != cudaSuccess) st = PP_ERR_CUDA;
     }
     if (st != PP_OK) {

@@ -342,8 +342,10 @@ cudaError_t launch_type(NormArgs& a, bool vec, bool grouped, bool e4m3, cudaStre
     const int staying = ((a.cols + 8 * kRowsChunks - 1) / (8 * kRowsChunks) + 31) / 32 * 32;
     a.stage_bytes = 2 * (int)(((size_t)a.cols * sizeof(T) + 15) / 16 * 16);
     const int each = std::min({680 / staying, (227 * 1024) / (kStages * a.stage_bytes + 2048), 16});
-    if (vec && staying <= kRowsThreads && each >= 1 && a.rows >= 4 * 148 * each)
-        return launch_rows<T>(a, 148 * each, staying, grouped, e4m3, stream);
+    if (vec && staying <= kRowsThreads && each >= 1) {
+        const int grid = sm_count() * each;
+        if (a.rows >= 4 * grid) return launch_rows<T>(a, grid, staying, grouped, e4m3, stream);
+    }
     // as few columns per thread as 1024 threads allow: the row's latency is one trip to memory either way
     int ch = 1;
     while (ch < 4 && a.cols > 1024 * 8 * ch) ch *= 2;

@@ -460,7 +460,7 @@ cudaError_t launch_q4_pack(void* dst, void* dst_sets, const void* codes, const v
     const int strips = strips_of(rows, paired), blocks = (cols + kQ4UnitCols - 1) / kQ4UnitCols, sets = q4_sets(group);
     const int groups = group ? (cols + group - 1) / group : 1;
     const int64_t n = (int64_t)count * strips * blocks;
-    const unsigned grid = (unsigned)std::min<int64_t>((n * 64 + 255) / 256, 148 * 32);
+    const unsigned grid = (unsigned)std::min<int64_t>((n * 64 + 255) / 256, sm_count() * 32);
     q4_pack_kernel<<<grid, 256, 0, stream>>>(static_cast<unsigned char*>(dst), static_cast<unsigned char*>(dst_sets), static_cast<const uint8_t*>(codes),
                                              static_cast<const uint16_t*>(scales), static_cast<const uint8_t*>(zeros), rows, cols, group, groups,
                                              strips, blocks, sets, q4_set_bytes(sets, zeros != nullptr), paired, n);

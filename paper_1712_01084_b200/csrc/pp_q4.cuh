@@ -172,8 +172,7 @@ __device__ __forceinline__ void f16_scale(float most, float& up, float& down) {
 // i / n for 0 <= i < 2^20 by the reciprocal of n: an integer division takes as long as a trip to L2.
 struct Divider {
     float r;
-    int n;
-    __device__ __forceinline__ explicit Divider(int d) : r(1.0f / (float)d), n(d) {}
+    __device__ __forceinline__ explicit Divider(int d) : r(1.0f / (float)d) {}
     __device__ __forceinline__ int div(int i) const { return (int)(((float)i + 0.5f) * r); }
 };
 
