@@ -472,12 +472,14 @@ pp_status_t pp_rmsnorm_q8(const void* x, int64_t ldx, const void* residual, int6
  * x_group       columns per scale of x: 0 = the row, or a multiple of 128
  * y             device, [batch][M] row-major, y_type PP_F32, PP_F16 or PP_BF16, rounded once from fp32 sums; no byte of it in x
  *               or x_scales
- * Up to two vectors (eight of PP_I8) of up to some 120,000 columns: float inputs enter the products as fixed point, per 128 columns of a vector, with an
- * error of at most 2^-31 of the largest magnitude among those 128, and sums are exact over a group's columns (up to 128).
- * More vectors, or wider ones: f32 enters with 22 bits, bf16 and f16 with all of theirs.  8-bit inputs enter exactly.  Sums are fp32.
- * Weights are read once for up to 16 vectors; larger batches repeat the pass.  Any alignment
- * of x works.  A vector with an infinity or a NaN gives outputs that are not finite, other vectors are not touched by it.  Only enqueues; calls on one handle may overlap on several streams (a handle
- * is never written).  Results do not depend on scheduling.
+ * Up to two vectors (eight of PP_I8) of up to some 120,000 columns: float inputs enter the products as fixed point, per 128
+ * columns of a vector, with an error of at most 2^-31 of the largest magnitude among those 128, and sums are exact over a
+ * group's columns (up to 128).  More vectors, or wider ones: f32 enters with 22 bits (elements below 2^-16 of the largest
+ * among their 128 with an absolute 2^-38 of it), f16 with all of its bits, bf16 with all of them down to 2^-30 of that largest.
+ * 8-bit inputs enter exactly.  Sums are fp32.  Weights are read once for up to 16 vectors; larger batches repeat the pass.
+ * Any alignment of x works.  A vector with an infinity or a NaN gives outputs that are not finite, other vectors are not
+ * touched by it.  Only enqueues; calls on one handle may overlap on several streams (a handle is never written).  Results do
+ * not depend on scheduling.
  * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED, PP_ERR_ALLOC, PP_ERR_CUDA.
  * pp_q4_launch_info: for clusters of 1, 2, 4 and 8 CTAs, how many the device holds at once (for reports). */
 typedef struct pp_q4 pp_q4_t;

@@ -28,8 +28,9 @@
 // act times the token's power of two that brings this bound to 2^26, so it cannot overflow, and 24 bits hold down to 2^-35 of
 // the bound (powers of two are up to 4 above it); with random rows the bound is about H times a typical element.  y takes the power of two back.
 //
-// us a call: 64 experts of 4096 x 2048, 8 a token, bf16, 16 tokens 442 (6.4 TB/s); 64 of 2048 x 1024, 4 tokens, 4 bits 33.0
-// (of 13 for the bytes: bound by instructions); 8 experts of 1024, 2 a token, one token 13.0 (bound by the steps' latency).
+// us in a graph and called one after another: 64 experts of 4096 x 2048, 8 a token, bf16, 16 tokens 453 (6.3 TB/s) and 487; 64 of
+// 2048 x 1024, 4 tokens, 4 bits 33.0 and 35.5 (of 13 for the bytes: bound by instructions); 8 experts of 1024, 2 a token, one
+// token 13.2 and 14.3 (bound by the steps' latency).
 #include "pp_q4.cuh"
 
 #include <algorithm>
@@ -1066,8 +1067,9 @@ template <int TILES> Kernel pick_kernel(const pp_moe* L) {
 // Tokens of an entry: what two tiles of columns hold, or what one does, two, where few experts have more than that (their
 // weights are then read again, from L2).  16-bit experts, bound by HBM, take two while they have less than a token each on
 // average (64 experts of 2048 x 1024, 8 a token: 4 tokens 61.7 us with two, 62.5 with five; 8 tokens 101.8 and 98.4); 4-bit
-// experts, bound by the products, up to two tokens each (4 tokens 33.8 and 41.5 us, 16 tokens 77.7 and 83.6; 8 experts of
-// 4096 x 2048, 4 tokens each, 69.3 and 57.9).
+// experts, bound by the products, up to two tokens each (4 tokens 33.1 us with two, 38.7 with four, all that two tiles of four
+// columns a token hold; 16 tokens, two each, 77.0 and 83.4; 8 experts of 4096 x 2048, three each 53.9 and 52.3, four each 67.1
+// and 59.8).
 int cap_of(int tokens, int top_k, int E, bool q4) {
     return (q4 ? tokens * top_k <= 2 * E : tokens * top_k < E) ? 8 / (q4 ? kByteCols : kActCols) : q4 ? kMaxCols / kByteCols : kMaxCap;
 }

@@ -12,8 +12,8 @@
 // (rmsnorm_q8_rows_kernel), each with a ring of rows on their way into shared memory by 16-byte asynchronous copies while
 // it works on the one before; a CTA per row stops the flow of bytes at every barrier.
 //
-// 8192 x 8192 bf16 with a residual: 80 us, 5.9 TB/s.  One row of 4096: 1.9 us.  2047 x 4095, whose rows start on any
-// two bytes: 18.6 us, bound by 2-byte accesses.
+// 8192 x 8192 bf16 with a residual: 76 us in a graph, 6.1 TB/s (80 us called one after another).  One row of 4096: 2.0 us.
+// 33 x 9216 to integers: 3.7 us.  2047 x 4095, whose rows start on any two bytes: 18.7 us, bound by 2-byte accesses.
 #include <algorithm>
 
 #include "pp_decode.cuh"
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_q8_kernel(const NormArgs a) {
 
 // Rows in the ring of a CTA, and the columns of a thread: 32, so that what a row costs each thread beside its elements (two
 // reductions, one barrier) is spread over many (8192 x 8192 bf16: 8 columns a thread 99 us, 16 86 us, 32 80 us; a CTA per row
-// 92 us).
+// 92 us.  With rows counted without a sign 32 take 76, with 64-bit numbers 83).
 constexpr int kStages = 3, kRowsChunks = 4, kRowsThreads = 320;
 
 // Rows that start on 16 bytes (VEC): a thread reads only what it has copied itself.

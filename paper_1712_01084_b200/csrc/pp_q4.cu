@@ -22,8 +22,9 @@
 // holds what the first one's 11 bits leave over); bf16 and f32 blocks of 128 columns are brought to [2^13, 2^14) by a power
 // of two first.  Eight vectors would be 32 columns of bytes.
 //
-// 8192 x 8192, us a call: one vector 9.3 to 9.7 (3.6 TB/s), four of bf16 11.5, eight 13.4, sixteen 17.0, sixteen of f32 23.5
-// (there a unit costs 256 cycles of matrix instructions and 300 of shared memory); 4096 x 4096, one vector, 4.9.
+// 8192 x 8192, us in a graph: one vector 9.8 (3.5 TB/s), two 10.8, four of bf16 11.5, eight 13.4, sixteen 16.9, sixteen of f32
+// 23.5 (there a unit costs 256 cycles of matrix instructions and 300 of shared memory); int8 9.2, eight vectors 13.3; e4m3 9.5,
+// 13.4; every 16 vectors more the same again.  4096 x 4096, one vector, 4.7.
 #include "pp_q4.cuh"
 
 #include <algorithm>
@@ -44,8 +45,8 @@ constexpr int kWarps = 16, kThreads = kWarps * 32, kMaxStrips = 64, kMaxTokens =
 constexpr int kParkLd = 20;           // floats between parked columns of 16 rows: a warp's 32 values hit 32 banks
 // Units each warp keeps in flight: 4 (70 KB an SM) keep HBM busy; 7 where x is small, so that more of the next call's weights
 // are on their way during this one's end; with 32 columns there is room for 3.  (7 also leave room for one CTA to an SM
-// only.  With two, the next call's CTAs start beside this one's; 8192 x 8192 then takes 8.7 us a call, but 12 us whenever
-// the CTAs of a call land on one SM twice, which lasts until the stream runs dry.  One: 9.3 us, always.)
+// only.  With two, the next call's CTAs start beside this one's; 8192 x 8192 then took 8.7 us a call, but 12 us whenever
+// the CTAs of a call land on one SM twice, which lasts until the stream runs dry.  One took 9.3 us, always.)
 __host__ __device__ constexpr int depth_of(int nt) { return nt == 4 ? 3 : nt == 1 ? 7 : 4; }
 constexpr int kShallow = 4;           // of binary16 products with one tile, where x leaves no room for 7
 // Columns of the product a vector takes.
