@@ -55,7 +55,7 @@ typedef enum {
 } pp_status_t;
 
 /* PP_F32 and PP_F16 are the element types of pruned layers; the others are inputs, outputs and weights of the decoder
- * operators (pp_rmsnorm_q8, pp_q4_*, pp_moe_*), which say what they take.  PP_E4M3: 8-bit float, 4 exponent and 3
+ * operators (pp_rmsnorm_q8, pp_q4_*, pp_moe_*, pp_kv_append, pp_paged_attention), which say what they take.  PP_E4M3: 8-bit float, 4 exponent and 3
  * mantissa bits, largest value 448, no infinities. */
 typedef enum { PP_F32 = 0, PP_F16 = 1, PP_BF16 = 2, PP_I8 = 3, PP_E4M3 = 4 } pp_dtype_t;
 typedef enum { PP_ACT_IDENTITY = 0, PP_ACT_RELU = 1 } pp_act_t;
@@ -529,6 +529,86 @@ pp_status_t pp_moe_destroy(pp_moe_t* layer);
 pp_status_t pp_moe_forward(pp_moe_t* layer, const void* x, int64_t ldx, pp_dtype_t x_type, void* y, pp_dtype_t y_type, int tokens,
                            int32_t* ids_out, float* gates_out, void* cuda_stream);
 pp_status_t pp_moe_status(pp_moe_t* layer, pp_status_t* status);
+
+/* ------------------------------------------------------------------------- *
+ * Paged key-value cache: the attention half of a decoding step.  Keys and values lie in pages of page_size tokens; a request's
+ * table row lists its pages, in the order of its tokens.  A step is pp_paged_plan (pages and slots of the new tokens),
+ * pp_kv_append (their keys and values into the cache) and pp_paged_attention (one new token of each request over its cache).
+ * All lengths, tables and slots stay on the device.  Nothing is kept between calls: calls on different streams may overlap,
+ * as long as none writes what another reads.  Inference only.
+ *
+ * A cache as the caller describes it (host struct, device pointers).  Head h of the token at place i of page p starts at
+ * k + p k_page + i k_token + h k_head, in elements; its head_dim values lie side by side.  So pages may be kept token by token or
+ * head by head, keys and values apart or interleaved, in one allocation or two.  No two rows may share bytes.
+ * dtype         PP_F32, PP_F16, PP_BF16; or PP_I8, PP_E4M3 with k_scales and v_scales, float [pages][page_size][kv_heads]: a
+ *               value is its code times the scale of its token and head.  Otherwise the scales are NULL
+ * head_dim      1..256; pages * page_size <= 2^40; page_size <= 2^20 */
+typedef struct pp_paged_cache {
+    void *k, *v;
+    float *k_scales, *v_scales;
+    int64_t k_page, k_token, k_head, v_page, v_token, v_head;
+    int pages, page_size, kv_heads, head_dim;
+    pp_dtype_t dtype;
+} pp_paged_cache_t;
+
+/* Pages and slots of a step.  Request r holds lengths[r] tokens and gets added[r] more (0: none; negative values count as 0, and
+ * lengths count as at most width * page_size, the capacity).  Pages that its new length needs are taken from free_pages, in the
+ * order of requests, from position *taken on, and entered in its table row; the row's other entries stay as they are.
+ * table         [requests][width], rows ld_table apart
+ * free_pages    [n_free]: pages to give out; those before *taken are in use.  Past its end an entry becomes -1
+ * taken_out     *taken + pages needed: more than n_free when there were not enough
+ * starts        [requests + 1]: first row of each request, then the number of rows in all; at most `rows`
+ * slots         [rows]: page * page_size + place of each new token, request after request; -1 without a page, past the
+ *               capacity and for rows behind the last token
+ * positions     [rows]: position of each new token in its sequence; 0 for rows behind the last token
+ * lengths_out   [requests]: min(lengths + added, capacity); may be lengths itself, as taken_out may be taken.  No other array
+ *               that is written may overlap another
+ * requests 0..8192, width >= 1, width * page_size < 2^31, rows >= 0.
+ * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (requests, capacity), PP_ERR_CUDA. */
+pp_status_t pp_paged_plan(const int32_t* lengths, const int32_t* added, int32_t* table, int64_t ld_table, int width,
+                          const int32_t* free_pages, int n_free, const int32_t* taken, int requests, int page_size, int rows,
+                          int64_t* slots, int32_t* positions, int32_t* starts, int32_t* lengths_out, int32_t* taken_out,
+                          void* cuda_stream);
+
+/* New keys and values into the cache, and rotary embedding.  Row t of k and v goes to slot slots[t] (page slot / page_size); a slot
+ * outside the cache, -1 for one, is left out.  With inv_freq the first 2 * pairs dimensions of each head of q and k are turned:
+ *     (x, y) -> (x cos a - y sin a, x sin a + y cos a),   a = positions[t] * inv_freq[i]   (the product in 64 bits)
+ * for the pairs (i, i + pairs), or (2i, 2i + 1) where interleaved is not 0.  Values are floats until they are rounded once: to
+ * dtype, or to 8 bits with the scale max|row| / Q of their token and head (Q = 127 or 448, code = round(value / scale), ties
+ * to even; a row with a NaN or an infinity has a NaN scale and unspecified codes).
+ * q, k, v       [tokens][heads or kv_heads][head_dim] of dtype (PP_F32, PP_F16, PP_BF16: the cache's type, or any with an 8-bit
+ *               cache), strides in elements; q NULL (heads 0): only the cache is written
+ * q_out         like q; may be q itself (same address and strides), else no byte of it in q, k or v
+ * slots         int64 [tokens], no slot twice; positions int32 [tokens] and inv_freq float [pairs], or both NULL with pairs 0
+ * pairs <= head_dim / 2; tokens >= 0.  Any alignment works; rows on 16 bytes (8 for 8-bit caches) are accessed more widely.
+ * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (types, head_dim), PP_ERR_CUDA. */
+pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q, int64_t q_token, int64_t q_head, int heads, void* q_out,
+                         int64_t o_token, int64_t o_head, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                         int64_t v_token, int64_t v_head, pp_dtype_t dtype, int tokens, const int64_t* slots,
+                         const int32_t* positions, const float* inv_freq, int pairs, int interleaved, void* cuda_stream);
+
+/* Attention of one new token of each request over the paged cache:
+ *     out[r][h] = sum_j p_j v[j][h / G],   p = softmax_j( scale * q[r][h] . k[j][h / G] ),   G = heads / kv_heads
+ * over the positions max(0, l - window) <= j < l of request r, l = min(lengths[r], width * page_size), all of them where window
+ * is 0.  The new token's own key and value are in the cache already (l counts it).  Positions whose table entry is no page of
+ * the cache (-1) are left out.  A row without positions gives 0 (lse -inf); so does one whose scores are all -inf.  What the
+ * cache holds elsewhere, NaN or not, is never used.
+ * q             [batch][heads][head_dim], strides in elements; q_type is the cache's type, or any float with an 8-bit cache
+ * table         [batch][width], rows ld_table apart; entries behind a request's length are not used
+ * out           [batch][heads][head_dim] of q_type, contiguous; no byte of it in q
+ * lse           float [batch][heads]: log of the sum of exp of the scores, or NULL
+ * workspace     pp_paged_attention_workspace bytes (0: NULL), 16-byte aligned, for this call alone while it runs; need not be
+ *               initialised.  Long sequences are divided over the GPU, and their parts joined through it
+ * Products are those of the 16-bit tensor-core instructions (exact products; float for PP_F32 caches), scores, softmax and sums
+ * are floats; p enters the second product as two 16-bit numbers (16 bits in all for PP_BF16, 22 otherwise).  Results do not
+ * depend on scheduling.  batch >= 0; heads a multiple of kv_heads; width * page_size < 2^31; window >= 0; scale finite.
+ * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (types, head_dim, capacity), PP_ERR_CUDA. */
+pp_status_t pp_paged_attention_workspace(const pp_paged_cache_t* cache, pp_dtype_t q_type, int batch, int heads, int width,
+                                         int window, int64_t* bytes);
+pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const void* q, int64_t q_row, int64_t q_head, pp_dtype_t q_type,
+                               const int32_t* table, int64_t ld_table, int width, const int32_t* lengths, int batch, int heads,
+                               float scale, int window, void* out, float* lse, void* workspace, int64_t workspace_bytes,
+                               void* cuda_stream);
 
 /* Self-check of host-side bookkeeping that needs no GPU (the table that remembers, per device, which kernels
  * already have their shared-memory opt-in): PP_OK, or PP_ERR_INVALID_ARG when a check fails.  One process may

@@ -100,6 +100,10 @@ def lib() -> ctypes.CDLL:
         "pp_moe_status": (ci, [vp, ctypes.POINTER(ci)]),
         "pp_moe_forward": (ci, [vp, vp, c64, ci, vp, ci, ci, vp, vp, vp]),
         "pp_q4_forward": (ci, [vp, vp, c64, ci, vp, ci, vp, ci, ci, ci, vp]),
+        "pp_paged_plan": (ci, [vp, vp, vp, c64, ci, vp, ci, vp, ci, ci, ci, vp, vp, vp, vp, vp, vp]),
+        "pp_kv_append": (ci, [vp, vp, c64, c64, ci, vp, c64, c64, vp, c64, c64, vp, c64, c64, ci, ci, vp, vp, vp, ci, ci, vp]),
+        "pp_paged_attention_workspace": (ci, [vp, ci, ci, ci, ci, ci, i64p]),
+        "pp_paged_attention": (ci, [vp, vp, c64, c64, ci, vp, c64, ci, vp, ci, ci, ctypes.c_float, ci, vp, vp, vp, c64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -677,7 +681,9 @@ def _load_torch():
     if _pp_torch.made_for != f"made for torch {torch.__version__}":
         raise ImportError(f"_pp_torch.so was {_pp_torch.made_for}, this is {torch.__version__}: build it again with "
                           "`python -m paper_1712_01084_b200.build`")
-    _pp_torch.init(*(ctypes.cast(f, ctypes.c_void_p).value for f in (library.pp_rmsnorm_q8, library.pp_q4_forward, library.pp_moe_forward)))
+    _pp_torch.init(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        library.pp_rmsnorm_q8, library.pp_q4_forward, library.pp_moe_forward, library.pp_paged_plan, library.pp_kv_append,
+        library.pp_paged_attention_workspace, library.pp_paged_attention)))
     _TYPES.update({torch.float32: PP_F32, torch.float16: PP_F16, torch.bfloat16: PP_BF16, torch.int8: PP_I8,
                    torch.float8_e4m3fn: PP_E4M3})
     _fast, _torch = _pp_torch, torch
@@ -865,4 +871,119 @@ def pp_moe_forward(layer: MoELayer, x, out_dtype=None, out=None, routing: bool =
                           None if stream is None else stream.cuda_stream)
     if r.__class__ is int:
         raise PPError(r, "pp_moe_forward")
+    return r
+
+
+# ------------------------------------------------------- paged key-value cache
+class _PagedCacheC(ctypes.Structure):
+    """pp_paged_cache_t."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scales", "v_scales")] + \
+               [(n, ctypes.c_int64) for n in ("k_page", "k_token", "k_head", "v_page", "v_token", "v_head")] + \
+               [(n, ctypes.c_int) for n in ("pages", "page_size", "kv_heads", "head_dim", "dtype")]
+
+
+class PagedCache:
+    """A paged key-value cache in the caller's tensors (pp_paged_cache_t).
+
+    k, v: CUDA [pages][page_size][kv_heads][head_dim], float32, float16, bfloat16, int8 or float8_e4m3fn, the last axis
+    contiguous; views of other orders are welcome (pages kept head by head: ``k.transpose(1, 2)``; keys and values in one
+    tensor: ``kv[:, 0]`` and ``kv[:, 1]``).  8-bit caches have k_scales and v_scales, contiguous float32
+    [pages][page_size][kv_heads].  The tensors stay the caller's; PagedCache.empty makes new ones."""
+
+    def __init__(self, k, v, k_scales=None, v_scales=None):
+        torch = _torch or _load_torch()
+        device = k.get_device() if k.is_cuda else -1
+        dtype = _type_of(k.dtype, "k")
+        if k.dim() != 4 or k.shape != v.shape or v.dtype != k.dtype or 0 in k.shape:
+            raise ValueError("k and v must be [pages][page_size][kv_heads][head_dim], of one shape and type")
+        for t, name in ((k, "k"), (v, "v")):
+            if not t.is_cuda or t.get_device() != device or (t.shape[3] > 1 and t.stride(3) != 1):
+                raise ValueError(f"{name} must be a CUDA tensor on device {device} with a contiguous last axis")
+        pages, page_size, kv_heads, head_dim = k.shape
+        scaled = dtype in (PP_I8, PP_E4M3)
+        if (k_scales is not None) != scaled or (v_scales is not None) != scaled:
+            raise ValueError("8-bit caches, and only they, have k_scales and v_scales")
+        if scaled:
+            _plain(k_scales, k.shape[:3], "k_scales", device, (torch.float32,))
+            _plain(v_scales, k.shape[:3], "v_scales", device, (torch.float32,))
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self._c = _PagedCacheC(k.data_ptr(), v.data_ptr(), ptr(k_scales), ptr(v_scales), *k.stride()[:3], *v.stride()[:3],
+                               pages, page_size, kv_heads, head_dim, dtype)
+        self._at = ctypes.addressof(self._c)
+        _check(lib().pp_paged_attention_workspace(self._at, PP_F32 if scaled else dtype, 0, kv_heads, 1, 0, ctypes.byref(ctypes.c_int64())),
+               "PagedCache")
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales    # keep the tensors alive
+        self.pages, self.page_size, self.kv_heads, self.head_dim, self.device = pages, page_size, kv_heads, head_dim, device
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=None, device=None) -> "PagedCache":
+        """A cache in new tensors, token by token; bfloat16 unless dtype says otherwise."""
+        torch = _torch or _load_torch()
+        dtype = torch.bfloat16 if dtype is None else dtype
+        make = lambda *shape, dtype: torch.empty(shape, dtype=dtype, device="cuda" if device is None else device)  # noqa: E731
+        k, v = (make(pages, page_size, kv_heads, head_dim, dtype=dtype) for _ in range(2))
+        scales = [make(pages, page_size, kv_heads, dtype=torch.float32) for _ in range(2)] if _type_of(dtype) in (PP_I8, PP_E4M3) else (None, None)
+        return cls(k, v, *scales)
+
+
+class PagedPlan:
+    """What pp_paged_plan writes for a step, in tensors that calls may use again: slots int64 [rows], positions int32 [rows],
+    starts int32 [requests + 1], lengths int32 [requests], taken int32 [1]."""
+
+    def __init__(self, requests: int, rows: int, device=None):
+        torch = _torch or _load_torch()
+        make = lambda n, dtype: torch.empty(n, dtype=dtype, device="cuda" if device is None else device)  # noqa: E731
+        self.slots = make(rows, torch.int64)
+        self.positions, self.starts, self.lengths, self.taken = (make(n, torch.int32) for n in (rows, requests + 1, requests, 1))
+
+
+def pp_paged_plan(lengths, added, table, free_pages, taken, page_size: int, rows: Optional[int] = None, out: Optional[PagedPlan] = None,
+                  stream=None) -> PagedPlan:
+    """Pages and slots of a step's new tokens (pp_paged_plan); enqueues on the current stream.
+
+    lengths, added: CUDA int32 [requests], tokens held and tokens to come; table int32 [requests][width], whose entries for new
+    pages are written; free_pages int32, given out from position taken[0] on.  rows: how many rows slots and positions have
+    (those behind the last token get slot -1).  out: a PagedPlan of this size; its lengths and taken may be the arguments
+    themselves, as in a loop over steps, whose pages and lengths then go on from call to call."""
+    if _fast is None:
+        _load_torch()
+    if out is None:
+        if rows is None:
+            raise ValueError("rows or out must be given")
+        out = PagedPlan(lengths.shape[0], rows, lengths.device)
+    elif rows is not None and rows != out.slots.shape[0]:
+        raise ValueError("out has another number of rows")
+    r = _fast.paged_plan(lengths, added, table, free_pages, taken, page_size, out.slots, out.positions, out.starts, out.lengths, out.taken,
+                         None if stream is None else stream.cuda_stream)
+    if r is not None:
+        raise PPError(r, "pp_paged_plan")
+    return out
+
+
+def pp_kv_append(cache: PagedCache, k, v, slots, q=None, positions=None, inv_freq=None, interleaved: bool = False, out=None, stream=None):
+    """New keys and values into the cache, with rotary embedding (pp_kv_append); enqueues on the current stream.
+
+    k, v: CUDA [tokens][kv_heads][head_dim] of the cache's type (any float type where the cache has 8 bits), q [tokens][heads]
+    [head_dim], the last axis contiguous; slots int64 [tokens], -1 for rows to leave out.  inv_freq float32 [pairs] and positions
+    int32 [tokens] turn the first 2 * pairs dimensions of q and k: pairs (i, i + pairs), or neighbours where interleaved.
+    Returns q turned, in a new tensor or in out (which may be q); None without q."""
+    r = _fast.kv_append(cache._at, cache.head_dim, cache.kv_heads, cache.device, k, v, slots, q, positions, inv_freq, interleaved, out,
+                        None if stream is None else stream.cuda_stream)
+    if r.__class__ is int:
+        raise PPError(r, "pp_kv_append")
+    return r
+
+
+def pp_paged_attention(cache: PagedCache, q, table, lengths, scale: Optional[float] = None, window: int = 0, out=None, lse: bool = False,
+                       stream=None):
+    """Attention of one new token of each request over the paged cache (pp_paged_attention); enqueues on the current stream.
+
+    q: CUDA [requests][heads][head_dim] of the cache's type (any float type where the cache has 8 bits); table int32
+    [requests][width]; lengths int32 [requests], the new token counted.  scale: 1 / sqrt(head_dim) unless given; window: the last
+    positions to look at, 0 for all.  Returns [requests][heads][head_dim] in q's type (in out, if given); lse: also the logarithm
+    of the sum of the exponentials, float32 [requests][heads]."""
+    r = _fast.paged_attention(cache._at, cache.head_dim, cache.kv_heads, cache.device, q, table, lengths, scale, window, out, lse,
+                              None if stream is None else stream.cuda_stream)
+    if r.__class__ is int:
+        raise PPError(r, "pp_paged_attention")
     return r

@@ -1,0 +1,949 @@
+// Attention of one new token of each request over a paged key-value cache.
+//
+//   out = sum_j p_j v_j,  p = softmax_j(scale q . k_j),  j over a request's last positions
+//
+// One pass over keys and values with a running maximum m and sum l: bound by the bytes of the cache, which are read once for all
+// query heads of a key-value head (up to 8 or 16 of them, the chunk).
+//
+// Division of work.  64 positions of one key-value head (and chunk) are a unit.  The units of all requests in a row, request after
+// request and head after head, are cut into equal parts, one for each CTA that the GPU holds at once, so that lengths of any mix
+// keep all SMs reading to the end.  A CTA finds its part from the lengths alone.  Where a cut falls inside a head's units the CTAs
+// write partial results (m, l, the weighted sum) to the workspace, and a second kernel joins them in the order of the sequence.
+//
+// A warp takes tiles of 16 positions of its own, through a ring in shared memory that 16-byte asynchronous copies fill: rows are
+// looked up in the table one by one, so pages may have any size and end anywhere.  Rows are an odd number of 16 bytes apart, so
+// that eight of them meet no bank twice.
+//
+// Matrix form (MmaCore), S^T[16 positions x 8 heads] = K Q^T and O^T[dim x 8 heads] += V^T P^T, by m16n8k16: the cache is the operand
+// with 16 rows, heads are the eight columns, so no instruction works on padding where a key-value head has eight query heads.
+// P^T changes from the layout of a result to that of an operand by 8x8 transposes in registers; it enters as two 16-bit numbers, the
+// rounded value and what the rounding left (one alone would add an error as large as the output's own rounding).  8-bit codes are
+// exact in f16; the scale of a key multiplies its score, that of a value its p.
+// Scalar form (ScalarCore): floats, a lane per position and half row for the scores, a lane per dimension for the sums.
+#include "pp_internal.h"
+#include "pp_paged.cuh"
+
+namespace pp {
+namespace {
+
+constexpr int kWarps = 4, kThreads = kWarps * 32, kTile = 16, kUnit = kWarps * kTile;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+struct AttnArgs {
+    const void* q;
+    const char *k, *v;                                       // strides below in bytes
+    const float *ks, *vs;
+    const int32_t *table, *lengths;
+    void* out;
+    float *lse, *ws;
+    int64_t q_row, q_head, k_page, k_token, k_head, v_page, v_token, v_head, ld_table;
+    Divisor page;
+    int pages, page_size, batch, capacity, window, heads, kv_heads, group, chunk, n_chunks, dim, granule, q_type, type;
+    float scale;                                             // times log2 e
+};
+
+// Floats of a partial result: m and l of each head of the chunk, then the sums.
+__host__ __device__ inline int64_t part_floats(int chunk, int dim) { return (int64_t)chunk * (dim + 2); }
+
+__device__ __forceinline__ int first_position(const AttnArgs& a, int length) { return a.window > 0 ? max(0, length - a.window) : 0; }
+__device__ __forceinline__ int length_of(const AttnArgs& a, int r) { return min(max(a.lengths[r], 0), a.capacity); }
+// Units of one head of a request: one at least, which writes the output of a request without positions.
+__device__ __forceinline__ int units_of(const AttnArgs& a, int r) {
+    const int n = length_of(a, r);
+    return max(1, (n - first_position(a, n) + kUnit - 1) / kUnit);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ float load_q(const AttnArgs& a, int64_t at) {
+    if (a.q_type == PP_F32) return static_cast<const float*>(a.q)[at];
+    if (a.q_type == PP_F16) return __half2float(static_cast<const __half*>(a.q)[at]);
+    return __bfloat162float(static_cast<const __nv_bfloat16*>(a.q)[at]);
+}
+__device__ __forceinline__ void store_out(const AttnArgs& a, int64_t at, float v) {
+    if (a.q_type == PP_F32) static_cast<float*>(a.out)[at] = v;
+    else if (a.q_type == PP_F16) static_cast<__half*>(a.out)[at] = __float2half_rn(v);
+    else static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
+}
+
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there) {   // zeros if not there
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(there ? BYTES : 0) : "memory");
+}
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void wait_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// What a warp reads: consecutive positions of one request and key-value head, in tiles kWarps * kTile apart.
+struct Reader {
+    const char *k, *v;
+    const float *ks, *vs;
+    const int32_t* row;                                      // of the table
+    int end, entry;                                          // entry: of the tile to be asked for next, for position lane & 15
+};
+
+// The table entry of this lane's position in the tile at `at`, -1 past the end.
+__device__ __forceinline__ int entry_of(const AttnArgs& a, const Reader& r, int at) {
+    const int p = at + (threadIdx.x & 15);
+    return p < r.end ? r.row[a.page.of((uint32_t)p)] : -1;
+}
+
+// Asks for the tile at `at`: 16 rows of keys, of values, and the scales of both.  Returns which rows are there (a bit each).
+// ES: bytes of an element, CHUNKS: 16-byte pieces of a row as the kernel sees it (rows that are shorter end in zeros).
+template <int ES, int CHUNKS, int PITCH, bool Q8>
+__device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, int at, uint32_t stage) {
+    constexpr int kTileBytes = kTile * PITCH;
+    const int lane = threadIdx.x & 31, p = at + (lane & 15);
+    const int entry = r.entry;
+    const bool there = (uint32_t)entry < (uint32_t)a.pages;  // -1 is none, and a number that is no page of the cache neither
+    const uint32_t bits = __ballot_sync(0xffffffffu, there) & 0xffffu;
+    r.entry = entry_of(a, r, at + kUnit);
+    int64_t off = 0;
+    int place = 0;
+    if (there) {
+        place = p - (int)a.page.of((uint32_t)p) * a.page_size;
+        off = lane < 16 ? (int64_t)entry * a.k_page + (int64_t)place * a.k_token : (int64_t)entry * a.v_page + (int64_t)place * a.v_token;
+    }
+    const auto copy = [&](auto bytes) {
+        constexpr int B = decltype(bytes)::value, kPieces = CHUNKS * 16 / B;
+        constexpr int kLanes = kPieces >= 32 ? 32 : kPieces > 16 ? 32 : kPieces > 8 ? 16 : kPieces > 4 ? 8 : 4;
+        const int own = a.dim * ES / B;
+#pragma unroll
+        for (int i = 0; i < kTile * kLanes / 32; ++i) {
+            const int row = i * (32 / kLanes) + lane / kLanes;
+            const int64_t ko = __shfl_sync(0xffffffffu, off, row), vo = __shfl_sync(0xffffffffu, off, 16 + row);
+            const bool has = (bits >> row) & 1;
+#pragma unroll
+            for (int c = lane & (kLanes - 1); c < kPieces; c += kLanes) {
+                const bool in = has && c < own;
+                const int piece = in ? c * B : 0;
+                copy_async<B>(stage + row * PITCH + c * B, r.k + ko + piece, in);
+                copy_async<B>(stage + kTileBytes + row * PITCH + c * B, r.v + vo + piece, in);
+            }
+        }
+    };
+    if (a.granule == 16) copy(std::integral_constant<int, 16>());
+    else if (a.granule == 8) copy(std::integral_constant<int, 8>());
+    else copy(std::integral_constant<int, 4>());
+    if constexpr (Q8) {
+        const int64_t token = there ? (int64_t)entry * a.page_size + place : 0;
+        copy_async<4>(stage + 2 * kTileBytes + lane * 4, (lane < 16 ? r.ks : r.vs) + token * a.kv_heads, there);
+    }
+    return bits;
+}
+
+// ------------------------------------------------------------------------------------------------ matrix form
+enum Kind { kBf16, kF16, kE4m3, kInt8 };
+
+__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void load_transposed(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose(uint32_t v) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+template <bool BF16> __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (BF16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Two numbers as one register of 16-bit ones, the first in the low half.
+template <bool BF16> __device__ __forceinline__ uint32_t pack2(float x, float y) {
+    if constexpr (BF16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        const __half2 v = __floats2half2_rn(x, y);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+}
+template <bool BF16> __device__ __forceinline__ float2 unpack2(uint32_t v) {
+    if constexpr (BF16) return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v));
+    else return __half22float2(*reinterpret_cast<const __half2*>(&v));
+}
+// Two 8-bit codes in the low bytes as two f16 numbers, exactly.
+template <int KIND> __device__ __forceinline__ uint32_t widen(uint32_t two) {
+    if constexpr (KIND == kE4m3) {
+        uint32_t d;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((uint16_t)two));
+        return d;
+    } else {                                                 // 0x6400 + u is 1024 + u; u = code + 128
+        const uint32_t u = __byte_perm(two ^ 0x8080u, 0x64646464u, 0x4140);
+        const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&u), __float2half2_rn(1152.0f));
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+}
+
+// DT: width of a row in elements, rounded up; NT: tiles of eight heads.  With SPLIT_Q (a.q_type f32, NT = 2) the second tile
+// holds what the rounding of the first one's eight heads to f16 left.
+template <int DT, int NT, int KIND> struct MmaCore {
+    static constexpr bool kQ8 = KIND >= kE4m3, kIsBf16 = KIND == kBf16;
+    static constexpr int kEs = kQ8 ? 1 : 2, kChunks = DT * kEs / 16, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
+    static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = kStage <= 5120 ? 4 : 3;
+    static constexpr int kHeads = 8 * NT, kMergePitch = DT + 4;
+    static constexpr int kQFloats = 0;
+    // p is at most 2^kLift: f16 numbers below 2^-24 are lost, and a p can be that small beside the largest one
+    static constexpr float kLift = kIsBf16 ? 0.0f : 14.0f;
+
+    uint32_t q[DT / 16][NT][2];
+    float acc[DT / 16][NT][4], m[NT][2], l[NT][2], f[NT][2], vm;
+
+    __device__ __forceinline__ void begin(const AttnArgs& a, int r, int head0, int n_heads, float*) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const bool split = kQ8 && a.q_type == PP_F32;
+        float factor[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const bool lows = split && nt == 1;
+            const int head = split ? g : nt * 8 + g;
+            const int64_t row = r * a.q_row + (int64_t)(head0 + head) * a.q_head;
+            const bool live = head < n_heads;
+            const auto element = [&](int d) { return live && d < a.dim ? load_q(a, row + d) : 0.0f; };
+            float down = 1.0f;                               // a power of two that brings the head's largest below 2: f16 ends at 65504
+            factor[nt] = a.scale;
+            if constexpr (kQ8) {
+                float most = 0.0f;
+#pragma unroll
+                for (int j = 0; j < DT / 16; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(element(16 * j + 4 * t + i)));
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                if (most > 0.0f && most < INFINITY) {
+                    const int e = min(max(((__float_as_int(most) >> 23) & 255) - 127, -126), 126);
+                    down = __int_as_float((127 - e) << 23);
+                    factor[nt] = a.scale * __int_as_float((127 + e) << 23);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < DT / 16; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int d = kQ8 ? 16 * j + 4 * t + 2 * i : 16 * j + 2 * t + 8 * i;   // codes: four neighbours to a lane, as they lie in its bytes
+                    const float x = element(d) * down, y = element(d + 1) * down;
+                    q[j][nt][i] = pack2<kIsBf16>(x, y);
+                    if (lows) {
+                        const float2 high = unpack2<kIsBf16>(q[j][nt][i]);
+                        q[j][nt][i] = pack2<kIsBf16>(x - high.x, y - high.y);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[j][nt][k] = 0.0f;
+                }
+        }
+        vm = 0.0f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                f[nt][b] = __shfl_sync(0xffffffffu, factor[nt], (2 * t + b) * 4);
+                m[nt][b] = -INFINITY;
+                l[nt][b] = 0.0f;
+            }
+    }
+
+    __device__ __forceinline__ void tile(const AttnArgs& a, uint32_t stage, uint32_t bits, float*) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const bool split = kQ8 && a.q_type == PP_F32;
+        float s[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] = 0.0f;
+        const uint32_t rows = stage + ((lane & 7) + ((lane >> 3) & 1) * 8) * kPitch + (lane >> 4) * 16;
+        if constexpr (kQ8) {
+#pragma unroll
+            for (int c = 0; c < kChunks; c += 2) {
+                uint32_t k[4];                               // rows g and g + 8 of one piece, then of the next
+                load_matrices(k, rows + c * 16);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t a0 = widen<KIND>(k[2 * i]), a2 = widen<KIND>(k[2 * i] >> 16), a1 = widen<KIND>(k[2 * i + 1]), a3 = widen<KIND>(k[2 * i + 1] >> 16);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma<kIsBf16>(s[nt], a0, a1, a2, a3, q[c + i][nt][0], q[c + i][nt][1]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < DT / 16; ++j) {
+                uint32_t k[4];
+                load_matrices(k, rows + j * 32);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<kIsBf16>(s[nt], k[0], k[1], k[2], k[3], q[j][nt][0], q[j][nt][1]);
+            }
+        }
+        if (NT == 2 && split)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[0][i] += s[NT - 1][i];
+                s[NT - 1][i] = 0.0f;
+            }
+
+        float w0 = 1.0f, w1 = 1.0f, change = 1.0f;           // weights of positions g and g + 8: the scales of their values
+        if constexpr (kQ8) {
+            float k0, k1, v0, v1;
+            const uint32_t at = stage + 2 * kTileBytes + g * 4;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k0) : "r"(at) : "memory");
+            asm volatile("ld.shared.f32 %0, [%1+32];" : "=f"(k1) : "r"(at) : "memory");
+            asm volatile("ld.shared.f32 %0, [%1+64];" : "=f"(v0) : "r"(at) : "memory");
+            asm volatile("ld.shared.f32 %0, [%1+96];" : "=f"(v1) : "r"(at) : "memory");
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                s[nt][0] *= k0, s[nt][1] *= k0;
+                s[nt][2] *= k1, s[nt][3] *= k1;
+            }
+            // relative to the largest scale so far, so that p times scale stays within f16; room for twice that avoids most changes
+            const float most = fmaxf(fabsf(v0), fabsf(v1));
+            if (__any_sync(0xffffffffu, most > vm)) {
+                float top = most;
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float now = top < 1e38f ? fmaxf(2.0f * top, 0x1p-100f) : top;   // 1 / vm stays finite
+                change = __fdiv_rn(vm, now);
+                vm = now;
+            }
+            const float inverse = vm > 0.0f ? __fdiv_rn(1.0f, vm) : 0.0f;
+            w0 = v0 * inverse;
+            w1 = v1 * inverse;
+        }
+
+        float p[NT][4], alpha[NT][2];
+        bool moved = kQ8 && change != 1.0f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[nt][i] *= f[nt][i & 1];
+                if (!((bits >> (i < 2 ? g : g + 8)) & 1)) s[nt][i] = -INFINITY;
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                float top = fmaxf(s[nt][b], s[nt][b + 2]);
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float now = fmaxf(m[nt][b], top), from = now == -INFINITY ? 0.0f : now;
+                alpha[nt][b] = exp2_fast(m[nt][b] - from);
+                moved |= m[nt][b] != now;
+                m[nt][b] = now;
+                p[nt][b] = exp2_fast(s[nt][b] - from + kLift);
+                p[nt][b + 2] = exp2_fast(s[nt][b + 2] - from + kLift);
+                l[nt][b] = l[nt][b] * alpha[nt][b] + (p[nt][b] + p[nt][b + 2]);
+                alpha[nt][b] *= change;
+            }
+        }
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int j = 0; j < DT / 16; ++j)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[j][nt][i] *= alpha[nt][i & 1];
+        }
+        uint32_t high[NT][2], low[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float x = p[nt][2 * i] * (i ? w1 : w0), y = p[nt][2 * i + 1] * (i ? w1 : w0);
+                const uint32_t h = pack2<kIsBf16>(x, y);
+                const float2 back = unpack2<kIsBf16>(h);
+                high[nt][i] = transpose(h);
+                low[nt][i] = transpose(pack2<kIsBf16>(x - back.x, y - back.y));
+            }
+        const uint32_t values = stage + kTileBytes;
+        if constexpr (kQ8) {
+            const uint32_t cols = values + ((lane & 7) + ((lane >> 3) & 1) * 8) * kPitch + (lane >> 4) * 16;
+#pragma unroll
+            for (int c = 0; c < kChunks; c += 2) {
+                uint32_t v[4];                               // positions 0..7 and 8..15 of one piece, then of the next
+                load_transposed(v, cols + c * 16);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    // bytes: dims 2g, 2g + 1 of position 2t, then of 2t + 1; row g of the product is dim 2g, row g + 8 dim 2g + 1
+                    const uint32_t x = __byte_perm(v[2 * i], 0, 0x3120), y = __byte_perm(v[2 * i + 1], 0, 0x3120);
+                    const uint32_t a0 = widen<KIND>(x), a1 = widen<KIND>(x >> 16), a2 = widen<KIND>(y), a3 = widen<KIND>(y >> 16);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        mma<kIsBf16>(acc[c + i][nt], a0, a1, a2, a3, high[nt][0], high[nt][1]);
+                        mma<kIsBf16>(acc[c + i][nt], a0, a1, a2, a3, low[nt][0], low[nt][1]);
+                    }
+                }
+            }
+        } else {
+            const uint32_t cols = values + ((lane & 7) + (lane >> 4) * 8) * kPitch + ((lane >> 3) & 1) * 16;
+#pragma unroll
+            for (int j = 0; j < DT / 16; ++j) {
+                uint32_t v[4];
+                load_transposed(v, cols + j * 32);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    mma<kIsBf16>(acc[j][nt], v[0], v[1], v[2], v[3], high[nt][0], high[nt][1]);
+                    mma<kIsBf16>(acc[j][nt], v[0], v[1], v[2], v[3], low[nt][0], low[nt][1]);
+                }
+            }
+        }
+    }
+
+    // m and l of this warp's positions, by head
+    __device__ __forceinline__ void state(float* warp_m, float* warp_l) {
+        const int lane = threadIdx.x & 31, t = lane & 3;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                float sum = l[nt][b];
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if (lane < 4) {
+                    warp_m[nt * 8 + 2 * t + b] = m[nt][b];
+                    warp_l[nt * 8 + 2 * t + b] = sum;
+                }
+            }
+    }
+    // its sums, times a factor by head
+    __device__ __forceinline__ void sums(const AttnArgs&, const float* factor, float* to) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int head = nt * 8 + 2 * t + b;
+                float by = factor[head];
+                if (kQ8) by = by == 0.0f ? 0.0f : by * vm;
+#pragma unroll
+                for (int j = 0; j < DT / 16; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        to[head * kMergePitch + 16 * j + (kQ8 ? 2 * g + i : g + 8 * i)] = acc[j][nt][b + 2 * i] * by;
+            }
+    }
+};
+
+// ------------------------------------------------------------------------------------------------ scalar form
+// DT: 64, 128, 192, 256; HN: query heads of the chunk.  ASYNC: floats that 4 bytes divide at least.  Otherwise any type and alignment:
+// elements are read one by one and stored as floats, times their scale.
+template <int DT, int HN, bool ASYNC> struct ScalarCore {
+    static constexpr bool kQ8 = false;
+    static constexpr int kEs = 4, kChunks = DT / 4, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
+    static constexpr int kHeads = HN, kMergePitch = DT;
+    static constexpr int kStage = 2 * kTileBytes + 16 * 4 * HN, kStages = DT == 256 ? 1 : DT == 192 ? 2 : 3;   // behind the rows: p by position and head
+    static constexpr int kQFloats = HN * DT;
+    static constexpr float kLift = 0.0f;
+
+    float acc[DT / 32][HN], m[HN], l[HN];
+
+    // q of the chunk, in shared memory for all warps; the caller's barrier follows
+    __device__ __forceinline__ void begin(const AttnArgs& a, int r, int head0, int n_heads, float* q) {
+        for (int i = threadIdx.x; i < HN * DT; i += kThreads) {
+            const int head = i / DT, d = i % DT;
+            q[i] = head < n_heads && d < a.dim ? load_q(a, r * a.q_row + (int64_t)(head0 + head) * a.q_head + d) * a.scale : 0.0f;
+        }
+#pragma unroll
+        for (int h = 0; h < HN; ++h) {
+            m[h] = -INFINITY;
+            l[h] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < DT / 32; ++i) acc[i][h] = 0.0f;
+        }
+    }
+
+    // ASYNC false: the tile at `at`, element by element
+    __device__ static uint32_t fetch(const AttnArgs& a, Reader& r, int at, float* stage) {
+        const int lane = threadIdx.x & 31, p = at + (lane & 15);
+        const int entry = r.entry;
+        const bool there = (uint32_t)entry < (uint32_t)a.pages;
+        const uint32_t bits = __ballot_sync(0xffffffffu, there) & 0xffffu;
+        r.entry = entry_of(a, r, at + kUnit);
+        int64_t off = 0;
+        float scale = 1.0f;
+        if (there) {
+            const int place = p - (int)a.page.of((uint32_t)p) * a.page_size;
+            off = lane < 16 ? (int64_t)entry * a.k_page + (int64_t)place * a.k_token : (int64_t)entry * a.v_page + (int64_t)place * a.v_token;
+            if (a.ks) scale = (lane < 16 ? r.ks : r.vs)[((int64_t)entry * a.page_size + place) * a.kv_heads];
+        }
+        for (int row = 0; row < kTile; ++row) {
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                const int64_t o = __shfl_sync(0xffffffffu, off, 16 * which + row);
+                const float by = __shfl_sync(0xffffffffu, scale, 16 * which + row);
+                const bool has = (bits >> row) & 1;
+                const char* src = (which ? r.v : r.k) + o;
+                float* dst = stage + (which * kTileBytes + row * kPitch) / 4;
+#pragma unroll
+                for (int i = 0; i < DT / 32; ++i) {
+                    const int d = lane + 32 * i;
+                    float x = 0.0f;
+                    if (has && d < a.dim) {
+                        if (a.type == PP_F32) x = reinterpret_cast<const float*>(src)[d];
+                        else if (a.type == PP_F16) x = __half2float(reinterpret_cast<const __half*>(src)[d]);
+                        else if (a.type == PP_BF16) x = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(src)[d]);
+                        else if (a.type == PP_E4M3) x = (float)reinterpret_cast<const __nv_fp8_e4m3*>(src)[d] * by;
+                        else x = (float)reinterpret_cast<const int8_t*>(src)[d] * by;
+                    }
+                    dst[d] = x;
+                }
+            }
+        }
+        return bits;
+    }
+
+    __device__ __forceinline__ void tile(const AttnArgs& a, float* stage, uint32_t bits, const float* q) {
+        const int lane = threadIdx.x & 31, key = lane & 15, half = lane >> 4;
+        float s[HN];
+#pragma unroll
+        for (int h = 0; h < HN; ++h) s[h] = 0.0f;
+        const float4* row = reinterpret_cast<const float4*>(stage + key * (kPitch / 4));
+#pragma unroll 4
+        for (int c = half; c < DT / 4; c += 2) {
+            const float4 k = row[c];
+#pragma unroll
+            for (int h = 0; h < HN; ++h) {
+                const float4 x = *reinterpret_cast<const float4*>(q + h * DT + 4 * c);
+                s[h] = fmaf(k.x, x.x, fmaf(k.y, x.y, fmaf(k.z, x.z, fmaf(k.w, x.w, s[h]))));
+            }
+        }
+        const bool there = (bits >> key) & 1;
+        float* p = stage + 2 * kTileBytes / 4;
+        float alpha[HN];
+        bool moved = false;
+#pragma unroll
+        for (int h = 0; h < HN; ++h) {
+            s[h] += __shfl_xor_sync(0xffffffffu, s[h], 16);
+            if (!there) s[h] = -INFINITY;
+            float top = s[h];
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const float now = fmaxf(m[h], top), from = now == -INFINITY ? 0.0f : now;
+            alpha[h] = exp2_fast(m[h] - from);
+            moved |= m[h] != now;
+            m[h] = now;
+            const float e = exp2_fast(s[h] - from);
+            l[h] = l[h] * alpha[h] + (half ? 0.0f : e);
+            if (!half) p[key * HN + h] = e;
+        }
+        __syncwarp();
+        if (moved) {
+#pragma unroll
+            for (int i = 0; i < DT / 32; ++i)
+#pragma unroll
+                for (int h = 0; h < HN; ++h) acc[i][h] *= alpha[h];
+        }
+        const float* v = stage + kTileBytes / 4 + lane;
+#pragma unroll 4
+        for (int j = 0; j < kTile; ++j) {
+            float w[HN];
+#pragma unroll
+            for (int h = 0; h < HN; ++h) w[h] = p[j * HN + h];
+#pragma unroll
+            for (int i = 0; i < DT / 32; ++i) {
+                const float x = v[j * (kPitch / 4) + 32 * i];
+#pragma unroll
+                for (int h = 0; h < HN; ++h) acc[i][h] = fmaf(w[h], x, acc[i][h]);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void state(float* warp_m, float* warp_l) {
+#pragma unroll
+        for (int h = 0; h < HN; ++h) {
+            float sum = l[h];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if ((threadIdx.x & 31) == 0) {
+                warp_m[h] = m[h];
+                warp_l[h] = sum;
+            }
+        }
+    }
+    __device__ __forceinline__ void sums(const AttnArgs&, const float* factor, float* to) {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int h = 0; h < HN; ++h)
+#pragma unroll
+            for (int i = 0; i < DT / 32; ++i) to[h * kMergePitch + lane + 32 * i] = acc[i][h] * factor[h];
+    }
+};
+
+// ---------------------------------------------------------------------------------------------- one kernel for both
+// Exclusive sums of the requests' units over the threads (a run of requests each), and the sum of all.
+__device__ __forceinline__ int64_t sum_before(int64_t mine, int64_t* warp_sums, int64_t& all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t up = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, up, o);
+        if (lane >= o) up += x;
+    }
+    if (lane == 31) warp_sums[warp] = up;
+    __syncthreads();
+    int64_t before = up - mine;
+    all = 0;
+    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) {
+        if (w < warp) before += warp_sums[w];
+        all += warp_sums[w];
+    }
+    return before;
+}
+
+// Unit at which CTA c of n starts, of u units, and the CTA that unit x belongs to.
+__device__ __forceinline__ int64_t part_start(int64_t c, int64_t n, int64_t u) { return c * u / n; }
+__device__ __forceinline__ int64_t part_of(int64_t x, int64_t n, int64_t u) { return ((x + 1) * n - 1) / u; }
+
+template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnArgs a) {
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ int64_t warp_sums[kWarps], found_base;
+    __shared__ int found;
+    __shared__ float warp_m[kWarps][Core::kHeads], warp_l[kWarps][Core::kHeads], factors[kWarps][Core::kHeads], all_m[Core::kHeads], all_l[Core::kHeads];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_release();
+    pdl_wait();
+
+    const int per_request = a.kv_heads * a.n_chunks;
+    const int each = (a.batch + kThreads - 1) / kThreads, r0 = min(tid * each, a.batch), r1 = min(r0 + each, a.batch);
+    int64_t mine = 0, all;
+    for (int r = r0; r < r1; ++r) mine += (int64_t)units_of(a, r) * per_request;
+    const int64_t before = sum_before(mine, warp_sums, all);
+    const int64_t n = min((int64_t)gridDim.x, all);
+    if (blockIdx.x >= n) return;
+    int64_t u = part_start(blockIdx.x, n, all);
+    const int64_t begin = u, end = part_start(blockIdx.x + 1, n, all);
+    if (u >= before && u < before + mine) {
+        int64_t base = before;
+        int r = r0;
+        for (;; ++r) {
+            const int64_t units = (int64_t)units_of(a, r) * per_request;
+            if (u < base + units) break;
+            base += units;
+        }
+        found = r;
+        found_base = base;
+    }
+    __syncthreads();
+    int r = found;
+    int64_t base = found_base;
+
+    unsigned char* own = ring + warp * Core::kStages * Core::kStage;
+    float* q = reinterpret_cast<float*>(ring + kWarps * Core::kStages * Core::kStage);
+    float* merge = reinterpret_cast<float*>(ring);           // after the tiles, in their place: [warp][head][kMergePitch]
+    Core core;
+    while (u < end) {
+        const int units = units_of(a, r);
+        const int unit = (int)(u - base), hc = unit / units, t0 = unit - hc * units;
+        const int t1 = (int)min((int64_t)units, t0 + (end - u));
+        const int length = length_of(a, r), low = first_position(a, length);
+        const int kv = hc / a.n_chunks, head_in = (hc - kv * a.n_chunks) * a.chunk, n_heads = min(a.chunk, a.group - head_in);
+        const int head0 = kv * a.group + head_in;
+
+        Reader reader;
+        reader.k = a.k + kv * a.k_head;
+        reader.v = a.v + kv * a.v_head;
+        reader.ks = a.ks + kv;
+        reader.vs = a.vs + kv;
+        reader.row = a.table + r * a.ld_table;
+        reader.end = min(length, low + t1 * kUnit);
+        int ask_at = low + t0 * kUnit + warp * kTile;
+        reader.entry = entry_of(a, reader, ask_at);
+        const int tiles = ask_at < reader.end ? (reader.end - ask_at + kUnit - 1) / kUnit : 0;
+        uint64_t there = 0;                                  // 16 bits for each stage: the rows that are there
+        int asked = 0, stage = 0;
+        const auto request = [&]() {
+            if (asked < tiles) {
+                uint32_t bits;
+                if constexpr (ASYNC) bits = ask<Core::kEs, Core::kChunks, Core::kPitch, Core::kQ8>(a, reader, ask_at, smem_at(own + stage * Core::kStage));
+                else bits = Core::fetch(a, reader, ask_at, reinterpret_cast<float*>(own + stage * Core::kStage));
+                there = (there & ~(0xffffull << (16 * stage))) | ((uint64_t)bits << (16 * stage));
+                ask_at += kUnit;
+            }
+            commit();
+            ++asked;
+            if (++stage == Core::kStages) stage = 0;
+        };
+#pragma unroll 1
+        for (int i = 0; i < Core::kStages - 1; ++i) request();
+        core.begin(a, r, head0, n_heads, q);
+        if (Core::kQFloats) __syncthreads();
+        int at = 0;
+#pragma unroll 1
+        for (int i = 0; i < tiles; ++i) {
+            if constexpr (Core::kStages > 1) {
+                wait_but<Core::kStages - 2>();
+                __syncwarp();                                // this tile is here, and every lane has left the one before it
+                request();
+            } else {
+                __syncwarp();
+                request();
+                wait_but<0>();
+                __syncwarp();
+            }
+            const uint32_t bits = (uint32_t)(there >> (16 * at)) & 0xffffu;
+            if constexpr (std::is_same_v<decltype(&Core::tile), void (Core::*)(const AttnArgs&, uint32_t, uint32_t, float*)>)
+                core.tile(a, smem_at(own + at * Core::kStage), bits, q);
+            else core.tile(a, reinterpret_cast<float*>(own + at * Core::kStage), bits, q);
+            if (++at == Core::kStages) at = 0;
+        }
+        wait_but<0>();
+        core.state(warp_m[warp], warp_l[warp]);
+        __syncthreads();                                     // the ring is free, and every warp's m and l are known
+        if (tid < kWarps * Core::kHeads) {
+            const int w = tid / Core::kHeads, h = tid % Core::kHeads;
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) top = fmaxf(top, warp_m[i][h]);
+            const auto weight = [&](int i) { return warp_m[i][h] == -INFINITY ? 0.0f : exp2_fast(warp_m[i][h] - top); };
+            factors[w][h] = weight(w);
+            if (w == 0) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) sum += warp_l[i][h] * weight(i);
+                all_m[h] = top;
+                all_l[h] = sum;
+            }
+        }
+        __syncthreads();
+        core.sums(a, factors[warp], merge + warp * Core::kHeads * Core::kMergePitch);
+        __syncthreads();
+        const bool whole = t0 == 0 && t1 == units;
+        float* part = whole ? nullptr : a.ws + (2 * blockIdx.x + (u != begin)) * part_floats(a.chunk, a.dim);
+        for (int i = tid; i < n_heads * a.dim; i += kThreads) {
+            const int h = i / a.dim, d = i - h * a.dim;
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) sum += merge[(w * Core::kHeads + h) * Core::kMergePitch + d];
+            if (whole) store_out(a, ((int64_t)r * a.heads + head0 + h) * a.dim + d, all_l[h] == 0.0f ? 0.0f : __fdiv_rn(sum, all_l[h]));
+            else part[2 * a.chunk + i] = sum;
+        }
+        if (tid < n_heads) {
+            if (!whole) {
+                part[tid] = all_m[tid];
+                part[a.chunk + tid] = all_l[tid];
+            } else if (a.lse) {
+                a.lse[(int64_t)r * a.heads + head0 + tid] = all_l[tid] == 0.0f ? -INFINITY : (all_m[tid] - Core::kLift + log2f(all_l[tid])) * kLn2;
+            }
+        }
+        __syncthreads();
+        u += t1 - t0;
+        if (u == base + (int64_t)units * per_request) {
+            base = u;
+            ++r;
+        }
+    }
+}
+
+// Joins the parts of one head of a request, if it was divided: a CTA each.
+constexpr int kJoinWarps = 8, kJoinThreads = kJoinWarps * 32;
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttnArgs a, int64_t grid, float lift) {
+    __shared__ int64_t warp_sums[kJoinWarps], warp_sums_low[kJoinWarps];
+    __shared__ float sums[kJoinWarps][kMaxHeadDim], some[kJoinWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int r = blockIdx.x / a.heads, head = blockIdx.x - r * a.heads;
+    const int kv = head / a.group, chunk = (head - kv * a.group) / a.chunk, in_chunk = head - kv * a.group - chunk * a.chunk;
+    const int per_request = a.kv_heads * a.n_chunks;
+    pdl_release();
+    pdl_wait();
+    int64_t mine = 0, below = 0, all, low;
+    for (int i = tid; i < a.batch; i += kJoinThreads) {
+        const int64_t units = (int64_t)units_of(a, i) * per_request;
+        mine += units;
+        if (i < r) below += units;
+    }
+    sum_before(mine, warp_sums, all);
+    sum_before(below, warp_sums_low, low);
+    const int units = units_of(a, r);
+    const int64_t s0 = low + (int64_t)(kv * a.n_chunks + chunk) * units, s1 = s0 + units, n = min(grid, all);
+    const int64_t c0 = part_of(s0, n, all), c1 = part_of(s1 - 1, n, all);
+    if (c0 == c1) return;
+    const int64_t floats = part_floats(a.chunk, a.dim);
+    const bool behind = part_start(c0, n, all) < s0;         // the first of the parts is its CTA's last piece
+    const auto part = [&](int64_t c) { return a.ws + (2 * c + (c == c0 && behind)) * floats; };
+    float top = -INFINITY, l = 0.0f;
+    for (int64_t c = c0 + tid; c <= c1; c += kJoinThreads) top = fmaxf(top, part(c)[in_chunk]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (lane == 0) some[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, some[w]);
+    constexpr int kPer = kMaxHeadDim / 32;
+    float acc[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) acc[i] = 0.0f;
+#pragma unroll 4
+    for (int64_t c = c0 + warp; c <= c1; c += kJoinWarps) {
+        const float* p = part(c);
+        const float pm = p[in_chunk], w = pm == -INFINITY ? 0.0f : exp2_fast(pm - top);
+        l += p[a.chunk + in_chunk] * w;
+        const float* x = p + 2 * a.chunk + in_chunk * a.dim;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (lane + 32 * i < a.dim) acc[i] += x[lane + 32 * i] * w;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) sums[warp][lane + 32 * i] = acc[i];
+    if (lane == 0) some[warp] = l;
+    __syncthreads();
+    l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) l += some[w];
+    for (int d = tid; d < a.dim; d += kJoinThreads) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w) sum += sums[w][d];
+        store_out(a, ((int64_t)r * a.heads + head) * a.dim + d, l == 0.0f ? 0.0f : __fdiv_rn(sum, l));
+    }
+    if (a.lse && tid == 0) a.lse[(int64_t)r * a.heads + head] = l == 0.0f ? -INFINITY : (top - lift + log2f(l)) * kLn2;
+}
+
+// ------------------------------------------------------------------------------------------------------ choice
+using Kernel = void (*)(const AttnArgs);
+struct Form {
+    Kernel kernel = nullptr;
+    int smem = 0, heads = 0;
+    float lift = 0.0f;
+    PerDeviceOnce* opt_in = nullptr;
+    int* resident = nullptr;                                 // CTAs that an SM holds, by device
+};
+
+template <class Core, bool ASYNC> Form form_of() {
+    static PerDeviceOnce opt_in;
+    static int resident[PerDeviceOnce::kMaxDevices] = {};
+    Form f;
+    f.kernel = attn_kernel<Core, ASYNC>;
+    f.smem = std::max(kWarps * Core::kStages * Core::kStage, kWarps * Core::kHeads * Core::kMergePitch * 4) + Core::kQFloats * 4;
+    f.heads = Core::kHeads;
+    f.lift = Core::kLift;
+    f.opt_in = &opt_in;
+    f.resident = resident;
+    return f;
+}
+template <int KIND> Form mma_form(int dim, bool two) {
+    if (two) return dim <= 64 ? form_of<MmaCore<64, 2, KIND>, true>() : dim <= 96 ? form_of<MmaCore<96, 2, KIND>, true>() : form_of<MmaCore<128, 2, KIND>, true>();
+    return dim <= 64 ? form_of<MmaCore<64, 1, KIND>, true>() : dim <= 96 ? form_of<MmaCore<96, 1, KIND>, true>()
+         : dim <= 128 ? form_of<MmaCore<128, 1, KIND>, true>() : dim <= 192 ? form_of<MmaCore<192, 1, KIND>, true>() : form_of<MmaCore<256, 1, KIND>, true>();
+}
+template <bool ASYNC> Form scalar_form(int dim, int group) {
+    if (dim <= 64) return group <= 1 ? form_of<ScalarCore<64, 1, ASYNC>, ASYNC>() : group <= 4 ? form_of<ScalarCore<64, 4, ASYNC>, ASYNC>() : form_of<ScalarCore<64, 8, ASYNC>, ASYNC>();
+    if (dim <= 128) return group <= 1 ? form_of<ScalarCore<128, 1, ASYNC>, ASYNC>() : group <= 4 ? form_of<ScalarCore<128, 4, ASYNC>, ASYNC>() : form_of<ScalarCore<128, 8, ASYNC>, ASYNC>();
+    if (dim <= 192) return group <= 1 ? form_of<ScalarCore<192, 1, ASYNC>, ASYNC>() : group <= 4 ? form_of<ScalarCore<192, 4, ASYNC>, ASYNC>() : form_of<ScalarCore<192, 8, ASYNC>, ASYNC>();
+    return group <= 1 ? form_of<ScalarCore<256, 1, ASYNC>, ASYNC>() : group <= 4 ? form_of<ScalarCore<256, 4, ASYNC>, ASYNC>() : form_of<ScalarCore<256, 8, ASYNC>, ASYNC>();
+}
+
+// The form of a call, the bytes of its asynchronous copies and its heads per chunk.
+Form choose(const pp_paged_cache_t& c, pp_dtype_t q_type, int group, int& granule, int& chunk) {
+    const int row = c.head_dim * type_bytes(c.dtype);
+    granule = std::min(cache_alignment(c), 16);
+    while (row % granule) granule /= 2;
+    const bool split = is_8bit(c.dtype) && q_type == PP_F32;  // q as two f16 numbers takes both tiles
+    chunk = 8;
+    if (granule >= 4 && c.dtype != PP_F32 && !(split && c.head_dim > 128)) {
+        // 16 heads where a key-value head has more than 8: above 128 dimensions their sums do not fit the registers
+        const bool two = split || (group > 8 && c.head_dim <= 128);
+        if (two && !split) chunk = 16;
+        switch (c.dtype) {
+            case PP_BF16: return mma_form<kBf16>(c.head_dim, two);
+            case PP_F16: return mma_form<kF16>(c.head_dim, two);
+            case PP_E4M3: return mma_form<kE4m3>(c.head_dim, two);
+            default: return mma_form<kInt8>(c.head_dim, two);
+        }
+    }
+    const Form f = granule >= 4 && c.dtype == PP_F32 ? scalar_form<true>(c.head_dim, group) : scalar_form<false>(c.head_dim, group);
+    chunk = f.heads;
+    return f;
+}
+
+// CTAs that the current device holds at once.
+cudaError_t grid_of(const Form& f, int& grid) {
+    int device = 0;
+    if (cudaError_t e = cudaGetDevice(&device)) return e;
+    if (!f.opt_in->is_done(device)) {
+        int n = 0;
+        if (cudaError_t e = cudaFuncSetAttribute(f.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, f.smem)) return e;
+        if (cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, f.kernel, kThreads, (size_t)f.smem)) return e;
+        if (device >= PerDeviceOnce::kMaxDevices) {
+            grid = std::max(n, 1) * sm_count();
+            return cudaSuccess;
+        }
+        f.resident[device] = std::max(n, 1);
+        f.opt_in->mark(device);
+    }
+    grid = f.resident[device] * sm_count();
+    return cudaSuccess;
+}
+
+pp_status_t check_call(const pp_paged_cache_t* cache, pp_dtype_t q_type, int batch, int heads, int width, int window) {
+    if (const pp_status_t st = check_cache(cache)) return st;
+    if (!is_float(q_type) || (q_type != cache->dtype && !is_8bit(cache->dtype))) return PP_ERR_UNSUPPORTED;
+    if (batch < 0 || heads < 1 || heads % cache->kv_heads || width < 1 || window < 0) return PP_ERR_INVALID_ARG;
+    if ((int64_t)width * cache->page_size > INT32_MAX - 2 * kUnit || heads > (1 << 20) || (int64_t)batch * heads > INT32_MAX) return PP_ERR_UNSUPPORTED;
+    return PP_OK;
+}
+
+// Whether any request can have more than one unit.
+bool divided(const pp_paged_cache_t& c, int width, int window) {
+    const int64_t capacity = (int64_t)width * c.page_size;
+    return (window > 0 ? std::min<int64_t>(window, capacity) : capacity) > kUnit;
+}
+
+}  // namespace
+}  // namespace pp
+
+extern "C" pp_status_t pp_paged_attention_workspace(const pp_paged_cache_t* cache, pp_dtype_t q_type, int batch, int heads, int width,
+                                                    int window, int64_t* bytes) {
+    using namespace pp;
+    if (!bytes) return PP_ERR_INVALID_ARG;
+    *bytes = 0;
+    if (const pp_status_t st = check_call(cache, q_type, batch, heads, width, window)) return st;
+    if (batch == 0 || !divided(*cache, width, window)) return PP_OK;
+    int granule, chunk, grid;
+    const Form f = choose(*cache, q_type, heads / cache->kv_heads, granule, chunk);
+    if (const cudaError_t e = grid_of(f, grid)) return status_of(e);
+    *bytes = (int64_t)grid * 2 * part_floats(chunk, cache->head_dim) * 4;
+    return PP_OK;
+}
+
+extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const void* q, int64_t q_row, int64_t q_head, pp_dtype_t q_type,
+                                          const int32_t* table, int64_t ld_table, int width, const int32_t* lengths, int batch, int heads,
+                                          float scale, int window, void* out, float* lse, void* workspace, int64_t workspace_bytes,
+                                          void* cuda_stream) {
+    using namespace pp;
+    if (const pp_status_t st = check_call(cache, q_type, batch, heads, width, window)) return st;
+    if (!(scale > -INFINITY && scale < INFINITY)) return PP_ERR_INVALID_ARG;
+    if (batch == 0) return PP_OK;
+    const pp_paged_cache_t& c = *cache;
+    const int tb = type_bytes(q_type);
+    const int64_t most = (int64_t)1 << 56;
+    if (!q || !table || !lengths || !out || q_row < 0 || q_head < 0 || q_row > most / batch || q_head > most / heads || ld_table < width || ld_table > most / batch)
+        return PP_ERR_INVALID_ARG;
+    if (!aligned_to(q, tb) || !aligned_to(out, tb) || !aligned_to(table, 4) || !aligned_to(lengths, 4) || !aligned_to(lse, 4) || !aligned_to(workspace, 16))
+        return PP_ERR_INVALID_ARG;
+    const int64_t q_span = ((batch - 1) * q_row + (heads - 1) * q_head + c.head_dim) * tb, out_span = (int64_t)batch * heads * c.head_dim * tb;
+    if (spans_meet(q, q_span, out, out_span)) return PP_ERR_INVALID_ARG;
+    const int group = heads / c.kv_heads;
+    int granule, chunk, grid;
+    const Form f = choose(c, q_type, group, granule, chunk);
+    if (const cudaError_t e = grid_of(f, grid)) return status_of(e);
+    const bool parts = divided(c, width, window);
+    const int64_t need = parts ? (int64_t)grid * 2 * part_floats(chunk, c.head_dim) * 4 : 0;
+    if (need && (!workspace || workspace_bytes < need)) return PP_ERR_INVALID_ARG;
+    const int es = type_bytes(c.dtype);
+    AttnArgs a{q, static_cast<const char*>(c.k), static_cast<const char*>(c.v), c.k_scales, c.v_scales, table, lengths, out, lse,
+               static_cast<float*>(workspace), q_row, q_head, c.k_page * es, c.k_token * es, c.k_head * es, c.v_page * es, c.v_token * es,
+               c.v_head * es, ld_table, Divisor((uint32_t)c.page_size), c.pages, c.page_size, batch, width * c.page_size, window, heads, c.kv_heads, group,
+               chunk, (group + chunk - 1) / chunk, c.head_dim, granule, q_type, c.dtype, scale * kLog2e};
+    const int64_t segments = (int64_t)batch * c.kv_heads * a.n_chunks;
+    if (!parts) grid = (int)std::min<int64_t>(grid, segments);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e = launch_pdl(f.kernel, dim3((unsigned)grid), dim3(kThreads), (size_t)f.smem, s, 1, a);
+    if (e == cudaSuccess && parts) e = launch_pdl(join_kernel, dim3((unsigned)(batch * heads)), dim3(kJoinThreads), 0, s, 1, a, (int64_t)grid, f.lift);
+    return status_of(e);
+}

@@ -1,0 +1,479 @@
+// Paged key-value cache: the plan of a step (pages and slots of the new tokens) and the append of their keys and values with
+// rotary embedding.
+//
+// Plan.  A request that holds h tokens and gets a more needs the pages ceil(h / p) .. ceil((h + a) / p); where they start in the
+// free list is an exclusive sum over the requests before it, as is the first row of its tokens.  Every CTA makes both sums
+// for all requests (a few thousand additions in shared memory, cheaper than a second launch that would wait for a first),
+// then takes its share of the rows, four to a thread: a binary search for the row's request, and its page from the free
+// list where it is a new one, else from the table, whose old entries nobody writes.
+//
+// Append.  All bandwidth for many tokens, all latency for few.  Eight elements to a lane and 8, 16 or 32 lanes to a head
+// (VEC): a lane has the same dimensions of every head, so its cosines and sines stay in registers, and the partner of a pair
+// sits in a neighbouring lane (halves) or in the lane itself (neighbouring pairs).  The angle is a product in 64 bits,
+// brought into a turn there: position 10^6 leaves a 32-bit angle 2^-5 of a radian.
+#include "pp_internal.h"
+#include "pp_paged.cuh"
+
+namespace pp {
+namespace {
+
+// -------------------------------------------------------------------------------------------------------- plan
+constexpr int kPlanThreads = 256, kPlanRows = 4, kMaxRequests = 8192;
+
+struct PlanArgs {
+    const int32_t *lengths, *added, *free_pages, *taken;
+    int32_t* table;
+    int64_t* slots;
+    int32_t *positions, *starts, *lengths_out, *taken_out;
+    int64_t ld_table;
+    int width, n_free, requests, page_size, rows, capacity;
+    Divisor page;
+    bool wide;                                               // slots and positions start on 16 bytes
+    bool rows_too, state_too;                                // what this launch writes: rows, starts and table; lengths_out and taken_out
+};
+
+__device__ __forceinline__ int sat32(int64_t v) { return v > INT32_MAX ? INT32_MAX : (int)v; }
+
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a) {
+    extern __shared__ int32_t plan_smem[];
+    int32_t* starts = plan_smem;                             // [requests + 1]
+    int32_t* have = starts + a.requests + 1;                 // [requests]
+    int32_t* base = have + a.requests;                       // [requests]: pages that requests before this one need
+    __shared__ int64_t warp_pages[8], warp_rows[8];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_release();
+    pdl_wait();
+    const int each = (a.requests + kPlanThreads - 1) / kPlanThreads, r0 = min(tid * each, a.requests), r1 = min(r0 + each, a.requests);
+    const int64_t taken = *a.taken;
+    int64_t pages = 0, rows = 0;
+    for (int r = r0; r < r1; ++r) {
+        const int h = min(max(a.lengths[r], 0), a.capacity), add = max(a.added[r], 0);
+        const int total = (int)min((int64_t)h + add, (int64_t)a.capacity);
+        have[r] = h;
+        base[r] = (int)(a.page.of(total + a.page_size - 1) - a.page.of(h + a.page_size - 1));
+        starts[r] = add;
+        pages += base[r];
+        rows += add;
+    }
+    int64_t before_pages = pages, before_rows = rows;        // inclusive, over the lanes, then over the warps
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t p = __shfl_up_sync(0xffffffffu, before_pages, o), q = __shfl_up_sync(0xffffffffu, before_rows, o);
+        if (lane >= o) before_pages += p, before_rows += q;
+    }
+    if (lane == 31) warp_pages[warp] = before_pages, warp_rows[warp] = before_rows;
+    __syncthreads();                                         // also: every length has been read before one is written
+    int64_t all_pages = 0, all_rows = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+        if (w == warp) before_pages += all_pages, before_rows += all_rows;
+        all_pages += warp_pages[w];
+        all_rows += warp_rows[w];
+    }
+    before_pages -= pages;
+    before_rows -= rows;
+    for (int r = r0; r < r1; ++r) {
+        const int need = base[r], add = starts[r];
+        base[r] = sat32(before_pages);
+        starts[r] = (int)min(before_rows, (int64_t)a.rows);
+        if (a.rows_too && blockIdx.x == 0) a.starts[r] = starts[r];
+        if (a.state_too && blockIdx.x == 0) a.lengths_out[r] = (int)min((int64_t)have[r] + add, (int64_t)a.capacity);
+        before_pages += need;
+        before_rows += add;
+    }
+    if (tid == 0) {
+        starts[a.requests] = (int)min(all_rows, (int64_t)a.rows);
+        if (blockIdx.x == 0 && a.rows_too) a.starts[a.requests] = starts[a.requests];
+        if (blockIdx.x == 0 && a.state_too) *a.taken_out = sat32(max(taken + all_pages, (int64_t)INT32_MIN));
+    }
+    __syncthreads();
+    if (!a.rows_too) return;
+
+    // the position in the free list of page `column` of request r, whose first new page is `first`
+    const auto given = [&](int r, int column, int first) {
+        const int64_t at = taken + base[r] + (column - first);
+        return at >= 0 && at < a.n_free ? a.free_pages[at] : -1;
+    };
+    for (int r = blockIdx.x * (kPlanThreads / 32) + warp; r < a.requests; r += gridDim.x * (kPlanThreads / 32)) {
+        const int total = (int)min((int64_t)have[r] + max(a.added[r], 0), (int64_t)a.capacity);
+        const int first = (int)a.page.of(have[r] + a.page_size - 1), need = (int)a.page.of(total + a.page_size - 1) - first;
+        for (int i = lane; i < need; i += 32) a.table[r * a.ld_table + first + i] = given(r, first + i, first);
+    }
+    const int64_t row0 = ((int64_t)blockIdx.x * kPlanThreads + tid) * kPlanRows;
+    if (row0 >= a.rows) return;
+    const int live = starts[a.requests];
+    int low = 0, high = a.requests;                          // the first request whose rows end behind row0, or requests
+    while (low < high) {
+        const int mid = (low + high) / 2;
+        if (starts[mid + 1] > row0) high = mid;
+        else low = mid + 1;
+    }
+    int64_t slot[kPlanRows];
+    int position[kPlanRows];
+#pragma unroll
+    for (int i = 0; i < kPlanRows; ++i) {
+        const int64_t row = row0 + i;
+        slot[i] = -1;
+        position[i] = 0;
+        if (row >= live) continue;
+        while (starts[low + 1] <= row) ++low;                // row < live: there is one
+        const int64_t p = have[low] + (row - starts[low]);
+        position[i] = sat32(p);
+        if (p < a.capacity) {
+            const int column = (int)a.page.of((uint32_t)p), first = (int)a.page.of(have[low] + a.page_size - 1);
+            const int number = column >= first ? given(low, column, first) : a.table[low * a.ld_table + column];
+            if (number >= 0) slot[i] = (int64_t)number * a.page_size + (p - (int64_t)column * a.page_size);
+        }
+    }
+    if (a.wide && row0 + kPlanRows <= a.rows) {
+        longlong2* s = reinterpret_cast<longlong2*>(a.slots + row0);
+        s[0] = make_longlong2(slot[0], slot[1]);
+        s[1] = make_longlong2(slot[2], slot[3]);
+        *reinterpret_cast<int4*>(a.positions + row0) = make_int4(position[0], position[1], position[2], position[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPlanRows; ++i)
+            if (row0 + i < a.rows) {
+                a.slots[row0 + i] = slot[i];
+                a.positions[row0 + i] = position[i];
+            }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------ append
+constexpr int kAppendThreads = 256;
+
+struct AppendArgs {
+    const void *q, *k, *v;
+    void *q_out, *ck, *cv;
+    float *ks, *vs;
+    const int64_t* slots;
+    const int32_t* positions;
+    const float* inv_freq;
+    int64_t q_token, q_head, o_token, o_head, k_token, k_head, v_token, v_head;
+    int64_t ck_page, ck_token, ck_head, cv_page, cv_token, cv_head, n_slots;
+    int heads, kv_heads, dim, page_size, pairs, interleaved, code_type, lanes;   // lanes: of a head (VEC)
+};
+
+// Cosine and sine of position * inv_freq, the angle brought into half a turn around 0 in 64 bits.
+__device__ __forceinline__ float2 turn(int position, float inv_freq) {
+    const double a = (double)position * (double)inv_freq;
+    const double n = rint(a * 0.15915494309189533577);
+    double r = fma(-n, 6.28318530717958647693, a);           // 2 pi as a sum of two doubles
+    r = fma(-n, 2.449293598294706414e-16, r);
+    float s, c;
+    sincosf((float)r, &s, &c);
+    return make_float2(c, s);
+}
+
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
+// 8-bit code of v / scale, to nearest even; scale is not 0.
+__device__ __forceinline__ uint8_t code_of(float v, float scale, bool e4m3) {
+    v = __fdiv_rn(v, scale);
+    if (e4m3) return (uint8_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3);
+    return (uint8_t)(int8_t)__float2int_rn(fminf(fmaxf(v, -127.0f), 127.0f));
+}
+// The scale of a row whose largest magnitude is `most` (NaN and infinity: NaN).
+__device__ __forceinline__ float scale_of(float most, bool e4m3) {
+    return most < INFINITY ? __fdiv_rn(most, e4m3 ? 448.0f : 127.0f) : __int_as_float(0x7fffffff);
+}
+
+// Page and place of a slot; slots above 32 bits are rare, and their division slow.
+__device__ __forceinline__ void split_slot(int64_t slot, int page_size, int64_t& page, int64_t& place) {
+    if (slot >> 32) page = slot / page_size;
+    else page = (uint32_t)slot / (uint32_t)page_size;
+    place = slot - page * page_size;
+}
+
+// The heads of a token in one order: those of q, of k, of v.
+struct Row { int kind, head; };
+__device__ __forceinline__ Row row_of(const AppendArgs& a, int i) {
+    if (i < a.heads) return {0, i};
+    if (i < a.heads + a.kv_heads) return {1, i - a.heads};
+    return {2, i - a.heads - a.kv_heads};
+}
+
+// VEC: a.lanes lanes to a head, eight elements to a lane.  Q8: the cache holds 8 bits.
+template <typename T, bool Q8>
+__global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs a) {
+    __shared__ float2 turns[kMaxHeadDim / 2];
+    const int tid = threadIdx.x, lanes = a.lanes, j = tid & (lanes - 1), groups = kAppendThreads / lanes;
+    const int64_t token = blockIdx.x;
+    const int rows = a.heads + 2 * a.kv_heads, first = blockIdx.y * groups + tid / lanes, step = gridDim.y * groups;
+    const int loops = (rows - (int)blockIdx.y * groups + step - 1) / step;   // the same for every thread: shuffles need them all
+    pdl_release();
+    pdl_wait();
+    const bool mine = 8 * j < a.dim;
+    const int64_t slot = a.slots[token];
+    const auto source = [&](int i) {
+        const Row r = row_of(a, i);
+        return r.kind == 0 ? static_cast<const T*>(a.q) + token * a.q_token + r.head * a.q_head
+             : r.kind == 1 ? static_cast<const T*>(a.k) + token * a.k_token + r.head * a.k_head
+                           : static_cast<const T*>(a.v) + token * a.v_token + r.head * a.v_head;
+    };
+    using Raw = Pack<T, 8>;
+    Raw raw;
+    if (mine && first < rows) raw = *reinterpret_cast<const Raw*>(source(first) + 8 * j);
+    if (a.pairs) {
+        const int position = a.positions[token];
+        for (int i = tid; i < a.pairs; i += kAppendThreads) turns[i] = turn(position, a.inv_freq[i]);
+        __syncthreads();
+    }
+    // this lane's turns; element e: cosine, and the sine with the sign of its place in the pair
+    const int lane = tid & 31;
+    int partner = lane;
+    float cosine[8], sine[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int d = 8 * j + e;
+        cosine[e] = 1.0f;
+        sine[e] = 0.0f;
+        if (d < 2 * a.pairs) {
+            const float2 t = turns[a.interleaved ? d / 2 : d < a.pairs ? d : d - a.pairs];
+            const bool second = a.interleaved ? (d & 1) : d >= a.pairs;
+            cosine[e] = t.x;
+            sine[e] = second ? t.y : -t.y;
+        }
+    }
+    const bool turned = 8 * j < 2 * a.pairs;
+    if (turned && !a.interleaved) partner = 8 * j < a.pairs ? lane + a.pairs / 8 : lane - a.pairs / 8;
+
+    const bool stored = slot >= 0 && slot < a.n_slots;
+    int64_t page = 0, place = 0;
+    if (stored) split_slot(slot, a.page_size, page, place);
+    for (int n = 0, i = first; n < loops; ++n, i += step) {
+        const bool live = mine && i < rows;
+        Raw next;
+        if (mine && i + step < rows) next = *reinterpret_cast<const Raw*>(source(i + step) + 8 * j);
+        const Row r = row_of(a, i);
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = live ? to_float(raw.v[e]) : 0.0f;
+        if (a.pairs) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = a.interleaved ? x[e ^ 1] : __shfl_sync(0xffffffffu, x[e], partner);
+            if (turned && r.kind < 2) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (8 * j + e < 2 * a.pairs) x[e] = fmaf(x[e], cosine[e], y[e] * sine[e]);
+            }
+        }
+        if (r.kind == 0) {
+            if (live) store_vec(static_cast<T*>(a.q_out) + token * a.o_token + r.head * a.o_head + 8 * j, x);
+        }
+        if constexpr (Q8) {
+            const bool e4m3 = a.code_type == PP_E4M3;
+            float most = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max_or_nan(most, fabsf(x[e]));
+            for (int o = 1; o < lanes; o <<= 1) most = max_or_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
+            if (r.kind != 0 && live && stored) {
+                const float scale = scale_of(most, e4m3);
+                uint32_t u[2] = {0, 0};
+                if (scale != 0.0f) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[e / 4] |= (uint32_t)code_of(x[e], scale, e4m3) << (8 * (e & 3));
+                }
+                uint8_t* dst = r.kind == 1 ? static_cast<uint8_t*>(a.ck) + page * a.ck_page + place * a.ck_token + r.head * a.ck_head
+                                           : static_cast<uint8_t*>(a.cv) + page * a.cv_page + place * a.cv_token + r.head * a.cv_head;
+                *reinterpret_cast<uint2*>(dst + 8 * j) = make_uint2(u[0], u[1]);
+                if (j == 0) (r.kind == 1 ? a.ks : a.vs)[slot * a.kv_heads + r.head] = scale;
+            }
+        } else if (r.kind != 0 && live && stored) {
+            T* dst = r.kind == 1 ? static_cast<T*>(a.ck) + page * a.ck_page + place * a.ck_token + r.head * a.ck_head
+                                 : static_cast<T*>(a.cv) + page * a.cv_page + place * a.cv_token + r.head * a.cv_head;
+            store_vec(dst + 8 * j, x);
+        }
+        raw = next;
+    }
+}
+
+// Any width and alignment: a warp to a head, element by element.
+template <typename T>
+__global__ void __launch_bounds__(kAppendThreads) append_any_kernel(const AppendArgs a) {
+    constexpr int kPer = kMaxHeadDim / 32;
+    __shared__ float2 turns[kMaxHeadDim / 2];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t token = blockIdx.x;
+    const int rows = a.heads + 2 * a.kv_heads;
+    pdl_release();
+    pdl_wait();
+    const int64_t slot = a.slots[token];
+    if (a.pairs) {
+        const int position = a.positions[token];
+        for (int i = tid; i < a.pairs; i += kAppendThreads) turns[i] = turn(position, a.inv_freq[i]);
+        __syncthreads();
+    }
+    const bool stored = slot >= 0 && slot < a.n_slots;
+    int64_t page = 0, place = 0;
+    if (stored) split_slot(slot, a.page_size, page, place);
+    for (int i = blockIdx.y * (kAppendThreads / 32) + warp; i < rows; i += gridDim.y * (kAppendThreads / 32)) {
+        const Row r = row_of(a, i);
+        const T* src = r.kind == 0 ? static_cast<const T*>(a.q) + token * a.q_token + r.head * a.q_head
+                     : r.kind == 1 ? static_cast<const T*>(a.k) + token * a.k_token + r.head * a.k_head
+                                   : static_cast<const T*>(a.v) + token * a.v_token + r.head * a.v_head;
+        float x[kPer];
+        float most = 0.0f;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const int d = lane + 32 * e;
+            x[e] = 0.0f;
+            if (d >= a.dim) continue;
+            x[e] = to_float(src[d]);
+            if (r.kind < 2 && d < 2 * a.pairs) {
+                const bool second = a.interleaved ? (d & 1) : d >= a.pairs;
+                const float2 t = turns[a.interleaved ? d / 2 : second ? d - a.pairs : d];
+                const float y = to_float(src[a.interleaved ? d ^ 1 : second ? d - a.pairs : d + a.pairs]);
+                x[e] = fmaf(x[e], t.x, y * (second ? t.y : -t.y));
+            }
+            most = max_or_nan(most, fabsf(x[e]));
+        }
+        __syncwarp();                                        // q_out may be q: every lane has read what another will write
+        if (r.kind == 0) {
+            T* dst = static_cast<T*>(a.q_out) + token * a.o_token + r.head * a.o_head;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (lane + 32 * e < a.dim) dst[lane + 32 * e] = from_float<T>(x[e]);
+            continue;
+        }
+        if (!stored) continue;
+        const int64_t at = r.kind == 1 ? page * a.ck_page + place * a.ck_token + r.head * a.ck_head : page * a.cv_page + place * a.cv_token + r.head * a.cv_head;
+        void* cache = r.kind == 1 ? a.ck : a.cv;
+        if (a.code_type == PP_E4M3 || a.code_type == PP_I8) {
+            const bool e4m3 = a.code_type == PP_E4M3;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) most = max_or_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
+            const float scale = scale_of(most, e4m3);
+            uint8_t* dst = static_cast<uint8_t*>(cache) + at;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (lane + 32 * e < a.dim) dst[lane + 32 * e] = scale != 0.0f ? code_of(x[e], scale, e4m3) : 0;
+            if (lane == 0) (r.kind == 1 ? a.ks : a.vs)[slot * a.kv_heads + r.head] = scale;
+        } else {
+            T* dst = static_cast<T*>(cache) + at;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (lane + 32 * e < a.dim) dst[lane + 32 * e] = from_float<T>(x[e]);
+        }
+    }
+}
+
+template <typename T> cudaError_t launch_append(const AppendArgs& a, bool vec, int tokens, cudaStream_t stream) {
+    const int rows = a.heads + 2 * a.kv_heads;
+    const int at_once = vec ? kAppendThreads / a.lanes : kAppendThreads / 32;
+    // a CTA per token where tokens fill the GPU; else a token's heads are divided, down to one to a group of lanes
+    int parts = 1;
+    while (parts * at_once < rows && (int64_t)tokens * parts < 4 * (int64_t)sm_count()) ++parts;
+    auto k = !vec ? append_any_kernel<T> : a.code_type == PP_E4M3 || a.code_type == PP_I8 ? append_kernel<T, true> : append_kernel<T, false>;
+    return launch_pdl(k, dim3((unsigned)tokens, (unsigned)parts), dim3(kAppendThreads), 0, stream, 1, a);
+}
+
+}  // namespace
+}  // namespace pp
+
+extern "C" pp_status_t pp_paged_plan(const int32_t* lengths, const int32_t* added, int32_t* table, int64_t ld_table, int width,
+                                     const int32_t* free_pages, int n_free, const int32_t* taken, int requests, int page_size, int rows,
+                                     int64_t* slots, int32_t* positions, int32_t* starts, int32_t* lengths_out, int32_t* taken_out,
+                                     void* cuda_stream) {
+    using namespace pp;
+    if (requests < 0 || width < 1 || page_size < 1 || rows < 0 || n_free < 0 || !taken || !starts || !taken_out) return PP_ERR_INVALID_ARG;
+    if (requests > 0 && (!lengths || !added || !table || !lengths_out || ld_table < width)) return PP_ERR_INVALID_ARG;
+    if ((rows > 0 && (!slots || !positions)) || (n_free > 0 && !free_pages)) return PP_ERR_INVALID_ARG;
+    const int64_t capacity = (int64_t)width * page_size;
+    if (requests > kMaxRequests || capacity > INT32_MAX - page_size) return PP_ERR_UNSUPPORTED;     // a length rounded up to pages fits too
+    if (ld_table > ((int64_t)1 << 40)) return PP_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)lengths, (const void*)added, (const void*)table, (const void*)free_pages, (const void*)taken,
+                          (const void*)positions, (const void*)starts, (const void*)lengths_out, (const void*)taken_out})
+        if (!aligned_to(p, 4)) return PP_ERR_INVALID_ARG;
+    if (!aligned_to(slots, 8)) return PP_ERR_INVALID_ARG;
+    const int64_t n = requests;
+    struct Span { const void* p; int64_t bytes; };
+    const Span in[] = {{lengths, 4 * n}, {added, 4 * n}, {free_pages, 4 * (int64_t)n_free}, {taken, 4}};
+    const Span out[] = {{table, n ? 4 * ((n - 1) * ld_table + width) : 0}, {slots, 8 * (int64_t)rows}, {positions, 4 * (int64_t)rows},
+                        {starts, 4 * (n + 1)}, {lengths_out, 4 * n}, {taken_out, 4}};
+    for (const Span& o : out) {
+        for (const Span& i : in) {
+            const bool in_place = o.p == i.p && ((i.p == lengths && o.p == lengths_out) || (i.p == taken && o.p == taken_out));
+            if (!in_place && spans_meet(o.p, o.bytes, i.p, i.bytes)) return PP_ERR_INVALID_ARG;
+        }
+        for (const Span& other : out)
+            if (&other != &o && spans_meet(o.p, o.bytes, other.p, other.bytes)) return PP_ERR_INVALID_ARG;
+    }
+    PlanArgs a{lengths, added, free_pages, taken, table, slots, positions, starts, lengths_out, taken_out, ld_table,
+               width, n_free, requests, page_size, rows, (int)capacity, Divisor((uint32_t)page_size), aligned_to(slots, 16) && aligned_to(positions, 16), true, true};
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const size_t smem = (3 * (size_t)requests + 1) * 4;
+    static PerDeviceOnce opt_in;
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return status_of(cudaErrorInvalidDevice);
+    if (smem > 48 * 1024 && !opt_in.is_done(device)) {
+        if (cudaError_t e = cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (3 * kMaxRequests + 1) * 4)) return status_of(e);
+        opt_in.mark(device);
+    }
+    const int64_t per = kPlanThreads * kPlanRows;
+    const unsigned grid = (unsigned)std::max<int64_t>(1, (rows + per - 1) / per);
+    // In place and with several CTAs, one would write a length that another has still to read: lengths and pages taken are then
+    // written by a launch of their own, behind the first.
+    const bool apart = grid > 1 && (lengths == lengths_out || taken == taken_out);
+    a.state_too = !apart;
+    cudaError_t e = launch_pdl(plan_kernel, dim3(grid), dim3(kPlanThreads), smem, stream, 1, a);
+    if (e == cudaSuccess && apart) {
+        a.rows_too = false;
+        a.state_too = true;
+        e = launch_pdl(plan_kernel, dim3(1), dim3(kPlanThreads), smem, stream, 1, a);
+    }
+    return status_of(e);
+}
+
+extern "C" pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q, int64_t q_token, int64_t q_head, int heads, void* q_out,
+                                    int64_t o_token, int64_t o_head, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                                    int64_t v_token, int64_t v_head, pp_dtype_t dtype, int tokens, const int64_t* slots,
+                                    const int32_t* positions, const float* inv_freq, int pairs, int interleaved, void* cuda_stream) {
+    using namespace pp;
+    if (const pp_status_t st = check_cache(cache)) return st;
+    const pp_paged_cache_t& c = *cache;
+    if (!is_float(dtype) || (c.dtype != dtype && !is_8bit(c.dtype))) return PP_ERR_UNSUPPORTED;
+    if (tokens < 0 || heads < 0 || heads > (1 << 20) || pairs < 0 || pairs > c.head_dim / 2 || (heads > 0) != (q != nullptr) || (q != nullptr) != (q_out != nullptr))
+        return PP_ERR_INVALID_ARG;
+    if ((pairs > 0) != (positions != nullptr) || (pairs > 0) != (inv_freq != nullptr)) return PP_ERR_INVALID_ARG;
+    if (tokens == 0) return PP_OK;
+    if (!k || !v || !slots) return PP_ERR_INVALID_ARG;
+    const int tb = type_bytes(dtype), dim = c.head_dim;
+    if (!aligned_to(q, tb) || !aligned_to(q_out, tb) || !aligned_to(k, tb) || !aligned_to(v, tb) || !aligned_to(slots, 8) || !aligned_to(positions, 4) ||
+        !aligned_to(inv_freq, 4)) return PP_ERR_INVALID_ARG;
+    const int64_t most = (int64_t)1 << 58;                   // no sum of offsets passes 63 bits
+    for (const int64_t s : {q_token, o_token, k_token, v_token})
+        if (s < 0 || s > most / tokens) return PP_ERR_INVALID_ARG;
+    for (const int64_t s : {q_head, o_head, k_head, v_head})
+        if (s < 0 || s > most >> 20) return PP_ERR_INVALID_ARG;
+    const auto span = [&](int64_t token, int64_t head, int n) { return (((int64_t)tokens - 1) * token + ((int64_t)n - 1) * head + dim) * tb; };
+    if (q) {
+        if (!rows_apart(1, 0, tokens, o_token, heads, o_head, dim)) return PP_ERR_INVALID_ARG;
+        const bool in_place = q == q_out && q_token == o_token && q_head == o_head;
+        // in place, q may be a part of rows that hold k and v too, as a projection's rows do: then no row of it may reach into theirs
+        if (!in_place && spans_meet(q, span(q_token, q_head, heads), q_out, span(o_token, o_head, heads))) return PP_ERR_INVALID_ARG;
+        const int64_t row = (((int64_t)heads - 1) * o_head + dim) * tb, other_k = (((int64_t)c.kv_heads - 1) * k_head + dim) * tb,
+                      other_v = (((int64_t)c.kv_heads - 1) * v_head + dim) * tb;
+        if (share_bytes(q_out, row, o_token * tb, tokens, k, other_k, k_token * tb, tokens) ||
+            share_bytes(q_out, row, o_token * tb, tokens, v, other_v, v_token * tb, tokens)) return PP_ERR_INVALID_ARG;
+    }
+    AppendArgs a{q, k, v, q_out, c.k, c.v, c.k_scales, c.v_scales, slots, positions, inv_freq,
+                 q_token, q_head, o_token, o_head, k_token, k_head, v_token, v_head,
+                 c.k_page, c.k_token, c.k_head, c.v_page, c.v_token, c.v_head, (int64_t)c.pages * c.page_size,
+                 heads, c.kv_heads, dim, c.page_size, pairs, interleaved != 0, c.dtype, 8};
+    while (a.lanes * 8 < dim) a.lanes *= 2;
+    // eight elements to an access where every row starts on one, and pairs of halves lie whole lanes apart
+    const auto wide = [&](const void* p, int64_t token, int64_t head, int n) { return !p || row_alignment(p, 1, 0, tokens, token, n, head, tb) == 16; };
+    const bool vec = dim % 8 == 0 && (interleaved || pairs % 8 == 0) && wide(q, q_token, q_head, heads) && wide(q_out, o_token, o_head, heads) &&
+                     wide(k, k_token, k_head, c.kv_heads) && wide(v, v_token, v_head, c.kv_heads) && cache_alignment(c) >= (is_8bit(c.dtype) ? 8 : 16);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = dtype == PP_F32 ? launch_append<float>(a, vec, tokens, s)
+                        : dtype == PP_F16 ? launch_append<__half>(a, vec, tokens, s) : launch_append<__nv_bfloat16>(a, vec, tokens, s);
+    return status_of(e);
+}

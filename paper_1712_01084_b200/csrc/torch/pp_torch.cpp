@@ -12,6 +12,8 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+
 #include "pp.h"
 
 namespace {
@@ -19,6 +21,10 @@ namespace {
 decltype(&pp_rmsnorm_q8) g_rmsnorm_q8;
 decltype(&pp_q4_forward) g_q4_forward;
 decltype(&pp_moe_forward) g_moe_forward;
+decltype(&pp_paged_plan) g_paged_plan;
+decltype(&pp_kv_append) g_kv_append;
+decltype(&pp_paged_attention_workspace) g_paged_attention_workspace;
+decltype(&pp_paged_attention) g_paged_attention;
 
 // A Python exception that is already set.
 struct Raised {};
@@ -259,12 +265,174 @@ PyObject* moe_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// (address of pp_rmsnorm_q8, of pp_q4_forward, of pp_moe_forward)
+// A CUDA vector of whole numbers, contiguous, with this many entries (-1: any).
+const at::Tensor& whole(PyObject* o, const char* name, at::ScalarType t, int64_t n, int device) {
+    const at::Tensor& x = tensor(o, name);
+    if (!x.is_cuda() || x.get_device() != device || x.dim() != 1 || !x.is_contiguous() || (n >= 0 && x.numel() != n) || x.numel() > INT32_MAX)
+        raise(PyExc_ValueError, n >= 0 ? "%s must be a contiguous CUDA vector on device %d with %lld entries" : "%s must be a contiguous CUDA vector on device %d",
+              name, device, (long long)n);
+    if (x.scalar_type() != t) raise(PyExc_TypeError, "%s must be %s", name, t == at::kLong ? "int64" : "int32");
+    return x;
+}
+// A block table: int32 [requests][width], rows contiguous.
+const at::Tensor& table_of(PyObject* o, int64_t requests, int device) {
+    const at::Tensor& x = tensor(o, "table");
+    if (!x.is_cuda() || x.get_device() != device || x.dim() != 2 || x.size(0) != requests || x.size(1) < 1 || x.size(1) > INT32_MAX ||
+        (x.size(1) > 1 && x.stride(1) != 1) || (requests > 1 && x.stride(0) < x.size(1)))
+        raise(PyExc_ValueError, "table must be a CUDA tensor [%lld][width] with contiguous rows, on device %d", (long long)requests, device);
+    if (x.scalar_type() != at::kInt) raise(PyExc_TypeError, "table must be int32");
+    return x;
+}
+// Heads of tokens: [tokens][heads][width], the last axis contiguous, any distances else.
+struct Heads { const at::Tensor* x; int64_t tokens, heads, token, head; };
+Heads heads_of(PyObject* o, const char* name, int64_t width, int device) {
+    const at::Tensor& x = tensor(o, name);
+    if (!x.is_cuda() || x.get_device() != device || x.dim() != 3 || x.size(2) != width || (width > 1 && x.stride(2) != 1) || x.size(0) > INT32_MAX || x.size(1) > INT32_MAX)
+        raise(PyExc_ValueError, "%s must be a CUDA tensor [tokens][heads][%lld] with contiguous heads, on device %d", name, (long long)width, device);
+    return {&x, x.size(0), x.size(1), x.size(0) > 1 ? x.stride(0) : 0, x.size(1) > 1 ? x.stride(1) : 0};
+}
+
+// (lengths, added, table, free_pages, taken, page_size, slots, positions, starts, lengths_out, taken_out, stream) -> None, or the status
+PyObject* paged_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 12, [&]() -> PyObject* {
+        const at::Tensor& first = tensor(a[0], "lengths");
+        const int device = first.is_cuda() ? (int)first.get_device() : -1;
+        const at::Tensor& lengths = whole(a[0], "lengths", at::kInt, -1, device);
+        const int64_t requests = lengths.numel();
+        const at::Tensor &added = whole(a[1], "added", at::kInt, requests, device), &table = table_of(a[2], requests, device);
+        const at::Tensor &pages = whole(a[3], "free_pages", at::kInt, -1, device), &taken = whole(a[4], "taken", at::kInt, 1, device);
+        const int page_size = number(a[5]);
+        const at::Tensor& slots = whole(a[6], "slots", at::kLong, -1, device);
+        const at::Tensor &positions = whole(a[7], "positions", at::kInt, slots.numel(), device), &starts = whole(a[8], "starts", at::kInt, requests + 1, device);
+        const at::Tensor &lengths_out = whole(a[9], "lengths_out", at::kInt, requests, device), &taken_out = whole(a[10], "taken_out", at::kInt, 1, device);
+        const Enqueue on(a[11], device);
+        const auto ints = [](const at::Tensor& t) { return static_cast<int32_t*>(t.data_ptr()); };
+        const pp_status_t st = g_paged_plan(ints(lengths), ints(added), ints(table), requests > 1 ? table.stride(0) : table.size(1), (int)table.size(1),
+                                            ints(pages), (int)pages.numel(), ints(taken), (int)requests, page_size, (int)slots.numel(),
+                                            static_cast<int64_t*>(slots.data_ptr()), ints(positions), ints(starts), ints(lengths_out), ints(taken_out), on.stream);
+        return st != PP_OK ? PyLong_FromLong(st) : keep(Py_None);
+    });
+}
+
+// (cache, head_dim, kv_heads, device, k, v, slots, q, positions, inv_freq, interleaved, out, stream) -> q turned or None, or the status
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 13, [&]() -> PyObject* {
+        const pp_paged_cache_t* cache = static_cast<const pp_paged_cache_t*>(address(a[0]));
+        const int64_t dim = number(a[1]), kv_heads = number(a[2]);
+        const int device = number(a[3]);
+        const Heads k = heads_of(a[4], "k", dim, device), v = heads_of(a[5], "v", dim, device);
+        const at::ScalarType t = k.x->scalar_type();
+        const pp_dtype_t dt = type_of(t, "k");
+        if (v.x->scalar_type() != t) raise(PyExc_TypeError, "v must have k's type");
+        if (k.heads != kv_heads || v.heads != kv_heads || v.tokens != k.tokens)
+            raise(PyExc_ValueError, "k and v must be [tokens][%lld][%lld]", (long long)kv_heads, (long long)dim);
+        const at::Tensor& slots = whole(a[6], "slots", at::kLong, k.tokens, device);
+        if ((a[8] == Py_None) != (a[9] == Py_None)) raise(PyExc_ValueError, "positions and inv_freq go together");
+        const int32_t* positions = nullptr;
+        const float* inv_freq = nullptr;
+        int64_t pairs = 0;
+        if (a[8] != Py_None) {
+            positions = static_cast<const int32_t*>(whole(a[8], "positions", at::kInt, k.tokens, device).const_data_ptr());
+            const at::Tensor& f = tensor(a[9], "inv_freq");
+            pairs = f.numel();
+            if (!f.is_cuda() || f.get_device() != device || f.dim() != 1 || !f.is_contiguous() || f.scalar_type() != at::kFloat || pairs < 1 || pairs > dim / 2)
+                raise(PyExc_ValueError, "inv_freq must be a contiguous float32 CUDA vector of 1 to %lld entries on device %d", (long long)(dim / 2), device);
+            inv_freq = static_cast<const float*>(f.const_data_ptr());
+        }
+        const bool interleaved = truth(a[10]);
+        const Enqueue on(a[12], device);
+        Heads q{nullptr, 0, 0, 0, 0}, o{nullptr, 0, 0, 0, 0};
+        at::Tensor out;
+        if (a[7] != Py_None) {
+            q = heads_of(a[7], "q", dim, device);
+            if (q.x->scalar_type() != t) raise(PyExc_TypeError, "q must have k's type");
+            if (q.tokens != k.tokens) raise(PyExc_ValueError, "q must have %lld tokens", (long long)k.tokens);
+            if (q.heads < 1) raise(PyExc_ValueError, "q must have heads");
+            if (a[11] != Py_None) {
+                o = heads_of(a[11], "out", dim, device);
+                if (o.x->scalar_type() != t || o.tokens != q.tokens || o.heads != q.heads) raise(PyExc_ValueError, "out must have q's shape and type");
+            } else {
+                out = fresh({q.tokens, q.heads, dim}, t, device);
+                o = {&out, q.tokens, q.heads, q.heads * dim, dim};
+            }
+        } else if (a[11] != Py_None) {
+            raise(PyExc_ValueError, "out without q");
+        }
+        const auto start = [](const Heads& h) -> void* { return h.x ? h.x->data_ptr() : nullptr; };
+        if (k.tokens > 0) {
+            const pp_status_t st = g_kv_append(cache, start(q), q.token, q.head, (int)q.heads, start(o), o.token, o.head, start(k), k.token, k.head, start(v),
+                                               v.token, v.head, dt, (int)k.tokens, static_cast<const int64_t*>(slots.const_data_ptr()), positions, inv_freq,
+                                               (int)pairs, interleaved, on.stream);
+            if (st != PP_OK) return PyLong_FromLong(st);
+        }
+        return a[11] != Py_None ? keep(a[11]) : out.defined() ? THPVariable_Wrap(out) : keep(Py_None);
+    });
+}
+
+// (cache, head_dim, kv_heads, device, q, table, lengths, scale, window, out, lse, stream) -> out or (out, lse), or the status
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 12, [&]() -> PyObject* {
+        const pp_paged_cache_t* cache = static_cast<const pp_paged_cache_t*>(address(a[0]));
+        const int64_t dim = number(a[1]), kv_heads = number(a[2]);
+        const int device = number(a[3]);
+        const Heads q = heads_of(a[4], "q", dim, device);
+        const at::ScalarType t = q.x->scalar_type();
+        const pp_dtype_t dt = type_of(t, "q");
+        if (q.heads < 1 || q.heads % kv_heads) raise(PyExc_ValueError, "q must have a multiple of %lld heads", (long long)kv_heads);
+        const at::Tensor &table = table_of(a[5], q.tokens, device), &lengths = whole(a[6], "lengths", at::kInt, q.tokens, device);
+        double scale = 1.0 / std::sqrt((double)dim);
+        if (a[7] != Py_None) {
+            scale = PyFloat_AsDouble(a[7]);
+            if (scale == -1.0 && PyErr_Occurred()) throw Raised{};
+        }
+        const int window = number(a[8]);
+        const bool want_lse = truth(a[10]);
+        const Enqueue on(a[11], device);
+        at::Tensor out;
+        if (a[9] != Py_None) {
+            out = tensor(a[9], "out");
+            if (!out.is_cuda() || out.get_device() != device || !out.is_contiguous() || out.sizes() != q.x->sizes() || out.scalar_type() != t)
+                raise(PyExc_ValueError, "out must be contiguous, with q's shape and type");
+        } else {
+            out = fresh({q.tokens, q.heads, dim}, t, device);
+        }
+        const at::Tensor lse = want_lse ? fresh({q.tokens, q.heads}, at::kFloat, device) : at::Tensor();
+        if (q.tokens > 0) {
+            int64_t bytes = 0;
+            pp_status_t st = g_paged_attention_workspace(cache, dt, (int)q.tokens, (int)q.heads, (int)table.size(1), window, &bytes);
+            if (st != PP_OK) return PyLong_FromLong(st);
+            // of this call alone: its memory goes back to the stream's pool, where later work of this stream may have it
+            const at::Tensor space = bytes ? fresh({bytes}, at::kByte, device) : at::Tensor();
+            st = g_paged_attention(cache, q.x->data_ptr(), q.token, q.head, dt, static_cast<const int32_t*>(table.const_data_ptr()),
+                                   q.tokens > 1 ? table.stride(0) : table.size(1), (int)table.size(1), static_cast<const int32_t*>(lengths.const_data_ptr()),
+                                   (int)q.tokens, (int)q.heads, (float)scale, window, out.data_ptr(), want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr,
+                                   bytes ? space.data_ptr() : nullptr, bytes, on.stream);
+            if (st != PP_OK) return PyLong_FromLong(st);
+        }
+        PyObject* first = a[9] != Py_None ? keep(a[9]) : THPVariable_Wrap(out);
+        if (!want_lse || !first) return first;
+        PyObject* all = PyTuple_New(2);
+        if (!all) {
+            Py_DECREF(first);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(all, 0, first);
+        PyTuple_SET_ITEM(all, 1, THPVariable_Wrap(lse));
+        return all;
+    });
+}
+
+// The addresses of pp_rmsnorm_q8, pp_q4_forward, pp_moe_forward, pp_paged_plan, pp_kv_append, pp_paged_attention_workspace,
+// pp_paged_attention
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 3, [&]() -> PyObject* {
+    return guarded(n, 7, [&]() -> PyObject* {
         g_rmsnorm_q8 = reinterpret_cast<decltype(g_rmsnorm_q8)>(address(a[0]));
         g_q4_forward = reinterpret_cast<decltype(g_q4_forward)>(address(a[1]));
         g_moe_forward = reinterpret_cast<decltype(g_moe_forward)>(address(a[2]));
+        g_paged_plan = reinterpret_cast<decltype(g_paged_plan)>(address(a[3]));
+        g_kv_append = reinterpret_cast<decltype(g_kv_append)>(address(a[4]));
+        g_paged_attention_workspace = reinterpret_cast<decltype(g_paged_attention_workspace)>(address(a[5]));
+        g_paged_attention = reinterpret_cast<decltype(g_paged_attention)>(address(a[6]));
         return keep(Py_None);
     });
 }
@@ -274,6 +442,9 @@ PyMethodDef methods[] = {
     {"rmsnorm_q8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rmsnorm_q8)), METH_FASTCALL, nullptr},
     {"q4_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(q4_forward)), METH_FASTCALL, nullptr},
     {"moe_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(moe_forward)), METH_FASTCALL, nullptr},
+    {"paged_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_plan)), METH_FASTCALL, nullptr},
+    {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_append)), METH_FASTCALL, nullptr},
+    {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attention)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pp_torch", "Decoder operators on PyTorch tensors.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
