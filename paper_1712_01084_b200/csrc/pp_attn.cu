@@ -39,18 +39,23 @@ struct AttnArgs {
     int64_t q_row, q_head, k_page, k_token, k_head, v_page, v_token, v_head, ld_table;
     Divisor page;
     int pages, page_size, batch, capacity, window, heads, kv_heads, group, chunk, n_chunks, dim, granule, q_type, type;
+    bool whole_tiles;                                        // pages are a whole number of tiles long
     float scale;                                             // times log2 e
 };
 
+// The workspace: a note for each CTA (four ints), then two partial results for each.
+__host__ __device__ inline int64_t notes_floats(int64_t ctas) { return 4 * ctas; }
 // Floats of a partial result: m and l of each head of the chunk, then the sums.
 __host__ __device__ inline int64_t part_floats(int chunk, int dim) { return (int64_t)chunk * (dim + 2); }
 
 __device__ __forceinline__ int first_position(const AttnArgs& a, int length) { return a.window > 0 ? max(0, length - a.window) : 0; }
+// Units start at a whole tile: where pages are whole tiles long, no tile then crosses from one page into another.
+__device__ __forceinline__ int first_tile(const AttnArgs& a, int length) { return first_position(a, length) & ~(kTile - 1); }
 __device__ __forceinline__ int length_of(const AttnArgs& a, int r) { return min(max(a.lengths[r], 0), a.capacity); }
 // Units of one head of a request: one at least, which writes the output of a request without positions.
 __device__ __forceinline__ int units_of(const AttnArgs& a, int r) {
     const int n = length_of(a, r);
-    return max(1, (n - first_position(a, n) + kUnit - 1) / kUnit);
+    return max(1, (n - first_tile(a, n) + kUnit - 1) / kUnit);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -60,10 +65,19 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-__device__ __forceinline__ float load_q(const AttnArgs& a, int64_t at) {
-    if (a.q_type == PP_F32) return static_cast<const float*>(a.q)[at];
-    if (a.q_type == PP_F16) return __half2float(static_cast<const __half*>(a.q)[at]);
-    return __bfloat162float(static_cast<const __nv_bfloat16*>(a.q)[at]);
+// The q rows of a chunk as floats [heads][DT] in shared memory, zeros where there is no head or dimension.
+template <int HEADS, int DT, typename T> __device__ __forceinline__ void stage_q(const AttnArgs& a, const T* q, int n_heads, float* to) {
+#pragma unroll 8
+    for (int i = threadIdx.x; i < HEADS * DT; i += kThreads) {
+        const int head = i / DT, d = i - head * DT;
+        to[i] = head < n_heads && d < a.dim ? to_float(q[head * a.q_head + d]) : 0.0f;
+    }
+}
+template <int HEADS, int DT> __device__ __forceinline__ void stage_q(const AttnArgs& a, int r, int head0, int n_heads, float* to) {
+    const int64_t at = r * a.q_row + head0 * a.q_head;
+    if (a.q_type == PP_BF16) stage_q<HEADS, DT>(a, static_cast<const __nv_bfloat16*>(a.q) + at, n_heads, to);
+    else if (a.q_type == PP_F16) stage_q<HEADS, DT>(a, static_cast<const __half*>(a.q) + at, n_heads, to);
+    else stage_q<HEADS, DT>(a, static_cast<const float*>(a.q) + at, n_heads, to);
 }
 __device__ __forceinline__ void store_out(const AttnArgs& a, int64_t at, float v) {
     if (a.q_type == PP_F32) static_cast<float*>(a.out)[at] = v;
@@ -83,13 +97,19 @@ struct Reader {
     const char *k, *v;
     const float *ks, *vs;
     const int32_t* row;                                      // of the table
-    int end, entry;                                          // entry: of the tile to be asked for next, for position lane & 15
+    int low, end, entry;                                     // positions low .. end - 1; entry: of the next tile, for position lane & 15
 };
 
-// The table entry of this lane's position in the tile at `at`, -1 past the end.
+// The table entry of this lane's position in the tile at `at`, -1 for positions that are not asked for.  In whole tiles all
+// lanes look up the first position's.
 __device__ __forceinline__ int entry_of(const AttnArgs& a, const Reader& r, int at) {
-    const int p = at + (threadIdx.x & 15);
-    return p < r.end ? r.row[a.page.of((uint32_t)p)] : -1;
+    const int p = a.whole_tiles ? at : at + (threadIdx.x & 15);
+    return (a.whole_tiles || p >= r.low) && p < r.end ? r.row[a.page.of((uint32_t)p)] : -1;
+}
+// Bits of the tile's positions between low and end.
+__device__ __forceinline__ uint32_t positions_of(const Reader& r, int at) {
+    const int from = max(0, r.low - at), to = min(kTile, r.end - at);
+    return ((1u << to) - 1u) & ~((1u << from) - 1u);
 }
 
 // Asks for the tile at `at`: 16 rows of keys, of values, and the scales of both.  Returns which rows are there (a bit each).
@@ -98,7 +118,38 @@ template <int ES, int CHUNKS, int PITCH, bool Q8>
 __device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, int at, uint32_t stage) {
     constexpr int kTileBytes = kTile * PITCH;
     const int lane = threadIdx.x & 31, p = at + (lane & 15);
-    const int entry = r.entry;
+    if (a.whole_tiles && a.granule == 16) {                  // one page: rows a fixed distance apart
+        constexpr int kLanes = CHUNKS > 16 ? 32 : CHUNKS > 8 ? 16 : CHUNKS > 4 ? 8 : 4, kRows = 32 / kLanes;
+        const bool is_page = (uint32_t)r.entry < (uint32_t)a.pages;
+        const int entry = is_page ? r.entry : 0, place = at - (int)a.page.of((uint32_t)at) * a.page_size;
+        const uint32_t bits = is_page ? positions_of(r, at) : 0;
+        r.entry = entry_of(a, r, at + kUnit);
+        const int row = lane / kLanes;
+        const char* k = r.k + (int64_t)entry * a.k_page + (int64_t)(place + row) * a.k_token;
+        const char* v = r.v + (int64_t)entry * a.v_page + (int64_t)(place + row) * a.v_token;
+#pragma unroll
+        for (int i = 0; i < kTile / kRows; ++i) {
+            const bool has = (bits >> (i * kRows + row)) & 1;
+#pragma unroll
+            for (int c0 = 0; c0 < CHUNKS; c0 += kLanes) {
+                const int c = c0 + (lane & (kLanes - 1));
+                if (CHUNKS % kLanes && c >= CHUNKS) continue;
+                const bool own = c * 16 < a.dim * ES;
+                const uint32_t dst = stage + (i * kRows + row) * PITCH + c * 16;
+                copy_async<16>(dst, k + (own ? c * 16 : 0), own && has);
+                copy_async<16>(dst + kTileBytes, v + (own ? c * 16 : 0), own && has);
+            }
+            k += kRows * a.k_token;
+            v += kRows * a.v_token;
+        }
+        if constexpr (Q8) {
+            const bool in = (bits >> (lane & 15)) & 1;
+            const int64_t token = (int64_t)entry * a.page_size + place + (in ? lane & 15 : 0);
+            copy_async<4>(stage + 2 * kTileBytes + lane * 4, (lane < 16 ? r.ks : r.vs) + token * a.kv_heads, in);
+        }
+        return bits;
+    }
+    const int entry = a.whole_tiles && (p < r.low || p >= r.end) ? -1 : r.entry;
     const bool there = (uint32_t)entry < (uint32_t)a.pages;  // -1 is none, and a number that is no page of the cache neither
     const uint32_t bits = __ballot_sync(0xffffffffu, there) & 0xffffu;
     r.entry = entry_of(a, r, at + kUnit);
@@ -172,16 +223,16 @@ template <bool BF16> __device__ __forceinline__ float2 unpack2(uint32_t v) {
     if constexpr (BF16) return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v));
     else return __half22float2(*reinterpret_cast<const __half2*>(&v));
 }
-// Two 8-bit codes in the low bytes as two f16 numbers, exactly.
-template <int KIND> __device__ __forceinline__ uint32_t widen(uint32_t two) {
+// Four 8-bit codes as two registers of two f16 numbers, exactly: bytes 0 and 1, bytes 2 and 3.
+template <int KIND> __device__ __forceinline__ void widen(uint32_t four, uint32_t& low, uint32_t& high) {
     if constexpr (KIND == kE4m3) {
-        uint32_t d;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((uint16_t)two));
-        return d;
+        asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h;}" : "=r"(low), "=r"(high) : "r"(four));
     } else {                                                 // 0x6400 + u is 1024 + u; u = code + 128
-        const uint32_t u = __byte_perm(two ^ 0x8080u, 0x64646464u, 0x4140);
-        const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&u), __float2half2_rn(1152.0f));
-        return *reinterpret_cast<const uint32_t*>(&v);
+        const uint32_t u = four ^ 0x80808080u, x = __byte_perm(u, 0x64646464u, 0x4140), y = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 bias = __float2half2_rn(1152.0f);
+        const __half2 p = __hsub2(*reinterpret_cast<const __half2*>(&x), bias), q = __hsub2(*reinterpret_cast<const __half2*>(&y), bias);
+        low = *reinterpret_cast<const uint32_t*>(&p);
+        high = *reinterpret_cast<const uint32_t*>(&q);
     }
 }
 
@@ -192,32 +243,31 @@ template <int DT, int NT, int KIND> struct MmaCore {
     static constexpr int kEs = kQ8 ? 1 : 2, kChunks = DT * kEs / 16, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
     static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = kStage <= 5120 ? 4 : 3;
     static constexpr int kHeads = 8 * NT, kMergePitch = DT + 4;
-    static constexpr int kQFloats = 0;
+    static constexpr int kQFloats = kHeads * DT;
     // p is at most 2^kLift: f16 numbers below 2^-24 are lost, and a p can be that small beside the largest one
     static constexpr float kLift = kIsBf16 ? 0.0f : 14.0f;
 
     uint32_t q[DT / 16][NT][2];
     float acc[DT / 16][NT][4], m[NT][2], l[NT][2], f[NT][2], vm;
 
-    __device__ __forceinline__ void begin(const AttnArgs& a, int r, int head0, int n_heads, float*) {
+    // from q in shared memory
+    __device__ __forceinline__ void begin(const AttnArgs& a, const float* rows) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
         const bool split = kQ8 && a.q_type == PP_F32;
         float factor[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const bool lows = split && nt == 1;
-            const int head = split ? g : nt * 8 + g;
-            const int64_t row = r * a.q_row + (int64_t)(head0 + head) * a.q_head;
-            const bool live = head < n_heads;
-            const auto element = [&](int d) { return live && d < a.dim ? load_q(a, row + d) : 0.0f; };
+            const float* row = rows + (split ? g : nt * 8 + g) * DT;
             float down = 1.0f;                               // a power of two that brings the head's largest below 2: f16 ends at 65504
             factor[nt] = a.scale;
             if constexpr (kQ8) {
                 float most = 0.0f;
 #pragma unroll
-                for (int j = 0; j < DT / 16; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(element(16 * j + 4 * t + i)));
+                for (int j = 0; j < DT / 16; ++j) {
+                    const float4 x = *reinterpret_cast<const float4*>(row + 16 * j + 4 * t);
+                    most = fmaxf(fmaxf(fmaxf(most, fabsf(x.x)), fmaxf(fabsf(x.y), fabsf(x.z))), fabsf(x.w));
+                }
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
                 if (most > 0.0f && most < INFINITY) {
@@ -231,7 +281,7 @@ template <int DT, int NT, int KIND> struct MmaCore {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int d = kQ8 ? 16 * j + 4 * t + 2 * i : 16 * j + 2 * t + 8 * i;   // codes: four neighbours to a lane, as they lie in its bytes
-                    const float x = element(d) * down, y = element(d + 1) * down;
+                    const float x = row[d] * down, y = row[d + 1] * down;
                     q[j][nt][i] = pack2<kIsBf16>(x, y);
                     if (lows) {
                         const float2 high = unpack2<kIsBf16>(q[j][nt][i]);
@@ -268,7 +318,9 @@ template <int DT, int NT, int KIND> struct MmaCore {
                 load_matrices(k, rows + c * 16);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const uint32_t a0 = widen<KIND>(k[2 * i]), a2 = widen<KIND>(k[2 * i] >> 16), a1 = widen<KIND>(k[2 * i + 1]), a3 = widen<KIND>(k[2 * i + 1] >> 16);
+                    uint32_t a0, a1, a2, a3;
+                    widen<KIND>(k[2 * i], a0, a2);
+                    widen<KIND>(k[2 * i + 1], a1, a3);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) mma<kIsBf16>(s[nt], a0, a1, a2, a3, q[c + i][nt][0], q[c + i][nt][1]);
                 }
@@ -370,8 +422,9 @@ template <int DT, int NT, int KIND> struct MmaCore {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     // bytes: dims 2g, 2g + 1 of position 2t, then of 2t + 1; row g of the product is dim 2g, row g + 8 dim 2g + 1
-                    const uint32_t x = __byte_perm(v[2 * i], 0, 0x3120), y = __byte_perm(v[2 * i + 1], 0, 0x3120);
-                    const uint32_t a0 = widen<KIND>(x), a1 = widen<KIND>(x >> 16), a2 = widen<KIND>(y), a3 = widen<KIND>(y >> 16);
+                    uint32_t a0, a1, a2, a3;
+                    widen<KIND>(__byte_perm(v[2 * i], 0, 0x3120), a0, a1);
+                    widen<KIND>(__byte_perm(v[2 * i + 1], 0, 0x3120), a2, a3);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         mma<kIsBf16>(acc[c + i][nt], a0, a1, a2, a3, high[nt][0], high[nt][1]);
@@ -442,12 +495,7 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
 
     float acc[DT / 32][HN], m[HN], l[HN];
 
-    // q of the chunk, in shared memory for all warps; the caller's barrier follows
-    __device__ __forceinline__ void begin(const AttnArgs& a, int r, int head0, int n_heads, float* q) {
-        for (int i = threadIdx.x; i < HN * DT; i += kThreads) {
-            const int head = i / DT, d = i % DT;
-            q[i] = head < n_heads && d < a.dim ? load_q(a, r * a.q_row + (int64_t)(head0 + head) * a.q_head + d) * a.scale : 0.0f;
-        }
+    __device__ __forceinline__ void begin(const AttnArgs&, const float*) {
 #pragma unroll
         for (int h = 0; h < HN; ++h) {
             m[h] = -INFINITY;
@@ -460,7 +508,7 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
     // ASYNC false: the tile at `at`, element by element
     __device__ static uint32_t fetch(const AttnArgs& a, Reader& r, int at, float* stage) {
         const int lane = threadIdx.x & 31, p = at + (lane & 15);
-        const int entry = r.entry;
+        const int entry = a.whole_tiles && (p < r.low || p >= r.end) ? -1 : r.entry;
         const bool there = (uint32_t)entry < (uint32_t)a.pages;
         const uint32_t bits = __ballot_sync(0xffffffffu, there) & 0xffffu;
         r.entry = entry_of(a, r, at + kUnit);
@@ -518,7 +566,7 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
         bool moved = false;
 #pragma unroll
         for (int h = 0; h < HN; ++h) {
-            s[h] += __shfl_xor_sync(0xffffffffu, s[h], 16);
+            s[h] = (s[h] + __shfl_xor_sync(0xffffffffu, s[h], 16)) * a.scale;
             if (!there) s[h] = -INFINITY;
             float top = s[h];
 #pragma unroll
@@ -576,33 +624,47 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
 
 // ---------------------------------------------------------------------------------------------- one kernel for both
 // Exclusive sums of the requests' units over the threads (a run of requests each), and the sum of all.
-__device__ __forceinline__ int64_t sum_before(int64_t mine, int64_t* warp_sums, int64_t& all) {
+__device__ __forceinline__ int sum_before(int mine, int* warp_sums, int& all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t up = mine;
+    int up = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t x = __shfl_up_sync(0xffffffffu, up, o);
+        const int x = __shfl_up_sync(0xffffffffu, up, o);
         if (lane >= o) up += x;
     }
     if (lane == 31) warp_sums[warp] = up;
     __syncthreads();
-    int64_t before = up - mine;
+    int before = up - mine;
     all = 0;
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) {
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
         if (w < warp) before += warp_sums[w];
         all += warp_sums[w];
     }
     return before;
 }
 
-// Unit at which CTA c of n starts, of u units, and the CTA that unit x belongs to.
-__device__ __forceinline__ int64_t part_start(int64_t c, int64_t n, int64_t u) { return c * u / n; }
-__device__ __forceinline__ int64_t part_of(int64_t x, int64_t n, int64_t u) { return ((x + 1) * n - 1) / u; }
+// u units cut into n parts, the first u % n of them one longer than the others: where part c starts, and the part of unit x.
+struct Cut {
+    int each, longer;
+    __device__ __forceinline__ Cut(int u, int n) : each(u / n), longer(u - u / n * n) {}
+    __device__ __forceinline__ int start(int c) const { return c * each + min(c, longer); }
+    __device__ __forceinline__ int of(int x) const {
+        const int edge = longer * (each + 1);
+        return x < edge ? x / (each + 1) : longer + (x - edge) / each;
+    }
+};
+
+// A head (chunk) whose units several CTAs share, noted by the first of them, which is the note's number.
+struct Note {
+    int last;                                                // the last of them; -1: no such head
+    int row, n_heads;                                        // first row of out, rows
+    int second;                                              // the first one's part is the second of its two
+};
 
 template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnArgs a) {
     extern __shared__ __align__(128) unsigned char ring[];
-    __shared__ int64_t warp_sums[kWarps], found_base;
-    __shared__ int found;
+    __shared__ int warp_sums[kWarps], found_base, found;
     __shared__ float warp_m[kWarps][Core::kHeads], warp_l[kWarps][Core::kHeads], factors[kWarps][Core::kHeads], all_m[Core::kHeads], all_l[Core::kHeads];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_release();
@@ -610,18 +672,20 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
 
     const int per_request = a.kv_heads * a.n_chunks;
     const int each = (a.batch + kThreads - 1) / kThreads, r0 = min(tid * each, a.batch), r1 = min(r0 + each, a.batch);
-    int64_t mine = 0, all;
-    for (int r = r0; r < r1; ++r) mine += (int64_t)units_of(a, r) * per_request;
-    const int64_t before = sum_before(mine, warp_sums, all);
-    const int64_t n = min((int64_t)gridDim.x, all);
-    if (blockIdx.x >= n) return;
-    int64_t u = part_start(blockIdx.x, n, all);
-    const int64_t begin = u, end = part_start(blockIdx.x + 1, n, all);
+    int mine = 0, all;
+    for (int r = r0; r < r1; ++r) mine += units_of(a, r) * per_request;
+    const int before = sum_before(mine, warp_sums, all);
+    const int n = min((int)gridDim.x, all), c = blockIdx.x;
+    Note* note = a.ws ? reinterpret_cast<Note*>(a.ws) + c : nullptr;
+    if (note && tid == 0) note->last = -1;
+    if (c >= n) return;
+    const Cut cut(all, n);
+    int u = cut.start(c);
+    const int begin = u, end = cut.start(c + 1);
     if (u >= before && u < before + mine) {
-        int64_t base = before;
-        int r = r0;
+        int base = before, r = r0;
         for (;; ++r) {
-            const int64_t units = (int64_t)units_of(a, r) * per_request;
+            const int units = units_of(a, r) * per_request;
             if (u < base + units) break;
             base += units;
         }
@@ -629,8 +693,7 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
         found_base = base;
     }
     __syncthreads();
-    int r = found;
-    int64_t base = found_base;
+    int r = found, base = found_base;
 
     unsigned char* own = ring + warp * Core::kStages * Core::kStage;
     float* q = reinterpret_cast<float*>(ring + kWarps * Core::kStages * Core::kStage);
@@ -638,9 +701,9 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
     Core core;
     while (u < end) {
         const int units = units_of(a, r);
-        const int unit = (int)(u - base), hc = unit / units, t0 = unit - hc * units;
-        const int t1 = (int)min((int64_t)units, t0 + (end - u));
-        const int length = length_of(a, r), low = first_position(a, length);
+        const int unit = u - base, hc = unit / units, t0 = unit - hc * units;
+        const int t1 = min(units, t0 + (end - u));
+        const int length = length_of(a, r), low = first_tile(a, length);
         const int kv = hc / a.n_chunks, head_in = (hc - kv * a.n_chunks) * a.chunk, n_heads = min(a.chunk, a.group - head_in);
         const int head0 = kv * a.group + head_in;
 
@@ -650,6 +713,7 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
         reader.ks = a.ks + kv;
         reader.vs = a.vs + kv;
         reader.row = a.table + r * a.ld_table;
+        reader.low = first_position(a, length);
         reader.end = min(length, low + t1 * kUnit);
         int ask_at = low + t0 * kUnit + warp * kTile;
         reader.entry = entry_of(a, reader, ask_at);
@@ -670,8 +734,9 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
         };
 #pragma unroll 1
         for (int i = 0; i < Core::kStages - 1; ++i) request();
-        core.begin(a, r, head0, n_heads, q);
-        if (Core::kQFloats) __syncthreads();
+        stage_q<Core::kHeads, Core::kQFloats / Core::kHeads>(a, r, head0, n_heads, q);
+        __syncthreads();
+        core.begin(a, q);
         int at = 0;
 #pragma unroll 1
         for (int i = 0; i < tiles; ++i) {
@@ -713,7 +778,8 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
         core.sums(a, factors[warp], merge + warp * Core::kHeads * Core::kMergePitch);
         __syncthreads();
         const bool whole = t0 == 0 && t1 == units;
-        float* part = whole ? nullptr : a.ws + (2 * blockIdx.x + (u != begin)) * part_floats(a.chunk, a.dim);
+        float* part = whole ? nullptr : a.ws + notes_floats(gridDim.x) + (2 * c + (u != begin)) * part_floats(a.chunk, a.dim);
+        if (!whole && t0 == 0 && tid == 0) *note = {cut.of(base + (hc + 1) * units - 1), r * a.heads + head0, n_heads, u != begin};
         for (int i = tid; i < n_heads * a.dim; i += kThreads) {
             const int h = i / a.dim, d = i - h * a.dim;
             float sum = 0.0f;
@@ -732,76 +798,61 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
         }
         __syncthreads();
         u += t1 - t0;
-        if (u == base + (int64_t)units * per_request) {
+        if (u == base + units * per_request) {
             base = u;
             ++r;
         }
     }
 }
 
-// Joins the parts of one head of a request, if it was divided: a CTA each.
-constexpr int kJoinWarps = 8, kJoinThreads = kJoinWarps * 32;
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttnArgs a, int64_t grid, float lift) {
-    __shared__ int64_t warp_sums[kJoinWarps], warp_sums_low[kJoinWarps];
-    __shared__ float sums[kJoinWarps][kMaxHeadDim], some[kJoinWarps];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int r = blockIdx.x / a.heads, head = blockIdx.x - r * a.heads;
-    const int kv = head / a.group, chunk = (head - kv * a.group) / a.chunk, in_chunk = head - kv * a.group - chunk * a.chunk;
-    const int per_request = a.kv_heads * a.n_chunks;
+// Joins the parts of the head (chunk) that CTA blockIdx.x has noted, if it has: as many warps to a row of out as there are, each
+// with its share of the parts.
+constexpr int kJoinWarps = 16, kJoinThreads = kJoinWarps * 32;
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttnArgs a, float lift) {
+    __shared__ float sums[kJoinWarps][kMaxHeadDim], ls[kJoinWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
     pdl_release();
     pdl_wait();
-    int64_t mine = 0, below = 0, all, low;
-    for (int i = tid; i < a.batch; i += kJoinThreads) {
-        const int64_t units = (int64_t)units_of(a, i) * per_request;
-        mine += units;
-        if (i < r) below += units;
-    }
-    sum_before(mine, warp_sums, all);
-    sum_before(below, warp_sums_low, low);
-    const int units = units_of(a, r);
-    const int64_t s0 = low + (int64_t)(kv * a.n_chunks + chunk) * units, s1 = s0 + units, n = min(grid, all);
-    const int64_t c0 = part_of(s0, n, all), c1 = part_of(s1 - 1, n, all);
-    if (c0 == c1) return;
+    const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.ws) + c0);
+    const Note note{raw.x, raw.y, raw.z, raw.w};
+    if (note.last < 0) return;
+    const int per = kJoinWarps / note.n_heads, h = warp / per, sub = warp - h * per;
+    const bool live = h < note.n_heads;
     const int64_t floats = part_floats(a.chunk, a.dim);
-    const bool behind = part_start(c0, n, all) < s0;         // the first of the parts is its CTA's last piece
-    const auto part = [&](int64_t c) { return a.ws + (2 * c + (c == c0 && behind)) * floats; };
-    float top = -INFINITY, l = 0.0f;
-    for (int64_t c = c0 + tid; c <= c1; c += kJoinThreads) top = fmaxf(top, part(c)[in_chunk]);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (lane == 0) some[warp] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, some[w]);
+    const float* parts = a.ws + notes_floats(gridDim.x) + h;
+    const auto part = [&](int c) { return parts + (2 * c + (c == c0 ? note.second : 0)) * floats; };
     constexpr int kPer = kMaxHeadDim / 32;
-    float acc[kPer];
+    float top = -INFINITY, l = 0.0f, acc[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) acc[i] = 0.0f;
-#pragma unroll 4
-    for (int64_t c = c0 + warp; c <= c1; c += kJoinWarps) {
-        const float* p = part(c);
-        const float pm = p[in_chunk], w = pm == -INFINITY ? 0.0f : exp2_fast(pm - top);
-        l += p[a.chunk + in_chunk] * w;
-        const float* x = p + 2 * a.chunk + in_chunk * a.dim;
+    if (live) {
+        for (int c = c0 + lane; c <= note.last; c += 32) top = fmaxf(top, *part(c));
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (lane + 32 * i < a.dim) acc[i] += x[lane + 32 * i] * w;
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+#pragma unroll 4
+        for (int c = c0 + sub; c <= note.last; c += per) {
+            const float* p = part(c);
+            const float m = p[0], w = m == -INFINITY ? 0.0f : exp2_fast(m - top);
+            l += p[a.chunk] * w;
+            const float* x = p - h + 2 * a.chunk + h * a.dim + lane;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (lane + 32 * i < a.dim) acc[i] += x[32 * i] * w;
+        }
     }
-    __syncthreads();
 #pragma unroll
     for (int i = 0; i < kPer; ++i) sums[warp][lane + 32 * i] = acc[i];
-    if (lane == 0) some[warp] = l;
+    if (lane == 0) ls[warp] = l;
     __syncthreads();
+    if (!live || sub) return;
     l = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) l += some[w];
-    for (int d = tid; d < a.dim; d += kJoinThreads) {
+    for (int w = 0; w < per; ++w) l += ls[warp + w];
+    for (int d = lane; d < a.dim; d += 32) {
         float sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kJoinWarps; ++w) sum += sums[w][d];
-        store_out(a, ((int64_t)r * a.heads + head) * a.dim + d, l == 0.0f ? 0.0f : __fdiv_rn(sum, l));
+        for (int w = 0; w < per; ++w) sum += sums[warp + w][d];
+        store_out(a, ((int64_t)note.row + h) * a.dim + d, l == 0.0f ? 0.0f : __fdiv_rn(sum, l));
     }
-    if (a.lse && tid == 0) a.lse[(int64_t)r * a.heads + head] = l == 0.0f ? -INFINITY : (top - lift + log2f(l)) * kLn2;
+    if (a.lse && lane == 0) a.lse[(int64_t)note.row + h] = l == 0.0f ? -INFINITY : (top - lift + log2f(l)) * kLn2;
 }
 
 // ------------------------------------------------------------------------------------------------------ choice
@@ -884,14 +935,16 @@ pp_status_t check_call(const pp_paged_cache_t* cache, pp_dtype_t q_type, int bat
     if (const pp_status_t st = check_cache(cache)) return st;
     if (!is_float(q_type) || (q_type != cache->dtype && !is_8bit(cache->dtype))) return PP_ERR_UNSUPPORTED;
     if (batch < 0 || heads < 1 || heads % cache->kv_heads || width < 1 || window < 0) return PP_ERR_INVALID_ARG;
-    if ((int64_t)width * cache->page_size > INT32_MAX - 2 * kUnit || heads > (1 << 20) || (int64_t)batch * heads > INT32_MAX) return PP_ERR_UNSUPPORTED;
+    const int64_t capacity = (int64_t)width * cache->page_size;
+    if (capacity > INT32_MAX - 2 * kUnit || heads > (1 << 20) || (int64_t)batch * heads > INT32_MAX) return PP_ERR_UNSUPPORTED;
+    if ((int64_t)batch * heads > INT32_MAX / (capacity / kUnit + 2)) return PP_ERR_UNSUPPORTED;     // units are counted in 32 bits
     return PP_OK;
 }
 
 // Whether any request can have more than one unit.
 bool divided(const pp_paged_cache_t& c, int width, int window) {
     const int64_t capacity = (int64_t)width * c.page_size;
-    return (window > 0 ? std::min<int64_t>(window, capacity) : capacity) > kUnit;
+    return (window > 0 ? std::min<int64_t>((int64_t)window + kTile - 1, capacity) : capacity) > kUnit;
 }
 
 }  // namespace
@@ -907,7 +960,7 @@ extern "C" pp_status_t pp_paged_attention_workspace(const pp_paged_cache_t* cach
     int granule, chunk, grid;
     const Form f = choose(*cache, q_type, heads / cache->kv_heads, granule, chunk);
     if (const cudaError_t e = grid_of(f, grid)) return status_of(e);
-    *bytes = (int64_t)grid * 2 * part_floats(chunk, cache->head_dim) * 4;
+    *bytes = (notes_floats(grid) + (int64_t)grid * 2 * part_floats(chunk, cache->head_dim)) * 4;
     return PP_OK;
 }
 
@@ -933,17 +986,17 @@ extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const v
     const Form f = choose(c, q_type, group, granule, chunk);
     if (const cudaError_t e = grid_of(f, grid)) return status_of(e);
     const bool parts = divided(c, width, window);
-    const int64_t need = parts ? (int64_t)grid * 2 * part_floats(chunk, c.head_dim) * 4 : 0;
+    const int64_t need = parts ? (notes_floats(grid) + (int64_t)grid * 2 * part_floats(chunk, c.head_dim)) * 4 : 0;
     if (need && (!workspace || workspace_bytes < need)) return PP_ERR_INVALID_ARG;
     const int es = type_bytes(c.dtype);
     AttnArgs a{q, static_cast<const char*>(c.k), static_cast<const char*>(c.v), c.k_scales, c.v_scales, table, lengths, out, lse,
-               static_cast<float*>(workspace), q_row, q_head, c.k_page * es, c.k_token * es, c.k_head * es, c.v_page * es, c.v_token * es,
+               parts ? static_cast<float*>(workspace) : nullptr, q_row, q_head, c.k_page * es, c.k_token * es, c.k_head * es, c.v_page * es, c.v_token * es,
                c.v_head * es, ld_table, Divisor((uint32_t)c.page_size), c.pages, c.page_size, batch, width * c.page_size, window, heads, c.kv_heads, group,
-               chunk, (group + chunk - 1) / chunk, c.head_dim, granule, q_type, c.dtype, scale * kLog2e};
+               chunk, (group + chunk - 1) / chunk, c.head_dim, granule, q_type, c.dtype, c.page_size % kTile == 0, scale * kLog2e};
     const int64_t segments = (int64_t)batch * c.kv_heads * a.n_chunks;
     if (!parts) grid = (int)std::min<int64_t>(grid, segments);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = launch_pdl(f.kernel, dim3((unsigned)grid), dim3(kThreads), (size_t)f.smem, s, 1, a);
-    if (e == cudaSuccess && parts) e = launch_pdl(join_kernel, dim3((unsigned)(batch * heads)), dim3(kJoinThreads), 0, s, 1, a, (int64_t)grid, f.lift);
+    if (e == cudaSuccess && parts) e = launch_pdl(join_kernel, dim3((unsigned)grid), dim3(kJoinThreads), 0, s, 1, a, f.lift);
     return status_of(e);
 }

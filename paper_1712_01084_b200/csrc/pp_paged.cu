@@ -18,7 +18,7 @@ namespace pp {
 namespace {
 
 // -------------------------------------------------------------------------------------------------------- plan
-constexpr int kPlanThreads = 256, kPlanRows = 4, kMaxRequests = 8192;
+constexpr int kPlanThreads = 256, kMaxRequests = 8192;
 
 struct PlanArgs {
     const int32_t *lengths, *added, *free_pages, *taken;
@@ -34,7 +34,8 @@ struct PlanArgs {
 
 __device__ __forceinline__ int sat32(int64_t v) { return v > INT32_MAX ? INT32_MAX : (int)v; }
 
-__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a) {
+// kPlanRows: neighbouring rows of a thread.
+template <int kPlanRows> __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a) {
     extern __shared__ int32_t plan_smem[];
     int32_t* starts = plan_smem;                             // [requests + 1]
     int32_t* have = starts + a.requests + 1;                 // [requests]
@@ -74,7 +75,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a) {
     before_rows -= rows;
     for (int r = r0; r < r1; ++r) {
         const int need = base[r], add = starts[r];
-        base[r] = sat32(before_pages);
+        base[r] = (int)before_pages;
         starts[r] = (int)min(before_rows, (int64_t)a.rows);
         if (a.rows_too && blockIdx.x == 0) a.starts[r] = starts[r];
         if (a.state_too && blockIdx.x == 0) a.lengths_out[r] = (int)min((int64_t)have[r] + add, (int64_t)a.capacity);
@@ -94,10 +95,15 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a) {
         const int64_t at = taken + base[r] + (column - first);
         return at >= 0 && at < a.n_free ? a.free_pages[at] : -1;
     };
-    for (int r = blockIdx.x * (kPlanThreads / 32) + warp; r < a.requests; r += gridDim.x * (kPlanThreads / 32)) {
-        const int total = (int)min((int64_t)have[r] + max(a.added[r], 0), (int64_t)a.capacity);
-        const int first = (int)a.page.of(have[r] + a.page_size - 1), need = (int)a.page.of(total + a.page_size - 1) - first;
-        for (int i = lane; i < need; i += 32) a.table[r * a.ld_table + first + i] = given(r, first + i, first);
+    for (int64_t i = (int64_t)blockIdx.x * kPlanThreads + tid; i < all_pages; i += (int64_t)gridDim.x * kPlanThreads) {
+        int low = 0, high = a.requests - 1;                  // the last request with base <= i: the one that needs page i
+        while (low < high) {
+            const int mid = (low + high + 1) / 2;
+            if (base[mid] <= i) low = mid;
+            else high = mid - 1;
+        }
+        const int first = (int)a.page.of(have[low] + a.page_size - 1), column = first + (int)(i - base[low]);
+        a.table[low * a.ld_table + column] = given(low, column, first);
     }
     const int64_t row0 = ((int64_t)blockIdx.x * kPlanThreads + tid) * kPlanRows;
     if (row0 >= a.rows) return;
@@ -108,28 +114,35 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a) {
         if (starts[mid + 1] > row0) high = mid;
         else low = mid + 1;
     }
-    int64_t slot[kPlanRows];
-    int position[kPlanRows];
+    int64_t place[kPlanRows];
+    int position[kPlanRows], number[kPlanRows];
+    const int32_t* from[kPlanRows];                          // where a row's page stands
 #pragma unroll
     for (int i = 0; i < kPlanRows; ++i) {
         const int64_t row = row0 + i;
-        slot[i] = -1;
-        position[i] = 0;
+        from[i] = nullptr;
+        place[i] = position[i] = 0;
         if (row >= live) continue;
         while (starts[low + 1] <= row) ++low;                // row < live: there is one
         const int64_t p = have[low] + (row - starts[low]);
         position[i] = sat32(p);
-        if (p < a.capacity) {
-            const int column = (int)a.page.of((uint32_t)p), first = (int)a.page.of(have[low] + a.page_size - 1);
-            const int number = column >= first ? given(low, column, first) : a.table[low * a.ld_table + column];
-            if (number >= 0) slot[i] = (int64_t)number * a.page_size + (p - (int64_t)column * a.page_size);
-        }
+        if (p >= a.capacity) continue;
+        const int column = (int)a.page.of((uint32_t)p), first = (int)a.page.of(have[low] + a.page_size - 1);
+        const int64_t at = taken + base[low] + (column - first);
+        place[i] = p - (int64_t)column * a.page_size;
+        if (column < first) from[i] = a.table + low * a.ld_table + column;
+        else if (at >= 0 && at < a.n_free) from[i] = a.free_pages + at;
     }
-    if (a.wide && row0 + kPlanRows <= a.rows) {
+#pragma unroll
+    for (int i = 0; i < kPlanRows; ++i) number[i] = from[i] ? *from[i] : -1;
+    int64_t slot[kPlanRows];
+#pragma unroll
+    for (int i = 0; i < kPlanRows; ++i) slot[i] = number[i] >= 0 ? (int64_t)number[i] * a.page_size + place[i] : -1;
+    if (kPlanRows == 4 && a.wide && row0 + kPlanRows <= a.rows) {
         longlong2* s = reinterpret_cast<longlong2*>(a.slots + row0);
-        s[0] = make_longlong2(slot[0], slot[1]);
-        s[1] = make_longlong2(slot[2], slot[3]);
-        *reinterpret_cast<int4*>(a.positions + row0) = make_int4(position[0], position[1], position[2], position[3]);
+        s[0] = make_longlong2(slot[0], slot[kPlanRows / 4]);
+        s[1] = make_longlong2(slot[kPlanRows / 2], slot[kPlanRows - 1]);
+        *reinterpret_cast<int4*>(a.positions + row0) = make_int4(position[0], position[kPlanRows / 4], position[kPlanRows / 2], position[kPlanRows - 1]);
     } else {
 #pragma unroll
         for (int i = 0; i < kPlanRows; ++i)
@@ -141,7 +154,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------------ append
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 256, kAhead = 4, kMaxTokens = 4;
 
 struct AppendArgs {
     const void *q, *k, *v;
@@ -152,17 +165,15 @@ struct AppendArgs {
     const float* inv_freq;
     int64_t q_token, q_head, o_token, o_head, k_token, k_head, v_token, v_head;
     int64_t ck_page, ck_token, ck_head, cv_page, cv_token, cv_head, n_slots;
-    int heads, kv_heads, dim, page_size, pairs, interleaved, code_type, lanes;   // lanes: of a head (VEC)
+    int heads, kv_heads, dim, page_size, pairs, interleaved, code_type, tokens, lanes, per_cta;   // the last two: VEC
 };
 
-// Cosine and sine of position * inv_freq, the angle brought into half a turn around 0 in 64 bits.
+// Cosine and sine of position * inv_freq: the angle in turns, less whole ones, in 64 bits (1 / (2 pi) as a sum of two doubles).
 __device__ __forceinline__ float2 turn(int position, float inv_freq) {
     const double a = (double)position * (double)inv_freq;
-    const double n = rint(a * 0.15915494309189533577);
-    double r = fma(-n, 6.28318530717958647693, a);           // 2 pi as a sum of two doubles
-    r = fma(-n, 2.449293598294706414e-16, r);
+    const double whole = rint(a * 0.15915494309189535), part = fma(a, -9.839338337591243e-18, fma(a, 0.15915494309189535, -whole));
     float s, c;
-    sincosf((float)r, &s, &c);
+    sincospif(2.0f * (float)part, &s, &c);
     return make_float2(c, s);
 }
 
@@ -198,99 +209,111 @@ __device__ __forceinline__ Row row_of(const AppendArgs& a, int i) {
     return {2, i - a.heads - a.kv_heads};
 }
 
-// VEC: a.lanes lanes to a head, eight elements to a lane.  Q8: the cache holds 8 bits.
+// VEC: a.lanes lanes to a head, eight elements to a lane, a.per_cta tokens to a CTA.  Q8: the cache holds 8 bits.
 template <typename T, bool Q8>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs a) {
-    __shared__ float2 turns[kMaxHeadDim / 2];
-    const int tid = threadIdx.x, lanes = a.lanes, j = tid & (lanes - 1), groups = kAppendThreads / lanes;
-    const int64_t token = blockIdx.x;
+__global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const AppendArgs a) {
+    __shared__ float2 turns[kMaxTokens][kMaxHeadDim / 2];
+    const int tid = threadIdx.x, lane = tid & 31, lanes = a.lanes, j = tid & (lanes - 1), groups = kAppendThreads / lanes;
+    const int64_t token0 = (int64_t)blockIdx.x * a.per_cta;
+    const int tokens = (int)min((int64_t)a.per_cta, a.tokens - token0);
     const int rows = a.heads + 2 * a.kv_heads, first = blockIdx.y * groups + tid / lanes, step = gridDim.y * groups;
     const int loops = (rows - (int)blockIdx.y * groups + step - 1) / step;   // the same for every thread: shuffles need them all
     pdl_release();
     pdl_wait();
     const bool mine = 8 * j < a.dim;
-    const int64_t slot = a.slots[token];
-    const auto source = [&](int i) {
+    const auto source = [&](int64_t token, int i) {
         const Row r = row_of(a, i);
         return r.kind == 0 ? static_cast<const T*>(a.q) + token * a.q_token + r.head * a.q_head
              : r.kind == 1 ? static_cast<const T*>(a.k) + token * a.k_token + r.head * a.k_head
                            : static_cast<const T*>(a.v) + token * a.v_token + r.head * a.v_head;
     };
     using Raw = Pack<T, 8>;
-    Raw raw;
-    if (mine && first < rows) raw = *reinterpret_cast<const Raw*>(source(first) + 8 * j);
+    Raw raw[kAhead];
+    const auto fetch = [&](int64_t token, int from) {        // a few rows on their way at once
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n)
+            if (mine && from + n * step < rows) raw[n] = *reinterpret_cast<const Raw*>(source(token, from + n * step) + 8 * j);
+    };
+    fetch(token0, first);
+    int64_t slot = a.slots[token0];
     if (a.pairs) {
-        const int position = a.positions[token];
-        for (int i = tid; i < a.pairs; i += kAppendThreads) turns[i] = turn(position, a.inv_freq[i]);
+        for (int i = tid; i < tokens * a.pairs; i += kAppendThreads) {
+            const int t = i / a.pairs, pair = i - t * a.pairs;
+            turns[t][pair] = turn(a.positions[token0 + t], a.inv_freq[pair]);
+        }
         __syncthreads();
     }
-    // this lane's turns; element e: cosine, and the sine with the sign of its place in the pair
-    const int lane = tid & 31;
-    int partner = lane;
-    float cosine[8], sine[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int d = 8 * j + e;
-        cosine[e] = 1.0f;
-        sine[e] = 0.0f;
-        if (d < 2 * a.pairs) {
-            const float2 t = turns[a.interleaved ? d / 2 : d < a.pairs ? d : d - a.pairs];
-            const bool second = a.interleaved ? (d & 1) : d >= a.pairs;
-            cosine[e] = t.x;
-            sine[e] = second ? t.y : -t.y;
-        }
-    }
     const bool turned = 8 * j < 2 * a.pairs;
-    if (turned && !a.interleaved) partner = 8 * j < a.pairs ? lane + a.pairs / 8 : lane - a.pairs / 8;
-
-    const bool stored = slot >= 0 && slot < a.n_slots;
-    int64_t page = 0, place = 0;
-    if (stored) split_slot(slot, a.page_size, page, place);
-    for (int n = 0, i = first; n < loops; ++n, i += step) {
-        const bool live = mine && i < rows;
-        Raw next;
-        if (mine && i + step < rows) next = *reinterpret_cast<const Raw*>(source(i + step) + 8 * j);
-        const Row r = row_of(a, i);
-        float x[8];
+    const int partner = !turned || a.interleaved ? lane : 8 * j < a.pairs ? lane + a.pairs / 8 : lane - a.pairs / 8;
+#pragma unroll 1
+    for (int t = 0; t < tokens; ++t) {
+        const int64_t token = token0 + t, next_slot = t + 1 < tokens ? a.slots[token + 1] : -1;
+        // this lane's turns; element e: cosine, and the sine with the sign of its place in the pair
+        float cosine[8], sine[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = live ? to_float(raw.v[e]) : 0.0f;
-        if (a.pairs) {
-            float y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = a.interleaved ? x[e ^ 1] : __shfl_sync(0xffffffffu, x[e], partner);
-            if (turned && r.kind < 2) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (8 * j + e < 2 * a.pairs) x[e] = fmaf(x[e], cosine[e], y[e] * sine[e]);
+        for (int e = 0; e < 8; ++e) {
+            const int d = 8 * j + e;
+            cosine[e] = 1.0f;
+            sine[e] = 0.0f;
+            if (d < 2 * a.pairs) {
+                const float2 by = turns[t][a.interleaved ? d / 2 : d < a.pairs ? d : d - a.pairs];
+                const bool second = a.interleaved ? (d & 1) : d >= a.pairs;
+                cosine[e] = by.x;
+                sine[e] = second ? by.y : -by.y;
             }
         }
-        if (r.kind == 0) {
-            if (live) store_vec(static_cast<T*>(a.q_out) + token * a.o_token + r.head * a.o_head + 8 * j, x);
-        }
-        if constexpr (Q8) {
-            const bool e4m3 = a.code_type == PP_E4M3;
-            float most = 0.0f;
+        const bool stored = slot >= 0 && slot < a.n_slots;
+        int64_t page = 0, place = 0;
+        if (stored) split_slot(slot, a.page_size, page, place);
+#pragma unroll 1
+        for (int done = 0; done < loops; done += kAhead) {
+            if (t || done) fetch(token, first + done * step);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) most = max_or_nan(most, fabsf(x[e]));
-            for (int o = 1; o < lanes; o <<= 1) most = max_or_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
-            if (r.kind != 0 && live && stored) {
-                const float scale = scale_of(most, e4m3);
-                uint32_t u[2] = {0, 0};
-                if (scale != 0.0f) {
+            for (int n = 0; n < kAhead; ++n) {
+                if (done + n >= loops) continue;
+                const int i = first + (done + n) * step;
+                const bool live = mine && i < rows;
+                const Row r = row_of(a, i);
+                float x[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) u[e / 4] |= (uint32_t)code_of(x[e], scale, e4m3) << (8 * (e & 3));
+                for (int e = 0; e < 8; ++e) x[e] = live ? to_float(raw[n].v[e]) : 0.0f;
+                if (a.pairs) {
+                    float y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = a.interleaved ? x[e ^ 1] : __shfl_sync(0xffffffffu, x[e], partner);
+                    if (turned && r.kind < 2) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (8 * j + e < 2 * a.pairs) x[e] = fmaf(x[e], cosine[e], y[e] * sine[e]);
+                    }
                 }
-                uint8_t* dst = r.kind == 1 ? static_cast<uint8_t*>(a.ck) + page * a.ck_page + place * a.ck_token + r.head * a.ck_head
-                                           : static_cast<uint8_t*>(a.cv) + page * a.cv_page + place * a.cv_token + r.head * a.cv_head;
-                *reinterpret_cast<uint2*>(dst + 8 * j) = make_uint2(u[0], u[1]);
-                if (j == 0) (r.kind == 1 ? a.ks : a.vs)[slot * a.kv_heads + r.head] = scale;
+                if (r.kind == 0 && live) store_vec(static_cast<T*>(a.q_out) + token * a.o_token + r.head * a.o_head + 8 * j, x);
+                if constexpr (Q8) {
+                    const bool e4m3 = a.code_type == PP_E4M3;
+                    float most = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) most = max_or_nan(most, fabsf(x[e]));
+                    for (int o = 1; o < lanes; o <<= 1) most = max_or_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
+                    if (r.kind != 0 && live && stored) {
+                        const float scale = scale_of(most, e4m3);
+                        uint32_t u[2] = {0, 0};
+                        if (scale != 0.0f) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) u[e / 4] |= (uint32_t)code_of(x[e], scale, e4m3) << (8 * (e & 3));
+                        }
+                        uint8_t* dst = r.kind == 1 ? static_cast<uint8_t*>(a.ck) + page * a.ck_page + place * a.ck_token + r.head * a.ck_head
+                                                   : static_cast<uint8_t*>(a.cv) + page * a.cv_page + place * a.cv_token + r.head * a.cv_head;
+                        *reinterpret_cast<uint2*>(dst + 8 * j) = make_uint2(u[0], u[1]);
+                        if (j == 0) (r.kind == 1 ? a.ks : a.vs)[slot * a.kv_heads + r.head] = scale;
+                    }
+                } else if (r.kind != 0 && live && stored) {
+                    T* dst = r.kind == 1 ? static_cast<T*>(a.ck) + page * a.ck_page + place * a.ck_token + r.head * a.ck_head
+                                         : static_cast<T*>(a.cv) + page * a.cv_page + place * a.cv_token + r.head * a.cv_head;
+                    store_vec(dst + 8 * j, x);
+                }
             }
-        } else if (r.kind != 0 && live && stored) {
-            T* dst = r.kind == 1 ? static_cast<T*>(a.ck) + page * a.ck_page + place * a.ck_token + r.head * a.ck_head
-                                 : static_cast<T*>(a.cv) + page * a.cv_page + place * a.cv_token + r.head * a.cv_head;
-            store_vec(dst + 8 * j, x);
         }
-        raw = next;
+        slot = next_slot;
     }
 }
 
@@ -364,14 +387,16 @@ __global__ void __launch_bounds__(kAppendThreads) append_any_kernel(const Append
     }
 }
 
-template <typename T> cudaError_t launch_append(const AppendArgs& a, bool vec, int tokens, cudaStream_t stream) {
+template <typename T> cudaError_t launch_append(AppendArgs& a, bool vec, int tokens, cudaStream_t stream) {
     const int rows = a.heads + 2 * a.kv_heads;
     const int at_once = vec ? kAppendThreads / a.lanes : kAppendThreads / 32;
     // a CTA per token where tokens fill the GPU; else a token's heads are divided, down to one to a group of lanes
     int parts = 1;
     while (parts * at_once < rows && (int64_t)tokens * parts < 4 * (int64_t)sm_count()) ++parts;
+    // many tokens: four to a CTA, whose sines then cost one trip through the long way of 64-bit arithmetic
+    if (vec && tokens >= 16 * sm_count()) a.per_cta = kMaxTokens;
     auto k = !vec ? append_any_kernel<T> : a.code_type == PP_E4M3 || a.code_type == PP_I8 ? append_kernel<T, true> : append_kernel<T, false>;
-    return launch_pdl(k, dim3((unsigned)tokens, (unsigned)parts), dim3(kAppendThreads), 0, stream, 1, a);
+    return launch_pdl(k, dim3((unsigned)(((int64_t)tokens + a.per_cta - 1) / a.per_cta), (unsigned)parts), dim3(kAppendThreads), 0, stream, 1, a);
 }
 
 }  // namespace
@@ -386,7 +411,8 @@ extern "C" pp_status_t pp_paged_plan(const int32_t* lengths, const int32_t* adde
     if (requests > 0 && (!lengths || !added || !table || !lengths_out || ld_table < width)) return PP_ERR_INVALID_ARG;
     if ((rows > 0 && (!slots || !positions)) || (n_free > 0 && !free_pages)) return PP_ERR_INVALID_ARG;
     const int64_t capacity = (int64_t)width * page_size;
-    if (requests > kMaxRequests || capacity > INT32_MAX - page_size) return PP_ERR_UNSUPPORTED;     // a length rounded up to pages fits too
+    // a length rounded up to pages and the pages of all requests fit 32 bits
+    if (requests > kMaxRequests || capacity > INT32_MAX - page_size || (int64_t)requests * width > INT32_MAX) return PP_ERR_UNSUPPORTED;
     if (ld_table > ((int64_t)1 << 40)) return PP_ERR_INVALID_ARG;
     for (const void* p : {(const void*)lengths, (const void*)added, (const void*)table, (const void*)free_pages, (const void*)taken,
                           (const void*)positions, (const void*)starts, (const void*)lengths_out, (const void*)taken_out})
@@ -409,24 +435,27 @@ extern "C" pp_status_t pp_paged_plan(const int32_t* lengths, const int32_t* adde
                width, n_free, requests, page_size, rows, (int)capacity, Divisor((uint32_t)page_size), aligned_to(slots, 16) && aligned_to(positions, 16), true, true};
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const size_t smem = (3 * (size_t)requests + 1) * 4;
-    static PerDeviceOnce opt_in;
+    // a row to a thread while one CTA holds them, or while CTAs are few; then four
+    const bool one = rows <= kPlanThreads || (rows > 4 * kPlanThreads && rows <= 2 * kPlanThreads * sm_count());
+    const auto kernel = one ? plan_kernel<1> : plan_kernel<4>;
+    static PerDeviceOnce opt_in[2];
     int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess) return status_of(cudaErrorInvalidDevice);
-    if (smem > 48 * 1024 && !opt_in.is_done(device)) {
-        if (cudaError_t e = cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (3 * kMaxRequests + 1) * 4)) return status_of(e);
-        opt_in.mark(device);
+    if (const cudaError_t e = cudaGetDevice(&device)) return status_of(e);
+    if (smem > 48 * 1024 && !opt_in[one].is_done(device)) {
+        if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (3 * kMaxRequests + 1) * 4)) return status_of(e);
+        opt_in[one].mark(device);
     }
-    const int64_t per = kPlanThreads * kPlanRows;
+    const int64_t per = kPlanThreads * (one ? 1 : 4);
     const unsigned grid = (unsigned)std::max<int64_t>(1, (rows + per - 1) / per);
     // In place and with several CTAs, one would write a length that another has still to read: lengths and pages taken are then
     // written by a launch of their own, behind the first.
     const bool apart = grid > 1 && (lengths == lengths_out || taken == taken_out);
     a.state_too = !apart;
-    cudaError_t e = launch_pdl(plan_kernel, dim3(grid), dim3(kPlanThreads), smem, stream, 1, a);
+    cudaError_t e = launch_pdl(kernel, dim3(grid), dim3(kPlanThreads), smem, stream, 1, a);
     if (e == cudaSuccess && apart) {
         a.rows_too = false;
         a.state_too = true;
-        e = launch_pdl(plan_kernel, dim3(1), dim3(kPlanThreads), smem, stream, 1, a);
+        e = launch_pdl(kernel, dim3(1), dim3(kPlanThreads), smem, stream, 1, a);
     }
     return status_of(e);
 }
@@ -466,7 +495,7 @@ extern "C" pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q
     AppendArgs a{q, k, v, q_out, c.k, c.v, c.k_scales, c.v_scales, slots, positions, inv_freq,
                  q_token, q_head, o_token, o_head, k_token, k_head, v_token, v_head,
                  c.k_page, c.k_token, c.k_head, c.v_page, c.v_token, c.v_head, (int64_t)c.pages * c.page_size,
-                 heads, c.kv_heads, dim, c.page_size, pairs, interleaved != 0, c.dtype, 8};
+                 heads, c.kv_heads, dim, c.page_size, pairs, interleaved != 0, c.dtype, tokens, 8, 1};
     while (a.lanes * 8 < dim) a.lanes *= 2;
     // eight elements to an access where every row starts on one, and pairs of halves lie whole lanes apart
     const auto wide = [&](const void* p, int64_t token, int64_t head, int n) { return !p || row_alignment(p, 1, 0, tokens, token, n, head, tb) == 16; };
