@@ -112,47 +112,15 @@ __device__ __forceinline__ uint32_t positions_of(const Reader& r, int at) {
     return ((1u << to) - 1u) & ~((1u << from) - 1u);
 }
 
-// Asks for the tile at `at`: 16 rows of keys, of values, and the scales of both.  Returns which rows are there (a bit each).
-// ES: bytes of an element, CHUNKS: 16-byte pieces of a row as the kernel sees it (rows that are shorter end in zeros).
+// Rows that are looked up one by one, in pieces of a.granule bytes.  Out of line: the usual form's code then stays short.
+// Returns which rows are there (a bit each).
 template <int ES, int CHUNKS, int PITCH, bool Q8>
-__device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, int at, uint32_t stage) {
+__device__ __noinline__ uint32_t ask_by_row(const AttnArgs& a, const char* k, const char* v, const float* ks, const float* vs, int low, int end, int entry, int at,
+                                            uint32_t stage) {
     constexpr int kTileBytes = kTile * PITCH;
     const int lane = threadIdx.x & 31, p = at + (lane & 15);
-    if (a.whole_tiles && a.granule == 16) {                  // one page: rows a fixed distance apart
-        constexpr int kLanes = CHUNKS > 16 ? 32 : CHUNKS > 8 ? 16 : CHUNKS > 4 ? 8 : 4, kRows = 32 / kLanes;
-        const bool is_page = (uint32_t)r.entry < (uint32_t)a.pages;
-        const int entry = is_page ? r.entry : 0, place = at - (int)a.page.of((uint32_t)at) * a.page_size;
-        const uint32_t bits = is_page ? positions_of(r, at) : 0;
-        r.entry = entry_of(a, r, at + kUnit);
-        const int row = lane / kLanes;
-        const char* k = r.k + (int64_t)entry * a.k_page + (int64_t)(place + row) * a.k_token;
-        const char* v = r.v + (int64_t)entry * a.v_page + (int64_t)(place + row) * a.v_token;
-#pragma unroll
-        for (int i = 0; i < kTile / kRows; ++i) {
-            const bool has = (bits >> (i * kRows + row)) & 1;
-#pragma unroll
-            for (int c0 = 0; c0 < CHUNKS; c0 += kLanes) {
-                const int c = c0 + (lane & (kLanes - 1));
-                if (CHUNKS % kLanes && c >= CHUNKS) continue;
-                const bool own = c * 16 < a.dim * ES;
-                const uint32_t dst = stage + (i * kRows + row) * PITCH + c * 16;
-                copy_async<16>(dst, k + (own ? c * 16 : 0), own && has);
-                copy_async<16>(dst + kTileBytes, v + (own ? c * 16 : 0), own && has);
-            }
-            k += kRows * a.k_token;
-            v += kRows * a.v_token;
-        }
-        if constexpr (Q8) {
-            const bool in = (bits >> (lane & 15)) & 1;
-            const int64_t token = (int64_t)entry * a.page_size + place + (in ? lane & 15 : 0);
-            copy_async<4>(stage + 2 * kTileBytes + lane * 4, (lane < 16 ? r.ks : r.vs) + token * a.kv_heads, in);
-        }
-        return bits;
-    }
-    const int entry = a.whole_tiles && (p < r.low || p >= r.end) ? -1 : r.entry;
-    const bool there = (uint32_t)entry < (uint32_t)a.pages;  // -1 is none, and a number that is no page of the cache neither
+    const bool there = p >= low && p < end && (uint32_t)entry < (uint32_t)a.pages;   // -1 is no page, and a number that is none of the cache's neither
     const uint32_t bits = __ballot_sync(0xffffffffu, there) & 0xffffu;
-    r.entry = entry_of(a, r, at + kUnit);
     int64_t off = 0;
     int place = 0;
     if (there) {
@@ -161,19 +129,18 @@ __device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, int at, ui
     }
     const auto copy = [&](auto bytes) {
         constexpr int B = decltype(bytes)::value, kPieces = CHUNKS * 16 / B;
-        constexpr int kLanes = kPieces >= 32 ? 32 : kPieces > 16 ? 32 : kPieces > 8 ? 16 : kPieces > 4 ? 8 : 4;
+        constexpr int kLanes = kPieces > 16 ? 32 : kPieces > 8 ? 16 : kPieces > 4 ? 8 : 4;
         const int own = a.dim * ES / B;
-#pragma unroll
+#pragma unroll 2
         for (int i = 0; i < kTile * kLanes / 32; ++i) {
             const int row = i * (32 / kLanes) + lane / kLanes;
             const int64_t ko = __shfl_sync(0xffffffffu, off, row), vo = __shfl_sync(0xffffffffu, off, 16 + row);
             const bool has = (bits >> row) & 1;
-#pragma unroll
             for (int c = lane & (kLanes - 1); c < kPieces; c += kLanes) {
                 const bool in = has && c < own;
                 const int piece = in ? c * B : 0;
-                copy_async<B>(stage + row * PITCH + c * B, r.k + ko + piece, in);
-                copy_async<B>(stage + kTileBytes + row * PITCH + c * B, r.v + vo + piece, in);
+                copy_async<B>(stage + row * PITCH + c * B, k + ko + piece, in);
+                copy_async<B>(stage + kTileBytes + row * PITCH + c * B, v + vo + piece, in);
             }
         }
     };
@@ -182,7 +149,46 @@ __device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, int at, ui
     else copy(std::integral_constant<int, 4>());
     if constexpr (Q8) {
         const int64_t token = there ? (int64_t)entry * a.page_size + place : 0;
-        copy_async<4>(stage + 2 * kTileBytes + lane * 4, (lane < 16 ? r.ks : r.vs) + token * a.kv_heads, there);
+        copy_async<4>(stage + 2 * kTileBytes + lane * 4, (lane < 16 ? ks : vs) + token * a.kv_heads, there);
+    }
+    return bits;
+}
+
+// Asks for the tile at `at`: 16 rows of keys, of values, and the scales of both.  Returns which rows are there.
+// ES: bytes of an element, CHUNKS: 16-byte pieces of a row as the kernel sees it (rows that are shorter end in zeros).
+template <int ES, int CHUNKS, int PITCH, bool Q8>
+__device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, int at, uint32_t stage) {
+    constexpr int kTileBytes = kTile * PITCH;
+    constexpr int kLanes = CHUNKS > 16 ? 32 : CHUNKS > 8 ? 16 : CHUNKS > 4 ? 8 : 4, kRows = 32 / kLanes;
+    const int found = r.entry;
+    r.entry = entry_of(a, r, at + kUnit);
+    if (!a.whole_tiles || a.granule != 16) return ask_by_row<ES, CHUNKS, PITCH, Q8>(a, r.k, r.v, r.ks, r.vs, r.low, r.end, found, at, stage);
+    // one page: rows a fixed distance apart
+    const int lane = threadIdx.x & 31, row = lane / kLanes;
+    const bool is_page = (uint32_t)found < (uint32_t)a.pages;
+    const int entry = is_page ? found : 0, place = at - (int)a.page.of((uint32_t)at) * a.page_size;
+    const uint32_t bits = is_page ? positions_of(r, at) : 0;
+    const char* k = r.k + (int64_t)entry * a.k_page + (int64_t)(place + row) * a.k_token;
+    const char* v = r.v + (int64_t)entry * a.v_page + (int64_t)(place + row) * a.v_token;
+#pragma unroll
+    for (int i = 0; i < kTile / kRows; ++i) {
+        const bool has = (bits >> (i * kRows + row)) & 1;
+#pragma unroll
+        for (int c0 = 0; c0 < CHUNKS; c0 += kLanes) {
+            const int c = c0 + (lane & (kLanes - 1));
+            if (CHUNKS % kLanes && c >= CHUNKS) continue;
+            const bool own = c * 16 < a.dim * ES;
+            const uint32_t dst = stage + (i * kRows + row) * PITCH + c * 16;
+            copy_async<16>(dst, k + (own ? c * 16 : 0), own && has);
+            copy_async<16>(dst + kTileBytes, v + (own ? c * 16 : 0), own && has);
+        }
+        k += kRows * a.k_token;
+        v += kRows * a.v_token;
+    }
+    if constexpr (Q8) {
+        const bool in = (bits >> (lane & 15)) & 1;
+        const int64_t token = (int64_t)entry * a.page_size + place + (in ? lane & 15 : 0);
+        copy_async<4>(stage + 2 * kTileBytes + lane * 4, (lane < 16 ? r.ks : r.vs) + token * a.kv_heads, in);
     }
     return bits;
 }
@@ -662,7 +668,7 @@ struct Note {
     int second;                                              // the first one's part is the second of its two
 };
 
-template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnArgs a) {
+template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) attn_kernel(const __grid_constant__ AttnArgs a) {
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ int warp_sums[kWarps], found_base, found;
     __shared__ float warp_m[kWarps][Core::kHeads], warp_l[kWarps][Core::kHeads], factors[kWarps][Core::kHeads], all_m[Core::kHeads], all_l[Core::kHeads];
@@ -732,21 +738,22 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
             ++asked;
             if (++stage == Core::kStages) stage = 0;
         };
-#pragma unroll 1
-        for (int i = 0; i < Core::kStages - 1; ++i) request();
-        stage_q<Core::kHeads, Core::kQFloats / Core::kHeads>(a, r, head0, n_heads, q);
-        __syncthreads();
-        core.begin(a, q);
         int at = 0;
 #pragma unroll 1
-        for (int i = 0; i < tiles; ++i) {
-            if constexpr (Core::kStages > 1) {
-                wait_but<Core::kStages - 2>();
+        for (int i = 1 - Core::kStages;; ++i) {              // one call of request: its code is long
+            if (i == 0) {
+                stage_q<Core::kHeads, Core::kQFloats / Core::kHeads>(a, r, head0, n_heads, q);
+                __syncthreads();
+                core.begin(a, q);
+            }
+            if (i >= tiles) break;
+            if (i >= 0) {
+                if constexpr (Core::kStages > 1) wait_but<Core::kStages - 2>();
                 __syncwarp();                                // this tile is here, and every lane has left the one before it
-                request();
-            } else {
-                __syncwarp();
-                request();
+            }
+            request();
+            if (i < 0) continue;
+            if constexpr (Core::kStages == 1) {
                 wait_but<0>();
                 __syncwarp();
             }

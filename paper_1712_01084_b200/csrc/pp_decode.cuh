@@ -114,6 +114,19 @@ template <typename T, int N> __device__ __forceinline__ void store_vec(T* p, con
     }
     *reinterpret_cast<Pack<T, N>*>(p) = u;
 }
+
+// Four 8-bit codes of floats, to nearest even.
+__device__ __forceinline__ uint32_t four_codes(const float* v, bool e4m3) {
+    if (e4m3) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
+        return lo | (hi << 16);
+    }
+    uint32_t u = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u |= (uint32_t)(__float2int_rn(fminf(fmaxf(v[i], -127.0f), 127.0f)) & 255) << (8 * i);
+    return u;
+}
 #endif
 
 }  // namespace pp

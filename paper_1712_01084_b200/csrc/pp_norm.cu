@@ -59,18 +59,6 @@ template <bool VEC> __device__ __forceinline__ int column(int c, int i) {
     return base + (VEC ? lane * 8 + i : i * 32 + lane);
 }
 
-__device__ __forceinline__ uint32_t four_codes(const float* v, bool e4m3) {
-    if (e4m3) {
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
-        return lo | (hi << 16);
-    }
-    uint32_t u = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u |= (uint32_t)(__float2int_rn(fminf(fmaxf(v[i], -127.0f), 127.0f)) & 255) << (8 * i);
-    return u;
-}
-
 // The weights of this thread's chunk c as floats, 0 past the row's end.
 template <typename T, bool VEC> __device__ __forceinline__ void load_weights(const NormArgs& a, int c, float (&w)[8]) {
     const int j0 = column<VEC>(c, 0);

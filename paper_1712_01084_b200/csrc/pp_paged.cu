@@ -7,9 +7,8 @@
 // then takes its share of the rows, four to a thread: a binary search for the row's request, and its page from the free
 // list where it is a new one, else from the table, whose old entries nobody writes.
 //
-// Append.  All bandwidth for many tokens, all latency for few.  Eight elements to a lane and 8, 16 or 32 lanes to a head
-// (VEC): a lane has the same dimensions of every head, so its cosines and sines stay in registers, and the partner of a pair
-// sits in a neighbouring lane (halves) or in the lane itself (neighbouring pairs).  The angle is a product in 64 bits,
+// Append.  All bandwidth for many tokens, all latency for few.  A lane has the same dimensions of every head, both elements of each
+// pair among them, so its cosines and sines stay in registers and serve two runs of eight (or four) elements of every row.  The angle is a product in 64 bits,
 // brought into a turn there: position 10^6 leaves a 32-bit angle 2^-5 of a radian.
 #include "pp_internal.h"
 #include "pp_paged.cuh"
@@ -154,7 +153,7 @@ template <int kPlanRows> __global__ void __launch_bounds__(kPlanThreads) plan_ke
 }
 
 // ------------------------------------------------------------------------------------------------------ append
-constexpr int kAppendThreads = 256, kAhead = 4, kMaxTokens = 4;
+constexpr int kAppendThreads = 256, kAhead = 2, kMaxTokens = 4, kMaxRows = 256;
 
 struct AppendArgs {
     const void *q, *k, *v;
@@ -165,7 +164,7 @@ struct AppendArgs {
     const float* inv_freq;
     int64_t q_token, q_head, o_token, o_head, k_token, k_head, v_token, v_head;
     int64_t ck_page, ck_token, ck_head, cv_page, cv_token, cv_head, n_slots;
-    int heads, kv_heads, dim, page_size, pairs, interleaved, code_type, tokens, lanes, per_cta;   // the last two: VEC
+    int heads, kv_heads, dim, page_size, pairs, interleaved, code_type, tokens, lanes, per_cta, per_part;   // the last three: VEC
 };
 
 // Cosine and sine of position * inv_freq: the angle in turns, less whole ones, in 64 bits (1 / (2 pi) as a sum of two doubles).
@@ -183,15 +182,15 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
     return d;
 }
 
-// 8-bit code of v / scale, to nearest even; scale is not 0.
-__device__ __forceinline__ uint8_t code_of(float v, float scale, bool e4m3) {
-    v = __fdiv_rn(v, scale);
-    if (e4m3) return (uint8_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3);
-    return (uint8_t)(int8_t)__float2int_rn(fminf(fmaxf(v, -127.0f), 127.0f));
-}
 // The scale of a row whose largest magnitude is `most` (NaN and infinity: NaN).
 __device__ __forceinline__ float scale_of(float most, bool e4m3) {
     return most < INFINITY ? __fdiv_rn(most, e4m3 ? 448.0f : 127.0f) : __int_as_float(0x7fffffff);
+}
+// What a row's values are multiplied with for their codes: 1 / scale.  Below 2^-100, where that would leave the range, values and
+// scale are brought nearer first (`up`), so that codes stay what they are down to the smallest numbers; a scale of 0 has codes of 0.
+__device__ __forceinline__ float inverse_of(float scale, float& up) {
+    up = scale < 0x1p-100f ? 0x1p64f : 1.0f;
+    return scale == 0.0f ? 0.0f : __frcp_rn(scale * up);
 }
 
 // Page and place of a slot; slots above 32 bits are rare, and their division slow.
@@ -209,111 +208,182 @@ __device__ __forceinline__ Row row_of(const AppendArgs& a, int i) {
     return {2, i - a.heads - a.kv_heads};
 }
 
-// VEC: a.lanes lanes to a head, eight elements to a lane, a.per_cta tokens to a CTA.  Q8: the cache holds 8 bits.
-template <typename T, bool Q8>
-__global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const AppendArgs a) {
-    __shared__ float2 turns[kMaxTokens][kMaxHeadDim / 2];
-    const int tid = threadIdx.x, lane = tid & 31, lanes = a.lanes, j = tid & (lanes - 1), groups = kAppendThreads / lanes;
-    const int64_t token0 = (int64_t)blockIdx.x * a.per_cta;
-    const int tokens = (int)min((int64_t)a.per_cta, a.tokens - token0);
-    const int rows = a.heads + 2 * a.kv_heads, first = blockIdx.y * groups + tid / lanes, step = gridDim.y * groups;
-    const int loops = (rows - (int)blockIdx.y * groups + step - 1) / step;   // the same for every thread: shuffles need them all
-    pdl_release();
-    pdl_wait();
-    const bool mine = 8 * j < a.dim;
-    const auto source = [&](int64_t token, int i) {
-        const Row r = row_of(a, i);
-        return r.kind == 0 ? static_cast<const T*>(a.q) + token * a.q_token + r.head * a.q_head
-             : r.kind == 1 ? static_cast<const T*>(a.k) + token * a.k_token + r.head * a.k_head
-                           : static_cast<const T*>(a.v) + token * a.v_token + r.head * a.v_head;
-    };
-    using Raw = Pack<T, 8>;
-    Raw raw[kAhead];
-    const auto fetch = [&](int64_t token, int from) {        // a few rows on their way at once
+// W elements as they lie in memory, in words: copies of 16-bit element types go one by one.
+template <typename T, int W> struct alignas(sizeof(T) * W > 16 ? 16 : sizeof(T) * W) Run { uint32_t word[W * sizeof(T) / 4]; };
+template <int W> __device__ __forceinline__ void unpack(float (&x)[W], const Run<float, W>& r) {
 #pragma unroll
-        for (int n = 0; n < kAhead; ++n)
-            if (mine && from + n * step < rows) raw[n] = *reinterpret_cast<const Raw*>(source(token, from + n * step) + 8 * j);
-    };
-    fetch(token0, first);
-    int64_t slot = a.slots[token0];
-    if (a.pairs) {
-        for (int i = tid; i < tokens * a.pairs; i += kAppendThreads) {
-            const int t = i / a.pairs, pair = i - t * a.pairs;
-            turns[t][pair] = turn(a.positions[token0 + t], a.inv_freq[pair]);
-        }
-        __syncthreads();
+    for (int i = 0; i < W; ++i) x[i] = __uint_as_float(r.word[i]);
+}
+template <int W> __device__ __forceinline__ void unpack(float (&x)[W], const Run<__half, W>& r) {
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r.word[i]));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
     }
-    const bool turned = 8 * j < 2 * a.pairs;
-    const int partner = !turned || a.interleaved ? lane : 8 * j < a.pairs ? lane + a.pairs / 8 : lane - a.pairs / 8;
-#pragma unroll 1
-    for (int t = 0; t < tokens; ++t) {
-        const int64_t token = token0 + t, next_slot = t + 1 < tokens ? a.slots[token + 1] : -1;
-        // this lane's turns; element e: cosine, and the sine with the sign of its place in the pair
-        float cosine[8], sine[8];
+}
+template <int W> __device__ __forceinline__ void unpack(float (&x)[W], const Run<__nv_bfloat16, W>& r) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int d = 8 * j + e;
-            cosine[e] = 1.0f;
-            sine[e] = 0.0f;
-            if (d < 2 * a.pairs) {
-                const float2 by = turns[t][a.interleaved ? d / 2 : d < a.pairs ? d : d - a.pairs];
-                const bool second = a.interleaved ? (d & 1) : d >= a.pairs;
-                cosine[e] = by.x;
-                sine[e] = second ? by.y : -by.y;
+    for (int i = 0; i < W / 2; ++i) {                        // a bf16 number is the upper half of its float
+        x[2 * i] = __uint_as_float(r.word[i] << 16);
+        x[2 * i + 1] = __uint_as_float(r.word[i] & 0xffff0000u);
+    }
+}
+template <typename T, int W> __device__ __forceinline__ void store_run(T* to, const float (&x)[W]) {
+    Run<T, W> r;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) r.word[i] = __float_as_uint(x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) {
+            if constexpr (std::is_same_v<T, __half>) {
+                const __half2 v = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+                r.word[i] = *reinterpret_cast<const uint32_t*>(&v);
+            } else {
+                const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+                r.word[i] = *reinterpret_cast<const uint32_t*>(&v);
             }
         }
+    }
+    *reinterpret_cast<Run<T, W>*>(to) = r;
+}
+
+// VEC: a lane has two runs of W elements of each head, the two halves of W pairs (or 2 W neighbours), so that a pair never leaves its
+// lane and both its elements take the same sine; a.lanes lanes make a head.  A CTA has a.per_cta tokens and a.per_part of their heads:
+// where these lie, and the turns, are worked out once and stand in shared memory, since a row itself is only some 50 instructions
+// (addresses made row by row: 167 us for 16384 tokens of 64 + 2 x 8 heads).  Q8: the cache holds 8 bits.
+template <typename T, bool Q8, int W>
+__global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const __grid_constant__ AppendArgs a) {
+    struct From { const char* src; char* dst; };             // of a head, to which a token's distance is added, in bytes
+    struct By { int64_t src, dst; };
+    __shared__ From head_at[kMaxRows];
+    __shared__ By token_at[kMaxTokens][3];                   // of q, k and v
+    __shared__ int64_t slots[kMaxTokens];                    // -1: not to be stored
+    __shared__ __align__(16) float cosines[kMaxTokens][kMaxHeadDim / 2], sines[kMaxTokens][kMaxHeadDim / 2];
+    constexpr int kEl = (int)sizeof(T), kCached = Q8 ? 1 : kEl;
+    const int tid = threadIdx.x, lanes = a.lanes, j = tid & (lanes - 1), groups = kAppendThreads / lanes;
+    const int64_t token0 = (int64_t)blockIdx.x * a.per_cta;
+    const int tokens = (int)min((int64_t)a.per_cta, a.tokens - token0);
+    const int row0 = blockIdx.y * a.per_part, rows = min(a.per_part, a.heads + 2 * a.kv_heads - row0);
+    const int q_rows = a.heads - row0, k_rows = q_rows + a.kv_heads;         // rows below are of q, of k; the others of v
+    // the runs of this lane: whole runs turn (halves), or the pairs below a.pairs (neighbours)
+    const bool halves = !a.interleaved && j * W < a.pairs;
+    const int run0 = halves ? j * W : 2 * j * W, run1 = halves ? a.pairs + j * W : run0 + W;
+    const bool has0 = run0 < a.dim, has1 = run1 < a.dim;
+    const int turned = min(max(a.pairs - j * W, 0), W);      // pairs of this lane that turn
+    for (int i = tid; i < rows; i += kAppendThreads) {
+        const bool is_q = i < q_rows, is_k = i < k_rows;
+        const int64_t head = i - (is_q ? -row0 : is_k ? q_rows : k_rows);
+        head_at[i].src = static_cast<const char*>(is_q ? a.q : is_k ? a.k : a.v) + head * (is_q ? a.q_head : is_k ? a.k_head : a.v_head) * kEl;
+        head_at[i].dst = static_cast<char*>(is_q ? a.q_out : is_k ? a.ck : a.cv) + head * (is_q ? a.o_head * kEl : (is_k ? a.ck_head : a.cv_head) * kCached);
+    }
+    pdl_release();
+    pdl_wait();
+    if (tid < tokens) {
+        const int64_t token = token0 + tid, slot = a.slots[token];
         const bool stored = slot >= 0 && slot < a.n_slots;
         int64_t page = 0, place = 0;
         if (stored) split_slot(slot, a.page_size, page, place);
+        slots[tid] = stored ? slot : -1;
+        token_at[tid][0] = {token * a.q_token * kEl, token * a.o_token * kEl};
+        token_at[tid][1] = {token * a.k_token * kEl, (page * a.ck_page + place * a.ck_token) * kCached};
+        token_at[tid][2] = {token * a.v_token * kEl, (page * a.cv_page + place * a.cv_token) * kCached};
+    }
+    for (int i = tid; i < tokens * a.pairs; i += kAppendThreads) {
+        const int t = i / a.pairs, pair = i - t * a.pairs;
+        const float2 by = turn(a.positions[token0 + t], a.inv_freq[pair]);
+        cosines[t][pair] = by.x;
+        sines[t][pair] = by.y;
+    }
+    __syncthreads();
+
+    struct Item { int t, row; };                             // rows of a token, then of the next, `groups` apart
+    const auto settle = [&](Item& i) {
+        while (i.row >= rows && i.t < tokens) i.row -= rows, ++i.t;
+    };
+    Run<T, W> raw[kAhead][2] = {};                           // zeros where nothing is read
+    Item asked{0, tid / lanes};
+    settle(asked);
+    const auto fetch = [&](Run<T, W> (&to)[2]) {
+        if (asked.t < tokens) {
+            const char* p = head_at[asked.row].src + token_at[asked.t][asked.row < q_rows ? 0 : asked.row < k_rows ? 1 : 2].src;
+            if (has0) to[0] = *reinterpret_cast<const Run<T, W>*>(p + run0 * kEl);
+            if (has1) to[1] = *reinterpret_cast<const Run<T, W>*>(p + run1 * kEl);
+        }
+        asked.row += groups;
+        settle(asked);
+    };
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) fetch(raw[n]);
+    Item at{0, tid / lanes};
+    settle(at);
+    const int loops = (tokens * rows + groups - 1) / groups; // the same for every thread: shuffles need them all
 #pragma unroll 1
-        for (int done = 0; done < loops; done += kAhead) {
-            if (t || done) fetch(token, first + done * step);
+    for (int n = 0; n < loops; ++n) {
+        const bool live = at.t < tokens;
+        const int t = live ? at.t : 0, row = live ? at.row : 0, kind = row < q_rows ? 0 : row < k_rows ? 1 : 2;
+        float x[W], y[W];
+        unpack(x, raw[0][0]);
+        unpack(y, raw[0][1]);
 #pragma unroll
-            for (int n = 0; n < kAhead; ++n) {
-                if (done + n >= loops) continue;
-                const int i = first + (done + n) * step;
-                const bool live = mine && i < rows;
-                const Row r = row_of(a, i);
-                float x[8];
+        for (int m = 0; m + 1 < kAhead; ++m) raw[m][0] = raw[m + 1][0], raw[m][1] = raw[m + 1][1];
+        fetch(raw[kAhead - 1]);
+        if (turned && kind < 2) {
+            float cosine[W], sine[W];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = live ? to_float(raw[n].v[e]) : 0.0f;
-                if (a.pairs) {
-                    float y[8];
+            for (int e = 0; e < W; e += 4) {
+                *reinterpret_cast<float4*>(cosine + e) = *reinterpret_cast<const float4*>(&cosines[t][j * W + e]);
+                *reinterpret_cast<float4*>(sine + e) = *reinterpret_cast<const float4*>(&sines[t][j * W + e]);
+            }
+            if (!a.interleaved) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = a.interleaved ? x[e ^ 1] : __shfl_sync(0xffffffffu, x[e], partner);
-                    if (turned && r.kind < 2) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (8 * j + e < 2 * a.pairs) x[e] = fmaf(x[e], cosine[e], y[e] * sine[e]);
-                    }
+                for (int e = 0; e < W; ++e) {
+                    const float u = x[e];
+                    x[e] = fmaf(u, cosine[e], -y[e] * sine[e]);
+                    y[e] = fmaf(u, sine[e], y[e] * cosine[e]);
                 }
-                if (r.kind == 0 && live) store_vec(static_cast<T*>(a.q_out) + token * a.o_token + r.head * a.o_head + 8 * j, x);
-                if constexpr (Q8) {
-                    const bool e4m3 = a.code_type == PP_E4M3;
-                    float most = 0.0f;
+            } else {                                         // element 2 e of the 2 W neighbours and the one behind it
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) most = max_or_nan(most, fabsf(x[e]));
-                    for (int o = 1; o < lanes; o <<= 1) most = max_or_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
-                    if (r.kind != 0 && live && stored) {
-                        const float scale = scale_of(most, e4m3);
-                        uint32_t u[2] = {0, 0};
-                        if (scale != 0.0f) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) u[e / 4] |= (uint32_t)code_of(x[e], scale, e4m3) << (8 * (e & 3));
-                        }
-                        uint8_t* dst = r.kind == 1 ? static_cast<uint8_t*>(a.ck) + page * a.ck_page + place * a.ck_token + r.head * a.ck_head
-                                                   : static_cast<uint8_t*>(a.cv) + page * a.cv_page + place * a.cv_token + r.head * a.cv_head;
-                        *reinterpret_cast<uint2*>(dst + 8 * j) = make_uint2(u[0], u[1]);
-                        if (j == 0) (r.kind == 1 ? a.ks : a.vs)[slot * a.kv_heads + r.head] = scale;
+                for (int e = 0; e < W; ++e) {
+                    float &p = e < W / 2 ? x[2 * (e % (W / 2))] : y[2 * (e % (W / 2))], &q = e < W / 2 ? x[2 * (e % (W / 2)) + 1] : y[2 * (e % (W / 2)) + 1];
+                    const float u = p;
+                    if (e < turned) {
+                        p = fmaf(u, cosine[e], -q * sine[e]);
+                        q = fmaf(u, sine[e], q * cosine[e]);
                     }
-                } else if (r.kind != 0 && live && stored) {
-                    T* dst = r.kind == 1 ? static_cast<T*>(a.ck) + page * a.ck_page + place * a.ck_token + r.head * a.ck_head
-                                         : static_cast<T*>(a.cv) + page * a.cv_page + place * a.cv_token + r.head * a.cv_head;
-                    store_vec(dst + 8 * j, x);
                 }
             }
         }
-        slot = next_slot;
+        char* to = head_at[row].dst + token_at[t][kind].dst;
+        if (!Q8 || kind == 0) {
+            if (live && (kind == 0 || slots[t] >= 0)) {
+                if (has0) store_run(reinterpret_cast<T*>(to) + run0, x);
+                if (has1) store_run(reinterpret_cast<T*>(to) + run1, y);
+            }
+        }
+        if (Q8 && __any_sync(0xffffffffu, kind != 0 && live)) {
+            const bool e4m3 = a.code_type == PP_E4M3;
+            float most = 0.0f;
+#pragma unroll
+            for (int e = 0; e < W; ++e) most = max_or_nan(max_or_nan(most, fabsf(x[e])), fabsf(y[e]));
+            for (int o = 1; o < lanes; o <<= 1) most = max_or_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
+            if (kind != 0 && live && slots[t] >= 0) {
+                const float scale = scale_of(most, e4m3);
+                Run<uint8_t, W> u, w;
+                float up;
+                const float by = inverse_of(scale, up);
+#pragma unroll
+                for (int e = 0; e < W; ++e) x[e] = x[e] * up * by, y[e] = y[e] * up * by;
+#pragma unroll
+                for (int e = 0; e < W; e += 4) u.word[e / 4] = four_codes(x + e, e4m3), w.word[e / 4] = four_codes(y + e, e4m3);
+                if (has0) *reinterpret_cast<Run<uint8_t, W>*>(to + run0) = u;
+                if (has1) *reinterpret_cast<Run<uint8_t, W>*>(to + run1) = w;
+                if (j == 0) (kind == 1 ? a.ks : a.vs)[slots[t] * a.kv_heads + (row - (kind == 1 ? q_rows : k_rows))] = scale;
+            }
+        }
+        at.row += groups;
+        settle(at);
     }
 }
 
@@ -374,9 +444,17 @@ __global__ void __launch_bounds__(kAppendThreads) append_any_kernel(const Append
             for (int o = 16; o; o >>= 1) most = max_or_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
             const float scale = scale_of(most, e4m3);
             uint8_t* dst = static_cast<uint8_t*>(cache) + at;
+            float up;
+            const float by = inverse_of(scale, up);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                if (lane + 32 * e < a.dim) dst[lane + 32 * e] = scale != 0.0f ? code_of(x[e], scale, e4m3) : 0;
+            for (int e = 0; e < kPer; ++e) x[e] = x[e] * up * by;
+#pragma unroll
+            for (int e = 0; e < kPer; e += 4) {
+                const uint32_t four = four_codes(x + e, e4m3);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (lane + 32 * (e + i) < a.dim) dst[lane + 32 * (e + i)] = (uint8_t)(four >> (8 * i));
+            }
             if (lane == 0) (r.kind == 1 ? a.ks : a.vs)[slot * a.kv_heads + r.head] = scale;
         } else {
             T* dst = static_cast<T*>(cache) + at;
@@ -387,16 +465,23 @@ __global__ void __launch_bounds__(kAppendThreads) append_any_kernel(const Append
     }
 }
 
-template <typename T> cudaError_t launch_append(AppendArgs& a, bool vec, int tokens, cudaStream_t stream) {
+template <typename T, bool Q8> cudaError_t launch_append(AppendArgs& a, int width, cudaStream_t stream) {
+    if (width) {
+        const int runs = (a.dim + 2 * width - 1) / (2 * width);
+        a.lanes = 1;
+        while (a.lanes < runs) a.lanes *= 2;
+    }
     const int rows = a.heads + 2 * a.kv_heads;
-    const int at_once = vec ? kAppendThreads / a.lanes : kAppendThreads / 32;
+    const int at_once = width ? kAppendThreads / a.lanes : kAppendThreads / 32;
     // a CTA per token where tokens fill the GPU; else a token's heads are divided, down to one to a group of lanes
-    int parts = 1;
-    while (parts * at_once < rows && (int64_t)tokens * parts < 4 * (int64_t)sm_count()) ++parts;
+    int parts = width ? (rows + kMaxRows - 1) / kMaxRows : 1;
+    while (parts * at_once < rows && (int64_t)a.tokens * parts < 4 * (int64_t)sm_count()) ++parts;
+    a.per_part = (rows + parts - 1) / parts;
+    parts = (rows + a.per_part - 1) / a.per_part;
     // many tokens: four to a CTA, whose sines then cost one trip through the long way of 64-bit arithmetic
-    if (vec && tokens >= 16 * sm_count()) a.per_cta = kMaxTokens;
-    auto k = !vec ? append_any_kernel<T> : a.code_type == PP_E4M3 || a.code_type == PP_I8 ? append_kernel<T, true> : append_kernel<T, false>;
-    return launch_pdl(k, dim3((unsigned)(((int64_t)tokens + a.per_cta - 1) / a.per_cta), (unsigned)parts), dim3(kAppendThreads), 0, stream, 1, a);
+    if (width && a.tokens >= 16 * sm_count()) a.per_cta = kMaxTokens;
+    const dim3 grid((unsigned)(((int64_t)a.tokens + a.per_cta - 1) / a.per_cta), (unsigned)parts);
+    return launch_pdl(width == 8 ? append_kernel<T, Q8, sizeof(T) == 4 ? 4 : 8> : width == 4 ? append_kernel<T, Q8, 4> : append_any_kernel<T>, grid, dim3(kAppendThreads), 0, stream, 1, a);
 }
 
 }  // namespace
@@ -495,14 +580,19 @@ extern "C" pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q
     AppendArgs a{q, k, v, q_out, c.k, c.v, c.k_scales, c.v_scales, slots, positions, inv_freq,
                  q_token, q_head, o_token, o_head, k_token, k_head, v_token, v_head,
                  c.k_page, c.k_token, c.k_head, c.v_page, c.v_token, c.v_head, (int64_t)c.pages * c.page_size,
-                 heads, c.kv_heads, dim, c.page_size, pairs, interleaved != 0, c.dtype, tokens, 8, 1};
-    while (a.lanes * 8 < dim) a.lanes *= 2;
-    // eight elements to an access where every row starts on one, and pairs of halves lie whole lanes apart
-    const auto wide = [&](const void* p, int64_t token, int64_t head, int n) { return !p || row_alignment(p, 1, 0, tokens, token, n, head, tb) == 16; };
-    const bool vec = dim % 8 == 0 && (interleaved || pairs % 8 == 0) && wide(q, q_token, q_head, heads) && wide(q_out, o_token, o_head, heads) &&
-                     wide(k, k_token, k_head, c.kv_heads) && wide(v, v_token, v_head, c.kv_heads) && cache_alignment(c) >= (is_8bit(c.dtype) ? 8 : 16);
+                 heads, c.kv_heads, dim, c.page_size, pairs, interleaved != 0, c.dtype, tokens, 1, 1, 1};
+    // eight or four elements to an access where every row starts on one, and runs of pairs are whole ones
+    const auto alignment = [&](const void* p, int64_t token, int64_t head, int n) { return !p ? 16 : row_alignment(p, 1, 0, tokens, token, n, head, tb); };
+    const int rows_on = std::min({alignment(q, q_token, q_head, heads), alignment(q_out, o_token, o_head, heads), alignment(k, k_token, k_head, c.kv_heads),
+                                  alignment(v, v_token, v_head, c.kv_heads)}), cache_on = cache_alignment(c);
+    const auto fits = [&](int w) {
+        return dim % w == 0 && (interleaved || pairs % w == 0) && rows_on >= std::min(16, w * tb) && cache_on >= std::min(16, w * type_bytes(c.dtype));
+    };
+    const int width = dtype != PP_F32 && fits(8) ? 8 : fits(4) ? 4 : 0;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    const cudaError_t e = dtype == PP_F32 ? launch_append<float>(a, vec, tokens, s)
-                        : dtype == PP_F16 ? launch_append<__half>(a, vec, tokens, s) : launch_append<__nv_bfloat16>(a, vec, tokens, s);
+    const bool q8 = is_8bit(c.dtype);
+    const cudaError_t e = dtype == PP_F32   ? (q8 ? launch_append<float, true>(a, width, s) : launch_append<float, false>(a, width, s))
+                          : dtype == PP_F16 ? (q8 ? launch_append<__half, true>(a, width, s) : launch_append<__half, false>(a, width, s))
+                                            : (q8 ? launch_append<__nv_bfloat16, true>(a, width, s) : launch_append<__nv_bfloat16, false>(a, width, s));
     return status_of(e);
 }
