@@ -39,14 +39,17 @@ struct AttnArgs {
     int64_t q_row, q_head, k_page, k_token, k_head, v_page, v_token, v_head, ld_table;
     Divisor page;
     int pages, page_size, batch, capacity, window, heads, kv_heads, group, chunk, n_chunks, dim, granule, q_type, type;
+    int cluster;                                             // CTAs that share a head (chunk); 0: all heads in a row, cut into equal parts
     bool whole_tiles;                                        // pages are a whole number of tiles long
+    bool wide_out;                                           // four neighbours of out are one access
     float scale;                                             // times log2 e
 };
 
-// The workspace: a note for each CTA (four ints), then two partial results for each.
+// The workspace: a note for each CTA (four ints), then two partial results for each.  A partial result: m and l of each head of the
+// chunk, then their sums, all on 16 bytes.
 __host__ __device__ inline int64_t notes_floats(int64_t ctas) { return 4 * ctas; }
-// Floats of a partial result: m and l of each head of the chunk, then the sums.
-__host__ __device__ inline int64_t part_floats(int chunk, int dim) { return (int64_t)chunk * (dim + 2); }
+__host__ __device__ inline int up4(int n) { return (n + 3) & ~3; }
+__host__ __device__ inline int64_t part_floats(int chunk, int dim) { return 2 * up4(chunk) + (int64_t)chunk * up4(dim); }
 
 __device__ __forceinline__ int first_position(const AttnArgs& a, int length) { return a.window > 0 ? max(0, length - a.window) : 0; }
 // Units start at a whole tile: where pages are whole tiles long, no tile then crosses from one page into another.
@@ -79,11 +82,39 @@ template <int HEADS, int DT> __device__ __forceinline__ void stage_q(const AttnA
     else if (a.q_type == PP_F16) stage_q<HEADS, DT>(a, static_cast<const __half*>(a.q) + at, n_heads, to);
     else stage_q<HEADS, DT>(a, static_cast<const float*>(a.q) + at, n_heads, to);
 }
-__device__ __forceinline__ void store_out(const AttnArgs& a, int64_t at, float v) {
-    if (a.q_type == PP_F32) static_cast<float*>(a.out)[at] = v;
-    else if (a.q_type == PP_F16) static_cast<__half*>(a.out)[at] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
+// Dimensions d .. d + 3 of a row of out.
+__device__ __forceinline__ void store_out(const AttnArgs& a, int64_t row, int d, float4 v) {
+    const int64_t at = row * a.dim + d;
+    if (a.wide_out) {
+        if (a.q_type == PP_F32) {
+            *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = v;
+        } else if (a.q_type == PP_F16) {
+            const __half2 x = __floats2half2_rn(v.x, v.y), y = __floats2half2_rn(v.z, v.w);
+            *reinterpret_cast<uint2*>(static_cast<__half*>(a.out) + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+        } else {
+            const __nv_bfloat162 x = __floats2bfloat162_rn(v.x, v.y), y = __floats2bfloat162_rn(v.z, v.w);
+            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+        }
+        return;
+    }
+    const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (d + i >= a.dim) break;
+        if (a.q_type == PP_F32) static_cast<float*>(a.out)[at + i] = f[i];
+        else if (a.q_type == PP_F16) static_cast<__half*>(a.out)[at + i] = __float2half_rn(f[i]);
+        else static_cast<__nv_bfloat16*>(a.out)[at + i] = __float2bfloat16_rn(f[i]);
+    }
 }
+__device__ __forceinline__ float4 add4(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+__device__ __forceinline__ float4 fma4(float4 a, float by, float4 b) { return make_float4(fmaf(a.x, by, b.x), fmaf(a.y, by, b.y), fmaf(a.z, by, b.z), fmaf(a.w, by, b.w)); }
+// A sum over l, 0 where nothing was summed.
+__device__ __forceinline__ float4 over(float4 v, float l) {
+    if (l == 0.0f) return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    return make_float4(__fdiv_rn(v.x, l), __fdiv_rn(v.y, l), __fdiv_rn(v.z, l), __fdiv_rn(v.w, l));
+}
+// exp2(m - top), 0 for a part without positions.
+__device__ __forceinline__ float weight_of(float m, float top) { return m == -INFINITY ? 0.0f : exp2_fast(m - top); }
 
 template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there) {   // zeros if not there
     if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -193,6 +224,14 @@ __device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, int at, ui
     return bits;
 }
 
+// The largest m of a head over the warps.
+template <int HEADS> __device__ __forceinline__ float top_of(const float (*m)[HEADS], int head) {
+    float top = m[0][head];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) top = fmaxf(top, m[w][head]);
+    return top;
+}
+
 // ------------------------------------------------------------------------------------------------ matrix form
 enum Kind { kBf16, kF16, kE4m3, kInt8 };
 
@@ -249,31 +288,54 @@ template <int DT, int NT, int KIND> struct MmaCore {
     static constexpr int kEs = kQ8 ? 1 : 2, kChunks = DT * kEs / 16, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
     static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = kStage <= 5120 ? 4 : 3;
     static constexpr int kHeads = 8 * NT, kMergePitch = DT + 4;
-    static constexpr int kQFloats = kHeads * DT;
+    static constexpr int kDim = DT;
+    static constexpr bool kStagesQ = false;
     // p is at most 2^kLift: f16 numbers below 2^-24 are lost, and a p can be that small beside the largest one
     static constexpr float kLift = kIsBf16 ? 0.0f : 14.0f;
 
     uint32_t q[DT / 16][NT][2];
     float acc[DT / 16][NT][4], m[NT][2], l[NT][2], f[NT][2], vm;
 
-    // from q in shared memory
-    __device__ __forceinline__ void begin(const AttnArgs& a, const float* rows) {
+    // q as the second operand of the scores: head g of each tile, two neighbouring dimensions to a register (16-bit caches), or four
+    // to two registers (codes, as they lie in a lane's bytes).  Rows of q start where such an access may.
+    __device__ __forceinline__ void begin(const AttnArgs& a, int r, int head0, int n_heads) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-        const bool split = kQ8 && a.q_type == PP_F32;
         float factor[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const bool lows = split && nt == 1;
-            const float* row = rows + (split ? g : nt * 8 + g) * DT;
-            float down = 1.0f;                               // a power of two that brings the head's largest below 2: f16 ends at 65504
             factor[nt] = a.scale;
-            if constexpr (kQ8) {
-                float most = 0.0f;
+            if constexpr (!kQ8) {
+                const uint32_t* row = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(a.q) + r * a.q_row + (int64_t)(head0 + nt * 8 + g) * a.q_head) + t;
+                const bool live = nt * 8 + g < n_heads;
 #pragma unroll
-                for (int j = 0; j < DT / 16; ++j) {
-                    const float4 x = *reinterpret_cast<const float4*>(row + 16 * j + 4 * t);
-                    most = fmaxf(fmaxf(fmaxf(most, fabsf(x.x)), fmaxf(fabsf(x.y), fabsf(x.z))), fabsf(x.w));
+                for (int j = 0; j < DT / 16; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) q[j][nt][i] = live && 16 * j + 8 * i + 2 * t < a.dim ? row[8 * j + 4 * i] : 0u;
+            } else {
+                const bool split = NT == 2 && a.q_type == PP_F32, lows = split && nt == 1;
+                const int head = split ? g : nt * 8 + g;
+                const int64_t row = r * a.q_row + (int64_t)(head0 + head) * a.q_head + 4 * t;
+                const bool live = head < n_heads;
+                float4 x[DT / 16];
+                if (a.q_type == PP_F32) {
+#pragma unroll
+                    for (int j = 0; j < DT / 16; ++j)
+                        x[j] = live && 16 * j + 4 * t < a.dim ? *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + row + 16 * j) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                } else {
+                    uint2 raw[DT / 16];
+#pragma unroll
+                    for (int j = 0; j < DT / 16; ++j)
+                        raw[j] = live && 16 * j + 4 * t < a.dim ? *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.q) + row + 16 * j) : make_uint2(0u, 0u);
+#pragma unroll
+                    for (int j = 0; j < DT / 16; ++j) {
+                        const float2 u = a.q_type == PP_F16 ? unpack2<false>(raw[j].x) : unpack2<true>(raw[j].x);
+                        const float2 v = a.q_type == PP_F16 ? unpack2<false>(raw[j].y) : unpack2<true>(raw[j].y);
+                        x[j] = make_float4(u.x, u.y, v.x, v.y);
+                    }
                 }
+                float most = 0.0f, down = 1.0f;              // down: a power of two that brings the head's largest below 2, for f16 ends at 65504
+#pragma unroll
+                for (int j = 0; j < DT / 16; ++j) most = fmaxf(fmaxf(fmaxf(most, fabsf(x[j].x)), fmaxf(fabsf(x[j].y), fabsf(x[j].z))), fabsf(x[j].w));
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
                 if (most > 0.0f && most < INFINITY) {
@@ -281,21 +343,22 @@ template <int DT, int NT, int KIND> struct MmaCore {
                     down = __int_as_float((127 - e) << 23);
                     factor[nt] = a.scale * __int_as_float((127 + e) << 23);
                 }
+#pragma unroll
+                for (int j = 0; j < DT / 16; ++j) {
+                    const float4 v = make_float4(x[j].x * down, x[j].y * down, x[j].z * down, x[j].w * down);
+                    q[j][nt][0] = pack2<false>(v.x, v.y);
+                    q[j][nt][1] = pack2<false>(v.z, v.w);
+                    if (lows) {
+                        const float2 u = unpack2<false>(q[j][nt][0]), w = unpack2<false>(q[j][nt][1]);
+                        q[j][nt][0] = pack2<false>(v.x - u.x, v.y - u.y);
+                        q[j][nt][1] = pack2<false>(v.z - w.x, v.w - w.y);
+                    }
+                }
             }
 #pragma unroll
             for (int j = 0; j < DT / 16; ++j)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int d = kQ8 ? 16 * j + 4 * t + 2 * i : 16 * j + 2 * t + 8 * i;   // codes: four neighbours to a lane, as they lie in its bytes
-                    const float x = row[d] * down, y = row[d + 1] * down;
-                    q[j][nt][i] = pack2<kIsBf16>(x, y);
-                    if (lows) {
-                        const float2 high = unpack2<kIsBf16>(q[j][nt][i]);
-                        q[j][nt][i] = pack2<kIsBf16>(x - high.x, y - high.y);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[j][nt][k] = 0.0f;
-                }
+                for (int k = 0; k < 4; ++k) acc[j][nt][k] = 0.0f;
         }
         vm = 0.0f;
 #pragma unroll
@@ -308,7 +371,7 @@ template <int DT, int NT, int KIND> struct MmaCore {
             }
     }
 
-    __device__ __forceinline__ void tile(const AttnArgs& a, uint32_t stage, uint32_t bits, float*) {
+    __device__ __forceinline__ void tile(const AttnArgs& a, uint32_t stage, uint32_t bits) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
         const bool split = kQ8 && a.q_type == PP_F32;
         float s[NT][4];
@@ -469,15 +532,15 @@ template <int DT, int NT, int KIND> struct MmaCore {
                 }
             }
     }
-    // its sums, times a factor by head
-    __device__ __forceinline__ void sums(const AttnArgs&, const float* factor, float* to) {
+    // its sums, relative to the largest m of all warps
+    __device__ __forceinline__ void sums(const float (*all)[kHeads], float* to) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int head = nt * 8 + 2 * t + b;
-                float by = factor[head];
+                float by = weight_of(m[nt][b], top_of<kHeads>(all, head));
                 if (kQ8) by = by == 0.0f ? 0.0f : by * vm;
 #pragma unroll
                 for (int j = 0; j < DT / 16; ++j)
@@ -496,12 +559,13 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
     static constexpr int kEs = 4, kChunks = DT / 4, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
     static constexpr int kHeads = HN, kMergePitch = DT;
     static constexpr int kStage = 2 * kTileBytes + 16 * 4 * HN, kStages = DT == 256 ? 1 : DT == 192 ? 2 : 3;   // behind the rows: p by position and head
-    static constexpr int kQFloats = HN * DT;
+    static constexpr int kDim = DT;
+    static constexpr bool kStagesQ = true;
     static constexpr float kLift = 0.0f;
 
     float acc[DT / 32][HN], m[HN], l[HN];
 
-    __device__ __forceinline__ void begin(const AttnArgs&, const float*) {
+    __device__ __forceinline__ void begin() {
 #pragma unroll
         for (int h = 0; h < HN; ++h) {
             m[h] = -INFINITY;
@@ -619,12 +683,14 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
             }
         }
     }
-    __device__ __forceinline__ void sums(const AttnArgs&, const float* factor, float* to) {
+    __device__ __forceinline__ void sums(const float (*all)[kHeads], float* to) {
         const int lane = threadIdx.x & 31;
 #pragma unroll
-        for (int h = 0; h < HN; ++h)
+        for (int h = 0; h < HN; ++h) {
+            const float by = weight_of(m[h], top_of<kHeads>(all, h));
 #pragma unroll
-            for (int i = 0; i < DT / 32; ++i) to[h * kMergePitch + lane + 32 * i] = acc[i][h] * factor[h];
+            for (int i = 0; i < DT / 32; ++i) to[h * kMergePitch + lane + 32 * i] = acc[i][h] * by;
+        }
     }
 };
 
@@ -668,48 +734,83 @@ struct Note {
     int second;                                              // the first one's part is the second of its two
 };
 
+// Thread-block clusters: a wait for all CTAs that also shows their writes, and reads of another CTA's shared memory.
+__device__ __forceinline__ void cluster_wait() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t at_rank(const void* p, int rank) {
+    uint32_t d;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(smem_at(p)), "r"(rank));
+    return d;
+}
+__device__ __forceinline__ float load_remote(uint32_t at) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 load_remote4(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ float lse_of(float m, float l, float lift) { return l == 0.0f ? -INFINITY : (m - lift + log2f(l)) * kLn2; }
+
 template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) attn_kernel(const __grid_constant__ AttnArgs a) {
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ int warp_sums[kWarps], found_base, found;
-    __shared__ float warp_m[kWarps][Core::kHeads], warp_l[kWarps][Core::kHeads], factors[kWarps][Core::kHeads], all_m[Core::kHeads], all_l[Core::kHeads];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ float warp_m[kWarps][Core::kHeads], warp_l[kWarps][Core::kHeads], all_m[Core::kHeads], all_l[Core::kHeads];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
     pdl_release();
     pdl_wait();
 
     const int per_request = a.kv_heads * a.n_chunks;
-    const int each = (a.batch + kThreads - 1) / kThreads, r0 = min(tid * each, a.batch), r1 = min(r0 + each, a.batch);
-    int mine = 0, all;
-    for (int r = r0; r < r1; ++r) mine += units_of(a, r) * per_request;
-    const int before = sum_before(mine, warp_sums, all);
-    const int n = min((int)gridDim.x, all), c = blockIdx.x;
-    Note* note = a.ws ? reinterpret_cast<Note*>(a.ws) + c : nullptr;
-    if (note && tid == 0) note->last = -1;
-    if (c >= n) return;
-    const Cut cut(all, n);
-    int u = cut.start(c);
-    const int begin = u, end = cut.start(c + 1);
-    if (u >= before && u < before + mine) {
-        int base = before, r = r0;
-        for (;; ++r) {
-            const int units = units_of(a, r) * per_request;
-            if (u < base + units) break;
-            base += units;
+    int r, base = 0, u = 0, begin = 0, end = 1, ctas = 0, all = 0;    // unit u of the row of all, request r's from base on
+    if (a.cluster) {
+        r = c / a.cluster / per_request;
+    } else {
+        const int each = (a.batch + kThreads - 1) / kThreads, r0 = min(tid * each, a.batch), r1 = min(r0 + each, a.batch);
+        int mine = 0;
+        for (r = r0; r < r1; ++r) mine += units_of(a, r) * per_request;
+        const int before = sum_before(mine, warp_sums, all);
+        ctas = min((int)gridDim.x, all);
+        if (tid == 0) reinterpret_cast<Note*>(a.ws)[c].last = -1;
+        if (c >= ctas) return;
+        const Cut cut(all, ctas);
+        u = begin = cut.start(c);
+        end = cut.start(c + 1);
+        if (u >= before && u < before + mine) {
+            base = before;
+            for (r = r0;; ++r) {
+                const int units = units_of(a, r) * per_request;
+                if (u < base + units) break;
+                base += units;
+            }
+            found = r;
+            found_base = base;
         }
-        found = r;
-        found_base = base;
+        __syncthreads();
+        r = found;
+        base = found_base;
     }
-    __syncthreads();
-    int r = found, base = found_base;
 
     unsigned char* own = ring + warp * Core::kStages * Core::kStage;
     float* q = reinterpret_cast<float*>(ring + kWarps * Core::kStages * Core::kStage);
     float* merge = reinterpret_cast<float*>(ring);           // after the tiles, in their place: [warp][head][kMergePitch]
-    Core core;
     while (u < end) {
-        const int units = units_of(a, r);
-        const int unit = u - base, hc = unit / units, t0 = unit - hc * units;
-        const int t1 = min(units, t0 + (end - u));
-        const int length = length_of(a, r), low = first_tile(a, length);
+        const int length = length_of(a, r), low = first_tile(a, length), units = units_of(a, r);
+        int hc, t0, t1;
+        if (a.cluster) {
+            const int segment = c / a.cluster, rank = c - segment * a.cluster;
+            const Cut cut(units, a.cluster);
+            hc = segment - r * per_request;
+            t0 = cut.start(rank);
+            t1 = cut.start(rank + 1);
+        } else {
+            hc = (u - base) / units;
+            t0 = u - base - hc * units;
+            t1 = min(units, t0 + (end - u));
+        }
         const int kv = hc / a.n_chunks, head_in = (hc - kv * a.n_chunks) * a.chunk, n_heads = min(a.chunk, a.group - head_in);
         const int head0 = kv * a.group + head_in;
 
@@ -738,13 +839,18 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
             ++asked;
             if (++stage == Core::kStages) stage = 0;
         };
+        Core core;
         int at = 0;
 #pragma unroll 1
         for (int i = 1 - Core::kStages;; ++i) {              // one call of request: its code is long
             if (i == 0) {
-                stage_q<Core::kHeads, Core::kQFloats / Core::kHeads>(a, r, head0, n_heads, q);
-                __syncthreads();
-                core.begin(a, q);
+                if constexpr (Core::kStagesQ) {
+                    stage_q<Core::kHeads, Core::kDim>(a, r, head0, n_heads, q);
+                    __syncthreads();
+                    core.begin();
+                } else {
+                    core.begin(a, r, head0, n_heads);
+                }
             }
             if (i >= tiles) break;
             if (i >= 0) {
@@ -758,50 +864,74 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
                 __syncwarp();
             }
             const uint32_t bits = (uint32_t)(there >> (16 * at)) & 0xffffu;
-            if constexpr (std::is_same_v<decltype(&Core::tile), void (Core::*)(const AttnArgs&, uint32_t, uint32_t, float*)>)
-                core.tile(a, smem_at(own + at * Core::kStage), bits, q);
-            else core.tile(a, reinterpret_cast<float*>(own + at * Core::kStage), bits, q);
+            if constexpr (Core::kStagesQ) core.tile(a, reinterpret_cast<float*>(own + at * Core::kStage), bits, q);
+            else core.tile(a, smem_at(own + at * Core::kStage), bits);
             if (++at == Core::kStages) at = 0;
         }
         wait_but<0>();
         core.state(warp_m[warp], warp_l[warp]);
         __syncthreads();                                     // the ring is free, and every warp's m and l are known
-        if (tid < kWarps * Core::kHeads) {
-            const int w = tid / Core::kHeads, h = tid % Core::kHeads;
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < kWarps; ++i) top = fmaxf(top, warp_m[i][h]);
-            const auto weight = [&](int i) { return warp_m[i][h] == -INFINITY ? 0.0f : exp2_fast(warp_m[i][h] - top); };
-            factors[w][h] = weight(w);
-            if (w == 0) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int i = 0; i < kWarps; ++i) sum += warp_l[i][h] * weight(i);
-                all_m[h] = top;
-                all_l[h] = sum;
-            }
-        }
-        __syncthreads();
-        core.sums(a, factors[warp], merge + warp * Core::kHeads * Core::kMergePitch);
-        __syncthreads();
-        const bool whole = t0 == 0 && t1 == units;
-        float* part = whole ? nullptr : a.ws + notes_floats(gridDim.x) + (2 * c + (u != begin)) * part_floats(a.chunk, a.dim);
-        if (!whole && t0 == 0 && tid == 0) *note = {cut.of(base + (hc + 1) * units - 1), r * a.heads + head0, n_heads, u != begin};
-        for (int i = tid; i < n_heads * a.dim; i += kThreads) {
-            const int h = i / a.dim, d = i - h * a.dim;
+        core.sums(warp_m, merge + warp * Core::kHeads * Core::kMergePitch);
+        if (tid < Core::kHeads) {
+            const float top = top_of<Core::kHeads>(warp_m, tid);
             float sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) sum += merge[(w * Core::kHeads + h) * Core::kMergePitch + d];
-            if (whole) store_out(a, ((int64_t)r * a.heads + head0 + h) * a.dim + d, all_l[h] == 0.0f ? 0.0f : __fdiv_rn(sum, all_l[h]));
-            else part[2 * a.chunk + i] = sum;
+            for (int w = 0; w < kWarps; ++w) sum += warp_l[w][tid] * weight_of(warp_m[w][tid], top);
+            all_m[tid] = top;
+            all_l[tid] = sum;
         }
-        if (tid < n_heads) {
-            if (!whole) {
+        __syncthreads();
+        const bool whole = t0 == 0 && t1 == units && a.cluster <= 1;
+        const int64_t row0 = (int64_t)r * a.heads + head0;
+        float* part = whole || a.cluster ? nullptr : a.ws + notes_floats(gridDim.x) + (2 * c + (u != begin)) * part_floats(a.chunk, a.dim);
+        constexpr int kFours = Core::kDim / 4;               // of a row
+        for (int i = tid; i < n_heads * kFours; i += kThreads) {
+            const int h = i / kFours, d = 4 * (i - h * kFours);
+            if (d >= a.dim) continue;
+            float4* at = reinterpret_cast<float4*>(merge + h * Core::kMergePitch + d);
+            float4 sum = *at;
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) sum = add4(sum, *(at + w * Core::kHeads * Core::kMergePitch / 4));
+            if (whole) store_out(a, row0 + h, d, over(sum, all_l[h]));
+            else if (part) *reinterpret_cast<float4*>(part + 2 * up4(a.chunk) + h * up4(a.dim) + d) = sum;
+            else *at = sum;
+        }
+        if (part) {
+            if (t0 == 0 && tid == 0) reinterpret_cast<Note*>(a.ws)[c] = {Cut(all, ctas).of(base + (hc + 1) * units - 1), (int)row0, n_heads, u != begin};
+            if (tid < n_heads) {
                 part[tid] = all_m[tid];
-                part[a.chunk + tid] = all_l[tid];
-            } else if (a.lse) {
-                a.lse[(int64_t)r * a.heads + head0 + tid] = all_l[tid] == 0.0f ? -INFINITY : (all_m[tid] - Core::kLift + log2f(all_l[tid])) * kLn2;
+                part[up4(a.chunk) + tid] = all_l[tid];
             }
+        } else if (whole && a.lse && tid < n_heads) {
+            a.lse[row0 + tid] = lse_of(all_m[tid], all_l[tid], Core::kLift);
+        }
+        if (a.cluster) {
+            if (a.cluster == 1) return;
+            // the parts of the cluster's CTAs, each of which joins a share of the rows
+            const int rank = c % a.cluster;
+            cluster_wait();
+            for (int i = tid + rank * kThreads; i < n_heads * kFours; i += kThreads * a.cluster) {
+                const int h = i / kFours, d = 4 * (i - h * kFours);
+                if (d >= a.dim) continue;
+                float m[8], top = -INFINITY, l = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    m[k] = k < a.cluster ? load_remote(at_rank(&all_m[h], k)) : -INFINITY;
+                    top = fmaxf(top, m[k]);
+                }
+                float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (k >= a.cluster) break;
+                    const float w = weight_of(m[k], top);
+                    l = fmaf(load_remote(at_rank(&all_l[h], k)), w, l);
+                    sum = fma4(load_remote4(at_rank(merge + h * Core::kMergePitch + d, k)), w, sum);
+                }
+                store_out(a, row0 + h, d, over(sum, l));
+                if (a.lse && d == 0) a.lse[row0 + h] = lse_of(top, l, Core::kLift);
+            }
+            cluster_wait();                                  // nobody leaves while another reads its shared memory
+            return;
         }
         __syncthreads();
         u += t1 - t0;
@@ -815,8 +945,9 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
 // Joins the parts of the head (chunk) that CTA blockIdx.x has noted, if it has: as many warps to a row of out as there are, each
 // with its share of the parts.
 constexpr int kJoinWarps = 16, kJoinThreads = kJoinWarps * 32;
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttnArgs a, float lift) {
-    __shared__ float sums[kJoinWarps][kMaxHeadDim], ls[kJoinWarps];
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttnArgs a, float lift) {
+    __shared__ float4 sums[kJoinWarps][kMaxHeadDim / 4];
+    __shared__ float ls[kJoinWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
     pdl_release();
     pdl_wait();
@@ -826,40 +957,39 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttnArgs a, fl
     const int per = kJoinWarps / note.n_heads, h = warp / per, sub = warp - h * per;
     const bool live = h < note.n_heads;
     const int64_t floats = part_floats(a.chunk, a.dim);
-    const float* parts = a.ws + notes_floats(gridDim.x) + h;
+    const float* parts = a.ws + notes_floats(gridDim.x);
     const auto part = [&](int c) { return parts + (2 * c + (c == c0 ? note.second : 0)) * floats; };
-    constexpr int kPer = kMaxHeadDim / 32;
-    float top = -INFINITY, l = 0.0f, acc[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] = 0.0f;
+    const int chunk4 = up4(a.chunk), dim4 = up4(a.dim);
+    float top = -INFINITY, l = 0.0f;
+    float4 acc[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
     if (live) {
-        for (int c = c0 + lane; c <= note.last; c += 32) top = fmaxf(top, *part(c));
+        for (int c = c0 + lane; c <= note.last; c += 32) top = fmaxf(top, part(c)[h]);
 #pragma unroll
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
 #pragma unroll 4
         for (int c = c0 + sub; c <= note.last; c += per) {
             const float* p = part(c);
-            const float m = p[0], w = m == -INFINITY ? 0.0f : exp2_fast(m - top);
-            l += p[a.chunk] * w;
-            const float* x = p - h + 2 * a.chunk + h * a.dim + lane;
+            const float w = weight_of(p[h], top);
+            l = fmaf(p[chunk4 + h], w, l);
+            const float4* x = reinterpret_cast<const float4*>(p + 2 * chunk4 + h * dim4) + lane;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (lane + 32 * i < a.dim) acc[i] += x[32 * i] * w;
+            for (int i = 0; i < 2; ++i)
+                if (4 * (lane + 32 * i) < a.dim) acc[i] = fma4(x[32 * i], w, acc[i]);
         }
     }
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) sums[warp][lane + 32 * i] = acc[i];
+    for (int i = 0; i < 2; ++i) sums[warp][lane + 32 * i] = acc[i];
     if (lane == 0) ls[warp] = l;
     __syncthreads();
     if (!live || sub) return;
     l = 0.0f;
     for (int w = 0; w < per; ++w) l += ls[warp + w];
-    for (int d = lane; d < a.dim; d += 32) {
-        float sum = 0.0f;
-        for (int w = 0; w < per; ++w) sum += sums[warp + w][d];
-        store_out(a, ((int64_t)note.row + h) * a.dim + d, l == 0.0f ? 0.0f : __fdiv_rn(sum, l));
+    for (int d = lane; 4 * d < a.dim; d += 32) {
+        float4 sum = sums[warp][d];
+        for (int w = 1; w < per; ++w) sum = add4(sum, sums[warp + w][d]);
+        store_out(a, (int64_t)note.row + h, 4 * d, over(sum, l));
     }
-    if (a.lse && lane == 0) a.lse[(int64_t)note.row + h] = l == 0.0f ? -INFINITY : (top - lift + log2f(l)) * kLn2;
+    if (a.lse && lane == 0) a.lse[(int64_t)note.row + h] = lse_of(top, l, lift);
 }
 
 // ------------------------------------------------------------------------------------------------------ choice
@@ -877,7 +1007,7 @@ template <class Core, bool ASYNC> Form form_of() {
     static int resident[PerDeviceOnce::kMaxDevices] = {};
     Form f;
     f.kernel = attn_kernel<Core, ASYNC>;
-    f.smem = std::max(kWarps * Core::kStages * Core::kStage, kWarps * Core::kHeads * Core::kMergePitch * 4) + Core::kQFloats * 4;
+    f.smem = std::max(kWarps * Core::kStages * Core::kStage, kWarps * Core::kHeads * Core::kMergePitch * 4) + (Core::kStagesQ ? Core::kHeads * Core::kDim * 4 : 0);
     f.heads = Core::kHeads;
     f.lift = Core::kLift;
     f.opt_in = &opt_in;
@@ -896,14 +1026,14 @@ template <bool ASYNC> Form scalar_form(int dim, int group) {
     return group <= 1 ? form_of<ScalarCore<256, 1, ASYNC>, ASYNC>() : group <= 4 ? form_of<ScalarCore<256, 4, ASYNC>, ASYNC>() : form_of<ScalarCore<256, 8, ASYNC>, ASYNC>();
 }
 
-// The form of a call, the bytes of its asynchronous copies and its heads per chunk.
-Form choose(const pp_paged_cache_t& c, pp_dtype_t q_type, int group, int& granule, int& chunk) {
+// The form of a call, the bytes of its asynchronous copies and its heads per chunk.  q_on: what divides the starts of q's rows, in bytes.
+Form choose(const pp_paged_cache_t& c, pp_dtype_t q_type, int q_on, int group, int& granule, int& chunk) {
     const int row = c.head_dim * type_bytes(c.dtype);
     granule = std::min(cache_alignment(c), 16);
     while (row % granule) granule /= 2;
     const bool split = is_8bit(c.dtype) && q_type == PP_F32;  // q as two f16 numbers takes both tiles
     chunk = 8;
-    if (granule >= 4 && c.dtype != PP_F32 && !(split && c.head_dim > 128)) {
+    if (granule >= 4 && c.dtype != PP_F32 && !(split && c.head_dim > 128) && q_on >= (!is_8bit(c.dtype) ? 4 : q_type == PP_F32 ? 16 : 8)) {
         // 16 heads where a key-value head has more than 8: above 128 dimensions their sums do not fit the registers
         const bool two = split || (group > 8 && c.head_dim <= 128);
         if (two && !split) chunk = 16;
@@ -948,10 +1078,23 @@ pp_status_t check_call(const pp_paged_cache_t* cache, pp_dtype_t q_type, int bat
     return PP_OK;
 }
 
-// Whether any request can have more than one unit.
-bool divided(const pp_paged_cache_t& c, int width, int window) {
-    const int64_t capacity = (int64_t)width * c.page_size;
-    return (window > 0 ? std::min<int64_t>((int64_t)window + kTile - 1, capacity) : capacity) > kUnit;
+// How a call is divided.
+struct Division {
+    int grid, cluster;                                       // cluster 0: equal parts of all units, joined by a second kernel
+    int64_t bytes;                                           // of workspace
+};
+// A cluster of up to eight CTAs to each head (chunk) needs no workspace, no sums over lengths and no second kernel, some 4 us in all, but
+// leaves SMs idle where heads are few and long, or lengths differ.  It is taken where its longest CTA has at most kMore units
+// more than an equal part would have, going by the table's width.
+constexpr int kMore = 3;
+Division divide(const pp_paged_cache_t& c, int batch, int width, int window, int chunk, int n_chunks, int resident) {
+    const int64_t capacity = (int64_t)width * c.page_size, longest = window > 0 ? std::min<int64_t>((int64_t)window + kTile - 1, capacity) : capacity;
+    const int64_t units = std::max<int64_t>(1, (longest + kUnit - 1) / kUnit), heads = (int64_t)batch * c.kv_heads * n_chunks;
+    int cluster = 1;
+    while (cluster < 8 && cluster < units && 2 * cluster * heads <= resident) cluster *= 2;
+    const int64_t waves = (heads * cluster + resident - 1) / resident, own = (units + cluster - 1) / cluster;
+    if (units == 1 || waves * own <= heads * units / resident + kMore) return {(int)(heads * cluster), cluster, 0};
+    return {resident, 0, (notes_floats(resident) + (int64_t)resident * 2 * part_floats(chunk, c.head_dim)) * 4};
 }
 
 }  // namespace
@@ -963,11 +1106,17 @@ extern "C" pp_status_t pp_paged_attention_workspace(const pp_paged_cache_t* cach
     if (!bytes) return PP_ERR_INVALID_ARG;
     *bytes = 0;
     if (const pp_status_t st = check_call(cache, q_type, batch, heads, width, window)) return st;
-    if (batch == 0 || !divided(*cache, width, window)) return PP_OK;
-    int granule, chunk, grid;
-    const Form f = choose(*cache, q_type, heads / cache->kv_heads, granule, chunk);
-    if (const cudaError_t e = grid_of(f, grid)) return status_of(e);
-    *bytes = (notes_floats(grid) + (int64_t)grid * 2 * part_floats(chunk, cache->head_dim)) * 4;
+    if (batch == 0) return PP_OK;
+    // enough for any alignment of q
+    int64_t most = 0;
+    for (const int q_on : {1, 16}) {
+        int granule, chunk, resident;
+        const int group = heads / cache->kv_heads;
+        const Form f = choose(*cache, q_type, q_on, group, granule, chunk);
+        if (const cudaError_t e = grid_of(f, resident)) return status_of(e);
+        most = std::max(most, divide(*cache, batch, width, window, chunk, (group + chunk - 1) / chunk, resident).bytes);
+    }
+    *bytes = most;
     return PP_OK;
 }
 
@@ -989,21 +1138,20 @@ extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const v
     const int64_t q_span = ((batch - 1) * q_row + (heads - 1) * q_head + c.head_dim) * tb, out_span = (int64_t)batch * heads * c.head_dim * tb;
     if (spans_meet(q, q_span, out, out_span)) return PP_ERR_INVALID_ARG;
     const int group = heads / c.kv_heads;
-    int granule, chunk, grid;
-    const Form f = choose(c, q_type, group, granule, chunk);
-    if (const cudaError_t e = grid_of(f, grid)) return status_of(e);
-    const bool parts = divided(c, width, window);
-    const int64_t need = parts ? (notes_floats(grid) + (int64_t)grid * 2 * part_floats(chunk, c.head_dim)) * 4 : 0;
-    if (need && (!workspace || workspace_bytes < need)) return PP_ERR_INVALID_ARG;
+    int granule, chunk, resident;
+    const Form f = choose(c, q_type, row_alignment(q, 1, 0, batch, q_row, heads, q_head, tb), group, granule, chunk);
+    if (const cudaError_t e = grid_of(f, resident)) return status_of(e);
+    const int n_chunks = (group + chunk - 1) / chunk;
+    const Division by = divide(c, batch, width, window, chunk, n_chunks, resident);
+    if (by.bytes && (!workspace || workspace_bytes < by.bytes)) return PP_ERR_INVALID_ARG;
     const int es = type_bytes(c.dtype);
     AttnArgs a{q, static_cast<const char*>(c.k), static_cast<const char*>(c.v), c.k_scales, c.v_scales, table, lengths, out, lse,
-               parts ? static_cast<float*>(workspace) : nullptr, q_row, q_head, c.k_page * es, c.k_token * es, c.k_head * es, c.v_page * es, c.v_token * es,
+               static_cast<float*>(workspace), q_row, q_head, c.k_page * es, c.k_token * es, c.k_head * es, c.v_page * es, c.v_token * es,
                c.v_head * es, ld_table, Divisor((uint32_t)c.page_size), c.pages, c.page_size, batch, width * c.page_size, window, heads, c.kv_heads, group,
-               chunk, (group + chunk - 1) / chunk, c.head_dim, granule, q_type, c.dtype, c.page_size % kTile == 0, scale * kLog2e};
-    const int64_t segments = (int64_t)batch * c.kv_heads * a.n_chunks;
-    if (!parts) grid = (int)std::min<int64_t>(grid, segments);
+               chunk, n_chunks, c.head_dim, granule, q_type, c.dtype, by.cluster, c.page_size % kTile == 0,
+               c.head_dim % 4 == 0 && aligned_to(out, std::min(16, 4 * tb)), scale * kLog2e};
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    cudaError_t e = launch_pdl(f.kernel, dim3((unsigned)grid), dim3(kThreads), (size_t)f.smem, s, 1, a);
-    if (e == cudaSuccess && parts) e = launch_pdl(join_kernel, dim3((unsigned)grid), dim3(kJoinThreads), 0, s, 1, a, f.lift);
+    cudaError_t e = launch_pdl(f.kernel, dim3((unsigned)by.grid), dim3(kThreads), (size_t)f.smem, s, std::max(1, by.cluster), a);
+    if (e == cudaSuccess && !by.cluster) e = launch_pdl(join_kernel, dim3((unsigned)by.grid), dim3(kJoinThreads), 0, s, 1, a, f.lift);
     return status_of(e);
 }
