@@ -39,6 +39,8 @@ struct AttnArgs {
     int64_t q_row, q_head, k_page, k_token, k_head, v_page, v_token, v_head, ld_table;
     Divisor page;
     int pages, page_size, batch, capacity, window, heads, kv_heads, group, chunk, n_chunks, dim, granule, q_type, type;
+    int notes;                                               // in the workspace
+    bool by_head;                                            // a note's place is the head's, not the CTA's
     int cluster;                                             // CTAs that share a head (chunk); 0: all heads in a row, cut into equal parts
     bool whole_tiles;                                        // pages are a whole number of tiles long
     bool wide_out;                                           // four neighbours of out are one access
@@ -281,14 +283,15 @@ template <int KIND> __device__ __forceinline__ void widen(uint32_t four, uint32_
     }
 }
 
-// DT: width of a row in elements, rounded up; NT: tiles of eight heads.  With SPLIT_Q (a.q_type f32, NT = 2) the second tile
+// DT: width of a row in elements, rounded up; NT: tiles of eight heads.  LOW: p enters as two numbers; one is enough where p is f16 and
+// the output bf16, whose own rounding is eight times as large.  With SPLIT_Q (a.q_type f32, NT = 2) the second tile
 // holds what the rounding of the first one's eight heads to f16 left.
-template <int DT, int NT, int KIND> struct MmaCore {
+template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
     static constexpr bool kQ8 = KIND >= kE4m3, kIsBf16 = KIND == kBf16;
     static constexpr int kEs = kQ8 ? 1 : 2, kChunks = DT * kEs / 16, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
-    static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = kStage <= 5120 ? 4 : 3;
+    static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = 2;
     static constexpr int kHeads = 8 * NT, kMergePitch = DT + 4;
-    static constexpr int kDim = DT;
+    static constexpr int kDim = DT, kCtas = kQ8 && DT * NT <= 128 ? 4 : kQ8 || DT * NT <= 64 ? 3 : 1;
     static constexpr bool kStagesQ = false;
     // p is at most 2^kLift: f16 numbers below 2^-24 are lost, and a p can be that small beside the largest one
     static constexpr float kLift = kIsBf16 ? 0.0f : 14.0f;
@@ -479,7 +482,7 @@ template <int DT, int NT, int KIND> struct MmaCore {
                 const uint32_t h = pack2<kIsBf16>(x, y);
                 const float2 back = unpack2<kIsBf16>(h);
                 high[nt][i] = transpose(h);
-                low[nt][i] = transpose(pack2<kIsBf16>(x - back.x, y - back.y));
+                if constexpr (LOW) low[nt][i] = transpose(pack2<kIsBf16>(x - back.x, y - back.y));
             }
         const uint32_t values = stage + kTileBytes;
         if constexpr (kQ8) {
@@ -497,7 +500,7 @@ template <int DT, int NT, int KIND> struct MmaCore {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         mma<kIsBf16>(acc[c + i][nt], a0, a1, a2, a3, high[nt][0], high[nt][1]);
-                        mma<kIsBf16>(acc[c + i][nt], a0, a1, a2, a3, low[nt][0], low[nt][1]);
+                        if constexpr (LOW) mma<kIsBf16>(acc[c + i][nt], a0, a1, a2, a3, low[nt][0], low[nt][1]);
                     }
                 }
             }
@@ -510,7 +513,7 @@ template <int DT, int NT, int KIND> struct MmaCore {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     mma<kIsBf16>(acc[j][nt], v[0], v[1], v[2], v[3], high[nt][0], high[nt][1]);
-                    mma<kIsBf16>(acc[j][nt], v[0], v[1], v[2], v[3], low[nt][0], low[nt][1]);
+                    if constexpr (LOW) mma<kIsBf16>(acc[j][nt], v[0], v[1], v[2], v[3], low[nt][0], low[nt][1]);
                 }
             }
         }
@@ -558,8 +561,8 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
     static constexpr bool kQ8 = false;
     static constexpr int kEs = 4, kChunks = DT / 4, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
     static constexpr int kHeads = HN, kMergePitch = DT;
-    static constexpr int kStage = 2 * kTileBytes + 16 * 4 * HN, kStages = DT == 256 ? 1 : DT == 192 ? 2 : 3;   // behind the rows: p by position and head
-    static constexpr int kDim = DT;
+    static constexpr int kStage = 2 * kTileBytes + 16 * 4 * HN, kStages = DT == 256 ? 1 : DT == 192 ? 2 : DT == 64 ? 2 : 3;   // behind the rows: p by position and head
+    static constexpr int kDim = DT, kCtas = 1;
     static constexpr bool kStagesQ = true;
     static constexpr float kLift = 0.0f;
 
@@ -727,11 +730,12 @@ struct Cut {
     }
 };
 
-// A head (chunk) whose units several CTAs share, noted by the first of them, which is the note's number.
+// A head (chunk) whose units several CTAs share, noted by the first of them: in the place of the head among all (a.by_head), or where
+// these are more than CTAs in that of the CTA, which can be the first one of one head only.
 struct Note {
-    int last;                                                // the last of them; -1: no such head
-    int row, n_heads;                                        // first row of out, rows
-    int second;                                              // the first one's part is the second of its two
+    int first, last;                                         // of the CTAs; last -1: no such head
+    int row;                                                 // the first of out
+    int rows;                                                // negative: the first one's part is the second of its two
 };
 
 // Thread-block clusters: a wait for all CTAs that also shows their writes, and reads of another CTA's shared memory.
@@ -756,7 +760,7 @@ __device__ __forceinline__ float4 load_remote4(uint32_t at) {
 
 __device__ __forceinline__ float lse_of(float m, float l, float lift) { return l == 0.0f ? -INFINITY : (m - lift + log2f(l)) * kLn2; }
 
-template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) attn_kernel(const __grid_constant__ AttnArgs a) {
+template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Core::kCtas) attn_kernel(const __grid_constant__ AttnArgs a) {
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ int warp_sums[kWarps], found_base, found;
     __shared__ float warp_m[kWarps][Core::kHeads], warp_l[kWarps][Core::kHeads], all_m[Core::kHeads], all_l[Core::kHeads];
@@ -774,7 +778,7 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
         for (r = r0; r < r1; ++r) mine += units_of(a, r) * per_request;
         const int before = sum_before(mine, warp_sums, all);
         ctas = min((int)gridDim.x, all);
-        if (tid == 0) reinterpret_cast<Note*>(a.ws)[c].last = -1;
+        if (!a.by_head && tid == 0) reinterpret_cast<Note*>(a.ws)[c].last = -1;
         if (c >= ctas) return;
         const Cut cut(all, ctas);
         u = begin = cut.start(c);
@@ -883,7 +887,7 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
         __syncthreads();
         const bool whole = t0 == 0 && t1 == units && a.cluster <= 1;
         const int64_t row0 = (int64_t)r * a.heads + head0;
-        float* part = whole || a.cluster ? nullptr : a.ws + notes_floats(gridDim.x) + (2 * c + (u != begin)) * part_floats(a.chunk, a.dim);
+        float* part = whole || a.cluster ? nullptr : a.ws + notes_floats(a.notes) + (2 * c + (u != begin)) * part_floats(a.chunk, a.dim);
         constexpr int kFours = Core::kDim / 4;               // of a row
         for (int i = tid; i < n_heads * kFours; i += kThreads) {
             const int h = i / kFours, d = 4 * (i - h * kFours);
@@ -897,12 +901,16 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
             else *at = sum;
         }
         if (part) {
-            if (t0 == 0 && tid == 0) reinterpret_cast<Note*>(a.ws)[c] = {Cut(all, ctas).of(base + (hc + 1) * units - 1), (int)row0, n_heads, u != begin};
+            if (t0 == 0 && tid == 0)
+                reinterpret_cast<Note*>(a.ws)[a.by_head ? r * per_request + hc : c] = {c, Cut(all, ctas).of(base + (hc + 1) * units - 1), (int)row0, u != begin ? -n_heads : n_heads};
             if (tid < n_heads) {
                 part[tid] = all_m[tid];
                 part[up4(a.chunk) + tid] = all_l[tid];
             }
-        } else if (whole && a.lse && tid < n_heads) {
+        } else if (whole && a.by_head && !a.cluster && tid == 0) {
+            reinterpret_cast<Note*>(a.ws)[r * per_request + hc].last = -1;
+        }
+        if (whole && a.lse && tid < n_heads) {
             a.lse[row0 + tid] = lse_of(all_m[tid], all_l[tid], Core::kLift);
         }
         if (a.cluster) {
@@ -942,54 +950,62 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads) at
     }
 }
 
-// Joins the parts of the head (chunk) that CTA blockIdx.x has noted, if it has: as many warps to a row of out as there are, each
-// with its share of the parts.
-constexpr int kJoinWarps = 16, kJoinThreads = kJoinWarps * 32;
+// Joins the parts of the head (chunk) of note blockIdx.x, if there is one: CTA blockIdx.y of gridDim.y takes a share of its rows, as many
+// warps to a row as there are, each with a share of the parts.  Its shared memory fits beside the first kernel's, so that it is
+// there when that ends.
+constexpr int kJoinWarps = 8, kJoinThreads = kJoinWarps * 32;
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttnArgs a, float lift) {
     __shared__ float4 sums[kJoinWarps][kMaxHeadDim / 4];
     __shared__ float ls[kJoinWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, step = gridDim.y;
     pdl_release();
     pdl_wait();
-    const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.ws) + c0);
+    const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.ws) + blockIdx.x);
     const Note note{raw.x, raw.y, raw.z, raw.w};
     if (note.last < 0) return;
-    const int per = kJoinWarps / note.n_heads, h = warp / per, sub = warp - h * per;
-    const bool live = h < note.n_heads;
-    const int64_t floats = part_floats(a.chunk, a.dim);
-    const float* parts = a.ws + notes_floats(gridDim.x);
-    const auto part = [&](int c) { return parts + (2 * c + (c == c0 ? note.second : 0)) * floats; };
-    const int chunk4 = up4(a.chunk), dim4 = up4(a.dim);
-    float top = -INFINITY, l = 0.0f;
-    float4 acc[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
-    if (live) {
-        for (int c = c0 + lane; c <= note.last; c += 32) top = fmaxf(top, part(c)[h]);
+    const int64_t floats = part_floats(a.chunk, a.dim), second = note.rows < 0 ? floats : 0;
+    const float* parts = a.ws + notes_floats(a.notes);
+    const auto part = [&](int c) { return parts + 2 * c * floats + (c == note.first ? second : 0); };
+    const int chunk4 = up4(a.chunk), dim4 = up4(a.dim), all_rows = abs(note.rows);
+    const int rows = (all_rows - (int)blockIdx.y + step - 1) / step;         // of this CTA
+    if (rows < 1) return;
+    const int at_once = min(rows, kJoinWarps), per = kJoinWarps / at_once, sub = warp % per;
+    for (int done = 0; done < rows; done += at_once) {
+        const int n = done + warp / per, h = blockIdx.y + n * step;
+        const bool live = warp / per < at_once && n < rows;
+        float top = -INFINITY, l = 0.0f;
+        float4 acc[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
+        if (live) {
+            for (int c = note.first + lane; c <= note.last; c += 32) top = fmaxf(top, part(c)[h]);
 #pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
 #pragma unroll 4
-        for (int c = c0 + sub; c <= note.last; c += per) {
-            const float* p = part(c);
-            const float w = weight_of(p[h], top);
-            l = fmaf(p[chunk4 + h], w, l);
-            const float4* x = reinterpret_cast<const float4*>(p + 2 * chunk4 + h * dim4) + lane;
+            for (int c = note.first + sub; c <= note.last; c += per) {
+                const float* p = part(c);
+                const float w = weight_of(p[h], top);
+                l = fmaf(p[chunk4 + h], w, l);
+                const float4* x = reinterpret_cast<const float4*>(p + 2 * chunk4 + h * dim4) + lane;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (4 * (lane + 32 * i) < a.dim) acc[i] = fma4(x[32 * i], w, acc[i]);
+                for (int i = 0; i < 2; ++i)
+                    if (4 * (lane + 32 * i) < a.dim) acc[i] = fma4(x[32 * i], w, acc[i]);
+            }
         }
-    }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) sums[warp][lane + 32 * i] = acc[i];
-    if (lane == 0) ls[warp] = l;
-    __syncthreads();
-    if (!live || sub) return;
-    l = 0.0f;
-    for (int w = 0; w < per; ++w) l += ls[warp + w];
-    for (int d = lane; 4 * d < a.dim; d += 32) {
-        float4 sum = sums[warp][d];
-        for (int w = 1; w < per; ++w) sum = add4(sum, sums[warp + w][d]);
-        store_out(a, (int64_t)note.row + h, 4 * d, over(sum, l));
+        for (int i = 0; i < 2; ++i) sums[warp][lane + 32 * i] = acc[i];
+        if (lane == 0) ls[warp] = l;
+        __syncthreads();
+        if (live && sub == 0) {
+            l = 0.0f;
+            for (int w = 0; w < per; ++w) l += ls[warp + w];
+            for (int d = lane; 4 * d < a.dim; d += 32) {
+                float4 sum = sums[warp][d];
+                for (int w = 1; w < per; ++w) sum = add4(sum, sums[warp + w][d]);
+                store_out(a, (int64_t)note.row + h, 4 * d, over(sum, l));
+            }
+            if (a.lse && lane == 0) a.lse[(int64_t)note.row + h] = lse_of(top, l, lift);
+        }
+        __syncthreads();
     }
-    if (a.lse && lane == 0) a.lse[(int64_t)note.row + h] = lse_of(top, l, lift);
 }
 
 // ------------------------------------------------------------------------------------------------------ choice
@@ -1014,10 +1030,10 @@ template <class Core, bool ASYNC> Form form_of() {
     f.resident = resident;
     return f;
 }
-template <int KIND> Form mma_form(int dim, bool two) {
-    if (two) return dim <= 64 ? form_of<MmaCore<64, 2, KIND>, true>() : dim <= 96 ? form_of<MmaCore<96, 2, KIND>, true>() : form_of<MmaCore<128, 2, KIND>, true>();
-    return dim <= 64 ? form_of<MmaCore<64, 1, KIND>, true>() : dim <= 96 ? form_of<MmaCore<96, 1, KIND>, true>()
-         : dim <= 128 ? form_of<MmaCore<128, 1, KIND>, true>() : dim <= 192 ? form_of<MmaCore<192, 1, KIND>, true>() : form_of<MmaCore<256, 1, KIND>, true>();
+template <int KIND, bool LOW> Form mma_form(int dim, bool two) {
+    if (two) return dim <= 64 ? form_of<MmaCore<64, 2, KIND, LOW>, true>() : dim <= 96 ? form_of<MmaCore<96, 2, KIND, LOW>, true>() : form_of<MmaCore<128, 2, KIND, LOW>, true>();
+    return dim <= 64 ? form_of<MmaCore<64, 1, KIND, LOW>, true>() : dim <= 96 ? form_of<MmaCore<96, 1, KIND, LOW>, true>()
+         : dim <= 128 ? form_of<MmaCore<128, 1, KIND, LOW>, true>() : dim <= 192 ? form_of<MmaCore<192, 1, KIND, LOW>, true>() : form_of<MmaCore<256, 1, KIND, LOW>, true>();
 }
 template <bool ASYNC> Form scalar_form(int dim, int group) {
     if (dim <= 64) return group <= 1 ? form_of<ScalarCore<64, 1, ASYNC>, ASYNC>() : group <= 4 ? form_of<ScalarCore<64, 4, ASYNC>, ASYNC>() : form_of<ScalarCore<64, 8, ASYNC>, ASYNC>();
@@ -1038,10 +1054,10 @@ Form choose(const pp_paged_cache_t& c, pp_dtype_t q_type, int q_on, int group, i
         const bool two = split || (group > 8 && c.head_dim <= 128);
         if (two && !split) chunk = 16;
         switch (c.dtype) {
-            case PP_BF16: return mma_form<kBf16>(c.head_dim, two);
-            case PP_F16: return mma_form<kF16>(c.head_dim, two);
-            case PP_E4M3: return mma_form<kE4m3>(c.head_dim, two);
-            default: return mma_form<kInt8>(c.head_dim, two);
+            case PP_BF16: return mma_form<kBf16, true>(c.head_dim, two);
+            case PP_F16: return mma_form<kF16, true>(c.head_dim, two);
+            case PP_E4M3: return q_type == PP_BF16 ? mma_form<kE4m3, false>(c.head_dim, two) : mma_form<kE4m3, true>(c.head_dim, two);
+            default: return q_type == PP_BF16 ? mma_form<kInt8, false>(c.head_dim, two) : mma_form<kInt8, true>(c.head_dim, two);
         }
     }
     const Form f = granule >= 4 && c.dtype == PP_F32 ? scalar_form<true>(c.head_dim, group) : scalar_form<false>(c.head_dim, group);
@@ -1056,6 +1072,10 @@ cudaError_t grid_of(const Form& f, int& grid) {
     if (!f.opt_in->is_done(device)) {
         int n = 0;
         if (cudaError_t e = cudaFuncSetAttribute(f.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, f.smem)) return e;
+        // An SM divides its memory between L1 and shared memory as its kernels ask, and changes that only when it is empty: with the second
+        // kernel's smaller wish in force the last of the CTAs would start when others end.
+        for (const void* k : {reinterpret_cast<const void*>(f.kernel), reinterpret_cast<const void*>(join_kernel)})
+            if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared)) return e;
         if (cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, f.kernel, kThreads, (size_t)f.smem)) return e;
         if (device >= PerDeviceOnce::kMaxDevices) {
             grid = std::max(n, 1) * sm_count();
@@ -1094,7 +1114,7 @@ Division divide(const pp_paged_cache_t& c, int batch, int width, int window, int
     while (cluster < 8 && cluster < units && 2 * cluster * heads <= resident) cluster *= 2;
     const int64_t waves = (heads * cluster + resident - 1) / resident, own = (units + cluster - 1) / cluster;
     if (units == 1 || waves * own <= heads * units / resident + kMore) return {(int)(heads * cluster), cluster, 0};
-    return {resident, 0, (notes_floats(resident) + (int64_t)resident * 2 * part_floats(chunk, c.head_dim)) * 4};
+    return {resident, 0, (notes_floats(std::min<int64_t>(heads, resident)) + (int64_t)resident * 2 * part_floats(chunk, c.head_dim)) * 4};
 }
 
 }  // namespace
@@ -1148,10 +1168,14 @@ extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const v
     AttnArgs a{q, static_cast<const char*>(c.k), static_cast<const char*>(c.v), c.k_scales, c.v_scales, table, lengths, out, lse,
                static_cast<float*>(workspace), q_row, q_head, c.k_page * es, c.k_token * es, c.k_head * es, c.v_page * es, c.v_token * es,
                c.v_head * es, ld_table, Divisor((uint32_t)c.page_size), c.pages, c.page_size, batch, width * c.page_size, window, heads, c.kv_heads, group,
-               chunk, n_chunks, c.head_dim, granule, q_type, c.dtype, by.cluster, c.page_size % kTile == 0,
+               chunk, n_chunks, c.head_dim, granule, q_type, c.dtype, (int)std::min<int64_t>((int64_t)batch * c.kv_heads * n_chunks, resident),
+               (int64_t)batch * c.kv_heads * n_chunks <= resident, by.cluster, c.page_size % kTile == 0,
                c.head_dim % 4 == 0 && aligned_to(out, std::min(16, 4 * tb)), scale * kLog2e};
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = launch_pdl(f.kernel, dim3((unsigned)by.grid), dim3(kThreads), (size_t)f.smem, s, std::max(1, by.cluster), a);
-    if (e == cudaSuccess && !by.cluster) e = launch_pdl(join_kernel, dim3((unsigned)by.grid), dim3(kJoinThreads), 0, s, 1, a, f.lift);
+    if (e == cudaSuccess && !by.cluster) {
+        const int shares = std::max(1, std::min({chunk, group, 2 * sm_count() / a.notes}));     // few notes: a CTA for each row, if there are so many
+        e = launch_pdl(join_kernel, dim3((unsigned)a.notes, (unsigned)shares), dim3(kJoinThreads), 0, s, 1, a, f.lift);
+    }
     return status_of(e);
 }
