@@ -1103,17 +1103,21 @@ struct Division {
     int grid, cluster;                                       // cluster 0: equal parts of all units, joined by a second kernel
     int64_t bytes;                                           // of workspace
 };
-// A cluster of up to eight CTAs to each head (chunk) needs no workspace, no sums over lengths and no second kernel, some 4 us in all, but
-// leaves SMs idle where heads are few and long, or lengths differ.  It is taken where its longest CTA has at most kMore units
-// more than an equal part would have, going by the table's width.
-constexpr int kMore = 3;
+// Costs in units of 64 positions to a CTA, some 0.6 us while latency rules, going by the table's width.  Equal parts of all units:
+// sums over lengths, the workspace and a second kernel, 4 us.  A CTA or a cluster of up to eight to each head (chunk): as many
+// rounds as the GPU needs for them, each a CTA's share and 2 us for its start and end; a cluster's exchange costs 2.3 us.
+constexpr int kEqualParts = 10, kRound = 3, kExchange = 4;
 Division divide(const pp_paged_cache_t& c, int batch, int width, int window, int chunk, int n_chunks, int resident) {
     const int64_t capacity = (int64_t)width * c.page_size, longest = window > 0 ? std::min<int64_t>((int64_t)window + kTile - 1, capacity) : capacity;
     const int64_t units = std::max<int64_t>(1, (longest + kUnit - 1) / kUnit), heads = (int64_t)batch * c.kv_heads * n_chunks;
-    int cluster = 1;
-    while (cluster < 8 && cluster < units && 2 * cluster * heads <= resident) cluster *= 2;
-    const int64_t waves = (heads * cluster + resident - 1) / resident, own = (units + cluster - 1) / cluster;
-    if (units == 1 || waves * own <= heads * units / resident + kMore) return {(int)(heads * cluster), cluster, 0};
+    int64_t least = heads * units / resident + kEqualParts, best = 0;
+    for (int64_t cluster = 1; cluster <= 8; cluster *= 2) {
+        const int64_t rounds = (heads * cluster + resident - 1) / resident, own = (units + cluster - 1) / cluster;
+        const int64_t cost = rounds * (own + kRound + (cluster > 1 ? kExchange : 0));
+        if (cost < least && heads * cluster <= INT32_MAX) least = cost, best = cluster;
+    }
+    if (units == 1) best = 1;                                // nothing to divide
+    if (best) return {(int)(heads * best), (int)best, 0};
     return {resident, 0, (notes_floats(std::min<int64_t>(heads, resident)) + (int64_t)resident * 2 * part_floats(chunk, c.head_dim)) * 4};
 }
 
