@@ -115,8 +115,10 @@ __device__ __forceinline__ float4 over(float4 v, float l) {
     if (l == 0.0f) return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     return make_float4(__fdiv_rn(v.x, l), __fdiv_rn(v.y, l), __fdiv_rn(v.z, l), __fdiv_rn(v.w, l));
 }
-// exp2(m - top), 0 for a part without positions.
-__device__ __forceinline__ float weight_of(float m, float top) { return m == -INFINITY ? 0.0f : exp2_fast(m - top); }
+// A running maximum starts at the lowest float, not at minus infinity: no difference of two of them is then a NaN.  It need not be the
+// maximum: it moves when a score is more than 2^kSlack above it, so that most tiles pass with one vote and no exchange of maxima.
+constexpr float kLowest = -3.402823466e38f, kSlack = 8.0f;
+__device__ __forceinline__ float weight_of(float m, float top) { return exp2_fast(m - top); }
 
 template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there) {   // zeros if not there
     if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -293,11 +295,12 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
     static constexpr int kHeads = 8 * NT, kMergePitch = DT + 4;
     static constexpr int kDim = DT, kCtas = kQ8 && DT * NT <= 128 ? 4 : kQ8 || DT * NT <= 64 ? 3 : 1;
     static constexpr bool kStagesQ = false;
-    // p is at most 2^kLift: f16 numbers below 2^-24 are lost, and a p can be that small beside the largest one
-    static constexpr float kLift = kIsBf16 ? 0.0f : 14.0f;
+    // p is at most 2^(kLift + kSlack): f16 numbers end at 65504, and below 2^-24 they are lost, which a p can be beside the largest one
+    static constexpr float kLift = kIsBf16 ? 0.0f : 7.0f;
 
     uint32_t q[DT / 16][NT][2];
-    float acc[DT / 16][NT][4], m[NT][2], l[NT][2], f[NT][2], vm;
+    // by head: the running maximum, kLift less it, the sum, what a product is multiplied with; the largest scale of a value and its inverse
+    float acc[DT / 16][NT][4], m[NT][2], c[NT][2], l[NT][2], f[NT][2], vm, inverse;
 
     // q as the second operand of the scores: head g of each tile, two neighbouring dimensions to a register (16-bit caches), or four
     // to two registers (codes, as they lie in a lane's bytes).  Rows of q start where such an access may.
@@ -363,13 +366,14 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) acc[j][nt][k] = 0.0f;
         }
-        vm = 0.0f;
+        vm = inverse = 0.0f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 f[nt][b] = __shfl_sync(0xffffffffu, factor[nt], (2 * t + b) * 4);
-                m[nt][b] = -INFINITY;
+                m[nt][b] = kLowest;
+                c[nt][b] = kLift - kLowest;
                 l[nt][b] = 0.0f;
             }
     }
@@ -413,9 +417,9 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
                 s[NT - 1][i] = 0.0f;
             }
 
-        float w0 = 1.0f, w1 = 1.0f, change = 1.0f;           // weights of positions g and g + 8: the scales of their values
+        float v0 = 1.0f, v1 = 1.0f, most = 0.0f;             // scales of the values at g and g + 8
         if constexpr (kQ8) {
-            float k0, k1, v0, v1;
+            float k0, k1;
             const uint32_t at = stage + 2 * kTileBytes + g * 4;
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k0) : "r"(at) : "memory");
             asm volatile("ld.shared.f32 %0, [%1+32];" : "=f"(k1) : "r"(at) : "memory");
@@ -426,53 +430,71 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
                 s[nt][0] *= k0, s[nt][1] *= k0;
                 s[nt][2] *= k1, s[nt][3] *= k1;
             }
-            // relative to the largest scale so far, so that p times scale stays within f16; room for twice that avoids most changes
-            const float most = fmaxf(fabsf(v0), fabsf(v1));
-            if (__any_sync(0xffffffffu, most > vm)) {
-                float top = most;
-#pragma unroll
-                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const float now = top < 1e38f ? fmaxf(2.0f * top, 0x1p-100f) : top;   // 1 / vm stays finite
-                change = __fdiv_rn(vm, now);
-                vm = now;
-            }
-            const float inverse = vm > 0.0f ? __fdiv_rn(1.0f, vm) : 0.0f;
-            w0 = v0 * inverse;
-            w1 = v1 * inverse;
+            most = fmaxf(fabsf(v0), fabsf(v1));
         }
-
-        float p[NT][4], alpha[NT][2];
-        bool moved = kQ8 && change != 1.0f;
+        float p[NT][4];                                      // logarithms first
+        const auto exponents = [&] {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[nt][i] *= f[nt][i & 1];
-                if (!((bits >> (i < 2 ? g : g + 8)) & 1)) s[nt][i] = -INFINITY;
-            }
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                float top = fmaxf(s[nt][b], s[nt][b + 2]);
-#pragma unroll
-                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const float now = fmaxf(m[nt][b], top), from = now == -INFINITY ? 0.0f : now;
-                alpha[nt][b] = exp2_fast(m[nt][b] - from);
-                moved |= m[nt][b] != now;
-                m[nt][b] = now;
-                p[nt][b] = exp2_fast(s[nt][b] - from + kLift);
-                p[nt][b + 2] = exp2_fast(s[nt][b + 2] - from + kLift);
-                l[nt][b] = l[nt][b] * alpha[nt][b] + (p[nt][b] + p[nt][b + 2]);
-                alpha[nt][b] *= change;
-            }
-        }
-        if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-            for (int j = 0; j < DT / 16; ++j)
+                for (int i = 0; i < 4; ++i) p[nt][i] = fmaf(s[nt][i], f[nt][i & 1], c[nt][i & 1]);
+            if (bits != 0xffffu) {
+                const bool first = (bits >> g) & 1, second = (bits >> (g + 8)) & 1;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[j][nt][i] *= alpha[nt][i & 1];
+                    for (int i = 0; i < 4; ++i)
+                        if (!(i < 2 ? first : second)) p[nt][i] = -INFINITY;
+            }
+        };
+        exponents();
+        float largest = p[0][0];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) largest = fmaxf(largest, p[nt][i]);
+        if (__any_sync(0xffffffffu, largest > kLift + kSlack || (kQ8 && most > vm))) {
+            float change = 1.0f;                             // of the values' common scale
+            if constexpr (kQ8) {
+                // scales enter p relative to the largest so far, so that the product stays within f16; room for twice that avoids most changes
+                float top = most;
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                if (top > vm) {
+                    const float now = top < 1e38f ? fmaxf(2.0f * top, 0x1p-100f) : top;      // 1 / vm stays finite
+                    change = __fdiv_rn(vm, now);
+                    vm = now;
+                    inverse = __fdiv_rn(1.0f, vm);
+                }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    float top = fmaxf(p[nt][b] > -INFINITY ? s[nt][b] * f[nt][b] : kLowest, p[nt][b + 2] > -INFINITY ? s[nt][b + 2] * f[nt][b] : kLowest);
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    const float now = fmaxf(m[nt][b], top), alpha = exp2_fast(m[nt][b] - now);
+                    m[nt][b] = now;
+                    c[nt][b] = kLift - now;
+                    l[nt][b] *= alpha;
+#pragma unroll
+                    for (int j = 0; j < DT / 16; ++j) {
+                        acc[j][nt][b] *= alpha * change;
+                        acc[j][nt][b + 2] *= alpha * change;
+                    }
+                }
+            exponents();
         }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                p[nt][b] = exp2_fast(p[nt][b]);
+                p[nt][b + 2] = exp2_fast(p[nt][b + 2]);
+                l[nt][b] += p[nt][b] + p[nt][b + 2];
+            }
+        const float w0 = kQ8 ? v0 * inverse : 1.0f, w1 = kQ8 ? v1 * inverse : 1.0f;
         uint32_t high[NT][2], low[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -544,7 +566,7 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
             for (int b = 0; b < 2; ++b) {
                 const int head = nt * 8 + 2 * t + b;
                 float by = weight_of(m[nt][b], top_of<kHeads>(all, head));
-                if (kQ8) by = by == 0.0f ? 0.0f : by * vm;
+                if (kQ8) by *= vm;
 #pragma unroll
                 for (int j = 0; j < DT / 16; ++j)
 #pragma unroll
@@ -571,7 +593,7 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
     __device__ __forceinline__ void begin() {
 #pragma unroll
         for (int h = 0; h < HN; ++h) {
-            m[h] = -INFINITY;
+            m[h] = kLowest;
             l[h] = 0.0f;
 #pragma unroll
             for (int i = 0; i < DT / 32; ++i) acc[i][h] = 0.0f;
@@ -635,30 +657,33 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
         }
         const bool there = (bits >> key) & 1;
         float* p = stage + 2 * kTileBytes / 4;
-        float alpha[HN];
-        bool moved = false;
+        bool higher = false;
 #pragma unroll
         for (int h = 0; h < HN; ++h) {
             s[h] = (s[h] + __shfl_xor_sync(0xffffffffu, s[h], 16)) * a.scale;
             if (!there) s[h] = -INFINITY;
-            float top = s[h];
+            higher |= s[h] - m[h] > kSlack;
+        }
+        if (__any_sync(0xffffffffu, higher)) {
 #pragma unroll
-            for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const float now = fmaxf(m[h], top), from = now == -INFINITY ? 0.0f : now;
-            alpha[h] = exp2_fast(m[h] - from);
-            moved |= m[h] != now;
-            m[h] = now;
-            const float e = exp2_fast(s[h] - from);
-            l[h] = l[h] * alpha[h] + (half ? 0.0f : e);
+            for (int h = 0; h < HN; ++h) {
+                float top = s[h];
+#pragma unroll
+                for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float now = fmaxf(m[h], top), alpha = exp2_fast(m[h] - now);
+                m[h] = now;
+                l[h] *= alpha;
+#pragma unroll
+                for (int i = 0; i < DT / 32; ++i) acc[i][h] *= alpha;
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < HN; ++h) {
+            const float e = exp2_fast(s[h] - m[h]);
+            l[h] += half ? 0.0f : e;
             if (!half) p[key * HN + h] = e;
         }
         __syncwarp();
-        if (moved) {
-#pragma unroll
-            for (int i = 0; i < DT / 32; ++i)
-#pragma unroll
-                for (int h = 0; h < HN; ++h) acc[i][h] *= alpha[h];
-        }
         const float* v = stage + kTileBytes / 4 + lane;
 #pragma unroll 4
         for (int j = 0; j < kTile; ++j) {
@@ -829,16 +854,16 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
         int ask_at = low + t0 * kUnit + warp * kTile;
         reader.entry = entry_of(a, reader, ask_at);
         const int tiles = ask_at < reader.end ? (reader.end - ask_at + kUnit - 1) / kUnit : 0;
-        uint64_t there = 0;                                  // 16 bits for each stage: the rows that are there
+        uint64_t there = 0;                                  // the rows that are there, 16 bits for each tile on its way, the last one's lowest
         int asked = 0, stage = 0;
         const auto request = [&]() {
+            uint32_t bits = 0;
             if (asked < tiles) {
-                uint32_t bits;
                 if constexpr (ASYNC) bits = ask<Core::kEs, Core::kChunks, Core::kPitch, Core::kQ8>(a, reader, ask_at, smem_at(own + stage * Core::kStage));
                 else bits = Core::fetch(a, reader, ask_at, reinterpret_cast<float*>(own + stage * Core::kStage));
-                there = (there & ~(0xffffull << (16 * stage))) | ((uint64_t)bits << (16 * stage));
                 ask_at += kUnit;
             }
+            there = there << 16 | bits;
             commit();
             ++asked;
             if (++stage == Core::kStages) stage = 0;
@@ -867,7 +892,7 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
                 wait_but<0>();
                 __syncwarp();
             }
-            const uint32_t bits = (uint32_t)(there >> (16 * at)) & 0xffffu;
+            const uint32_t bits = (uint32_t)(there >> (16 * (Core::kStages - 1))) & 0xffffu;
             if constexpr (Core::kStagesQ) core.tile(a, reinterpret_cast<float*>(own + at * Core::kStage), bits, q);
             else core.tile(a, smem_at(own + at * Core::kStage), bits);
             if (++at == Core::kStages) at = 0;
@@ -921,10 +946,10 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
             for (int i = tid + rank * kThreads; i < n_heads * kFours; i += kThreads * a.cluster) {
                 const int h = i / kFours, d = 4 * (i - h * kFours);
                 if (d >= a.dim) continue;
-                float m[8], top = -INFINITY, l = 0.0f;
+                float m[8], top = kLowest, l = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    m[k] = k < a.cluster ? load_remote(at_rank(&all_m[h], k)) : -INFINITY;
+                    m[k] = k < a.cluster ? load_remote(at_rank(&all_m[h], k)) : kLowest;
                     top = fmaxf(top, m[k]);
                 }
                 float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -973,7 +998,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     for (int done = 0; done < rows; done += at_once) {
         const int n = done + warp / per, h = blockIdx.y + n * step;
         const bool live = warp / per < at_once && n < rows;
-        float top = -INFINITY, l = 0.0f;
+        float top = kLowest, l = 0.0f;
         float4 acc[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
         if (live) {
             for (int c = note.first + lane; c <= note.last; c += 32) top = fmaxf(top, part(c)[h]);
