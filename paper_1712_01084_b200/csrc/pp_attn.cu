@@ -39,6 +39,7 @@ struct AttnArgs {
     int64_t q_row, q_head, k_page, k_token, k_head, v_page, v_token, v_head, ld_table;
     Divisor page;
     int pages, page_size, batch, capacity, window, heads, kv_heads, group, chunk, n_chunks, dim, granule, q_type, type;
+    int inbox;                                               // where a cluster's CTAs write in each other's shared memory, in bytes
     int notes;                                               // in the workspace
     bool by_head;                                            // a note's place is the head's, not the CTA's
     int cluster;                                             // CTAs that share a head (chunk); 0: all heads in a row, cut into equal parts
@@ -293,7 +294,10 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
     static constexpr int kEs = kQ8 ? 1 : 2, kChunks = DT * kEs / 16, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
     static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = 2;
     static constexpr int kHeads = 8 * NT, kMergePitch = DT + 4;
-    static constexpr int kDim = DT, kCtas = kQ8 && DT * NT <= 128 ? 4 : kQ8 || DT * NT <= 64 ? 3 : 1;
+    // Resident CTAs that the registers are cut for.  16-bit rows of 128: no more than two by their shared memory.  They keep 140 KB on
+    // their way to an SM, and with three (or a third stage) the SMs' shares of the memory differ so much that the last CTA ends 20 %
+    // behind the mean (64 x 8192: 254 us with two, 268 with three).
+    static constexpr int kDim = DT, kCtas = kQ8 && DT * NT <= 128 ? 4 : kQ8 || DT * NT <= 96 ? 3 : 1, kLeastSmem = kQ8 || DT < 128 ? 0 : 77 * 1024;
     static constexpr bool kStagesQ = false;
     // p is at most 2^(kLift + kSlack): f16 numbers end at 65504, and below 2^-24 they are lost, which a p can be beside the largest one
     static constexpr float kLift = kIsBf16 ? 0.0f : 7.0f;
@@ -584,7 +588,7 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
     static constexpr int kEs = 4, kChunks = DT / 4, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
     static constexpr int kHeads = HN, kMergePitch = DT;
     static constexpr int kStage = 2 * kTileBytes + 16 * 4 * HN, kStages = DT == 256 ? 1 : DT == 192 ? 2 : DT == 64 ? 2 : 3;   // behind the rows: p by position and head
-    static constexpr int kDim = DT, kCtas = 1;
+    static constexpr int kDim = DT, kCtas = 1, kLeastSmem = 0;
     static constexpr bool kStagesQ = true;
     static constexpr float kLift = 0.0f;
 
@@ -763,24 +767,18 @@ struct Note {
     int rows;                                                // negative: the first one's part is the second of its two
 };
 
-// Thread-block clusters: a wait for all CTAs that also shows their writes, and reads of another CTA's shared memory.
-__device__ __forceinline__ void cluster_wait() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t at_rank(const void* p, int rank) {
+// Thread-block clusters: a barrier in two halves, the second of which shows what others wrote before the first, and writes into another
+// CTA's shared memory.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t at_rank(uint32_t own, int rank) {
     uint32_t d;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(smem_at(p)), "r"(rank));
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(own), "r"(rank));
     return d;
 }
-__device__ __forceinline__ float load_remote(uint32_t at) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-    return v;
-}
-__device__ __forceinline__ float4 load_remote4(uint32_t at) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
-    return v;
+__device__ __forceinline__ void store_remote(uint32_t at, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); }
+__device__ __forceinline__ void store_remote4(uint32_t at, float4 v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
 __device__ __forceinline__ float lse_of(float m, float l, float lift) { return l == 0.0f ? -INFINITY : (m - lift + log2f(l)) * kLn2; }
@@ -791,6 +789,7 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
     __shared__ float warp_m[kWarps][Core::kHeads], warp_l[kWarps][Core::kHeads], all_m[Core::kHeads], all_l[Core::kHeads];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
     pdl_release();
+    if (a.cluster > 1) cluster_arrive();                     // awaited before the first write to another CTA's memory: it has started by then
     pdl_wait();
 
     const int per_request = a.kv_heads * a.n_chunks;
@@ -914,16 +913,21 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
         const int64_t row0 = (int64_t)r * a.heads + head0;
         float* part = whole || a.cluster ? nullptr : a.ws + notes_floats(a.notes) + (2 * c + (u != begin)) * part_floats(a.chunk, a.dim);
         constexpr int kFours = Core::kDim / 4;               // of a row
+        // a cluster's CTAs share the rows' fours among them, round robin: each sends its part of a four to the CTA that joins it
+        float4* inbox = reinterpret_cast<float4*>(ring + a.inbox);                             // [rank][its fours]
+        float(*others)[2][Core::kHeads] = reinterpret_cast<float(*)[2][Core::kHeads]>(inbox + Core::kHeads * kFours + 8);   // [rank]: m and l
+        const int rank = a.cluster > 1 ? c % a.cluster : 0, share = a.cluster > 1 ? (n_heads * kFours + a.cluster - 1) / a.cluster : 0;
+        if (a.cluster > 1) cluster_wait();
         for (int i = tid; i < n_heads * kFours; i += kThreads) {
             const int h = i / kFours, d = 4 * (i - h * kFours);
             if (d >= a.dim) continue;
-            float4* at = reinterpret_cast<float4*>(merge + h * Core::kMergePitch + d);
+            const float4* at = reinterpret_cast<const float4*>(merge + h * Core::kMergePitch + d);
             float4 sum = *at;
 #pragma unroll
-            for (int w = 1; w < kWarps; ++w) sum = add4(sum, *(at + w * Core::kHeads * Core::kMergePitch / 4));
+            for (int w = 1; w < kWarps; ++w) sum = add4(sum, at[w * Core::kHeads * Core::kMergePitch / 4]);
             if (whole) store_out(a, row0 + h, d, over(sum, all_l[h]));
             else if (part) *reinterpret_cast<float4*>(part + 2 * up4(a.chunk) + h * up4(a.dim) + d) = sum;
-            else *at = sum;
+            else store_remote4(at_rank(smem_at(inbox + rank * share + i / a.cluster), i % a.cluster), sum);
         }
         if (part) {
             if (t0 == 0 && tid == 0)
@@ -940,30 +944,27 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
         }
         if (a.cluster) {
             if (a.cluster == 1) return;
-            // the parts of the cluster's CTAs, each of which joins a share of the rows
-            const int rank = c % a.cluster;
+            for (int i = tid; i < a.cluster * n_heads; i += kThreads) {
+                const int to = i / n_heads, h = i - to * n_heads;
+                store_remote(at_rank(smem_at(&others[rank][0][h]), to), all_m[h]);
+                store_remote(at_rank(smem_at(&others[rank][1][h]), to), all_l[h]);
+            }
+            cluster_arrive();
             cluster_wait();
-            for (int i = tid + rank * kThreads; i < n_heads * kFours; i += kThreads * a.cluster) {
-                const int h = i / kFours, d = 4 * (i - h * kFours);
-                if (d >= a.dim) continue;
-                float m[8], top = kLowest, l = 0.0f;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    m[k] = k < a.cluster ? load_remote(at_rank(&all_m[h], k)) : kLowest;
-                    top = fmaxf(top, m[k]);
-                }
+            for (int n = tid; n < share; n += kThreads) {
+                const int i = n * a.cluster + rank, h = i / kFours, d = 4 * (i - h * kFours);
+                if (h >= n_heads || d >= a.dim) continue;
+                float top = kLowest, l = 0.0f;
+                for (int k = 0; k < a.cluster; ++k) top = fmaxf(top, others[k][0][h]);
                 float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    if (k >= a.cluster) break;
-                    const float w = weight_of(m[k], top);
-                    l = fmaf(load_remote(at_rank(&all_l[h], k)), w, l);
-                    sum = fma4(load_remote4(at_rank(merge + h * Core::kMergePitch + d, k)), w, sum);
+                for (int k = 0; k < a.cluster; ++k) {
+                    const float w = weight_of(others[k][0][h], top);
+                    l = fmaf(others[k][1][h], w, l);
+                    sum = fma4(inbox[k * share + n], w, sum);
                 }
                 store_out(a, row0 + h, d, over(sum, l));
                 if (a.lse && d == 0) a.lse[row0 + h] = lse_of(top, l, Core::kLift);
             }
-            cluster_wait();                                  // nobody leaves while another reads its shared memory
             return;
         }
         __syncthreads();
@@ -1037,7 +1038,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
 using Kernel = void (*)(const AttnArgs);
 struct Form {
     Kernel kernel = nullptr;
-    int smem = 0, heads = 0;
+    int smem = 0, inbox = 0, heads = 0;
     float lift = 0.0f;
     PerDeviceOnce* opt_in = nullptr;
     int* resident = nullptr;                                 // CTAs that an SM holds, by device
@@ -1048,7 +1049,8 @@ template <class Core, bool ASYNC> Form form_of() {
     static int resident[PerDeviceOnce::kMaxDevices] = {};
     Form f;
     f.kernel = attn_kernel<Core, ASYNC>;
-    f.smem = std::max(kWarps * Core::kStages * Core::kStage, kWarps * Core::kHeads * Core::kMergePitch * 4) + (Core::kStagesQ ? Core::kHeads * Core::kDim * 4 : 0);
+    f.inbox = std::max(kWarps * Core::kStages * Core::kStage, kWarps * Core::kHeads * Core::kMergePitch * 4) + (Core::kStagesQ ? Core::kHeads * Core::kDim * 4 : 0);
+    f.smem = std::max(Core::kLeastSmem, f.inbox + Core::kHeads * Core::kDim * 4 + 8 * 16 + 8 * 2 * Core::kHeads * 4);    // shares are rounded up for each rank
     f.heads = Core::kHeads;
     f.lift = Core::kLift;
     f.opt_in = &opt_in;
@@ -1197,8 +1199,8 @@ extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const v
     AttnArgs a{q, static_cast<const char*>(c.k), static_cast<const char*>(c.v), c.k_scales, c.v_scales, table, lengths, out, lse,
                static_cast<float*>(workspace), q_row, q_head, c.k_page * es, c.k_token * es, c.k_head * es, c.v_page * es, c.v_token * es,
                c.v_head * es, ld_table, Divisor((uint32_t)c.page_size), c.pages, c.page_size, batch, width * c.page_size, window, heads, c.kv_heads, group,
-               chunk, n_chunks, c.head_dim, granule, q_type, c.dtype, (int)std::min<int64_t>((int64_t)batch * c.kv_heads * n_chunks, resident),
-               (int64_t)batch * c.kv_heads * n_chunks <= resident, by.cluster, c.page_size % kTile == 0,
+               chunk, n_chunks, c.head_dim, granule, q_type, c.dtype, f.inbox,
+               (int)std::min<int64_t>((int64_t)batch * c.kv_heads * n_chunks, by.grid), (int64_t)batch * c.kv_heads * n_chunks <= by.grid, by.cluster, c.page_size % kTile == 0,
                c.head_dim % 4 == 0 && aligned_to(out, std::min(16, 4 * tb)), scale * kLog2e};
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = launch_pdl(f.kernel, dim3((unsigned)by.grid), dim3(kThreads), (size_t)f.smem, s, std::max(1, by.cluster), a);
