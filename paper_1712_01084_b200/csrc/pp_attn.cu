@@ -287,9 +287,9 @@ template <int KIND> __device__ __forceinline__ void widen(uint32_t four, uint32_
 }
 
 // DT: width of a row in elements, rounded up; NT: tiles of eight heads.  LOW: p enters as two numbers; one is enough where p is f16 and
-// the output bf16, whose own rounding is eight times as large.  With SPLIT_Q (a.q_type f32, NT = 2) the second tile
-// holds what the rounding of the first one's eight heads to f16 left.
-template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
+// the output bf16, whose own rounding is eight times as large.  QP: numbers to an element of q, two for
+// floats (the second is what the rounding to f16 left).
+template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
     static constexpr bool kQ8 = KIND >= kE4m3, kIsBf16 = KIND == kBf16;
     static constexpr int kEs = kQ8 ? 1 : 2, kChunks = DT * kEs / 16, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
     static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = 2;
@@ -302,7 +302,7 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
     // p is at most 2^(kLift + kSlack): f16 numbers end at 65504, and below 2^-24 they are lost, which a p can be beside the largest one
     static constexpr float kLift = kIsBf16 ? 0.0f : 7.0f;
 
-    uint32_t q[DT / 16][NT][2];
+    uint32_t q[DT / 16][NT][2][QP];
     // by head: the running maximum, kLift less it, the sum, what a product is multiplied with; the largest scale of a value and its inverse
     float acc[DT / 16][NT][4], m[NT][2], c[NT][2], l[NT][2], f[NT][2], vm, inverse;
 
@@ -320,14 +320,12 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
 #pragma unroll
                 for (int j = 0; j < DT / 16; ++j)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) q[j][nt][i] = live && 16 * j + 8 * i + 2 * t < a.dim ? row[8 * j + 4 * i] : 0u;
+                    for (int i = 0; i < 2; ++i) q[j][nt][i][0] = live && 16 * j + 8 * i + 2 * t < a.dim ? row[8 * j + 4 * i] : 0u;
             } else {
-                const bool split = NT == 2 && a.q_type == PP_F32, lows = split && nt == 1;
-                const int head = split ? g : nt * 8 + g;
-                const int64_t row = r * a.q_row + (int64_t)(head0 + head) * a.q_head + 4 * t;
-                const bool live = head < n_heads;
+                const int64_t row = r * a.q_row + (int64_t)(head0 + nt * 8 + g) * a.q_head + 4 * t;
+                const bool live = nt * 8 + g < n_heads;
                 float4 x[DT / 16];
-                if (a.q_type == PP_F32) {
+                if constexpr (QP == 2) {
 #pragma unroll
                     for (int j = 0; j < DT / 16; ++j)
                         x[j] = live && 16 * j + 4 * t < a.dim ? *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + row + 16 * j) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -356,12 +354,12 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
 #pragma unroll
                 for (int j = 0; j < DT / 16; ++j) {
                     const float4 v = make_float4(x[j].x * down, x[j].y * down, x[j].z * down, x[j].w * down);
-                    q[j][nt][0] = pack2<false>(v.x, v.y);
-                    q[j][nt][1] = pack2<false>(v.z, v.w);
-                    if (lows) {
-                        const float2 u = unpack2<false>(q[j][nt][0]), w = unpack2<false>(q[j][nt][1]);
-                        q[j][nt][0] = pack2<false>(v.x - u.x, v.y - u.y);
-                        q[j][nt][1] = pack2<false>(v.z - w.x, v.w - w.y);
+                    q[j][nt][0][0] = pack2<false>(v.x, v.y);
+                    q[j][nt][1][0] = pack2<false>(v.z, v.w);
+                    if constexpr (QP == 2) {
+                        const float2 u = unpack2<false>(q[j][nt][0][0]), w = unpack2<false>(q[j][nt][1][0]);
+                        q[j][nt][0][1] = pack2<false>(v.x - u.x, v.y - u.y);
+                        q[j][nt][1][1] = pack2<false>(v.z - w.x, v.w - w.y);
                     }
                 }
             }
@@ -384,7 +382,6 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
 
     __device__ __forceinline__ void tile(const AttnArgs& a, uint32_t stage, uint32_t bits) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-        const bool split = kQ8 && a.q_type == PP_F32;
         float s[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -402,7 +399,9 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
                     widen<KIND>(k[2 * i], a0, a2);
                     widen<KIND>(k[2 * i + 1], a1, a3);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma<kIsBf16>(s[nt], a0, a1, a2, a3, q[c + i][nt][0], q[c + i][nt][1]);
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < QP; ++e) mma<kIsBf16>(s[nt], a0, a1, a2, a3, q[c + i][nt][0][e], q[c + i][nt][1][e]);
                 }
             }
         } else {
@@ -411,16 +410,9 @@ template <int DT, int NT, int KIND, bool LOW> struct MmaCore {
                 uint32_t k[4];
                 load_matrices(k, rows + j * 32);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<kIsBf16>(s[nt], k[0], k[1], k[2], k[3], q[j][nt][0], q[j][nt][1]);
+                for (int nt = 0; nt < NT; ++nt) mma<kIsBf16>(s[nt], k[0], k[1], k[2], k[3], q[j][nt][0][0], q[j][nt][1][0]);
             }
         }
-        if (NT == 2 && split)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[0][i] += s[NT - 1][i];
-                s[NT - 1][i] = 0.0f;
-            }
-
         float v0 = 1.0f, v1 = 1.0f, most = 0.0f;             // scales of the values at g and g + 8
         if constexpr (kQ8) {
             float k0, k1;
@@ -1057,10 +1049,14 @@ template <class Core, bool ASYNC> Form form_of() {
     f.resident = resident;
     return f;
 }
-template <int KIND, bool LOW> Form mma_form(int dim, bool two) {
-    if (two) return dim <= 64 ? form_of<MmaCore<64, 2, KIND, LOW>, true>() : dim <= 96 ? form_of<MmaCore<96, 2, KIND, LOW>, true>() : form_of<MmaCore<128, 2, KIND, LOW>, true>();
-    return dim <= 64 ? form_of<MmaCore<64, 1, KIND, LOW>, true>() : dim <= 96 ? form_of<MmaCore<96, 1, KIND, LOW>, true>()
-         : dim <= 128 ? form_of<MmaCore<128, 1, KIND, LOW>, true>() : dim <= 192 ? form_of<MmaCore<192, 1, KIND, LOW>, true>() : form_of<MmaCore<256, 1, KIND, LOW>, true>();
+template <int KIND, bool LOW, int QP> Form mma_form(int dim, bool two) {
+    if constexpr (QP == 1)
+        if (two) return dim <= 64 ? form_of<MmaCore<64, 2, KIND, LOW, QP>, true>() : dim <= 96 ? form_of<MmaCore<96, 2, KIND, LOW, QP>, true>() : form_of<MmaCore<128, 2, KIND, LOW, QP>, true>();
+    return dim <= 64 ? form_of<MmaCore<64, 1, KIND, LOW, QP>, true>() : dim <= 96 ? form_of<MmaCore<96, 1, KIND, LOW, QP>, true>()
+         : dim <= 128 ? form_of<MmaCore<128, 1, KIND, LOW, QP>, true>() : dim <= 192 ? form_of<MmaCore<192, 1, KIND, LOW, QP>, true>() : form_of<MmaCore<256, 1, KIND, LOW, QP>, true>();
+}
+template <int KIND> Form mma_form8(pp_dtype_t q_type, int dim, bool two) {
+    return q_type == PP_BF16 ? mma_form<KIND, false, 1>(dim, two) : q_type == PP_F16 ? mma_form<KIND, true, 1>(dim, two) : mma_form<KIND, true, 2>(dim, false);
 }
 template <bool ASYNC> Form scalar_form(int dim, int group) {
     if (dim <= 64) return group <= 1 ? form_of<ScalarCore<64, 1, ASYNC>, ASYNC>() : group <= 4 ? form_of<ScalarCore<64, 4, ASYNC>, ASYNC>() : form_of<ScalarCore<64, 8, ASYNC>, ASYNC>();
@@ -1074,17 +1070,16 @@ Form choose(const pp_paged_cache_t& c, pp_dtype_t q_type, int q_on, int group, i
     const int row = c.head_dim * type_bytes(c.dtype);
     granule = std::min(cache_alignment(c), 16);
     while (row % granule) granule /= 2;
-    const bool split = is_8bit(c.dtype) && q_type == PP_F32;  // q as two f16 numbers takes both tiles
     chunk = 8;
-    if (granule >= 4 && c.dtype != PP_F32 && !(split && c.head_dim > 128) && q_on >= (!is_8bit(c.dtype) ? 4 : q_type == PP_F32 ? 16 : 8)) {
-        // 16 heads where a key-value head has more than 8: above 128 dimensions their sums do not fit the registers
-        const bool two = split || (group > 8 && c.head_dim <= 128);
-        if (two && !split) chunk = 16;
+    if (granule >= 4 && c.dtype != PP_F32 && q_on >= (!is_8bit(c.dtype) ? 4 : q_type == PP_F32 ? 16 : 8)) {
+        // 16 heads where a key-value head has more than 8: above 128 dimensions, or with q as two numbers, they do not fit the registers
+        const bool two = group > 8 && c.head_dim <= 128 && q_type != PP_F32;
+        if (two) chunk = 16;
         switch (c.dtype) {
-            case PP_BF16: return mma_form<kBf16, true>(c.head_dim, two);
-            case PP_F16: return mma_form<kF16, true>(c.head_dim, two);
-            case PP_E4M3: return q_type == PP_BF16 ? mma_form<kE4m3, false>(c.head_dim, two) : mma_form<kE4m3, true>(c.head_dim, two);
-            default: return q_type == PP_BF16 ? mma_form<kInt8, false>(c.head_dim, two) : mma_form<kInt8, true>(c.head_dim, two);
+            case PP_BF16: return mma_form<kBf16, true, 1>(c.head_dim, two);
+            case PP_F16: return mma_form<kF16, true, 1>(c.head_dim, two);
+            case PP_E4M3: return mma_form8<kE4m3>(q_type, c.head_dim, two);
+            default: return mma_form8<kInt8>(q_type, c.head_dim, two);
         }
     }
     const Form f = granule >= 4 && c.dtype == PP_F32 ? scalar_form<true>(c.head_dim, group) : scalar_form<false>(c.head_dim, group);
