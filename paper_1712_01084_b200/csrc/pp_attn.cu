@@ -43,7 +43,8 @@ struct AttnArgs {
     int notes;                                               // in the workspace
     bool by_head;                                            // a note's place is the head's, not the CTA's
     int cluster;                                             // CTAs that share a head (chunk); 0: all heads in a row, cut into equal parts
-    bool whole_tiles;                                        // pages are a whole number of tiles long
+    int unit_in_page;                                        // kUnit modulo the page size
+    bool whole_tiles;                                        // no tile crosses pages, distances fit 32 bits, and pieces are 16 or 8 bytes
     bool wide_out;                                           // four neighbours of out are one access
     float scale;                                             // times log2 e
 };
@@ -133,14 +134,26 @@ struct Reader {
     const char *k, *v;
     const float *ks, *vs;
     const int32_t* row;                                      // of the table
-    int low, end, entry;                                     // positions low .. end - 1; entry: of the next tile, for position lane & 15
+    int low, end;                                            // positions low .. end - 1 count
+    int at, n, place;                                        // the next tile: its position, its number, and where in its page it starts
+    int entry, next;                                         // table entries, see below
 };
 
-// The table entry of this lane's position in the tile at `at`, -1 for positions that are not asked for.  In whole tiles all
-// lanes look up the first position's.
-__device__ __forceinline__ int entry_of(const AttnArgs& a, const Reader& r, int at) {
-    const int p = a.whole_tiles ? at : at + (threadIdx.x & 15);
-    return (a.whole_tiles || p >= r.low) && p < r.end ? r.row[a.page.of((uint32_t)p)] : -1;
+// Table entries.  In whole tiles (a.whole_tiles) lane i holds that of the i-th tile of a batch of 32, and of the batch behind it;
+// otherwise that of position lane & 15 of the next tile.  -1: not asked for.
+__device__ __forceinline__ int entry_of(const AttnArgs& a, const Reader& r, int at) { return at < r.end ? r.row[a.page.of((uint32_t)at)] : -1; }
+__device__ __forceinline__ int position_entry(const AttnArgs& a, const Reader& r, int at) {
+    const int p = at + (threadIdx.x & 15);
+    return p >= r.low ? entry_of(a, r, p) : -1;
+}
+__device__ __forceinline__ void start(const AttnArgs& a, Reader& r) {
+    r.n = 0;
+    if (a.whole_tiles) {
+        r.place = r.at - (int)a.page.of((uint32_t)r.at) * a.page_size;
+        r.next = entry_of(a, r, r.at + (int)(threadIdx.x & 31) * kUnit);
+    } else {
+        r.entry = position_entry(a, r, r.at);
+    }
 }
 // Bits of the tile's positions between low and end.
 __device__ __forceinline__ uint32_t positions_of(const Reader& r, int at) {
@@ -190,41 +203,79 @@ __device__ __noinline__ uint32_t ask_by_row(const AttnArgs& a, const char* k, co
     return bits;
 }
 
-// Asks for the tile at `at`: 16 rows of keys, of values, and the scales of both.  Returns which rows are there.
+// The same for rows a fixed distance apart, in pieces of 8 bytes.
+template <int CHUNKS, int PITCH>
+__device__ __noinline__ void ask_eights(const char* k, const char* v, uint32_t k_token, uint32_t v_token, int own, uint32_t bits, uint32_t stage) {
+    constexpr int kPieces = CHUNKS * 2, kLanes = kPieces > 16 ? 32 : kPieces > 8 ? 16 : 8, kRows = 32 / kLanes;
+    const int lane = threadIdx.x & 31, row = lane / kLanes;
+    for (int c = lane & (kLanes - 1); c < kPieces; c += kLanes) {
+        const bool in = c < own;
+#pragma unroll 4
+        for (int i = row; i < kTile; i += kRows) {
+            const bool has = in && ((bits >> i) & 1);
+            copy_async<8>(stage + i * PITCH + c * 8, k + (uint64_t)i * k_token + (in ? c * 8 : 0), has);
+            copy_async<8>(stage + kTile * PITCH + i * PITCH + c * 8, v + (uint64_t)i * v_token + (in ? c * 8 : 0), has);
+        }
+    }
+}
+
+// Asks for the next tile: 16 rows of keys, of values, and the scales of both.  Returns which rows are there.
 // ES: bytes of an element, CHUNKS: 16-byte pieces of a row as the kernel sees it (rows that are shorter end in zeros).
 template <int ES, int CHUNKS, int PITCH, bool Q8>
-__device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, int at, uint32_t stage) {
+__device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, uint32_t stage) {
     constexpr int kTileBytes = kTile * PITCH;
     constexpr int kLanes = CHUNKS > 16 ? 32 : CHUNKS > 8 ? 16 : CHUNKS > 4 ? 8 : 4, kRows = 32 / kLanes;
-    const int found = r.entry;
-    r.entry = entry_of(a, r, at + kUnit);
-    if (!a.whole_tiles || a.granule != 16) return ask_by_row<ES, CHUNKS, PITCH, Q8>(a, r.k, r.v, r.ks, r.vs, r.low, r.end, found, at, stage);
-    // one page: rows a fixed distance apart
-    const int lane = threadIdx.x & 31, row = lane / kLanes;
+    const int lane = threadIdx.x & 31, at = r.at;
+    r.at += kUnit;
+    if (!a.whole_tiles) {
+        const int found = r.entry;
+        r.entry = position_entry(a, r, r.at);
+        return ask_by_row<ES, CHUNKS, PITCH, Q8>(a, r.k, r.v, r.ks, r.vs, r.low, r.end, found, at, stage);
+    }
+    if (r.n % 32 == 0) {
+        r.entry = r.next;
+        r.next = entry_of(a, r, at + (32 + lane) * kUnit);
+    }
+    const int found = __shfl_sync(0xffffffffu, r.entry, r.n % 32);
+    ++r.n;
+    const int place = r.place;
+    r.place += a.unit_in_page;
+    if (r.place >= a.page_size) r.place -= a.page_size;
+    // rows a fixed distance apart, which fits 32 bits
     const bool is_page = (uint32_t)found < (uint32_t)a.pages;
-    const int entry = is_page ? found : 0, place = at - (int)a.page.of((uint32_t)at) * a.page_size;
-    const uint32_t bits = is_page ? positions_of(r, at) : 0;
-    const char* k = r.k + (int64_t)entry * a.k_page + (int64_t)(place + row) * a.k_token;
-    const char* v = r.v + (int64_t)entry * a.v_page + (int64_t)(place + row) * a.v_token;
+    const uint32_t entry = is_page ? (uint32_t)found : 0u, bits = is_page ? positions_of(r, at) : 0u;
+    const uint32_t k_token = (uint32_t)a.k_token, v_token = (uint32_t)a.v_token;
+    const char* k = r.k + (uint64_t)entry * (uint32_t)a.k_page + (uint64_t)(uint32_t)place * k_token;
+    const char* v = r.v + (uint64_t)entry * (uint32_t)a.v_page + (uint64_t)(uint32_t)place * v_token;
+    if (a.granule == 16) {
+        const int row = lane / kLanes;
+        k += (uint64_t)(uint32_t)row * k_token;
+        v += (uint64_t)(uint32_t)row * v_token;
+        const auto copy = [&](auto all) {                    // all: every row is there
 #pragma unroll
-    for (int i = 0; i < kTile / kRows; ++i) {
-        const bool has = (bits >> (i * kRows + row)) & 1;
+            for (int i = 0; i < kTile / kRows; ++i) {
+                const bool has = decltype(all)::value || ((bits >> (i * kRows + row)) & 1);
 #pragma unroll
-        for (int c0 = 0; c0 < CHUNKS; c0 += kLanes) {
-            const int c = c0 + (lane & (kLanes - 1));
-            if (CHUNKS % kLanes && c >= CHUNKS) continue;
-            const bool own = c * 16 < a.dim * ES;
-            const uint32_t dst = stage + (i * kRows + row) * PITCH + c * 16;
-            copy_async<16>(dst, k + (own ? c * 16 : 0), own && has);
-            copy_async<16>(dst + kTileBytes, v + (own ? c * 16 : 0), own && has);
-        }
-        k += kRows * a.k_token;
-        v += kRows * a.v_token;
+                for (int c0 = 0; c0 < CHUNKS; c0 += kLanes) {
+                    const int c = c0 + (lane & (kLanes - 1));
+                    if (CHUNKS % kLanes && c >= CHUNKS) continue;
+                    const bool own = c * 16 < a.dim * ES;
+                    const int piece = own ? c * 16 : 0;
+                    const uint32_t dst = stage + (i * kRows + row) * PITCH + c * 16;
+                    copy_async<16>(dst, k + (uint64_t)(uint32_t)(i * kRows) * k_token + piece, own && has);
+                    copy_async<16>(dst + kTileBytes, v + (uint64_t)(uint32_t)(i * kRows) * v_token + piece, own && has);
+                }
+            }
+        };
+        if (bits == 0xffffu) copy(std::true_type());
+        else copy(std::false_type());
+    } else {
+        ask_eights<CHUNKS, PITCH>(k, v, k_token, v_token, a.dim * ES / 8, bits, stage);
     }
     if constexpr (Q8) {
         const bool in = (bits >> (lane & 15)) & 1;
-        const int64_t token = (int64_t)entry * a.page_size + place + (in ? lane & 15 : 0);
-        copy_async<4>(stage + 2 * kTileBytes + lane * 4, (lane < 16 ? r.ks : r.vs) + token * a.kv_heads, in);
+        const uint32_t token = entry * (uint32_t)a.page_size + (uint32_t)place + (in ? lane & 15 : 0);       // below 2^32 (a.whole_tiles)
+        copy_async<4>(stage + 2 * kTileBytes + lane * 4, (lane < 16 ? r.ks : r.vs) + (uint64_t)token * (uint32_t)a.kv_heads, in);
     }
     return bits;
 }
@@ -292,12 +343,12 @@ template <int KIND> __device__ __forceinline__ void widen(uint32_t four, uint32_
 template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
     static constexpr bool kQ8 = KIND >= kE4m3, kIsBf16 = KIND == kBf16;
     static constexpr int kEs = kQ8 ? 1 : 2, kChunks = DT * kEs / 16, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
-    static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = 2;
+    static constexpr int kCtas = kQ8 && DT * NT <= 128 ? 4 : kQ8 || DT * NT <= 96 ? 3 : 1;      // resident ones that the registers are cut for
+    static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = DT <= 64 ? 3 : 2;
     static constexpr int kHeads = 8 * NT, kMergePitch = DT + 4;
-    // Resident CTAs that the registers are cut for.  16-bit rows of 128: no more than two by their shared memory.  They keep 140 KB on
-    // their way to an SM, and with three (or a third stage) the SMs' shares of the memory differ so much that the last CTA ends 20 %
-    // behind the mean (64 x 8192: 254 us with two, 268 with three).
-    static constexpr int kDim = DT, kCtas = kQ8 && DT * NT <= 128 ? 4 : kQ8 || DT * NT <= 96 ? 3 : 1, kLeastSmem = kQ8 || DT < 128 ? 0 : 77 * 1024;
+    // 16-bit rows of 128: no more than two CTAs by their shared memory.  With three, or a third stage, the SMs' shares of the memory differ
+    // so much that the last CTA ends 20 % behind the mean (64 x 8192: 254 us with two, 268 with three).
+    static constexpr int kDim = DT, kLeastSmem = kQ8 || DT < 128 ? 0 : 77 * 1024;
     static constexpr bool kStagesQ = false;
     // p is at most 2^(kLift + kSlack): f16 numbers end at 65504, and below 2^-24 they are lost, which a p can be beside the largest one
     static constexpr float kLift = kIsBf16 ? 0.0f : 7.0f;
@@ -596,13 +647,13 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
         }
     }
 
-    // ASYNC false: the tile at `at`, element by element
-    __device__ static uint32_t fetch(const AttnArgs& a, Reader& r, int at, float* stage) {
-        const int lane = threadIdx.x & 31, p = at + (lane & 15);
-        const int entry = a.whole_tiles && (p < r.low || p >= r.end) ? -1 : r.entry;
-        const bool there = (uint32_t)entry < (uint32_t)a.pages;
+    // ASYNC false: the next tile, element by element
+    __device__ static uint32_t fetch(const AttnArgs& a, Reader& r, float* stage) {
+        const int lane = threadIdx.x & 31, p = r.at + (lane & 15), entry = r.entry;
+        const bool there = p >= r.low && p < r.end && (uint32_t)entry < (uint32_t)a.pages;
         const uint32_t bits = __ballot_sync(0xffffffffu, there) & 0xffffu;
-        r.entry = entry_of(a, r, at + kUnit);
+        r.at += kUnit;
+        r.entry = position_entry(a, r, r.at);
         int64_t off = 0;
         float scale = 1.0f;
         if (there) {
@@ -842,17 +893,16 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
         reader.row = a.table + r * a.ld_table;
         reader.low = first_position(a, length);
         reader.end = min(length, low + t1 * kUnit);
-        int ask_at = low + t0 * kUnit + warp * kTile;
-        reader.entry = entry_of(a, reader, ask_at);
-        const int tiles = ask_at < reader.end ? (reader.end - ask_at + kUnit - 1) / kUnit : 0;
+        reader.at = low + t0 * kUnit + warp * kTile;
+        const int tiles = reader.at < reader.end ? (reader.end - reader.at + kUnit - 1) / kUnit : 0;
+        start(a, reader);
         uint64_t there = 0;                                  // the rows that are there, 16 bits for each tile on its way, the last one's lowest
         int asked = 0, stage = 0;
         const auto request = [&]() {
             uint32_t bits = 0;
             if (asked < tiles) {
-                if constexpr (ASYNC) bits = ask<Core::kEs, Core::kChunks, Core::kPitch, Core::kQ8>(a, reader, ask_at, smem_at(own + stage * Core::kStage));
-                else bits = Core::fetch(a, reader, ask_at, reinterpret_cast<float*>(own + stage * Core::kStage));
-                ask_at += kUnit;
+                if constexpr (ASYNC) bits = ask<Core::kEs, Core::kChunks, Core::kPitch, Core::kQ8>(a, reader, smem_at(own + stage * Core::kStage));
+                else bits = Core::fetch(a, reader, reinterpret_cast<float*>(own + stage * Core::kStage));
             }
             there = there << 16 | bits;
             commit();
@@ -1032,6 +1082,7 @@ struct Form {
     Kernel kernel = nullptr;
     int smem = 0, inbox = 0, heads = 0;
     float lift = 0.0f;
+    bool async = false;
     PerDeviceOnce* opt_in = nullptr;
     int* resident = nullptr;                                 // CTAs that an SM holds, by device
 };
@@ -1045,6 +1096,7 @@ template <class Core, bool ASYNC> Form form_of() {
     f.smem = std::max(Core::kLeastSmem, f.inbox + Core::kHeads * Core::kDim * 4 + 8 * 16 + 8 * 2 * Core::kHeads * 4);    // shares are rounded up for each rank
     f.heads = Core::kHeads;
     f.lift = Core::kLift;
+    f.async = ASYNC;
     f.opt_in = &opt_in;
     f.resident = resident;
     return f;
@@ -1191,11 +1243,14 @@ extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const v
     const Division by = divide(c, batch, width, window, chunk, n_chunks, resident);
     if (by.bytes && (!workspace || workspace_bytes < by.bytes)) return PP_ERR_INVALID_ARG;
     const int es = type_bytes(c.dtype);
+    const int64_t far = std::max({c.k_page, c.k_token, c.v_page, c.v_token}) * es;
+    // the form that reads element by element has its own way
+    const bool whole = c.page_size % kTile == 0 && granule >= 8 && far <= UINT32_MAX && (int64_t)c.pages * c.page_size <= UINT32_MAX && f.async;
     AttnArgs a{q, static_cast<const char*>(c.k), static_cast<const char*>(c.v), c.k_scales, c.v_scales, table, lengths, out, lse,
                static_cast<float*>(workspace), q_row, q_head, c.k_page * es, c.k_token * es, c.k_head * es, c.v_page * es, c.v_token * es,
                c.v_head * es, ld_table, Divisor((uint32_t)c.page_size), c.pages, c.page_size, batch, width * c.page_size, window, heads, c.kv_heads, group,
                chunk, n_chunks, c.head_dim, granule, q_type, c.dtype, f.inbox,
-               (int)std::min<int64_t>((int64_t)batch * c.kv_heads * n_chunks, by.grid), (int64_t)batch * c.kv_heads * n_chunks <= by.grid, by.cluster, c.page_size % kTile == 0,
+               (int)std::min<int64_t>((int64_t)batch * c.kv_heads * n_chunks, by.grid), (int64_t)batch * c.kv_heads * n_chunks <= by.grid, by.cluster, kUnit % c.page_size, whole,
                c.head_dim % 4 == 0 && aligned_to(out, std::min(16, 4 * tb)), scale * kLog2e};
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = launch_pdl(f.kernel, dim3((unsigned)by.grid), dim3(kThreads), (size_t)f.smem, s, std::max(1, by.cluster), a);
