@@ -40,20 +40,22 @@ struct AttnArgs {
     Divisor page;
     int pages, page_size, batch, capacity, window, heads, kv_heads, group, chunk, n_chunks, dim, granule, q_type, type;
     int inbox;                                               // where a cluster's CTAs write in each other's shared memory, in bytes
-    int notes;                                               // in the workspace
+    int notes, part_rows;                                    // in the workspace; rows of a partial result
     bool by_head;                                            // a note's place is the head's, not the CTA's
     int cluster;                                             // CTAs that share a head (chunk); 0: all heads in a row, cut into equal parts
-    int unit_in_page;                                        // kUnit modulo the page size
+    // A unit of work: 64 positions of one key-value head, 16 to a warp, or (across) 16 positions of four heads, one to a warp
+    int unit, unit_in_page;                                  // its positions; these modulo the page size
+    bool across;
     bool whole_tiles;                                        // no tile crosses pages, distances fit 32 bits, and pieces are 16 or 8 bytes
     bool wide_out;                                           // four neighbours of out are one access
     float scale;                                             // times log2 e
 };
 
-// The workspace: a note for each CTA (four ints), then two partial results for each.  A partial result: m and l of each head of the
-// chunk, then their sums, all on 16 bytes.
+// The workspace: a note for each CTA (four ints), then two partial results for each.  A partial result: m and l of each row,
+// then their sums, all on 16 bytes.
 __host__ __device__ inline int64_t notes_floats(int64_t ctas) { return 4 * ctas; }
 __host__ __device__ inline int up4(int n) { return (n + 3) & ~3; }
-__host__ __device__ inline int64_t part_floats(int chunk, int dim) { return 2 * up4(chunk) + (int64_t)chunk * up4(dim); }
+__host__ __device__ inline int64_t part_floats(int rows, int dim) { return 2 * up4(rows) + (int64_t)rows * up4(dim); }
 
 __device__ __forceinline__ int first_position(const AttnArgs& a, int length) { return a.window > 0 ? max(0, length - a.window) : 0; }
 // Units start at a whole tile: where pages are whole tiles long, no tile then crosses from one page into another.
@@ -62,7 +64,7 @@ __device__ __forceinline__ int length_of(const AttnArgs& a, int r) { return min(
 // Units of one head of a request: one at least, which writes the output of a request without positions.
 __device__ __forceinline__ int units_of(const AttnArgs& a, int r) {
     const int n = length_of(a, r);
-    return max(1, (n - first_tile(a, n) + kUnit - 1) / kUnit);
+    return max(1, (n - first_tile(a, n) + a.unit - 1) / a.unit);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -129,7 +131,7 @@ template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, co
 __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void wait_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// What a warp reads: consecutive positions of one request and key-value head, in tiles kWarps * kTile apart.
+// What a warp reads: positions of one request and key-value head, in tiles a.unit apart.
 struct Reader {
     const char *k, *v;
     const float *ks, *vs;
@@ -150,7 +152,7 @@ __device__ __forceinline__ void start(const AttnArgs& a, Reader& r) {
     r.n = 0;
     if (a.whole_tiles) {
         r.place = r.at - (int)a.page.of((uint32_t)r.at) * a.page_size;
-        r.next = entry_of(a, r, r.at + (int)(threadIdx.x & 31) * kUnit);
+        r.next = entry_of(a, r, r.at + (int)(threadIdx.x & 31) * a.unit);
     } else {
         r.entry = position_entry(a, r, r.at);
     }
@@ -226,7 +228,7 @@ __device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, uint32_t s
     constexpr int kTileBytes = kTile * PITCH;
     constexpr int kLanes = CHUNKS > 16 ? 32 : CHUNKS > 8 ? 16 : CHUNKS > 4 ? 8 : 4, kRows = 32 / kLanes;
     const int lane = threadIdx.x & 31, at = r.at;
-    r.at += kUnit;
+    r.at += a.unit;
     if (!a.whole_tiles) {
         const int found = r.entry;
         r.entry = position_entry(a, r, r.at);
@@ -234,7 +236,7 @@ __device__ __forceinline__ uint32_t ask(const AttnArgs& a, Reader& r, uint32_t s
     }
     if (r.n % 32 == 0) {
         r.entry = r.next;
-        r.next = entry_of(a, r, at + (32 + lane) * kUnit);
+        r.next = entry_of(a, r, at + (32 + lane) * a.unit);
     }
     const int found = __shfl_sync(0xffffffffu, r.entry, r.n % 32);
     ++r.n;
@@ -343,7 +345,8 @@ template <int KIND> __device__ __forceinline__ void widen(uint32_t four, uint32_
 template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
     static constexpr bool kQ8 = KIND >= kE4m3, kIsBf16 = KIND == kBf16;
     static constexpr int kEs = kQ8 ? 1 : 2, kChunks = DT * kEs / 16, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
-    static constexpr int kCtas = kQ8 && DT * NT <= 128 ? 4 : kQ8 || DT * NT <= 96 ? 3 : 1;      // resident ones that the registers are cut for
+    // Resident CTAs that the registers are cut for: by those that sums and q take
+    static constexpr int kHeld = DT * NT * (4 + 2 * QP) / 16, kCtas = kQ8 ? (kHeld <= 36 ? 4 : kHeld <= 64 ? 3 : 2) : kHeld <= 36 ? 3 : 1;
     static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = DT <= 64 ? 3 : 2;
     static constexpr int kHeads = 8 * NT, kMergePitch = DT + 4;
     // 16-bit rows of 128: no more than two CTAs by their shared memory.  With three, or a third stage, the SMs' shares of the memory differ
@@ -604,15 +607,15 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
                 }
             }
     }
-    // its sums, relative to the largest m of all warps
-    __device__ __forceinline__ void sums(const float (*all)[kHeads], float* to) {
+    // its sums, relative to the largest m of all warps or to its own
+    __device__ __forceinline__ void sums(const float (*all)[kHeads], bool own, float* to) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int head = nt * 8 + 2 * t + b;
-                float by = weight_of(m[nt][b], top_of<kHeads>(all, head));
+                float by = own ? 1.0f : weight_of(m[nt][b], top_of<kHeads>(all, head));
                 if (kQ8) by *= vm;
 #pragma unroll
                 for (int j = 0; j < DT / 16; ++j)
@@ -652,7 +655,7 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
         const int lane = threadIdx.x & 31, p = r.at + (lane & 15), entry = r.entry;
         const bool there = p >= r.low && p < r.end && (uint32_t)entry < (uint32_t)a.pages;
         const uint32_t bits = __ballot_sync(0xffffffffu, there) & 0xffffu;
-        r.at += kUnit;
+        r.at += a.unit;
         r.entry = position_entry(a, r, r.at);
         int64_t off = 0;
         float scale = 1.0f;
@@ -758,11 +761,11 @@ template <int DT, int HN, bool ASYNC> struct ScalarCore {
             }
         }
     }
-    __device__ __forceinline__ void sums(const float (*all)[kHeads], float* to) {
+    __device__ __forceinline__ void sums(const float (*all)[kHeads], bool own, float* to) {
         const int lane = threadIdx.x & 31;
 #pragma unroll
         for (int h = 0; h < HN; ++h) {
-            const float by = weight_of(m[h], top_of<kHeads>(all, h));
+            const float by = own ? 1.0f : weight_of(m[h], top_of<kHeads>(all, h));
 #pragma unroll
             for (int i = 0; i < DT / 32; ++i) to[h * kMergePitch + lane + 32 * i] = acc[i][h] * by;
         }
@@ -835,7 +838,7 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
     if (a.cluster > 1) cluster_arrive();                     // awaited before the first write to another CTA's memory: it has started by then
     pdl_wait();
 
-    const int per_request = a.kv_heads * a.n_chunks;
+    const int per_request = (a.across ? a.kv_heads / kWarps : a.kv_heads) * a.n_chunks;
     int r, base = 0, u = 0, begin = 0, end = 1, ctas = 0, all = 0;    // unit u of the row of all, request r's from base on
     if (a.cluster) {
         r = c / a.cluster / per_request;
@@ -882,8 +885,8 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
             t0 = u - base - hc * units;
             t1 = min(units, t0 + (end - u));
         }
-        const int kv = hc / a.n_chunks, head_in = (hc - kv * a.n_chunks) * a.chunk, n_heads = min(a.chunk, a.group - head_in);
-        const int head0 = kv * a.group + head_in;
+        const int first_kv = hc / a.n_chunks * (a.across ? kWarps : 1), kv = a.across ? first_kv + warp : first_kv;
+        const int head_in = hc % a.n_chunks * a.chunk, n_heads = min(a.chunk, a.group - head_in), head0 = kv * a.group + head_in;
 
         Reader reader;
         reader.k = a.k + kv * a.k_head;
@@ -892,9 +895,9 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
         reader.vs = a.vs + kv;
         reader.row = a.table + r * a.ld_table;
         reader.low = first_position(a, length);
-        reader.end = min(length, low + t1 * kUnit);
-        reader.at = low + t0 * kUnit + warp * kTile;
-        const int tiles = reader.at < reader.end ? (reader.end - reader.at + kUnit - 1) / kUnit : 0;
+        reader.end = min(length, low + t1 * a.unit);
+        reader.at = low + t0 * a.unit + (a.across ? 0 : warp * kTile);
+        const int tiles = reader.at < reader.end ? (reader.end - reader.at + a.unit - 1) / a.unit : 0;
         start(a, reader);
         uint64_t there = 0;                                  // the rows that are there, 16 bits for each tile on its way, the last one's lowest
         int asked = 0, stage = 0;
@@ -941,8 +944,8 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
         wait_but<0>();
         core.state(warp_m[warp], warp_l[warp]);
         __syncthreads();                                     // the ring is free, and every warp's m and l are known
-        core.sums(warp_m, merge + warp * Core::kHeads * Core::kMergePitch);
-        if (tid < Core::kHeads) {
+        core.sums(warp_m, a.across, merge + warp * Core::kHeads * Core::kMergePitch);
+        if (!a.across && tid < Core::kHeads) {
             const float top = top_of<Core::kHeads>(warp_m, tid);
             float sum = 0.0f;
 #pragma unroll
@@ -952,37 +955,52 @@ template <class Core, bool ASYNC> __global__ void __launch_bounds__(kThreads, Co
         }
         __syncthreads();
         const bool whole = t0 == 0 && t1 == units && a.cluster <= 1;
-        const int64_t row0 = (int64_t)r * a.heads + head0;
-        float* part = whole || a.cluster ? nullptr : a.ws + notes_floats(a.notes) + (2 * c + (u != begin)) * part_floats(a.chunk, a.dim);
+        const int64_t row0 = (int64_t)r * a.heads + first_kv * a.group + head_in;
+        float* part = whole || a.cluster ? nullptr : a.ws + notes_floats(a.notes) + (2 * c + (u != begin)) * part_floats(a.part_rows, a.dim);
         constexpr int kFours = Core::kDim / 4;               // of a row
         // a cluster's CTAs share the rows' fours among them, round robin: each sends its part of a four to the CTA that joins it
         float4* inbox = reinterpret_cast<float4*>(ring + a.inbox);                             // [rank][its fours]
         float(*others)[2][Core::kHeads] = reinterpret_cast<float(*)[2][Core::kHeads]>(inbox + Core::kHeads * kFours + 8);   // [rank]: m and l
         const int rank = a.cluster > 1 ? c % a.cluster : 0, share = a.cluster > 1 ? (n_heads * kFours + a.cluster - 1) / a.cluster : 0;
         if (a.cluster > 1) cluster_wait();
-        for (int i = tid; i < n_heads * kFours; i += kThreads) {
-            const int h = i / kFours, d = 4 * (i - h * kFours);
-            if (d >= a.dim) continue;
-            const float4* at = reinterpret_cast<const float4*>(merge + h * Core::kMergePitch + d);
-            float4 sum = *at;
+        if (a.across) {                                      // a warp's rows are its own
+            for (int i = lane; i < n_heads * kFours; i += 32) {
+                const int h = i / kFours, d = 4 * (i - h * kFours);
+                if (d >= a.dim) continue;
+                const float4 sum = *reinterpret_cast<const float4*>(merge + (warp * Core::kHeads + h) * Core::kMergePitch + d);
+                if (whole) store_out(a, row0 + warp * a.group + h, d, over(sum, warp_l[warp][h]));
+                else *reinterpret_cast<float4*>(part + 2 * up4(a.part_rows) + (warp * a.chunk + h) * up4(a.dim) + d) = sum;
+            }
+        } else {
+            for (int i = tid; i < n_heads * kFours; i += kThreads) {
+                const int h = i / kFours, d = 4 * (i - h * kFours);
+                if (d >= a.dim) continue;
+                const float4* at = reinterpret_cast<const float4*>(merge + h * Core::kMergePitch + d);
+                float4 sum = *at;
 #pragma unroll
-            for (int w = 1; w < kWarps; ++w) sum = add4(sum, at[w * Core::kHeads * Core::kMergePitch / 4]);
-            if (whole) store_out(a, row0 + h, d, over(sum, all_l[h]));
-            else if (part) *reinterpret_cast<float4*>(part + 2 * up4(a.chunk) + h * up4(a.dim) + d) = sum;
-            else store_remote4(at_rank(smem_at(inbox + rank * share + i / a.cluster), i % a.cluster), sum);
+                for (int w = 1; w < kWarps; ++w) sum = add4(sum, at[w * Core::kHeads * Core::kMergePitch / 4]);
+                if (whole) store_out(a, row0 + h, d, over(sum, all_l[h]));
+                else if (part) *reinterpret_cast<float4*>(part + 2 * up4(a.part_rows) + h * up4(a.dim) + d) = sum;
+                else store_remote4(at_rank(smem_at(inbox + rank * share + i / a.cluster), i % a.cluster), sum);
+            }
         }
         if (part) {
             if (t0 == 0 && tid == 0)
                 reinterpret_cast<Note*>(a.ws)[a.by_head ? r * per_request + hc : c] = {c, Cut(all, ctas).of(base + (hc + 1) * units - 1), (int)row0, u != begin ? -n_heads : n_heads};
-            if (tid < n_heads) {
-                part[tid] = all_m[tid];
-                part[up4(a.chunk) + tid] = all_l[tid];
-            }
         } else if (whole && a.by_head && !a.cluster && tid == 0) {
             reinterpret_cast<Note*>(a.ws)[r * per_request + hc].last = -1;
         }
-        if (whole && a.lse && tid < n_heads) {
-            a.lse[row0 + tid] = lse_of(all_m[tid], all_l[tid], Core::kLift);
+        if (part || (whole && a.lse)) {
+            const int w = a.across ? tid / n_heads : 0, h = tid - w * n_heads;
+            if (w < (a.across ? kWarps : 1) && h < n_heads) {
+                const float m = a.across ? warp_m[w][h] : all_m[h], l = a.across ? warp_l[w][h] : all_l[h];
+                if (part) {
+                    part[w * a.chunk + h] = m;
+                    part[up4(a.part_rows) + w * a.chunk + h] = l;
+                } else {
+                    a.lse[row0 + w * a.group + h] = lse_of(m, l, Core::kLift);
+                }
+            }
         }
         if (a.cluster) {
             if (a.cluster == 1) return;
@@ -1031,16 +1049,18 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.ws) + blockIdx.x);
     const Note note{raw.x, raw.y, raw.z, raw.w};
     if (note.last < 0) return;
-    const int64_t floats = part_floats(a.chunk, a.dim), second = note.rows < 0 ? floats : 0;
+    const int64_t floats = part_floats(a.part_rows, a.dim), second = note.rows < 0 ? floats : 0;
     const float* parts = a.ws + notes_floats(a.notes);
     const auto part = [&](int c) { return parts + 2 * c * floats + (c == note.first ? second : 0); };
-    const int chunk4 = up4(a.chunk), dim4 = up4(a.dim), all_rows = abs(note.rows);
+    const int rows4 = up4(a.part_rows), dim4 = up4(a.dim), n_heads = abs(note.rows), all_rows = n_heads * (a.across ? kWarps : 1);
     const int rows = (all_rows - (int)blockIdx.y + step - 1) / step;         // of this CTA
     if (rows < 1) return;
     const int at_once = min(rows, kJoinWarps), per = kJoinWarps / at_once, sub = warp % per;
     for (int done = 0; done < rows; done += at_once) {
-        const int n = done + warp / per, h = blockIdx.y + n * step;
+        const int n = done + warp / per, row = blockIdx.y + n * step, head = row / n_heads;   // head: of the four (across)
         const bool live = warp / per < at_once && n < rows;
+        const int h = head * a.chunk + row - head * n_heads;
+        const int64_t to = (int64_t)note.row + head * a.group + row - head * n_heads;
         float top = kLowest, l = 0.0f;
         float4 acc[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
         if (live) {
@@ -1051,8 +1071,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
             for (int c = note.first + sub; c <= note.last; c += per) {
                 const float* p = part(c);
                 const float w = weight_of(p[h], top);
-                l = fmaf(p[chunk4 + h], w, l);
-                const float4* x = reinterpret_cast<const float4*>(p + 2 * chunk4 + h * dim4) + lane;
+                l = fmaf(p[rows4 + h], w, l);
+                const float4* x = reinterpret_cast<const float4*>(p + 2 * rows4 + h * dim4) + lane;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     if (4 * (lane + 32 * i) < a.dim) acc[i] = fma4(x[32 * i], w, acc[i]);
@@ -1068,9 +1088,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
             for (int d = lane; 4 * d < a.dim; d += 32) {
                 float4 sum = sums[warp][d];
                 for (int w = 1; w < per; ++w) sum = add4(sum, sums[warp + w][d]);
-                store_out(a, (int64_t)note.row + h, 4 * d, over(sum, l));
+                store_out(a, to, 4 * d, over(sum, l));
             }
-            if (a.lse && lane == 0) a.lse[(int64_t)note.row + h] = lse_of(top, l, lift);
+            if (a.lse && lane == 0) a.lse[to] = lse_of(top, l, lift);
         }
         __syncthreads();
     }
@@ -1082,7 +1102,7 @@ struct Form {
     Kernel kernel = nullptr;
     int smem = 0, inbox = 0, heads = 0;
     float lift = 0.0f;
-    bool async = false;
+    bool async = false, shares_q = false;
     PerDeviceOnce* opt_in = nullptr;
     int* resident = nullptr;                                 // CTAs that an SM holds, by device
 };
@@ -1097,6 +1117,7 @@ template <class Core, bool ASYNC> Form form_of() {
     f.heads = Core::kHeads;
     f.lift = Core::kLift;
     f.async = ASYNC;
+    f.shares_q = Core::kStagesQ;
     f.opt_in = &opt_in;
     f.resident = resident;
     return f;
@@ -1175,13 +1196,15 @@ pp_status_t check_call(const pp_paged_cache_t* cache, pp_dtype_t q_type, int bat
 // How a call is divided.
 struct Division {
     int grid, cluster;                                       // cluster 0: equal parts of all units, joined by a second kernel
+    bool across;                                             // of four heads at once
+    int notes, part_rows;
     int64_t bytes;                                           // of workspace
 };
 // Costs in units of 64 positions to a CTA, some 0.6 us while latency rules, going by the table's width.  Equal parts of all units:
 // sums over lengths, the workspace and a second kernel, 4 us.  A CTA or a cluster of up to eight to each head (chunk): as many
 // rounds as the GPU needs for them, each a CTA's share and 2 us for its start and end; a cluster's exchange costs 2.3 us.
 constexpr int kEqualParts = 10, kRound = 3, kExchange = 4;
-Division divide(const pp_paged_cache_t& c, int batch, int width, int window, int chunk, int n_chunks, int resident) {
+Division divide(const pp_paged_cache_t& c, const Form& f, int batch, int width, int window, int chunk, int n_chunks, int resident) {
     const int64_t capacity = (int64_t)width * c.page_size, longest = window > 0 ? std::min<int64_t>((int64_t)window + kTile - 1, capacity) : capacity;
     const int64_t units = std::max<int64_t>(1, (longest + kUnit - 1) / kUnit), heads = (int64_t)batch * c.kv_heads * n_chunks;
     int64_t least = heads * units / resident + kEqualParts, best = 0;
@@ -1191,8 +1214,14 @@ Division divide(const pp_paged_cache_t& c, int batch, int width, int window, int
         if (cost < least && heads * cluster <= INT32_MAX) least = cost, best = cluster;
     }
     if (units == 1) best = 1;                                // nothing to divide
-    if (best) return {(int)(heads * best), (int)best, 0};
-    return {resident, 0, (notes_floats(std::min<int64_t>(heads, resident)) + (int64_t)resident * 2 * part_floats(chunk, c.head_dim)) * 4};
+    if (best) return {(int)(heads * best), (int)best, false, 0, 0, 0};
+    // Four neighbouring heads at once where the scales of their rows share lines of memory, or their rows do: where heads lie side by side
+    // and a row is no multiple of 256 bytes, heads read one after another fetch the lines between them twice (32 x 6000, eight
+    // heads of 72 / 96: 88 / 98 us one by one, 72 / 84 us by four; 256-byte rows: 103 against 105; 16 query heads to each: 61 against 68).
+    const bool side_by_side = c.k_head < c.k_token && c.head_dim * type_bytes(c.dtype) % 256 != 0;
+    const bool across = c.kv_heads % kWarps == 0 && !f.shares_q && chunk <= 8 && (is_8bit(c.dtype) || side_by_side);
+    const int notes = (int)std::min<int64_t>(across ? heads / kWarps : heads, resident), rows = across ? kWarps * chunk : chunk;
+    return {resident, 0, across, notes, rows, (notes_floats(notes) + (int64_t)resident * 2 * part_floats(rows, c.head_dim)) * 4};
 }
 
 }  // namespace
@@ -1212,7 +1241,7 @@ extern "C" pp_status_t pp_paged_attention_workspace(const pp_paged_cache_t* cach
         const int group = heads / cache->kv_heads;
         const Form f = choose(*cache, q_type, q_on, group, granule, chunk);
         if (const cudaError_t e = grid_of(f, resident)) return status_of(e);
-        most = std::max(most, divide(*cache, batch, width, window, chunk, (group + chunk - 1) / chunk, resident).bytes);
+        most = std::max(most, divide(*cache, f, batch, width, window, chunk, (group + chunk - 1) / chunk, resident).bytes);
     }
     *bytes = most;
     return PP_OK;
@@ -1240,7 +1269,7 @@ extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const v
     const Form f = choose(c, q_type, row_alignment(q, 1, 0, batch, q_row, heads, q_head, tb), group, granule, chunk);
     if (const cudaError_t e = grid_of(f, resident)) return status_of(e);
     const int n_chunks = (group + chunk - 1) / chunk;
-    const Division by = divide(c, batch, width, window, chunk, n_chunks, resident);
+    const Division by = divide(c, f, batch, width, window, chunk, n_chunks, resident);
     if (by.bytes && (!workspace || workspace_bytes < by.bytes)) return PP_ERR_INVALID_ARG;
     const int es = type_bytes(c.dtype);
     const int64_t far = std::max({c.k_page, c.k_token, c.v_page, c.v_token}) * es;
@@ -1250,12 +1279,13 @@ extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const v
                static_cast<float*>(workspace), q_row, q_head, c.k_page * es, c.k_token * es, c.k_head * es, c.v_page * es, c.v_token * es,
                c.v_head * es, ld_table, Divisor((uint32_t)c.page_size), c.pages, c.page_size, batch, width * c.page_size, window, heads, c.kv_heads, group,
                chunk, n_chunks, c.head_dim, granule, q_type, c.dtype, f.inbox,
-               (int)std::min<int64_t>((int64_t)batch * c.kv_heads * n_chunks, by.grid), (int64_t)batch * c.kv_heads * n_chunks <= by.grid, by.cluster, kUnit % c.page_size, whole,
+               by.notes, by.part_rows, (int64_t)batch * (by.across ? c.kv_heads / kWarps : c.kv_heads) * n_chunks <= by.grid, by.cluster,
+               by.across ? kTile : kUnit, (by.across ? kTile : kUnit) % c.page_size, by.across, whole,
                c.head_dim % 4 == 0 && aligned_to(out, std::min(16, 4 * tb)), scale * kLog2e};
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = launch_pdl(f.kernel, dim3((unsigned)by.grid), dim3(kThreads), (size_t)f.smem, s, std::max(1, by.cluster), a);
     if (e == cudaSuccess && !by.cluster) {
-        const int shares = std::max(1, std::min({chunk, group, 2 * sm_count() / a.notes}));     // few notes: a CTA for each row, if there are so many
+        const int shares = std::max(1, std::min({std::min(chunk, group) * (by.across ? kWarps : 1), 2 * sm_count() / a.notes}));     // few notes: a CTA for each row, if there are so many
         e = launch_pdl(join_kernel, dim3((unsigned)a.notes, (unsigned)shares), dim3(kJoinThreads), 0, s, 1, a, f.lift);
     }
     return status_of(e);

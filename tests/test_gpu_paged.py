@@ -442,6 +442,21 @@ def test_attention_over_few_and_many(dtype, kind, lengths):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("heads,kv_heads,dim,page,heads_first", [(8, 4, 128, 16, False), (32, 8, 64, 32, True), (12, 12, 96, 16, False), (80, 4, 64, 8, False), (16, 16, 72, 48, False),
+                                                                 (36, 4, 256, 16, False), (12, 6, 64, 16, False)])
+def test_attention_long_and_short_at_once(dtype, kind, heads, kv_heads, dim, page, heads_first):
+    """Lengths that no even division fits: all heads in a row, cut into equal parts, four heads at a time where their number allows it."""
+    case = _attention_case(dim, dtype, kind, heads, kv_heads, dim, page, [9000, 1, 0, 5000, 64, 17000, 333], heads_first, width=17000 // page + 400)
+    _check_attention(*case)
+    _check_attention(*case, window=3001)
+    c, q, table, lengths = case
+    got, lse = pb.pp_paged_attention(c, q, table, lengths, lse=True)
+    again, lse2 = pb.pp_paged_attention(c, q, table, lengths, lse=True)
+    assert torch.equal(got, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", KINDS)
 def test_attention_with_large_scores(dtype, kind):
     # one key far above the others, and a scale that makes most p vanish
     c, q, table, lengths = _attention_case(4, dtype, kind, 4, 2, 64, 16, [300, 2000], spread=3.0)
