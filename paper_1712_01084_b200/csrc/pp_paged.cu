@@ -153,7 +153,7 @@ template <int kPlanRows> __global__ void __launch_bounds__(kPlanThreads) plan_ke
 }
 
 // ------------------------------------------------------------------------------------------------------ append
-constexpr int kAppendThreads = 256, kAhead = 2, kMaxTokens = 4, kMaxRows = 256;
+constexpr int kAppendThreads = 256, kMaxTokens = 4, kMaxRows = 256;
 
 struct AppendArgs {
     const void *q, *k, *v;
@@ -251,10 +251,11 @@ template <typename T, int W> __device__ __forceinline__ void store_run(T* to, co
 
 // VEC: a lane has two runs of W elements of each head, the two halves of W pairs (or 2 W neighbours), so that a pair never leaves its
 // lane and both its elements take the same sine; a.lanes lanes make a head.  A CTA has a.per_cta tokens and a.per_part of their heads:
-// where these lie, and the turns, are worked out once and stand in shared memory, since a row itself is only some 50 instructions
-// (addresses made row by row: 167 us for 16384 tokens of 64 + 2 x 8 heads).  Q8: the cache holds 8 bits.
+// where these lie, and the turns, are worked out once and stand in shared memory, since a row itself is only some 50 instructions.
+// The next row is on its way while one is worked on; four CTAs to an SM are more than a second row ahead is worth (16384 tokens of
+// 64 + 2 x 8 heads of 128: 107 us, 6.3 TB/s; three CTAs and two rows ahead 118; addresses made row by row 167).  Q8: the cache holds 8 bits.
 template <typename T, bool Q8, int W>
-__global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const __grid_constant__ AppendArgs a) {
     struct From { const char* src; char* dst; };             // of a head, to which a token's distance is added, in bytes
     struct By { int64_t src, dst; };
     __shared__ From head_at[kMaxRows];
@@ -278,17 +279,43 @@ __global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const __grid_
         head_at[i].src = static_cast<const char*>(is_q ? a.q : is_k ? a.k : a.v) + head * (is_q ? a.q_head : is_k ? a.k_head : a.v_head) * kEl;
         head_at[i].dst = static_cast<char*>(is_q ? a.q_out : is_k ? a.ck : a.cv) + head * (is_q ? a.o_head * kEl : (is_k ? a.ck_head : a.cv_head) * kCached);
     }
+    if (tid < tokens) {
+        const int64_t token = token0 + tid;
+        token_at[tid][0].src = token * a.q_token * kEl;
+        token_at[tid][1].src = token * a.k_token * kEl;
+        token_at[tid][2].src = token * a.v_token * kEl;
+    }
     pdl_release();
+    __syncthreads();
     pdl_wait();
+
+    struct Item { int t, row; };                             // rows of a token, then of the next, `groups` apart
+    const auto settle = [&](Item& i) {
+        while (i.row >= rows && i.t < tokens) i.row -= rows, ++i.t;
+    };
+    Run<T, W> raw[2] = {};                                   // the next row's runs, zeros where nothing is read
+    Item asked{0, tid / lanes};
+    settle(asked);
+    const auto fetch = [&] {
+        if (asked.t < tokens) {
+            const char* p = head_at[asked.row].src + token_at[asked.t][asked.row < q_rows ? 0 : asked.row < k_rows ? 1 : 2].src;
+            if (has0) raw[0] = *reinterpret_cast<const Run<T, W>*>(p + run0 * kEl);
+            if (has1) raw[1] = *reinterpret_cast<const Run<T, W>*>(p + run1 * kEl);
+        }
+        asked.row += groups;
+        settle(asked);
+    };
+    fetch();
+    // under the first rows' way: where the tokens go, and the turns
     if (tid < tokens) {
         const int64_t token = token0 + tid, slot = a.slots[token];
         const bool stored = slot >= 0 && slot < a.n_slots;
         int64_t page = 0, place = 0;
         if (stored) split_slot(slot, a.page_size, page, place);
         slots[tid] = stored ? slot : -1;
-        token_at[tid][0] = {token * a.q_token * kEl, token * a.o_token * kEl};
-        token_at[tid][1] = {token * a.k_token * kEl, (page * a.ck_page + place * a.ck_token) * kCached};
-        token_at[tid][2] = {token * a.v_token * kEl, (page * a.cv_page + place * a.cv_token) * kCached};
+        token_at[tid][0].dst = token * a.o_token * kEl;
+        token_at[tid][1].dst = (page * a.ck_page + place * a.ck_token) * kCached;
+        token_at[tid][2].dst = (page * a.cv_page + place * a.cv_token) * kCached;
     }
     for (int i = tid; i < tokens * a.pairs; i += kAppendThreads) {
         const int t = i / a.pairs, pair = i - t * a.pairs;
@@ -297,25 +324,6 @@ __global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const __grid_
         sines[t][pair] = by.y;
     }
     __syncthreads();
-
-    struct Item { int t, row; };                             // rows of a token, then of the next, `groups` apart
-    const auto settle = [&](Item& i) {
-        while (i.row >= rows && i.t < tokens) i.row -= rows, ++i.t;
-    };
-    Run<T, W> raw[kAhead][2] = {};                           // zeros where nothing is read
-    Item asked{0, tid / lanes};
-    settle(asked);
-    const auto fetch = [&](Run<T, W> (&to)[2]) {
-        if (asked.t < tokens) {
-            const char* p = head_at[asked.row].src + token_at[asked.t][asked.row < q_rows ? 0 : asked.row < k_rows ? 1 : 2].src;
-            if (has0) to[0] = *reinterpret_cast<const Run<T, W>*>(p + run0 * kEl);
-            if (has1) to[1] = *reinterpret_cast<const Run<T, W>*>(p + run1 * kEl);
-        }
-        asked.row += groups;
-        settle(asked);
-    };
-#pragma unroll
-    for (int n = 0; n < kAhead; ++n) fetch(raw[n]);
     Item at{0, tid / lanes};
     settle(at);
     const int loops = (tokens * rows + groups - 1) / groups; // the same for every thread: shuffles need them all
@@ -324,11 +332,9 @@ __global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const __grid_
         const bool live = at.t < tokens;
         const int t = live ? at.t : 0, row = live ? at.row : 0, kind = row < q_rows ? 0 : row < k_rows ? 1 : 2;
         float x[W], y[W];
-        unpack(x, raw[0][0]);
-        unpack(y, raw[0][1]);
-#pragma unroll
-        for (int m = 0; m + 1 < kAhead; ++m) raw[m][0] = raw[m + 1][0], raw[m][1] = raw[m + 1][1];
-        fetch(raw[kAhead - 1]);
+        unpack(x, raw[0]);
+        unpack(y, raw[1]);
+        fetch();
         if (turned && kind < 2) {
             float cosine[W], sine[W];
 #pragma unroll
