@@ -563,7 +563,7 @@ typedef struct pp_paged_cache {
  * positions     [rows]: position of each new token in its sequence; 0 for rows behind the last token
  * lengths_out   [requests]: min(lengths + added, capacity); may be lengths itself, as taken_out may be taken.  No other array
  *               that is written may overlap another
- * requests 0..8192, width >= 1, width * page_size < 2^31, rows >= 0.
+ * requests 0..8192, width >= 1, (width + 1) * page_size < 2^31, requests * width < 2^31, rows >= 0.
  * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (requests, capacity), PP_ERR_CUDA. */
 pp_status_t pp_paged_plan(const int32_t* lengths, const int32_t* added, int32_t* table, int64_t ld_table, int width,
                           const int32_t* free_pages, int n_free, const int32_t* taken, int requests, int page_size, int rows,
@@ -600,8 +600,10 @@ pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q, int64_t q
  * workspace     pp_paged_attention_workspace bytes (0: NULL), 16-byte aligned, for this call alone while it runs; need not be
  *               initialised.  Long sequences are divided over the GPU, and their parts joined through it
  * Products are those of the 16-bit tensor-core instructions (exact products; float for PP_F32 caches), scores, softmax and sums
- * are floats; p enters the second product as two 16-bit numbers (16 bits in all for PP_BF16, 22 otherwise).  Results do not
- * depend on scheduling.  batch >= 0; heads a multiple of kv_heads; width * page_size < 2^31; window >= 0; scale finite.
+ * are floats; p enters the second product as two 16-bit numbers (16 bits in all for PP_BF16, 22 otherwise), with 8-bit caches and a
+ * PP_BF16 output as one f16 number (11 bits); float q with 8-bit caches as two f16 numbers (22 bits).  Results do not
+ * depend on scheduling.  batch >= 0; heads a multiple of kv_heads; width * page_size < 2^31 - 2^13; batch * heads times the table's
+ * 64ths of positions < 2^31; window >= 0; scale finite.
  * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (types, head_dim, capacity), PP_ERR_CUDA. */
 pp_status_t pp_paged_attention_workspace(const pp_paged_cache_t* cache, pp_dtype_t q_type, int batch, int heads, int width,
                                          int window, int64_t* bytes);

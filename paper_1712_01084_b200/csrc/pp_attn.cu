@@ -27,6 +27,8 @@ namespace pp {
 namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32, kTile = 16, kUnit = kWarps * kTile;
+constexpr int kAheadMost = 8192;
+static_assert(kAheadMost > 65 * kUnit);
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct AttnArgs {
@@ -1051,7 +1053,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     if (note.last < 0) return;
     const int64_t floats = part_floats(a.part_rows, a.dim), second = note.rows < 0 ? floats : 0;
     const float* parts = a.ws + notes_floats(a.notes);
-    const auto part = [&](int c) { return parts + 2 * c * floats + (c == note.first ? second : 0); };
+    const auto part = [&](int c) { return parts + 2 * c * floats + (c == note.first ? second : 0); };     // read past L1: written by other SMs
     const int rows4 = up4(a.part_rows), dim4 = up4(a.dim), n_heads = abs(note.rows), all_rows = n_heads * (a.across ? kWarps : 1);
     const int rows = (all_rows - (int)blockIdx.y + step - 1) / step;         // of this CTA
     if (rows < 1) return;
@@ -1064,18 +1066,18 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         float top = kLowest, l = 0.0f;
         float4 acc[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
         if (live) {
-            for (int c = note.first + lane; c <= note.last; c += 32) top = fmaxf(top, part(c)[h]);
+            for (int c = note.first + lane; c <= note.last; c += 32) top = fmaxf(top, __ldcg(part(c) + h));
 #pragma unroll
             for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
 #pragma unroll 4
             for (int c = note.first + sub; c <= note.last; c += per) {
                 const float* p = part(c);
-                const float w = weight_of(p[h], top);
-                l = fmaf(p[rows4 + h], w, l);
+                const float w = weight_of(__ldcg(p + h), top);
+                l = fmaf(__ldcg(p + rows4 + h), w, l);
                 const float4* x = reinterpret_cast<const float4*>(p + 2 * rows4 + h * dim4) + lane;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    if (4 * (lane + 32 * i) < a.dim) acc[i] = fma4(x[32 * i], w, acc[i]);
+                    if (4 * (lane + 32 * i) < a.dim) acc[i] = fma4(__ldcg(x + 32 * i), w, acc[i]);
             }
         }
 #pragma unroll
@@ -1188,7 +1190,8 @@ pp_status_t check_call(const pp_paged_cache_t* cache, pp_dtype_t q_type, int bat
     if (!is_float(q_type) || (q_type != cache->dtype && !is_8bit(cache->dtype))) return PP_ERR_UNSUPPORTED;
     if (batch < 0 || heads < 1 || heads % cache->kv_heads || width < 1 || window < 0) return PP_ERR_INVALID_ARG;
     const int64_t capacity = (int64_t)width * cache->page_size;
-    if (capacity > INT32_MAX - 2 * kUnit || heads > (1 << 20) || (int64_t)batch * heads > INT32_MAX) return PP_ERR_UNSUPPORTED;
+    // positions are 32 bits, and entries are looked up 63 units ahead of a tile (Reader)
+    if (capacity > INT32_MAX - kAheadMost || heads > (1 << 20) || (int64_t)batch * heads > INT32_MAX) return PP_ERR_UNSUPPORTED;
     if ((int64_t)batch * heads > INT32_MAX / (capacity / kUnit + 2)) return PP_ERR_UNSUPPORTED;     // units are counted in 32 bits
     return PP_OK;
 }

@@ -576,12 +576,15 @@ extern "C" pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q
     if (q) {
         if (!rows_apart(1, 0, tokens, o_token, heads, o_head, dim)) return PP_ERR_INVALID_ARG;
         const bool in_place = q == q_out && q_token == o_token && q_head == o_head;
-        // in place, q may be a part of rows that hold k and v too, as a projection's rows do: then no row of it may reach into theirs
-        if (!in_place && spans_meet(q, span(q_token, q_head, heads), q_out, span(o_token, o_head, heads))) return PP_ERR_INVALID_ARG;
-        const int64_t row = (((int64_t)heads - 1) * o_head + dim) * tb, other_k = (((int64_t)c.kv_heads - 1) * k_head + dim) * tb,
-                      other_v = (((int64_t)c.kv_heads - 1) * v_head + dim) * tb;
-        if (share_bytes(q_out, row, o_token * tb, tokens, k, other_k, k_token * tb, tokens) ||
-            share_bytes(q_out, row, o_token * tb, tokens, v, other_v, v_token * tb, tokens)) return PP_ERR_INVALID_ARG;
+        // A token's rows of each array, q_token (k_token ...) apart: arrays with one distance may lie in one another's gaps, as the parts of a
+        // projection's rows do; others may not meet at all.
+        const int64_t out_row = (((int64_t)heads - 1) * o_head + dim) * tb;
+        const auto meets = [&](const void* p, int64_t token, int64_t head, int n) {
+            const int64_t row = (((int64_t)n - 1) * head + dim) * tb;
+            if (token == o_token) return share_bytes(q_out, out_row, o_token * tb, tokens, p, row, token * tb, tokens);
+            return spans_meet(p, span(token, head, n), q_out, span(o_token, o_head, heads));
+        };
+        if ((!in_place && meets(q, q_token, q_head, heads)) || meets(k, k_token, k_head, c.kv_heads) || meets(v, v_token, v_head, c.kv_heads)) return PP_ERR_INVALID_ARG;
     }
     AppendArgs a{q, k, v, q_out, c.k, c.v, c.k_scales, c.v_scales, slots, positions, inv_freq,
                  q_token, q_head, o_token, o_head, k_token, k_head, v_token, v_head,

@@ -308,6 +308,11 @@ def test_append_of_nothing_and_refusals():
     h = x.half()
     with pytest.raises(pb.PPError, match="UNSUPPORTED"):                                     # no rounding to another 16-bit type
         call(k=h, v=h, q=h)
+    row = torch.randn(3, 8, 16, device="cuda").bfloat16()                                    # out beside q, k and v in their rows
+    got = pb.pp_kv_append(c, row[:, 2:4], row[:, 4:6], slots, q=row[:, :2], positions=positions, inv_freq=f, out=row[:, 6:])
+    assert torch.equal(got, pb.pp_kv_append(c, row[:, 2:4], row[:, 4:6], slots, q=row[:, :2], positions=positions, inv_freq=f))
+    with pytest.raises(pb.PPError, match="INVALID_ARG"):                                     # out across k in its rows
+        pb.pp_kv_append(c, row[:, 2:4], row[:, 4:6], slots, q=row[:, :2], positions=positions, inv_freq=f, out=row[:, 3:5])
     wide = torch.zeros(4, 2, 16, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(pb.PPError, match="INVALID_ARG"):                                     # out across q
         call(q=wide[:3], out=wide[1:])
@@ -388,9 +393,12 @@ def _bound(out, mass, slack, positions, dtype, kind):
     """A score is a sum of head_dim exact products held in 32 bits, whose additions err by 2^-23 of the largest partial sum at most, and a
     few roundings of the factors; the exponential's argument rounds by 2^-24 of itself; p and the sum of p then err by `slack` and
     2^-21 (exponential, factors of a running maximum), p enters the second product rounded to 16 bits (bf16 caches: 2^-17; else
-    less), and a sum over n positions in 32 bits passes at most n / 8 + 600 additions (two instructions a tile of 16; four warps;
+    less, but for a bf16 output over 8 bits, where it is one f16 number: half a step is 2^-11 of p, and only the numerator has it,
+    since the sum of p is taken before: sum |dp v| <= 2^-11 sum p |v|), and a sum over n positions in 32 bits passes at most n / 8 + 600 additions (two instructions a tile of 16; four warps;
     some 300 parts, and their joining).  All errors of p count twice: above and below the fraction."""
     grow = 2 * (slack + 2.0 ** -21 + 2.0 ** -17) + (positions / 8 + 600) * 2.0 ** -23
+    if dtype == torch.bfloat16 and kind in (torch.int8, torch.float8_e4m3fn):
+        grow = grow + 2.0 ** -11
     return ROUND[dtype] * out.abs() * (1 + 1e-6) + FLOOR[dtype] + grow[..., None] * mass
 
 
@@ -402,7 +410,8 @@ def _check_attention(c, q, table, lengths, window=0, scale=None, got=None):
     o, e = got
     assert o.shape == q.shape and o.dtype == q.dtype and e.dtype == torch.float32
     most = float(lengths.max()) if lengths.numel() else 0.0
-    err, bound = (o.double() - want).abs(), _bound(want, mass, slack, most, q.dtype, None)
+    most = min(most, window) if window else most
+    err, bound = (o.double() - want).abs(), _bound(want, mass, slack, most, q.dtype, c.k.dtype)
     assert bool((err <= bound).all()), float((err / bound).max())
     none = torch.isinf(lse)
     assert torch.equal(torch.isinf(e) & (e < 0), none) and bool((o[none] == 0).all())
@@ -478,6 +487,28 @@ def test_attention_skips_what_is_no_page(dtype, kind):
 def test_attention_lengths_outside_the_table():
     c, q, table, lengths = _attention_case(7, "bf16", "bf16", 4, 1, 64, 16, [64, 30, 64])
     _check_attention(c, q, table, _ints([1000, -3, 2 ** 31 - 1]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kv_heads", [1, 4])
+@pytest.mark.parametrize("page", [16, 1])
+def test_attention_at_the_end_of_the_longest_table(kv_heads, page):
+    """Positions just below 2^31 - 2^13: looking ahead of the last one stays within the numbers."""
+    width = (2 ** 31 - 1 - 8192) // page
+    if page == 1:
+        width = 2 ** 20                                                      # a table of 8 GB is not worth it: the same tail, far from the limit
+    c, q, _, _ = _attention_case(15, "bf16", "e4m3", 4 * kv_heads, kv_heads, 64, page, [60])
+    c.k_scales.fill_(0.01)
+    c.v_scales.fill_(0.02)
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    last = -(-60 // page)
+    table[0, -last:] = torch.arange(last, dtype=torch.int32, device="cuda")
+    n = width * page
+    for length, window in ((n, 50), (n - 3, 41), (2 ** 31 - 1, 33)):
+        _check_attention(c, q, table, _ints([length]), window=window)
+    if page == 16:
+        with pytest.raises(pb.PPError, match="UNSUPPORTED"):
+            pb.pp_paged_attention(c, q, torch.full((1, 2 ** 27), -1, dtype=torch.int32, device="cuda"), _ints([5]))
 
 
 @pytest.mark.gpu
