@@ -1,25 +1,36 @@
-// Attention of one new token of each request over a paged key-value cache.
+// Attention of one new token of each request over a paged key-value cache: the kernels (pp_attn.cu has the choice among them).
 //
 //   out = sum_j p_j v_j,  p = softmax_j(scale q . k_j),  j over a request's last positions
 //
 // One pass over keys and values with a running maximum m and sum l: bound by the bytes of the cache, which are read once for all
-// query heads of a key-value head (up to 8 or 16 of them, the chunk).
+// query heads of a key-value head (up to 8 or 16 of them, the chunk).  m only moves when a score passes it by 2^8: then sums and l
+// are scaled; else a tile costs one vote.
 //
-// Division of work.  64 positions of one key-value head (and chunk) are a unit.  The units of all requests in a row, request after
-// request and head after head, are cut into equal parts, one for each CTA that the GPU holds at once, so that lengths of any mix
-// keep all SMs reading to the end.  A CTA finds its part from the lengths alone.  Where a cut falls inside a head's units the CTAs
-// write partial results (m, l, the weighted sum) to the workspace, and a second kernel joins them in the order of the sequence.
+// Division of work.  64 positions of one key-value head (and chunk) are a unit, 16 to a warp; or 16 positions of four heads, one
+// to a warp, where the heads' rows or scales share lines of memory.  Three ways (divide in pp_attn.cu):
+//   * equal parts: the units of all requests in a row, request after request and head after head, are cut into equal parts, one
+//     for each CTA that the GPU holds at once, so that lengths of any mix keep all SMs reading to the end.  A CTA finds its part
+//     from the lengths alone.  Where a cut falls inside a head's units the CTAs write partial results (m, l, the weighted sum)
+//     to the workspace, and a second kernel joins them in the order of the sequence;
+//   * a cluster of two to eight CTAs to a head: each sends its part of a row to the CTA that joins it, over shared memory;
+//   * a CTA to a head, or to four.
 //
-// A warp takes tiles of 16 positions of its own, through a ring in shared memory that 16-byte asynchronous copies fill: rows are
-// looked up in the table one by one, so pages may have any size and end anywhere.  Rows are an odd number of 16 bytes apart, so
-// that eight of them meet no bank twice.
+// A warp takes tiles of 16 positions of its own, through a ring in shared memory that 16-byte asynchronous copies fill.  Pages may
+// have any size and end anywhere; where they are whole tiles long a tile costs one look-up, its entries fetched 32 tiles at a
+// time, else every row has its own.  Rows are an odd number of 16 bytes apart, so that eight of them meet no bank twice.
 //
 // Matrix form (MmaCore), S^T[16 positions x 8 heads] = K Q^T and O^T[dim x 8 heads] += V^T P^T, by m16n8k16: the cache is the operand
 // with 16 rows, heads are the eight columns, so no instruction works on padding where a key-value head has eight query heads.
-// P^T changes from the layout of a result to that of an operand by 8x8 transposes in registers; it enters as two 16-bit numbers, the
-// rounded value and what the rounding left (one alone would add an error as large as the output's own rounding).  8-bit codes are
-// exact in f16; the scale of a key multiplies its score, that of a value its p.
+// Not tcgen05: with 8 to 16 heads to a row of the cache the matrix pipe is busy 15 to 18 % of the time, and codes have to pass
+// through registers to be widened.  P^T changes from the layout of a result to that of an operand by 8x8 transposes in registers;
+// it enters as two 16-bit numbers, the rounded value and what the rounding left (one alone would add an error as large as the
+// output's own rounding), or as one where that is an eighth of it.  8-bit codes are exact in f16; the scale of a key multiplies
+// its score, that of a value its p.
 // Scalar form (ScalarCore): floats, a lane per position and half row for the scores, a lane per dimension for the sums.
+//
+// In a graph, heads of 128, 32 query heads over 8: 64 requests of 4096 to 8192 bf16 252 us, 6.4 TB/s of what they hold; one of 131072
+// 95 us, 5.7 TB/s; 33 of 6000 to 12000 in 8 bits with 64 heads 120 us, 5.3 TB/s; one of 513 6.3 us; 6 of 500 to 1000 floats, 16 heads
+// of 64, 12.3 us.
 #pragma once
 #include "pp_internal.h"
 #include "pp_paged.cuh"

@@ -4,12 +4,13 @@
 // Plan.  A request that holds h tokens and gets a more needs the pages ceil(h / p) .. ceil((h + a) / p); where they start in the
 // free list is an exclusive sum over the requests before it, as is the first row of its tokens.  Every CTA makes both sums
 // for all requests (a few thousand additions in shared memory, cheaper than a second launch that would wait for a first),
-// then takes its share of the rows, four to a thread: a binary search for the row's request, and its page from the free
-// list where it is a new one, else from the table, whose old entries nobody writes.
+// then takes its share of the pages and of the rows: a binary search for the request, and for a row its page from the free list
+// where it is a new one, else from the table, whose old entries nobody writes.  All latency: 2.1 us for one request, 3.2 for 256
+// (4.9 with a warp to a request's pages and four rows to a thread), 5.9 for 48 prompts with 200,000 tokens.
 //
-// Append.  All bandwidth for many tokens, all latency for few.  A lane has the same dimensions of every head, both elements of each
-// pair among them, so its cosines and sines stay in registers and serve two runs of eight (or four) elements of every row.  The angle is a product in 64 bits,
-// brought into a turn there: position 10^6 leaves a 32-bit angle 2^-5 of a radian.
+// Append.  All bandwidth for many tokens, all latency for few.  Both elements of a pair are in one lane and take the same sine.  The
+// angle is a product in 64 bits, brought into a turn there: position 10^6 leaves a 32-bit angle 2^-5 of a radian.  16384 tokens
+// of 64 + 2 x 8 heads of 128, bf16: 107 us, 6.3 TB/s; one token 2.1 us.
 #include "pp_internal.h"
 #include "pp_paged.cuh"
 
