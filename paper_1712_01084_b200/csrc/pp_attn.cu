@@ -5,14 +5,14 @@ namespace pp {
 namespace attn {
 namespace {
 
-// Joins the parts of the head (chunk) of note blockIdx.x, if there is one: CTA blockIdx.y of gridDim.y takes a share of its rows, as many
-// warps to a row as there are, each with a share of the parts.  Its shared memory fits beside the first kernel's, so that it is
-// there when that ends.
+// Joins the parts of the head (chunk) of note blockIdx.x, if there is one.  CTA blockIdx.y takes a share of its rows and, of their
+// dimensions, one of SLICES.  As many warps to a row as there are, and as many parts at once to a warp as there are slices: few
+// heads of many parts are joined by many CTAs.  One pass, with a running maximum for each warp and part at once.
 constexpr int kJoinWarps = 8, kJoinThreads = kJoinWarps * 32;
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttnArgs a, float lift) {
+template <int SLICES> __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttnArgs a, float lift) {
     __shared__ float4 sums[kJoinWarps][kMaxHeadDim / 4];
-    __shared__ float ls[kJoinWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, step = gridDim.y;
+    __shared__ float ls[kJoinWarps], tops[kJoinWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, step = gridDim.y / SLICES, share = blockIdx.y / SLICES, slice = blockIdx.y % SLICES;
     pdl_release();
     pdl_wait();
     const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.ws) + blockIdx.x);
@@ -22,44 +22,66 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     const float* parts = a.ws + notes_floats(a.notes);
     const auto part = [&](int c) { return parts + 2 * c * floats + (c == note.first ? second : 0); };     // read past L1: written by other SMs
     const int rows4 = up4(a.part_rows), dim4 = up4(a.dim), n_heads = abs(note.rows), all_rows = n_heads * (a.across ? kWarps : 1);
-    const int rows = (all_rows - (int)blockIdx.y + step - 1) / step;         // of this CTA
+    const int rows = (all_rows - share + step - 1) / step;   // of this CTA
     if (rows < 1) return;
+    // a part takes 32 / SLICES lanes, up to two fours of dimensions each
+    constexpr int lanes = 32 / SLICES;
+    const int column = lane % lanes, group = lane / lanes, fours = (dim4 / 4 + SLICES - 1) / SLICES, first4 = slice * fours;
     const int at_once = min(rows, kJoinWarps), per = kJoinWarps / at_once, sub = warp % per;
     for (int done = 0; done < rows; done += at_once) {
-        const int n = done + warp / per, row = blockIdx.y + n * step, head = row / n_heads;   // head: of the four (across)
+        const int n = done + warp / per, row = share + n * step, head = row / n_heads;        // head: of the four (across)
         const bool live = warp / per < at_once && n < rows;
         const int h = head * a.chunk + row - head * n_heads;
         const int64_t to = (int64_t)note.row + head * a.group + row - head * n_heads;
         float top = kLowest, l = 0.0f;
         float4 acc[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
         if (live) {
-            for (int c = note.first + lane; c <= note.last; c += 32) top = fmaxf(top, __ldcg(part(c) + h));
-#pragma unroll
-            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
 #pragma unroll 4
-            for (int c = note.first + sub; c <= note.last; c += per) {
+            for (int c = note.first + sub * SLICES + group; c <= note.last; c += per * SLICES) {
                 const float* p = part(c);
-                const float w = weight_of(__ldcg(p + h), top);
-                l = fmaf(__ldcg(p + rows4 + h), w, l);
-                const float4* x = reinterpret_cast<const float4*>(p + 2 * rows4 + h * dim4) + lane;
+                const float4* x = reinterpret_cast<const float4*>(p + 2 * rows4 + h * dim4) + first4 + column;
+                const float m = __ldcg(p + h), sum = __ldcg(p + rows4 + h), now = fmaxf(top, m), before = weight_of(top, now), w = weight_of(m, now);
+                l = fmaf(l, before, sum * w);
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    if (4 * (lane + 32 * i) < a.dim) acc[i] = fma4(__ldcg(x + 32 * i), w, acc[i]);
+                    if (column + lanes * i < fours && 4 * (first4 + column + lanes * i) < a.dim) {
+                        const float4 v = __ldcg(x + lanes * i);
+                        acc[i] = fma4(v, w, make_float4(acc[i].x * before, acc[i].y * before, acc[i].z * before, acc[i].w * before));
+                    }
+                top = now;
+            }
+#pragma unroll
+            for (int o = lanes; o < 32; o <<= 1) {
+                const float m = __shfl_xor_sync(0xffffffffu, top, o), now = fmaxf(top, m), mine = weight_of(top, now), w = weight_of(m, now);
+                l = fmaf(l, mine, __shfl_xor_sync(0xffffffffu, l, o) * w);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float4 v = make_float4(__shfl_xor_sync(0xffffffffu, acc[i].x, o), __shfl_xor_sync(0xffffffffu, acc[i].y, o),
+                                                 __shfl_xor_sync(0xffffffffu, acc[i].z, o), __shfl_xor_sync(0xffffffffu, acc[i].w, o));
+                    acc[i] = fma4(v, w, make_float4(acc[i].x * mine, acc[i].y * mine, acc[i].z * mine, acc[i].w * mine));
+                }
+                top = now;
             }
         }
+        if (group == 0) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) sums[warp][lane + 32 * i] = acc[i];
-        if (lane == 0) ls[warp] = l;
+            for (int i = 0; i < 2; ++i) sums[warp][column + lanes * i] = acc[i];
+        }
+        if (lane == 0) {
+            ls[warp] = l;
+            tops[warp] = top;
+        }
         __syncthreads();
         if (live && sub == 0) {
+            for (int w = 1; w < per; ++w) top = fmaxf(top, tops[warp + w]);
             l = 0.0f;
-            for (int w = 0; w < per; ++w) l += ls[warp + w];
-            for (int d = lane; 4 * d < a.dim; d += 32) {
-                float4 sum = sums[warp][d];
-                for (int w = 1; w < per; ++w) sum = add4(sum, sums[warp + w][d]);
-                store_out(a, to, 4 * d, over(sum, l));
+            for (int w = 0; w < per; ++w) l = fmaf(ls[warp + w], weight_of(tops[warp + w], top), l);
+            for (int f = lane; f < fours && 4 * (first4 + f) < a.dim; f += 32) {
+                float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                for (int w = 0; w < per; ++w) sum = fma4(sums[warp + w][f], weight_of(tops[warp + w], top), sum);
+                store_out(a, to, 4 * (first4 + f), over(sum, l));
             }
-            if (a.lse && lane == 0) a.lse[to] = lse_of(top, l, lift);
+            if (a.lse && lane == 0 && slice == 0) a.lse[to] = lse_of(top, l, lift);
         }
         __syncthreads();
     }
@@ -101,7 +123,8 @@ cudaError_t grid_of(const Form& f, int& grid) {
         if (cudaError_t e = cudaFuncSetAttribute(f.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, f.smem)) return e;
         // An SM divides its memory between L1 and shared memory as its kernels ask, and changes that only when it is empty: with the second
         // kernel's smaller wish in force the last of the CTAs would start when others end.
-        for (const void* k : {reinterpret_cast<const void*>(f.kernel), reinterpret_cast<const void*>(join_kernel)})
+        for (const void* k : {reinterpret_cast<const void*>(f.kernel), reinterpret_cast<const void*>(join_kernel<1>), reinterpret_cast<const void*>(join_kernel<2>),
+                              reinterpret_cast<const void*>(join_kernel<4>)})
             if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared)) return e;
         if (cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, f.kernel, kThreads, (size_t)f.smem)) return e;
         if (device >= PerDeviceOnce::kMaxDevices) {
@@ -158,7 +181,8 @@ Division divide(const pp_paged_cache_t& c, const Form& f, int batch, int width, 
     // and a row is no multiple of 256 bytes, heads read one after another fetch the lines between them twice (32 x 6000, eight
     // heads of 72 / 96: 88 / 98 us one by one, 72 / 84 us by four; 256-byte rows: 103 against 105; 16 query heads to each: 61 against 68).
     const bool side_by_side = c.k_head < c.k_token && c.head_dim * type_bytes(c.dtype) % 256 != 0;
-    const bool across = fours && chunk <= 8 && (is_8bit(c.dtype) || side_by_side);
+    // A row's parts then are four times as many, so heads have to be, too.
+    const bool across = fours && chunk <= 8 && 4 * heads >= resident && (is_8bit(c.dtype) || side_by_side);
     const int notes = (int)std::min<int64_t>(across ? heads / kWarps : heads, resident), rows = across ? kWarps * chunk : chunk;
     return {resident, 0, across, notes, rows, (notes_floats(notes) + (int64_t)resident * 2 * part_floats(rows, c.head_dim)) * 4};
 }
@@ -226,8 +250,11 @@ extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const v
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = launch_pdl(f.kernel, dim3((unsigned)by.grid), dim3(kThreads), (size_t)f.smem, s, std::max(1, by.cluster), a);
     if (e == cudaSuccess && !by.cluster) {
-        const int shares = std::max(1, std::min({std::min(chunk, group) * (by.across ? kWarps : 1), 2 * sm_count() / a.notes}));     // few notes: a CTA for each row, if there are so many
-        e = launch_pdl(join_kernel, dim3((unsigned)a.notes, (unsigned)shares), dim3(kJoinThreads), 0, s, 1, a, f.lift);
+        // few notes: a CTA for each row, then for each slice of its dimensions, if the GPU has so many
+        const int rows = std::min(chunk, group) * (by.across ? kWarps : 1), room = 2 * sm_count() / a.notes;
+        const int shares = std::max(1, std::min(rows, room)), slices = room >= 4 * rows ? 4 : room >= 2 * rows ? 2 : 1;
+        const auto join = slices == 4 ? join_kernel<4> : slices == 2 ? join_kernel<2> : join_kernel<1>;
+        e = launch_pdl(join, dim3((unsigned)a.notes, (unsigned)(shares * slices)), dim3(kJoinThreads), 0, s, 1, a, f.lift);
     }
     return status_of(e);
 }

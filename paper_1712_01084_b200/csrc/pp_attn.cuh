@@ -365,7 +365,7 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
     static constexpr bool kQ8 = KIND >= kE4m3, kIsBf16 = KIND == kBf16;
     static constexpr int kEs = kQ8 ? 1 : 2, kChunks = DT * kEs / 16, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
     // Resident CTAs that the registers are cut for: by those that sums and q take
-    static constexpr int kHeld = DT * NT * (4 + 2 * QP) / 16, kCtas = kQ8 ? (kHeld <= 36 ? 4 : kHeld <= 64 ? 3 : 2) : kHeld <= 36 ? 3 : 1;
+    static constexpr int kHeld = DT * NT * (4 + 2 * QP) / 16, kCtas = kQ8 ? (kHeld <= 48 ? 4 : kHeld <= 64 ? 3 : 2) : kHeld <= 36 ? 3 : 1;
     static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = DT <= 64 ? 3 : 2;
     static constexpr int kHeads = 8 * NT, kMergePitch = DT + 4;
     // 16-bit rows of 128: no more than two CTAs by their shared memory.  With three, or a third stage, the SMs' shares of the memory differ
@@ -864,29 +864,50 @@ template <class Core, Reading READING> __global__ void __launch_bounds__(kThread
     if (a.cluster) {
         r = c / a.cluster / per_request;
     } else {
-        const int each = (a.batch + kThreads - 1) / kThreads, r0 = min(tid * each, a.batch), r1 = min(r0 + each, a.batch);
-        int mine = 0;
-        for (r = r0; r < r1; ++r) mine += units_of(a, r) * per_request;
-        const int before = sum_before(mine, warp_sums, all);
+        int mine = 0, before;
+        int r0, r1;
+        if (a.batch <= 32) {                                 // a request to a lane, in every warp: no barrier
+            r0 = min(lane, a.batch), r1 = min(lane + 1, a.batch);
+            if (lane < a.batch) mine = units_of(a, lane) * per_request;
+            int up = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, up, o);
+                if (lane >= o) up += x;
+            }
+            all = __shfl_sync(0xffffffffu, up, 31);
+            before = up - mine;
+        } else {
+            const int each = (a.batch + kThreads - 1) / kThreads;
+            r0 = min(tid * each, a.batch), r1 = min(r0 + each, a.batch);
+            for (r = r0; r < r1; ++r) mine += units_of(a, r) * per_request;
+            before = sum_before(mine, warp_sums, all);
+        }
         ctas = min((int)gridDim.x, all);
         if (!a.by_head && tid == 0) reinterpret_cast<Note*>(a.ws)[c].last = -1;
         if (c >= ctas) return;
         const Cut cut(all, ctas);
         u = begin = cut.start(c);
         end = cut.start(c + 1);
-        if (u >= before && u < before + mine) {
-            base = before;
-            for (r = r0;; ++r) {
-                const int units = units_of(a, r) * per_request;
-                if (u < base + units) break;
-                base += units;
+        if (a.batch <= 32) {
+            const int at = __ffs(__ballot_sync(0xffffffffu, u >= before && u < before + mine)) - 1;
+            r = at;
+            base = __shfl_sync(0xffffffffu, before, at);
+        } else {
+            if (u >= before && u < before + mine) {
+                base = before;
+                for (r = r0;; ++r) {
+                    const int units = units_of(a, r) * per_request;
+                    if (u < base + units) break;
+                    base += units;
+                }
+                found = r;
+                found_base = base;
             }
-            found = r;
-            found_base = base;
+            __syncthreads();
+            r = found;
+            base = found_base;
         }
-        __syncthreads();
-        r = found;
-        base = found_base;
     }
 
     unsigned char* own = ring + warp * Core::kStages * Core::kStage;
@@ -985,6 +1006,7 @@ template <class Core, Reading READING> __global__ void __launch_bounds__(kThread
         const int rank = a.cluster > 1 ? c % a.cluster : 0, share = a.cluster > 1 ? (n_heads * kFours + a.cluster - 1) / a.cluster : 0;
         if (a.cluster > 1) cluster_wait();
         if (a.across) {                                      // a warp's rows are its own
+#pragma unroll 1
             for (int i = lane; i < n_heads * kFours; i += 32) {
                 const int h = i / kFours, d = 4 * (i - h * kFours);
                 if (d >= a.dim) continue;
@@ -993,6 +1015,7 @@ template <class Core, Reading READING> __global__ void __launch_bounds__(kThread
                 else *reinterpret_cast<float4*>(part + 2 * up4(a.part_rows) + (warp * a.chunk + h) * up4(a.dim) + d) = sum;
             }
         } else {
+#pragma unroll 1
             for (int i = tid; i < n_heads * kFours; i += kThreads) {
                 const int h = i / kFours, d = 4 * (i - h * kFours);
                 if (d >= a.dim) continue;
@@ -1025,6 +1048,7 @@ template <class Core, Reading READING> __global__ void __launch_bounds__(kThread
         }
         if (a.cluster) {
             if (a.cluster == 1) return;
+#pragma unroll 1
             for (int i = tid; i < a.cluster * n_heads; i += kThreads) {
                 const int to = i / n_heads, h = i - to * n_heads;
                 store_remote(at_rank(smem_at(&others[rank][0][h]), to), all_m[h]);
@@ -1032,12 +1056,15 @@ template <class Core, Reading READING> __global__ void __launch_bounds__(kThread
             }
             cluster_arrive();
             cluster_wait();
+#pragma unroll 1
             for (int n = tid; n < share; n += kThreads) {
                 const int i = n * a.cluster + rank, h = i / kFours, d = 4 * (i - h * kFours);
                 if (h >= n_heads || d >= a.dim) continue;
                 float top = kLowest, l = 0.0f;
+#pragma unroll 1
                 for (int k = 0; k < a.cluster; ++k) top = fmaxf(top, others[k][0][h]);
                 float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
                 for (int k = 0; k < a.cluster; ++k) {
                     const float w = weight_of(others[k][0][h], top);
                     l = fmaf(others[k][1][h], w, l);
