@@ -156,7 +156,7 @@ struct Division {
     int notes, part_rows;
     int64_t bytes;                                           // of workspace
 };
-// Costs in units of 64 positions to a CTA, some 0.6 us while latency rules, going by the table's width.  Equal parts of all units:
+// Costs in units of 64 positions to a CTA, some 0.6 us while latency rules (twice that in the scalar form), going by the table's width.  Equal parts of all units:
 // sums over lengths, the workspace and a second kernel, 4 us.  A CTA or a cluster of up to eight to each head (chunk): as many
 // rounds as the GPU needs for them, each a CTA's share and 2 us for its start and end; a cluster's exchange costs 2.3 us.
 constexpr int kEqualParts = 10, kRound = 3, kExchange = 4;
@@ -164,10 +164,11 @@ Division divide(const pp_paged_cache_t& c, const Form& f, int batch, int width, 
     const bool fours = c.kv_heads % kWarps == 0 && !f.shares_q;
     const int64_t capacity = (int64_t)width * c.page_size, longest = window > 0 ? std::min<int64_t>((int64_t)window + kTile - 1, capacity) : capacity;
     const int64_t units = std::max<int64_t>(1, (longest + kUnit - 1) / kUnit), heads = (int64_t)batch * c.kv_heads * n_chunks;
-    int64_t least = heads * units / resident + kEqualParts, best = 0;
+    const int64_t weight = f.shares_q ? 2 : 1;
+    int64_t least = weight * (heads * units / resident + 1) + kEqualParts, best = 0;
     for (int64_t cluster = 1; cluster <= 8; cluster *= 2) {
         const int64_t rounds = (heads * cluster + resident - 1) / resident, own = (units + cluster - 1) / cluster;
-        const int64_t cost = rounds * (own + kRound + (cluster > 1 ? kExchange : 0));
+        const int64_t cost = rounds * (weight * own + kRound + (cluster > 1 ? kExchange : 0));
         if (cost < least && heads * cluster <= INT32_MAX) least = cost, best = cluster;
     }
     if (units == 1) best = 1;                                // nothing to divide
@@ -181,8 +182,8 @@ Division divide(const pp_paged_cache_t& c, const Form& f, int batch, int width, 
     // and a row is no multiple of 256 bytes, heads read one after another fetch the lines between them twice (32 x 6000, eight
     // heads of 72 / 96: 88 / 98 us one by one, 72 / 84 us by four; 256-byte rows: 103 against 105; 16 query heads to each: 61 against 68).
     const bool side_by_side = c.k_head < c.k_token && c.head_dim * type_bytes(c.dtype) % 256 != 0;
-    // A row's parts then are four times as many, so heads have to be, too.
-    const bool across = fours && chunk <= 8 && 4 * heads >= resident && (is_8bit(c.dtype) || side_by_side);
+    // A row's parts then are four times as many, and so are a CTA's rows: it takes a dozen units to a CTA and as many heads to pay.
+    const bool across = fours && chunk <= 8 && 4 * heads >= resident && heads * units >= 12 * (int64_t)resident && (is_8bit(c.dtype) || side_by_side);
     const int notes = (int)std::min<int64_t>(across ? heads / kWarps : heads, resident), rows = across ? kWarps * chunk : chunk;
     return {resident, 0, across, notes, rows, (notes_floats(notes) + (int64_t)resident * 2 * part_floats(rows, c.head_dim)) * 4};
 }
