@@ -114,27 +114,41 @@ Choice choose(const pp_paged_cache_t& c, pp_dtype_t q_type, int q_on, int group)
     return {f, own, granule, f.heads, whole && own != kElements};
 }
 
-// CTAs that the current device holds at once.
-cudaError_t grid_of(const Form& f, int& grid) {
+// Clusters of 1, 2, 4 and 8 CTAs that the current device holds at once.  A cluster keeps to one group of SMs, so those of eight are fewer
+// than an eighth of the CTAs: 36 of them, for which there were CTAs enough, took two rounds (9 x 1000, heads of 256: 17 us).
+cudaError_t hold(const Form& f, int (&n)[4]) {
     int device = 0;
     if (cudaError_t e = cudaGetDevice(&device)) return e;
-    if (!f.opt_in->is_done(device)) {
-        int n = 0;
-        if (cudaError_t e = cudaFuncSetAttribute(f.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, f.smem)) return e;
-        // An SM divides its memory between L1 and shared memory as its kernels ask, and changes that only when it is empty: with the second
-        // kernel's smaller wish in force the last of the CTAs would start when others end.
-        for (const void* k : {reinterpret_cast<const void*>(f.kernel), reinterpret_cast<const void*>(join_kernel<1>), reinterpret_cast<const void*>(join_kernel<2>),
-                              reinterpret_cast<const void*>(join_kernel<4>)})
-            if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared)) return e;
-        if (cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, f.kernel, kThreads, (size_t)f.smem)) return e;
-        if (device >= PerDeviceOnce::kMaxDevices) {
-            grid = std::max(n, 1) * sm_count();
-            return cudaSuccess;
-        }
-        f.resident[device] = std::max(n, 1);
+    if (f.opt_in->is_done(device)) {
+        for (int i = 0; i < 4; ++i) n[i] = f.resident[device][i];
+        return cudaSuccess;
+    }
+    if (cudaError_t e = cudaFuncSetAttribute(f.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, f.smem)) return e;
+    // An SM divides its memory between L1 and shared memory as its kernels ask, and changes that only when it is empty: with the second
+    // kernel's smaller wish in force the last of the CTAs would start when others end.
+    for (const void* k : {reinterpret_cast<const void*>(f.kernel), reinterpret_cast<const void*>(join_kernel<1>), reinterpret_cast<const void*>(join_kernel<2>),
+                          reinterpret_cast<const void*>(join_kernel<4>)})
+        if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared)) return e;
+    int each = 0;
+    if (cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, f.kernel, kThreads, (size_t)f.smem)) return e;
+    n[0] = std::max(each, 1) * sm_count();
+    for (int i = 1; i < 4; ++i) {
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = 1u << i;
+        at.val.clusterDim.y = at.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(1u << i);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = (size_t)f.smem;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        if (cudaError_t e = cudaOccupancyMaxActiveClusters(&n[i], f.kernel, &cfg)) return e;
+    }
+    if (device < PerDeviceOnce::kMaxDevices) {
+        for (int i = 0; i < 4; ++i) f.resident[device][i] = n[i];
         f.opt_in->mark(device);
     }
-    grid = f.resident[device] * sm_count();
     return cudaSuccess;
 }
 
@@ -160,22 +174,25 @@ struct Division {
 // sums over lengths, the workspace and a second kernel, 4 us.  A CTA or a cluster of up to eight to each head (chunk): as many
 // rounds as the GPU needs for them, each a CTA's share and 2 us for its start and end; a cluster's exchange costs 2.3 us.
 constexpr int kEqualParts = 10, kRound = 3, kExchange = 4;
-Division divide(const pp_paged_cache_t& c, const Form& f, int batch, int width, int window, int chunk, int n_chunks, int resident) {
+Division divide(const pp_paged_cache_t& c, const Form& f, int batch, int width, int window, int chunk, int n_chunks, const int (&held)[4]) {
+    const int resident = held[0];
     const bool fours = c.kv_heads % kWarps == 0 && !f.shares_q;
     const int64_t capacity = (int64_t)width * c.page_size, longest = window > 0 ? std::min<int64_t>((int64_t)window + kTile - 1, capacity) : capacity;
     const int64_t units = std::max<int64_t>(1, (longest + kUnit - 1) / kUnit), heads = (int64_t)batch * c.kv_heads * n_chunks;
     const int64_t weight = f.shares_q ? 2 : 1;
     int64_t least = weight * (heads * units / resident + 1) + kEqualParts, best = 0;
-    for (int64_t cluster = 1; cluster <= 8; cluster *= 2) {
-        const int64_t rounds = (heads * cluster + resident - 1) / resident, own = (units + cluster - 1) / cluster;
+    for (int i = 0; i < 4; ++i) {
+        const int64_t cluster = 1 << i, rounds = held[i] ? (heads + held[i] - 1) / held[i] : INT32_MAX, own = (units + cluster - 1) / cluster;
         const int64_t cost = rounds * (weight * own + kRound + (cluster > 1 ? kExchange : 0));
         if (cost < least && heads * cluster <= INT32_MAX) least = cost, best = cluster;
     }
-    if (units == 1) best = 1;                                // nothing to divide
+    if (units == 1 && best != 1) {                           // nothing to divide
+        best = 1;
+        least = (heads + resident - 1) / resident * (weight + kRound);
+    }
     if (fours && best != 0) {                                // short heads, more than the GPU holds: a warp to each, four to a CTA
         const int64_t cost = (heads / kWarps + resident - 1) / resident * (kWarps * units + kRound);
-        const int64_t one = (heads * best + resident - 1) / resident * ((units + best - 1) / best + kRound + (best > 1 ? kExchange : 0));
-        if (cost < one) return {(int)(heads / kWarps), 1, true, 0, 0, 0};
+        if (cost < least) return {(int)(heads / kWarps), 1, true, 0, 0, 0};
     }
     if (best) return {(int)(heads * best), (int)best, false, 0, 0, 0};
     // Four neighbouring heads at once where the scales of their rows share lines of memory, or their rows do: where heads lie side by side
@@ -203,11 +220,11 @@ extern "C" pp_status_t pp_paged_attention_workspace(const pp_paged_cache_t* cach
     // enough for any alignment of q
     int64_t most = 0;
     for (const int q_on : {1, 16}) {
-        int resident;
+        int held[4];
         const int group = heads / cache->kv_heads;
         const Choice by = choose(*cache, q_type, q_on, group);
-        if (const cudaError_t e = grid_of(by.form, resident)) return status_of(e);
-        most = std::max(most, divide(*cache, by.form, batch, width, window, by.chunk, (group + by.chunk - 1) / by.chunk, resident).bytes);
+        if (const cudaError_t e = hold(by.form, held)) return status_of(e);
+        most = std::max(most, divide(*cache, by.form, batch, width, window, by.chunk, (group + by.chunk - 1) / by.chunk, held).bytes);
     }
     *bytes = most;
     return PP_OK;
@@ -235,10 +252,10 @@ extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const v
     const Choice chosen = choose(c, q_type, row_alignment(q, 1, 0, batch, q_row, heads, q_head, tb), group);
     const Form& f = chosen.form;
     const int chunk = chosen.chunk;
-    int resident;
-    if (const cudaError_t e = grid_of(f, resident)) return status_of(e);
+    int held[4];
+    if (const cudaError_t e = hold(f, held)) return status_of(e);
     const int n_chunks = (group + chunk - 1) / chunk;
-    const Division by = divide(c, f, batch, width, window, chunk, n_chunks, resident);
+    const Division by = divide(c, f, batch, width, window, chunk, n_chunks, held);
     if (by.bytes && (!workspace || workspace_bytes < by.bytes)) return PP_ERR_INVALID_ARG;
     const int es = type_bytes(c.dtype);
     AttnArgs a{q, static_cast<const char*>(c.k), static_cast<const char*>(c.v), c.k_scales, c.v_scales, table, lengths, out, lse,

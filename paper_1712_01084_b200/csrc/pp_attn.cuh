@@ -1092,12 +1092,12 @@ struct Form {
     float lift = 0.0f;
     bool shares_q = false;
     PerDeviceOnce* opt_in = nullptr;
-    int* resident = nullptr;                                 // CTAs that an SM holds, by device
+    int (*resident)[4] = nullptr;                            // clusters of 1, 2, 4 and 8 CTAs that a device holds, by device
 };
 
 template <class Core, Reading READING> Form form_of() {
     static PerDeviceOnce opt_in;
-    static int resident[PerDeviceOnce::kMaxDevices] = {};
+    static int resident[PerDeviceOnce::kMaxDevices][4] = {};
     Form f;
     f.kernel = attn_kernel<Core, READING>;
     f.inbox = std::max(kWarps * Core::kStages * Core::kStage, kWarps * Core::kHeads * Core::kMergePitch * 4) + (Core::kStagesQ ? Core::kHeads * Core::kDim * 4 : 0);
