@@ -154,7 +154,7 @@ template <int kPlanRows> __global__ void __launch_bounds__(kPlanThreads) plan_ke
 }
 
 // ------------------------------------------------------------------------------------------------------ append
-constexpr int kAppendThreads = 256, kMaxTokens = 4, kMaxRows = 256;
+constexpr int kAppendThreads = 256, kMaxTokens = 8, kMaxRows = 256, kAppendCtas = 4;   // the last: of an SM
 
 struct AppendArgs {
     const void *q, *k, *v;
@@ -254,9 +254,9 @@ template <typename T, int W> __device__ __forceinline__ void store_run(T* to, co
 // lane and both its elements take the same sine; a.lanes lanes make a head.  A CTA has a.per_cta tokens and a.per_part of their heads:
 // where these lie, and the turns, are worked out once and stand in shared memory, since a row itself is only some 50 instructions.
 // The next row is on its way while one is worked on; four CTAs to an SM are more than a second row ahead is worth (16384 tokens of
-// 64 + 2 x 8 heads of 128: 107 us, 6.3 TB/s; three CTAs and two rows ahead 118; addresses made row by row 167).  Q8: the cache holds 8 bits.
+// 64 + 2 x 8 heads of 128: 108 us, 6.2 TB/s; three CTAs and two rows ahead 118; addresses made row by row 167).  Q8: the cache holds 8 bits.
 template <typename T, bool Q8, int W>
-__global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads, kAppendCtas) append_kernel(const __grid_constant__ AppendArgs a) {
     struct From { const char* src; char* dst; };             // of a head, to which a token's distance is added, in bytes
     struct By { int64_t src, dst; };
     __shared__ From head_at[kMaxRows];
@@ -485,8 +485,17 @@ template <typename T, bool Q8> cudaError_t launch_append(AppendArgs& a, int widt
     while (parts * at_once < rows && (int64_t)a.tokens * parts < 4 * (int64_t)sm_count()) ++parts;
     a.per_part = (rows + parts - 1) / parts;
     parts = (rows + a.per_part - 1) / a.per_part;
-    // many tokens: four to a CTA, whose sines then cost one trip through the long way of 64-bit arithmetic
-    if (width && a.tokens >= 16 * sm_count()) a.per_cta = kMaxTokens;
+    // many tokens: as many to a CTA, up to eight, as leave the fewest to the CTAs that one place of an SM runs in turn, with one more for
+    // each CTA's start (four to a CTA against this rule: 16384 tokens of 64 + 2 x 8 heads of 128 by seven 108.5, 107.9 us; 4095 of 16-bit
+    // heads of 256 17.2, 16.5; others of thousands of tokens 43.3, 39.6 and 21.3, 17.0)
+    if (width && a.tokens >= 16 * sm_count()) {
+        const int64_t at_once = (int64_t)sm_count() * kAppendCtas;
+        int64_t least = INT64_MAX;
+        for (int per = 1; per <= kMaxTokens; ++per) {
+            const int64_t cost = (((int64_t)a.tokens + per - 1) / per * parts + at_once - 1) / at_once * (per + 1);
+            if (cost < least) least = cost, a.per_cta = per;
+        }
+    }
     const dim3 grid((unsigned)(((int64_t)a.tokens + a.per_cta - 1) / a.per_cta), (unsigned)parts);
     return launch_pdl(width == 8 ? append_kernel<T, Q8, sizeof(T) == 4 ? 4 : 8> : width == 4 ? append_kernel<T, Q8, 4> : append_any_kernel<T>, grid, dim3(kAppendThreads), 0, stream, 1, a);
 }
