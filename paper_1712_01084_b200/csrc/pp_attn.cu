@@ -1,6 +1,8 @@
 // Attention over a paged key-value cache: the kernel that joins parts, the choice of form and division, and the C interface.
 #include "pp_attn.cuh"
 
+#include <mutex>
+
 namespace pp {
 namespace attn {
 namespace {
@@ -119,6 +121,8 @@ Choice choose(const pp_paged_cache_t& c, pp_dtype_t q_type, int q_on, int group)
 cudaError_t hold(const Form& f, int (&n)[4]) {
     int device = 0;
     if (cudaError_t e = cudaGetDevice(&device)) return e;
+    static std::mutex first;                                 // of two first calls at once the second reads what the first one found
+    const std::lock_guard<std::mutex> one(first);
     if (f.opt_in->is_done(device)) {
         for (int i = 0; i < 4; ++i) n[i] = f.resident[device][i];
         return cudaSuccess;
@@ -170,8 +174,8 @@ struct Division {
     int notes, part_rows;
     int64_t bytes;                                           // of workspace
 };
-// Costs in units of 64 positions to a CTA, some 0.6 us while latency rules (twice that in the scalar form), going by the table's width.  Equal parts of all units:
-// sums over lengths, the workspace and a second kernel, 4 us.  A CTA or a cluster of up to eight to each head (chunk): as many
+// Costs in units of 64 positions to a CTA, some 0.6 us while latency rules (twice that in the scalar form), going by the table's
+// width.  Equal parts of all units: sums over lengths, the workspace and a second kernel, 4 us.  A CTA or a cluster of up to eight to each head (chunk): as many
 // rounds as the GPU needs for them, each a CTA's share and 2 us for its start and end; a cluster's exchange costs 2.3 us.
 constexpr int kEqualParts = 10, kRound = 3, kExchange = 4;
 Division divide(const pp_paged_cache_t& c, const Form& f, int batch, int width, int window, int chunk, int n_chunks, const int (&held)[4]) {

@@ -258,6 +258,22 @@ def test_append_matches_definition(dtype, kind, case):
     _check_append(c, before, k, v, slots, q, positions, inv_freq, interleaved, q, got, kind)
 
 
+# from 16 tokens to an SM on a CTA takes several of them: one fewer than that, ragged ends, heads that two CTAs share, no q, no turn
+MANY = [(2, 1, 64, 2367, 32, False, {}), (2, 1, 64, 2368, 32, False, {}), (4, 2, 128, 4099, 32, True, {"page": 3}), (1, 1, 72, 16411, 36, False, {"page": 16}),
+        (6, 2, 256, 5003, 128, False, {"heads_first": True}), (0, 2, 96, 9001, 48, False, {}), (256, 8, 16, 2500, 8, False, {}), (2, 2, 80, 7001, 0, False, {})]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", [("f32", "f32"), ("bf16", "bf16"), ("f16", "int8"), ("f32", "e4m3")])
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_append_of_many_tokens(dtype, kind, case):
+    heads, kv, dim, tokens, pairs, interleaved, kw = MANY[case]
+    c, before, q, k, v, slots, positions, inv_freq, interleaved = _append_case(100 + case, dtype, kind, heads, kv, dim, tokens, pairs, interleaved,
+                                                                              skip=(0, 3, 8, tokens - 1), **kw)
+    got = pb.pp_kv_append(c, k, v, slots, q=q, positions=positions, inv_freq=inv_freq, interleaved=interleaved)
+    _check_append(c, before, k, v, slots, q, positions, inv_freq, interleaved, q, got, kind)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,kind,dim,shift", [("bf16", "bf16", 128, 0), ("f16", "int8", 96, 0), ("f32", "f32", 10, 1), ("bf16", "e4m3", 64, 5)])
 @pytest.mark.parametrize("interleaved", [False, True])
