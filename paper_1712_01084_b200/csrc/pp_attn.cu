@@ -175,9 +175,12 @@ struct Division {
     int64_t bytes;                                           // of workspace
 };
 // Costs in units of 64 positions to a CTA, some 0.6 us while latency rules (twice that in the scalar form), going by the table's
-// width.  Equal parts of all units: sums over lengths, the workspace and a second kernel, 4 us.  A CTA or a cluster of up to eight to each head (chunk): as many
-// rounds as the GPU needs for them, each a CTA's share and 2 us for its start and end; a cluster's exchange costs 2.3 us.
-constexpr int kEqualParts = 10, kRound = 3, kExchange = 4;
+// width.  Equal parts of all units: sums over lengths, the workspace and a second kernel, 4 us, and CTAs that share their SM with as
+// many others as it holds.  A CTA or a cluster of up to eight to each head (chunk): as many rounds as the GPU needs for them, each a
+// CTA's share and 2 us for its start and end; a cluster's exchange costs 2.3 us; and a 32nd of a long share, since heads that do not
+// fill the GPU leave memory idle.  With 10 for equal parts and no 32nd: 2 x 3000, heads of 64, 11.5 us for 8.7 now, 23 x 1025 in 8
+// bits 17.6 for 15.3, 12 x 1500 with 16-bit heads of 256 30.1 for 32.2; with 12 and no 32nd 30 x 3000 bf16 57.7 for 52.0.
+constexpr int kEqualParts = 12, kRound = 3, kExchange = 4;
 Division divide(const pp_paged_cache_t& c, const Form& f, int batch, int width, int window, int chunk, int n_chunks, const int (&held)[4]) {
     const int resident = held[0];
     const bool fours = c.kv_heads % kWarps == 0 && !f.shares_q;
@@ -187,7 +190,7 @@ Division divide(const pp_paged_cache_t& c, const Form& f, int batch, int width, 
     int64_t least = weight * (heads * units / resident + 1) + kEqualParts, best = 0;
     for (int i = 0; i < 4; ++i) {
         const int64_t cluster = 1 << i, rounds = held[i] ? (heads + held[i] - 1) / held[i] : INT32_MAX, own = (units + cluster - 1) / cluster;
-        const int64_t cost = rounds * (weight * own + kRound + (cluster > 1 ? kExchange : 0));
+        const int64_t cost = rounds * (weight * own + own / 32 + kRound + (cluster > 1 ? kExchange : 0));
         if (cost < least && heads * cluster <= INT32_MAX) least = cost, best = cluster;
     }
     if (units == 1 && best != 1) {                           // nothing to divide

@@ -21,16 +21,16 @@
 //
 // Matrix form (MmaCore), S^T[16 positions x 8 heads] = K Q^T and O^T[dim x 8 heads] += V^T P^T, by m16n8k16: the cache is the operand
 // with 16 rows, heads are the eight columns, so no instruction works on padding where a key-value head has eight query heads.
-// Not tcgen05: with 8 to 16 heads to a row of the cache the matrix pipe is busy 15 to 18 % of the time, and codes have to pass
+// Not tcgen05: with 8 to 16 heads to a row of the cache the matrix pipe is busy 15 to 19 % of the time, and codes have to pass
 // through registers to be widened.  P^T changes from the layout of a result to that of an operand by 8x8 transposes in registers;
 // it enters as two 16-bit numbers, the rounded value and what the rounding left (one alone would add an error as large as the
 // output's own rounding), or as one where that is an eighth of it.  8-bit codes are exact in f16; the scale of a key multiplies
 // its score, that of a value its p.
 // Scalar form (ScalarCore): floats, a lane per position and half row for the scores, a lane per dimension for the sums.
 //
-// In a graph, heads of 128, 32 query heads over 8: 64 requests of 4096 to 8192 bf16 252 us, 6.4 TB/s of what they hold; one of 131072
-// 95 us, 5.7 TB/s; 33 of 6000 to 12000 in 8 bits with 64 heads 120 us, 5.3 TB/s; one of 513 6.3 us; 6 of 500 to 1000 floats, 16 heads
-// of 64, 12.3 us.
+// In a graph, heads of 128, 32 query heads over 8: 64 requests of 4096 to 8192 bf16 248 us, 6.5 TB/s of what they hold; one of 131072
+// 91 us, 5.9 TB/s; 33 of 6000 to 12000 in 8 bits with 64 heads 122 us, 5.2 TB/s; one of 513 6.3 us; 6 of 500 to 1000 floats, 16 heads
+// of 64, 12.0 us.
 #pragma once
 #include "pp_internal.h"
 #include "pp_paged.cuh"
@@ -364,7 +364,8 @@ template <int KIND> __device__ __forceinline__ void widen(uint32_t four, uint32_
 template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
     static constexpr bool kQ8 = KIND >= kE4m3, kIsBf16 = KIND == kBf16;
     static constexpr int kEs = kQ8 ? 1 : 2, kChunks = DT * kEs / 16, kPitch = 16 * (kChunks | 1), kTileBytes = kTile * kPitch;
-    // Resident CTAs that the registers are cut for: by those that sums and q take
+    // Resident CTAs that the registers are cut for: by those that sums and q take.  8-bit rows of 128, four against three: 32 x 6000 64.6
+    // and 66.1 us, in pages of one token 74.3 and 84.9, 33 x 12000 with 64 heads 122.3 and 120.7
     static constexpr int kHeld = DT * NT * (4 + 2 * QP) / 16, kCtas = kQ8 ? (kHeld <= 48 ? 4 : kHeld <= 64 ? 3 : 2) : kHeld <= 36 ? 3 : 1;
     static constexpr int kStage = 2 * kTileBytes + (kQ8 ? 128 : 0), kStages = DT <= 64 ? 3 : 2;
     static constexpr int kHeads = 8 * NT, kMergePitch = DT + 4;

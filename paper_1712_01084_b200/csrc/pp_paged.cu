@@ -10,7 +10,7 @@
 //
 // Append.  All bandwidth for many tokens, all latency for few.  Both elements of a pair are in one lane and take the same sine.  The
 // angle is a product in 64 bits, brought into a turn there: position 10^6 leaves a 32-bit angle 2^-5 of a radian.  16384 tokens
-// of 64 + 2 x 8 heads of 128, bf16: 107 us, 6.3 TB/s; one token 2.1 us.
+// of 64 + 2 x 8 heads of 128, bf16: 108 us, 6.2 TB/s; one token 2.1 us.
 #include "pp_internal.h"
 #include "pp_paged.cuh"
 
