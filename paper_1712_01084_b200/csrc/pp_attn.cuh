@@ -138,6 +138,9 @@ __device__ __forceinline__ float4 over(float4 v, float l) {
 // maximum: it moves when a score is more than 2^kSlack above it, so that most tiles pass with one vote and no exchange of maxima.
 constexpr float kLowest = -3.402823466e38f, kSlack = 8.0f;
 __device__ __forceinline__ float weight_of(float m, float top) { return exp2_fast(m - top); }
+// 2^n for n < 128, 0 below the normal numbers; and the power of two of a positive number (-127 for what is smaller than normal ones).
+__device__ __forceinline__ float power(int n) { return n < -126 ? 0.0f : __int_as_float((n + 127) << 23); }
+__device__ __forceinline__ int exponent(float x) { return ((__float_as_int(x) >> 23) & 255) - 127; }
 
 template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there) {   // zeros if not there
     if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -373,12 +376,16 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
     // so much that the last CTA ends 20 % behind the mean (64 x 8192: 254 us with two, 268 with three).
     static constexpr int kDim = DT, kLeastSmem = kQ8 || DT < 128 ? 0 : 77 * 1024;
     static constexpr bool kStagesQ = false;
-    // p is at most 2^(kLift + kSlack): f16 numbers end at 65504, and below 2^-24 they are lost, which a p can be beside the largest one
-    static constexpr float kLift = kIsBf16 ? 0.0f : 7.0f;
+    // p is at most 2^(kLift + kSlack): f16 numbers end at 65504, and below 2^-24 they are lost, which a p can be beside the largest one.
+    // Over 8 bits p itself stays a float, and its product with the scale of a value is what f16 has to hold (`by`).
+    static constexpr float kLift = KIND == kF16 ? 7.0f : 0.0f;
+    static constexpr int kMostProduct = 15, kProduct = 6;    // powers of two: products stay below the one, the largest starts above the other
+    static constexpr int kMostBy = 100;
 
     uint32_t q[DT / 16][NT][2][QP];
-    // by head: the running maximum, kLift less it, the sum, what a product is multiplied with; the largest scale of a value and its inverse
-    float acc[DT / 16][NT][4], m[NT][2], c[NT][2], l[NT][2], f[NT][2], vm, inverse;
+    // by head: the running maximum, kLift less it, the sum, what a product is multiplied with.  8 bits: m is a whole number, so that changes
+    // of it are powers of two; `by`, a power of two, brings the products of p and their values' scales into f16
+    float acc[DT / 16][NT][4], m[NT][2], c[NT][2], l[NT][2], f[NT][2], by[NT][2];
 
     // q as the second operand of the scores: head g of each tile, two neighbouring dimensions to a register (16-bit caches), or four
     // to two registers (codes, as they lie in a lane's bytes).  Rows of q start where such an access may.
@@ -442,7 +449,6 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) acc[j][nt][k] = 0.0f;
         }
-        vm = inverse = 0.0f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -451,6 +457,7 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
                 m[nt][b] = kLowest;
                 c[nt][b] = kLift - kLowest;
                 l[nt][b] = 0.0f;
+                by[nt][b] = power(kMostBy);
             }
     }
 
@@ -487,7 +494,7 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
                 for (int nt = 0; nt < NT; ++nt) mma<kIsBf16>(s[nt], k[0], k[1], k[2], k[3], q[j][nt][0][0], q[j][nt][1][0]);
             }
         }
-        float v0 = 1.0f, v1 = 1.0f, most = 0.0f;             // scales of the values at g and g + 8
+        float v0 = 1.0f, v1 = 1.0f;                          // scales of the values at g and g + 8
         if constexpr (kQ8) {
             float k0, k1;
             const uint32_t at = stage + 2 * kTileBytes + g * 4;
@@ -500,16 +507,15 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
                 s[nt][0] *= k0, s[nt][1] *= k0;
                 s[nt][2] *= k1, s[nt][3] *= k1;
             }
-            most = fmaxf(fabsf(v0), fabsf(v1));
         }
-        float p[NT][4];                                      // logarithms first
+        const bool first = (bits >> g) & 1, second = (bits >> (g + 8)) & 1;
+        float p[NT][4], x[NT][4];                            // p (logarithms first); the factors of the values' codes
         const auto exponents = [&] {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) p[nt][i] = fmaf(s[nt][i], f[nt][i & 1], c[nt][i & 1]);
             if (bits != 0xffffu) {
-                const bool first = (bits >> g) & 1, second = (bits >> (g + 8)) & 1;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -517,64 +523,85 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
                         if (!(i < 2 ? first : second)) p[nt][i] = -INFINITY;
             }
         };
+        const auto products = [&] {                          // of p and the scales of its values
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[nt][i] = exp2_fast(p[nt][i]);
+                    x[nt][i] = kQ8 ? p[nt][i] * (i < 2 ? v0 : v1) * by[nt][i & 1] : p[nt][i];
+                }
+        };
         exponents();
-        float largest = p[0][0];
+        float largest = p[0][0], heaviest = 0.0f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) largest = fmaxf(largest, p[nt][i]);
-        if (__any_sync(0xffffffffu, largest > kLift + kSlack || (kQ8 && most > vm))) {
-            float change = 1.0f;                             // of the values' common scale
-            if constexpr (kQ8) {
-                // scales enter p relative to the largest so far, so that the product stays within f16; room for twice that avoids most changes
-                float top = most;
+        if constexpr (kQ8) {
+            products();
 #pragma unroll
-                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                if (top > vm) {
-                    const float now = top < 1e38f ? fmaxf(2.0f * top, 0x1p-100f) : top;      // 1 / vm stays finite
-                    change = __fdiv_rn(vm, now);
-                    vm = now;
-                    inverse = __fdiv_rn(1.0f, vm);
-                }
-            }
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) heaviest = fmaxf(heaviest, fabsf(x[nt][i]));
+        }
+        if (__any_sync(0xffffffffu, largest > kLift + kSlack || (kQ8 && heaviest >= power(kMostProduct)))) {
+            int up[NT][2];                                   // by how many powers of two m rises (8 bits)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    float top = fmaxf(p[nt][b] > -INFINITY ? s[nt][b] * f[nt][b] : kLowest, p[nt][b + 2] > -INFINITY ? s[nt][b + 2] * f[nt][b] : kLowest);
+                    float top = fmaxf(first ? s[nt][b] * f[nt][b] : kLowest, second ? s[nt][b + 2] * f[nt][b] : kLowest);
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    const float now = fmaxf(m[nt][b], top), alpha = exp2_fast(m[nt][b] - now);
+                    const float now = fmaxf(m[nt][b], kQ8 ? ceilf(top) : top);
+                    if constexpr (kQ8) {
+                        up[nt][b] = (int)fminf(now - m[nt][b], 512.0f);
+                        l[nt][b] *= power(-up[nt][b]);
+                    } else {
+                        const float alpha = exp2_fast(m[nt][b] - now);
+                        l[nt][b] *= alpha;
+#pragma unroll
+                        for (int j = 0; j < DT / 16; ++j) acc[j][nt][b] *= alpha, acc[j][nt][b + 2] *= alpha;
+                    }
                     m[nt][b] = now;
                     c[nt][b] = kLift - now;
-                    l[nt][b] *= alpha;
-#pragma unroll
-                    for (int j = 0; j < DT / 16; ++j) {
-                        acc[j][nt][b] *= alpha * change;
-                        acc[j][nt][b + 2] *= alpha * change;
-                    }
                 }
             exponents();
+            if constexpr (kQ8) {
+                // by follows the largest product, not the largest scale: a large value at a position of no weight takes no bits from the others.
+                // Products so far allow it to rise as m does; those of this tile may bring it down.
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        float top = fmaxf(fabsf(exp2_fast(p[nt][b]) * v0), fabsf(exp2_fast(p[nt][b + 2]) * v1));
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        const int held = exponent(by[nt][b]), may = min(held + up[nt][b], kMostBy), heavy = exponent(top);
+                        const int now = heavy + may < kMostProduct ? may : max(kProduct - heavy, -126);
+                        by[nt][b] = power(now);
+                        const float change = power(now - held - up[nt][b]);       // 1 at most
+#pragma unroll
+                        for (int j = 0; j < DT / 16; ++j) acc[j][nt][b] *= change, acc[j][nt][b + 2] *= change;
+                    }
+                products();
+            }
         }
+        if constexpr (!kQ8) products();
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                p[nt][b] = exp2_fast(p[nt][b]);
-                p[nt][b + 2] = exp2_fast(p[nt][b + 2]);
-                l[nt][b] += p[nt][b] + p[nt][b + 2];
-            }
-        const float w0 = kQ8 ? v0 * inverse : 1.0f, w1 = kQ8 ? v1 * inverse : 1.0f;
+            for (int b = 0; b < 2; ++b) l[nt][b] += p[nt][b] + p[nt][b + 2];
         uint32_t high[NT][2], low[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float x = p[nt][2 * i] * (i ? w1 : w0), y = p[nt][2 * i + 1] * (i ? w1 : w0);
-                const uint32_t h = pack2<kIsBf16>(x, y);
+                const uint32_t h = pack2<kIsBf16>(x[nt][2 * i], x[nt][2 * i + 1]);
                 const float2 back = unpack2<kIsBf16>(h);
                 high[nt][i] = transpose(h);
-                if constexpr (LOW) low[nt][i] = transpose(pack2<kIsBf16>(x - back.x, y - back.y));
+                if constexpr (LOW) low[nt][i] = transpose(pack2<kIsBf16>(x[nt][2 * i] - back.x, x[nt][2 * i + 1] - back.y));
             }
         const uint32_t values = stage + kTileBytes;
         if constexpr (kQ8) {
@@ -635,13 +662,13 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int head = nt * 8 + 2 * t + b;
-                float by = own ? 1.0f : weight_of(m[nt][b], top_of<kHeads>(all, head));
-                if (kQ8) by *= vm;
+                float weight = own ? 1.0f : weight_of(m[nt][b], top_of<kHeads>(all, head));
+                if (kQ8) weight *= power(-exponent(by[nt][b]));
 #pragma unroll
                 for (int j = 0; j < DT / 16; ++j)
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
-                        to[head * kMergePitch + 16 * j + (kQ8 ? 2 * g + i : g + 8 * i)] = acc[j][nt][b + 2 * i] * by;
+                        to[head * kMergePitch + 16 * j + (kQ8 ? 2 * g + i : g + 8 * i)] = acc[j][nt][b + 2 * i] * weight;
             }
     }
 };
