@@ -380,7 +380,7 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
     // Over 8 bits p itself stays a float, and its product with the scale of a value is what f16 has to hold (`by`).
     static constexpr float kLift = KIND == kF16 ? 7.0f : 0.0f;
     static constexpr int kMostProduct = 15, kProduct = 6;    // powers of two: products stay below the one, the largest starts above the other
-    static constexpr int kMostBy = 100;
+    static constexpr int kMostBy = 126;
 
     uint32_t q[DT / 16][NT][2][QP];
     // by head: the running maximum, kLift less it, the sum, what a product is multiplied with.  8 bits: m is a whole number, so that changes

@@ -110,7 +110,7 @@ def test_attention_over_scales_of_every_size(dtype, kind, spread, order, heads, 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,kind", [("bf16", "e4m3"), ("f16", "int8"), ("f32", "e4m3"), ("f32", "int8")])
-@pytest.mark.parametrize("scale", [0.0, 2.0 ** -110, 2.0 ** -20, 2.0 ** 100])
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -118, 2.0 ** -110, 2.0 ** -20, 2.0 ** 100])
 def test_attention_over_scales_near_the_ends(dtype, kind, scale):
     """All values at one far scale, and then one of ordinary size among them."""
     if scale > 1 and dtype == "f16":
