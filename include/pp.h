@@ -574,8 +574,8 @@ pp_status_t pp_paged_plan(const int32_t* lengths, const int32_t* added, int32_t*
  * outside the cache, -1 for one, is left out.  With inv_freq the first 2 * pairs dimensions of each head of q and k are turned:
  *     (x, y) -> (x cos a - y sin a, x sin a + y cos a),   a = positions[t] * inv_freq[i]   (the product in 64 bits)
  * for the pairs (i, i + pairs), or (2i, 2i + 1) where interleaved is not 0.  Values are floats until they are rounded once: to
- * dtype, or to 8 bits with the scale max|row| / Q of their token and head (Q = 127 or 448, code = round(value / scale), ties
- * to even; a row with a NaN or an infinity has a NaN scale and unspecified codes).
+ * dtype, or to 8 bits with the scale max|row| / Q of their token and head (Q = 127 or 448, code = round(value / scale), each
+ * quotient a rounded float, ties to even; a row with a NaN or an infinity has a NaN scale and unspecified codes).
  * q, k, v       [tokens][heads or kv_heads][head_dim] of dtype (PP_F32, PP_F16, PP_BF16: the cache's type, or any with an 8-bit
  *               cache), strides in elements; q NULL (heads 0): only the cache is written
  * q_out         like q; may be q itself (same address and strides), else no byte of it in q, k or v
