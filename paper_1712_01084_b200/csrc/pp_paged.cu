@@ -552,7 +552,8 @@ extern "C" pp_status_t pp_paged_plan(const int32_t* lengths, const int32_t* adde
     static PerDeviceOnce opt_in[2];
     int device = 0;
     if (const cudaError_t e = cudaGetDevice(&device)) return status_of(e);
-    if (smem > 48 * 1024 && !opt_in[one].is_done(device)) {
+    // 48 KB that a launch has by itself are for the kernel's own arrays too: asked for well below
+    if (smem > 32 * 1024 && !opt_in[one].is_done(device)) {
         if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (3 * kMaxRequests + 1) * 4)) return status_of(e);
         opt_in[one].mark(device);
     }
