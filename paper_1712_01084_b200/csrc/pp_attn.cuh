@@ -386,6 +386,7 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
     // by head: the running maximum, kLift less it, the sum, what a product is multiplied with.  8 bits: m is a whole number, so that changes
     // of it are powers of two; `by`, a power of two, brings the products of p and their values' scales into f16
     float acc[DT / 16][NT][4], m[NT][2], c[NT][2], l[NT][2], f[NT][2], by[NT][2];
+    bool far;                                                // a maximum of the warp's is so large that steps of floats show: every tile then changes them
 
     // q as the second operand of the scores: head g of each tile, two neighbouring dimensions to a register (16-bit caches), or four
     // to two registers (codes, as they lie in a lane's bytes).  Rows of q start where such an access may.
@@ -449,6 +450,7 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) acc[j][nt][k] = 0.0f;
         }
+        far = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -510,11 +512,16 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
         }
         const bool first = (bits >> g) & 1, second = (bits >> (g + 8)) & 1;
         float p[NT][4], x[NT][4];                            // p (logarithms first); the factors of the values' codes
-        const auto exponents = [&] {
+        const auto exponents = [&](auto again) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[nt][i] = fmaf(s[nt][i], f[nt][i & 1], c[nt][i & 1]);
+                for (int i = 0; i < 4; ++i) {
+                    p[nt][i] = fmaf(s[nt][i], f[nt][i & 1], c[nt][i & 1]);
+                    // A fused product has more bits than the maximum: their difference is up to half a step of the maximum, which from 2^20 on is
+                    // no small part of a power of two, and from 2^27 on leaves f16 above or below.  Rounded products are on its steps.
+                    if (decltype(again)::value && far) p[nt][i] = __fadd_rn(__fmul_rn(s[nt][i], f[nt][i & 1]), -m[nt][i & 1]) + kLift;
+                }
             if (bits != 0xffffu) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -532,7 +539,7 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
                     x[nt][i] = kQ8 ? p[nt][i] * (i < 2 ? v0 : v1) * by[nt][i & 1] : p[nt][i];
                 }
         };
-        exponents();
+        exponents(std::false_type());
         float largest = p[0][0], heaviest = 0.0f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -545,8 +552,9 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) heaviest = fmaxf(heaviest, fabsf(x[nt][i]));
         }
-        if (__any_sync(0xffffffffu, largest > kLift + kSlack || (kQ8 && heaviest >= power(kMostProduct)))) {
+        if (__any_sync(0xffffffffu, far || largest > kLift + kSlack || (kQ8 && heaviest >= power(kMostProduct)))) {
             int up[NT][2];                                   // by how many powers of two m rises (8 bits)
+            bool large = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -566,8 +574,10 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
                     }
                     m[nt][b] = now;
                     c[nt][b] = kLift - now;
+                    large |= fabsf(now) >= 0x1p20f && now != kLowest;
                 }
-            exponents();
+            far = __any_sync(0xffffffffu, large);
+            exponents(std::true_type());
             if constexpr (kQ8) {
                 // by follows the largest product, not the largest scale: a large value at a position of no weight takes no bits from the others.
                 // Products so far allow it to rise as m does; those of this tile may bring it down.
