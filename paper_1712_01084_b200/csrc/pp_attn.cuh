@@ -424,11 +424,12 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
                     }
                 }
                 float most = 0.0f, down = 1.0f;              // down: a power of two that brings the head's largest below 2, for f16 ends at 65504
+                const auto finite = [](float v) { return fabsf(v) < INFINITY ? fabsf(v) : 0.0f; };
 #pragma unroll
-                for (int j = 0; j < DT / 16; ++j) most = fmaxf(fmaxf(fmaxf(most, fabsf(x[j].x)), fmaxf(fabsf(x[j].y), fabsf(x[j].z))), fabsf(x[j].w));
+                for (int j = 0; j < DT / 16; ++j) most = fmaxf(fmaxf(fmaxf(most, finite(x[j].x)), fmaxf(finite(x[j].y), finite(x[j].z))), finite(x[j].w));
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-                if (most > 0.0f && most < INFINITY) {
+                if (most > 0.0f) {
                     const int e = min(max(((__float_as_int(most) >> 23) & 255) - 127, -126), 126);
                     down = __int_as_float((127 - e) << 23);
                     factor[nt] = a.scale * __int_as_float((127 + e) << 23);
@@ -440,8 +441,9 @@ template <int DT, int NT, int KIND, bool LOW, int QP> struct MmaCore {
                     q[j][nt][1][0] = pack2<false>(v.z, v.w);
                     if constexpr (QP == 2) {
                         const float2 u = unpack2<false>(q[j][nt][0][0]), w = unpack2<false>(q[j][nt][1][0]);
-                        q[j][nt][0][1] = pack2<false>(v.x - u.x, v.y - u.y);
-                        q[j][nt][1][1] = pack2<false>(v.z - w.x, v.w - w.y);
+                        const auto rest = [](float a, float b) { return fabsf(b) == INFINITY ? 0.0f : a - b; };
+                        q[j][nt][0][1] = pack2<false>(rest(v.x, u.x), rest(v.y, u.y));
+                        q[j][nt][1][1] = pack2<false>(rest(v.z, w.x), rest(v.w, w.y));
                     }
                 }
             }
