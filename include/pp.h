@@ -603,7 +603,10 @@ pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q, int64_t q
  * are floats; p enters the second product as two 16-bit numbers (16 bits in all for PP_BF16, 22 otherwise), with 8-bit caches and a
  * PP_BF16 output as one f16 number (11 bits); float q with 8-bit caches as two f16 numbers (22 bits).  With 8-bit caches p enters
  * times the scale of its value, which costs a product below 2^-20 of its head's largest (2^-9 where two numbers have 22) some of these
- * bits: it is off by 2^-31 of the largest at most.  Results do not depend on scheduling.  batch >= 0; heads a multiple of kv_heads; width * page_size < 2^31 - 2^13; batch * heads times the table's
+ * bits: it is off by 2^-31 of the largest at most.  16-bit q with 8-bit caches is one f16 number relative to its head's largest element
+ * (elements below 2^-14 of it lose bits, 2^-25 of it at most).  Exponentials are those of ex2.approx, subnormal ones 0.  A dimension in
+ * which a value with weight is infinite comes out infinite or NaN (the rest of p times an infinity); others are not touched by it.
+ * Results do not depend on scheduling.  batch >= 0; heads a multiple of kv_heads; width * page_size < 2^31 - 2^13; batch * heads times the table's
  * 64ths of positions < 2^31; window >= 0; scale finite.
  * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (types, head_dim, capacity), PP_ERR_CUDA. */
 pp_status_t pp_paged_attention_workspace(const pp_paged_cache_t* cache, pp_dtype_t q_type, int batch, int heads, int width,

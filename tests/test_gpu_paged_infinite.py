@@ -34,3 +34,24 @@ def test_attention_of_an_infinite_q(dtype, kind, shift):
     rest = torch.ones(2, 4, dtype=torch.bool, device="cuda")
     rest[0, 0] = rest[0, 1] = rest[1, 3] = False
     assert bool(torch.isfinite(o[rest]).all()) and bool(torch.isfinite(lse[rest]).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,kind", [k for k in KINDS if k[1] not in TOP])
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_attention_over_an_infinite_value(dtype, kind, shift, sign):
+    """A dimension in which a value is infinite is not finite, whatever the alignment; the other dimensions and heads are as without it."""
+    c, q, table, n = _attention_case(4, dtype, kind, 4, 2, 64, 16, [100, 40])
+    pages, page, g, d = c.k.shape
+    k, v = (torch.zeros(pages, page, g, d + 8 * shift + shift, dtype=c.k.dtype, device="cuda")[..., shift:shift + d] for _ in range(2))
+    k.copy_(c.k)
+    v.copy_(c.v)
+    c = pb.PagedCache(k, v)
+    want = pb.pp_paged_attention(c, q, table, n)
+    v[int(table[0, 2]), 3, 1, 7] = sign * math.inf
+    v[int(table[1, 0]), 0, 0, 20] = sign * math.inf
+    got = pb.pp_paged_attention(c, q, table, n)
+    bad = torch.zeros_like(got, dtype=torch.bool)
+    bad[0, 2:, 7] = bad[1, :2, 20] = True
+    assert not bool(torch.isfinite(got[bad]).any()) and torch.equal(got[~bad], want[~bad])
