@@ -539,7 +539,9 @@ pp_status_t pp_moe_status(pp_moe_t* layer, pp_status_t* status);
  *
  * A cache as the caller describes it (host struct, device pointers).  Head h of the token at place i of page p starts at
  * k + p k_page + i k_token + h k_head, in elements; its head_dim values lie side by side.  So pages may be kept token by token or
- * head by head, keys and values apart or interleaved, in one allocation or two.  No two rows may share bytes.
+ * head by head, keys and values apart or interleaved, in one allocation or two.  No two rows may share bytes, nor rows and scales.
+ * An output, a workspace, slots or positions may lie between rows, but not on them: calls are refused where they do (rows of keys on rows
+ * of values where both have the same strides).
  * dtype         PP_F32, PP_F16, PP_BF16; or PP_I8, PP_E4M3 with k_scales and v_scales, float [pages][page_size][kv_heads]: a
  *               value is its code times the scale of its token and head.  Otherwise the scales are NULL
  * head_dim      1..256; pages * page_size <= 2^40; page_size <= 2^20 */
@@ -578,7 +580,8 @@ pp_status_t pp_paged_plan(const int32_t* lengths, const int32_t* added, int32_t*
  * quotient a rounded float, ties to even; a row with a NaN or an infinity has a NaN scale and unspecified codes).
  * q, k, v       [tokens][heads or kv_heads][head_dim] of dtype (PP_F32, PP_F16, PP_BF16: the cache's type, or any with an 8-bit
  *               cache), strides in elements; q NULL (heads 0): only the cache is written
- * q_out         like q; may be q itself (same address and strides), else no byte of it in q, k or v
+ * q_out         like q; may be q itself (same address and strides), else no byte of it in q, k or v.  k and v may be rows of the cache,
+ *               as long as none of these is written
  * slots         int64 [tokens], no slot twice; positions int32 [tokens] and inv_freq float [pairs], or both NULL with pairs 0
  * pairs <= head_dim / 2; tokens >= 0.  Any alignment works; rows on 16 bytes (8 for 8-bit caches) are accessed more widely.
  * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (types, head_dim), PP_ERR_CUDA. */
@@ -595,7 +598,7 @@ pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q, int64_t q
  * cache holds elsewhere, NaN or not, is never used.
  * q             [batch][heads][head_dim], strides in elements; q_type is the cache's type, or any float with an 8-bit cache
  * table         [batch][width], rows ld_table apart; entries behind a request's length are not used
- * out           [batch][heads][head_dim] of q_type, contiguous; no byte of it in q
+ * out           [batch][heads][head_dim] of q_type, contiguous; no byte of out, lse or workspace in one another or in what is read
  * lse           float [batch][heads]: log of the sum of exp of the scores, or NULL
  * workspace     pp_paged_attention_workspace bytes (0: NULL), 16-byte aligned, for this call alone while it runs; need not be
  *               initialised.  Long sequences are divided over the GPU, and their parts joined through it

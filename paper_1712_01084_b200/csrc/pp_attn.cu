@@ -254,7 +254,18 @@ extern "C" pp_status_t pp_paged_attention(const pp_paged_cache_t* cache, const v
     if (!aligned_to(q, tb) || !aligned_to(out, tb) || !aligned_to(table, 4) || !aligned_to(lengths, 4) || !aligned_to(lse, 4) || !aligned_to(workspace, 16))
         return PP_ERR_INVALID_ARG;
     const int64_t q_span = ((batch - 1) * q_row + (heads - 1) * q_head + c.head_dim) * tb, out_span = (int64_t)batch * heads * c.head_dim * tb;
-    if (spans_meet(q, q_span, out, out_span)) return PP_ERR_INVALID_ARG;
+    // nothing that is written may lie on what is read, nor on one another
+    const Held cached(c);
+    struct Span { const void* p; int64_t bytes; };
+    const Span written[] = {{out, out_span}, {lse, (int64_t)batch * heads * 4}, {workspace, workspace_bytes}};
+    const Span read[] = {{q, q_span}, {table, ((int64_t)(batch - 1) * ld_table + width) * 4}, {lengths, (int64_t)batch * 4}};
+    for (const Span& w : written) {
+        for (const Span& r : read)
+            if (spans_meet(w.p, w.bytes, r.p, r.bytes)) return PP_ERR_INVALID_ARG;
+        for (const Span& other : written)
+            if (&other != &w && spans_meet(w.p, w.bytes, other.p, other.bytes)) return PP_ERR_INVALID_ARG;
+        if (cached.meet(w.p, w.bytes)) return PP_ERR_INVALID_ARG;
+    }
     const int group = heads / c.kv_heads;
     const Choice chosen = choose(c, q_type, row_alignment(q, 1, 0, batch, q_row, heads, q_head, tb), group);
     const Form& f = chosen.form;

@@ -593,6 +593,9 @@ extern "C" pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q
         if (s < 0 || s > most / tokens) return PP_ERR_INVALID_ARG;
     for (const int64_t s : {q_head, o_head, k_head, v_head})
         if (s < 0 || s > most >> 20) return PP_ERR_INVALID_ARG;
+    const Held held(c);
+    if (held.meet(slots, 8 * (int64_t)tokens) || held.meet(positions, 4 * (int64_t)tokens) || held.meet(inv_freq, 4 * (int64_t)pairs))
+        return PP_ERR_INVALID_ARG;
     const auto span = [&](int64_t token, int64_t head, int n) { return (((int64_t)tokens - 1) * token + ((int64_t)n - 1) * head + dim) * tb; };
     if (q) {
         if (!rows_apart(1, 0, tokens, o_token, heads, o_head, dim)) return PP_ERR_INVALID_ARG;
@@ -605,6 +608,10 @@ extern "C" pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q
             if (token == o_token) return share_bytes(q_out, out_row, o_token * tb, tokens, p, row, token * tb, tokens);
             return spans_meet(p, span(token, head, n), q_out, span(o_token, o_head, heads));
         };
+        // the cache is written too, and what says where to is read meanwhile
+        const Rows turned(q_out, 1, 0, tokens, o_token, heads, o_head, dim, tb);
+        if (held.meet(q_out, turned.span()) || turned.meet(slots, 8 * (int64_t)tokens) || turned.meet(positions, 4 * (int64_t)tokens) ||
+            turned.meet(inv_freq, 4 * (int64_t)pairs)) return PP_ERR_INVALID_ARG;
         if ((!in_place && meets(q, q_token, q_head, heads)) || meets(k, k_token, k_head, c.kv_heads) || meets(v, v_token, v_head, c.kv_heads)) return PP_ERR_INVALID_ARG;
     }
     AppendArgs a{q, k, v, q_out, c.k, c.v, c.k_scales, c.v_scales, slots, positions, inv_freq,
