@@ -928,13 +928,15 @@ class PagedCache:
 
 class PagedPlan:
     """What pp_paged_plan writes for a step, in tensors that calls may use again: slots int64 [rows], positions int32 [rows],
-    starts int32 [requests + 1], lengths int32 [requests], taken int32 [1]."""
+    starts int32 [requests + 1], lengths int32 [requests], taken int32 [1].  lengths and taken start at 0, for a first step that goes on
+    from them (start=False: not set, for a call that only writes them)."""
 
-    def __init__(self, requests: int, rows: int, device=None):
+    def __init__(self, requests: int, rows: int, device=None, start: bool = True):
         torch = _torch or _load_torch()
-        make = lambda n, dtype: torch.empty(n, dtype=dtype, device="cuda" if device is None else device)  # noqa: E731
+        make = lambda n, dtype, fill=torch.empty: fill(n, dtype=dtype, device="cuda" if device is None else device)  # noqa: E731
         self.slots = make(rows, torch.int64)
-        self.positions, self.starts, self.lengths, self.taken = (make(n, torch.int32) for n in (rows, requests + 1, requests, 1))
+        self.positions, self.starts = make(rows, torch.int32), make(requests + 1, torch.int32)
+        self.lengths, self.taken = (make(n, torch.int32, torch.zeros if start else torch.empty) for n in (requests, 1))
 
 
 def pp_paged_plan(lengths, added, table, free_pages, taken, page_size: int, rows: Optional[int] = None, out: Optional[PagedPlan] = None,
@@ -950,7 +952,7 @@ def pp_paged_plan(lengths, added, table, free_pages, taken, page_size: int, rows
     if out is None:
         if rows is None:
             raise ValueError("rows or out must be given")
-        out = PagedPlan(lengths.shape[0], rows, lengths.device)
+        out = PagedPlan(lengths.shape[0], rows, lengths.device, start=False)
     elif rows is not None and rows != out.slots.shape[0]:
         raise ValueError("out has another number of rows")
     r = _fast.paged_plan(lengths, added, table, free_pages, taken, page_size, out.slots, out.positions, out.starts, out.lengths, out.taken,
