@@ -596,7 +596,9 @@ pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q, int64_t q
  * is 0.  The new token's own key and value are in the cache already (l counts it).  Positions whose table entry is no page of
  * the cache (-1) are left out.  A row without positions gives 0 (lse -inf); so does one whose scores are all -inf.  What the
  * cache holds elsewhere, NaN or not, is never used.
- * q             [batch][heads][head_dim], strides in elements; q_type is the cache's type, or any float with an 8-bit cache
+ * q             [batch][heads][head_dim], strides in elements; q_type is the cache's type, or any float with an 8-bit cache.  Any start
+ *               works, but rows of q that are not on 4 bytes (8 with an 8-bit cache, 16 where q is PP_F32 then) make the whole cache be
+ *               read element by element, as rows of the cache off 4 bytes do: 13 to 21 times the time
  * table         [batch][width], rows ld_table apart; entries behind a request's length are not used
  * out           [batch][heads][head_dim] of q_type, contiguous; no byte of out, lse or workspace in one another or in what is read
  * lse           float [batch][heads]: log of the sum of exp of the scores, or NULL
@@ -606,7 +608,7 @@ pp_status_t pp_kv_append(const pp_paged_cache_t* cache, const void* q, int64_t q
  * are floats; p enters the second product as two 16-bit numbers (16 bits in all for PP_BF16, 22 otherwise), with 8-bit caches and a
  * PP_BF16 output as one f16 number (11 bits); float q with 8-bit caches as two f16 numbers (22 bits).  With 8-bit caches p enters
  * times the scale of its value, which costs a product below 2^-20 of its head's largest (2^-9 where two numbers have 22) some of these
- * bits: it is off by 2^-31 of the largest at most.  16-bit q with 8-bit caches is one f16 number relative to its head's largest element
+ * bits: it is off by 2^-31 of the largest at most; with PP_F16 caches p is off by 2^-32 of the head's largest.  16-bit q with 8-bit caches is one f16 number relative to its head's largest element
  * (elements below 2^-14 of it lose bits, 2^-25 of it at most).  Exponentials are those of ex2.approx, subnormal ones 0.  A dimension in
  * which a value with weight is infinite comes out infinite or NaN (the rest of p times an infinity); others are not touched by it.
  * Results do not depend on scheduling.  batch >= 0; heads a multiple of kv_heads; width * page_size < 2^31 - 2^13; batch * heads times the table's

@@ -2,9 +2,10 @@
 //
 //   out = sum_j p_j v_j,  p = softmax_j(scale q . k_j),  j over a request's last positions
 //
-// One pass over keys and values with a running maximum m and sum l: bound by the bytes of the cache, which are read once for all
-// query heads of a key-value head (up to 8 or 16 of them, the chunk).  m only moves when a score passes it by 2^8: then sums and l
-// are scaled; else a tile costs one vote.
+// One pass over keys and values with a running maximum m and sum l: bound by the bytes of the cache, which are read once for a chunk of
+// query heads of a key-value head, 16 of them up to 128 dimensions and 8 above, in floats, and for float q over 8 bits.  Chunks of one
+// head are heads of their own in what follows: more query heads than a chunk read the cache again, from L2 while it holds it.  m only
+// moves when a score passes it by 2^8: then sums and l are scaled; else a tile costs one vote.
 //
 // Division of work.  64 positions of one key-value head (and chunk) are a unit, 16 to a warp; or 16 positions of four heads, one
 // to a warp, where the heads' rows or scales share lines of memory.  Three ways (divide in pp_attn.cu):
@@ -28,9 +29,9 @@
 // its score, that of a value its p.
 // Scalar form (ScalarCore): floats, a lane per position and half row for the scores, a lane per dimension for the sums.
 //
-// In a graph, heads of 128, 32 query heads over 8: 64 requests of 4096 to 8192 bf16 248 us, 6.5 TB/s of what they hold; one of 131072
-// 91 us, 5.9 TB/s; 33 of 6000 to 12000 in 8 bits with 64 heads 122 us, 5.2 TB/s; one of 513 6.3 us; 6 of 500 to 1000 floats, 16 heads
-// of 64, 12.0 us.
+// In a graph, heads of 128, 32 query heads over 8: 64 requests of 4096 to 8192 bf16 247 to 252 us, 6.5 TB/s of what they hold; one of
+// 131072 91 to 93 us, 5.8 TB/s; 33 of 6000 to 12000 in 8 bits with 64 heads 120 to 123 us, 5.2 TB/s; one of 513 6.4 us; 6 of 500 to 1000
+// floats, 16 heads of 64, 12.0 us.
 #pragma once
 #include "pp_internal.h"
 #include "pp_paged.cuh"
